@@ -707,6 +707,125 @@ int bgl_pipeline_run(bgl_pipeline_t *p, const int32_t *seeds, int64_t seed_batch
                      const uint64_t *rng_seeds, int64_t steps, int64_t first_step, int64_t *n_input,
                      int64_t *n_hit, int64_t *n_hit_tier, bgl_batch_fn on_batch, void *user);
 
+/* ------------------------------------------------------------- the model's layers */
+
+/*
+ * What a model does first with a batch: a layer over the feature rows, with one
+ * weight for all rows or one per group of rows (a graph whose nodes have
+ * types, such as users and items), the layer's gradients, and, for the update
+ * of its weight, the orthogonalised gradient.  Rows are those of a lookup's
+ * out_rows; a stream that uses them first passes bgl_cache_wait_rows.
+ *
+ * Matrices are rows of values, stride values apart (row i at data + i * stride;
+ * stride >= the row's width, alignment that of the values).  Products are summed
+ * in fp32; results are rounded once, to the layer's type.  All calls enqueue on
+ * `stream`, allocate nothing, keep nothing between calls and can be captured.
+ */
+#define BGL_F32 0
+#define BGL_BF16 1
+
+#define BGL_ACT_NONE 0
+#define BGL_ACT_RELU 1
+#define BGL_ACT_GELU 2 /* z Phi(z), with the error function */
+#define BGL_ACT_SILU 3 /* z / (1 + exp(-z)) */
+
+#define BGL_RESIDUAL_NONE 0
+#define BGL_RESIDUAL_BEFORE 1 /* y = act(x W' + b + r) */
+#define BGL_RESIDUAL_AFTER 2  /* y = act(x W' + b) + r */
+
+#define BGL_MAX_GROUPS 1024
+#define BGL_MAX_DIM 16384
+
+typedef struct {
+    int32_t dtype;      /* of x, weight, bias, residual, y, saved and all gradients */
+    int32_t activation;
+    int32_t residual;
+    int32_t in_dim;
+    int32_t out_dim;
+    int32_t num_groups; /* 0: one weight for all rows */
+} bgl_linear_t;
+
+/*
+ * Sort a batch's rows by group, for a layer with groups: row i belongs to group
+ * group_of[ids[i]] (ids null: group_of[i]).  Rows of one group keep their order.
+ *   group_of    device, num_nodes values; one outside [0, num_groups), or an id
+ *               outside [0, num_nodes), means the row belongs to no group
+ *   ids         device, n node ids (a batch's input_nodes), or null
+ *   rows        device, receives the n rows in group order, those of no group last
+ *   offsets     device, receives num_groups + 1 ints: group g has rows[offsets[g] ..
+ *               offsets[g+1])
+ *   workspace   device, 256-byte aligned, >= bgl_group_rows_workspace_bytes(n, num_groups)
+ * Errors: BGL_EINVAL (null or misaligned pointers, num_groups < 1, n outside [0, 2^31),
+ * ids null with num_nodes < n), BGL_EUNSUPPORTED (num_groups > BGL_MAX_GROUPS),
+ * BGL_ECAPACITY (workspace too small), BGL_EHIP.
+ */
+int bgl_group_rows_workspace_bytes(int64_t n, int32_t num_groups, size_t *bytes);
+int bgl_group_rows(const int32_t *group_of, int64_t num_nodes, const int32_t *ids, int64_t n,
+                   int32_t num_groups, int32_t *rows, int32_t *offsets, void *workspace,
+                   size_t workspace_bytes, void *stream);
+
+/*
+ * z = x W' + b (+ residual), y = act(z) (+ residual), for n rows.
+ *   rows, offsets  layers with groups: as written by bgl_group_rows (rows null: the
+ *               rows are in group order already).  Row i of x, residual, y and saved
+ *               stays row i.  Rows of no group have z = 0 (+ residual).
+ *               Positions outside [0, n) are left out; a row named twice is undefined.
+ *   weight      device, out_dim x in_dim (num_groups of them one after the other), tight
+ *   bias        device, out_dim (num_groups x out_dim), or null
+ *   residual    n rows of out_dim; null without one.  May be y itself.
+ *   saved       n rows of out_dim that receive z for the backward call, or null
+ * y and saved must not overlap x, the weights or each other.  n = 0 does nothing.
+ * Errors: BGL_EINVAL (null or misaligned pointers, strides, sizes < 1, unknown
+ * types), BGL_EUNSUPPORTED (in_dim or out_dim > BGL_MAX_DIM, num_groups > BGL_MAX_GROUPS), BGL_EHIP.
+ */
+int bgl_linear_forward(const bgl_linear_t *layer, int64_t n, const int32_t *rows,
+                       const int32_t *offsets, const void *x, int64_t x_stride, const void *weight,
+                       const void *bias, const void *residual, int64_t residual_stride, void *y,
+                       int64_t y_stride, void *saved, int64_t saved_stride, void *stream);
+
+/*
+ * The layer's gradients: dz = dy act'(z), dx = dz W, dweight = dz' x, dbias = the
+ * sum of dz's rows.  Each of dx, dweight, dbias and dresidual may be null
+ * (dbias is not given without dweight; without dweight x may be null, without dx weight may).
+ *   saved       z of the forward call; unused (may be null) without an activation
+ *   dresidual   receives dz; only for BGL_RESIDUAL_BEFORE (behind the activation the
+ *               residual's gradient is dy itself).  May be dy itself.
+ *   workspace   device, 256-byte aligned, >= bgl_linear_workspace_bytes(layer, n)
+ * Gradients are written, not added to.  Rows of no group: dx = 0, nothing of them in
+ * dweight and dbias; a group without rows has dweight = dbias = 0.  The order of the sums is
+ * fixed by n, the sizes and the groups: repeated calls give the same bits.
+ * Errors: as bgl_linear_forward, plus BGL_EINVAL (dbias without dweight, dresidual of
+ * another kind of layer), BGL_ECAPACITY (workspace too small).
+ */
+int bgl_linear_workspace_bytes(const bgl_linear_t *layer, int64_t n, size_t *bytes);
+int bgl_linear_backward(const bgl_linear_t *layer, int64_t n, const int32_t *rows,
+                        const int32_t *offsets, const void *dy, int64_t dy_stride, const void *x,
+                        int64_t x_stride, const void *weight, const void *saved,
+                        int64_t saved_stride, void *dx, int64_t dx_stride, void *dweight,
+                        void *dbias, void *dresidual, int64_t dresidual_stride, void *workspace,
+                        size_t workspace_bytes, void *stream);
+
+/*
+ * Orthogonalise updates by Newton-Schulz steps: X = U / (|U|_F + eps), then `steps`
+ * times X <- a X + (b X X' + c (X X')^2) X, for each of `batch` matrices of
+ * rows x cols.  Singular vectors stay, singular values go towards 1.
+ *   coefficients  host, {a, b, c}; with them no singular value in [0, 1] may grow beyond 64
+ *                 on the way
+ *   out           may be the update itself (same strides), else apart from it
+ *   matrix strides in values; unused for batch = 1
+ *   workspace     device, 256-byte aligned, >= bgl_orthogonalize_workspace_bytes(...)
+ * Computed to about fp32's precision whatever the type, and rounded once.
+ * Errors: BGL_EINVAL (null or misaligned pointers, sizes < 1, strides, steps outside
+ * [1, 64], eps < 0), BGL_EUNSUPPORTED (sizes > BGL_MAX_DIM, batch > 65,535, coefficients
+ * that diverge), BGL_ECAPACITY, BGL_EHIP.
+ */
+int bgl_orthogonalize_workspace_bytes(int64_t batch, int32_t rows, int32_t cols, int32_t dtype,
+                                      size_t *bytes);
+int bgl_orthogonalize(const void *update, int64_t update_matrix_stride, int64_t update_row_stride,
+                      int64_t batch, int32_t rows, int32_t cols, int32_t dtype, int32_t steps,
+                      const float *coefficients, float eps, void *out, int64_t out_matrix_stride,
+                      int64_t out_row_stride, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -27,6 +27,12 @@ BGL_DEVICE, BGL_HOST_PINNED, BGL_HOST_PINNED_COL = 0, 1, 2
  STAGE_INSERT_MAP, STAGE_INSERT_ROWS, STAGE_LINK_COPY, STAGE_ASSEMBLE_PRE, STAGE_ASSEMBLE) = range(9)
 STAGE_NAMES = ["probe", "miss_list", "gather_hit", "fetch_miss", "insert_map", "insert_rows", "link_copy",
                "assemble_pre", "assemble"]
+BGL_F32, BGL_BF16 = 0, 1
+BGL_MAX_GROUPS = 1024
+BGL_MAX_DIM = 16384
+DTYPES = {torch.float32: BGL_F32, torch.bfloat16: BGL_BF16}
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+RESIDUALS = {"none": 0, "before": 1, "after": 2}
 
 EXPORTS = [
     "bgl_last_error", "bgl_graph_load_csr", "bgl_graph_destroy", "bgl_sample_workspace_bytes",
@@ -41,6 +47,9 @@ EXPORTS = [
     "bgl_order_bfs_sequence", "bgl_order_proximity", "bgl_order_choose_sequences",
     "bgl_order_shuffling_error",
     "bgl_pipeline_create", "bgl_pipeline_destroy", "bgl_pipeline_set_cache", "bgl_pipeline_set_tier", "bgl_pipeline_streams", "bgl_pipeline_last_batch", "bgl_pipeline_run",
+    "bgl_group_rows_workspace_bytes", "bgl_group_rows",
+    "bgl_linear_workspace_bytes", "bgl_linear_forward", "bgl_linear_backward",
+    "bgl_orthogonalize_workspace_bytes", "bgl_orthogonalize",
 ]
 
 
@@ -60,6 +69,10 @@ class SubgraphStruct(C.Structure):
         ("cap_edges", C.c_int64 * BGL_MAX_HOPS),
         ("counts", C.c_void_p),
     ]
+
+
+class LinearStruct(C.Structure):
+    _fields_ = [(name, C.c_int32) for name in ("dtype", "activation", "residual", "in_dim", "out_dim", "num_groups")]
 
 
 class PipelineBuffers(C.Structure):
@@ -127,6 +140,14 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     L.bgl_pipeline_streams.argtypes = [vp, C.POINTER(vp), C.POINTER(vp)]
     L.bgl_pipeline_last_batch.argtypes = [vp, C.POINTER(vp), C.POINTER(i64)]
     L.bgl_pipeline_run.argtypes = [vp, vp, i64, vp, i64, i64, vp, vp, vp, BATCH_FN, vp]
+    L.bgl_group_rows_workspace_bytes.argtypes = [i64, i32, C.POINTER(C.c_size_t)]
+    L.bgl_group_rows.argtypes = [vp, i64, vp, i64, i32, vp, vp, vp, C.c_size_t, vp]
+    L.bgl_linear_workspace_bytes.argtypes = [C.POINTER(LinearStruct), i64, C.POINTER(C.c_size_t)]
+    L.bgl_linear_forward.argtypes = [C.POINTER(LinearStruct), i64, vp, vp, vp, i64, vp, vp, vp, i64, vp, i64, vp, i64, vp]
+    L.bgl_linear_backward.argtypes = [C.POINTER(LinearStruct), i64, vp, vp, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp,
+                                      vp, i64, vp, C.c_size_t, vp]
+    L.bgl_orthogonalize_workspace_bytes.argtypes = [i64, i32, i32, i32, C.POINTER(C.c_size_t)]
+    L.bgl_orthogonalize.argtypes = [vp, i64, i64, i64, i32, i32, i32, i32, vp, C.c_float, vp, i64, i64, vp, C.c_size_t, vp]
     for name in EXPORTS:
         if name != "bgl_last_error":
             getattr(L, name).restype = ci
@@ -515,3 +536,160 @@ def order_choose_sequences(graph: Graph, train_nodes, roots, shifts, batch: int,
                                             C.byref(chosen), errs.ctypes.data, order.ctypes.data,
                                             _stream_handle(stream)))
     return chosen.value, errs[: chosen.value].copy(), order
+
+
+def _workspace(nbytes: int) -> torch.Tensor:
+    """Device memory of at least `nbytes` bytes, 256-byte aligned."""
+    w = torch.empty(nbytes + 256, dtype=torch.uint8, device="cuda")
+    return w[(-w.data_ptr()) % 256:]
+
+
+def _matrix(name: str, t: Optional[torch.Tensor], n: int, width: int, dtype):
+    """(address, row stride) of n device rows of `width` values; the values of a row are neighbours."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or t.dtype != dtype:
+        raise ValueError(f"{name}: expected a device tensor of {dtype}")
+    if tuple(t.shape) != (n, width):
+        raise ValueError(f"{name}: expected shape {(n, width)}, got {tuple(t.shape)}")
+    if n > 0 and width > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the values of a row must be contiguous")
+    return t.data_ptr(), (t.stride(0) if n > 1 else max(width, 1))
+
+
+def _weights(name: str, t: Optional[torch.Tensor], shape, dtype):
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    return _dev_ptr(t, dtype)
+
+
+class RowGroups:
+    """bgl_group_rows: a batch's rows in group order, for layers with groups; owns rows, offsets and the workspace for
+    batches of up to max_rows rows."""
+
+    def __init__(self, max_rows: int, num_groups: int):
+        _require_gpu()
+        self.max_rows, self.num_groups, self.n = int(max_rows), int(num_groups), 0
+        nbytes = C.c_size_t(0)
+        _check(lib().bgl_group_rows_workspace_bytes(self.max_rows, self.num_groups, C.byref(nbytes)))
+        self.workspace = _workspace(int(nbytes.value))
+        self._rows = torch.empty(max(self.max_rows, 1), dtype=torch.int32, device="cuda")
+        self.offsets = torch.zeros(self.num_groups + 1, dtype=torch.int32, device="cuda")
+
+    @property
+    def rows(self) -> torch.Tensor:
+        """The batch's rows in group order (int32), those of no group last."""
+        return self._rows[: self.n]
+
+    def build(self, group_of: torch.Tensor, ids: Optional[torch.Tensor] = None, n: Optional[int] = None, stream=None) -> None:
+        """Row i of the batch belongs to group group_of[ids[i]] (group_of[i] without ids).  n: rows of the batch (default: all
+        of ids or group_of)."""
+        have = group_of.numel() if ids is None else ids.numel()
+        n = have if n is None else int(n)
+        if n < 0 or n > min(self.max_rows, have):
+            raise ValueError(f"n = {n} is more than the ids, or than the {self.max_rows} rows there is room for")
+        _check(lib().bgl_group_rows(_dev_ptr(group_of, torch.int32), group_of.numel(), _dev_ptr(ids, torch.int32), n, self.num_groups,
+                                    self._rows.data_ptr(), self.offsets.data_ptr(), self.workspace.data_ptr(),
+                                    self.workspace.numel(), _stream_handle(stream)))
+        self.n = n
+
+
+class Linear:
+    """bgl_linear_forward / bgl_linear_backward for layers of one shape, over batches of up to max_rows rows; owns the backward
+    call's workspace (allocated with the first backward call), so calls on one object must follow one another in stream order.
+
+    y = act(x weight' + bias [+ residual]) [+ residual]; activation: none, relu, gelu, silu; residual: none, before (the
+    activation), after.  num_groups > 0: weight (num_groups, out_dim, in_dim) and bias (num_groups, out_dim), and every call is
+    given the batch's RowGroups."""
+
+    def __init__(self, max_rows: int, in_dim: int, out_dim: int, dtype=torch.float32, activation: str = "none",
+                 residual: str = "none", num_groups: int = 0):
+        _require_gpu()
+        if dtype not in DTYPES or activation not in ACTIVATIONS or residual not in RESIDUALS:
+            raise ValueError(f"unknown dtype, activation or residual: {dtype}, {activation}, {residual}")
+        self.max_rows, self.in_dim, self.out_dim, self.dtype = int(max_rows), int(in_dim), int(out_dim), dtype
+        self.num_groups = int(num_groups)
+        self.struct = LinearStruct(DTYPES[dtype], ACTIVATIONS[activation], RESIDUALS[residual], self.in_dim, self.out_dim,
+                                   self.num_groups)
+        self._bytes(self.max_rows)      # (checks the arguments)
+        self._lead = (self.num_groups,) if self.num_groups else ()
+        self.workspace = None
+
+    def _bytes(self, n: int) -> int:
+        nbytes = C.c_size_t(0)
+        _check(lib().bgl_linear_workspace_bytes(C.byref(self.struct), n, C.byref(nbytes)))
+        return int(nbytes.value)
+
+    def _groups(self, groups: Optional[RowGroups], n: int):
+        if (groups is None) != (self.num_groups == 0):
+            raise ValueError("a layer with groups, and only such a layer, needs the batch's groups")
+        if groups is None:
+            return None, None
+        if groups.num_groups != self.num_groups or groups.n != n:
+            raise ValueError(f"groups are of {groups.n} rows in {groups.num_groups}, the layer's call of {n} rows in {self.num_groups}")
+        return groups._rows.data_ptr(), groups.offsets.data_ptr()
+
+    def forward(self, x, weight, y, bias=None, residual=None, saved=None, groups: Optional[RowGroups] = None, stream=None) -> None:
+        """Writes y, and saved = the pre-activation if given (the backward call of a layer with an activation needs it)."""
+        n = int(x.shape[0])
+        if n > self.max_rows:
+            raise ValueError(f"{n} rows, the layer was made for {self.max_rows}")
+        _check(lib().bgl_linear_forward(
+            C.byref(self.struct), n, *self._groups(groups, n), *_matrix("x", x, n, self.in_dim, self.dtype),
+            _weights("weight", weight, self._lead + (self.out_dim, self.in_dim), self.dtype),
+            _weights("bias", bias, self._lead + (self.out_dim,), self.dtype),
+            *_matrix("residual", residual, n, self.out_dim, self.dtype), *_matrix("y", y, n, self.out_dim, self.dtype),
+            *_matrix("saved", saved, n, self.out_dim, self.dtype), _stream_handle(stream)))
+
+    def backward(self, dy, x=None, weight=None, saved=None, dx=None, dweight=None, dbias=None, dresidual=None,
+                 groups: Optional[RowGroups] = None, stream=None) -> None:
+        """Writes the gradients that are given memory: dx (needs weight), dweight (needs x), dbias (with dweight), dresidual (the
+        residual before the activation)."""
+        n = int(dy.shape[0])
+        if n > self.max_rows:
+            raise ValueError(f"{n} rows, the layer was made for {self.max_rows}")
+        need = self._bytes(n)
+        if self.workspace is None or self.workspace.numel() < need:
+            self.workspace = _workspace(max(need, self._bytes(self.max_rows)))
+        _check(lib().bgl_linear_backward(
+            C.byref(self.struct), n, *self._groups(groups, n), *_matrix("dy", dy, n, self.out_dim, self.dtype),
+            *_matrix("x", x, n, self.in_dim, self.dtype),
+            _weights("weight", weight, self._lead + (self.out_dim, self.in_dim), self.dtype),
+            *_matrix("saved", saved, n, self.out_dim, self.dtype), *_matrix("dx", dx, n, self.in_dim, self.dtype),
+            _weights("dweight", dweight, self._lead + (self.out_dim, self.in_dim), self.dtype),
+            _weights("dbias", dbias, self._lead + (self.out_dim,), self.dtype),
+            *_matrix("dresidual", dresidual, n, self.out_dim, self.dtype),
+            self.workspace.data_ptr(), self.workspace.numel(), _stream_handle(stream)))
+
+
+class Orthogonalizer:
+    """bgl_orthogonalize for `batch` matrices of rows x cols; owns the workspace."""
+
+    def __init__(self, batch: int, rows: int, cols: int, dtype=torch.float32, steps: int = 5,
+                 coefficients: Sequence[float] = (3.4445, -4.7750, 2.0315), eps: float = 1e-7):
+        _require_gpu()
+        if dtype not in DTYPES:
+            raise ValueError(f"unknown dtype: {dtype}")
+        self.shape, self.dtype, self.steps, self.eps = (int(batch), int(rows), int(cols)), dtype, int(steps), float(eps)
+        self.coefficients = np.ascontiguousarray(coefficients, dtype=np.float32)
+        if self.coefficients.shape != (3,):
+            raise ValueError("three coefficients")
+        nbytes = C.c_size_t(0)
+        _check(lib().bgl_orthogonalize_workspace_bytes(*self.shape, DTYPES[dtype], C.byref(nbytes)))
+        self.workspace = _workspace(int(nbytes.value))
+
+    def run(self, update: torch.Tensor, out: torch.Tensor, stream=None) -> None:
+        """out = update, orthogonalised; both (batch, rows, cols), or (rows, cols) for a batch of one; out may be update."""
+        def strides(name, t):
+            t = t[None] if t.dim() == 2 else t
+            if not t.is_cuda or t.dtype != self.dtype or tuple(t.shape) != self.shape:
+                raise ValueError(f"{name}: expected a device tensor of {self.dtype}, shape {self.shape}")
+            if self.shape[2] > 1 and t.stride(2) != 1:
+                raise ValueError(f"{name}: the values of a row must be contiguous")
+            return t.data_ptr(), t.stride(0), (t.stride(1) if self.shape[1] > 1 else self.shape[2])
+        src, dst = strides("update", update), strides("out", out)
+        _check(lib().bgl_orthogonalize(src[0], src[1], src[2], *self.shape, DTYPES[self.dtype], self.steps, self.coefficients.ctypes.data,
+                                       self.eps, dst[0], dst[1], dst[2], self.workspace.data_ptr(), self.workspace.numel(),
+                                       _stream_handle(stream)))

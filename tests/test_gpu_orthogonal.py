@@ -1,0 +1,179 @@
+"""Orthogonalised updates against the definition in 64 bits.
+
+A rounding error of one step lies in all directions alike and is enlarged by each later step by at most a (the polynomial's slope at 0,
+its largest), so an error e of the first step ends as a^(steps-1) e at most.  Every step rounds X, P and Q (22 bits: 2^-22 of values whose
+Frobenius norms are at most those below) and sums in fp32; with sqrt(m) for the norm that P and Q have beyond X's:
+|error|_F <= steps * a^steps * 16 * 2^-22 * max(1, |X|_F of any step), and the type's rounding of the result on top."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+USUAL = (3.4445, -4.7750, 2.0315)
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    return torch
+
+
+@pytest.fixture(scope="module")
+def B(torch):
+    from paper_2112_08541_amd import binding
+    binding.lib()
+    return binding
+
+
+def steps64(u, coefficients, steps, eps):
+    a, b, c = (float(np.float32(v)) for v in coefficients)
+    x = u / (np.sqrt((u * u).sum()) + float(np.float32(eps)))
+    if x.shape[0] > x.shape[1]:
+        return np.ascontiguousarray(_steps(np.ascontiguousarray(x.T), a, b, c, steps)[0].T), _steps(x.T, a, b, c, steps)[1]
+    return _steps(x, a, b, c, steps)
+
+
+def _steps(x, a, b, c, steps):
+    most = 1.0
+    for _ in range(steps):
+        p = x @ x.T
+        x = a * x + (b * p + c * p @ p) @ x
+        most = max(most, np.linalg.norm(x))
+    return x, most
+
+
+def check(torch, B, u, dtype, steps=5, coefficients=USUAL, eps=1e-7, in_place=False):
+    dt = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    t = torch.from_numpy(np.asarray(u, dtype=np.float32)).to(dt).cuda()
+    o = B.Orthogonalizer(*t.shape, dtype=dt, steps=steps, coefficients=coefficients, eps=eps)
+    values = t.double().cpu().numpy()
+    out = t if in_place else torch.full_like(t, float("nan"))
+    o.run(t, out)
+    got = out.double().cpu().numpy()
+    assert np.isfinite(got).all()
+    for i in range(t.shape[0]):
+        want, most = steps64(values[i], coefficients, steps, eps)
+        bound = steps * abs(coefficients[0]) ** steps * 16 * 2.0 ** -22 * most
+        bound += (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * np.linalg.norm(want) * 1.01
+        off = np.linalg.norm(got[i] - want)
+        assert off <= bound, f"matrix {i}: {off:.3g} off, bound {bound:.3g}, norm {np.linalg.norm(want):.3g}"
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("batch,rows,cols", [(1, 1, 1), (1, 1, 300), (3, 300, 1), (2, 2, 3), (1, 31, 33), (4, 32, 32), (2, 64, 100),
+                                             (3, 100, 64), (8, 47, 128), (9, 128, 47), (1, 128, 128), (2, 129, 127), (1, 200, 500),
+                                             (16, 160, 96), (1, 700, 257), (40, 130, 140)])
+def test_updates_match_the_definition(torch, B, dtype, batch, rows, cols):
+    rng = np.random.default_rng([batch, rows, cols])
+    check(torch, B, rng.standard_normal((batch, rows, cols)) * 1e-3, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_tiles(torch, B, dtype):
+    rng = np.random.default_rng(5)
+    check(torch, B, rng.standard_normal((90, 200, 250)), dtype, steps=3)
+    check(torch, B, rng.standard_normal((270, 70, 130)), dtype, steps=2)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(48, 80), (200, 150)])
+def test_updates_of_every_size_and_rank(torch, B, dtype, rows, cols):
+    rng = np.random.default_rng(7)
+    one = np.outer(rng.integers(-3, 4, rows), rng.integers(-3, 4, cols)).astype(np.float64)      # rank 1, exact in both types
+    few = np.zeros((rows, cols))
+    few[::7, ::5] = rng.integers(-8, 9, few[::7, ::5].shape)
+    steep = np.diag(2.0 ** -np.arange(rows))[:, :cols] if rows <= cols else np.diag(2.0 ** -np.arange(cols))
+    pad = np.zeros((rows, cols))
+    pad[: steep.shape[0], : steep.shape[1]] = steep
+    eye = np.eye(rows, cols)
+    check(torch, B, np.stack([one, few, pad, eye, one * 1e15, eye * 1e-20]), dtype)
+
+
+def test_nothing_stays_nothing_and_one_bad_matrix_stays_alone(torch, B):
+    u = torch.randn((9, 40, 70), device="cuda")
+    u[0] = 0
+    u[3, 2, 1] = float("nan")
+    u[5, 0, 0] = float("inf")
+    out = torch.empty_like(u)
+    o = B.Orthogonalizer(9, 40, 70)
+    o.run(u, out)
+    got = out.cpu().numpy()
+    assert (got[0] == 0).all() and np.isnan(got[3]).all()
+    fine = [1, 2, 4, 6, 7, 8]
+    assert np.isfinite(got[fine]).all()
+    clean = torch.empty((6, 40, 70), device="cuda")
+    B.Orthogonalizer(6, 40, 70).run(u[fine].contiguous(), clean)
+    assert np.allclose(clean.cpu().numpy(), got[fine], atol=1e-5)
+
+
+@pytest.mark.parametrize("coefficients,steps", [((1.5, -0.5, 0.0), 12), ((2.0, -1.5, 0.5), 4), ((1.0, 0.0, 0.0), 3), ((0.0, 0.0, 0.0), 1)])
+def test_other_coefficients(torch, B, coefficients, steps):
+    rng = np.random.default_rng(8)
+    check(torch, B, rng.standard_normal((2, 60, 90)), "f32", steps=steps, coefficients=coefficients)
+
+
+def test_the_usual_steps_bring_singular_values_to_one(torch, B):
+    u = torch.randn((3, 64, 200), device="cuda")
+    out = torch.empty_like(u)
+    B.Orthogonalizer(3, 64, 200).run(u, out)
+    s = np.linalg.svd(out.double().cpu().numpy(), compute_uv=False)
+    assert s.min() > 0.6 and s.max() < 1.3
+
+
+def test_strides_in_place_streams_and_repeats(torch, B):
+    rng = np.random.default_rng(9)
+    check(torch, B, rng.standard_normal((3, 50, 70)), "f32", in_place=True)
+    check(torch, B, rng.standard_normal((3, 150, 70)), "bf16", in_place=True)
+    wide = torch.randn((4, 66, 131), device="cuda")
+    u = wide[:, 1:61, 3:103]
+    o = B.Orthogonalizer(4, 60, 100)
+    plain = torch.empty((4, 60, 100), device="cuda")
+    o.run(u.contiguous(), plain)
+    room = torch.full((4, 70, 120), 5.0, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    o.run(u, room[:, 2:62, 5:105], stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(room[:, 2:62, 5:105], plain)
+    room[:, 2:62, 5:105] = 5.0
+    assert bool((room == 5.0).all())
+    one = torch.empty((60, 100), device="cuda")
+    B.Orthogonalizer(1, 60, 100).run(u[2], one)
+    assert np.allclose(one.cpu().numpy(), plain[2].cpu().numpy(), atol=1e-5)
+
+
+def test_captured_calls_replay(torch, B):
+    for shape in ((3, 100, 60), (2, 300, 200)):
+        u = torch.randn(shape, device="cuda")
+        out, again = torch.empty_like(u), torch.empty_like(u)
+        o = B.Orthogonalizer(*shape)
+        o.run(u, out)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            o.run(u, out)
+        for i in range(4):
+            u.normal_()
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            got = out.clone()
+            o.run(u, again)
+            torch.cuda.synchronize()
+            assert torch.equal(got, again), i
+
+
+def test_the_binding_refuses_what_does_not_fit(torch, B):
+    o = B.Orthogonalizer(2, 10, 12)
+    f = lambda *s, **k: torch.zeros(s, device="cuda", **k)      # noqa: E731
+    for bad in (lambda: o.run(f(2, 10, 11), f(2, 10, 12)), lambda: o.run(f(2, 10, 12), f(10, 12)), lambda: o.run(f(2, 10, 12).cpu(), f(2, 10, 12)),
+                lambda: o.run(f(2, 12, 10).transpose(1, 2), f(2, 10, 12)), lambda: o.run(f(2, 10, 12, dtype=torch.bfloat16), f(2, 10, 12)),
+                lambda: B.Orthogonalizer(1, 4, 4, torch.float16), lambda: B.Orthogonalizer(1, 4, 4, coefficients=(1.0, 2.0))):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: B.Orthogonalizer(1, 0, 4), lambda: B.Orthogonalizer(1, 4, 4, steps=0).run(f(4, 4), f(4, 4)),
+                lambda: B.Orthogonalizer(1, 4, 4, coefficients=(9.0, 9.0, 9.0)).run(f(4, 4), f(4, 4)),
+                lambda: o.run(f(1, 10, 12).expand(2, 10, 12), f(2, 10, 12))):
+        with pytest.raises(B.BglError):
+            bad()
