@@ -717,7 +717,7 @@ int bgl_pipeline_run(bgl_pipeline_t *p, const int32_t *seeds, int64_t seed_batch
  * out_rows; a stream that uses them first passes bgl_cache_wait_rows.
  *
  * Matrices are rows of values, stride values apart (row i at data + i * stride;
- * stride >= the row's width, alignment that of the values).  Products are summed
+ * the row's width <= stride < 2^31, alignment that of the values).  Products are summed
  * in fp32; results are rounded once, to the layer's type.  All calls enqueue on
  * `stream`, allocate nothing, keep nothing between calls and can be captured.
  */

@@ -11,6 +11,8 @@
 #include "bgl_internal.h"
 #include "bgl_tile.h"
 
+#include <type_traits>
+
 namespace bgl {
 namespace {
 
@@ -22,22 +24,42 @@ constexpr int kGroupTiles = 256;     // workgroups of one grouping pass at most
 constexpr int kGroupTileRows = 2048; // rows a workgroup takes at least
 
 // ----------------------------------------------------------------- activations
-template <int ACT>
-__device__ __forceinline__ float activate(float z)
+// The library's erff and expf are 30 to 50 instructions, which made the epilogue of 428,377 x 256 gelu values longer than their stores.
+// exp: the hardware's 2^x.
+__device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
+
+// Phi(z) = erfc(-z / sqrt 2) / 2 and phi(z) sqrt(2 pi) = exp(-z^2 / 2), by Abramowitz and Stegun 7.1.26: erfc(x) = (a1 t + .. + a5 t^5) exp(-x^2),
+// t = 1 / (1 + 0.3275911 x), x >= 0, off by 1.5e-7 at most.
+__device__ __forceinline__ float normal_cdf(float z, float &bell)
 {
-    if constexpr (ACT == BGL_ACT_RELU) return z < 0.0f ? 0.0f : z;  // (NaN stays)
-    if constexpr (ACT == BGL_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-    if constexpr (ACT == BGL_ACT_SILU) return z / (1.0f + expf(-z));
+    const float x = fabsf(z) * 0.70710678118654752f;
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
+    bell = exp_fast(-x * x);
+    const float tail = 0.5f * bell * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    return z < 0.0f ? tail : 1.0f - tail;
+}
+
+__device__ __forceinline__ float activate(int act, float z)
+{
+    if (act == BGL_ACT_RELU) return z < 0.0f ? 0.0f : z;  // (NaN stays)
+    if (act == BGL_ACT_GELU) {
+        float bell;
+        return z * normal_cdf(z, bell);
+    }
+    if (act == BGL_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + exp_fast(-z));
     return z;
 }
-template <int ACT>
-__device__ __forceinline__ float slope(float z)
+__device__ __forceinline__ float slope(int act, float z)
 {
-    if constexpr (ACT == BGL_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
-    if constexpr (ACT == BGL_ACT_GELU) return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
-    if constexpr (ACT == BGL_ACT_SILU) {
-        const float p = 1.0f / (1.0f + expf(-z));
-        return p * (1.0f + z * (1.0f - p));
+    if (act == BGL_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
+    if (act == BGL_ACT_GELU) {
+        float bell;
+        const float p = normal_cdf(z, bell);
+        return fmaf(z * bell, 0.39894228040143268f, p);
+    }
+    if (act == BGL_ACT_SILU) {
+        const float p = __builtin_amdgcn_rcpf(1.0f + exp_fast(-z));
+        return p * fmaf(z, 1.0f - p, 1.0f);
     }
     return 1.0f;
 }
@@ -97,27 +119,27 @@ __device__ __forceinline__ Span find_span(const Groups &q, int64_t n, int classe
     return s;
 }
 
-// Tiles of the groups before group g (g < 64 * passes), and g's own.
-__device__ __forceinline__ void tiles_before(const Groups &q, int64_t n, int tile_rows, int g, int64_t &before, int &own)
+// The groups' rows in units of unit_rows (a group's last may be short): those of the groups before g, g's own, all.
+__device__ __forceinline__ void count_units(const Groups &q, int64_t n, int unit_rows, int g, int64_t &before, int &own, int64_t &all)
 {
     if (q.groups == 0) {
         before = 0;
-        own = (int)((n + tile_rows - 1) / tile_rows);
+        all = own = (int)((n + unit_rows - 1) / unit_rows);
         return;
     }
     const int lane = threadIdx.x & 63;
-    before = 0;
-    for (int g0 = 0;; g0 += 64) {
+    before = all = 0;
+    own = 0;
+    for (int g0 = 0; g0 < q.groups; g0 += 64) {
         int64_t lo = 0, hi = 0;
         if (g0 + lane < q.groups) group_range(q, n, g0 + lane, lo, hi);
-        const int tiles = (int)((hi - lo + tile_rows - 1) / tile_rows);
-        const int upto = wave_incl_scan(tiles);
-        if (g < g0 + 64) {
-            own = __shfl(tiles, g - g0);
-            before += __shfl(upto, g - g0) - own;
-            return;
+        const int units = (int)((hi - lo + unit_rows - 1) / unit_rows);
+        const int upto = wave_incl_scan(units);
+        if (g >= g0 && g < g0 + 64) {
+            own = __shfl(units, g - g0);
+            before = all + __shfl(upto, g - g0) - own;
         }
-        before += __shfl(upto, 63);
+        all += __shfl(upto, 63);
     }
 }
 
@@ -129,22 +151,29 @@ __device__ __forceinline__ int32_t row_at(const Groups &q, int64_t n, int64_t po
 
 // ----------------------------------------------------------------- columns of a row
 template <class T, int TT>
+struct Cols {
+    typename T::elem e[TT];
+};
+template <class T, int TT>
+__device__ __forceinline__ Cols<T, TT> load_cols_upto(const typename T::elem *p, int left)
+{
+    Cols<T, TT> pack;
+    if (left >= TT) return load_any<Cols<T, TT>>(p);
+#pragma unroll
+    for (int i = 0; i < TT; ++i) pack.e[i] = i < left ? p[i] : (typename T::elem)0;
+    return pack;
+}
+template <class T, int TT>
 __device__ __forceinline__ void load_cols(const typename T::elem *p, int left, float (&v)[TT])
 {
-    struct Pack { typename T::elem e[TT]; } pack;
-    if (left >= TT) {
-        pack = load_any<Pack>(p);
-    } else {
-#pragma unroll
-        for (int i = 0; i < TT; ++i) pack.e[i] = i < left ? p[i] : (typename T::elem)0;
-    }
+    const Cols<T, TT> pack = load_cols_upto<T, TT>(p, left);
 #pragma unroll
     for (int i = 0; i < TT; ++i) v[i] = T::get(pack.e[i]);
 }
 template <class T, int TT>
 __device__ __forceinline__ void store_cols(typename T::elem *p, int left, const float (&v)[TT])
 {
-    struct Pack { typename T::elem e[TT]; } pack;
+    Cols<T, TT> pack;
 #pragma unroll
     for (int i = 0; i < TT; ++i) pack.e[i] = T::put(v[i]);
     if (left >= TT) {
@@ -165,86 +194,127 @@ struct RowsArgs {
     typename T::elem *y, *saved;
     int64_t n, x_stride, y_stride, residual_stride, saved_stride, row_tiles;
     int K, N, col_tiles;  // summed and kept width
-    int residual_mode;
+    int residual_mode, activation;
     Groups q;
 };
 
-template <class T, bool B_OC, int TT, int ACT>
+// The tile's sums, in LDS, to their rows: a thread has VEC neighbouring columns of every so many rows.  WHOLE: N is a multiple of VEC.
+template <class T, class C, class R, bool WHOLE>
+__device__ __forceinline__ void finish_rows(const RowsArgs<T> &a, const float *sums, const int32_t *row_of, int part, int group, int n0)
+{
+    constexpr int W = R::W, V = T::VEC, PER_ROW = W / V, ROWS = kThreads / PER_ROW, PASSES = R::ROWS > ROWS ? R::ROWS / ROWS : 1;
+    constexpr int BATCH = PASSES < 8 ? PASSES : 8;
+    using Piece = Cols<T, V>;
+    const int c = (int)(threadIdx.x % PER_ROW) * V, r0 = threadIdx.x / PER_ROW, left = a.N - n0 - c;
+    if (left <= 0 || c >= C::BB || r0 >= R::ROWS) return;
+    float bias[V] = {};
+    if (a.bias && group >= 0) load_cols<T, V>(a.bias + (int64_t)group * a.N + n0 + c, WHOLE ? V : left, bias);
+#pragma unroll
+    for (int p0 = 0; p0 < PASSES; p0 += BATCH) {
+        int32_t row[BATCH];
+        Piece res[BATCH];
+#pragma unroll
+        for (int p = 0; p < BATCH; ++p) row[p] = row_of[R::row(part, r0 + (p0 + p) * ROWS)];
+        if (a.residual_mode) {  // all asked for before the first is used: one after the other they took longer than the product
+#pragma unroll
+            for (int p = 0; p < BATCH; ++p) {
+                const typename T::elem *from = a.residual + (row[p] < 0 ? 0 : row[p]) * a.residual_stride + n0 + c;
+                res[p] = WHOLE ? load_any<Piece>(from) : load_cols_upto<T, V>(from, left);
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < BATCH; ++p) {
+            float v[V];
+#pragma unroll
+            for (int u = 0; u < V; u += 4) {
+                const f32x4 four = *reinterpret_cast<const f32x4 *>(sums + result_place<W>(r0 + (p0 + p) * ROWS, c + u));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[u + e] = four[e] + bias[u + e];
+            }
+            if (a.residual_mode == BGL_RESIDUAL_BEFORE) {
+#pragma unroll
+                for (int u = 0; u < V; ++u) v[u] += T::get(res[p].e[u]);
+            }
+            if (row[p] < 0) continue;
+            if (a.saved) store_cols<T, V>(a.saved + row[p] * a.saved_stride + n0 + c, WHOLE ? V : left, v);
+            if (a.activation) {
+#pragma unroll
+                for (int u = 0; u < V; ++u) v[u] = activate(a.activation, v[u]);
+            }
+            if (a.residual_mode == BGL_RESIDUAL_AFTER) {
+#pragma unroll
+                for (int u = 0; u < V; ++u) v[u] += T::get(res[p].e[u]);
+            }
+            store_cols<T, V>(a.y + row[p] * a.y_stride + n0 + c, WHOLE ? V : left, v);
+        }
+    }
+}
+
+template <class T, bool B_OC, class C>
 __global__ __launch_bounds__(kThreads, 2) void k_linear_rows(RowsArgs<T> a)
 {
-    constexpr int BO = 32 * TT;
-    __shared__ __attribute__((aligned(16))) uint32_t lds[2][2][BO * kDwords];
-    __shared__ int32_t row_of[BO];
+    using A = KcOperand<T, C::BA>;
+    using B = std::conditional_t<B_OC, OcOperand<T, C::BB, false>, KcOperand<T, C::BB>>;
+    using R = Result<C, A::LDS + B::LDS>;
+    constexpr int LDS = A::LDS + B::LDS > R::SIZE ? A::LDS + B::LDS : R::SIZE;
+    __shared__ __attribute__((aligned(16))) uint32_t lds[LDS];
+    __shared__ int32_t row_of[C::BA];
     int64_t rt;
     int ct;
     if (!tile_of(blockIdx.x, a.row_tiles, a.col_tiles, rt, ct)) return;
-    const Span s = find_span(a.q, a.n, a.q.groups + (a.q.groups > 0), BO, rt);
+    const Span s = find_span(a.q, a.n, a.q.groups + (a.q.groups > 0), C::BA, rt);
     if (s.group < 0) return;
-    const bool grouped = a.q.groups > 0, none = grouped && s.group == a.q.groups;
-    const int n0 = ct * BO, K = none ? 0 : a.K;
+    const bool none = a.q.groups > 0 && s.group == a.q.groups;
+    const int n0 = ct * C::BB, K = none ? 0 : a.K;
     const typename T::elem *w = a.w + (none ? 0 : (int64_t)s.group * a.N * a.K);
 
-    if ((int)threadIdx.x < BO) row_of[threadIdx.x] = (int)threadIdx.x < s.count ? row_at(a.q, a.n, s.start + threadIdx.x) : -1;
+    if ((int)threadIdx.x < C::BA) row_of[threadIdx.x] = (int)threadIdx.x < s.count ? row_at(a.q, a.n, s.start + threadIdx.x) : -1;
     __syncthreads();
-    KcOperand<T, BO, TT> rows;
-    rows.init([&](int i) {
-        const int32_t r = row_of[i];
-        return a.x + (r < 0 ? 0 : r) * a.x_stride;
-    });
-    constexpr int BK = KcOperand<T, BO, TT>::BK;
-    f32x4 acc[TT][TT] = {};
-    const int wave = threadIdx.x / kWave, a_off = (wave >> 1) * 16 * TT, b_off = (wave & 1) * 16 * TT;
-    const int tiles = (K + BK - 1) / BK;
-    auto loop = [&](auto &weight, auto load) {
-        if (tiles == 0) return;
-        rows.load(0, K);
-        load(0);
-        for (int i = 0; i < tiles; ++i) {
-            rows.store(lds[i & 1][0]);
-            weight.store(lds[i & 1][1]);
-            __syncthreads();
-            if (i + 1 < tiles) {
-                rows.load((i + 1) * BK, K);
-                load((i + 1) * BK);
-            }
-            const int steps = (K - i * BK + 16 * T::PER - 1) / (16 * T::PER);
-            multiply<T, false, B_OC, BO, TT>(lds[i & 1][0], lds[i & 1][1], a_off, b_off, steps, acc);
+    f32x4 acc[C::FA][C::FB] = {};
+    if (K > 0) {
+        A rows;
+        B weight;
+        rows.init([&](int i) {
+            const int32_t r = row_of[i];
+            return a.x + (r < 0 ? 0 : r) * a.x_stride;
+        });
+        if constexpr (B_OC) {
+            weight.init(w, a.N, K, n0, a.N);
+            weight.range(nullptr, 0, K);
+        } else {
+            weight.init([&](int i) { return w + (int64_t)(n0 + i < a.N ? n0 + i : a.N - 1) * a.K; });
         }
-    };
-    if constexpr (B_OC) {
-        OcOperand<T, BO, TT> weight;
-        weight.init(w, a.N, nullptr, 0, K, K, n0, a.N);
-        loop(weight, [&](int k0) { weight.load(k0); });
-    } else {
-        KcOperand<T, BO, TT> weight;
-        weight.init([&](int i) { return w + (int64_t)(n0 + i < a.N ? n0 + i : a.N - 1) * a.K; });
-        loop(weight, [&](int k0) { weight.load(k0, K); });
+        pipeline(
+            (K + A::BK - 1) / A::BK,
+            [&](int i) {
+                rows.load(i, K);
+                if constexpr (B_OC) weight.load(i);
+                else weight.load(i, K);
+            },
+            [&] {
+                rows.store(lds);
+                if constexpr (B_OC) weight.settle();
+                weight.store(lds + A::LDS);
+            },
+            [&](int i) {
+                const int steps = (K - i * A::BK + 16 * T::PER - 1) / (16 * T::PER);
+                multiply<T, A, B, C>(lds, lds + A::LDS, steps, acc);
+            });
     }
-
-    const int l = threadIdx.x & 63, c = n0 + b_off + TT * (l & 15), left = a.N - c;
-    if (left <= 0) return;
-    float bias[TT] = {};
-    if (a.bias && !none) load_cols<T, TT>(a.bias + (int64_t)s.group * a.N + c, left, bias);
+    float *sums = reinterpret_cast<float *>(lds);
 #pragma unroll
-    for (int t = 0; t < TT; ++t)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int32_t r = row_of[a_off + TT * (4 * (l >> 4) + j) + t];
-            if (r < 0) continue;
-            float v[TT], res[TT] = {};
-            if (a.residual_mode) load_cols<T, TT>(a.residual + r * a.residual_stride + c, left, res);
-#pragma unroll
-            for (int u = 0; u < TT; ++u) v[u] = acc[t][u][j] + bias[u] + (a.residual_mode == BGL_RESIDUAL_BEFORE ? res[u] : 0.0f);
-            if (a.saved) store_cols<T, TT>(a.saved + r * a.saved_stride + c, left, v);
-#pragma unroll
-            for (int u = 0; u < TT; ++u) v[u] = activate<ACT>(v[u]) + (a.residual_mode == BGL_RESIDUAL_AFTER ? res[u] : 0.0f);
-            store_cols<T, TT>(a.y + r * a.y_stride + c, left, v);
-        }
+    for (int part = 0; part < R::PARTS; ++part) {
+        if (part) __syncthreads();
+        R::put(sums, part, acc);
+        __syncthreads();
+        if (a.N % T::VEC == 0) finish_rows<T, C, R, true>(a, sums, row_of, part, none ? -1 : s.group, n0);
+        else finish_rows<T, C, R, false>(a, sums, row_of, part, none ? -1 : s.group, n0);
+    }
 }
 
 // ----------------------------------------------------------------- dz
-template <class T, int ACT>
-__global__ __launch_bounds__(kThreads) void k_linear_dz(const typename T::elem *dy, int64_t dy_stride, const typename T::elem *saved,
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_linear_dz(int act, const typename T::elem *dy, int64_t dy_stride, const typename T::elem *saved,
                                                         int64_t saved_stride, typename T::elem *dz, int64_t dz_stride, int64_t n, int N)
 {
     constexpr int V = T::VEC;
@@ -255,120 +325,155 @@ __global__ __launch_bounds__(kThreads) void k_linear_dz(const typename T::elem *
         const int c = (int)(i % per_row) * V, left = N - c;
         float d[V], z[V];
         load_cols<T, V>(dy + r * dy_stride + c, left, d);
-        if constexpr (ACT != BGL_ACT_NONE) {
+        if (act) {
             load_cols<T, V>(saved + r * saved_stride + c, left, z);
 #pragma unroll
-            for (int e = 0; e < V; ++e) d[e] *= slope<ACT>(z[e]);
+            for (int e = 0; e < V; ++e) d[e] *= slope(act, z[e]);
         }
         store_cols<T, V>(dz + r * dz_stride + c, left, d);
     }
 }
 
 // ----------------------------------------------------------------- dW, db
-// A workgroup takes one tile of dW and one range of a group's rows; partial sums go to `part`, range by range: N * K of dW, N of db.
+// The rows of all groups are cut into units of 64 and dealt evenly to `shares` workgroups for each tile of dW: a share may end one group
+// and begin the next, so that no workgroup has more than its part however the sizes fall.  Share w leaves its sums for group g in slot w + g
+// of `part` (both grow along the rows, so no two meet in a slot): A_dim * B_dim of the matrix, then out_dim of db.
+// Side A is the wider of dz and x, side B the narrower; the matrix is laid out [A][B].
+constexpr int kUnit = 64;
+
 template <class T>
 struct WeightArgs {
-    const typename T::elem *dz, *x;
+    const typename T::elem *a, *b;
     float *part;
-    int64_t n, dz_stride, x_stride, ranges;
-    int N, K, range_rows, n_tiles, k_tiles;
-    bool with_bias;
+    int64_t n, a_stride, b_stride;
+    int a_dim, b_dim, shares, a_tiles, b_tiles;
+    int bias;  // which side is dz, if db is asked for: 1 A, 2 B, else 0
     Groups q;
 };
 
-template <class T, int TT>
-__global__ __launch_bounds__(kThreads, 2) void k_linear_dw(WeightArgs<T> a)
+template <class Op, int V>
+__device__ __forceinline__ void add_rows(const Op &op, float (&sum)[V])
 {
-    constexpr int BO = 32 * TT;
-    __shared__ __attribute__((aligned(16))) uint32_t lds[2][2][BO * kDwords];
-    int64_t range;
-    int tile;
-    if (!tile_of(blockIdx.x, a.ranges, a.n_tiles * a.k_tiles, range, tile)) return;
-    const Span s = find_span(a.q, a.n, a.q.groups, a.range_rows, range);
-    if (s.group < 0) return;
-    const int n0 = tile / a.k_tiles * BO, k0 = tile % a.k_tiles * BO;
-    using Op = OcOperand<T, BO, TT>;
-    Op up, rows;
-    up.init(a.dz, a.dz_stride, a.q.index, s.start, s.count, a.n, n0, a.N);
-    rows.init(a.x, a.x_stride, a.q.index, s.start, s.count, a.n, k0, a.K);
-    const bool bias = a.with_bias && k0 == 0;
-    float sum[T::VEC] = {};
-    f32x4 acc[TT][TT] = {};
-    const int wave = threadIdx.x / kWave, a_off = (wave >> 1) * 16 * TT, b_off = (wave & 1) * 16 * TT;
-    const int tiles = (s.count + Op::BK - 1) / Op::BK;
-    up.load(0);
-    rows.load(0);
-    for (int i = 0; i < tiles; ++i) {
-        up.store(lds[i & 1][0]);
-        rows.store(lds[i & 1][1]);
-        if (bias) {
+    if (op.idle()) return;
 #pragma unroll
-            for (int p = 0; p < Op::PASSES; ++p)
+    for (int p = 0; p < Op::PASSES; ++p) {
+        const auto v = __builtin_bit_cast(Cols<typename Op::type, V>, op.reg[p]);
 #pragma unroll
-                for (int h = 0; h < T::PER; ++h) {
-                    struct Pack { typename T::elem e[T::VEC]; };
-                    const Pack v = __builtin_bit_cast(Pack, up.reg[p][h]);
-#pragma unroll
-                    for (int e = 0; e < T::VEC; ++e) sum[e] += T::get(v.e[e]);
-                }
-        }
-        __syncthreads();
-        if (i + 1 < tiles) {
-            up.load((int64_t)(i + 1) * Op::BK);
-            rows.load((int64_t)(i + 1) * Op::BK);
-        }
-        const int steps = (s.count - i * Op::BK + 16 * T::PER - 1) / (16 * T::PER);
-        multiply<T, true, true, BO, TT>(lds[i & 1][0], lds[i & 1][1], a_off, b_off, steps, acc);
+        for (int e = 0; e < V; ++e) sum[e] += Op::type::get(v.e[e]);
     }
-    float *part = a.part + range * ((int64_t)a.N * a.K + a.N);
-    const int l = threadIdx.x & 63, c = k0 + b_off + TT * (l & 15), left = a.K - c;
-    if (left > 0) {
+}
+// The threads' column sums, those of one column in order.
+template <class Op, int V>
+__device__ __forceinline__ void put_sums(const Op &op, float *lds, const float (&sum)[V], float *to, int o0, int O)
+{
+    __syncthreads();
 #pragma unroll
-        for (int t = 0; t < TT; ++t)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int r = n0 + a_off + TT * (4 * (l >> 4) + j) + t;
-                if (r >= a.N) continue;
-                float v[TT];
-#pragma unroll
-                for (int u = 0; u < TT; ++u) v[u] = acc[t][u][j];
-                store_cols<F32, TT>(part + (int64_t)r * a.K + c, left, v);
-            }
-    }
-    if (bias) {  // the threads of one column chunk, in order
-        __syncthreads();
-        float *sums = reinterpret_cast<float *>(&lds[0][0][0]);
-#pragma unroll
-        for (int e = 0; e < T::VEC; ++e) sums[threadIdx.x * T::VEC + e] = sum[e];
-        __syncthreads();
-        if ((int)threadIdx.x < BO && n0 + (int)threadIdx.x < a.N) {
-            float v = 0.0f;
-            for (int i = 0; i < Op::ROWS; ++i) v += sums[i * BO + threadIdx.x];
-            part[(int64_t)a.N * a.K + n0 + threadIdx.x] = v;
-        }
+    for (int e = 0; e < V; ++e) lds[threadIdx.x * V + e] = op.idle() ? 0.0f : sum[e];
+    __syncthreads();
+    if ((int)threadIdx.x < Op::W && (int)threadIdx.x < Op::BOUND && o0 + (int)threadIdx.x < O) {
+        float v = 0.0f;
+        for (int i = 0; i < Op::ROWS; ++i) v += lds[i * Op::W + threadIdx.x];
+        to[o0 + threadIdx.x] = v;
     }
 }
 
-// dW and db of group blockIdx.y: the partial sums of its ranges, added in a fixed order.
+template <class T, bool LIST, class C>
+__global__ __launch_bounds__(kThreads, 2) void k_linear_dw(WeightArgs<T> a)
+{
+    using A = OcOperand<T, C::BA, LIST>;
+    using B = OcOperand<T, C::BB, LIST>;
+    constexpr int SUMS = kThreads * T::VEC, LDS = A::LDS + B::LDS > SUMS ? A::LDS + B::LDS : SUMS;
+    __shared__ __attribute__((aligned(16))) uint32_t lds[LDS];
+    int64_t share;
+    int tile;
+    if (!tile_of(blockIdx.x, a.shares, a.a_tiles * a.b_tiles, share, tile)) return;
+    const int a0 = tile / a.b_tiles * C::BA, b0 = tile % a.b_tiles * C::BB;
+    int64_t before, units;
+    int own;
+    count_units(a.q, a.n, kUnit, 0, before, own, units);
+    const int64_t last = (share + 1) * units / a.shares;
+    A left;
+    B right;
+    left.init(a.a, a.a_stride, a.n, a0, a.a_dim);
+    right.init(a.b, a.b_stride, a.n, b0, a.b_dim);
+    const bool bias_a = a.bias == 1 && b0 == 0, bias_b = a.bias == 2 && a0 == 0;
+    const int64_t len = (int64_t)a.a_dim * a.b_dim + (a.bias == 2 ? a.b_dim : a.a_dim);
+    for (int64_t unit = share * units / a.shares; unit < last;) {
+        const Span s = find_span(a.q, a.n, a.q.groups, kUnit, unit);
+        int64_t lo = 0, hi = a.n;
+        if (a.q.groups > 0) group_range(a.q, a.n, s.group, lo, hi);
+        const int64_t room = (last - unit) * kUnit;
+        const int count = (int)(hi - s.start < room ? hi - s.start : room);
+        unit += (count + kUnit - 1) / kUnit;
+        left.range(a.q.index, s.start, count);
+        right.range(a.q.index, s.start, count);
+        float sum[T::VEC] = {};
+        f32x4 acc[C::FA][C::FB] = {};
+        pipeline(
+            (count + A::BK - 1) / A::BK,
+            [&](int i) {
+                left.load(i);
+                right.load(i);
+            },
+            [&] {
+                left.settle();
+                right.settle();
+                left.store(lds);
+                right.store(lds + A::LDS);
+                if (bias_a) add_rows(left, sum);
+                if (bias_b) add_rows(right, sum);
+            },
+            [&](int i) {
+                const int steps = (count - i * A::BK + 16 * T::PER - 1) / (16 * T::PER);
+                multiply<T, A, B, C>(lds, lds + A::LDS, steps, acc);
+            });
+        float *part = a.part + (share + s.group) * len;
+        const int l = threadIdx.x & 63, r = a0 + C::a_off() + 4 * (l >> 4), c = b0 + C::b_off() + (l & 15);
+#pragma unroll
+        for (int i = 0; i < C::FA; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int t = 0; t < C::FB; ++t)
+                    if (r + 16 * i + j < a.a_dim && c + 16 * t < a.b_dim) part[(int64_t)(r + 16 * i + j) * a.b_dim + c + 16 * t] = acc[i][t][j];
+        if (bias_a) put_sums(left, reinterpret_cast<float *>(lds), sum, part + (int64_t)a.a_dim * a.b_dim, a0, a.a_dim);
+        if (bias_b) put_sums(right, reinterpret_cast<float *>(lds), sum, part + (int64_t)a.a_dim * a.b_dim, b0, a.b_dim);
+        __syncthreads();  // (the next group's first tile goes where these were read)
+    }
+}
+
+// dW and db of group blockIdx.y: what the shares left of it, added in a fixed order.
 template <class T>
-__global__ __launch_bounds__(kThreads) void k_linear_reduce(const float *part, int64_t n, int range_rows, int64_t NK, int N, Groups q,
-                                                            typename T::elem *dw, typename T::elem *db)
+struct ReduceArgs {
+    const float *part;
+    typename T::elem *dw, *db;
+    int64_t n;
+    int N, K, shares;
+    bool swapped;  // the parts' matrix is [K][N]
+    Groups q;
+};
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_linear_reduce(ReduceArgs<T> a)
 {
     __shared__ float4 sums[kThreads];
     const int g = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x / kWave;
-    int64_t first;
-    int count;
-    tiles_before(q, n, range_rows, g, first, count);
-    const int64_t len = NK + N, e = ((int64_t)blockIdx.x * 64 + lane) * 4;
+    int64_t before, units;
+    int own;
+    count_units(a.q, a.n, kUnit, g, before, own, units);
+    const int64_t NK = (int64_t)a.N * a.K, len = NK + a.N, e = ((int64_t)blockIdx.x * 64 + lane) * 4;
     const int left = len - e < 4 ? (int)(len - e) : 4;
     float v[4] = {};
-    if (left > 0)
-        for (int i = wave; i < count; i += kThreads / kWave) {
-            float w[4];
-            load_cols<F32, 4>(part + (first + i) * len + e, left, w);
+    if (left > 0 && own > 0) {
+        const int64_t first = ((before + 1) * a.shares - 1) / units, last = ((before + own) * a.shares - 1) / units;
+#pragma unroll 4
+        for (int64_t w = first + wave; w <= last; w += kThreads / kWave) {
+            float p[4];
+            load_cols<F32, 4>(a.part + (w + g) * len + e, left, p);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) v[u] += w[u];
+            for (int u = 0; u < 4; ++u) v[u] += p[u];
         }
+    }
     sums[threadIdx.x] = float4{v[0], v[1], v[2], v[3]};
     __syncthreads();
     if (wave || left <= 0) return;
@@ -379,8 +484,11 @@ __global__ __launch_bounds__(kThreads) void k_linear_reduce(const float *part, i
     }
     for (int u = 0; u < left; ++u) {
         const int64_t at = e + u;
-        if (at < NK) dw[g * NK + at] = T::put(v[u]);
-        else if (db) db[(int64_t)g * N + at - NK] = T::put(v[u]);
+        if (at >= NK) {
+            if (a.db) a.db[(int64_t)g * a.N + at - NK] = T::put(v[u]);
+        } else {
+            a.dw[g * NK + (a.swapped ? at % a.N * a.K + at / a.N : at)] = T::put(v[u]);
+        }
     }
 }
 
@@ -543,6 +651,7 @@ int check_rows(const char *name, const void *p, int64_t stride, int width, int e
     }
     if (!aligned(p, es)) BGL_FAIL(BGL_EINVAL, "%s must be aligned to its elements", name);
     if (stride < width) BGL_FAIL(BGL_EINVAL, "%s: stride %lld is less than the row's %d values", name, (long long)stride, width);
+    if (stride > INT32_MAX) BGL_FAIL(BGL_EUNSUPPORTED, "%s: stride %lld does not fit 31 bits", name, (long long)stride);
     return BGL_OK;
 }
 
@@ -552,59 +661,83 @@ int check_rows(const char *name, const void *p, int64_t stride, int width, int e
         if (rc__ != BGL_OK) return rc__; \
     } while (0)
 
-// How the backward pass cuts a layer's rows.  128 x 128 tiles of dW where both sides fill one, else 64 x 64; ranges of rows so that some
-// 512 workgroups (two on each CU) have one tile and one range each.
+// Cuts of a product into workgroup tiles.  Wide results take 128 x 128; one that fits into fewer than 8 fragments of 16 columns takes as many as
+// it has (100 columns: 7), the four wavefronts one above the other.  Where that makes too few workgroups for the 256 CUs, 64 rows.
+using Large = Cut<2, 2, 4, 4>;
+using Small = Cut<2, 2, 2, 2>;
+template <int F>
+using Narrow = Cut<4, 1, 2, F>;
+template <int F>
+using SmallNarrow = Cut<4, 1, 1, F>;
+
+template <class Do>
+void with_cut(bool large, int cols, Do call)
+{
+    const int f = (cols + 15) / 16;
+    if (large) {
+        switch (f) {
+        case 1: return call(Narrow<1>{});
+        case 2: return call(Narrow<2>{});
+        case 3: return call(Narrow<3>{});
+        case 4: return call(Narrow<4>{});
+        case 5: return call(Narrow<5>{});
+        case 6: return call(Narrow<6>{});
+        case 7: return call(Narrow<7>{});
+        default: return call(Large{});
+        }
+    }
+    switch (f) {
+    case 1: return call(SmallNarrow<1>{});
+    case 2: return call(SmallNarrow<2>{});
+    case 3: return call(SmallNarrow<3>{});
+    default: return call(Small{});
+    }
+}
+
+// How the backward pass cuts a layer's rows: some 512 workgroups (two on each CU), each with one tile of dW and an equal share of the rows.
 struct WeightPlan {
-    int tt, n_tiles, k_tiles, range_rows;
-    int64_t ranges;  // upper bound; with groups each may end in a short one
+    bool swapped, large;
+    int a_dim, b_dim, a_tiles, b_tiles, shares;
+    int64_t slots;
     size_t dz_bytes, dz_stride, part_bytes;
 };
 
 WeightPlan plan_weight(const bgl_linear_t *l, int64_t n)
 {
     WeightPlan p;
-    p.tt = l->in_dim > 64 && l->out_dim > 64 ? 4 : 2;
-    const int bo = 32 * p.tt;
-    p.n_tiles = (int)ceil_div(l->out_dim, bo);
-    p.k_tiles = (int)ceil_div(l->in_dim, bo);
-    const int64_t tiles = (int64_t)p.n_tiles * p.k_tiles;
-    int64_t rows = ceil_div(n * tiles, 512);
-    rows = rows < 256 ? 256 : rows > n ? (n > 0 ? n : 1) : rows;
-    p.range_rows = (int)(ceil_div(rows, 64) * 64 > INT32_MAX ? INT32_MAX / 64 * 64 : ceil_div(rows, 64) * 64);
-    p.ranges = n / p.range_rows + (l->num_groups > 0 ? (l->num_groups < n ? l->num_groups : n) : 1);
+    p.swapped = l->in_dim > l->out_dim;
+    p.a_dim = p.swapped ? l->in_dim : l->out_dim;
+    p.b_dim = p.swapped ? l->out_dim : l->in_dim;
+    p.large = p.a_dim > 64;
+    with_cut(p.large, p.b_dim, [&](auto cut) {
+        p.a_tiles = (int)ceil_div(p.a_dim, decltype(cut)::BA);
+        p.b_tiles = (int)ceil_div(p.b_dim, decltype(cut)::BB);
+    });
+    const int64_t most = ceil_div(n > 0 ? n : 1, 4 * kUnit), want = 512 / ((int64_t)p.a_tiles * p.b_tiles);
+    p.shares = (int)(want < 1 ? 1 : want < most ? want : most);
+    p.slots = p.shares + (l->num_groups > 1 ? l->num_groups - 1 : 0);
     const int per = 16 / elem_bytes(l);
     p.dz_stride = round_up(l->out_dim, per);
     p.dz_bytes = l->activation == BGL_ACT_NONE ? 0 : round_up((size_t)n * p.dz_stride * elem_bytes(l), 256);
-    p.part_bytes = (size_t)p.ranges * ((size_t)l->out_dim * l->in_dim + l->out_dim) * sizeof(float);
+    p.part_bytes = (size_t)p.slots * ((size_t)l->out_dim * l->in_dim + l->out_dim) * sizeof(float);
     return p;
 }
 
-template <class T, bool B_OC, int TT>
-void launch_rows_act(const RowsArgs<T> &a, int act, int64_t blocks, hipStream_t st)
-{
-    if constexpr (B_OC) {
-        k_linear_rows<T, B_OC, TT, BGL_ACT_NONE><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a);
-    } else {
-        if (act == BGL_ACT_RELU) k_linear_rows<T, B_OC, TT, BGL_ACT_RELU><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a);
-        else if (act == BGL_ACT_GELU) k_linear_rows<T, B_OC, TT, BGL_ACT_GELU><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a);
-        else if (act == BGL_ACT_SILU) k_linear_rows<T, B_OC, TT, BGL_ACT_SILU><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a);
-        else k_linear_rows<T, B_OC, TT, BGL_ACT_NONE><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a);
-    }
-}
-
-// 128 x 128 tiles where they are enough for the 256 CUs and the width fills one, else 64 x 64.
+// 128 rows to a tile where such tiles are enough for the 256 CUs, else 64.
 template <class T, bool B_OC>
-int launch_rows(RowsArgs<T> &a, int act, hipStream_t st)
+int launch_rows(RowsArgs<T> &a, hipStream_t st)
 {
     const int64_t extra = a.q.groups > 0 ? (a.q.groups + 1 < a.n ? a.q.groups + 1 : a.n) : 1;
-    const bool big = a.N > 64 && ceil_div(a.n, 128) * ceil_div(a.N, 128) >= 256;
-    const int bo = big ? 128 : 64;
-    a.row_tiles = a.n / bo + extra;
-    a.col_tiles = (int)ceil_div(a.N, bo);
-    const int64_t blocks = tile_count(a.row_tiles, a.col_tiles);
+    const bool large = ceil_div(a.n, Large::BA) * ceil_div(a.N, Large::BB) >= 256;
+    int64_t blocks = 0;
+    with_cut(large, a.N, [&](auto cut) {
+        using C = decltype(cut);
+        a.row_tiles = a.n / C::BA + extra;
+        a.col_tiles = (int)ceil_div(a.N, C::BB);
+        blocks = tile_count(a.row_tiles, a.col_tiles);
+        if (blocks <= INT32_MAX) k_linear_rows<T, B_OC, C><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a);
+    });
     if (blocks > INT32_MAX) BGL_FAIL(BGL_EUNSUPPORTED, "%lld rows of width %d need too many workgroups", (long long)a.n, a.N);
-    if (big) launch_rows_act<T, B_OC, 4>(a, act, blocks, st);
-    else launch_rows_act<T, B_OC, 2>(a, act, blocks, st);
     BGL_HIP(hipGetLastError());
     return BGL_OK;
 }
@@ -619,9 +752,9 @@ int forward(const bgl_linear_t *l, int64_t n, const Groups &q, const void *x, in
     a.y = (E *)y, a.saved = (E *)saved;
     a.n = n, a.x_stride = x_stride, a.y_stride = y_stride, a.residual_stride = residual_stride, a.saved_stride = saved_stride;
     a.K = l->in_dim, a.N = l->out_dim;
-    a.residual_mode = l->residual;
+    a.residual_mode = l->residual, a.activation = l->activation;
     a.q = q;
-    return launch_rows<T, false>(a, l->activation, st);
+    return launch_rows<T, false>(a, st);
 }
 
 template <class T>
@@ -630,21 +763,9 @@ int launch_dz(int act, const void *dy, int64_t dy_stride, const void *saved, int
     using E = typename T::elem;
     const int64_t total = n * ceil_div(N, T::VEC), blocks = ceil_div(total, kThreads);
     const dim3 grid((unsigned)(blocks < 8192 ? blocks : 8192)), block(kThreads);
-#define BGL_DZ(ACT) k_linear_dz<T, ACT><<<grid, block, 0, st>>>((const E *)dy, dy_stride, (const E *)saved, saved_stride, (E *)dz, dz_stride, n, N)
-    if (act == BGL_ACT_RELU) BGL_DZ(BGL_ACT_RELU);
-    else if (act == BGL_ACT_GELU) BGL_DZ(BGL_ACT_GELU);
-    else if (act == BGL_ACT_SILU) BGL_DZ(BGL_ACT_SILU);
-    else BGL_DZ(BGL_ACT_NONE);
-#undef BGL_DZ
+    k_linear_dz<T><<<grid, block, 0, st>>>(act, (const E *)dy, dy_stride, (const E *)saved, saved_stride, (E *)dz, dz_stride, n, N);
     BGL_HIP(hipGetLastError());
     return BGL_OK;
-}
-
-template <class T, int TT>
-void launch_dw(const WeightArgs<T> &a, hipStream_t st)
-{
-    const int64_t blocks = tile_count(a.ranges, a.n_tiles * a.k_tiles);
-    k_linear_dw<T, TT><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a);
 }
 
 template <class T>
@@ -669,23 +790,29 @@ int backward(const bgl_linear_t *l, int64_t n, const Groups &q, const void *dy, 
         a.n = n, a.x_stride = dz_stride, a.y_stride = dx_stride;
         a.K = l->out_dim, a.N = l->in_dim;
         a.q = q;
-        BGL_TRY((launch_rows<T, true>(a, BGL_ACT_NONE, st)));
+        BGL_TRY((launch_rows<T, true>(a, st)));
     }
-    if (dweight || dbias) {
-        WeightArgs<T> a{};
-        a.dz = (const E *)dz, a.x = (const E *)x, a.part = reinterpret_cast<float *>((char *)workspace + p.dz_bytes);
-        a.n = n, a.dz_stride = dz_stride, a.x_stride = x_stride, a.ranges = p.ranges;
-        a.N = l->out_dim, a.K = l->in_dim, a.range_rows = p.range_rows, a.n_tiles = p.n_tiles, a.k_tiles = p.k_tiles;
-        a.with_bias = dbias != nullptr;
-        a.q = q;
+    if (dweight) {
+        float *part = reinterpret_cast<float *>((char *)workspace + p.dz_bytes);
         if (n > 0) {
-            if (p.tt == 4) launch_dw<T, 4>(a, st);
-            else launch_dw<T, 2>(a, st);
+            WeightArgs<T> a{};
+            a.a = (const E *)(p.swapped ? x : dz), a.b = (const E *)(p.swapped ? dz : x);
+            a.a_stride = p.swapped ? x_stride : dz_stride, a.b_stride = p.swapped ? dz_stride : x_stride;
+            a.part = part, a.n = n, a.a_dim = p.a_dim, a.b_dim = p.b_dim, a.shares = p.shares, a.a_tiles = p.a_tiles, a.b_tiles = p.b_tiles;
+            a.bias = p.swapped ? 2 : 1;
+            a.q = q;
+            const dim3 grid((unsigned)tile_count(p.shares, p.a_tiles * p.b_tiles)), block(kThreads);
+            with_cut(p.large, p.b_dim, [&](auto cut) {
+                if (q.index) k_linear_dw<T, true, decltype(cut)><<<grid, block, 0, st>>>(a);
+                else k_linear_dw<T, false, decltype(cut)><<<grid, block, 0, st>>>(a);
+            });
             BGL_HIP(hipGetLastError());
         }
-        const int64_t NK = (int64_t)l->out_dim * l->in_dim, len = NK + l->out_dim;
-        k_linear_reduce<T><<<dim3((unsigned)ceil_div(len, 256), (unsigned)classes), dim3(kThreads), 0, st>>>(a.part, n, p.range_rows, NK, l->out_dim, q,
-                                                                                                         (E *)dweight, (E *)dbias);
+        ReduceArgs<T> r{};
+        r.part = part, r.dw = (E *)dweight, r.db = (E *)dbias, r.n = n, r.N = l->out_dim, r.K = l->in_dim, r.shares = p.shares, r.swapped = p.swapped;
+        r.q = q;
+        const int64_t len = (int64_t)l->out_dim * l->in_dim + l->out_dim;
+        k_linear_reduce<T><<<dim3((unsigned)ceil_div(len, 256), (unsigned)classes), dim3(kThreads), 0, st>>>(r);
         BGL_HIP(hipGetLastError());
     }
     return BGL_OK;

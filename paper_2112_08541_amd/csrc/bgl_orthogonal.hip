@@ -45,10 +45,14 @@ __device__ __forceinline__ void split(float v, uint16_t &hi, uint16_t &lo)
     hi = __builtin_bit_cast(uint16_t, h);
     lo = __builtin_bit_cast(uint16_t, (_Float16)(v - (float)h));
 }
-__device__ __forceinline__ float joined(const uint16_t *row, int c)
+// four neighbouring values of a split row, from column c (a multiple of 4)
+__device__ __forceinline__ void joined4(const uint32_t *row, int c, float (&v)[4])
 {
-    const uint16_t *at = row + (c >> 5) * 64 + (c & 31);
-    return (float)__builtin_bit_cast(_Float16, at[0]) + (float)__builtin_bit_cast(_Float16, at[32]);
+    typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+    const uint16_t *at = reinterpret_cast<const uint16_t *>(row) + (c >> 5) * 64 + (c & 31);
+    const f16x4 hi = *reinterpret_cast<const f16x4 *>(at), lo = *reinterpret_cast<const f16x4 *>(at + 32);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (float)hi[e] + (float)lo[e];
 }
 // TT neighbouring values of a split row, from column c (a multiple of TT)
 template <int TT>
@@ -118,7 +122,8 @@ template <int TT, int STAGE, class T>
 __global__ __launch_bounds__(kThreads, 2) void k_ortho_product(OrthoArgs a, int from, int row_tiles, int col_tiles)
 {
     constexpr int BO = 32 * TT;
-    __shared__ __attribute__((aligned(16))) uint32_t lds[2][2][BO * kDwords];
+    using C = Cut<2, 2, TT, TT>;
+    __shared__ __attribute__((aligned(16))) uint32_t lds[BO * BO > 2 * KcOperand<F32, BO>::LDS ? BO * BO : 2 * KcOperand<F32, BO>::LDS];  // both operands; the sums afterwards
     constexpr bool SYMMETRIC = STAGE == GRAM || STAGE == POLY;
     const int tiles = SYMMETRIC ? row_tiles * (row_tiles + 1) / 2 : row_tiles * col_tiles;
     int64_t matrix;
@@ -142,92 +147,97 @@ __global__ __launch_bounds__(kThreads, 2) void k_ortho_product(OrthoArgs a, int 
     const uint32_t *right = STAGE == GRAM ? a.x[from] + mn : STAGE == POLY ? a.p + mm : a.xt[from] + nm;
     const int K = STAGE == GRAM ? a.np : a.mp, cols = SYMMETRIC ? a.m : a.n;
     const int r0 = rt * BO, c0 = ct * BO;
-    KcOperand<F32, BO, TT> l, r;  // (its 32 dwords are 32 pairs of halves here)
+    KcOperand<F32, BO> l, r;  // (its 32 dwords are 32 pairs of halves here)
     l.init([&](int i) { return reinterpret_cast<const float *>(left) + (int64_t)(r0 + i < a.m ? r0 + i : a.m - 1) * K; });
     r.init([&](int i) { return reinterpret_cast<const float *>(right) + (int64_t)(c0 + i < cols ? c0 + i : cols - 1) * K; });
     f32x4 acc[TT][TT] = {};
-    const int wave = threadIdx.x / kWave, a_off = (wave >> 1) * 16 * TT, b_off = (wave & 1) * 16 * TT;
-    l.load(0, K);
-    r.load(0, K);
-    for (int k = 0, i = 0; k < K; k += kDwords, ++i) {
-        l.store(lds[i & 1][0]);
-        r.store(lds[i & 1][1]);
-        __syncthreads();
-        if (k + kDwords < K) {
-            l.load(k + kDwords, K);
-            r.load(k + kDwords, K);
-        }
-        uint32_t ah[TT][4], al[TT][4], bh[TT][4], bl[TT][4];
-        read_kc<BO, TT>(lds[i & 1][0], a_off, 0, ah);
-        read_kc<BO, TT>(lds[i & 1][1], b_off, 0, bh);
-        read_kc<BO, TT>(lds[i & 1][0], a_off, 1, al);
-        read_kc<BO, TT>(lds[i & 1][1], b_off, 1, bl);
-        auto mma = [&](uint32_t(&x)[TT][4], uint32_t(&y)[TT][4]) {
+    using Op = KcOperand<F32, BO>;
+    pipeline(
+        K / kDwords,
+        [&](int i) {
+            l.load_whole(i);
+            r.load_whole(i);
+        },
+        [&] {
+            l.store(lds);
+            r.store(lds + Op::LDS);
+        },
+        [&](int) {
+            uint32_t ah[TT][4], al[TT][4], bh[TT][4], bl[TT][4];
+            Op::read(lds, C::a_off(), 0, ah);
+            Op::read(lds + Op::LDS, C::b_off(), 0, bh);
+            Op::read(lds, C::a_off(), 1, al);
+            Op::read(lds + Op::LDS, C::b_off(), 1, bl);
+            const auto mma = [&](uint32_t(&x)[TT][4], uint32_t(&y)[TT][4]) {
 #pragma unroll
-            for (int s = 0; s < TT; ++s)
+                for (int s = 0; s < TT; ++s)
 #pragma unroll
-                for (int u = 0; u < TT; ++u)
-                    acc[s][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x[s]), __builtin_bit_cast(f16x8, y[u]), acc[s][u], 0, 0, 0);
-        };
-        mma(ah, bh);
-        mma(ah, bl);
-        mma(al, bh);
-    }
-    const int lane = threadIdx.x & 63, c = c0 + b_off + TT * (lane & 15);
+                    for (int u = 0; u < TT; ++u)
+                        acc[s][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x[s]), __builtin_bit_cast(f16x8, y[u]), acc[s][u], 0, 0, 0);
+            };
+            mma(ah, bh);
+            mma(ah, bl);
+            mma(al, bh);
+        });
     const float scale = STAGE == GRAM ? 1.0f / (a.sx * a.sx) : STAGE == POLY ? 1.0f / (a.sp * a.sp) : 1.0f / (a.sq * a.sx);
+    float *sums = reinterpret_cast<float *>(lds);
+    Result<C, BO * BO>::put(sums, 0, acc);
+    __syncthreads();
+    // four columns of a row, then (for the copies in the other order) four rows of a column
+    constexpr int FOURS = BO / 4;
+    if constexpr (SYMMETRIC) {
+        uint32_t *to = (STAGE == GRAM ? a.p : a.q) + mm;
+        for (int i = threadIdx.x; i < BO * FOURS; i += kThreads) {
+            const int r = i / FOURS, c = i % FOURS * 4;
+            if (r0 + r >= a.m || c0 + c >= a.mp) continue;
+            f32x4 *at = reinterpret_cast<f32x4 *>(sums + result_place<BO>(r, c));
+            f32x4 v = *at;
+            float w[4];
+            float p[4] = {};
+            if (STAGE == POLY) joined4(a.p + mm + (int64_t)(r0 + r) * a.mp, c0 + c, p);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int rr = r0 + a_off + TT * (4 * (lane >> 4) + j);  // the lane's TT rows from rr, TT columns from c
-        float v[TT][TT];
-#pragma unroll
-        for (int s = 0; s < TT; ++s)
-#pragma unroll
-            for (int u = 0; u < TT; ++u) v[s][u] = acc[s][u][j] * scale;
-        if constexpr (SYMMETRIC) {
-            uint32_t *to = (STAGE == GRAM ? a.p : a.q) + mm;
-#pragma unroll
-            for (int s = 0; s < TT; ++s)
-#pragma unroll
-                for (int u = 0; u < TT; ++u) {
-                    const bool in = rr + s < a.m && c + u < a.m;
-                    if (STAGE == POLY && in)
-                        v[s][u] = (rr + s == c + u ? a.a : 0.0f) + a.b * (joined(reinterpret_cast<const uint16_t *>(a.p + mm + (int64_t)(rr + s) * a.mp), c + u) / a.sp) + a.c * v[s][u];
-                    v[s][u] = in ? v[s][u] * (STAGE == GRAM ? a.sp : a.sq) : 0.0f;
-                }
-#pragma unroll
-            for (int s = 0; s < TT; ++s)
-                if (rr + s < a.m && c < a.mp) store_split<TT>(to + (int64_t)(rr + s) * a.mp, c, v[s]);
-            if (rt != ct)
-#pragma unroll
-                for (int u = 0; u < TT; ++u) {
-                    float w[TT];
-#pragma unroll
-                    for (int s = 0; s < TT; ++s) w[s] = v[s][u];
-                    if (c + u < a.m && rr < a.mp) store_split<TT>(to + (int64_t)(c + u) * a.mp, rr, w);
-                }
-        } else if constexpr (STAGE == APPLY) {
-#pragma unroll
-            for (int s = 0; s < TT; ++s)
-#pragma unroll
-                for (int u = 0; u < TT; ++u) v[s][u] = rr + s < a.m && c + u < a.n ? v[s][u] * a.sx : 0.0f;
-#pragma unroll
-            for (int s = 0; s < TT; ++s)
-                if (rr + s < a.m && c < a.np) store_split<TT>(a.x[from ^ 1] + mn + (int64_t)(rr + s) * a.np, c, v[s]);
-#pragma unroll
-            for (int u = 0; u < TT; ++u) {
-                float w[TT];
-#pragma unroll
-                for (int s = 0; s < TT; ++s) w[s] = v[s][u];
-                if (c + u < a.n && rr < a.mp) store_split<TT>(a.xt[from ^ 1] + nm + (int64_t)(c + u) * a.mp, rr, w);
+            for (int e = 0; e < 4; ++e) {
+                v[e] *= scale;
+                if (STAGE == POLY) v[e] = (r0 + r == c0 + c + e ? a.a : 0.0f) + a.b * (p[e] / a.sp) + a.c * v[e];
+                v[e] = w[e] = c0 + c + e < a.m ? v[e] * (STAGE == GRAM ? a.sp : a.sq) : 0.0f;
             }
-        } else {
-            typename T::elem *out = (typename T::elem *)a.out + matrix * a.out_matrix;
+            if (rt != ct) *at = v;
+            store_split<4>(to + (int64_t)(r0 + r) * a.mp, c0 + c, w);
+        }
+        if (rt == ct) return;
+        __syncthreads();
+        for (int i = threadIdx.x; i < BO * FOURS; i += kThreads) {  // (the columns are whole here: ct < rt)
+            const int c = i % BO, r = i / BO * 4;
+            if (r0 + r >= a.mp) continue;
+            float w[4];
 #pragma unroll
-            for (int s = 0; s < TT; ++s)
+            for (int e = 0; e < 4; ++e) w[e] = r0 + r + e < a.m ? sums[result_place<BO>(r + e, c)] : 0.0f;
+            store_split<4>(to + (int64_t)(c0 + c) * a.mp, r0 + r, w);
+        }
+    } else if constexpr (STAGE == APPLY) {
+        for (int i = threadIdx.x; i < BO * FOURS; i += kThreads) {
+            const int r = i / FOURS, c = i % FOURS * 4;
+            if (r0 + r >= a.m || c0 + c >= a.np) continue;
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(sums + result_place<BO>(r, c));
+            float w[4];
 #pragma unroll
-                for (int u = 0; u < TT; ++u)
-                    if (rr + s < a.m && c + u < a.n)
-                        out[a.tall ? (int64_t)(c + u) * a.out_row + rr + s : (int64_t)(rr + s) * a.out_row + c + u] = T::put(v[s][u]);
+            for (int e = 0; e < 4; ++e) w[e] = c0 + c + e < a.n ? v[e] * scale * a.sx : 0.0f;
+            store_split<4>(a.x[from ^ 1] + mn + (int64_t)(r0 + r) * a.np, c0 + c, w);
+        }
+        for (int i = threadIdx.x; i < BO * FOURS; i += kThreads) {
+            const int c = i % BO, r = i / BO * 4;
+            if (c0 + c >= a.n || r0 + r >= a.mp) continue;
+            float w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = r0 + r + e < a.m ? sums[result_place<BO>(r + e, c)] * scale * a.sx : 0.0f;
+            store_split<4>(a.xt[from ^ 1] + nm + (int64_t)(c0 + c) * a.mp, r0 + r, w);
+        }
+    } else {
+        typename T::elem *out = (typename T::elem *)a.out + matrix * a.out_matrix;
+        for (int i = threadIdx.x; i < BO * BO; i += kThreads) {
+            const int r = a.tall ? i % BO : i / BO, c = a.tall ? i / BO : i % BO;
+            if (r0 + r < a.m && c0 + c < a.n)
+                out[a.tall ? (int64_t)(c0 + c) * a.out_row + r0 + r : (int64_t)(r0 + r) * a.out_row + c0 + c] = T::put(sums[result_place<BO>(r, c)] * scale);
         }
     }
 }

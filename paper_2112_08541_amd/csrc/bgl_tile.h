@@ -2,15 +2,14 @@
 // registers into LDS and from there as fragments of 16 x 16 MFMA instructions.  Shared by the layers and the orthogonalised updates.
 //
 // A tile of an operand is BO rows (the index that survives the product) by 32 dwords of the summed index: 32 values of fp32, 64 of
-// bf16.  Operands come in two orders:
-//   summed index contiguous (Kc)    LDS [BO][32 dwords] of 16-byte chunks; chunk c of row r lies at c ^ ((r / T) & 7), so that the 8
-//                                   lanes a 16-byte read serves at a time, whose rows are T apart, meet all banks
-//   kept index contiguous (Oc)      LDS [32 dwords][BO]: a dword is one value (fp32), or the values of two neighbouring summed indices
-//                                   (bf16), paired in registers on the way from global memory
-// A wavefront computes T x T fragments of 16 x 16.  Fragment t holds rows T * i + t (not 16 * t + i): a lane's T fragments then are T
-// neighbouring rows, which makes an Oc read one 4T-byte load, and its T accumulators T neighbouring columns of the result.
+// bf16 (BK).  Operands come in two orders:
+//   summed index contiguous (Kc)    LDS [BO][32 dwords] of 16-byte chunks; chunk c of row r lies at c ^ (r & 7), so that the 8 lanes a
+//                                   16-byte read serves at a time, each with a row of its own, meet all banks
+//   kept index contiguous (Oc)      LDS [BK][BO], blocks of 16 columns moved about within a row so that the rows a read meets lie in
+//                                   different banks.  fp32 fragments are read value by value; bf16 fragments, which need neighbouring summed
+//                                   indices in a register, by the LDS read that transposes 4 x 16 values among 16 lanes
 // Which summed index sits in which lane is free as long as both operands agree: lane group g = lane / 16 has dwords 4g .. 4g+3 of
-// each 16.  Loads need no alignment beyond the element's (global memory takes unaligned vector accesses).
+// each 16 (8 values of bf16, 4 of fp32).  Loads need no alignment beyond the element's (global memory takes unaligned vector accesses).
 #pragma once
 
 #include "bgl_internal.h"
@@ -20,6 +19,7 @@ namespace tile {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 constexpr int kDwords = 32;  // of the summed index per tile
@@ -49,6 +49,22 @@ struct BF16 {
     }
 };
 
+// A workgroup of WA x WB wavefronts, each with FA x FB fragments.
+template <int WA, int WB, int FA_, int FB_>
+struct Cut {
+    static_assert(WA * WB * kWave == kThreads, "");
+    static constexpr int FA = FA_, FB = FB_, BA = 16 * WA * FA, BB = 16 * WB * FB;
+    static __device__ __forceinline__ int a_off() { return (int)(threadIdx.x / kWave) / WB * 16 * FA; }
+    static __device__ __forceinline__ int b_off() { return (int)(threadIdx.x / kWave) % WB * 16 * FB; }
+};
+
+constexpr int up_to_power(int x)
+{
+    int p = 16;
+    while (p < x) p *= 2;
+    return p;
+}
+
 template <class V>
 __device__ __forceinline__ V load_any(const void *p)
 {
@@ -57,28 +73,45 @@ __device__ __forceinline__ V load_any(const void *p)
     return v;
 }
 
-// Values [0, left) of up to 16 bytes, the others zero.
+// The values of 16 bytes moved `by` places towards the first, zeros behind them; nothing is left of them from VEC places on.
 template <class T>
-__device__ __forceinline__ uint4 load_part(const typename T::elem *p, int left)
+__device__ __forceinline__ uint4 move_down(const uint4 &v, int by)
 {
+    const int bits = by * (32 / T::PER);
+    uint32_t d[5] = {v.x, v.y, v.z, v.w, 0};
+    if constexpr (T::PER == 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[i] = __builtin_amdgcn_alignbit(d[i + 1], d[i], bits & 31);
+    }
+    const bool one = bits & 32, two = bits & 64, none = bits >= 128;
+    uint32_t e[4] = {one ? d[1] : d[0], one ? d[2] : d[1], one ? d[3] : d[2], one ? 0 : d[3]};
+    return uint4{none ? 0 : two ? e[2] : e[0], none ? 0 : two ? e[3] : e[1], none || two ? 0 : e[2], none || two ? 0 : e[3]};
+}
+
+// The first `left` values at p (any number: none for left <= 0, at most VEC), zeros behind them, for a row of `width` values whose end is
+// p + left: one load that ends where the row does.  Rows shorter than 16 bytes are read value by value.
+template <class T>
+__device__ __forceinline__ uint4 load_end(const typename T::elem *p, int left, int width)
+{
+    if (width >= T::VEC) {
+        const int back = left >= T::VEC ? 0 : T::VEC - left;
+        return move_down<T>(load_any<uint4>(p - back), back);
+    }
     typename T::elem v[T::VEC];
 #pragma unroll
     for (int e = 0; e < T::VEC; ++e) v[e] = e < left ? p[e] : (typename T::elem)0;
     return __builtin_bit_cast(uint4, v);
 }
 
-template <class T>
-__device__ __forceinline__ uint4 load_upto(const typename T::elem *p, int left)
-{
-    if (left >= T::VEC) return load_any<uint4>(p);
-    return left > 0 ? load_part<T>(p, left) : uint4{0, 0, 0, 0};
-}
+// Both operands keep the next tile on its way in registers while the present one is multiplied out of LDS.  Loads of whole tiles have no
+// branch among them: with branches every load waits for those before it.
 
 // A Kc operand: the thread brings chunk (tid & 7) of rows (tid >> 3) + 32 * pass.
-template <class T, int BO, int TT>
+template <class T, int BO>
 struct KcOperand {
-    static constexpr int PASSES = BO / 32;
+    static constexpr int PASSES = (BO + 31) / 32;
     static constexpr int BK = kDwords * T::PER;
+    static constexpr int LDS = PASSES * 32 * kDwords;  // dwords
     const typename T::elem *at[PASSES];
     uint4 reg[PASSES];
 
@@ -89,151 +122,231 @@ struct KcOperand {
 #pragma unroll
         for (int p = 0; p < PASSES; ++p) at[p] = row((int)(threadIdx.x >> 3) + 32 * p) + (threadIdx.x & 7) * T::VEC;
     }
-    __device__ __forceinline__ void load(int k0, int K)
+    __device__ __forceinline__ void load_whole(int tile)
     {
-        if (k0 + BK <= K) {
 #pragma unroll
-            for (int p = 0; p < PASSES; ++p) reg[p] = load_any<uint4>(at[p] + k0);
-        } else {
-            const int left = K - k0 - (int)(threadIdx.x & 7) * T::VEC;
+        for (int p = 0; p < PASSES; ++p) reg[p] = load_any<uint4>(at[p] + tile * BK);
+    }
+    __device__ __forceinline__ void load(int tile, int K)
+    {
+        if ((tile + 1) * BK <= K) return load_whole(tile);
+        const int left = K - tile * BK - (int)(threadIdx.x & 7) * T::VEC;
 #pragma unroll
-            for (int p = 0; p < PASSES; ++p) reg[p] = load_upto<T>(at[p] + k0, left);
-        }
+        for (int p = 0; p < PASSES; ++p) reg[p] = load_end<T>(at[p] + tile * BK, left, K);
     }
     __device__ __forceinline__ void store(uint32_t *lds) const
     {
 #pragma unroll
         for (int p = 0; p < PASSES; ++p) {
             const int r = (threadIdx.x >> 3) + 32 * p, c = threadIdx.x & 7;
-            *reinterpret_cast<uint4 *>(lds + r * kDwords + ((c ^ ((r / TT) & 7)) << 2)) = reg[p];
+            *reinterpret_cast<uint4 *>(lds + r * kDwords + ((c ^ (r & 7)) << 2)) = reg[p];
+        }
+    }
+    // F fragments of rows from `off`, 16 dwords of the summed index from 16 * step
+    template <int F>
+    static __device__ __forceinline__ void read(const uint32_t *lds, int off, int step, uint32_t (&f)[F][4])
+    {
+        const int l = threadIdx.x & 63;
+        const uint32_t *from = lds + (off + (l & 15)) * kDwords + (((step * 4 + (l >> 4)) ^ (l & 7)) << 2);
+#pragma unroll
+        for (int t = 0; t < F; ++t) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(from + t * 16 * kDwords);
+            f[t][0] = v.x, f[t][1] = v.y, f[t][2] = v.z, f[t][3] = v.w;
         }
     }
 };
 
-// An Oc operand: values (k, o) at base + row(k) * stride + o, k counted in the tile's range of `count` summed rows.
-template <class T, int BO, int TT>
+// An Oc operand: values (k, o) at base + row(k) * stride + o, k counted in a range of `count` > 0 summed rows.  LIST: row(k) = rows[k], and
+// numbers outside [0, total) have no row; else row(k) = first + k.  Rows outside are read from one that exists and zeroed on the way to
+// LDS; columns that do not exist hold anything (they make columns of the result that are not stored).
+template <class T, int BO, bool LIST>
 struct OcOperand {
+    using type = T;
+    static constexpr int BOUND = BO;
     static constexpr int BK = kDwords * T::PER;
-    static constexpr int PER_ROW = BO / T::VEC;              // threads a row takes
-    static constexpr int ROWS = kThreads / PER_ROW;          // dword rows a pass takes
-    static constexpr int PASSES = kDwords / ROWS;
-    const typename T::elem *base;  // of the thread's first value
-    int64_t stride;
-    const int32_t *rows;           // of the range's first row, or null: rows first, first + 1, ...
-    int64_t first, total;
-    int64_t count;
-    int left;                      // values from the thread's first one to the row's end
-    int32_t next[PASSES][T::PER];  // row numbers of the tile that is loaded next, -1 for none
-    uint4 reg[PASSES][T::PER];
+    static constexpr int W = up_to_power(BO);        // columns of a row in LDS
+    static constexpr int LDS = kDwords * W;          // dwords
+    static constexpr int PER_ROW = W / T::VEC;       // threads a row takes
+    static constexpr int ROWS = kThreads / PER_ROW;  // rows a pass takes
+    static constexpr int PASSES = ROWS < BK ? BK / ROWS : 1;
+    static constexpr int ALL = (1 << PASSES) - 1;
+    const typename T::elem *base;  // of the thread's first value (of its chunk, moved back so that it ends with the row)
+    uint32_t stride;
+    const int32_t *rows;           // of the range's first row
+    int32_t first, total, count;
+    int back;                      // how far base was moved; VEC where the thread has no columns
+    bool ends;                     // a chunk of the tile is cut by the row's end
+    bool narrow;                   // rows shorter than 16 bytes
+    uint32_t next[PASSES];         // row numbers of the tile that is loaded next
+    int live_next, live;           // which of them (of those in reg) exist, one bit each
+    uint4 reg[PASSES];
 
     __device__ __forceinline__ int kk(int pass) const { return (int)threadIdx.x / PER_ROW + ROWS * pass; }
-    __device__ __forceinline__ void init(const typename T::elem *p, int64_t ld, const int32_t *index, int64_t from, int64_t n, int64_t of, int o0, int O)
+    __device__ __forceinline__ bool idle() const { return ROWS > BK && kk(0) >= BK; }
+    __device__ __forceinline__ void init(const typename T::elem *p, int64_t ld, int64_t of, int o0, int O)
     {
-        const int o = o0 + (int)(threadIdx.x % PER_ROW) * T::VEC;
-        left = O - o;
-        base = p + (left > 0 ? o : 0);
-        stride = ld;
-        rows = index ? index + from : nullptr;
-        first = from;
+        const int o = o0 + (int)(threadIdx.x % PER_ROW) * T::VEC, left = O - o;
+        narrow = O < T::VEC;
+        ends = o0 + W > O && O % T::VEC != 0;
+        back = left >= T::VEC ? 0 : left > 0 ? T::VEC - left : T::VEC;
+        base = p + (narrow ? 0 : left > 0 ? o - back : 0);
+        stride = (uint32_t)ld;
+        total = (int32_t)of;
+    }
+    // The range of summed rows: from position `from` of the row order, n of them.
+    __device__ __forceinline__ void range(const int32_t *index, int64_t from, int n)
+    {
+        rows = index + from;
+        first = (int32_t)from;
         count = n;
-        total = of;
         seek(0);
     }
-    __device__ __forceinline__ void seek(int64_t k0)
+    __device__ __forceinline__ void seek(int tile)
     {
+        live_next = 0;
 #pragma unroll
-        for (int p = 0; p < PASSES; ++p)
-#pragma unroll
-            for (int h = 0; h < T::PER; ++h) {
-                const int64_t k = k0 + kk(p) * T::PER + h;
-                int32_t r = -1;
-                if (k < count) {
-                    r = rows ? rows[k] : (int32_t)(first + k);
-                    if ((uint32_t)r >= (uint64_t)total) r = -1;
-                }
-                next[p][h] = r;
-            }
+        for (int p = 0; p < PASSES; ++p) {
+            const int k = tile * BK + kk(p);
+            const int at = k < count ? k : count - 1;
+            const int32_t r = LIST ? rows[at] : first + at;
+            const bool named = !LIST || (uint32_t)r < (uint32_t)total;
+            next[p] = named ? r : 0;
+            live_next |= (int)(named && k < count) << p;
+        }
     }
-    __device__ __forceinline__ void load(int64_t k0)
+    __device__ __forceinline__ void load(int tile)
     {
+        uint32_t now[PASSES];
 #pragma unroll
-        for (int p = 0; p < PASSES; ++p)
+        for (int p = 0; p < PASSES; ++p) now[p] = next[p];
+        live = live_next;
+        seek(tile + 1);  // before the loads: waiting for these numbers then waits for no later load
+        if (idle()) return;
+        if (!narrow) {
 #pragma unroll
-            for (int h = 0; h < T::PER; ++h) {
-                const int32_t r = next[p][h];
-                reg[p][h] = r >= 0 ? load_upto<T>(base + r * stride, left) : uint4{0, 0, 0, 0};
-            }
-        seek(k0 + BK);
+            for (int p = 0; p < PASSES; ++p) reg[p] = load_any<uint4>(base + (uint64_t)now[p] * stride);
+        } else {
+#pragma unroll
+            for (int p = 0; p < PASSES; ++p) reg[p] = load_end<T>(base + (uint64_t)now[p] * stride, T::VEC - back, 0);
+        }
+    }
+    // Zeroes rows that do not exist and puts cut chunks in place; once for each loaded tile, before store().
+    __device__ __forceinline__ void settle()
+    {
+        if (!ends && __all(live == ALL)) return;
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) reg[p] = move_down<T>(reg[p], !(live >> p & 1) ? T::VEC : narrow ? 0 : back);
+    }
+    // where column c of row k lies, in values from the tile's start
+    static __device__ __forceinline__ int place(int k, int c)
+    {
+        constexpr int BLOCKS = W / 16;
+        int move;
+        if constexpr (T::PER == 1) {
+            return k * W + ((c + 16 * (k >> 2)) & (W - 1));
+        } else {
+            if constexpr (BLOCKS == 8) move = (k & 3) | (k >> 3 & 1) << 2;
+            else if constexpr (BLOCKS == 4) move = (k >> 1 & 1) | (k >> 3 & 1) << 1;
+            else if constexpr (BLOCKS == 2) move = k >> 3 & 1;
+            else move = 0;
+            return k * W + (((c >> 4) ^ move) << 4 | (c & 15));
+        }
     }
     __device__ __forceinline__ void store(uint32_t *lds) const
     {
+        if (idle()) return;
+        typename T::elem *to = reinterpret_cast<typename T::elem *>(lds);
 #pragma unroll
-        for (int p = 0; p < PASSES; ++p) {
-            uint32_t *to = lds + kk(p) * BO + (threadIdx.x % PER_ROW) * T::VEC;
-            if constexpr (T::PER == 1) {
-                *reinterpret_cast<uint4 *>(to) = reg[p][0];
-            } else {
-                const uint32_t lo[4] = {reg[p][0].x, reg[p][0].y, reg[p][0].z, reg[p][0].w};
-                const uint32_t hi[4] = {reg[p][1].x, reg[p][1].y, reg[p][1].z, reg[p][1].w};
-                uint32_t out[8];
+        for (int p = 0; p < PASSES; ++p) *reinterpret_cast<uint4 *>(to + place(kk(p), (int)(threadIdx.x % PER_ROW) * T::VEC)) = reg[p];
+    }
+    template <int F>
+    static __device__ __forceinline__ void read(const uint32_t *lds, int off, int step, uint32_t (&f)[F][4])
+    {
+        const int l = threadIdx.x & 63, i = l & 15, g = l >> 4;
+        if constexpr (T::PER == 1) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    out[2 * i] = __builtin_amdgcn_perm(hi[i], lo[i], 0x05040100);      // low halves of (lo, hi)
-                    out[2 * i + 1] = __builtin_amdgcn_perm(hi[i], lo[i], 0x07060302);  // high halves
+            for (int t = 0; t < F; ++t)
+#pragma unroll
+                for (int p = 0; p < 4; ++p) f[t][p] = lds[place(step * 16 + 4 * g, off + 16 * t + i) + p * W];
+        } else {
+            // lane (i / 4, i % 4) of 16 names columns 4 (i % 4) .. +3 of row i / 4, and gets column i of the four rows
+#pragma unroll
+            for (int t = 0; t < F; ++t) {
+                const uint16_t *from = reinterpret_cast<const uint16_t *>(lds) + place(step * 32 + 8 * g + (i >> 2), off + 16 * t + 4 * (i & 3));
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const auto at = (__attribute__((address_space(3))) s16x4 *)(uint16_t *)(from + 4 * h * W);
+                    const uint2 v = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(at));
+                    f[t][2 * h] = v.x, f[t][2 * h + 1] = v.y;
                 }
-                *reinterpret_cast<uint4 *>(to) = uint4{out[0], out[1], out[2], out[3]};
-                *reinterpret_cast<uint4 *>(to + 4) = uint4{out[4], out[5], out[6], out[7]};
             }
         }
     }
 };
 
-// The T fragments of a wavefront whose rows start at `off`, 16 dwords of the summed index from 16 * step.
-template <int BO, int TT>
-__device__ __forceinline__ void read_kc(const uint32_t *lds, int off, int step, uint32_t (&f)[TT][4])
+// The tiles of one product: load(tile) into registers, store() from there to LDS, compute(tile) out of LDS.  One LDS buffer and two
+// barriers a tile: the room a second buffer would take holds another workgroup, which fills the waits of this one.
+template <class Load, class Store, class Compute>
+__device__ __forceinline__ void pipeline(int tiles, Load load, Store store, Compute compute)
 {
-    const int l = threadIdx.x & 63;
-    const uint32_t *from = lds + (off + TT * (l & 15)) * kDwords + (((step * 4 + (l >> 4)) ^ (l & 7)) << 2);
-#pragma unroll
-    for (int t = 0; t < TT; ++t) {
-        const uint4 v = *reinterpret_cast<const uint4 *>(from + t * kDwords);
-        f[t][0] = v.x, f[t][1] = v.y, f[t][2] = v.z, f[t][3] = v.w;
-    }
-}
-template <int BO, int TT>
-__device__ __forceinline__ void read_oc(const uint32_t *lds, int off, int step, uint32_t (&f)[TT][4])
-{
-    const int l = threadIdx.x & 63;
-    const uint32_t *from = lds + (step * 16 + 4 * (l >> 4)) * BO + off + TT * (l & 15);
-#pragma unroll
-    for (int p = 0; p < 4; ++p) {
-        if constexpr (TT == 4) {
-            const uint4 v = *reinterpret_cast<const uint4 *>(from + p * BO);
-            f[0][p] = v.x, f[1][p] = v.y, f[2][p] = v.z, f[3][p] = v.w;
-        } else {
-            static_assert(TT == 2, "");
-            const uint2 v = *reinterpret_cast<const uint2 *>(from + p * BO);
-            f[0][p] = v.x, f[1][p] = v.y;
-        }
+    if (tiles <= 0) return;
+    load(0);
+    for (int i = 0; i < tiles; ++i) {
+        store();
+        __syncthreads();
+        if (i + 1 < tiles) load(i + 1);
+        compute(i);
+        __syncthreads();
     }
 }
 
 // One tile of both operands into the accumulators; `steps` of 16 dwords hold values.
-template <class T, bool A_OC, bool B_OC, int BO, int TT>
-__device__ __forceinline__ void multiply(const uint32_t *a_lds, const uint32_t *b_lds, int a_off, int b_off, int steps, f32x4 (&acc)[TT][TT])
+template <class T, class A, class B, class C>
+__device__ __forceinline__ void multiply(const uint32_t *a_lds, const uint32_t *b_lds, int steps, f32x4 (&acc)[C::FA][C::FB])
 {
+    const auto products = [&](const uint32_t(&a)[C::FA][4], const uint32_t(&b)[C::FB][4]) {
 #pragma unroll
-    for (int s = 0; s < kDwords / 16; ++s) {
-        if (s >= steps) break;
-        uint32_t a[TT][4], b[TT][4];
-        if constexpr (A_OC) read_oc<BO, TT>(a_lds, a_off, s, a); else read_kc<BO, TT>(a_lds, a_off, s, a);
-        if constexpr (B_OC) read_oc<BO, TT>(b_lds, b_off, s, b); else read_kc<BO, TT>(b_lds, b_off, s, b);
+        for (int i = 0; i < C::FA; ++i)
 #pragma unroll
-        for (int i = 0; i < TT; ++i)
+            for (int j = 0; j < C::FB; ++j) acc[i][j] = T::mma(a[i], b[j], acc[i][j]);
+    };
 #pragma unroll
-            for (int j = 0; j < TT; ++j) acc[i][j] = T::mma(a[i], b[j], acc[i][j]);
+    for (int step = 0; step < 2; ++step) {
+        if (step >= steps) break;
+        uint32_t a[C::FA][4], b[C::FB][4];
+        A::read(a_lds, C::a_off(), step, a);
+        B::read(b_lds, C::b_off(), step, b);
+        products(a, b);
     }
 }
+
+// A lane's accumulators: row 4 * (lane / 16) + j of a fragment's 16, column lane % 16.  Through LDS they become rows that threads read
+// in pieces of 4 columns or more: fp32, blocks of 16 columns moved on by a block for every 4 rows.  Fragments go there FH of FA at a time
+// (WA * 16 * FH rows of the tile): as many as the operands' LDS has room for.
+template <int W>
+__device__ __forceinline__ int result_place(int r, int c) { return r * W + ((c + 16 * (r >> 2)) & (W - 1)); }
+
+template <class C, int LDS>
+struct Result {
+    static constexpr int W = up_to_power(C::BB), WA = C::BA / 16 / C::FA;
+    static constexpr int fit(int fh) { return fh == 1 || (C::FA % fh == 0 && WA * 16 * fh * W <= LDS) ? fh : fit(fh - 1); }
+    static constexpr int FH = fit(C::FA), PARTS = C::FA / FH, ROWS = WA * 16 * FH, SIZE = ROWS * W;
+    // the tile's row that row r of a part is
+    static __device__ __forceinline__ int row(int part, int r) { return r / (16 * FH) * 16 * C::FA + part * 16 * FH + r % (16 * FH); }
+    static __device__ __forceinline__ void put(float *lds, int part, const f32x4 (&acc)[C::FA][C::FB])
+    {
+        const int l = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < C::FA; ++i) {
+            if (i / FH != part) continue;
+#pragma unroll
+            for (int t = 0; t < C::FB; ++t)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    lds[result_place<W>(C::a_off() / C::FA * FH + 16 * (i % FH) + 4 * (l >> 4) + j, C::b_off() + 16 * t + (l & 15))] = acc[i][t][j];
+        }
+    }
+};
 
 // Work is dealt to workgroups in an order that keeps the tiles of one row block, which read the same rows, on one XCD (workgroup
 // numbers go round the eight XCDs).
