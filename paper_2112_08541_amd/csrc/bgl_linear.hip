@@ -39,29 +39,54 @@ __device__ __forceinline__ float normal_cdf(float z, float &bell)
     return z < 0.0f ? tail : 1.0f - tail;
 }
 
-__device__ __forceinline__ float activate(int act, float z)
+template <int ACT>
+__device__ __forceinline__ float activate(float z)
 {
-    if (act == BGL_ACT_RELU) return z < 0.0f ? 0.0f : z;  // (NaN stays)
-    if (act == BGL_ACT_GELU) {
+    if constexpr (ACT == BGL_ACT_RELU) return z < 0.0f ? 0.0f : z;  // (NaN stays)
+    if constexpr (ACT == BGL_ACT_GELU) {
         float bell;
         return z * normal_cdf(z, bell);
     }
-    if (act == BGL_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + exp_fast(-z));
+    if constexpr (ACT == BGL_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + exp_fast(-z));
     return z;
 }
-__device__ __forceinline__ float slope(int act, float z)
+template <int ACT>
+__device__ __forceinline__ float slope(float z)
 {
-    if (act == BGL_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
-    if (act == BGL_ACT_GELU) {
+    if constexpr (ACT == BGL_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
+    if constexpr (ACT == BGL_ACT_GELU) {
         float bell;
         const float p = normal_cdf(z, bell);
         return fmaf(z * bell, 0.39894228040143268f, p);
     }
-    if (act == BGL_ACT_SILU) {
+    if constexpr (ACT == BGL_ACT_SILU) {
         const float p = __builtin_amdgcn_rcpf(1.0f + exp_fast(-z));
         return p * fmaf(z, 1.0f - p, 1.0f);
     }
     return 1.0f;
+}
+// One choice for several values: one for each kept their chains apart.
+template <int V>
+__device__ __forceinline__ void activate_all(int act, float (&v)[V])
+{
+    const auto all = [&](auto which) {
+#pragma unroll
+        for (int u = 0; u < V; ++u) v[u] = activate<decltype(which)::value>(v[u]);
+    };
+    if (act == BGL_ACT_RELU) all(std::integral_constant<int, BGL_ACT_RELU>{});
+    else if (act == BGL_ACT_GELU) all(std::integral_constant<int, BGL_ACT_GELU>{});
+    else if (act == BGL_ACT_SILU) all(std::integral_constant<int, BGL_ACT_SILU>{});
+}
+template <int V>
+__device__ __forceinline__ void times_slope(int act, const float (&z)[V], float (&d)[V])
+{
+    const auto all = [&](auto which) {
+#pragma unroll
+        for (int u = 0; u < V; ++u) d[u] *= slope<decltype(which)::value>(z[u]);
+    };
+    if (act == BGL_ACT_RELU) all(std::integral_constant<int, BGL_ACT_RELU>{});
+    else if (act == BGL_ACT_GELU) all(std::integral_constant<int, BGL_ACT_GELU>{});
+    else if (act == BGL_ACT_SILU) all(std::integral_constant<int, BGL_ACT_SILU>{});
 }
 
 // ----------------------------------------------------------------- groups
@@ -79,6 +104,9 @@ __device__ __forceinline__ void group_range(const Groups &q, int64_t n, int g, i
     lo = lo < 0 ? 0 : lo > n ? n : lo;  // (offsets are device data: no value of theirs leads outside)
     hi = hi < lo ? lo : hi > n ? n : hi;
 }
+
+// A value that is the same in all lanes, said so: loops and branches that depend on it then need no lane masks.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 struct Span {
     int group;      // -1: there is no such tile
@@ -106,15 +134,14 @@ __device__ __forceinline__ Span find_span(const Groups &q, int64_t n, int classe
         const uint64_t past = __ballot(before + upto > t);
         if (past) {
             const int k = __ffsll((unsigned long long)past) - 1;
-            const int64_t first = before + __shfl(upto - tiles, k);
-            const int64_t from = __shfl((int)lo, k) + (t - first) * tile_rows;
-            const int64_t left = __shfl((int)hi, k) - from;
-            s.group = __builtin_amdgcn_readfirstlane(g0 + k);
-            s.start = __builtin_amdgcn_readfirstlane((int)from);
-            s.count = __builtin_amdgcn_readfirstlane((int)(left < tile_rows ? left : tile_rows));
+            const int64_t first = before + uniform(__shfl(upto - tiles, k));
+            s.group = g0 + k;
+            s.start = uniform(__shfl((int)lo, k)) + (t - first) * tile_rows;
+            const int64_t left = uniform(__shfl((int)hi, k)) - s.start;
+            s.count = (int)(left < tile_rows ? left : tile_rows);
             return s;
         }
-        before += __shfl(upto, 63);
+        before += uniform(__shfl(upto, 63));
     }
     return s;
 }
@@ -136,10 +163,10 @@ __device__ __forceinline__ void count_units(const Groups &q, int64_t n, int unit
         const int units = (int)((hi - lo + unit_rows - 1) / unit_rows);
         const int upto = wave_incl_scan(units);
         if (g >= g0 && g < g0 + 64) {
-            own = __shfl(units, g - g0);
-            before = all + __shfl(upto, g - g0) - own;
+            own = uniform(__shfl(units, g - g0));
+            before = all + uniform(__shfl(upto, g - g0)) - own;
         }
-        all += __shfl(upto, 63);
+        all += uniform(__shfl(upto, 63));
     }
 }
 
@@ -237,10 +264,7 @@ __device__ __forceinline__ void finish_rows(const RowsArgs<T> &a, const float *s
             }
             if (row[p] < 0) continue;
             if (a.saved) store_cols<T, V>(a.saved + row[p] * a.saved_stride + n0 + c, WHOLE ? V : left, v);
-            if (a.activation) {
-#pragma unroll
-                for (int u = 0; u < V; ++u) v[u] = activate(a.activation, v[u]);
-            }
+            activate_all(a.activation, v);
             if (a.residual_mode == BGL_RESIDUAL_AFTER) {
 #pragma unroll
                 for (int u = 0; u < V; ++u) v[u] += T::get(res[p].e[u]);
@@ -250,11 +274,11 @@ __device__ __forceinline__ void finish_rows(const RowsArgs<T> &a, const float *s
     }
 }
 
-template <class T, bool B_OC, class C>
+template <class T, bool B_OC, class C, bool NARROW>
 __global__ __launch_bounds__(kThreads, 2) void k_linear_rows(RowsArgs<T> a)
 {
     using A = KcOperand<T, C::BA>;
-    using B = std::conditional_t<B_OC, OcOperand<T, C::BB, false>, KcOperand<T, C::BB>>;
+    using B = std::conditional_t<B_OC, OcOperand<T, C::BB, false, NARROW>, KcOperand<T, C::BB>>;
     using R = Result<C, A::LDS + B::LDS>;
     constexpr int LDS = A::LDS + B::LDS > R::SIZE ? A::LDS + B::LDS : R::SIZE;
     __shared__ __attribute__((aligned(16))) uint32_t lds[LDS];
@@ -298,7 +322,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_linear_rows(RowsArgs<T> a)
             },
             [&](int i) {
                 const int steps = (K - i * A::BK + 16 * T::PER - 1) / (16 * T::PER);
-                multiply<T, A, B, C>(lds, lds + A::LDS, steps, acc);
+                multiply<T, A, B, C>(lds, lds + A::LDS, steps, acc, [](const auto &, const auto &) {});
             });
     }
     float *sums = reinterpret_cast<float *>(lds);
@@ -327,8 +351,7 @@ __global__ __launch_bounds__(kThreads) void k_linear_dz(int act, const typename 
         load_cols<T, V>(dy + r * dy_stride + c, left, d);
         if (act) {
             load_cols<T, V>(saved + r * saved_stride + c, left, z);
-#pragma unroll
-            for (int e = 0; e < V; ++e) d[e] *= slope(act, z[e]);
+            times_slope(act, z, d);
         }
         store_cols<T, V>(dz + r * dz_stride + c, left, d);
     }
@@ -351,38 +374,13 @@ struct WeightArgs {
     Groups q;
 };
 
-template <class Op, int V>
-__device__ __forceinline__ void add_rows(const Op &op, float (&sum)[V])
-{
-    if (op.idle()) return;
-#pragma unroll
-    for (int p = 0; p < Op::PASSES; ++p) {
-        const auto v = __builtin_bit_cast(Cols<typename Op::type, V>, op.reg[p]);
-#pragma unroll
-        for (int e = 0; e < V; ++e) sum[e] += Op::type::get(v.e[e]);
-    }
-}
-// The threads' column sums, those of one column in order.
-template <class Op, int V>
-__device__ __forceinline__ void put_sums(const Op &op, float *lds, const float (&sum)[V], float *to, int o0, int O)
-{
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < V; ++e) lds[threadIdx.x * V + e] = op.idle() ? 0.0f : sum[e];
-    __syncthreads();
-    if ((int)threadIdx.x < Op::W && (int)threadIdx.x < Op::BOUND && o0 + (int)threadIdx.x < O) {
-        float v = 0.0f;
-        for (int i = 0; i < Op::ROWS; ++i) v += lds[i * Op::W + threadIdx.x];
-        to[o0 + threadIdx.x] = v;
-    }
-}
-
-template <class T, bool LIST, class C>
+template <class T, bool LIST, class C, bool NARROW>
 __global__ __launch_bounds__(kThreads, 2) void k_linear_dw(WeightArgs<T> a)
 {
-    using A = OcOperand<T, C::BA, LIST>;
-    using B = OcOperand<T, C::BB, LIST>;
-    constexpr int SUMS = kThreads * T::VEC, LDS = A::LDS + B::LDS > SUMS ? A::LDS + B::LDS : SUMS;
+    using A = OcOperand<T, C::BA, LIST, NARROW>;
+    using B = OcOperand<T, C::BB, LIST, NARROW>;
+    using R = Result<C, A::LDS + B::LDS>;
+    constexpr int LDS = A::LDS + B::LDS > R::SIZE ? A::LDS + B::LDS : R::SIZE, SUMS = C::FA > C::FB ? C::FA : C::FB;
     __shared__ __attribute__((aligned(16))) uint32_t lds[LDS];
     int64_t share;
     int tile;
@@ -396,19 +394,21 @@ __global__ __launch_bounds__(kThreads, 2) void k_linear_dw(WeightArgs<T> a)
     B right;
     left.init(a.a, a.a_stride, a.n, a0, a.a_dim);
     right.init(a.b, a.b_stride, a.n, b0, a.b_dim);
-    const bool bias_a = a.bias == 1 && b0 == 0, bias_b = a.bias == 2 && a0 == 0;
+    // dz's columns are summed from the fragments, by the wavefronts whose tiles are the first of their rows or columns
+    const bool bias_a = a.bias == 1 && b0 == 0 && uniform(C::b_off()) == 0, bias_b = a.bias == 2 && a0 == 0 && uniform(C::a_off()) == 0;
     const int64_t len = (int64_t)a.a_dim * a.b_dim + (a.bias == 2 ? a.b_dim : a.a_dim);
     for (int64_t unit = share * units / a.shares; unit < last;) {
         const Span s = find_span(a.q, a.n, a.q.groups, kUnit, unit);
         int64_t lo = 0, hi = a.n;
         if (a.q.groups > 0) group_range(a.q, a.n, s.group, lo, hi);
+        hi = uniform((int)hi);
         const int64_t room = (last - unit) * kUnit;
         const int count = (int)(hi - s.start < room ? hi - s.start : room);
         unit += (count + kUnit - 1) / kUnit;
         left.range(a.q.index, s.start, count);
         right.range(a.q.index, s.start, count);
-        float sum[T::VEC] = {};
         f32x4 acc[C::FA][C::FB] = {};
+        float sum[SUMS] = {};
         pipeline(
             (count + A::BK - 1) / A::BK,
             [&](int i) {
@@ -420,24 +420,50 @@ __global__ __launch_bounds__(kThreads, 2) void k_linear_dw(WeightArgs<T> a)
                 right.settle();
                 left.store(lds);
                 right.store(lds + A::LDS);
-                if (bias_a) add_rows(left, sum);
-                if (bias_b) add_rows(right, sum);
             },
             [&](int i) {
                 const int steps = (count - i * A::BK + 16 * T::PER - 1) / (16 * T::PER);
-                multiply<T, A, B, C>(lds, lds + A::LDS, steps, acc);
+                multiply<T, A, B, C>(lds, lds + A::LDS, steps, acc, [&](const auto &l, const auto &r) {
+                    if (bias_a) {
+#pragma unroll
+                        for (int f = 0; f < C::FA; ++f) sum[f] = T::sum(l[f], sum[f]);
+                    } else if (bias_b) {
+#pragma unroll
+                        for (int f = 0; f < C::FB; ++f) sum[f] = T::sum(r[f], sum[f]);
+                    }
+                });
             });
         float *part = a.part + (share + s.group) * len;
-        const int l = threadIdx.x & 63, r = a0 + C::a_off() + 4 * (l >> 4), c = b0 + C::b_off() + (l & 15);
+        float *sums = reinterpret_cast<float *>(lds);
 #pragma unroll
-        for (int i = 0; i < C::FA; ++i)
+        for (int half = 0; half < R::PARTS; ++half) {
+            if (half) __syncthreads();
+            R::put(sums, half, acc);
+            __syncthreads();
+            constexpr int PER_ROW = R::W / 4, ROWS = kThreads / PER_ROW;
+            const int c = (int)(threadIdx.x % PER_ROW) * 4, columns = a.b_dim - b0 - c;
+#pragma unroll 1  // (unrolled, its addresses were kept in registers through the products: 256 of them, and memory)
+            for (int i = threadIdx.x / PER_ROW; i < R::ROWS; i += ROWS) {
+                const int r = a0 + R::row(half, i);
+                if (r >= a.a_dim || columns <= 0 || c >= C::BB) continue;
+                const f32x4 four = *reinterpret_cast<const f32x4 *>(sums + result_place<R::W>(i, c));
+                float *to = part + (int64_t)r * a.b_dim + b0 + c;
+                if (columns >= 4) __builtin_memcpy(to, &four, 16);
+                else
+                    for (int e = 0; e < columns; ++e) to[e] = four[e];
+            }
+        }
+        if (bias_a || bias_b) {  // a lane has the sum over its lane group's part of the rows
+            const int lane = threadIdx.x & 63;
+            const int o0 = (bias_a ? a0 + C::a_off() : b0 + C::b_off()) + lane, O = bias_a ? a.a_dim : a.b_dim, frags = bias_a ? C::FA : C::FB;
+            float *to = part + (int64_t)a.a_dim * a.b_dim;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int t = 0; t < C::FB; ++t)
-                    if (r + 16 * i + j < a.a_dim && c + 16 * t < a.b_dim) part[(int64_t)(r + 16 * i + j) * a.b_dim + c + 16 * t] = acc[i][t][j];
-        if (bias_a) put_sums(left, reinterpret_cast<float *>(lds), sum, part + (int64_t)a.a_dim * a.b_dim, a0, a.a_dim);
-        if (bias_b) put_sums(right, reinterpret_cast<float *>(lds), sum, part + (int64_t)a.a_dim * a.b_dim, b0, a.b_dim);
+            for (int f = 0; f < SUMS; ++f) {
+                sum[f] += __shfl_xor(sum[f], 16);
+                sum[f] += __shfl_xor(sum[f], 32);
+                if (f < frags && lane < 16 && o0 + 16 * f < O) to[o0 + 16 * f] = sum[f];
+            }
+        }
         __syncthreads();  // (the next group's first tile goes where these were read)
     }
 }
@@ -670,27 +696,30 @@ using Narrow = Cut<4, 1, 2, F>;
 template <int F>
 using SmallNarrow = Cut<4, 1, 1, F>;
 
+// call(cut, narrow): narrow where a row may be shorter than `vec` values.
 template <class Do>
-void with_cut(bool large, int cols, Do call)
+void with_cut(bool large, int cols, int vec, Do call)
 {
     const int f = (cols + 15) / 16;
+    const std::true_type yes{};
+    const std::false_type no{};
     if (large) {
         switch (f) {
-        case 1: return call(Narrow<1>{});
-        case 2: return call(Narrow<2>{});
-        case 3: return call(Narrow<3>{});
-        case 4: return call(Narrow<4>{});
-        case 5: return call(Narrow<5>{});
-        case 6: return call(Narrow<6>{});
-        case 7: return call(Narrow<7>{});
-        default: return call(Large{});
+        case 1: return cols < vec ? call(Narrow<1>{}, yes) : call(Narrow<1>{}, no);
+        case 2: return call(Narrow<2>{}, no);
+        case 3: return call(Narrow<3>{}, no);
+        case 4: return call(Narrow<4>{}, no);
+        case 5: return call(Narrow<5>{}, no);
+        case 6: return call(Narrow<6>{}, no);
+        case 7: return call(Narrow<7>{}, no);
+        default: return call(Large{}, no);
         }
     }
     switch (f) {
-    case 1: return call(SmallNarrow<1>{});
-    case 2: return call(SmallNarrow<2>{});
-    case 3: return call(SmallNarrow<3>{});
-    default: return call(Small{});
+    case 1: return cols < vec ? call(SmallNarrow<1>{}, yes) : call(SmallNarrow<1>{}, no);
+    case 2: return call(SmallNarrow<2>{}, no);
+    case 3: return call(SmallNarrow<3>{}, no);
+    default: return call(Small{}, no);
     }
 }
 
@@ -709,7 +738,7 @@ WeightPlan plan_weight(const bgl_linear_t *l, int64_t n)
     p.a_dim = p.swapped ? l->in_dim : l->out_dim;
     p.b_dim = p.swapped ? l->out_dim : l->in_dim;
     p.large = p.a_dim > 64;
-    with_cut(p.large, p.b_dim, [&](auto cut) {
+    with_cut(p.large, p.b_dim, 0, [&](auto cut, auto) {
         p.a_tiles = (int)ceil_div(p.a_dim, decltype(cut)::BA);
         p.b_tiles = (int)ceil_div(p.b_dim, decltype(cut)::BB);
     });
@@ -730,12 +759,12 @@ int launch_rows(RowsArgs<T> &a, hipStream_t st)
     const int64_t extra = a.q.groups > 0 ? (a.q.groups + 1 < a.n ? a.q.groups + 1 : a.n) : 1;
     const bool large = ceil_div(a.n, Large::BA) * ceil_div(a.N, Large::BB) >= 256;
     int64_t blocks = 0;
-    with_cut(large, a.N, [&](auto cut) {
+    with_cut(large, a.N, T::VEC, [&](auto cut, auto narrow) {
         using C = decltype(cut);
         a.row_tiles = a.n / C::BA + extra;
         a.col_tiles = (int)ceil_div(a.N, C::BB);
         blocks = tile_count(a.row_tiles, a.col_tiles);
-        if (blocks <= INT32_MAX) k_linear_rows<T, B_OC, C><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a);
+        if (blocks <= INT32_MAX) k_linear_rows<T, B_OC, C, B_OC && decltype(narrow)::value><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a);
     });
     if (blocks > INT32_MAX) BGL_FAIL(BGL_EUNSUPPORTED, "%lld rows of width %d need too many workgroups", (long long)a.n, a.N);
     BGL_HIP(hipGetLastError());
@@ -802,9 +831,9 @@ int backward(const bgl_linear_t *l, int64_t n, const Groups &q, const void *dy, 
             a.bias = p.swapped ? 2 : 1;
             a.q = q;
             const dim3 grid((unsigned)tile_count(p.shares, p.a_tiles * p.b_tiles)), block(kThreads);
-            with_cut(p.large, p.b_dim, [&](auto cut) {
-                if (q.index) k_linear_dw<T, true, decltype(cut)><<<grid, block, 0, st>>>(a);
-                else k_linear_dw<T, false, decltype(cut)><<<grid, block, 0, st>>>(a);
+            with_cut(p.large, p.b_dim, T::VEC, [&](auto cut, auto narrow) {
+                if (q.index) k_linear_dw<T, true, decltype(cut), decltype(narrow)::value><<<grid, block, 0, st>>>(a);
+                else k_linear_dw<T, false, decltype(cut), decltype(narrow)::value><<<grid, block, 0, st>>>(a);
             });
             BGL_HIP(hipGetLastError());
         }

@@ -18,6 +18,7 @@ namespace bgl {
 namespace tile {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
@@ -26,9 +27,14 @@ constexpr int kDwords = 32;  // of the summed index per tile
 
 struct F32 {
     typedef float elem;
+    typedef uint32_t bits;
     static constexpr int PER = 1, VEC = 4;  // values per dword, per 16 bytes
     static __device__ __forceinline__ float get(elem v) { return v; }
     static __device__ __forceinline__ elem put(float v) { return v; }
+    static __device__ __forceinline__ float sum(const uint32_t (&a)[4], float c)
+    {
+        return c + ((__uint_as_float(a[0]) + __uint_as_float(a[1])) + (__uint_as_float(a[2]) + __uint_as_float(a[3])));
+    }
     // 16 dwords of the summed index: four instructions of 4 values
     static __device__ __forceinline__ f32x4 mma(const uint32_t (&a)[4], const uint32_t (&b)[4], f32x4 c)
     {
@@ -40,9 +46,17 @@ struct F32 {
 
 struct BF16 {
     typedef uint16_t elem;
+    typedef uint16_t bits;
     static constexpr int PER = 2, VEC = 8;
     static __device__ __forceinline__ float get(elem v) { return __uint_as_float((uint32_t)v << 16); }
     static __device__ __forceinline__ elem put(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }  // to nearest even
+    static __device__ __forceinline__ float sum(const uint32_t (&a)[4], float c)
+    {
+        const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+        for (int p = 0; p < 4; ++p) c = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, a[p]), ones, c, false);
+        return c;
+    }
     static __device__ __forceinline__ f32x4 mma(const uint32_t (&a)[4], const uint32_t (&b)[4], f32x4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -97,10 +111,13 @@ __device__ __forceinline__ uint4 load_end(const typename T::elem *p, int left, i
         const int back = left >= T::VEC ? 0 : T::VEC - left;
         return move_down<T>(load_any<uint4>(p - back), back);
     }
-    typename T::elem v[T::VEC];
+    uint32_t d[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int e = 0; e < T::VEC; ++e) v[e] = e < left ? p[e] : (typename T::elem)0;
-    return __builtin_bit_cast(uint4, v);
+    for (int e = 0; e < T::VEC - 1; ++e) {
+        if (e < left) d[e / T::PER] |= (uint32_t)__builtin_bit_cast(typename T::bits, p[e]) << (e % T::PER * 16);
+        __builtin_amdgcn_sched_barrier(0);  // (one at a time: this rare case would take 64 registers beside the products')
+    }
+    return uint4{d[0], d[1], d[2], d[3]};
 }
 
 // Both operands keep the next tile on its way in registers while the present one is multiplied out of LDS.  Loads of whole tiles have no
@@ -158,11 +175,10 @@ struct KcOperand {
 
 // An Oc operand: values (k, o) at base + row(k) * stride + o, k counted in a range of `count` > 0 summed rows.  LIST: row(k) = rows[k], and
 // numbers outside [0, total) have no row; else row(k) = first + k.  Rows outside are read from one that exists and zeroed on the way to
-// LDS; columns that do not exist hold anything (they make columns of the result that are not stored).
-template <class T, int BO, bool LIST>
+// LDS; columns that do not exist hold anything (they make columns of the result that are not stored).  NARROW:
+// rows may be shorter than 16 bytes (a template's affair because that code, never run, still took the others' registers).
+template <class T, int BO, bool LIST, bool NARROW>
 struct OcOperand {
-    using type = T;
-    static constexpr int BOUND = BO;
     static constexpr int BK = kDwords * T::PER;
     static constexpr int W = up_to_power(BO);        // columns of a row in LDS
     static constexpr int LDS = kDwords * W;          // dwords
@@ -177,8 +193,8 @@ struct OcOperand {
     int back;                      // how far base was moved; VEC where the thread has no columns
     bool ends;                     // a chunk of the tile is cut by the row's end
     bool narrow;                   // rows shorter than 16 bytes
-    uint32_t next[PASSES];         // row numbers of the tile that is loaded next
-    int live_next, live;           // which of them (of those in reg) exist, one bit each
+    int32_t next[LIST ? PASSES : 1];  // row numbers of the tile that is loaded next
+    int live;                      // which rows of the tile in reg exist, one bit each
     uint4 reg[PASSES];
 
     __device__ __forceinline__ int kk(int pass) const { return (int)threadIdx.x / PER_ROW + ROWS * pass; }
@@ -186,7 +202,7 @@ struct OcOperand {
     __device__ __forceinline__ void init(const typename T::elem *p, int64_t ld, int64_t of, int o0, int O)
     {
         const int o = o0 + (int)(threadIdx.x % PER_ROW) * T::VEC, left = O - o;
-        narrow = O < T::VEC;
+        narrow = NARROW && O < T::VEC;
         ends = o0 + W > O && O % T::VEC != 0;
         back = left >= T::VEC ? 0 : left > 0 ? T::VEC - left : T::VEC;
         base = p + (narrow ? 0 : left > 0 ? o - back : 0);
@@ -196,39 +212,45 @@ struct OcOperand {
     // The range of summed rows: from position `from` of the row order, n of them.
     __device__ __forceinline__ void range(const int32_t *index, int64_t from, int n)
     {
-        rows = index + from;
+        if constexpr (LIST) rows = index + from;
         first = (int32_t)from;
         count = n;
         seek(0);
     }
+    // LIST: asks for the row numbers of a tile
     __device__ __forceinline__ void seek(int tile)
     {
-        live_next = 0;
+        if constexpr (LIST) {
 #pragma unroll
-        for (int p = 0; p < PASSES; ++p) {
-            const int k = tile * BK + kk(p);
-            const int at = k < count ? k : count - 1;
-            const int32_t r = LIST ? rows[at] : first + at;
-            const bool named = !LIST || (uint32_t)r < (uint32_t)total;
-            next[p] = named ? r : 0;
-            live_next |= (int)(named && k < count) << p;
+            for (int p = 0; p < PASSES; ++p) {
+                const int k = tile * BK + kk(p);
+                next[p] = rows[k < count ? k : count - 1];
+            }
         }
     }
     __device__ __forceinline__ void load(int tile)
     {
         uint32_t now[PASSES];
+        live = 0;
 #pragma unroll
-        for (int p = 0; p < PASSES; ++p) now[p] = next[p];
-        live = live_next;
+        for (int p = 0; p < PASSES; ++p) {
+            const int k = tile * BK + kk(p);
+            const uint32_t r = LIST ? next[LIST ? p : 0] : first + (k < count ? k : count - 1);
+            const bool named = !LIST || r < (uint32_t)total;
+            now[p] = named ? r : 0;
+            live |= (int)(named && k < count) << p;
+        }
         seek(tile + 1);  // before the loads: waiting for these numbers then waits for no later load
         if (idle()) return;
-        if (!narrow) {
+        if constexpr (NARROW) {
+            if (narrow) {
 #pragma unroll
-            for (int p = 0; p < PASSES; ++p) reg[p] = load_any<uint4>(base + (uint64_t)now[p] * stride);
-        } else {
-#pragma unroll
-            for (int p = 0; p < PASSES; ++p) reg[p] = load_end<T>(base + (uint64_t)now[p] * stride, T::VEC - back, 0);
+                for (int p = 0; p < PASSES; ++p) reg[p] = load_end<T>(base + (uint64_t)now[p] * stride, T::VEC - back, 0);
+                return;
+            }
         }
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) reg[p] = load_any<uint4>(base + (uint64_t)now[p] * stride);
     }
     // Zeroes rows that do not exist and puts cut chunks in place; once for each loaded tile, before store().
     __device__ __forceinline__ void settle()
@@ -300,9 +322,9 @@ __device__ __forceinline__ void pipeline(int tiles, Load load, Store store, Comp
     }
 }
 
-// One tile of both operands into the accumulators; `steps` of 16 dwords hold values.
-template <class T, class A, class B, class C>
-__device__ __forceinline__ void multiply(const uint32_t *a_lds, const uint32_t *b_lds, int steps, f32x4 (&acc)[C::FA][C::FB])
+// One tile of both operands into the accumulators; `steps` of 16 dwords hold values.  also(a, b) sees each step's fragments.
+template <class T, class A, class B, class C, class Also>
+__device__ __forceinline__ void multiply(const uint32_t *a_lds, const uint32_t *b_lds, int steps, f32x4 (&acc)[C::FA][C::FB], Also also)
 {
     const auto products = [&](const uint32_t(&a)[C::FA][4], const uint32_t(&b)[C::FB][4]) {
 #pragma unroll
@@ -317,6 +339,7 @@ __device__ __forceinline__ void multiply(const uint32_t *a_lds, const uint32_t *
         A::read(a_lds, C::a_off(), step, a);
         B::read(b_lds, C::b_off(), step, b);
         products(a, b);
+        also(a, b);
     }
 }
 
@@ -335,7 +358,8 @@ struct Result {
     static __device__ __forceinline__ int row(int part, int r) { return r / (16 * FH) * 16 * C::FA + part * 16 * FH + r % (16 * FH); }
     static __device__ __forceinline__ void put(float *lds, int part, const f32x4 (&acc)[C::FA][C::FB])
     {
-        const int l = threadIdx.x & 63;
+        int l = threadIdx.x & 63;
+        asm volatile("" : "+v"(l));  // (the addresses are made here: around an outer loop they would be kept in 32 registers)
 #pragma unroll
         for (int i = 0; i < C::FA; ++i) {
             if (i / FH != part) continue;
