@@ -63,13 +63,16 @@ struct BF16 {
     }
 };
 
+// The thread's number among the 256 that make one product; a workgroup may have several such teams.
+__device__ __forceinline__ int team_thread() { return threadIdx.x & (kThreads - 1); }
+
 // A workgroup of WA x WB wavefronts, each with FA x FB fragments.
 template <int WA, int WB, int FA_, int FB_>
 struct Cut {
     static_assert(WA * WB * kWave == kThreads, "");
     static constexpr int FA = FA_, FB = FB_, BA = 16 * WA * FA, BB = 16 * WB * FB;
-    static __device__ __forceinline__ int a_off() { return (int)(threadIdx.x / kWave) / WB * 16 * FA; }
-    static __device__ __forceinline__ int b_off() { return (int)(threadIdx.x / kWave) % WB * 16 * FB; }
+    static __device__ __forceinline__ int a_off() { return team_thread() / kWave / WB * 16 * FA; }
+    static __device__ __forceinline__ int b_off() { return team_thread() / kWave % WB * 16 * FB; }
 };
 
 constexpr int up_to_power(int x)
@@ -137,7 +140,7 @@ struct KcOperand {
     __device__ __forceinline__ void init(Row row)
     {
 #pragma unroll
-        for (int p = 0; p < PASSES; ++p) at[p] = row((int)(threadIdx.x >> 3) + 32 * p) + (threadIdx.x & 7) * T::VEC;
+        for (int p = 0; p < PASSES; ++p) at[p] = row((team_thread() >> 3) + 32 * p) + (team_thread() & 7) * T::VEC;
     }
     __device__ __forceinline__ void load_whole(int tile)
     {
@@ -147,7 +150,7 @@ struct KcOperand {
     __device__ __forceinline__ void load(int tile, int K)
     {
         if ((tile + 1) * BK <= K) return load_whole(tile);
-        const int left = K - tile * BK - (int)(threadIdx.x & 7) * T::VEC;
+        const int left = K - tile * BK - (int)(team_thread() & 7) * T::VEC;
 #pragma unroll
         for (int p = 0; p < PASSES; ++p) reg[p] = load_end<T>(at[p] + tile * BK, left, K);
     }
@@ -155,7 +158,7 @@ struct KcOperand {
     {
 #pragma unroll
         for (int p = 0; p < PASSES; ++p) {
-            const int r = (threadIdx.x >> 3) + 32 * p, c = threadIdx.x & 7;
+            const int r = (team_thread() >> 3) + 32 * p, c = team_thread() & 7;
             *reinterpret_cast<uint4 *>(lds + r * kDwords + ((c ^ (r & 7)) << 2)) = reg[p];
         }
     }
@@ -197,11 +200,11 @@ struct OcOperand {
     int live;                      // which rows of the tile in reg exist, one bit each
     uint4 reg[PASSES];
 
-    __device__ __forceinline__ int kk(int pass) const { return (int)threadIdx.x / PER_ROW + ROWS * pass; }
+    __device__ __forceinline__ int kk(int pass) const { return team_thread() / PER_ROW + ROWS * pass; }
     __device__ __forceinline__ bool idle() const { return ROWS > BK && kk(0) >= BK; }
     __device__ __forceinline__ void init(const typename T::elem *p, int64_t ld, int64_t of, int o0, int O)
     {
-        const int o = o0 + (int)(threadIdx.x % PER_ROW) * T::VEC, left = O - o;
+        const int o = o0 + team_thread() % PER_ROW * T::VEC, left = O - o;
         narrow = NARROW && O < T::VEC;
         ends = o0 + W > O && O % T::VEC != 0;
         back = left >= T::VEC ? 0 : left > 0 ? T::VEC - left : T::VEC;
@@ -279,7 +282,7 @@ struct OcOperand {
         if (idle()) return;
         typename T::elem *to = reinterpret_cast<typename T::elem *>(lds);
 #pragma unroll
-        for (int p = 0; p < PASSES; ++p) *reinterpret_cast<uint4 *>(to + place(kk(p), (int)(threadIdx.x % PER_ROW) * T::VEC)) = reg[p];
+        for (int p = 0; p < PASSES; ++p) *reinterpret_cast<uint4 *>(to + place(kk(p), team_thread() % PER_ROW * T::VEC)) = reg[p];
     }
     template <int F>
     static __device__ __forceinline__ void read(const uint32_t *lds, int off, int step, uint32_t (&f)[F][4])
@@ -356,7 +359,7 @@ struct Result {
     static constexpr int FH = fit(C::FA), PARTS = C::FA / FH, ROWS = WA * 16 * FH, SIZE = ROWS * W;
     // the tile's row that row r of a part is
     static __device__ __forceinline__ int row(int part, int r) { return r / (16 * FH) * 16 * C::FA + part * 16 * FH + r % (16 * FH); }
-    static __device__ __forceinline__ void put(float *lds, int part, const f32x4 (&acc)[C::FA][C::FB])
+    static __device__ __forceinline__ void put(float *lds, int part, const f32x4 (&acc)[C::FA][C::FB], bool add = false)
     {
         int l = threadIdx.x & 63;
         asm volatile("" : "+v"(l));  // (the addresses are made here: around an outer loop they would be kept in 32 registers)
@@ -366,8 +369,10 @@ struct Result {
 #pragma unroll
             for (int t = 0; t < C::FB; ++t)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    lds[result_place<W>(C::a_off() / C::FA * FH + 16 * (i % FH) + 4 * (l >> 4) + j, C::b_off() + 16 * t + (l & 15))] = acc[i][t][j];
+                for (int j = 0; j < 4; ++j) {
+                    float *to = lds + result_place<W>(C::a_off() / C::FA * FH + 16 * (i % FH) + 4 * (l >> 4) + j, C::b_off() + 16 * t + (l & 15));
+                    *to = add ? *to + acc[i][t][j] : acc[i][t][j];
+                }
         }
     }
 };
