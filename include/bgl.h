@@ -773,7 +773,8 @@ int bgl_group_rows(const int32_t *group_of, int64_t num_nodes, const int32_t *id
  *   weight      device, out_dim x in_dim (num_groups of them one after the other), tight
  *   bias        device, out_dim (num_groups x out_dim), or null
  *   residual    n rows of out_dim; null without one.  May be y itself.
- *   saved       n rows of out_dim that receive z for the backward call, or null
+ *   saved       n rows of out_dim that receive z for the backward call, or null (the values
+ *               are that call's affair: a bf16 layer keeps the z of gelu and silu as halves)
  * y and saved must not overlap x, the weights or each other.  n = 0 does nothing.
  * Errors: BGL_EINVAL (null or misaligned pointers, strides, sizes < 1, unknown
  * types), BGL_EUNSUPPORTED (in_dim or out_dim > BGL_MAX_DIM, num_groups > BGL_MAX_GROUPS), BGL_EHIP.

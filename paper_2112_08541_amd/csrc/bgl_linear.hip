@@ -65,6 +65,25 @@ __device__ __forceinline__ float slope(float z)
     }
     return 1.0f;
 }
+// z as it is kept for the backward call, in the layer's width.  bf16 layers keep the z of gelu and silu as a half: three bits more, so that the slope
+// adds nothing to what rounding dz costs; beyond its range, where the slope is 0 or 1, the end of it.  relu's z stays bf16: only its sign counts, and
+// no z > 0 may become 0.
+template <class T>
+__device__ __forceinline__ typename T::elem keep(int act, float z)
+{
+    if constexpr (T::PER == 2) {
+        if (act == BGL_ACT_GELU || act == BGL_ACT_SILU) return __builtin_bit_cast(uint16_t, (_Float16)(z > 65504.0f ? 65504.0f : z < -65504.0f ? -65504.0f : z));
+    }
+    return T::put(z);
+}
+template <class T>
+__device__ __forceinline__ float kept(int act, typename T::elem v)
+{
+    if constexpr (T::PER == 2) {
+        if (act == BGL_ACT_GELU || act == BGL_ACT_SILU) return (float)__builtin_bit_cast(_Float16, v);
+    }
+    return T::get(v);
+}
 // One choice for several values: one for each kept their chains apart.
 template <int V>
 __device__ __forceinline__ void activate_all(int act, float (&v)[V])
@@ -198,11 +217,8 @@ __device__ __forceinline__ void load_cols(const typename T::elem *p, int left, f
     for (int i = 0; i < TT; ++i) v[i] = T::get(pack.e[i]);
 }
 template <class T, int TT>
-__device__ __forceinline__ void store_cols(typename T::elem *p, int left, const float (&v)[TT])
+__device__ __forceinline__ void store_piece(typename T::elem *p, int left, const Cols<T, TT> &pack)
 {
-    Cols<T, TT> pack;
-#pragma unroll
-    for (int i = 0; i < TT; ++i) pack.e[i] = T::put(v[i]);
     if (left >= TT) {
         __builtin_memcpy(p, &pack, sizeof(pack));
     } else {
@@ -210,6 +226,14 @@ __device__ __forceinline__ void store_cols(typename T::elem *p, int left, const 
         for (int i = 0; i < TT; ++i)
             if (i < left) p[i] = pack.e[i];
     }
+}
+template <class T, int TT>
+__device__ __forceinline__ void store_cols(typename T::elem *p, int left, const float (&v)[TT])
+{
+    Cols<T, TT> pack;
+#pragma unroll
+    for (int i = 0; i < TT; ++i) pack.e[i] = T::put(v[i]);
+    store_piece<T, TT>(p, left, pack);
 }
 
 // ----------------------------------------------------------------- forward, and dx
@@ -223,13 +247,18 @@ struct RowsArgs {
     int K, N, col_tiles;  // summed and kept width
     int residual_mode, activation;
     Groups q;
+    // dx from dy: z as kept by the forward call, and where dz goes (null: nowhere)
+    const typename T::elem *z;
+    typename T::elem *dz;
+    int64_t z_stride, dz_stride;
+    int z_activation;
 };
 
 // The tile's sums, in LDS, to their rows: a thread has VEC neighbouring columns of every so many rows.  WHOLE: N is a multiple of VEC.
-template <class T, class C, class R, bool WHOLE>
+template <class T, class C, class R, bool WHOLE, int TEAMS>
 __device__ __forceinline__ void finish_rows(const RowsArgs<T> &a, const float *sums, const int32_t *row_of, int part, int group, int n0)
 {
-    constexpr int W = R::W, V = T::VEC, PER_ROW = W / V, ROWS = kThreads / PER_ROW, PASSES = R::ROWS > ROWS ? R::ROWS / ROWS : 1;
+    constexpr int W = R::W, V = T::VEC, PER_ROW = W / V, ROWS = kThreads * TEAMS / PER_ROW, PASSES = R::ROWS > ROWS ? R::ROWS / ROWS : 1;
     constexpr int BATCH = PASSES < 8 ? PASSES : 8;
     using Piece = Cols<T, V>;
     const int c = (int)(threadIdx.x % PER_ROW) * V, r0 = threadIdx.x / PER_ROW, left = a.N - n0 - c;
@@ -254,7 +283,9 @@ __device__ __forceinline__ void finish_rows(const RowsArgs<T> &a, const float *s
             float v[V];
 #pragma unroll
             for (int u = 0; u < V; u += 4) {
-                const f32x4 four = *reinterpret_cast<const f32x4 *>(sums + result_place<W>(r0 + (p0 + p) * ROWS, c + u));
+                f32x4 four = {};
+#pragma unroll
+                for (int t = 0; t < TEAMS; ++t) four += *reinterpret_cast<const f32x4 *>(sums + t * R::SIZE + result_place<W>(r0 + (p0 + p) * ROWS, c + u));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[u + e] = four[e] + bias[u + e];
             }
@@ -263,7 +294,12 @@ __device__ __forceinline__ void finish_rows(const RowsArgs<T> &a, const float *s
                 for (int u = 0; u < V; ++u) v[u] += T::get(res[p].e[u]);
             }
             if (row[p] < 0) continue;
-            if (a.saved) store_cols<T, V>(a.saved + row[p] * a.saved_stride + n0 + c, WHOLE ? V : left, v);
+            if (a.saved) {
+                Piece piece;
+#pragma unroll
+                for (int u = 0; u < V; ++u) piece.e[u] = keep<T>(a.activation, v[u]);
+                store_piece<T, V>(a.saved + row[p] * a.saved_stride + n0 + c, WHOLE ? V : left, piece);
+            }
             activate_all(a.activation, v);
             if (a.residual_mode == BGL_RESIDUAL_AFTER) {
 #pragma unroll
@@ -274,13 +310,64 @@ __device__ __forceinline__ void finish_rows(const RowsArgs<T> &a, const float *s
     }
 }
 
-template <class T, bool B_OC, class C, bool NARROW>
-__global__ __launch_bounds__(kThreads, 2) void k_linear_rows(RowsArgs<T> a)
+// The operand dz = dy act'(z) of dx, made on its way to LDS; `write` says whether this workgroup stores it too.
+template <class T, int BO>
+struct DzOperand : KcOperand<T, BO> {
+    using Base = KcOperand<T, BO>;
+    const typename T::elem *saved;
+    typename T::elem *dz;
+    int64_t saved_stride, dz_stride;
+    int32_t row[Base::PASSES];
+    uint4 z[Base::PASSES];
+    int act, tile, K;
+
+    template <class Row>
+    __device__ __forceinline__ void rows(Row row_of)
+    {
+#pragma unroll
+        for (int p = 0; p < Base::PASSES; ++p) row[p] = row_of((team_thread() >> 3) + 32 * p);
+    }
+    __device__ __forceinline__ void load(int t, int width)
+    {
+        tile = t;
+        Base::load(t, width);
+        const int first = t * Base::BK + (team_thread() & 7) * T::VEC, left = width - first;
+#pragma unroll
+        for (int p = 0; p < Base::PASSES; ++p) {
+            const typename T::elem *from = saved + (row[p] < 0 ? 0 : row[p]) * saved_stride + first;
+            z[p] = (t + 1) * Base::BK <= width ? load_any<uint4>(from) : load_end<T>(from, left, width);
+        }
+    }
+    __device__ __forceinline__ void store(uint32_t *lds)
+    {
+        const int first = tile * Base::BK + (team_thread() & 7) * T::VEC, left = K - first;
+#pragma unroll
+        for (int p = 0; p < Base::PASSES; ++p) {
+            auto d = __builtin_bit_cast(Cols<T, T::VEC>, Base::reg[p]);
+            const auto s = __builtin_bit_cast(Cols<T, T::VEC>, z[p]);
+            float dv[T::VEC], zv[T::VEC];
+#pragma unroll
+            for (int e = 0; e < T::VEC; ++e) dv[e] = T::get(d.e[e]), zv[e] = kept<T>(act, s.e[e]);
+            times_slope(act, zv, dv);
+#pragma unroll
+            for (int e = 0; e < T::VEC; ++e) d.e[e] = T::put(dv[e]);
+            Base::reg[p] = __builtin_bit_cast(uint4, d);
+            if (dz && row[p] >= 0) store_piece<T, T::VEC>(dz + row[p] * dz_stride + first, left, d);
+        }
+        Base::store(lds);
+    }
+};
+
+// DZ: x is dy, and dz is made from it and from z on the way (dx alone, where one tile has all columns).  TEAMS of 256 threads take the summed
+// index's tiles in turn; their sums meet when the rows are finished.
+template <class T, bool B_OC, class C, bool NARROW, int TEAMS, bool DZ>
+__global__ __launch_bounds__(kThreads * TEAMS, 2) void k_linear_rows(RowsArgs<T> a)
 {
-    using A = KcOperand<T, C::BA>;
+    using A = std::conditional_t<DZ, DzOperand<T, C::BA>, KcOperand<T, C::BA>>;
     using B = std::conditional_t<B_OC, OcOperand<T, C::BB, false, NARROW>, KcOperand<T, C::BB>>;
-    using R = Result<C, A::LDS + B::LDS>;
-    constexpr int LDS = A::LDS + B::LDS > R::SIZE ? A::LDS + B::LDS : R::SIZE;
+    constexpr int OPERANDS = A::LDS + B::LDS;
+    using R = Result<C, OPERANDS>;
+    constexpr int LDS = TEAMS * (OPERANDS > R::SIZE ? OPERANDS : R::SIZE);
     __shared__ __attribute__((aligned(16))) uint32_t lds[LDS];
     __shared__ int32_t row_of[C::BA];
     int64_t rt;
@@ -289,7 +376,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_linear_rows(RowsArgs<T> a)
     const Span s = find_span(a.q, a.n, a.q.groups + (a.q.groups > 0), C::BA, rt);
     if (s.group < 0) return;
     const bool none = a.q.groups > 0 && s.group == a.q.groups;
-    const int n0 = ct * C::BB, K = none ? 0 : a.K;
+    const int n0 = ct * C::BB, K = none && !DZ ? 0 : a.K;  // (rows of no group have a dz too)
     const typename T::elem *w = a.w + (none ? 0 : (int64_t)s.group * a.N * a.K);
 
     if ((int)threadIdx.x < C::BA) row_of[threadIdx.x] = (int)threadIdx.x < s.count ? row_at(a.q, a.n, s.start + threadIdx.x) : -1;
@@ -302,37 +389,53 @@ __global__ __launch_bounds__(kThreads, 2) void k_linear_rows(RowsArgs<T> a)
             const int32_t r = row_of[i];
             return a.x + (r < 0 ? 0 : r) * a.x_stride;
         });
+        if constexpr (DZ) {
+            rows.rows([&](int i) { return row_of[i]; });
+            rows.saved = a.z, rows.saved_stride = a.z_stride, rows.dz = a.dz, rows.dz_stride = a.dz_stride;
+            rows.act = a.z_activation, rows.K = K;
+        }
         if constexpr (B_OC) {
             weight.init(w, a.N, K, n0, a.N);
             weight.range(nullptr, 0, K);
         } else {
             weight.init([&](int i) { return w + (int64_t)(n0 + i < a.N ? n0 + i : a.N - 1) * a.K; });
         }
+        const int team = TEAMS > 1 ? uniform(threadIdx.x / kThreads) : 0, tiles = (K + A::BK - 1) / A::BK;
+        uint32_t *mine = lds + team * OPERANDS;
         pipeline(
-            (K + A::BK - 1) / A::BK,
+            (tiles + TEAMS - 1) / TEAMS,
             [&](int i) {
-                rows.load(i, K);
-                if constexpr (B_OC) weight.load(i);
-                else weight.load(i, K);
+                if (TEAMS > 1 && i * TEAMS + team >= tiles) return;
+                rows.load(i * TEAMS + team, K);
+                if constexpr (B_OC) weight.load(i * TEAMS + team);
+                else weight.load(i * TEAMS + team, K);
             },
-            [&] {
-                rows.store(lds);
+            [&](int i) {
+                if (TEAMS > 1 && i * TEAMS + team >= tiles) return;
+                rows.store(mine);
                 if constexpr (B_OC) weight.settle();
-                weight.store(lds + A::LDS);
+                weight.store(mine + A::LDS);
             },
             [&](int i) {
-                const int steps = (K - i * A::BK + 16 * T::PER - 1) / (16 * T::PER);
-                multiply<T, A, B, C>(lds, lds + A::LDS, steps, acc, [](const auto &, const auto &) {});
+                if (TEAMS > 1 && i * TEAMS + team >= tiles) return;
+                const int steps = (K - (i * TEAMS + team) * A::BK + 16 * T::PER - 1) / (16 * T::PER);
+                multiply<T, A, B, C>(mine, mine + A::LDS, steps, acc, [](const auto &, const auto &) {});
             });
+        if (DZ && none) {
+#pragma unroll
+            for (auto &line : acc)
+#pragma unroll
+                for (auto &f : line) f = f32x4{};
+        }
     }
     float *sums = reinterpret_cast<float *>(lds);
 #pragma unroll
     for (int part = 0; part < R::PARTS; ++part) {
         if (part) __syncthreads();
-        R::put(sums, part, acc);
+        R::put(sums + (TEAMS > 1 ? threadIdx.x / kThreads : 0) * R::SIZE, part, acc);
         __syncthreads();
-        if (a.N % T::VEC == 0) finish_rows<T, C, R, true>(a, sums, row_of, part, none ? -1 : s.group, n0);
-        else finish_rows<T, C, R, false>(a, sums, row_of, part, none ? -1 : s.group, n0);
+        if (a.N % T::VEC == 0) finish_rows<T, C, R, true, TEAMS>(a, sums, row_of, part, none ? -1 : s.group, n0);
+        else finish_rows<T, C, R, false, TEAMS>(a, sums, row_of, part, none ? -1 : s.group, n0);
     }
 }
 
@@ -350,7 +453,9 @@ __global__ __launch_bounds__(kThreads) void k_linear_dz(int act, const typename 
         float d[V], z[V];
         load_cols<T, V>(dy + r * dy_stride + c, left, d);
         if (act) {
-            load_cols<T, V>(saved + r * saved_stride + c, left, z);
+            const auto piece = load_cols_upto<T, V>(saved + r * saved_stride + c, left);
+#pragma unroll
+            for (int e = 0; e < V; ++e) z[e] = kept<T>(act, piece.e[e]);
             times_slope(act, z, d);
         }
         store_cols<T, V>(dz + r * dz_stride + c, left, d);
@@ -363,6 +468,9 @@ __global__ __launch_bounds__(kThreads) void k_linear_dz(int act, const typename 
 // of `part` (both grow along the rows, so no two meet in a slot): A_dim * B_dim of the matrix, then out_dim of db.
 // Side A is the wider of dz and x, side B the narrower; the matrix is laid out [A][B].
 constexpr int kUnit = 64;
+
+// No share is empty (rows of no group make units fewer than the host can know), so every slot between a group's first and last is written.
+__device__ __forceinline__ int64_t shares_of(int64_t units, int planned) { return units < planned ? units : planned; }
 
 template <class T>
 struct WeightArgs {
@@ -389,7 +497,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_linear_dw(WeightArgs<T> a)
     int64_t before, units;
     int own;
     count_units(a.q, a.n, kUnit, 0, before, own, units);
-    const int64_t last = (share + 1) * units / a.shares;
+    const int64_t shares = shares_of(units, a.shares);
+    if (share >= shares) return;
+    const int64_t last = (share + 1) * units / shares;
     A left;
     B right;
     left.init(a.a, a.a_stride, a.n, a0, a.a_dim);
@@ -397,7 +507,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_linear_dw(WeightArgs<T> a)
     // dz's columns are summed from the fragments, by the wavefronts whose tiles are the first of their rows or columns
     const bool bias_a = a.bias == 1 && b0 == 0 && uniform(C::b_off()) == 0, bias_b = a.bias == 2 && a0 == 0 && uniform(C::a_off()) == 0;
     const int64_t len = (int64_t)a.a_dim * a.b_dim + (a.bias == 2 ? a.b_dim : a.a_dim);
-    for (int64_t unit = share * units / a.shares; unit < last;) {
+    for (int64_t unit = share * units / shares; unit < last;) {
         const Span s = find_span(a.q, a.n, a.q.groups, kUnit, unit);
         int64_t lo = 0, hi = a.n;
         if (a.q.groups > 0) group_range(a.q, a.n, s.group, lo, hi);
@@ -415,7 +525,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_linear_dw(WeightArgs<T> a)
                 left.load(i);
                 right.load(i);
             },
-            [&] {
+            [&](int) {
                 left.settle();
                 right.settle();
                 left.store(lds);
@@ -491,7 +601,7 @@ __global__ __launch_bounds__(kThreads) void k_linear_reduce(ReduceArgs<T> a)
     const int left = len - e < 4 ? (int)(len - e) : 4;
     float v[4] = {};
     if (left > 0 && own > 0) {
-        const int64_t first = ((before + 1) * a.shares - 1) / units, last = ((before + own) * a.shares - 1) / units;
+        const int64_t shares = shares_of(units, a.shares), first = ((before + 1) * shares - 1) / units, last = ((before + own) * shares - 1) / units;
 #pragma unroll 4
         for (int64_t w = first + wave; w <= last; w += kThreads / kWave) {
             float p[4];
@@ -585,25 +695,32 @@ __global__ __launch_bounds__(kGroupThreads) void k_group_place(GroupArgs a)
     }
     __syncthreads();
     // the groups' totals over all tiles, and what the tiles before this one have of each
+    int32_t *total = base + classes;  // [classes]
+    if (!SINGLE) {
+        for (int g = threadIdx.x; g < classes; g += kGroupThreads) total[g] = base[g] = 0;
+        __syncthreads();
+        const int all = (int)gridDim.x * classes, mine = (int)blockIdx.x * classes;
+        for (int i = threadIdx.x; i < all; i += kGroupThreads) {  // (whole numbers: any order gives the same sum)
+            const int g = i % classes, c = a.counts[i];
+            if (c) atomicAdd(&total[g], c);
+            if (c && i < mine) atomicAdd(&base[g], c);
+        }
+        __syncthreads();
+    }
     int carry = 0;
     for (int g0 = 0; g0 < classes; g0 += kGroupThreads) {
         const int g = g0 + threadIdx.x;
-        int total = 0, below = 0;
+        int count = 0;
         if (g < classes) {
-            if (SINGLE) {
-                for (int w = 0; w < WAVES; ++w) total += sh[w * classes + g];
-            } else {
-                for (int t = 0; t < (int)gridDim.x; ++t) {
-                    const int c = a.counts[(int64_t)t * classes + g];
-                    total += c;
-                    if (t < (int)blockIdx.x) below += c;
-                }
-            }
+            if (SINGLE)
+                for (int w = 0; w < WAVES; ++w) count += sh[w * classes + g];
+            else
+                count = total[g];
         }
         int all;
-        const int before = block_excl_scan<kGroupThreads>(total, scan, all);
+        const int before = block_excl_scan<kGroupThreads>(count, scan, all);
         if (g < classes) {
-            base[g] = carry + before + below;
+            base[g] = carry + before + (SINGLE ? 0 : base[g]);
             if (blockIdx.x == 0) a.offsets[g] = carry + before;  // offsets[groups]: the end of the last group
         }
         carry += all;
@@ -742,7 +859,7 @@ WeightPlan plan_weight(const bgl_linear_t *l, int64_t n)
         p.a_tiles = (int)ceil_div(p.a_dim, decltype(cut)::BA);
         p.b_tiles = (int)ceil_div(p.b_dim, decltype(cut)::BB);
     });
-    const int64_t most = ceil_div(n > 0 ? n : 1, 4 * kUnit), want = 512 / ((int64_t)p.a_tiles * p.b_tiles);
+    const int64_t most = ceil_div(n > 0 ? n : 1, kUnit), want = 512 / ((int64_t)p.a_tiles * p.b_tiles);
     p.shares = (int)(want < 1 ? 1 : want < most ? want : most);
     p.slots = p.shares + (l->num_groups > 1 ? l->num_groups - 1 : 0);
     const int per = 16 / elem_bytes(l);
@@ -752,19 +869,21 @@ WeightPlan plan_weight(const bgl_linear_t *l, int64_t n)
     return p;
 }
 
-// 128 rows to a tile where such tiles are enough for the 256 CUs, else 64.
-template <class T, bool B_OC>
+// 128 rows to a tile where such tiles are enough for the 256 CUs, else 64, with four teams: few workgroups then wait for their loads once instead
+// of once for each tile of the summed index.
+template <class T, bool B_OC, bool DZ>
 int launch_rows(RowsArgs<T> &a, hipStream_t st)
 {
     const int64_t extra = a.q.groups > 0 ? (a.q.groups + 1 < a.n ? a.q.groups + 1 : a.n) : 1;
-    const bool large = ceil_div(a.n, Large::BA) * ceil_div(a.N, Large::BB) >= 256;
+    const bool large = ceil_div(a.n, 128) * ceil_div(a.N, 128) >= 256;
     int64_t blocks = 0;
     with_cut(large, a.N, T::VEC, [&](auto cut, auto narrow) {
         using C = decltype(cut);
+        constexpr int TEAMS = C::BA == 64 ? 4 : 1;
         a.row_tiles = a.n / C::BA + extra;
         a.col_tiles = (int)ceil_div(a.N, C::BB);
         blocks = tile_count(a.row_tiles, a.col_tiles);
-        if (blocks <= INT32_MAX) k_linear_rows<T, B_OC, C, B_OC && decltype(narrow)::value><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a);
+        if (blocks <= INT32_MAX) k_linear_rows<T, B_OC, C, B_OC && decltype(narrow)::value, TEAMS, DZ><<<dim3((unsigned)blocks), dim3(kThreads * TEAMS), 0, st>>>(a);
     });
     if (blocks > INT32_MAX) BGL_FAIL(BGL_EUNSUPPORTED, "%lld rows of width %d need too many workgroups", (long long)a.n, a.N);
     BGL_HIP(hipGetLastError());
@@ -783,7 +902,7 @@ int forward(const bgl_linear_t *l, int64_t n, const Groups &q, const void *x, in
     a.K = l->in_dim, a.N = l->out_dim;
     a.residual_mode = l->residual, a.activation = l->activation;
     a.q = q;
-    return launch_rows<T, false>(a, st);
+    return launch_rows<T, false, false>(a, st);
 }
 
 template <class T>
@@ -807,19 +926,27 @@ int backward(const bgl_linear_t *l, int64_t n, const Groups &q, const void *dy, 
     const int classes = l->num_groups > 0 ? l->num_groups : 1;
     const void *dz = dy;
     int64_t dz_stride = dy_stride;
-    if (n > 0 && (dresidual || l->activation != BGL_ACT_NONE)) {
+    // dz is made where dx first needs it if a tile of dx has all its columns (128 at most): every column tile would make it again
+    const bool act = l->activation != BGL_ACT_NONE, together = act && dx && n > 0 && l->in_dim <= Large::BB;
+    if (n > 0 && (dresidual || act)) {
         void *to = dresidual ? dresidual : workspace;
         dz_stride = dresidual ? dresidual_stride : (int64_t)p.dz_stride;
-        BGL_TRY(launch_dz<T>(l->activation, dy, dy_stride, saved, saved_stride, to, dz_stride, n, l->out_dim, st));
+        if (!together) BGL_TRY(launch_dz<T>(l->activation, dy, dy_stride, saved, saved_stride, to, dz_stride, n, l->out_dim, st));
         dz = to;
     }
     if (dx && n > 0) {
         RowsArgs<T> a{};
-        a.x = (const E *)dz, a.w = (const E *)weight, a.y = (E *)dx;
-        a.n = n, a.x_stride = dz_stride, a.y_stride = dx_stride;
+        a.x = (const E *)(together ? dy : dz), a.w = (const E *)weight, a.y = (E *)dx;
+        a.n = n, a.x_stride = together ? dy_stride : dz_stride, a.y_stride = dx_stride;
         a.K = l->out_dim, a.N = l->in_dim;
         a.q = q;
-        BGL_TRY((launch_rows<T, true>(a, st)));
+        if (together) {
+            a.z = (const E *)saved, a.z_stride = saved_stride, a.z_activation = l->activation;
+            a.dz = dresidual || dweight ? (E *)dz : nullptr, a.dz_stride = dz_stride;
+            BGL_TRY((launch_rows<T, true, true>(a, st)));
+        } else {
+            BGL_TRY((launch_rows<T, true, false>(a, st)));
+        }
     }
     if (dweight) {
         float *part = reinterpret_cast<float *>((char *)workspace + p.dz_bytes);
@@ -958,7 +1085,7 @@ try {
     a.group = (uint16_t *)workspace;
     a.counts = (int32_t *)((char *)workspace + round_up((size_t)n * sizeof(uint16_t), 256));
     const hipStream_t st = (hipStream_t)stream;
-    const size_t classes = (size_t)num_groups + 1, place = (kGroupThreads / kWave + 1) * classes * sizeof(int32_t);
+    const size_t classes = (size_t)num_groups + 1, place = (kGroupThreads / kWave + 2) * classes * sizeof(int32_t);
     if (tiles <= 1) {
         k_group_place<true><<<dim3(1), dim3(kGroupThreads), place, st>>>(a);
     } else {

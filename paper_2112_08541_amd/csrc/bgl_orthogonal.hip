@@ -245,7 +245,7 @@ __global__ __launch_bounds__(kThreads * TEAMS, 2) void k_ortho_product(OrthoArgs
                 r.load_whole(i * TEAMS + team);
             }
         },
-        [&] {
+        [&](int) {
             l.store(mine);
             r.store(mine + Op::LDS);
         },

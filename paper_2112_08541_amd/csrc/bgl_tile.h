@@ -309,7 +309,7 @@ struct OcOperand {
     }
 };
 
-// The tiles of one product: load(tile) into registers, store() from there to LDS, compute(tile) out of LDS.  One LDS buffer and two
+// The tiles of one product: load(tile) into registers, store(tile) from there to LDS, compute(tile) out of LDS.  One LDS buffer and two
 // barriers a tile: the room a second buffer would take holds another workgroup, which fills the waits of this one.
 template <class Load, class Store, class Compute>
 __device__ __forceinline__ void pipeline(int tiles, Load load, Store store, Compute compute)
@@ -317,7 +317,7 @@ __device__ __forceinline__ void pipeline(int tiles, Load load, Store store, Comp
     if (tiles <= 0) return;
     load(0);
     for (int i = 0; i < tiles; ++i) {
-        store();
+        store(i);
         __syncthreads();
         if (i + 1 < tiles) load(i + 1);
         compute(i);

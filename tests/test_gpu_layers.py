@@ -242,6 +242,31 @@ def test_groups_of_rows_already_in_order_and_rows_left_out(torch, B):
     assert np.isfinite(wild).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,typed", [(5000, 0), (5000, 1), (5000, 70), (40_000, 130)])
+def test_batches_whose_rows_mostly_belong_to_no_group(torch, B, dtype, n, typed):
+    """Fewer groups' rows than the backward call planned shares for."""
+    dt, K, N, G = dtype_of(torch, dtype), 40, 24, 4
+    rng = np.random.default_rng([n, typed])
+    group = np.full(n, -1, dtype=np.int32)
+    group[rng.permutation(n)[:typed]] = rng.integers(0, G, typed)
+    x, x64 = rows_of(torch, rng, n, K, dt)
+    dy, dy64 = rows_of(torch, rng, n, N, dt)
+    w = torch.from_numpy(rng.standard_normal((G, N, K)).astype(np.float32)).to(dt).cuda()
+    ref = Reference(x64, w.double().cpu().numpy(), None, None, "none", "none", U if dtype == "f32" else 2.0 ** -8, group)
+    rg, lay = B.RowGroups(n, G), B.Linear(n, K, N, dt, num_groups=G)
+    rg.build(torch.from_numpy(group).cuda())
+    y, dx, dw, db = torch.empty_like(dy), torch.empty_like(x), torch.full_like(w, float("nan")), torch.full((G, N), float("nan"), dtype=dt, device="cuda")
+    lay.workspace = B._workspace(lay._bytes(n)).view(torch.uint8).fill_(0xFF)      # NaN wherever nothing is written
+    lay.forward(x, w, y, groups=rg)
+    lay.backward(dy, x, w, dx=dx, dweight=dw, dbias=db, groups=rg)
+    want = ref.gradients(dy64, True)
+    close("y", y, ref.y, ref.y_bound)
+    close("dx", dx, *want["dx"])
+    close("dweight", dw, *want["dweight"])
+    close("dbias", db, *want["dbias"])
+
+
 def test_no_rows(torch, B):
     for groups in (0, 3):
         lay = B.Linear(0, 8, 5, torch.float32, "relu", "none", groups)
