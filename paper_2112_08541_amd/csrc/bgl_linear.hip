@@ -165,8 +165,8 @@ __device__ __forceinline__ Span find_span(const Groups &q, int64_t n, int classe
     return s;
 }
 
-// The groups' rows in units of unit_rows (a group's last may be short): those of the groups before g, g's own, all.
-__device__ __forceinline__ void count_units(const Groups &q, int64_t n, int unit_rows, int g, int64_t &before, int &own, int64_t &all)
+// The rows of the first `classes` groups in units of unit_rows (a group's last may be short): those of the groups before g, g's own, all.
+__device__ __forceinline__ void count_units(const Groups &q, int64_t n, int classes, int unit_rows, int g, int64_t &before, int &own, int64_t &all)
 {
     if (q.groups == 0) {
         before = 0;
@@ -176,9 +176,9 @@ __device__ __forceinline__ void count_units(const Groups &q, int64_t n, int unit
     const int lane = threadIdx.x & 63;
     before = all = 0;
     own = 0;
-    for (int g0 = 0; g0 < q.groups; g0 += 64) {
+    for (int g0 = 0; g0 < classes; g0 += 64) {
         int64_t lo = 0, hi = 0;
-        if (g0 + lane < q.groups) group_range(q, n, g0 + lane, lo, hi);
+        if (g0 + lane < classes) group_range(q, n, g0 + lane, lo, hi);
         const int units = (int)((hi - lo + unit_rows - 1) / unit_rows);
         const int upto = wave_incl_scan(units);
         if (g >= g0 && g < g0 + 64) {
@@ -440,25 +440,95 @@ __global__ __launch_bounds__(kThreads * TEAMS, 2) void k_linear_rows(RowsArgs<T>
 }
 
 // ----------------------------------------------------------------- dz
+constexpr int kUnit = 64;
+
+// No share is empty (rows of no group make units fewer than the host can know), so every slot between a group's first and last is written.
+__device__ __forceinline__ int64_t shares_of(int64_t units, int planned) { return units < planned ? units : planned; }
+
+// dz of all rows, in group order, and the sums of its columns before they are rounded (bf16: sums of rounded values would be off by as much again as
+// the result's own rounding).  The rows, in units of kUnit, are dealt evenly to `shares` workgroups; share w leaves its sums for group g in slot
+// w + g of `part`.  A thread has VEC neighbouring columns, kDzColumns of a workgroup's rows at a time at most (blockIdx.y: which).
+constexpr int kDzColumns = 2048;
+
 template <class T>
-__global__ __launch_bounds__(kThreads) void k_linear_dz(int act, const typename T::elem *dy, int64_t dy_stride, const typename T::elem *saved,
-                                                        int64_t saved_stride, typename T::elem *dz, int64_t dz_stride, int64_t n, int N)
+struct DzArgs {
+    const typename T::elem *dy, *saved;
+    typename T::elem *dz;
+    float *part;  // null: no sums
+    int64_t n, dy_stride, saved_stride, dz_stride;
+    int N, act, shares, classes;
+    Groups q;
+};
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_linear_dz(DzArgs<T> a)
 {
     constexpr int V = T::VEC;
-    const int per_row = (N + V - 1) / V;
-    const int64_t total = n * per_row;
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
-        const int64_t r = i / per_row;
-        const int c = (int)(i % per_row) * V, left = N - c;
-        float d[V], z[V];
-        load_cols<T, V>(dy + r * dy_stride + c, left, d);
-        if (act) {
-            const auto piece = load_cols_upto<T, V>(saved + r * saved_stride + c, left);
+    constexpr int COLUMNS = kThreads * V < kDzColumns ? kThreads * V : kDzColumns;
+    __shared__ float sums[kThreads * V];
+    const int first = blockIdx.y * COLUMNS, width = a.N - first < COLUMNS ? a.N - first : COLUMNS, per_row = (width + V - 1) / V, rows = kThreads / per_row;
+    const int lane_row = threadIdx.x / per_row, c = first + (int)(threadIdx.x % per_row) * V, left = a.N - c;
+    const bool idle = lane_row >= rows;
+    int64_t before, units;
+    int own;
+    count_units(a.q, a.n, a.classes, kUnit, 0, before, own, units);
+    const int64_t shares = shares_of(units, a.shares), share = blockIdx.x;
+    if (share >= shares) return;
+    const int64_t last = (share + 1) * units / shares;
+    for (int64_t unit = share * units / shares; unit < last;) {
+        const Span s = find_span(a.q, a.n, a.classes, kUnit, unit);
+        int64_t lo = 0, hi = a.n;
+        if (a.q.groups > 0) group_range(a.q, a.n, s.group, lo, hi);
+        hi = uniform((int)hi);
+        const int64_t room = (last - unit) * kUnit, end = hi - s.start < room ? hi : s.start + room;
+        unit += (end - s.start + kUnit - 1) / kUnit;
+        float sum[V] = {};
+        const auto all = [&](auto whole) {  // whole: N is a multiple of VEC
+            constexpr int BATCH = 4;        // rows whose loads are on their way together
+            using Piece = Cols<T, V>;
+            for (int64_t at = s.start + lane_row; at < end; at += BATCH * rows) {
+                int32_t r[BATCH];
+                Piece d[BATCH], z[BATCH];
 #pragma unroll
-            for (int e = 0; e < V; ++e) z[e] = kept<T>(act, piece.e[e]);
-            times_slope(act, z, d);
+                for (int p = 0; p < BATCH; ++p) {
+                    const int64_t here = at + p * rows;
+                    r[p] = row_at(a.q, a.n, here < end ? here : end - 1);
+                    if (here >= end) r[p] = -1;
+                }
+#pragma unroll
+                for (int p = 0; p < BATCH; ++p) {
+                    const int64_t from = r[p] < 0 ? 0 : r[p];
+                    d[p] = decltype(whole)::value ? load_any<Piece>(a.dy + from * a.dy_stride + c) : load_cols_upto<T, V>(a.dy + from * a.dy_stride + c, left);
+                    if (a.act) z[p] = decltype(whole)::value ? load_any<Piece>(a.saved + from * a.saved_stride + c) : load_cols_upto<T, V>(a.saved + from * a.saved_stride + c, left);
+                }
+#pragma unroll
+                for (int p = 0; p < BATCH; ++p) {
+                    float dv[V], zv[V];
+#pragma unroll
+                    for (int e = 0; e < V; ++e) dv[e] = T::get(d[p].e[e]), zv[e] = a.act ? kept<T>(a.act, z[p].e[e]) : 0.0f;
+                    times_slope(a.act, zv, dv);
+                    if (r[p] < 0) continue;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) sum[e] += dv[e];
+                    store_cols<T, V>(a.dz + r[p] * a.dz_stride + c, decltype(whole)::value ? V : left, dv);
+                }
+            }
+        };
+        if (!idle) {
+            if (a.N % V == 0) all(std::true_type{});
+            else all(std::false_type{});
         }
-        store_cols<T, V>(dz + r * dz_stride + c, left, d);
+        if (a.part && s.group < (a.q.groups ? a.q.groups : 1)) {
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < V; ++e) sums[threadIdx.x * V + e] = sum[e];
+            __syncthreads();
+            for (int i = threadIdx.x; i < width; i += kThreads) {
+                float v = 0.0f;
+                for (int r = 0; r < rows; ++r) v += sums[r * per_row * V + i];
+                a.part[(share + s.group) * a.N + first + i] = v;
+            }
+        }
     }
 }
 
@@ -467,17 +537,12 @@ __global__ __launch_bounds__(kThreads) void k_linear_dz(int act, const typename 
 // and begin the next, so that no workgroup has more than its part however the sizes fall.  Share w leaves its sums for group g in slot w + g
 // of `part` (both grow along the rows, so no two meet in a slot): A_dim * B_dim of the matrix, then out_dim of db.
 // Side A is the wider of dz and x, side B the narrower; the matrix is laid out [A][B].
-constexpr int kUnit = 64;
-
-// No share is empty (rows of no group make units fewer than the host can know), so every slot between a group's first and last is written.
-__device__ __forceinline__ int64_t shares_of(int64_t units, int planned) { return units < planned ? units : planned; }
-
 template <class T>
 struct WeightArgs {
     const typename T::elem *a, *b;
     float *part;
     int64_t n, a_stride, b_stride;
-    int a_dim, b_dim, shares, a_tiles, b_tiles;
+    int a_dim, b_dim, N, shares, a_tiles, b_tiles;
     int bias;  // which side is dz, if db is asked for: 1 A, 2 B, else 0
     Groups q;
 };
@@ -496,7 +561,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_linear_dw(WeightArgs<T> a)
     const int a0 = tile / a.b_tiles * C::BA, b0 = tile % a.b_tiles * C::BB;
     int64_t before, units;
     int own;
-    count_units(a.q, a.n, kUnit, 0, before, own, units);
+    count_units(a.q, a.n, a.q.groups, kUnit, 0, before, own, units);
     const int64_t shares = shares_of(units, a.shares);
     if (share >= shares) return;
     const int64_t last = (share + 1) * units / shares;
@@ -506,7 +571,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_linear_dw(WeightArgs<T> a)
     right.init(a.b, a.b_stride, a.n, b0, a.b_dim);
     // dz's columns are summed from the fragments, by the wavefronts whose tiles are the first of their rows or columns
     const bool bias_a = a.bias == 1 && b0 == 0 && uniform(C::b_off()) == 0, bias_b = a.bias == 2 && a0 == 0 && uniform(C::a_off()) == 0;
-    const int64_t len = (int64_t)a.a_dim * a.b_dim + (a.bias == 2 ? a.b_dim : a.a_dim);
+    const int64_t len = (int64_t)a.a_dim * a.b_dim + a.N;
     for (int64_t unit = share * units / shares; unit < last;) {
         const Span s = find_span(a.q, a.n, a.q.groups, kUnit, unit);
         int64_t lo = 0, hi = a.n;
@@ -583,8 +648,9 @@ template <class T>
 struct ReduceArgs {
     const float *part;
     typename T::elem *dw, *db;
+    const float *dz_part;  // db's parts, if the dz kernel made them: [slot][N]
     int64_t n;
-    int N, K, shares;
+    int N, K, shares, dz_shares, dz_classes, matrix_blocks;
     bool swapped;  // the parts' matrix is [K][N]
     Groups q;
 };
@@ -596,7 +662,22 @@ __global__ __launch_bounds__(kThreads) void k_linear_reduce(ReduceArgs<T> a)
     const int g = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x / kWave;
     int64_t before, units;
     int own;
-    count_units(a.q, a.n, kUnit, g, before, own, units);
+    if ((int)blockIdx.x >= a.matrix_blocks) {  // db
+        count_units(a.q, a.n, a.dz_classes, kUnit, g, before, own, units);
+        const int c = ((int)blockIdx.x - a.matrix_blocks) * 64 + lane;
+        float v = 0.0f;
+        if (c < a.N && own > 0) {
+            const int64_t shares = shares_of(units, a.dz_shares), first = ((before + 1) * shares - 1) / units, last = ((before + own) * shares - 1) / units;
+#pragma unroll 8
+            for (int64_t w = first + wave; w <= last; w += kThreads / kWave) v += a.dz_part[(w + g) * a.N + c];
+        }
+        float *column = reinterpret_cast<float *>(sums);
+        column[threadIdx.x] = v;
+        __syncthreads();
+        if (wave == 0 && c < a.N) a.db[(int64_t)g * a.N + c] = T::put(column[lane] + column[64 + lane] + column[128 + lane] + column[192 + lane]);
+        return;
+    }
+    count_units(a.q, a.n, a.q.groups, kUnit, g, before, own, units);
     const int64_t NK = (int64_t)a.N * a.K, len = NK + a.N, e = ((int64_t)blockIdx.x * 64 + lane) * 4;
     const int left = len - e < 4 ? (int)(len - e) : 4;
     float v[4] = {};
@@ -621,7 +702,7 @@ __global__ __launch_bounds__(kThreads) void k_linear_reduce(ReduceArgs<T> a)
     for (int u = 0; u < left; ++u) {
         const int64_t at = e + u;
         if (at >= NK) {
-            if (a.db) a.db[(int64_t)g * a.N + at - NK] = T::put(v[u]);
+            if (a.db && !a.dz_part) a.db[(int64_t)g * a.N + at - NK] = T::put(v[u]);
         } else {
             a.dw[g * NK + (a.swapped ? at % a.N * a.K + at / a.N : at)] = T::put(v[u]);
         }
@@ -845,7 +926,9 @@ struct WeightPlan {
     bool swapped, large;
     int a_dim, b_dim, a_tiles, b_tiles, shares;
     int64_t slots;
-    size_t dz_bytes, dz_stride, part_bytes;
+    bool sums_with_dz;  // db comes from the dz kernel
+    int dz_shares;
+    size_t dz_bytes, dz_stride, part_bytes, dz_part_bytes, bytes;
 };
 
 WeightPlan plan_weight(const bgl_linear_t *l, int64_t n)
@@ -865,7 +948,13 @@ WeightPlan plan_weight(const bgl_linear_t *l, int64_t n)
     const int per = 16 / elem_bytes(l);
     p.dz_stride = round_up(l->out_dim, per);
     p.dz_bytes = l->activation == BGL_ACT_NONE ? 0 : round_up((size_t)n * p.dz_stride * elem_bytes(l), 256);
-    p.part_bytes = (size_t)p.slots * ((size_t)l->out_dim * l->in_dim + l->out_dim) * sizeof(float);
+    p.part_bytes = round_up((size_t)p.slots * ((size_t)l->out_dim * l->in_dim + l->out_dim) * sizeof(float), 256);
+    // some eight workgroups on each CU for dz, fewer where rows are so wide that their sums would count
+    const int64_t dz_most = l->out_dim > 512 ? (1 << 20) / l->out_dim : 2048;
+    p.dz_shares = (int)(most < dz_most ? most : dz_most);
+    p.sums_with_dz = l->dtype == BGL_BF16 && (l->activation == BGL_ACT_GELU || l->activation == BGL_ACT_SILU);
+    p.dz_part_bytes = p.sums_with_dz ? (size_t)(p.dz_shares + l->num_groups) * l->out_dim * sizeof(float) : 0;
+    p.bytes = p.dz_bytes + p.part_bytes + p.dz_part_bytes;
     return p;
 }
 
@@ -906,32 +995,31 @@ int forward(const bgl_linear_t *l, int64_t n, const Groups &q, const void *x, in
 }
 
 template <class T>
-int launch_dz(int act, const void *dy, int64_t dy_stride, const void *saved, int64_t saved_stride, void *dz, int64_t dz_stride, int64_t n, int N, hipStream_t st)
-{
-    using E = typename T::elem;
-    const int64_t total = n * ceil_div(N, T::VEC), blocks = ceil_div(total, kThreads);
-    const dim3 grid((unsigned)(blocks < 8192 ? blocks : 8192)), block(kThreads);
-    k_linear_dz<T><<<grid, block, 0, st>>>(act, (const E *)dy, dy_stride, (const E *)saved, saved_stride, (E *)dz, dz_stride, n, N);
-    BGL_HIP(hipGetLastError());
-    return BGL_OK;
-}
-
-template <class T>
 int backward(const bgl_linear_t *l, int64_t n, const Groups &q, const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, const void *weight,
              const void *saved, int64_t saved_stride, void *dx, int64_t dx_stride, void *dweight, void *dbias, void *dresidual,
              int64_t dresidual_stride, void *workspace, hipStream_t st)
 {
     using E = typename T::elem;
     const WeightPlan p = plan_weight(l, n);
-    const int classes = l->num_groups > 0 ? l->num_groups : 1;
+    const int classes = l->num_groups > 0 ? l->num_groups : 1, dz_classes = l->num_groups > 0 ? l->num_groups + 1 : 0;
     const void *dz = dy;
     int64_t dz_stride = dy_stride;
+    float *dz_part = p.sums_with_dz && dbias ? reinterpret_cast<float *>((char *)workspace + p.dz_bytes + p.part_bytes) : nullptr;
     // dz is made where dx first needs it if a tile of dx has all its columns (128 at most): every column tile would make it again
-    const bool act = l->activation != BGL_ACT_NONE, together = act && dx && n > 0 && l->in_dim <= Large::BB;
+    const bool act = l->activation != BGL_ACT_NONE, together = act && dx && n > 0 && l->in_dim <= Large::BB && !dz_part;
     if (n > 0 && (dresidual || act)) {
         void *to = dresidual ? dresidual : workspace;
         dz_stride = dresidual ? dresidual_stride : (int64_t)p.dz_stride;
-        if (!together) BGL_TRY(launch_dz<T>(l->activation, dy, dy_stride, saved, saved_stride, to, dz_stride, n, l->out_dim, st));
+        if (!together) {
+            DzArgs<T> a{};
+            a.dy = (const E *)dy, a.saved = (const E *)saved, a.dz = (E *)to, a.part = dz_part;
+            a.n = n, a.dy_stride = dy_stride, a.saved_stride = saved_stride, a.dz_stride = dz_stride;
+            a.N = l->out_dim, a.act = l->activation, a.shares = p.dz_shares, a.classes = dz_classes;
+            a.q = q;
+            const int columns = kThreads * T::VEC < kDzColumns ? kThreads * T::VEC : kDzColumns;
+            k_linear_dz<T><<<dim3((unsigned)p.dz_shares, (unsigned)ceil_div(l->out_dim, columns)), dim3(kThreads), 0, st>>>(a);
+            BGL_HIP(hipGetLastError());
+        }
         dz = to;
     }
     if (dx && n > 0) {
@@ -954,8 +1042,8 @@ int backward(const bgl_linear_t *l, int64_t n, const Groups &q, const void *dy, 
             WeightArgs<T> a{};
             a.a = (const E *)(p.swapped ? x : dz), a.b = (const E *)(p.swapped ? dz : x);
             a.a_stride = p.swapped ? x_stride : dz_stride, a.b_stride = p.swapped ? dz_stride : x_stride;
-            a.part = part, a.n = n, a.a_dim = p.a_dim, a.b_dim = p.b_dim, a.shares = p.shares, a.a_tiles = p.a_tiles, a.b_tiles = p.b_tiles;
-            a.bias = p.swapped ? 2 : 1;
+            a.part = part, a.n = n, a.a_dim = p.a_dim, a.b_dim = p.b_dim, a.N = l->out_dim, a.shares = p.shares, a.a_tiles = p.a_tiles, a.b_tiles = p.b_tiles;
+            a.bias = dz_part || !dbias ? 0 : p.swapped ? 2 : 1;
             a.q = q;
             const dim3 grid((unsigned)tile_count(p.shares, p.a_tiles * p.b_tiles)), block(kThreads);
             with_cut(p.large, p.b_dim, T::VEC, [&](auto cut, auto narrow) {
@@ -967,8 +1055,10 @@ int backward(const bgl_linear_t *l, int64_t n, const Groups &q, const void *dy, 
         ReduceArgs<T> r{};
         r.part = part, r.dw = (E *)dweight, r.db = (E *)dbias, r.n = n, r.N = l->out_dim, r.K = l->in_dim, r.shares = p.shares, r.swapped = p.swapped;
         r.q = q;
-        const int64_t len = (int64_t)l->out_dim * l->in_dim + l->out_dim;
-        k_linear_reduce<T><<<dim3((unsigned)ceil_div(len, 256), (unsigned)classes), dim3(kThreads), 0, st>>>(r);
+        r.dz_part = dz_part, r.dz_shares = p.dz_shares, r.dz_classes = dz_classes;
+        r.matrix_blocks = (int)ceil_div((int64_t)l->out_dim * l->in_dim + l->out_dim, 256);
+        const int blocks = r.matrix_blocks + (dz_part ? (int)ceil_div(l->out_dim, 64) : 0);
+        k_linear_reduce<T><<<dim3((unsigned)blocks, (unsigned)classes), dim3(kThreads), 0, st>>>(r);
         BGL_HIP(hipGetLastError());
     }
     return BGL_OK;
@@ -1006,7 +1096,7 @@ try {
     if (!bytes) BGL_FAIL(BGL_EINVAL, "bytes is null");
     BGL_TRY(check_layer(layer, n));
     const WeightPlan p = plan_weight(layer, n);
-    *bytes = p.dz_bytes + p.part_bytes;
+    *bytes = p.bytes;
     return BGL_OK;
 } BGL_NOTHROW_END
 
@@ -1048,10 +1138,9 @@ try {
     if (dbias && !dweight) BGL_FAIL(BGL_EINVAL, "dbias without dweight");
     if (!aligned(dweight, es) || !aligned(dbias, es)) BGL_FAIL(BGL_EINVAL, "dweight or dbias is misaligned");
     const WeightPlan p = plan_weight(layer, n);
-    if (p.dz_bytes + p.part_bytes > 0) {
+    if (p.bytes > 0) {
         if (!workspace || !aligned(workspace, 256)) BGL_FAIL(BGL_EINVAL, "workspace is null or not 256-byte aligned");
-        if (workspace_bytes < p.dz_bytes + p.part_bytes)
-            BGL_FAIL(BGL_ECAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, p.dz_bytes + p.part_bytes);
+        if (workspace_bytes < p.bytes) BGL_FAIL(BGL_ECAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, p.bytes);
     }
     const Groups q{offsets, rows, layer->num_groups};
     return layer->dtype == BGL_F32 ? backward<tile::F32>(layer, n, q, dy, dy_stride, x, x_stride, weight, saved, saved_stride, dx, dx_stride, dweight, dbias, dresidual, dresidual_stride, workspace, (hipStream_t)stream)
