@@ -655,7 +655,8 @@ struct ReduceArgs {
     Groups q;
 };
 
-template <class T>
+// SPLIT: the four wavefronts take the shares of 256 values in turn; else (many groups, a few shares each) 256 values each.
+template <class T, bool SPLIT>
 __global__ __launch_bounds__(kThreads) void k_linear_reduce(ReduceArgs<T> a)
 {
     __shared__ float4 sums[kThreads];
@@ -678,26 +679,28 @@ __global__ __launch_bounds__(kThreads) void k_linear_reduce(ReduceArgs<T> a)
         return;
     }
     count_units(a.q, a.n, a.q.groups, kUnit, g, before, own, units);
-    const int64_t NK = (int64_t)a.N * a.K, len = NK + a.N, e = ((int64_t)blockIdx.x * 64 + lane) * 4;
+    const int64_t NK = (int64_t)a.N * a.K, len = NK + a.N, e = ((SPLIT ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave) * 64 + lane) * 4;
     const int left = len - e < 4 ? (int)(len - e) : 4;
     float v[4] = {};
     if (left > 0 && own > 0) {
         const int64_t shares = shares_of(units, a.shares), first = ((before + 1) * shares - 1) / units, last = ((before + own) * shares - 1) / units;
 #pragma unroll 4
-        for (int64_t w = first + wave; w <= last; w += kThreads / kWave) {
+        for (int64_t w = first + (SPLIT ? wave : 0); w <= last; w += SPLIT ? kThreads / kWave : 1) {
             float p[4];
             load_cols<F32, 4>(a.part + (w + g) * len + e, left, p);
 #pragma unroll
             for (int u = 0; u < 4; ++u) v[u] += p[u];
         }
     }
-    sums[threadIdx.x] = float4{v[0], v[1], v[2], v[3]};
-    __syncthreads();
-    if (wave || left <= 0) return;
+    if constexpr (SPLIT) {
+        sums[threadIdx.x] = float4{v[0], v[1], v[2], v[3]};
+        __syncthreads();
+        if (wave) return;
 #pragma unroll
-    for (int w = 1; w < kThreads / kWave; ++w) {
-        const float4 o = sums[w * 64 + lane];
-        v[0] += o.x, v[1] += o.y, v[2] += o.z, v[3] += o.w;
+        for (int w = 1; w < kThreads / kWave; ++w) {
+            const float4 o = sums[w * 64 + lane];
+            v[0] += o.x, v[1] += o.y, v[2] += o.z, v[3] += o.w;
+        }
     }
     for (int u = 0; u < left; ++u) {
         const int64_t at = e + u;
@@ -1056,9 +1059,11 @@ int backward(const bgl_linear_t *l, int64_t n, const Groups &q, const void *dy, 
         r.part = part, r.dw = (E *)dweight, r.db = (E *)dbias, r.n = n, r.N = l->out_dim, r.K = l->in_dim, r.shares = p.shares, r.swapped = p.swapped;
         r.q = q;
         r.dz_part = dz_part, r.dz_shares = p.dz_shares, r.dz_classes = dz_classes;
-        r.matrix_blocks = (int)ceil_div((int64_t)l->out_dim * l->in_dim + l->out_dim, 256);
-        const int blocks = r.matrix_blocks + (dz_part ? (int)ceil_div(l->out_dim, 64) : 0);
-        k_linear_reduce<T><<<dim3((unsigned)blocks, (unsigned)classes), dim3(kThreads), 0, st>>>(r);
+        const bool split = p.shares > 8 * classes;  // more than two shares for each wavefront
+        r.matrix_blocks = (int)ceil_div((int64_t)l->out_dim * l->in_dim + l->out_dim, split ? 256 : 1024);
+        const dim3 grid((unsigned)(r.matrix_blocks + (dz_part ? (int)ceil_div(l->out_dim, 64) : 0)), (unsigned)classes);
+        if (split) k_linear_reduce<T, true><<<grid, dim3(kThreads), 0, st>>>(r);
+        else k_linear_reduce<T, false><<<grid, dim3(kThreads), 0, st>>>(r);
         BGL_HIP(hipGetLastError());
     }
     return BGL_OK;

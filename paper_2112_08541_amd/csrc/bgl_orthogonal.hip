@@ -531,19 +531,37 @@ size_t whole_bytes(int mp, int np)
     return bm * (bm + 1) / 2 <= kWholeWaves && bm * bn <= kWholeWaves * kWholeRounds && bytes + 1024 <= 160 * 1024 ? bytes : 0;
 }
 
-// Powers of two that keep X, P and Q below a quarter of fp16's largest value.  False: with these coefficients the steps lead out of bounds.
-bool scales(float a, float b, float c, int steps, OrthoArgs &o)
+// The largest |a s + b s^3 + c s^5| and |a + b s^2 + c s^4| for s in [0, most]: at the ends or where the slope is 0.
+void largest(double a, double b, double c, double most, double &p, double &q)
 {
-    double most_x = 1.0, most_q = 0.0;
-    for (int i = 0; i <= 4096; ++i) {
-        double s = i / 4096.0;
-        for (int k = 0; k < steps; ++k) {
-            const double q = a + b * s * s + c * s * s * s * s;
-            s *= q;
-            if (!(std::fabs(s) < 64.0) || !(std::fabs(q) < 4096.0)) return false;
-            most_x = std::fmax(most_x, std::fabs(s));
-            most_q = std::fmax(most_q, std::fabs(q));
-        }
+    p = q = 0.0;
+    const auto look = [&](double t) {  // t = s^2
+        if (!(t >= 0.0 && t <= most * most)) return;
+        const double v = std::fabs(a + b * t + c * t * t);
+        q = std::fmax(q, v);
+        p = std::fmax(p, v * std::sqrt(t));
+    };
+    look(0.0);
+    look(most * most);
+    look(-b / (2.0 * c));                                // of q
+    const double root = std::sqrt(9.0 * b * b - 20.0 * a * c);  // of p: a + 3 b t + 5 c t^2 = 0 (none: NaN, which look() leaves out)
+    look((-3.0 * b + root) / (10.0 * c));
+    look((-3.0 * b - root) / (10.0 * c));
+    look(-a / (3.0 * b));  // c = 0
+}
+
+// Powers of two that keep X, P and Q below a quarter of fp16's largest value.  False: with these coefficients the steps may lead out of bounds.
+bool scales(double a, double b, double c, int steps, OrthoArgs &o)
+{
+    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
+    double now = 1.0, most_x = 1.0, most_q = 0.0;
+    for (int k = 0; k < steps; ++k) {
+        double p, q;
+        largest(a, b, c, now, p, q);
+        if (!(p < 64.0) || !(q < 4096.0)) return false;
+        now = p;
+        most_x = std::fmax(most_x, p);
+        most_q = std::fmax(most_q, q);
     }
     const auto power = [](double most) { return (float)std::exp2(std::floor(std::log2(16384.0 / most))); };
     o.sx = power(most_x);
@@ -581,8 +599,9 @@ int check_matrices(int64_t batch, int32_t rows, int32_t cols, int32_t dtype)
 }
 
 // 128 x 128 tiles (half the reads) where most CUs have one and the sums are long enough to pay for the larger tile's ends, else 64 x 64; two
-// teams to a tile.  All five steps: 2 of 1024 x 2048 504 us with the larger tiles for Q X (1,024 long, 256 tiles), 528 without; 24 of 256 x 512 (256
-// long, 192 tiles) 211 and 202.  One team instead of two: 512 and 229; four: 551 and 210.
+// teams to a tile, four where the CUs have one tile at most and the sums are long.  All five steps: 2 of 1024 x 2048 468 us with the larger tiles for
+// Q X (1,024 long, 256 tiles), 500 without; 24 of 256 x 512 (256 long, 192 tiles) 185 and 176.  Four teams instead of two: 1 of 1024 x 1024 232 us
+// instead of 254, 4 of 400 x 800 (shorter sums) 214 instead of 195, 24 of 256 x 512 206 instead of 176.
 template <int STAGE, class T>
 void launch_product(const OrthoArgs &a, int from, hipStream_t st)
 {
@@ -594,12 +613,15 @@ void launch_product(const OrthoArgs &a, int from, hipStream_t st)
     };
     int rt, ct;
     const int64_t large = tiles(128, rt, ct);
-    if (large >= 192 && (STAGE == GRAM ? a.np : a.mp) >= 512) {
+    const int depth = STAGE == GRAM ? a.np : a.mp;
+    if (large >= 192 && depth >= 512) {
         k_ortho_product<4, STAGE, T, 2><<<dim3((unsigned)((large + 7) / 8 * 8)), dim3(2 * kThreads), 0, st>>>(a, from, rt, ct);
         return;
     }
     const int64_t small = tiles(64, rt, ct);
-    k_ortho_product<2, STAGE, T, 2><<<dim3((unsigned)((small + 7) / 8 * 8)), dim3(2 * kThreads), 0, st>>>(a, from, rt, ct);
+    const dim3 grid((unsigned)((small + 7) / 8 * 8));
+    if (small <= 256 && depth >= 640) k_ortho_product<2, STAGE, T, 4><<<grid, dim3(4 * kThreads), 0, st>>>(a, from, rt, ct);
+    else k_ortho_product<2, STAGE, T, 2><<<grid, dim3(2 * kThreads), 0, st>>>(a, from, rt, ct);
 }
 
 template <class T>
