@@ -665,17 +665,22 @@ __global__ __launch_bounds__(kThreads) void k_linear_reduce(ReduceArgs<T> a)
     int own;
     if ((int)blockIdx.x >= a.matrix_blocks) {  // db
         count_units(a.q, a.n, a.dz_classes, kUnit, g, before, own, units);
-        const int c = ((int)blockIdx.x - a.matrix_blocks) * 64 + lane;
+        constexpr int STRIPES = kThreads / 16;  // 16 columns to a workgroup: a large group's hundreds of shares are read 16 at a time
+        const int stripe = threadIdx.x / 16, c = ((int)blockIdx.x - a.matrix_blocks) * 16 + (threadIdx.x & 15);
         float v = 0.0f;
         if (c < a.N && own > 0) {
             const int64_t shares = shares_of(units, a.dz_shares), first = ((before + 1) * shares - 1) / units, last = ((before + own) * shares - 1) / units;
 #pragma unroll 8
-            for (int64_t w = first + wave; w <= last; w += kThreads / kWave) v += a.dz_part[(w + g) * a.N + c];
+            for (int64_t w = first + stripe; w <= last; w += STRIPES) v += a.dz_part[(w + g) * a.N + c];
         }
         float *column = reinterpret_cast<float *>(sums);
         column[threadIdx.x] = v;
         __syncthreads();
-        if (wave == 0 && c < a.N) a.db[(int64_t)g * a.N + c] = T::put(column[lane] + column[64 + lane] + column[128 + lane] + column[192 + lane]);
+        if (stripe || c >= a.N) return;
+        v = 0.0f;
+#pragma unroll
+        for (int i = 0; i < STRIPES; ++i) v += column[i * 16 + threadIdx.x];
+        a.db[(int64_t)g * a.N + c] = T::put(v);
         return;
     }
     count_units(a.q, a.n, a.q.groups, kUnit, g, before, own, units);
@@ -684,13 +689,18 @@ __global__ __launch_bounds__(kThreads) void k_linear_reduce(ReduceArgs<T> a)
     float v[4] = {};
     if (left > 0 && own > 0) {
         const int64_t shares = shares_of(units, a.shares), first = ((before + 1) * shares - 1) / units, last = ((before + own) * shares - 1) / units;
-#pragma unroll 4
-        for (int64_t w = first + (SPLIT ? wave : 0); w <= last; w += SPLIT ? kThreads / kWave : 1) {
-            float p[4];
-            load_cols<F32, 4>(a.part + (w + g) * len + e, left, p);
+        constexpr int STEP = SPLIT ? kThreads / kWave : 1;
+        const auto add = [&](auto whole) {
+#pragma unroll 8
+            for (int64_t w = first + (SPLIT ? wave : 0); w <= last; w += STEP) {
+                const float *from = a.part + (w + g) * len + e;
+                const auto p = decltype(whole)::value ? load_any<Cols<F32, 4>>(from) : load_cols_upto<F32, 4>(from, left);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) v[u] += p[u];
-        }
+                for (int u = 0; u < 4; ++u) v[u] += p.e[u];
+            }
+        };
+        if (left == 4) add(std::true_type{});
+        else add(std::false_type{});
     }
     if constexpr (SPLIT) {
         sums[threadIdx.x] = float4{v[0], v[1], v[2], v[3]};
@@ -952,10 +962,10 @@ WeightPlan plan_weight(const bgl_linear_t *l, int64_t n)
     p.dz_stride = round_up(l->out_dim, per);
     p.dz_bytes = l->activation == BGL_ACT_NONE ? 0 : round_up((size_t)n * p.dz_stride * elem_bytes(l), 256);
     p.part_bytes = round_up((size_t)p.slots * ((size_t)l->out_dim * l->in_dim + l->out_dim) * sizeof(float), 256);
-    // some eight workgroups on each CU for dz, fewer where rows are so wide that their sums would count
-    const int64_t dz_most = l->out_dim > 512 ? (1 << 20) / l->out_dim : 2048;
-    p.dz_shares = (int)(most < dz_most ? most : dz_most);
+    // eight workgroups on each CU for dz with its sums, fewer where rows are so wide that the sums would count, more without sums
     p.sums_with_dz = l->dtype == BGL_BF16 && (l->activation == BGL_ACT_GELU || l->activation == BGL_ACT_SILU);
+    const int64_t dz_most = !p.sums_with_dz ? 8192 : l->out_dim > 512 ? (1 << 20) / l->out_dim : 2048;
+    p.dz_shares = (int)(most < dz_most ? most : dz_most);
     p.dz_part_bytes = p.sums_with_dz ? (size_t)(p.dz_shares + l->num_groups) * l->out_dim * sizeof(float) : 0;
     p.bytes = p.dz_bytes + p.part_bytes + p.dz_part_bytes;
     return p;
@@ -1061,7 +1071,7 @@ int backward(const bgl_linear_t *l, int64_t n, const Groups &q, const void *dy, 
         r.dz_part = dz_part, r.dz_shares = p.dz_shares, r.dz_classes = dz_classes;
         const bool split = p.shares > 8 * classes;  // more than two shares for each wavefront
         r.matrix_blocks = (int)ceil_div((int64_t)l->out_dim * l->in_dim + l->out_dim, split ? 256 : 1024);
-        const dim3 grid((unsigned)(r.matrix_blocks + (dz_part ? (int)ceil_div(l->out_dim, 64) : 0)), (unsigned)classes);
+        const dim3 grid((unsigned)(r.matrix_blocks + (dz_part ? (int)ceil_div(l->out_dim, 16) : 0)), (unsigned)classes);
         if (split) k_linear_reduce<T, true><<<grid, dim3(kThreads), 0, st>>>(r);
         else k_linear_reduce<T, false><<<grid, dim3(kThreads), 0, st>>>(r);
         BGL_HIP(hipGetLastError());
