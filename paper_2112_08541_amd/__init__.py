@@ -9,7 +9,7 @@ without the HIP library being loaded.
 """
 import importlib
 
-__all__ = ["binding", "inputs", "buildlib", "pipeline"]
+__all__ = ["binding", "inputs", "buildlib", "pipeline", "sage"]
 
 
 def __getattr__(name):
