@@ -33,11 +33,12 @@ struct OrthoArgs {
     int64_t in_matrix, in_row, out_matrix, out_row;  // strides in values
     int64_t batch;
     int m, n, mp, np;           // m <= n; padded to whole blocks of 32
+    int lm, ln;                 // dwords from one split row to the next, of P and Q and of X
     bool tall;                  // the update has n rows and m columns
     float a, b, c, eps;
     float sx, sp, sq;           // what X, P and Q are scaled by
     double *norms;              // [batch][kNormParts]
-    uint32_t *x[2], *p, *q;     // split rows: [m][np], [m][mp], [m][mp] per matrix
+    uint32_t *x[2], *p, *q;     // split rows: [m][ln], [m][lm], [m][lm] per matrix
 };
 
 __device__ __forceinline__ void split(float v, uint16_t &hi, uint16_t &lo)
@@ -122,10 +123,10 @@ __global__ __launch_bounds__(kThreads) void k_ortho_start(OrthoArgs a)
         tile[r][c] = v * a.sx;
     }
     __syncthreads();
-    uint32_t *x = a.x[0] + matrix * a.m * a.np;
+    uint32_t *x = a.x[0] + matrix * a.m * a.ln;
     for (int i = threadIdx.x; i < 64 * 16; i += kThreads) {
         const int s = i / 16, f = i % 16 * 4;
-        if (r0 + s < a.m && c0 + f < a.np) store_split<4>(x + (int64_t)(r0 + s) * a.np, c0 + f, {tile[s][f], tile[s][f + 1], tile[s][f + 2], tile[s][f + 3]});
+        if (r0 + s < a.m && c0 + f < a.np) store_split<4>(x + (int64_t)(r0 + s) * a.ln, c0 + f, {tile[s][f], tile[s][f + 1], tile[s][f + 2], tile[s][f + 3]});
     }
 }
 
@@ -153,11 +154,11 @@ struct SplitColumns {
     const uint32_t *base;
     int stride, rows;
     uint4 reg[PASSES];
-    __device__ __forceinline__ void init(const uint32_t *x, int np, int m, int c0)
+    __device__ __forceinline__ void init(const uint32_t *x, int np, int ld, int m, int c0)
     {
         const int c = c0 + team_thread() % PER_ROW * 4;
         base = x + (c < np ? c : 0);  // (a dword of a split row for each column)
-        stride = np;
+        stride = ld;
         rows = m;
     }
     __device__ __forceinline__ void load_whole(int tile)
@@ -222,18 +223,18 @@ __global__ __launch_bounds__(kThreads * TEAMS, 2) void k_ortho_product(OrthoArgs
     } else {
         ct = t / row_tiles, rt = t % row_tiles;
     }
-    const int64_t mm = matrix * a.m * a.mp, mn = matrix * a.m * a.np;
+    const int64_t mm = matrix * a.m * a.lm, mn = matrix * a.m * a.ln;
     const uint32_t *left = STAGE == GRAM ? a.x[from] + mn : STAGE == POLY ? a.p + mm : a.q + mm;
     const uint32_t *right = STAGE == GRAM ? left : STAGE == POLY ? left : a.x[from] + mn;
-    const int K = STAGE == GRAM ? a.np : a.mp, cols = SYMMETRIC ? a.m : a.n;
+    const int K = STAGE == GRAM ? a.np : a.mp, ld = STAGE == GRAM ? a.ln : a.lm, cols = SYMMETRIC ? a.m : a.n;
     const int r0 = rt * BO, c0 = ct * BO;
     using Op = KcOperand<F32, BO>;  // (its 32 dwords are 32 pairs of halves here)
     using Right = std::conditional_t<SYMMETRIC, Op, SplitColumns<BO>>;
     Op l;
     Right r;
-    l.init([&](int i) { return reinterpret_cast<const float *>(left) + (int64_t)(r0 + i < a.m ? r0 + i : a.m - 1) * K; });
-    if constexpr (SYMMETRIC) r.init([&](int i) { return reinterpret_cast<const float *>(right) + (int64_t)(c0 + i < cols ? c0 + i : cols - 1) * K; });
-    else r.init(right, a.np, a.m, c0);
+    l.init([&](int i) { return reinterpret_cast<const float *>(left) + (int64_t)(r0 + i < a.m ? r0 + i : a.m - 1) * ld; });
+    if constexpr (SYMMETRIC) r.init([&](int i) { return reinterpret_cast<const float *>(right) + (int64_t)(c0 + i < cols ? c0 + i : cols - 1) * ld; });
+    else r.init(right, a.np, a.ln, a.m, c0);
     f32x4 acc[TT][TT] = {};
     const int team = threadIdx.x / kThreads, depth = K / kDwords;
     uint32_t *mine = lds + team * 2 * Op::LDS;
@@ -276,7 +277,7 @@ __global__ __launch_bounds__(kThreads * TEAMS, 2) void k_ortho_product(OrthoArgs
             f32x4 v = *at;
             float w[4];
             float p[4] = {};
-            if (STAGE == POLY) joined4(a.p + mm + (int64_t)(r0 + r) * a.mp, c0 + c, p);
+            if (STAGE == POLY) joined4(a.p + mm + (int64_t)(r0 + r) * a.lm, c0 + c, p);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 v[e] *= scale;
@@ -284,7 +285,7 @@ __global__ __launch_bounds__(kThreads * TEAMS, 2) void k_ortho_product(OrthoArgs
                 v[e] = w[e] = c0 + c + e < a.m ? v[e] * (STAGE == GRAM ? a.sp : a.sq) : 0.0f;
             }
             if (rt != ct) *at = v;
-            store_split<4>(to + (int64_t)(r0 + r) * a.mp, c0 + c, w);
+            store_split<4>(to + (int64_t)(r0 + r) * a.lm, c0 + c, w);
         }
         if (rt == ct) return;
         __syncthreads();
@@ -294,7 +295,7 @@ __global__ __launch_bounds__(kThreads * TEAMS, 2) void k_ortho_product(OrthoArgs
             float w[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) w[e] = r0 + r + e < a.m ? sums[result_place<BO>(r + e, c)] : 0.0f;
-            store_split<4>(to + (int64_t)(c0 + c) * a.mp, r0 + r, w);
+            store_split<4>(to + (int64_t)(c0 + c) * a.lm, r0 + r, w);
         }
     } else if constexpr (STAGE == APPLY) {
         for (int i = threadIdx.x; i < BO * FOURS; i += THREADS) {
@@ -304,7 +305,7 @@ __global__ __launch_bounds__(kThreads * TEAMS, 2) void k_ortho_product(OrthoArgs
             float w[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) w[e] = c0 + c + e < a.n ? v[e] * scale * a.sx : 0.0f;
-            store_split<4>(a.x[from ^ 1] + mn + (int64_t)(r0 + r) * a.np, c0 + c, w);
+            store_split<4>(a.x[from ^ 1] + mn + (int64_t)(r0 + r) * a.ln, c0 + c, w);
         }
     } else {
         typename T::elem *out = (typename T::elem *)a.out + matrix * a.out_matrix;
@@ -571,7 +572,7 @@ bool scales(double a, double b, double c, int steps, OrthoArgs &o)
 }
 
 struct OrthoSizes {
-    int m, n, mp, np;
+    int m, n, mp, np, lm, ln;
     size_t norms, x, p, total;
 };
 
@@ -583,8 +584,12 @@ OrthoSizes ortho_sizes(int64_t batch, int32_t rows, int32_t cols)
     s.mp = (int)round_up(s.m, 32);
     s.np = (int)round_up(s.n, 32);
     s.norms = round_up((size_t)batch * kNormParts * sizeof(double), 256);
-    s.x = round_up((size_t)batch * s.m * s.np * 4, 256);
-    s.p = round_up((size_t)batch * s.m * s.mp * 4, 256);
+    // Rows an odd number of 256 bytes apart, so that the 128 bytes a tile reads of each of its rows lie in different channels of the L2 (1 of 1280 x
+    // 1280: rows 5,120 bytes apart 345 us, 5,376 apart 319; 20 of 160 x 640 166 and 154; others within 2 %).
+    s.lm = (int)round_up(s.mp + 64, 128) - 64;
+    s.ln = (int)round_up(s.np + 64, 128) - 64;
+    s.x = round_up((size_t)batch * s.m * s.ln * 4, 256);
+    s.p = round_up((size_t)batch * s.m * s.lm * 4, 256);
     s.total = s.norms + 2 * (s.x + s.p);
     return s;
 }
@@ -683,7 +688,7 @@ try {
     if (!scales(a.a, a.b, a.c, steps, a)) BGL_FAIL(BGL_EUNSUPPORTED, "with coefficients %g, %g, %g the singular values grow out of bounds", a.a, a.b, a.c);
     a.update = update, a.out = out;
     a.in_matrix = update_matrix_stride, a.in_row = update_row_stride, a.out_matrix = out_matrix_stride, a.out_row = out_row_stride;
-    a.batch = batch, a.m = s.m, a.n = s.n, a.mp = s.mp, a.np = s.np, a.tall = rows > cols;
+    a.batch = batch, a.m = s.m, a.n = s.n, a.mp = s.mp, a.np = s.np, a.lm = s.lm, a.ln = s.ln, a.tall = rows > cols;
     char *at = (char *)workspace;
     a.norms = (double *)at, at += s.norms;
     for (int i = 0; i < 2; ++i) a.x[i] = (uint32_t *)at, at += s.x;
