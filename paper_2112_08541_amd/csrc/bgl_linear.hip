@@ -973,13 +973,14 @@ WeightPlan plan_weight(const bgl_linear_t *l, int64_t n)
 
 // 128 rows to a tile where such tiles are enough for the 256 CUs, else 64, with four teams: few workgroups then wait for their loads once instead
 // of once for each tile of the summed index.
+bool large_tiles(int64_t n, int64_t cols) { return ceil_div(n, 128) * ceil_div(cols, 128) >= 256; }
+
 template <class T, bool B_OC, bool DZ>
 int launch_rows(RowsArgs<T> &a, hipStream_t st)
 {
     const int64_t extra = a.q.groups > 0 ? (a.q.groups + 1 < a.n ? a.q.groups + 1 : a.n) : 1;
-    const bool large = ceil_div(a.n, 128) * ceil_div(a.N, 128) >= 256;
     int64_t blocks = 0;
-    with_cut(large, a.N, T::VEC, [&](auto cut, auto narrow) {
+    with_cut(large_tiles(a.n, a.N), a.N, T::VEC, [&](auto cut, auto narrow) {
         using C = decltype(cut);
         constexpr int TEAMS = C::BA == 64 ? 4 : 1;
         a.row_tiles = a.n / C::BA + extra;
@@ -1018,8 +1019,10 @@ int backward(const bgl_linear_t *l, int64_t n, const Groups &q, const void *dy, 
     const void *dz = dy;
     int64_t dz_stride = dy_stride;
     float *dz_part = p.sums_with_dz && dbias ? reinterpret_cast<float *>((char *)workspace + p.dz_bytes + p.part_bytes) : nullptr;
-    // dz is made where dx first needs it if a tile of dx has all its columns (128 at most): every column tile would make it again
-    const bool act = l->activation != BGL_ACT_NONE, together = act && dx && n > 0 && l->in_dim <= Large::BB && !dz_part;
+    // dz is made where dx first needs it if dx has 128 columns at most: every column tile makes it again.  Not where dz takes dy's place and few rows
+    // have tiles of 64 columns: the second column's tile may still be reading the dy that the first one replaces.
+    const bool act = l->activation != BGL_ACT_NONE, alone = large_tiles(n, l->in_dim) || l->in_dim <= Small::BB;
+    const bool together = act && dx && n > 0 && l->in_dim <= Large::BB && !dz_part && (alone || dresidual != dy);
     if (n > 0 && (dresidual || act)) {
         void *to = dresidual ? dresidual : workspace;
         dz_stride = dresidual ? dresidual_stride : (int64_t)p.dz_stride;

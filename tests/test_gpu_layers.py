@@ -372,6 +372,27 @@ def test_residual_may_be_the_output_and_dz_may_be_dy(torch, B):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("dtype,act", [("f32", "silu"), ("f32", "relu"), ("bf16", "relu"), ("bf16", "gelu")])
+@pytest.mark.parametrize("n,K,N,groups", [(700, 100, 300, 0), (5485, 128, 520, 0), (900, 65, 260, 4), (33_000, 128, 70, 0)])
+def test_dz_in_the_place_of_dy_where_dx_has_more_than_one_tile_of_columns(torch, B, dtype, act, n, K, N, groups):
+    dt, G = dtype_of(torch, dtype), max(groups, 1)
+    x, w, dy = (torch.randn(s, device="cuda").to(dt) for s in ((n, K), (G, N, K), (n, N)))
+    w = w if groups else w[0]
+    rg = None
+    if groups:
+        rg = B.RowGroups(n, groups)
+        rg.build(torch.randint(-1, groups, (n,), dtype=torch.int32, device="cuda"))
+    lay = B.Linear(n, K, N, dt, act, "before", groups)
+    y, saved, dr = (torch.empty((n, N), dtype=dt, device="cuda") for _ in range(3))
+    lay.forward(x, w, y, residual=dy, saved=saved, groups=rg)
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    lay.backward(dy, x, w, saved, dx, dw, dresidual=dr, groups=rg)
+    d2, dx2, dw2 = dy.clone(), torch.empty_like(dx), torch.empty_like(dw)
+    lay.backward(d2, x, w, saved, dx2, dw2, dresidual=d2, groups=rg)
+    for a, b in ((dr, d2), (dx, dx2), (dw, dw2)):
+        assert torch.equal(a, b)
+
+
 def test_another_stream_than_the_current_one(torch, B):
     s = torch.cuda.Stream()
     run_layer(torch, B, "bf16", 3000, 100, 72, "gelu", "before", seed=12, stream=s)
