@@ -792,6 +792,7 @@ int bgl_linear_forward(const bgl_linear_t *layer, int64_t n, const int32_t *rows
  *   dresidual   receives dz; only for BGL_RESIDUAL_BEFORE (behind the activation the
  *               residual's gradient is dy itself).  May be dy itself.
  *   workspace   device, 256-byte aligned, >= bgl_linear_workspace_bytes(layer, n)
+ * No output may overlap an input (but dresidual dy, with its stride) or another output.
  * Gradients are written, not added to.  Rows of no group: dx = 0, nothing of them in
  * dweight and dbias; a group without rows has dweight = dbias = 0.  The order of the sums is
  * fixed by n, the sizes and the groups: repeated calls give the same bits.

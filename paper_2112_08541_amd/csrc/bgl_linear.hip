@@ -239,6 +239,18 @@ __device__ __forceinline__ void store_cols(typename T::elem *p, int left, const 
 // ----------------------------------------------------------------- forward, and dx
 // One kernel for both: rows (n x K) times a weight whose summed index is contiguous (forward: out_dim x in_dim, B_OC false) or is
 // not (dx: the summed index is out_dim, B_OC true).
+//
+// A workgroup makes one tile of the result from operands staged through 32 KB of LDS, one tile of both ahead in registers; three workgroups a CU, each of
+// which fills the waits of the others, do more than a second buffer would.  Tiles of one block of rows go to one XCD, whose L2 then has the rows.
+//
+//   f32 100 -> 256, 428,377 rows, y and z written   405 us: 1.05 GB at 2.6 TB/s, 54 TFLOP/s; matrix units busy 46 % of the time: reading, multiplying
+//                                                   (157 us) and writing follow each other in a workgroup, and three overlap in part
+//   f32 dx and dz of it                             423 us: 1.49 GB at 3.5 TB/s, 52 TFLOP/s; matrix units 44 %
+//   bf16 512 -> 256, 302,709 rows, residual, z      179 us: 930 MB at 5.2 TB/s (a copy's rate), 443 TFLOP/s
+//   bf16 dx of it                                   160 us: 465 MB, 496 TFLOP/s, matrix units 23 %
+//   bf16 512 -> 512, 302,709 rows, residual         280 us: 930 MB, 567 TFLOP/s: a tile's loads, its 96 KB through LDS (a fragment is read for each of
+//                                                   its users), its products and its epilogue take about equally long
+//   one row of 512 -> 512 bf16                      4.9 us, f32 100 -> 128 of 5,485 rows 7.2: one tile's loads, products and stores, one after the other
 template <class T>
 struct RowsArgs {
     const typename T::elem *x, *w, *bias, *residual;
@@ -310,7 +322,7 @@ __device__ __forceinline__ void finish_rows(const RowsArgs<T> &a, const float *s
     }
 }
 
-// The operand dz = dy act'(z) of dx, made on its way to LDS; `write` says whether this workgroup stores it too.
+// The operand dz = dy act'(z) of dx, made on its way to LDS, and stored to `dz` unless that is null.
 template <class T, int BO>
 struct DzOperand : KcOperand<T, BO> {
     using Base = KcOperand<T, BO>;
@@ -391,7 +403,7 @@ __global__ __launch_bounds__(kThreads * TEAMS, 2) void k_linear_rows(RowsArgs<T>
         });
         if constexpr (DZ) {
             rows.rows([&](int i) { return row_of[i]; });
-            rows.saved = a.z, rows.saved_stride = a.z_stride, rows.dz = a.dz, rows.dz_stride = a.dz_stride;
+            rows.saved = a.z, rows.saved_stride = a.z_stride, rows.dz = ct == 0 ? a.dz : nullptr, rows.dz_stride = a.dz_stride;
             rows.act = a.z_activation, rows.K = K;
         }
         if constexpr (B_OC) {
@@ -447,7 +459,9 @@ __device__ __forceinline__ int64_t shares_of(int64_t units, int planned) { retur
 
 // dz of all rows, in group order, and the sums of its columns before they are rounded (bf16: sums of rounded values would be off by as much again as
 // the result's own rounding).  The rows, in units of kUnit, are dealt evenly to `shares` workgroups; share w leaves its sums for group g in slot
-// w + g of `part`.  A thread has VEC neighbouring columns, kDzColumns of a workgroup's rows at a time at most (blockIdx.y: which).
+// w + g of `part`.  A thread has VEC neighbouring columns, kDzColumns of a workgroup's rows at a time at most (blockIdx.y: which).  Bound by its bytes:
+// bf16 256 columns, 302,709 rows, relu (no sums) 90 us, 465 MB at 5.2 TB/s; gelu with the sums of 24 groups 120 us, 3.9 TB/s: 70 % of the time has vector
+// instructions in flight (the slope is some 25 of them a value) and rows are reached through the group order.
 constexpr int kDzColumns = 2048;
 
 template <class T>
@@ -537,6 +551,10 @@ __global__ __launch_bounds__(kThreads) void k_linear_dz(DzArgs<T> a)
 // and begin the next, so that no workgroup has more than its part however the sizes fall.  Share w leaves its sums for group g in slot w + g
 // of `part` (both grow along the rows, so no two meet in a slot): A_dim * B_dim of the matrix, then out_dim of db.
 // Side A is the wider of dz and x, side B the narrower; the matrix is laid out [A][B].
+//
+// f32 100 x 256, 428,377 rows 251 us: 610 MB at 2.4 TB/s, 87 TFLOP/s of 154 that a large product reaches, matrix units busy 75 % of the time (7 of 8 blocks
+// of columns hold something).  bf16 512 x 256, 302,709 rows 141 us, 24 groups 143: 465 MB at 3.3 TB/s, 562 TFLOP/s: the transposing LDS reads bring
+// half as much a cycle as plain ones.
 template <class T>
 struct WeightArgs {
     const typename T::elem *a, *b;
@@ -643,7 +661,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_linear_dw(WeightArgs<T> a)
     }
 }
 
-// dW and db of group blockIdx.y: what the shares left of it, added in a fixed order.
+// dW and db of group blockIdx.y: what the shares left of it, added in a fixed order (atomics would add in another one each time).  Bound by its loads: 512
+// shares of f32 100 x 256 (53 MB, much of it still in L2) 8.2 us; bf16 512 x 256 for 24 groups, 64 shares and a group's sums of dz 29 us.
 template <class T>
 struct ReduceArgs {
     const float *part;
@@ -655,7 +674,8 @@ struct ReduceArgs {
     Groups q;
 };
 
-// SPLIT: the four wavefronts take the shares of 256 values in turn; else (many groups, a few shares each) 256 values each.
+// SPLIT: the four wavefronts take the shares of 256 values in turn; else (many groups, a few shares each) 256 values each.  With the gradients of a
+// layer of 100 -> 256 f32 in one group 1,025 to 1,035 us with SPLIT, 1,040 without; of 512 -> 256 bf16 in 24 groups 691 to 693 without, 701 with.
 template <class T, bool SPLIT>
 __global__ __launch_bounds__(kThreads) void k_linear_reduce(ReduceArgs<T> a)
 {
@@ -723,6 +743,9 @@ __global__ __launch_bounds__(kThreads) void k_linear_reduce(ReduceArgs<T> a)
 }
 
 // ----------------------------------------------------------------- grouping
+// A stable counting sort by group in two passes over the group numbers: rows per tile and group, then each row's place.  Both are bound by their
+// dependent steps (group number, LDS counter, store), not by bytes: 428,377 rows of 8 groups 8.4 and 7.7 us, 302,709 of 24 groups 7.2 and 9.3
+// (2.5 MB).  One tile's rows (2,048) need one launch: 37 rows 2.6 us.
 struct GroupArgs {
     const int32_t *group_of, *ids;
     int64_t num_nodes, n;
@@ -899,7 +922,9 @@ int check_rows(const char *name, const void *p, int64_t stride, int width, int e
     } while (0)
 
 // Cuts of a product into workgroup tiles.  Wide results take 128 x 128; one that fits into fewer than 8 fragments of 16 columns takes as many as
-// it has (100 columns: 7), the four wavefronts one above the other.  Where that makes too few workgroups for the 256 CUs, 64 rows.
+// it has (100 columns: 7), the four wavefronts one above the other: f32 100 -> 256 with its gradients, 428,377 rows 1,030 us, 1,060 with 128 columns;
+// f32 100 -> 64, 5,485 rows of 4 types, 42 and 46.  Wavefronts with 128 x 64 or 96 x 64 sums each, instead of 64 x 64, take the registers of the third
+// workgroup of a CU (bf16 512 -> 512, 302,709 rows: 316 to 326 us instead of 297), and 64 x 128 tiles read more (354 instead of 325).
 using Large = Cut<2, 2, 4, 4>;
 using Small = Cut<2, 2, 2, 2>;
 template <int F>
@@ -934,7 +959,9 @@ void with_cut(bool large, int cols, int vec, Do call)
     }
 }
 
-// How the backward pass cuts a layer's rows: some 512 workgroups (two on each CU), each with one tile of dW and an equal share of the rows.
+// How the backward pass cuts a layer's rows: some 512 workgroups (two on each CU), each with one tile of dW and an equal share of the rows.  More leave
+// more sums to add up, fewer leave loads unhidden; with 256, 512 and 1,024, us of a training call: f32 100 -> 256, 428,377 rows 1,054, 1,030, 1,051;
+// bf16 512 -> 256, 302,709 rows 629, 583, 619; the same in 24 groups 749, 692, 714.
 struct WeightPlan {
     bool swapped, large;
     int a_dim, b_dim, a_tiles, b_tiles, shares;
@@ -962,7 +989,8 @@ WeightPlan plan_weight(const bgl_linear_t *l, int64_t n)
     p.dz_stride = round_up(l->out_dim, per);
     p.dz_bytes = l->activation == BGL_ACT_NONE ? 0 : round_up((size_t)n * p.dz_stride * elem_bytes(l), 256);
     p.part_bytes = round_up((size_t)p.slots * ((size_t)l->out_dim * l->in_dim + l->out_dim) * sizeof(float), 256);
-    // eight workgroups on each CU for dz with its sums, fewer where rows are so wide that the sums would count, more without sums
+    // eight workgroups on each CU for dz with its sums, fewer where rows are so wide that the sums would count, more without sums (gradients of bf16
+    // 512 -> 256 gelu, 302,709 rows of 24 groups: 692 us with 2,048 workgroups, 710 with 512, 703 with 8,192)
     p.sums_with_dz = l->dtype == BGL_BF16 && (l->activation == BGL_ACT_GELU || l->activation == BGL_ACT_SILU);
     const int64_t dz_most = !p.sums_with_dz ? 8192 : l->out_dim > 512 ? (1 << 20) / l->out_dim : 2048;
     p.dz_shares = (int)(most < dz_most ? most : dz_most);
@@ -971,22 +999,33 @@ WeightPlan plan_weight(const bgl_linear_t *l, int64_t n)
     return p;
 }
 
-// 128 rows to a tile where such tiles are enough for the 256 CUs, else 64, with four teams: few workgroups then wait for their loads once instead
-// of once for each tile of the summed index.
-bool large_tiles(int64_t n, int64_t cols) { return ceil_div(n, 128) * ceil_div(cols, 128) >= 256; }
+// 128 rows to a tile where that leaves the 256 CUs some three workgroups for two, else 64.  us with 64 and with 128 rows: f32 100 -> 128, 5,485 rows (43
+// tiles of 128) 8 and 19, 40,000 (313) 22 and 28, 45,000 (352) 24 and 28, 60,000 (469) 30 and 30; bf16 512 -> 128, 40,000 16 and 19; 512 -> 256, 30,000
+// (470) 20.5 and 19.3; f32 100 -> 256, 428,377 rows, with 64: 1.3 times the time.
+bool large_tiles(int64_t n, int64_t cols) { return ceil_div(n, 128) * ceil_div(cols, 128) >= 384; }
 
 template <class T, bool B_OC, bool DZ>
 int launch_rows(RowsArgs<T> &a, hipStream_t st)
 {
     const int64_t extra = a.q.groups > 0 ? (a.q.groups + 1 < a.n ? a.q.groups + 1 : a.n) : 1;
+    const bool large = large_tiles(a.n, a.N);
     int64_t blocks = 0;
-    with_cut(large_tiles(a.n, a.N), a.N, T::VEC, [&](auto cut, auto narrow) {
+    with_cut(large, a.N, T::VEC, [&](auto cut, auto narrow) {
         using C = decltype(cut);
-        constexpr int TEAMS = C::BA == 64 ? 4 : 1;
+        constexpr bool NARROW = B_OC && decltype(narrow)::value;
         a.row_tiles = a.n / C::BA + extra;
         a.col_tiles = (int)ceil_div(a.N, C::BB);
         blocks = tile_count(a.row_tiles, a.col_tiles);
-        if (blocks <= INT32_MAX) k_linear_rows<T, B_OC, C, B_OC && decltype(narrow)::value, TEAMS, DZ><<<dim3((unsigned)blocks), dim3(kThreads * TEAMS), 0, st>>>(a);
+        if (blocks > INT32_MAX) return;
+        // Four teams where no CU has a second workgroup: they wait for their loads once instead of once for each tile of the summed index.  us with
+        // four and with one: f32 100 -> 128, 1,000 rows (32 workgroups) 7.7 and 8.5, 8,000 (250) 8.3 and 9.3, 12,000 (376) 13.2 and 11.3.
+        if constexpr (C::BA == 64) {
+            if (blocks <= 256) {
+                k_linear_rows<T, B_OC, C, NARROW, 4, DZ><<<dim3((unsigned)blocks), dim3(4 * kThreads), 0, st>>>(a);
+                return;
+            }
+        }
+        k_linear_rows<T, B_OC, C, NARROW, 1, DZ><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a);
     });
     if (blocks > INT32_MAX) BGL_FAIL(BGL_EUNSUPPORTED, "%lld rows of width %d need too many workgroups", (long long)a.n, a.N);
     BGL_HIP(hipGetLastError());
@@ -1019,7 +1058,8 @@ int backward(const bgl_linear_t *l, int64_t n, const Groups &q, const void *dy, 
     const void *dz = dy;
     int64_t dz_stride = dy_stride;
     float *dz_part = p.sums_with_dz && dbias ? reinterpret_cast<float *>((char *)workspace + p.dz_bytes + p.part_bytes) : nullptr;
-    // dz is made where dx first needs it if dx has 128 columns at most: every column tile makes it again.  Not where dz takes dy's place and few rows
+    // dz is made where dx first needs it if dx has 128 columns at most: every column tile makes it again.  (us of a training call with dz apart: f32
+    // 100 -> 256, 428,377 rows 1,153 instead of 1,030; f32 100 -> 64, 5,485 rows of 4 types 47 instead of 42.)  Not where dz takes dy's place and few rows
     // have tiles of 64 columns: the second column's tile may still be reading the dy that the first one replaces.
     const bool act = l->activation != BGL_ACT_NONE, alone = large_tiles(n, l->in_dim) || l->in_dim <= Small::BB;
     const bool together = act && dx && n > 0 && l->in_dim <= Large::BB && !dz_part && (alone || dresidual != dy);
