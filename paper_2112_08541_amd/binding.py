@@ -544,6 +544,16 @@ def _workspace(nbytes: int) -> torch.Tensor:
     return w[(-w.data_ptr()) % 256:]
 
 
+def _first_call(owner, stream) -> None:
+    """The owner's memory was taken, and its zeros are written, on the stream that was current then: the first call, if on another
+    one, waits for that.  (A capture begins with the device idle and must not wait for work outside it.)"""
+    made, owner._made = owner._made, None
+    if made is not None and not torch.cuda.is_current_stream_capturing():
+        on = torch.cuda.current_stream() if stream is None else stream
+        if on != made:
+            on.wait_stream(made)
+
+
 def _matrix(name: str, t: Optional[torch.Tensor], n: int, width: int, dtype):
     """(address, row stride) of n device rows of `width` values; the values of a row are neighbours."""
     if t is None:
@@ -578,6 +588,7 @@ class RowGroups:
         self.workspace = _workspace(int(nbytes.value))
         self._rows = torch.empty(max(self.max_rows, 1), dtype=torch.int32, device="cuda")
         self.offsets = torch.zeros(self.num_groups + 1, dtype=torch.int32, device="cuda")
+        self._made = torch.cuda.current_stream()
 
     @property
     def rows(self) -> torch.Tensor:
@@ -591,6 +602,8 @@ class RowGroups:
         n = have if n is None else int(n)
         if n < 0 or n > min(self.max_rows, have):
             raise ValueError(f"n = {n} is more than the ids, or than the {self.max_rows} rows there is room for")
+        if self._made is not None:
+            _first_call(self, stream)
         _check(lib().bgl_group_rows(_dev_ptr(group_of, torch.int32), group_of.numel(), _dev_ptr(ids, torch.int32), n, self.num_groups,
                                     self._rows.data_ptr(), self.offsets.data_ptr(), self.workspace.data_ptr(),
                                     self.workspace.numel(), _stream_handle(stream)))
@@ -683,6 +696,7 @@ class Orthogonalizer:
         nbytes = C.c_size_t(0)
         _check(lib().bgl_orthogonalize_workspace_bytes(*self.shape, DTYPES[dtype], C.byref(nbytes)))
         self.workspace = _workspace(int(nbytes.value))
+        self._made = torch.cuda.current_stream()
 
     def run(self, update: torch.Tensor, out: torch.Tensor, stream=None) -> None:
         """out = update, orthogonalised; both (batch, rows, cols), or (rows, cols) for a batch of one; out may be update."""
@@ -694,6 +708,8 @@ class Orthogonalizer:
                 raise ValueError(f"{name}: the values of a row must be contiguous")
             return t.data_ptr(), t.stride(0), (t.stride(1) if self.shape[1] > 1 else self.shape[2])
         src, dst = strides("update", update), strides("out", out)
+        if self._made is not None:
+            _first_call(self, stream)
         _check(lib().bgl_orthogonalize(src[0], src[1], src[2], *self.shape, DTYPES[self.dtype], self.steps, self.coefficients.ctypes.data,
                                        self.eps, dst[0], dst[1], dst[2], self.workspace.data_ptr(), self.workspace.numel(),
                                        _stream_handle(stream)))

@@ -399,6 +399,18 @@ def test_another_stream_than_the_current_one(torch, B):
     run_layer(torch, B, "f32", 500, 100, 72, "gelu", "before", groups=3, seed=13, stream=s)
 
 
+def test_groups_built_on_another_stream_before_the_current_one_has_cleared_them(torch, B):
+    n, group = 3000, torch.randint(0, 5, (3000,), dtype=torch.int32, device="cuda")
+    want = torch.cat([torch.zeros(1, dtype=torch.int64), torch.bincount(group.cpu(), minlength=5).cumsum(0)])
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)               # some ms of the current stream, in front of the zeros
+    rg = B.RowGroups(n, 5)
+    rg.build(group, stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(rg.offsets.cpu().long(), want)
+
+
 def test_rows_beyond_four_gigabytes(torch, B):
     """Row strides that take the last rows' addresses past 32 bits, of bytes and (bf16) of values."""
     n, K, N, stride = 70_000, 16, 24, 64_000
