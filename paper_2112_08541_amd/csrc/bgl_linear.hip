@@ -1058,11 +1058,13 @@ int backward(const bgl_linear_t *l, int64_t n, const Groups &q, const void *dy, 
     const void *dz = dy;
     int64_t dz_stride = dy_stride;
     float *dz_part = p.sums_with_dz && dbias ? reinterpret_cast<float *>((char *)workspace + p.dz_bytes + p.part_bytes) : nullptr;
-    // dz is made where dx first needs it if dx has 128 columns at most: every column tile makes it again.  (us of a training call with dz apart: f32
-    // 100 -> 256, 428,377 rows 1,153 instead of 1,030; f32 100 -> 64, 5,485 rows of 4 types 47 instead of 42.)  Not where dz takes dy's place and few rows
-    // have tiles of 64 columns: the second column's tile may still be reading the dy that the first one replaces.
-    const bool act = l->activation != BGL_ACT_NONE, alone = large_tiles(n, l->in_dim) || l->in_dim <= Small::BB;
-    const bool together = act && dx && n > 0 && l->in_dim <= Large::BB && !dz_part && (alone || dresidual != dy);
+    // dz is made where dx first needs it if few tiles of columns make it again, or few rows make a launch count: us of a training call so and with dz
+    // apart, f32 gelu 100 -> 256, 428,377 rows 1,030 and 1,153, 256 -> 256, 100,000 rows 489 and 497, 512 -> 256 848 and 809; bf16 relu 256 -> 256 168
+    // and 171, 512 -> 256 239 and 225; 512 -> 128, 5,485 rows f32 57 and 60, bf16 36 and 41.  Not where dz takes dy's place and dx has several tiles of
+    // columns: one may still be reading the dy that the first replaces.
+    const bool large = large_tiles(n, l->in_dim), alone = l->in_dim <= (large ? Large::BB : Small::BB);
+    const bool act = l->activation != BGL_ACT_NONE;
+    const bool together = act && dx && n > 0 && l->in_dim <= (large ? 256 : 512) && !dz_part && (alone || dresidual != dy);
     if (n > 0 && (dresidual || act)) {
         void *to = dresidual ? dresidual : workspace;
         dz_stride = dresidual ? dresidual_stride : (int64_t)p.dz_stride;

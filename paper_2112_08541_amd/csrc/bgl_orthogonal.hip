@@ -615,7 +615,8 @@ int check_matrices(int64_t batch, int32_t rows, int32_t cols, int32_t dtype)
 // 128 x 128 tiles (half the reads) where most CUs have one and the sums are long enough to pay for the larger tile's ends, else 64 x 64; two
 // teams to a tile, four where the CUs have one tile at most and the sums are long.  All five steps: 2 of 1024 x 2048 468 us with the larger tiles for
 // Q X (1,024 long, 256 tiles), 500 without; 24 of 256 x 512 (256 long, 192 tiles) 185 and 176.  Four teams instead of two: 1 of 1024 x 1024 232 us
-// instead of 254, 4 of 400 x 800 (shorter sums) 214 instead of 195, 24 of 256 x 512 206 instead of 176.
+// instead of 254, 4 of 400 x 800 (shorter sums) 214 instead of 195, 24 of 256 x 512 206 instead of 176, 2 of 1024 x 2048 (272 tiles) 541 instead of 498, 5 of
+// 640 x 640 (275 tiles) 298 instead of 265.
 template <int STAGE, class T>
 void launch_product(const OrthoArgs &a, int from, hipStream_t st)
 {

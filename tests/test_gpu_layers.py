@@ -372,6 +372,12 @@ def test_residual_may_be_the_output_and_dz_may_be_dy(torch, B):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("dtype,act,mode", [("f32", "silu", "none"), ("bf16", "relu", "before")])
+@pytest.mark.parametrize("n,K,N,groups", [(25_000, 250, 40, 0), (25_500, 200, 33, 3), (900, 500, 70, 2), (300, 512, 130, 0)])
+def test_several_tiles_of_dx_columns(torch, B, dtype, act, mode, n, K, N, groups):
+    run_layer(torch, B, dtype, n, K, N, act, mode, groups=groups, seed=21)
+
+
 @pytest.mark.parametrize("dtype,act", [("f32", "silu"), ("f32", "relu"), ("bf16", "relu"), ("bf16", "gelu")])
 @pytest.mark.parametrize("n,K,N,groups", [(700, 100, 300, 0), (5485, 128, 520, 0), (900, 65, 260, 4), (33_000, 128, 70, 0)])
 def test_dz_in_the_place_of_dy_where_dx_has_more_than_one_tile_of_columns(torch, B, dtype, act, n, K, N, groups):
