@@ -53,7 +53,6 @@ __device__ __forceinline__ float activate(float z)
 template <int ACT>
 __device__ __forceinline__ float slope(float z)
 {
-    if constexpr (ACT == BGL_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
     if constexpr (ACT == BGL_ACT_GELU) {
         float bell;
         const float p = normal_cdf(z, bell);
@@ -103,9 +102,14 @@ __device__ __forceinline__ void times_slope(int act, const float (&z)[V], float 
 #pragma unroll
         for (int u = 0; u < V; ++u) d[u] *= slope<decltype(which)::value>(z[u]);
     };
-    if (act == BGL_ACT_RELU) all(std::integral_constant<int, BGL_ACT_RELU>{});
-    else if (act == BGL_ACT_GELU) all(std::integral_constant<int, BGL_ACT_GELU>{});
-    else if (act == BGL_ACT_SILU) all(std::integral_constant<int, BGL_ACT_SILU>{});
+    if (act == BGL_ACT_RELU) {  // (no product: a dy that is not finite leaves nothing where z <= 0)
+#pragma unroll
+        for (int u = 0; u < V; ++u) d[u] = z[u] > 0.0f ? d[u] : 0.0f;
+    } else if (act == BGL_ACT_GELU) {
+        all(std::integral_constant<int, BGL_ACT_GELU>{});
+    } else if (act == BGL_ACT_SILU) {
+        all(std::integral_constant<int, BGL_ACT_SILU>{});
+    }
 }
 
 // ----------------------------------------------------------------- groups

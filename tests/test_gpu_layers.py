@@ -304,6 +304,24 @@ def test_values_that_are_not_finite_stay_in_their_row(torch, B, dtype, n):
     assert np.isposinf(got[1]).all() and np.isnan(got[4]).all() and (got[7] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,K", [(40, 24), (40, 600)])
+def test_dy_that_is_not_finite_leaves_nothing_where_relu_is_closed(torch, B, dtype, n, K):
+    dt, N = dtype_of(torch, dtype), 32
+    x, w = torch.ones((n, K), dtype=dt, device="cuda"), torch.ones((N, K), dtype=dt, device="cuda")
+    w[::2] = -1                                                  # z < 0 in the even columns
+    dy = torch.ones((n, N), dtype=dt, device="cuda")
+    dy[1, 2], dy[3, 4], dy[5, 6] = float("inf"), float("nan"), float("-inf")
+    lay = B.Linear(n, K, N, dt, "relu", "before")
+    y, saved, dz = (torch.empty((n, N), dtype=dt, device="cuda") for _ in range(3))
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(N, dtype=dt, device="cuda")
+    lay.forward(x, w, y, residual=torch.zeros_like(y), saved=saved)
+    lay.backward(dy, x, w, saved, dx, dw, db, dz)
+    want = (torch.arange(N, device="cuda") % 2).to(dt)
+    assert torch.equal(dz, want.expand(n, N)) and torch.equal(db, n * want)
+    assert torch.equal(dx, torch.full_like(dx, N / 2)) and torch.equal(dw, (n * want)[:, None].expand(N, K))
+
+
 def test_gradients_match_differences(torch, B):
     """(L(p + h d) - L(p - h d)) / 2h of L = sum(dy y), in 64 bits, against the gradient's product with d."""
     n, K, N, G = 60, 20, 28, 3
