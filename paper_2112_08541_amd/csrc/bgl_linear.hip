@@ -1135,11 +1135,11 @@ int group_tiles(int64_t n, int64_t &tile_rows)
     return (int)ceil_div(n, tile_rows);
 }
 
+// Room for as many tiles as group_tiles() may cut n rows or fewer into: a longer batch's tiles are rounded up to more rows, so it can have fewer.
 size_t group_bytes(int64_t n, int groups)
 {
-    int64_t tile_rows;
-    const int tiles = group_tiles(n, tile_rows);
-    return round_up((size_t)n * sizeof(uint16_t), 256) + (size_t)(tiles > 0 ? tiles : 1) * (groups + 1) * sizeof(int32_t);
+    const int64_t tiles = ceil_div(n, kGroupTileRows);
+    return round_up((size_t)n * sizeof(uint16_t), 256) + (size_t)(tiles < 1 ? 1 : tiles < kGroupTiles ? tiles : kGroupTiles) * (groups + 1) * sizeof(int32_t);
 }
 
 int check_group_sizes(int64_t n, int32_t num_groups)

@@ -506,3 +506,15 @@ def test_the_binding_refuses_what_does_not_fit(torch, B):
                 lambda: lay.forward(x, w, y, residual=f(10, 4)), lambda: lay.backward(y, x, w, dx=x, dresidual=y)):
         with pytest.raises(B.BglError):
             bad()
+
+
+@pytest.mark.parametrize("most,n,groups", [(524_800, 524_288, 8), (560_000, 524_288, 1024), (655_361, 655_360, 100)])
+def test_room_for_many_rows_is_room_for_fewer(torch, B, most, n, groups):
+    """A batch a little smaller than the largest is cut into more tiles than that one."""
+    rg = B.RowGroups(most, groups)
+    of = torch.randint(-1, groups, (n,), dtype=torch.int32, device="cuda")
+    rg.build(of)
+    key = of.cpu().numpy()
+    key = np.where(key < 0, groups, key)
+    assert np.array_equal(rg.rows.cpu().numpy(), np.argsort(key, kind="stable"))
+    assert np.array_equal(rg.offsets.cpu().numpy(), np.searchsorted(np.sort(key), np.arange(groups + 1)))

@@ -138,3 +138,29 @@ def test_the_binding_names_what_the_header_numbers(B):
     assert (B.BGL_MAX_GROUPS, B.BGL_MAX_DIM) == (define["BGL_MAX_GROUPS"], define["BGL_MAX_DIM"])
     assert B.ACTIVATIONS == {k[8:].lower(): v for k, v in define.items() if k.startswith("BGL_ACT_")}
     assert B.RESIDUALS == {k[13:].lower(): v for k, v in define.items() if k.startswith("BGL_RESIDUAL_")}
+
+
+@pytest.mark.parametrize("groups", [1, 8, 100, 1024])
+def test_a_workspace_for_many_rows_is_enough_for_fewer(B, L, groups):
+    """Around every size at which the rows of a grouping tile, or the tiles or shares of a layer's gradients, change."""
+    edges = [0, 1, 63, 64, 65, 2047, 2048, 2049, 8191, 8192, 8193]
+    edges += [k * 131_072 + d for k in range(1, 24) for d in (-512, -1, 0, 1, 511, 512)] + [2**31 - 1 - 131_072, 2**31 - 1]
+
+    def grows(need):
+        sizes = [need(n) for n in sorted(edges)]
+        assert all(a <= b for a, b in zip(sizes, sizes[1:])), [n for n, a, b in zip(sorted(edges), sizes, sizes[1:]) if a > b]
+
+    def grouping(n):
+        out = C.c_size_t()
+        assert L.bgl_group_rows_workspace_bytes(n, groups, C.byref(out)) == B.BGL_OK
+        return out.value
+    grows(grouping)
+    for dtype in (0, 1):
+        for activation in range(4):
+            l = layer(B, dtype, activation, 0, 100, 256, groups)
+
+            def gradients(n):
+                out = C.c_size_t()
+                assert L.bgl_linear_workspace_bytes(C.byref(l), n, C.byref(out)) == B.BGL_OK
+                return out.value
+            grows(gradients)
