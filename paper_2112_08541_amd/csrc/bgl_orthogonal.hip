@@ -7,7 +7,7 @@
 // 48 cycles, the fp32 instructions for the same tile 256.  One half alone (2^-11) will not do: the steps enlarge what lies in the
 // directions of small singular values by up to a^steps (485 for the usual coefficients), rounding errors included.  Values are kept near the upper
 // end of fp16's range by powers of two, known beforehand because the singular values are: |X| <= 1 to begin with, so the coefficients alone
-// say how large X, P and Q can become.  Sums are fp32, the norm is summed in fp64.
+// say how large X, P and Q can become.  Sums are fp32, the norm is fp64.
 //
 // A split row holds for each 32 values 32 hi, then 32 lo: 128 bytes, what a tile takes of a row.  X X' and P P read two operands along their rows;
 // Q X reads X across them, by the transposing LDS read.  P and Q are symmetric: tiles on and below the diagonal are
@@ -68,6 +68,9 @@ __device__ __forceinline__ void store_split(uint32_t *row, int c, const float (&
     *reinterpret_cast<Pack *>(at + 32) = lo;
 }
 
+// In 64 bits: the norm of fp32 values may lie beyond fp32's largest, and without eps among its subnormal ones.
+__device__ __forceinline__ double inverse_norm(double sum, float eps) { return 1.0 / (sqrt(sum) + (double)eps); }
+
 // Sums of squares of equal shares of a matrix, for the norm: one pass in 256 workgroups a matrix, bound by its launch and a few dependent loads (24 of
 // 256 x 512 bf16 5.2 us, 2 of 2048 x 1024 f32 4.4).
 template <class T>
@@ -113,7 +116,7 @@ __global__ __launch_bounds__(kThreads) void k_ortho_start(OrthoArgs a)
     for (int i = 0; i < kNormParts / 64; ++i) sum += a.norms[matrix * kNormParts + i * 64 + (threadIdx.x & 63)];
 #pragma unroll
     for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-    const float norm = (float)sqrt(sum) + a.eps;
+    const double inverse = inverse_norm(sum, a.eps);
     const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
     const typename T::elem *u = (const typename T::elem *)a.update + matrix * a.in_matrix;
     for (int i = threadIdx.x; i < 64 * 64; i += kThreads) {
@@ -121,7 +124,7 @@ __global__ __launch_bounds__(kThreads) void k_ortho_start(OrthoArgs a)
         const int r = a.tall ? fast : slow, c = a.tall ? slow : fast;
         float v = 0.0f;
         if (r0 + r < a.m && c0 + c < a.n)
-            v = T::get(u[a.tall ? (int64_t)(c0 + c) * a.in_row + r0 + r : (int64_t)(r0 + r) * a.in_row + c0 + c]) / norm;
+            v = (float)(T::get(u[a.tall ? (int64_t)(c0 + c) * a.in_row + r0 + r : (int64_t)(r0 + r) * a.in_row + c0 + c]) * inverse);
         tile[r][c] = v * a.sx;
     }
     __syncthreads();
@@ -416,11 +419,11 @@ __global__ __launch_bounds__(kWholeThreads) void k_ortho_whole(OrthoArgs a, int 
     __syncthreads();
     sum = 0.0;
     for (int w = 0; w < kWholeWaves; ++w) sum += partial[w];
-    const float norm = (float)sqrt(sum) + a.eps;
+    const double inverse = inverse_norm(sum, a.eps);
     const int pad_rows = a.tall ? a.np : a.mp, pad_cols = a.tall ? a.mp : a.np;
     for (int i = threadIdx.x; i < pad_rows * pad_cols; i += kWholeThreads) {
         const int r = i / pad_cols, c = i % pad_cols;
-        const float v = r < rows && c < cols ? T::get(u[(int64_t)r * a.in_row + c]) / norm * a.sx : 0.0f;
+        const float v = r < rows && c < cols ? (float)(T::get(u[(int64_t)r * a.in_row + c]) * inverse) * a.sx : 0.0f;
         whole_put(x, a.np, a.tall ? c : r, a.tall ? r : c, v);
     }
     __syncthreads();

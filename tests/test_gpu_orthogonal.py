@@ -177,3 +177,14 @@ def test_the_binding_refuses_what_does_not_fit(torch, B):
                 lambda: o.run(f(1, 10, 12).expand(2, 10, 12), f(2, 10, 12))):
         with pytest.raises(B.BglError):
             bad()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(48, 80), (200, 150)])
+def test_updates_whose_norm_is_beyond_fp32(torch, B, dtype, rows, cols):
+    """Finite values with a norm of 10^40, and values among fp32's last subnormal ones with no eps."""
+    rng = np.random.default_rng(12)
+    signs = rng.choice([-1.0, 1.0], (2, rows, cols))
+    check(torch, B, signs * np.array([2.0 ** 127, 2.0 ** 126])[:, None, None], dtype)
+    if dtype == "f32":
+        check(torch, B, np.eye(rows, cols)[None] * 2.0 ** -147, dtype, eps=0.0)
