@@ -24,42 +24,69 @@ constexpr int kGroupTiles = 256;     // workgroups of one grouping pass at most
 constexpr int kGroupTileRows = 2048; // rows a workgroup takes at least
 
 // ----------------------------------------------------------------- activations
-// The library's erff and expf are 30 to 50 instructions, which made the epilogue of 428,377 x 256 gelu values longer than their stores.
-// exp: the hardware's 2^x.
-__device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
+// The library's erff and expf are 30 to 50 instructions, which made the epilogue of 428,377 x 256 gelu values longer than their stores.  The forms here are
+// as near in the tails as elsewhere, relative to the value: fp32 layers to some units of the last place, bf16 layers to 2^-15 or nearer, which rounding
+// to the type outweighs a hundred times.
+constexpr float kLog2e = 1.44269504088896341f, kLog2eRest = 1.92596299e-8f, kLn2 = 0.693147180559945309f;
 
-// Phi(z) = erfc(-z / sqrt 2) / 2 and phi(z) sqrt(2 pi) = exp(-z^2 / 2), by Abramowitz and Stegun 7.1.26: erfc(x) = (a1 t + .. + a5 t^5) exp(-x^2),
-// t = 1 / (1 + 0.3275911 x), x >= 0, off by 1.5e-7 at most.
-__device__ __forceinline__ float normal_cdf(float z, float &bell)
+// exp(x + rest) for |x| <= 150 or so, |rest| small.  fp32: the hardware's 2^x of the rounded argument, times what rounding it left out; bf16 without that,
+// which is |x| 2^-24 of the value.
+template <class T>
+__device__ __forceinline__ float exp_near(float x, float rest)
 {
-    const float x = fabsf(z) * 0.70710678118654752f;
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
-    bell = exp_fast(-x * x);
-    const float tail = 0.5f * bell * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-    return z < 0.0f ? tail : 1.0f - tail;
+    const float whole = x * kLog2e, power = __builtin_amdgcn_exp2f(whole);
+    if constexpr (T::PER == 2) return power;
+    const float left = fmaf(rest, kLog2e, fmaf(x, kLog2eRest, fmaf(x, kLog2e, -whole)));
+    return power * fmaf(left, kLn2, 1.0f);
 }
 
-template <int ACT>
+// Phi(z) and, in `bell`, exp(-z^2 / 2) = phi(z) sqrt(2 pi).  Phi(-a) = bell R(a) for a >= 0, where R(a) = erfc(a / sqrt 2) exp(a^2 / 2) / 2 falls slowly: a
+// rational function with positive coefficients (nothing cancels), fitted to the least relative error on [0, 14], beyond which bell is 0: 5.5e-9 with
+// five and six coefficients, 3.8e-7 with four and five.
+template <class T>
+__device__ __forceinline__ float normal_cdf(float z, float &bell)
+{
+    const float a = fminf(fabsf(z), 16.0f), square = -0.5f * a * a;  // (NaN: 16, and z makes the result NaN)
+    float above, below;
+    if constexpr (T::PER == 2) {
+        above = fmaf(a, fmaf(a, fmaf(a, 0.0170477093f, 0.119531738f), 0.361971406f), 0.49999981f);
+        below = fmaf(a, fmaf(a, fmaf(a, fmaf(a, 0.0427372715f, 0.299418992f), 0.953440215f), 1.52180854f), 1.0f);
+    } else {
+        above = fmaf(a, fmaf(a, fmaf(a, fmaf(a, 0.00407761085f, 0.040372551f), 0.182461808f), 0.437250858f), 0.5f);
+        below = fmaf(a, fmaf(a, fmaf(a, fmaf(a, fmaf(a, 0.0102209259f, 0.101205788f), 0.467429045f), 1.1992906f), 1.67238667f), 1.0f);
+    }
+    bell = exp_near<T>(square, fmaf(-0.5f * a, a, -square));
+    const float tail = bell * above * __builtin_amdgcn_rcpf(below);
+    return z < 0.0f ? tail : 1.0f - tail;
+}
+template <class T>
+__device__ __forceinline__ float logistic(float z)
+{
+    if constexpr (T::PER == 1) z = __builtin_amdgcn_fmed3f(z, -150.0f, 150.0f);  // (past fp32's largest exp, and what rounding leaves out is finite)
+    return __builtin_amdgcn_rcpf(1.0f + exp_near<T>(-z, 0.0f));
+}
+
+template <class T, int ACT>
 __device__ __forceinline__ float activate(float z)
 {
     if constexpr (ACT == BGL_ACT_RELU) return z < 0.0f ? 0.0f : z;  // (NaN stays)
     if constexpr (ACT == BGL_ACT_GELU) {
         float bell;
-        return z * normal_cdf(z, bell);
+        return z * normal_cdf<T>(z, bell);
     }
-    if constexpr (ACT == BGL_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + exp_fast(-z));
+    if constexpr (ACT == BGL_ACT_SILU) return z * logistic<T>(z);
     return z;
 }
-template <int ACT>
+template <class T, int ACT>
 __device__ __forceinline__ float slope(float z)
 {
     if constexpr (ACT == BGL_ACT_GELU) {
         float bell;
-        const float p = normal_cdf(z, bell);
+        const float p = normal_cdf<T>(z, bell);
         return fmaf(z * bell, 0.39894228040143268f, p);
     }
     if constexpr (ACT == BGL_ACT_SILU) {
-        const float p = __builtin_amdgcn_rcpf(1.0f + exp_fast(-z));
+        const float p = logistic<T>(z);
         return p * fmaf(z, 1.0f - p, 1.0f);
     }
     return 1.0f;
@@ -84,23 +111,23 @@ __device__ __forceinline__ float kept(int act, typename T::elem v)
     return T::get(v);
 }
 // One choice for several values: one for each kept their chains apart.
-template <int V>
+template <class T, int V>
 __device__ __forceinline__ void activate_all(int act, float (&v)[V])
 {
     const auto all = [&](auto which) {
 #pragma unroll
-        for (int u = 0; u < V; ++u) v[u] = activate<decltype(which)::value>(v[u]);
+        for (int u = 0; u < V; ++u) v[u] = activate<T, decltype(which)::value>(v[u]);
     };
     if (act == BGL_ACT_RELU) all(std::integral_constant<int, BGL_ACT_RELU>{});
     else if (act == BGL_ACT_GELU) all(std::integral_constant<int, BGL_ACT_GELU>{});
     else if (act == BGL_ACT_SILU) all(std::integral_constant<int, BGL_ACT_SILU>{});
 }
-template <int V>
+template <class T, int V>
 __device__ __forceinline__ void times_slope(int act, const float (&z)[V], float (&d)[V])
 {
     const auto all = [&](auto which) {
 #pragma unroll
-        for (int u = 0; u < V; ++u) d[u] *= slope<decltype(which)::value>(z[u]);
+        for (int u = 0; u < V; ++u) d[u] *= slope<T, decltype(which)::value>(z[u]);
     };
     if (act == BGL_ACT_RELU) {  // (no product: a dy that is not finite leaves nothing where z <= 0)
 #pragma unroll
@@ -316,7 +343,7 @@ __device__ __forceinline__ void finish_rows(const RowsArgs<T> &a, const float *s
                 for (int u = 0; u < V; ++u) piece.e[u] = keep<T>(a.activation, v[u]);
                 store_piece<T, V>(a.saved + row[p] * a.saved_stride + n0 + c, WHOLE ? V : left, piece);
             }
-            activate_all(a.activation, v);
+            activate_all<T>(a.activation, v);
             if (a.residual_mode == BGL_RESIDUAL_AFTER) {
 #pragma unroll
                 for (int u = 0; u < V; ++u) v[u] += T::get(res[p].e[u]);
@@ -364,7 +391,7 @@ struct DzOperand : KcOperand<T, BO> {
             float dv[T::VEC], zv[T::VEC];
 #pragma unroll
             for (int e = 0; e < T::VEC; ++e) dv[e] = T::get(d.e[e]), zv[e] = kept<T>(act, s.e[e]);
-            times_slope(act, zv, dv);
+            times_slope<T>(act, zv, dv);
 #pragma unroll
             for (int e = 0; e < T::VEC; ++e) d.e[e] = T::put(dv[e]);
             Base::reg[p] = __builtin_bit_cast(uint4, d);
@@ -524,7 +551,7 @@ __global__ __launch_bounds__(kThreads) void k_linear_dz(DzArgs<T> a)
                     float dv[V], zv[V];
 #pragma unroll
                     for (int e = 0; e < V; ++e) dv[e] = T::get(d[p].e[e]), zv[e] = a.act ? kept<T>(a.act, z[p].e[e]) : 0.0f;
-                    times_slope(a.act, zv, dv);
+                    times_slope<T>(a.act, zv, dv);
                     if (r[p] < 0) continue;
 #pragma unroll
                     for (int e = 0; e < V; ++e) sum[e] += dv[e];

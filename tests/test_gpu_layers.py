@@ -518,3 +518,42 @@ def test_room_for_many_rows_is_room_for_fewer(torch, B, most, n, groups):
     key = np.where(key < 0, groups, key)
     assert np.array_equal(rg.rows.cpu().numpy(), np.argsort(key, kind="stable"))
     assert np.array_equal(rg.offsets.cpu().numpy(), np.searchsorted(np.sort(key), np.arange(groups + 1)))
+
+
+def single_values(torch, B, dtype, act, z):
+    """act(z) and its slope as a layer of one weight of 1 makes them: the product is exact, so nothing else has a part in it."""
+    dt = dtype_of(torch, dtype)
+    x = torch.from_numpy(z.astype(np.float32)).to(dt).cuda()[:, None]
+    lay, one = B.Linear(len(z), 1, 1, dt, act), torch.ones((1, 1), dtype=dt, device="cuda")
+    y, saved, dx = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+    lay.forward(x, one, y, saved=saved)
+    lay.backward(torch.ones_like(x), x, one, saved, dx)
+    return tuple(t.double().cpu().numpy()[:, 0] for t in (x, y, dx))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+def test_activations_are_right_to_the_last_places_in_the_tails_too(torch, B, dtype, act):
+    """Relative to the value, not to 1.  fp32, in unit roundoffs u: gelu's Phi(-|z|) is the product of an exponential (its hardware 2^x 2, the
+    rest of its argument and the product 3), a numerator and a denominator (2 each), a reciprocal (2) and two products: 16 with the
+    rational function's own 0.1 and z; silu 10 for exponential 5, sum, reciprocal 2 and product.  Slopes: the same of each term; silu's 1 - p has p's error.  bf16:
+    2^-15 of the value, and the type's rounding; the slope there sees z rounded to a half."""
+    from scipy.special import erfc
+    rng = np.random.default_rng(31)
+    far = 12.5 if act == "gelu" else 80.0
+    z = np.concatenate([rng.uniform(-far, far, 60_000), rng.uniform(-1, 1, 30_000), 2.0 ** rng.uniform(-30, 3, 5000), -2.0 ** rng.uniform(-30, 3, 5000)])
+    z, y, dx = single_values(torch, B, dtype, act, z)
+    if act == "gelu":
+        p, places = 0.5 * erfc(-z / np.sqrt(2)), 16
+        bell = z * np.exp(-z * z / 2) / np.sqrt(2 * np.pi)
+        slope, mass = p + bell, p + np.abs(bell)
+    else:
+        p, places = 1 / (1 + np.exp(-z)), 10
+        slope, mass = p * (1 + z * (1 - p)), p * (1 + np.abs(z) * (1 - p)) + np.abs(z) * p * p
+    want = z * p
+    relative = (places + 1) * U if dtype == "f32" else 2.0 ** -8 * 1.001 + 2.0 ** -15
+    off = np.abs(y - want) / (np.abs(want) * relative + 2.0 ** -120)
+    assert off.max() <= 1, f"value: {off.max():.1f} times the bound at z = {z[off.argmax()]}"
+    e = (places + 2) * U * mass if dtype == "f32" else 2.0 ** -8 * 1.001 * np.abs(slope) + 2.0 ** -15 * mass + 0.8 * (2.0 ** -11 * np.abs(z) + 2.0 ** -24)
+    off = np.abs(dx - slope) / (e + 2.0 ** -120)
+    assert off.max() <= 1, f"slope: {off.max():.1f} times the bound at z = {z[off.argmax()]}"
