@@ -19,6 +19,7 @@ import numpy as np
 import torch
 
 from . import binding as B
+from .pipeline import NativePipeline
 
 
 def neighbor_mean(h: torch.Tensor, row_ptr: torch.Tensor, col: torch.Tensor):
@@ -146,7 +147,12 @@ def blocks_of(batch: B.SampledBatch):
 
 
 def train(pipe, model: TypedSage, seeds: torch.Tensor, rng_seeds, steps: int, types: torch.Tensor, labels: torch.Tensor) -> np.ndarray:
-    """Trains on `steps` batches of a MinibatchPipeline; labels: of every node.  Returns (loss, correct) per batch."""
+    """Trains on `steps` batches of a MinibatchPipeline, or of a NativePipeline without a host tier (with one its sampling has a stream
+    that only the library knows, which could not be kept off the batch in use); labels: of every node.  A batch's sampling workspace is
+    read until its step has ended, so the sampling and map updates of later batches wait for that: preparation overlaps the
+    fetch, not the training step.  Returns (loss, correct) per batch."""
+    if isinstance(pipe, NativePipeline) and pipe.tier is not None:
+        raise ValueError("train() cannot order a NativePipeline with a host tier: use a MinibatchPipeline")
     results = []
 
     def on_batch(_step, batch, n, p):

@@ -69,3 +69,21 @@ def test_training_through_the_pipeline(torch):
     history = sage.main(epochs=5)
     assert np.isfinite(history).all()
     assert history[-1, 0] < 0.8 * history[0, 0] and history[-1, 1] > 1.3 * history[0, 1]
+
+
+def test_both_loops_without_a_tier_train_alike(torch):
+    """The sums of the neighbors' mean come in any order, so the losses of a few steps agree to some places only."""
+    from paper_2112_08541_amd import binding as B, inputs, sage
+    from paper_2112_08541_amd.pipeline import MinibatchPipeline, NativePipeline
+    cfg = inputs.CONFIGS["tiny"]
+    w = inputs.make_workload(cfg, pinned=True)
+    graph = B.Graph(w.row_ptr, w.col)
+    types, labels = sage.synthetic_task(w, 3, 4)
+    bounds = [min(cfg.num_nodes, cfg.batch * int(np.prod([1 + f for f in cfg.fanouts[:h]]))) for h in range(len(cfg.fanouts) + 1)]
+    seeds, losses = torch.from_numpy(w.seed_batches).cuda(), []
+    for loop in (MinibatchPipeline, NativePipeline):
+        cache = B.Cache(cfg.cache_rows, w.features.ctypes.data, num_nodes=cfg.num_nodes, row_bytes=cfg.row_bytes)
+        pipe = loop(graph, cache, cfg.batch, cfg.fanouts, cfg.row_bytes)
+        model = sage.TypedSage(bounds, cfg.feat_dim, 32, 4, 3)
+        losses.append(sage.train(pipe, model, seeds, w.rng_seeds, 6, types, labels)[:, 0])
+    assert np.isfinite(losses).all() and np.allclose(losses[0], losses[1], rtol=1e-3)

@@ -164,3 +164,12 @@ def test_a_workspace_for_many_rows_is_enough_for_fewer(B, L, groups):
                 assert L.bgl_linear_workspace_bytes(C.byref(l), n, C.byref(out)) == B.BGL_OK
                 return out.value
             grows(gradients)
+
+
+def test_training_refuses_a_pipeline_whose_sampling_it_cannot_order():
+    from paper_2112_08541_amd import sage
+    from paper_2112_08541_amd.pipeline import NativePipeline
+    pipe = object.__new__(NativePipeline)
+    pipe._tier = object()
+    with pytest.raises(ValueError, match="tier"):
+        sage.train(pipe, None, None, None, 0, None, None)
