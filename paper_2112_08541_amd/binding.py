@@ -648,8 +648,13 @@ class Linear:
         return groups._rows.data_ptr(), groups.offsets.data_ptr()
 
     def forward(self, x, weight, y, bias=None, residual=None, saved=None, groups: Optional[RowGroups] = None, stream=None) -> None:
-        """Writes y, and saved = the pre-activation if given (the backward call of a layer with an activation needs it)."""
+        """Writes y, and saved = the pre-activation if given (the backward call of a layer with an activation needs it).  Torch's own
+        differentiation does not see the call: tensors that require gradients are refused, as by torch's functions with an out argument, unless
+        gradient mode is off (under torch.no_grad(), or in the forward of a torch.autograd.Function whose backward makes the backward call)."""
         n = int(x.shape[0])
+        if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or bias is not None and bias.requires_grad
+                                        or residual is not None and residual.requires_grad):
+            raise ValueError("the layer does not record gradients: call it under torch.no_grad() and make the backward call yourself")
         if n > self.max_rows:
             raise ValueError(f"{n} rows, the layer was made for {self.max_rows}")
         _check(lib().bgl_linear_forward(

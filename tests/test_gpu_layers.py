@@ -557,3 +557,36 @@ def test_activations_are_right_to_the_last_places_in_the_tails_too(torch, B, dty
     e = (places + 2) * U * mass if dtype == "f32" else 2.0 ** -8 * 1.001 * np.abs(slope) + 2.0 ** -15 * mass + 0.8 * (2.0 ** -11 * np.abs(z) + 2.0 ** -24)
     off = np.abs(dx - slope) / (e + 2.0 ** -120)
     assert off.max() <= 1, f"slope: {off.max():.1f} times the bound at z = {z[off.argmax()]}"
+
+
+def test_tensors_that_require_gradients_are_refused_rather_than_their_gradients_lost(torch, B):
+    n, K, N = 70, 20, 12
+    lay = B.Linear(n, K, N, torch.float32, "silu", "before")
+    x, w, b, r, dy = (torch.randn(s, device="cuda") for s in ((n, K), (N, K), (N,), (n, N), (n, N)))
+    y, saved, dx, dr, dw, db = (torch.empty_like(t) for t in (dy, dy, x, dy, w, b))
+    given = dict(x=x, weight=w, bias=b, residual=r)
+    for name in given:
+        some = {k: t.clone().requires_grad_() if k == name else t for k, t in given.items()}
+        with pytest.raises(ValueError, match="gradients"):
+            lay.forward(y=y, **some)
+        with torch.no_grad():
+            lay.forward(y=y, **some)
+
+    class Layer(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, w, b, r):
+            out = torch.empty_like(r)
+            lay.forward(x, w, out, b, r, saved)
+            ctx.save_for_backward(x, w)
+            return out
+
+        @staticmethod
+        def backward(ctx, d):
+            lay.backward(d.contiguous(), *ctx.saved_tensors, saved, dx, dw, db, dr)
+            return dx.clone(), dw.clone(), db.clone(), dr.clone()
+    leaves = [t.clone().requires_grad_() for t in (x, w, b, r)]
+    Layer.apply(*leaves).backward(dy)
+    lay.forward(x, w, y, b, r, saved)
+    lay.backward(dy, x, w, saved, dx, dw, db, dr)
+    for leaf, want in zip(leaves, (dx, dw, db, dr)):
+        assert torch.equal(leaf.grad, want)
