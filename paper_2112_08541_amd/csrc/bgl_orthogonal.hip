@@ -615,9 +615,15 @@ int check_matrices(int64_t batch, int32_t rows, int32_t cols, int32_t dtype)
     return BGL_OK;
 }
 
-// 128 x 128 tiles (half the reads) where most CUs have one and the sums are long enough to pay for the larger tile's ends, else 64 x 64; two
-// teams to a tile, four where the CUs have one tile at most and the sums are long.  All five steps: 2 of 1024 x 2048 468 us with the larger tiles for
-// Q X (1,024 long, 256 tiles), 500 without; 24 of 256 x 512 (256 long, 192 tiles) 185 and 176.  Four teams instead of two: 1 of 1024 x 1024 232 us
+// 128 x 128 tiles (half the reads), where the sums are long enough to pay for the larger tile's ends (512), where the tiles are one for most CUs or
+// more than three for two (257 to 384 leave half of the CUs idle for the second), and where they cover the result with no more than a 16th of it for nothing
+// beyond what tiles of 64 do.  All five steps, us, with the larger tiles and without: Q X of 2 of 1024 x 2048 (256 tiles) 468 and 500, 1 of 3200 x 3200
+// (625) 2,834 and 3,150, 24 of 256 x 512 (256 long) 185 and 176, 3 of 1280 x 1280 (300) 734 and 668, 4 of 1000 x 1300 (352) 642 and 615, 14 of 520 x 900 (a
+// fifth for nothing) 593 and 528; X X' and P P of 7 of 1024 x 1024 (252) 734 and 745, 3 of 1536 x 1536 (234) 952 and 1,001, 1 of 2560 x 2560 (210) 1,381 and
+// 1,593, 2 of 2560 x 2560 (420) 2,711 and 2,867, 1 of 3500 x 3500 (406) 3,524 and 3,927, 8 of 1024 x 1024 (288) 968 and 832, 2 of 2048 x 2048 (272) 1,725
+// and 1,489, 13 of 640 x 640 (an 11th for nothing) 525 and 468, 20 of 520 x 700 (a third) 729 and 577.
+//
+// Else 64 x 64; two teams to a tile, four where the CUs have one tile at most and the sums are long.  Four teams instead of two: 1 of 1024 x 1024 232 us
 // instead of 254, 4 of 400 x 800 (shorter sums) 214 instead of 195, 24 of 256 x 512 206 instead of 176, 2 of 1024 x 2048 (272 tiles) 541 instead of 498, 5 of
 // 640 x 640 (275 tiles) 298 instead of 265.
 template <int STAGE, class T>
@@ -630,13 +636,14 @@ void launch_product(const OrthoArgs &a, int from, hipStream_t st)
         return a.batch * (SYMMETRIC ? (int64_t)rt * (rt + 1) / 2 : (int64_t)rt * ct);
     };
     int rt, ct;
-    const int64_t large = tiles(128, rt, ct);
+    const int64_t small = tiles(64, rt, ct), large = tiles(128, rt, ct);
     const int depth = STAGE == GRAM ? a.np : a.mp;
-    if (large >= 192 && depth >= 512) {
+    const bool filled = large >= 192 && (large <= 256 || large > 384), covers = 64 * large <= 17 * small;
+    if (filled && covers && depth >= 512) {
         k_ortho_product<4, STAGE, T, 2><<<dim3((unsigned)((large + 7) / 8 * 8)), dim3(2 * kThreads), 0, st>>>(a, from, rt, ct);
         return;
     }
-    const int64_t small = tiles(64, rt, ct);
+    tiles(64, rt, ct);
     const dim3 grid((unsigned)((small + 7) / 8 * 8));
     if (small <= 256 && depth >= 640) k_ortho_product<2, STAGE, T, 4><<<grid, dim3(4 * kThreads), 0, st>>>(a, from, rt, ct);
     else k_ortho_product<2, STAGE, T, 2><<<grid, dim3(2 * kThreads), 0, st>>>(a, from, rt, ct);

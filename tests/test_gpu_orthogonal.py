@@ -188,3 +188,57 @@ def test_updates_whose_norm_is_beyond_fp32(torch, B, dtype, rows, cols):
     check(torch, B, signs * np.array([2.0 ** 127, 2.0 ** 126])[:, None, None], dtype)
     if dtype == "f32":
         check(torch, B, np.eye(rows, cols)[None] * 2.0 ** -147, dtype, eps=0.0)
+
+
+def chosen_kernels(batch, rows, cols):
+    """(tile side, teams) of each stage's kernel, by the rule that the library's source states today: shapes that a new rule sends elsewhere are noticed."""
+    import os
+    import re
+    from paper_2112_08541_amd import buildlib
+    text = open(os.path.join(buildlib.CSRC, "bgl_orthogonal.hip")).read()
+    least, one, more, a, b = (int(v) for v in re.search(r"filled = large >= (\d+) && \(large <= (\d+) \|\| large > (\d+)\), covers = (\d+) \* large <= (\d+) \* small;",
+                                                        text).groups())
+    depth_large, = (int(v) for v in re.search(r"if \(filled && covers && depth >= (\d+)\)", text).groups())
+    few, depth_four = (int(v) for v in re.search(r"if \(small <= (\d+) && depth >= (\d+)\)", text).groups())
+    m, n = sorted((rows, cols))
+    up = lambda v, to: -(-v // to)      # noqa: E731
+
+    def stage(symmetric, depth):
+        def tiles(side):
+            r, c = up(m, side), up(n, side)
+            return batch * (r * (r + 1) // 2 if symmetric else r * c)
+        small, large = tiles(64), tiles(128)
+        if large >= least and (large <= one or large > more) and a * large <= b * small and depth >= depth_large:
+            return 128, 2
+        return 64, 4 if small <= few and depth >= depth_four else 2
+    mp, np_ = 32 * up(m, 32), 32 * up(n, 32)
+    return [stage(True, np_), stage(True, mp), stage(False, mp)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("batch,rows,cols,kernels", [
+    (6, 997, 1299, [(128, 2)] * 3), (6, 1299, 997, [(128, 2)] * 3), (7, 1024, 1024, [(128, 2)] * 3),
+    (1, 651, 703, [(64, 4)] * 3), (1, 703, 651, [(64, 4)] * 3), (1, 640, 1024, [(64, 4)] * 3),
+    (3, 1000, 1600, [(64, 2), (64, 2), (64, 2)]), (2, 1024, 2000, [(64, 2), (64, 2), (128, 2)]), (2, 2000, 1024, [(64, 2), (64, 2), (128, 2)])])
+def test_every_kernel_of_the_products(torch, B, dtype, batch, rows, cols, kernels):
+    """Larger and smaller tiles, two and four teams, both orders, whole tiles and remainders; against 64 bits on the GPU."""
+    assert chosen_kernels(batch, rows, cols) == kernels
+    steps, eps = 2, 1e-7
+    dt = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    u = torch.randn((batch, rows, cols), device="cuda", generator=torch.Generator(device="cuda").manual_seed(rows)).to(dt)
+    out = torch.full_like(u, float("nan"))
+    B.Orthogonalizer(batch, rows, cols, dt, steps, USUAL, eps).run(u, out)
+    a, b, c = (float(np.float32(v)) for v in USUAL)
+    for i in range(batch):
+        x = u[i].double()
+        x = x / (x.square().sum().sqrt() + float(np.float32(eps)))
+        x = x.t().contiguous() if rows > cols else x
+        most = 1.0
+        for _ in range(steps):
+            p = x @ x.t().contiguous()
+            x = a * x + (b * p + c * p @ p) @ x
+            most = max(most, float(x.norm()))
+        want = x.t() if rows > cols else x
+        bound = steps * a ** steps * 16 * 2.0 ** -22 * most + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * float(want.norm()) * 1.01
+        off = float((out[i].double() - want).norm())
+        assert off <= bound, f"matrix {i}: {off:.3g} off, bound {bound:.3g}"
