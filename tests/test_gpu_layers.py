@@ -590,3 +590,95 @@ def test_tensors_that_require_gradients_are_refused_rather_than_their_gradients_
     lay.backward(dy, x, w, saved, dx, dw, db, dr)
     for leaf, want in zip(leaves, (dx, dw, db, dr)):
         assert torch.equal(leaf.grad, want)
+
+
+def rows_for_large_tiles(columns):
+    """The fewest rows whose product of `columns` columns the library makes in tiles of 128 rows, by the rule that its source states today."""
+    import os
+    import re
+    from paper_2112_08541_amd import buildlib
+    text = open(os.path.join(buildlib.CSRC, "bgl_linear.hip")).read()
+    least, = re.search(r"bool large_tiles\(int64_t n, int64_t cols\) \{ return ceil_div\(n, 128\) \* ceil_div\(cols, 128\) >= (\d+); \}", text).groups()
+    return (-(-int(least) // -(-columns // 128)) - 1) * 128 + 1
+
+
+def exact_layer(torch, B, dtype, n, K, N, act, mode, groups=0, in_place=False, want_dx=True, seed=0):
+    """A layer over small whole numbers: all sums are whole and below 2^24, so every output has one right value, which is then
+    rounded to the type once; a row or a column left out, or counted twice, is another one."""
+    dt, G = dtype_of(torch, dtype), max(groups, 1)
+    gen = torch.Generator(device="cuda").manual_seed(1000 * seed + n)
+    whole = lambda *s: torch.randint(-2, 3, s, generator=gen, device="cuda").to(dt)      # noqa: E731
+    x, w, b, dy = whole(n, K), whole(G, N, K), whole(G, N), whole(n, N)
+    r = whole(n, N) if mode != "none" else None
+    group, rg = torch.zeros(n, dtype=torch.int64, device="cuda"), None
+    if groups:
+        of = torch.randint(-1, groups, (n,), generator=gen, dtype=torch.int32, device="cuda")
+        rg = B.RowGroups(n, groups)
+        rg.build(of)
+        group = of.long()
+    z = torch.zeros((n, N), dtype=torch.float64, device="cuda")
+    members = [torch.nonzero(group == g).squeeze(1) for g in range(G)]
+    for g, at in enumerate(members):
+        z[at] = x[at].double() @ w[g].double().t().contiguous() + b[g].double()
+    if mode == "before":
+        z += r.double()
+    y64 = z.clamp(min=0) if act == "relu" else z
+    if mode == "after":
+        y64 = y64 + r.double()
+    dz = dy.double() * (z > 0) if act == "relu" else dy.double()
+    dx64 = torch.zeros((n, K), dtype=torch.float64, device="cuda")
+    dw64, db64 = torch.zeros((G, N, K), dtype=torch.float64, device="cuda"), torch.zeros((G, N), dtype=torch.float64, device="cuda")
+    for g, at in enumerate(members):
+        dx64[at] = dz[at] @ w[g].double()
+        dw64[g] = dz[at].t().contiguous() @ x[at].double()
+        db64[g] = dz[at].sum(0)
+    assert max(float(t.abs().max()) for t in (z, dx64, dw64, db64)) < 2 ** 24
+    lay = B.Linear(n, K, N, dt, act, mode, groups)
+    lay.workspace = B._workspace(lay._bytes(n)).fill_(0xFF)      # NaN wherever nothing is written
+    y, dw, db = torch.full_like(dy, float("nan")), torch.full_like(w, float("nan")), torch.full_like(b, float("nan"))
+    saved = torch.full_like(dy, float("nan")) if act != "none" else None
+    dx = torch.full_like(x, float("nan")) if want_dx else None
+    dres = None if mode != "before" else dy if in_place else torch.full_like(dy, float("nan"))
+    one = lambda t: t if groups else t[0]      # noqa: E731
+    lay.forward(x, one(w), y, one(b), r, saved, rg)
+    lay.backward(dy, x, one(w), saved, dx, one(dw), one(db), dres, rg)
+    for name, got, want in (("y", y, y64), ("dx", dx, dx64), ("dresidual", dres, dz), ("dweight", dw, dw64), ("dbias", db, db64)):
+        if got is not None:
+            wrong = got != want.to(dt)
+            assert not bool(wrong.any()), f"{name}: {int(wrong.sum())} of {wrong.numel()} values, the first at {torch.nonzero(wrong)[0].tolist()}"
+
+
+# one width for each number of blocks of 16 columns up to a tile's eight, whole and cut, and two tiles of columns
+WIDTHS = [3, 16, 31, 45, 64, 77, 96, 100, 127, 250]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("groups", [0, 5])
+@pytest.mark.parametrize("i", range(len(WIDTHS)))
+def test_large_tiles_of_every_width(torch, B, dtype, i, groups):
+    """Forward tiles as wide as N, those of dx as wide as K; dz made within dx (relu) and none (no activation)."""
+    K, N = WIDTHS[i], WIDTHS[-1 - i]
+    n = rows_for_large_tiles(min(K, N)) + 45
+    exact_layer(torch, B, dtype, n, K, N, "relu", "before", groups, seed=1)
+    exact_layer(torch, B, dtype, n, K, N, "none", "after", groups, seed=2)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("groups", [0, 5])
+@pytest.mark.parametrize("K,N", [(100, 256), (512, 256), (300, 40), (260, 130), (128, 70), (200, 33)])
+def test_large_tiles_with_dz_within_dx_apart_and_in_the_place_of_dy(torch, B, dtype, K, N, groups):
+    """dx of one tile of columns, of two, and of so many that dz is made before it; the same with dz in dy's place."""
+    n = max(rows_for_large_tiles(K), rows_for_large_tiles(N)) + 83
+    exact_layer(torch, B, dtype, n, K, N, "relu", "before", groups, seed=3)
+    exact_layer(torch, B, dtype, n, K, N, "relu", "before", groups, in_place=True, seed=4)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("groups", [0, 40])
+@pytest.mark.parametrize("width", WIDTHS)
+def test_no_row_is_left_out_of_a_weight_gradient_of_any_width(torch, B, dtype, width, groups):
+    """The narrower side of dW's tiles as wide as `width`, on either side of the product; small tiles of the other products too."""
+    n = rows_for_large_tiles(128) // 3
+    exact_layer(torch, B, dtype, n, width, 300, "none", "none", groups, want_dx=False, seed=5)
+    exact_layer(torch, B, dtype, n, 140, width, "relu", "before", groups, seed=6)
+    exact_layer(torch, B, dtype, n, width, 60, "none", "none", groups, seed=7)
