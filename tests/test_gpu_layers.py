@@ -682,3 +682,57 @@ def test_no_row_is_left_out_of_a_weight_gradient_of_any_width(torch, B, dtype, w
     exact_layer(torch, B, dtype, n, width, 300, "none", "none", groups, want_dx=False, seed=5)
     exact_layer(torch, B, dtype, n, 140, width, "relu", "before", groups, seed=6)
     exact_layer(torch, B, dtype, n, width, 60, "none", "none", groups, seed=7)
+
+
+@pytest.mark.parametrize("dtype,act", [("f32", "gelu"), ("f32", "silu"), ("bf16", "gelu"), ("bf16", "silu")])
+@pytest.mark.parametrize("K,N,groups", [(100, 96, 0), (300, 160, 0), (40, 256, 6)])
+def test_gradients_of_smooth_activations_miss_no_row(torch, B, dtype, act, K, N, groups):
+    """dresidual is dz as the products read it, so dx and dW are its products but for their own sums and the type's rounding.  bf16 layers add db up
+    before dz is rounded: against the slopes of z as it was kept, a half, within 2^-15 of each term (the activation's) and the sum's error.  The sums' errors
+    are taken as 8 sqrt(rows) u of the largest partial sum a random walk of the terms reaches, not as the linear worst case, which hides hundreds of rows."""
+    dt, G = dtype_of(torch, dtype), max(groups, 1)
+    n = max(rows_for_large_tiles(K), rows_for_large_tiles(N)) + 17
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    f = lambda *s: torch.randn(s, generator=gen, device="cuda")      # noqa: E731
+    x, w, b, r, dy = f(n, K).to(dt), (f(G, N, K) / K ** 0.5).to(dt), f(G, N).to(dt), f(n, N).to(dt), f(n, N).to(dt)
+    group, rg = torch.zeros(n, dtype=torch.int64, device="cuda"), None
+    if groups:
+        of = torch.randint(-1, groups, (n,), generator=gen, dtype=torch.int32, device="cuda")
+        rg, group = B.RowGroups(n, groups), of.long()
+        rg.build(of)
+    lay = B.Linear(n, K, N, dt, act, "before", groups)
+    y, saved, dres, dx, dw, db = (torch.full_like(t, float("nan")) for t in (dy, dy, dy, x, w, b))
+    one = lambda t: t if groups else t[0]      # noqa: E731
+    lay.forward(x, one(w), y, one(b), r, saved, rg)
+    lay.backward(dy, x, one(w), saved, dx, one(dw), one(db), dres, rg)
+    v = U if dtype == "f32" else 2.0 ** -8
+    z = (saved.view(torch.float16) if dtype == "bf16" else saved).double()
+    if act == "gelu":
+        p = 0.5 * torch.special.erfc(-z / 2 ** 0.5)
+        bell = z * torch.exp(-z * z / 2) / (2 * np.pi) ** 0.5
+        slope, mass = p + bell, p + bell.abs()
+    else:
+        p = torch.sigmoid(z)
+        slope, mass = p * (1 + z * (1 - p)), p * (1 + z.abs() * (1 - p)) + z.abs() * p * p
+    dz, d64 = dy.double() * slope, dres.double()
+    places = 20 * U if dtype == "f32" else 2.0 ** -15
+    near = lambda name, got, want, bound: _near(torch, name, got, want, bound)      # noqa: E731
+    near("dresidual", dres, dz, v * 1.001 * dz.abs() + places * dy.double().abs() * mass + 1e-30)
+    for g in range(G):
+        at = torch.nonzero(group == g).squeeze(1)
+        x64, w64, d = x[at].double(), w[g].double(), d64[at]
+        z64 = x64 @ w64.t().contiguous() + b[g].double() + r[at].double()
+        kept = 2.0 ** -11 if dtype == "bf16" else U
+        near("z", (saved.view(torch.float16) if dtype == "bf16" else saved)[at], z64,
+             kept * 1.001 * z64.abs() + (K + 4) * U * (x64.abs() @ w64.abs().t().contiguous() + b[g].double().abs() + r[at].double().abs()) + 2.0 ** -24)
+        near("dx", dx[at], d @ w64, v * 1.001 * (d @ w64).abs() + (N + 4) * U * (d.abs() @ w64.abs()) + 1e-30)
+        walk = (d.square().t().contiguous() @ x64.square()).sqrt()
+        near("dweight", dw[g], d.t().contiguous() @ x64, v * 1.001 * (d.t().contiguous() @ x64).abs() + 8 * len(at) ** 0.5 * U * walk + 1e-30)
+        want = dz[at].sum(0)
+        near("dbias", db[g], want, v * 1.001 * want.abs() + 8 * len(at) ** 0.5 * U * dz[at].square().sum(0).sqrt()
+             + places * (dy[at].double().abs() * mass[at]).sum(0) + 1e-30)
+
+
+def _near(torch, name, got, want, bound):
+    off = ((got.double() - want).abs() / bound)
+    assert bool(torch.isfinite(got).all()) and float(off.max()) <= 1.0, f"{name}: {float(off.max()):.2f} times the bound"
