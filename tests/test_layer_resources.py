@@ -18,3 +18,18 @@ def test_no_kernel_of_the_layers_spills(source, kernels):
         # forward products with 128 x 128 tiles (cut <2, 2, 4, 4>)
         if re.search(r"k_linear_rows.*Lb0E.*CutILi2ELi2ELi4ELi4E", name):
             assert u["Occupancy"] >= 3 and u["LDS Size"] <= 160 * 1024 // 3, (name, u)
+
+
+def test_every_row_product_keeps_its_workgroups_on_a_cu():
+    """Row products of one team: three workgroups of large tiles on a CU, two where dz is made on the way (rows of dy and of z wait in registers
+    side by side), five of small tiles, four with dz; dW: two."""
+    least, seen = {(128, "0"): 3, (128, "1"): 2, (64, "0"): 5, (64, "1"): 4}, set()
+    for name, u in resource_usage("bgl_linear.hip").items():
+        m = re.search(r"k_linear_rows.*CutILi(\d)ELi\dELi(\d)ELi\dEEELb\dELi1ELb(\d)E", name)
+        if m:
+            kind = 16 * int(m.group(1)) * int(m.group(2)), m.group(3)        # rows of a tile; dz or not
+            seen.add(kind)
+            assert u["Occupancy"] >= least[kind], (kind, name, u)
+        if "k_linear_dw" in name:
+            assert u["Occupancy"] >= 2, (name, u)
+    assert seen == set(least)
