@@ -718,7 +718,9 @@ int bgl_pipeline_run(bgl_pipeline_t *p, const int32_t *seeds, int64_t seed_batch
  *
  * Matrices are rows of values, stride values apart (row i at data + i * stride;
  * the row's width <= stride < 2^31, alignment that of the values).  Products are summed
- * in fp32; results are rounded once, to the layer's type.  All calls enqueue on
+ * in fp32 and results rounded to the layer's type, once, but that a bf16 layer's gradients
+ * see z and dz rounded: z as it was kept (gelu and silu: to a half), and dz, with these
+ * two, to bf16 where the products of dx and dweight read it.  All calls enqueue on
  * `stream`, allocate nothing, keep nothing between calls and can be captured.
  */
 #define BGL_F32 0
@@ -726,8 +728,8 @@ int bgl_pipeline_run(bgl_pipeline_t *p, const int32_t *seeds, int64_t seed_batch
 
 #define BGL_ACT_NONE 0
 #define BGL_ACT_RELU 1
-#define BGL_ACT_GELU 2 /* z Phi(z), with the error function */
-#define BGL_ACT_SILU 3 /* z / (1 + exp(-z)) */
+#define BGL_ACT_GELU 2 /* z Phi(z), with the error function: fp32 right to 16 u of the value, u = 2^-24 */
+#define BGL_ACT_SILU 3 /* z / (1 + exp(-z)): to 10 u */
 
 #define BGL_RESIDUAL_NONE 0
 #define BGL_RESIDUAL_BEFORE 1 /* y = act(x W' + b + r) */

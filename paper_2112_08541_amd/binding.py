@@ -616,7 +616,11 @@ class Linear:
 
     y = act(x weight' + bias [+ residual]) [+ residual]; activation: none, relu, gelu, silu; residual: none, before (the
     activation), after.  num_groups > 0: weight (num_groups, out_dim, in_dim) and bias (num_groups, out_dim), and every call is
-    given the batch's RowGroups."""
+    given the batch's RowGroups.
+
+    Sums are fp32.  In bf16, gelu and silu keep z as a half in `saved`, and their dz is rounded to bf16 before dx and dweight (not
+    dbias) are made of it.  Like RowGroups and Orthogonalizer, an object is kept until its calls on other streams than the one it was
+    made on have ended."""
 
     def __init__(self, max_rows: int, in_dim: int, out_dim: int, dtype=torch.float32, activation: str = "none",
                  residual: str = "none", num_groups: int = 0):

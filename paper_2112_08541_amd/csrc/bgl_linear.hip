@@ -6,8 +6,10 @@
 //   dx = dz W                                                     k_linear_dx
 //   dW = dz' x, db = sum dz                                       k_linear_dw (by ranges of rows), k_linear_reduce
 //
-// Sums are kept in fp32 whatever the type; z is rounded to the type where it is kept for the gradient, dz because the matrix units
-// read it in the type (bf16: off by 2^-8 of themselves at most, as the rows they meet are).
+// Sums are kept in fp32 whatever the type, and every result is rounded once.  What is rounded besides, in bf16 layers: z where it is kept for the gradient
+// (gelu and silu: to a half, 2^-11; relu: to bf16, of which only the sign counts) and the dz of gelu and silu, because the matrix units read it in the type
+// (2^-8 of itself at most, as the rows and weights that it meets are; without an activation and with relu it is dy or 0).  dx and dW are then some 1.4 times
+// as far off as with dz in 32 bits; db is summed before.
 #include "bgl_internal.h"
 #include "bgl_tile.h"
 
@@ -271,14 +273,15 @@ __device__ __forceinline__ void store_cols(typename T::elem *p, int left, const 
 // One kernel for both: rows (n x K) times a weight whose summed index is contiguous (forward: out_dim x in_dim, B_OC false) or is
 // not (dx: the summed index is out_dim, B_OC true).
 //
-// A workgroup makes one tile of the result from operands staged through 32 KB of LDS, one tile of both ahead in registers; three workgroups a CU, each of
-// which fills the waits of the others, do more than a second buffer would.  Tiles of one block of rows go to one XCD, whose L2 then has the rows.
+// A workgroup makes one tile of the result from operands staged through 32 KB of LDS, one tile of both ahead in registers; three workgroups a CU (two
+// with dz), each of which fills the waits of the others, do more than a second buffer would.  Tiles of one block of rows go to one XCD, whose L2 then has the rows.
 //
-//   f32 100 -> 256, 428,377 rows, y and z written   405 us: 1.05 GB at 2.6 TB/s, 54 TFLOP/s; matrix units busy 46 % of the time: reading, multiplying
-//                                                   (157 us) and writing follow each other in a workgroup, and three overlap in part
-//   f32 dx and dz of it                             423 us: 1.49 GB at 3.5 TB/s, 52 TFLOP/s; matrix units 44 %
-//   bf16 512 -> 256, 302,709 rows, residual, z      179 us: 930 MB at 5.2 TB/s (a copy's rate), 443 TFLOP/s
-//   bf16 dx of it                                   160 us: 465 MB, 496 TFLOP/s, matrix units 23 %
+//   f32 100 -> 256, 428,377 rows, gelu, y and z written   414 us: 1.05 GB at 2.5 TB/s, 53 TFLOP/s; matrix units busy 44 % of the time: reading,
+//                                                   multiplying (157 us) and writing follow each other in a workgroup, and three overlap in part
+//   f32 dx and dz of it                             445 us: 1.49 GB at 3.3 TB/s, 49 TFLOP/s; matrix units 42 %; dz made on the way takes the registers of
+//                                                   the third workgroup
+//   bf16 512 -> 256, 302,709 rows, residual, z      179 us: 775 MB at 4.3 TB/s, 443 TFLOP/s
+//   bf16 dx of it                                   161 us: 465 MB, 493 TFLOP/s, matrix units 23 %
 //   bf16 512 -> 512, 302,709 rows, residual         280 us: 930 MB, 567 TFLOP/s: a tile's loads, its 96 KB through LDS (a fragment is read for each of
 //                                                   its users), its products and its epilogue take about equally long
 //   one row of 512 -> 512 bf16                      4.9 us, f32 100 -> 128 of 5,485 rows 7.2: one tile's loads, products and stores, one after the other
@@ -401,7 +404,7 @@ struct DzOperand : KcOperand<T, BO> {
     }
 };
 
-// DZ: x is dy, and dz is made from it and from z on the way (dx alone, where one tile has all columns).  TEAMS of 256 threads take the summed
+// DZ: x is dy, and dz is made from it and from z on the way (dx of few tiles of columns, each of which makes it again).  TEAMS of 256 threads take the summed
 // index's tiles in turn; their sums meet when the rows are finished.
 template <class T, bool B_OC, class C, bool NARROW, int TEAMS, bool DZ>
 __global__ __launch_bounds__(kThreads * TEAMS, 2) void k_linear_rows(RowsArgs<T> a)
@@ -491,8 +494,8 @@ __device__ __forceinline__ int64_t shares_of(int64_t units, int planned) { retur
 // dz of all rows, in group order, and the sums of its columns before they are rounded (bf16: sums of rounded values would be off by as much again as
 // the result's own rounding).  The rows, in units of kUnit, are dealt evenly to `shares` workgroups; share w leaves its sums for group g in slot
 // w + g of `part`.  A thread has VEC neighbouring columns, kDzColumns of a workgroup's rows at a time at most (blockIdx.y: which).  Bound by its bytes:
-// bf16 256 columns, 302,709 rows, relu (no sums) 90 us, 465 MB at 5.2 TB/s; gelu with the sums of 24 groups 120 us, 3.9 TB/s: 70 % of the time has vector
-// instructions in flight (the slope is some 25 of them a value) and rows are reached through the group order.
+// bf16 256 columns, 302,709 rows, relu (no sums) 90 us, 465 MB at 5.2 TB/s; gelu with the sums of 24 groups 122 us, 3.8 TB/s: 69 % of the time has vector
+// instructions in flight (the slope is some 30 of them a value) and rows are reached through the group order.
 constexpr int kDzColumns = 2048;
 
 template <class T>
@@ -903,12 +906,6 @@ __global__ __launch_bounds__(kGroupThreads) void k_group_place(GroupArgs a)
 }
 
 // ----------------------------------------------------------------- host side
-struct Shape {
-    const bgl_linear_t *l;
-    int64_t n;
-    int classes;  // groups at least one
-};
-
 int check_layer(const bgl_linear_t *l, int64_t n)
 {
     if (!l) BGL_FAIL(BGL_EINVAL, "layer is null");
@@ -953,8 +950,15 @@ int check_rows(const char *name, const void *p, int64_t stride, int width, int e
     } while (0)
 
 // Cuts of a product into workgroup tiles.  Wide results take 128 x 128; one that fits into fewer than 8 fragments of 16 columns takes as many as
-// it has (100 columns: 7), the four wavefronts one above the other: f32 100 -> 256 with its gradients, 428,377 rows 1,030 us, 1,060 with 128 columns;
-// f32 100 -> 64, 5,485 rows of 4 types, 42 and 46.  Wavefronts with 128 x 64 or 96 x 64 sums each, instead of 64 x 64, take the registers of the third
+// it has (100 columns: 7), the four wavefronts one above the other.  us so and with 128 columns (large tiles) or 64 (small ones), 100,000 rows of 512, then
+// dW over 100,000 rows:
+//   columns                 16           32           48           64           80           96           112
+//   forward f32         41 and 146   48 and 147   66 and 146   83 and 146  104 and 147  117 and 147  136 and 148
+//   forward bf16        21 and 30    21 and 30    24 and 29    24 and 29    26 and 30    28 and 30    29 and 30
+//   dW f32              40 and 123   48 and 122   62 and 122   74 and 123   89 and 124  102 and 125  117 and 126
+//   dW bf16             25 and 31    26 and 31    28 and 32    29 and 31    32 and 33    33 and 33    34 and 34.5
+//   forward f32, 5,485 rows  9.5 and 16  11 and 16  13 and 16; dW 14 and 23, 16 and 24, 19 and 25; bf16 there within 1 us, dW 12 and 15, 13 and 16, 16 and 17.5
+// dx as forward.  f32 100 -> 256 with its gradients, 428,377 rows 1,030 and 1,060; f32 100 -> 64, 5,485 rows of 4 types, 42 and 46.  Wavefronts with 128 x 64 or 96 x 64 sums each, instead of 64 x 64, take the registers of the third
 // workgroup of a CU (bf16 512 -> 512, 302,709 rows: 316 to 326 us instead of 297), and 64 x 128 tiles read more (354 instead of 325).
 using Large = Cut<2, 2, 4, 4>;
 using Small = Cut<2, 2, 2, 2>;
