@@ -656,8 +656,8 @@ class Linear:
         differentiation does not see the call: tensors that require gradients are refused, as by torch's functions with an out argument, unless
         gradient mode is off (under torch.no_grad(), or in the forward of a torch.autograd.Function whose backward makes the backward call)."""
         n = int(x.shape[0])
-        if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or bias is not None and bias.requires_grad
-                                        or residual is not None and residual.requires_grad):
+        if torch.is_grad_enabled() and (x.requires_grad or weight is not None and weight.requires_grad
+                                        or bias is not None and bias.requires_grad or residual is not None and residual.requires_grad):
             raise ValueError("the layer does not record gradients: call it under torch.no_grad() and make the backward call yourself")
         if n > self.max_rows:
             raise ValueError(f"{n} rows, the layer was made for {self.max_rows}")

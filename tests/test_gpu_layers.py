@@ -736,3 +736,18 @@ def test_gradients_of_smooth_activations_miss_no_row(torch, B, dtype, act, K, N,
 def _near(torch, name, got, want, bound):
     off = ((got.double() - want).abs() / bound)
     assert bool(torch.isfinite(got).all()) and float(off.max()) <= 1.0, f"{name}: {float(off.max()):.2f} times the bound"
+
+
+def test_a_layer_without_its_weight_is_the_librarys_error(torch, B):
+    x, y = torch.zeros((3, 8), device="cuda"), torch.zeros((3, 4), device="cuda")
+    with pytest.raises(B.BglError, match="weight"):
+        B.Linear(3, 8, 4).forward(x, None, y)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+def test_activations_of_values_that_are_not_finite(torch, B, dtype, act):
+    """z times a probability: infinity stays, minus infinity meets 0 and is not a number, as in the formula; nothing else is touched."""
+    z = np.array([np.inf, np.nan, -np.inf, 1e30, -1e30, 0.0, -0.0])
+    _, y, _ = single_values(torch, B, dtype, act, z)
+    assert np.isposinf(y[0]) and np.isnan(y[1]) and np.isnan(y[2]) and abs(y[3] / 1e30 - 1) < 0.01 and (y[4:] == 0).all()
