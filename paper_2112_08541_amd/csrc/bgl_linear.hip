@@ -959,8 +959,8 @@ int check_rows(const char *name, const void *p, int64_t stride, int width, int e
 //   dW bf16             25 and 31    26 and 31    28 and 32    29 and 31    32 and 33    33 and 33    34 and 34.5
 //   5,485 rows, forward f32  7.6 and 14  9.3 and 14  12 and 14  (bf16: 6.0 either way, the call's host time)
 //   5,485 rows, dW f32       12 and 22   15 and 23   18 and 24; bf16 11 and 14, 12 and 15, 14 and 16
-// dx as forward.  f32 100 -> 256 with its gradients, 428,377 rows 1,030 and 1,060; f32 100 -> 64, 5,485 rows of 4 types, 42 and 46.  Wavefronts with 128 x 64 or 96 x 64 sums each, instead of 64 x 64, take the registers of the third
-// workgroup of a CU (bf16 512 -> 512, 302,709 rows: 316 to 326 us instead of 297), and 64 x 128 tiles read more (354 instead of 325).
+// dx as forward.  f32 100 -> 256 with its gradients, 428,377 rows 1,030 and 1,060; f32 100 -> 64, 5,485 rows of 4 types, 42 and 46.
+// Wavefronts with 128 x 64 or 96 x 64 sums each, instead of 64 x 64, take the registers of the third workgroup of a CU (bf16 512 -> 512, 302,709 rows: 316 to 326 us instead of 297), and 64 x 128 tiles read more (354 instead of 325).
 using Large = Cut<2, 2, 4, 4>;
 using Small = Cut<2, 2, 2, 2>;
 template <int F>
