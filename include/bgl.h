@@ -830,6 +830,43 @@ int bgl_orthogonalize(const void *update, int64_t update_matrix_stride, int64_t 
                       const float *coefficients, float eps, void *out, int64_t out_matrix_stride,
                       int64_t out_row_stride, void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * Layer norm over each row: m = mean(x), v = mean((x - m)^2), r = 1 / sqrt(v + eps),
+ * y = (x - m) r weight + bias.
+ *   weight, bias  device, width values each; null: ones, zeros
+ *   y             n rows of width; may be x itself (with its stride)
+ *   saved         device, n pairs of floats that receive m and r for the backward call, or null
+ * Sums are fp32; squares that leave its range do no harm (rows of values up to 1e38 are normalised as others).
+ * A row with a value that is not finite is NaN; other rows are not touched by it.
+ * n = 0 does nothing.
+ * Errors: BGL_EINVAL (null or misaligned pointers, strides, width < 1, eps outside
+ * [1e-12, inf), n outside [0, 2^31), unknown types), BGL_EUNSUPPORTED (width > BGL_MAX_DIM), BGL_EHIP.
+ */
+typedef struct {
+    int32_t dtype; /* of x, weight, bias, y and all gradients */
+    int32_t width;
+    float eps;
+} bgl_layer_norm_t;
+
+int bgl_layer_norm_forward(const bgl_layer_norm_t *norm, int64_t n, const void *x, int64_t x_stride,
+                           const void *weight, const void *bias, void *y, int64_t y_stride,
+                           float *saved, void *stream);
+
+/*
+ * Its gradients: with h = (x - m) r and d = dy weight, dx = r (d - mean(d) - h mean(d h)),
+ * dweight = the sum of dy h over the rows, dbias = that of dy.  Each may be null.
+ *   dx          may be dy itself (with its stride)
+ *   workspace   device, 256-byte aligned, >= bgl_layer_norm_workspace_bytes(norm, n); unused without dweight and dbias
+ * Gradients are written, not added to (zeros for n = 0).  The order of the sums is fixed by n
+ * and the width: repeated calls give the same bits.
+ * Errors: as bgl_layer_norm_forward, plus BGL_ECAPACITY (workspace too small).
+ */
+int bgl_layer_norm_workspace_bytes(const bgl_layer_norm_t *norm, int64_t n, size_t *bytes);
+int bgl_layer_norm_backward(const bgl_layer_norm_t *norm, int64_t n, const void *dy,
+                            int64_t dy_stride, const void *x, int64_t x_stride, const void *weight,
+                            const float *saved, void *dx, int64_t dx_stride, void *dweight,
+                            void *dbias, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -50,6 +50,7 @@ EXPORTS = [
     "bgl_group_rows_workspace_bytes", "bgl_group_rows",
     "bgl_linear_workspace_bytes", "bgl_linear_forward", "bgl_linear_backward",
     "bgl_orthogonalize_workspace_bytes", "bgl_orthogonalize",
+    "bgl_layer_norm_workspace_bytes", "bgl_layer_norm_forward", "bgl_layer_norm_backward",
 ]
 
 
@@ -73,6 +74,10 @@ class SubgraphStruct(C.Structure):
 
 class LinearStruct(C.Structure):
     _fields_ = [(name, C.c_int32) for name in ("dtype", "activation", "residual", "in_dim", "out_dim", "num_groups")]
+
+
+class LayerNormStruct(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("width", C.c_int32), ("eps", C.c_float)]
 
 
 class PipelineBuffers(C.Structure):
@@ -148,6 +153,10 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
                                       vp, i64, vp, C.c_size_t, vp]
     L.bgl_orthogonalize_workspace_bytes.argtypes = [i64, i32, i32, i32, C.POINTER(C.c_size_t)]
     L.bgl_orthogonalize.argtypes = [vp, i64, i64, i64, i32, i32, i32, i32, vp, C.c_float, vp, i64, i64, vp, C.c_size_t, vp]
+    norm = C.POINTER(LayerNormStruct)
+    L.bgl_layer_norm_workspace_bytes.argtypes = [norm, i64, C.POINTER(C.c_size_t)]
+    L.bgl_layer_norm_forward.argtypes = [norm, i64, vp, i64, vp, vp, vp, i64, vp, vp]
+    L.bgl_layer_norm_backward.argtypes = [norm, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp, vp, C.c_size_t, vp]
     for name in EXPORTS:
         if name != "bgl_last_error":
             getattr(L, name).restype = ci
@@ -576,6 +585,12 @@ def _weights(name: str, t: Optional[torch.Tensor], shape, dtype):
     return _dev_ptr(t, dtype)
 
 
+def _refuse_gradients(who: str, *tensors) -> None:
+    """Torch's own differentiation does not see the library's calls."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise ValueError(f"{who} does not record gradients: call it under torch.no_grad() and make the backward call yourself")
+
+
 class RowGroups:
     """bgl_group_rows: a batch's rows in group order, for layers with groups; owns rows, offsets and the workspace for
     batches of up to max_rows rows."""
@@ -722,3 +737,53 @@ class Orthogonalizer:
         _check(lib().bgl_orthogonalize(src[0], src[1], src[2], *self.shape, DTYPES[self.dtype], self.steps, self.coefficients.ctypes.data,
                                        self.eps, dst[0], dst[1], dst[2], self.workspace.data_ptr(), self.workspace.numel(),
                                        _stream_handle(stream)))
+
+
+class LayerNorm:
+    """bgl_layer_norm_forward / bgl_layer_norm_backward over rows of `width` values, batches of up to max_rows rows; owns the backward call's
+    workspace (allocated with the first backward call), so calls on one object must follow one another in stream order.
+
+    y = (x - mean) / sqrt(variance + eps) * weight + bias, with sums in fp32.  Like Linear, an object is kept until its calls on other
+    streams than the one it was made on have ended."""
+
+    def __init__(self, max_rows: int, width: int, dtype=torch.float32, eps: float = 1e-5):
+        _require_gpu()
+        if dtype not in DTYPES:
+            raise ValueError(f"unknown dtype: {dtype}")
+        self.max_rows, self.width, self.dtype, self.eps = int(max_rows), int(width), dtype, float(eps)
+        self.struct = LayerNormStruct(DTYPES[dtype], self.width, self.eps)
+        self._ref = C.byref(self.struct)
+        self._bytes()       # (checks the arguments)
+        self.workspace = None
+
+    def _bytes(self) -> int:
+        nbytes = C.c_size_t(0)
+        _check(lib().bgl_layer_norm_workspace_bytes(self._ref, self.max_rows, C.byref(nbytes)))
+        return int(nbytes.value)
+
+    def forward(self, x, y, weight=None, bias=None, saved=None, stream=None) -> None:
+        """Writes y (which may be x), and saved = (n, 2) floats if given (the backward call needs them).  Tensors that require gradients are
+        refused as by Linear.forward."""
+        n = int(x.shape[0])
+        _refuse_gradients("the norm", x, weight, bias)
+        if n > self.max_rows:
+            raise ValueError(f"{n} rows, the norm was made for {self.max_rows}")
+        _check(lib().bgl_layer_norm_forward(
+            self._ref, n, *_matrix("x", x, n, self.width, self.dtype), _weights("weight", weight, (self.width,), self.dtype),
+            _weights("bias", bias, (self.width,), self.dtype), *_matrix("y", y, n, self.width, self.dtype),
+            _weights("saved", saved, (n, 2), torch.float32), _stream_handle(stream)))
+
+    def backward(self, dy, x, saved, weight=None, dx=None, dweight=None, dbias=None, stream=None) -> None:
+        """Writes the gradients that are given memory: dx (which may be dy), dweight, dbias."""
+        n = int(dy.shape[0])
+        if n > self.max_rows:
+            raise ValueError(f"{n} rows, the norm was made for {self.max_rows}")
+        if self.workspace is None:
+            self.workspace = _workspace(self._bytes())
+            if stream is not None:      # (the memory may have been another tensor's on the current stream)
+                stream.wait_stream(torch.cuda.current_stream())
+        _check(lib().bgl_layer_norm_backward(
+            self._ref, n, *_matrix("dy", dy, n, self.width, self.dtype), *_matrix("x", x, n, self.width, self.dtype),
+            _weights("weight", weight, (self.width,), self.dtype), _weights("saved", saved, (n, 2), torch.float32),
+            *_matrix("dx", dx, n, self.width, self.dtype), _weights("dweight", dweight, (self.width,), self.dtype),
+            _weights("dbias", dbias, (self.width,), self.dtype), self.workspace.data_ptr(), self.workspace.numel(), _stream_handle(stream)))

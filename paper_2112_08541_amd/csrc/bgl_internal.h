@@ -36,6 +36,12 @@ void set_error(const char *fmt, ...);
         }                                                                           \
     } while (0)
 
+#define BGL_TRY(call)                  \
+    do {                               \
+        const int rc__ = (call);       \
+        if (rc__ != BGL_OK) return rc__; \
+    } while (0)
+
 // The C ABI promises that nothing throws: every entry point is a function-try-block whose
 // handler returns this (called inside the handler: it looks at the exception in flight).
 inline int caught()
@@ -58,6 +64,19 @@ inline int caught()
 inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// A matrix argument: rows of `width` values of `es` bytes, `stride` values apart.
+inline int check_rows(const char *name, const void *p, int64_t stride, int width, int es, bool needed)
+{
+    if (!p) {
+        if (needed) BGL_FAIL(BGL_EINVAL, "%s is null", name);
+        return BGL_OK;
+    }
+    if (!aligned(p, es)) BGL_FAIL(BGL_EINVAL, "%s must be aligned to its elements", name);
+    if (stride < width) BGL_FAIL(BGL_EINVAL, "%s: stride %lld is less than the row's %d values", name, (long long)stride, width);
+    if (stride > INT32_MAX) BGL_FAIL(BGL_EUNSUPPORTED, "%s: stride %lld does not fit 31 bits", name, (long long)stride);
+    return BGL_OK;
+}
 
 }  // namespace bgl
 

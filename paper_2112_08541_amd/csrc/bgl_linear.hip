@@ -931,24 +931,6 @@ int check_groups(const bgl_linear_t *l, const int32_t *rows, const int32_t *offs
 
 int elem_bytes(const bgl_linear_t *l) { return l->dtype == BGL_F32 ? 4 : 2; }
 
-int check_rows(const char *name, const void *p, int64_t stride, int width, int es, bool needed)
-{
-    if (!p) {
-        if (needed) BGL_FAIL(BGL_EINVAL, "%s is null", name);
-        return BGL_OK;
-    }
-    if (!aligned(p, es)) BGL_FAIL(BGL_EINVAL, "%s must be aligned to its elements", name);
-    if (stride < width) BGL_FAIL(BGL_EINVAL, "%s: stride %lld is less than the row's %d values", name, (long long)stride, width);
-    if (stride > INT32_MAX) BGL_FAIL(BGL_EUNSUPPORTED, "%s: stride %lld does not fit 31 bits", name, (long long)stride);
-    return BGL_OK;
-}
-
-#define BGL_TRY(call)                  \
-    do {                               \
-        const int rc__ = (call);       \
-        if (rc__ != BGL_OK) return rc__; \
-    } while (0)
-
 // Cuts of a product into workgroup tiles.  Wide results take 128 x 128; one that fits into fewer than 8 fragments of 16 columns takes as many as
 // it has (100 columns: 7), the four wavefronts one above the other.  us so and with 128 columns (large tiles) or 64 (small ones), 100,000 rows of 512, then
 // dW over 100,000 rows:
