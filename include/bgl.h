@@ -867,6 +867,63 @@ int bgl_layer_norm_backward(const bgl_layer_norm_t *norm, int64_t n, const void 
                             const float *saved, void *dx, int64_t dx_stride, void *dweight,
                             void *dbias, void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * Losses over the class scores z = x W' + b of n rows, which are not kept: softmax cross
+ * entropy with a label, and distillation from a teacher's best classes, alone or together.
+ *   labels            device, n classes, or null.  label_loss = log sum exp(z) - z[label]; a label outside
+ *                     [0, classes) means that the row has none: loss 0, no gradient
+ *   teacher_classes   device, n x top classes, or null; one outside [0, classes) is not there
+ *   teacher_scores    device, n x top scores s of these classes.  With p = softmax(s / t) over the classes that are there and
+ *                     q = softmax(z / t) over all, t the temperature: teacher_loss = t^2 sum p (log p - log q).  A row with none, or
+ *                     with scores of -inf alone, has loss 0 and no gradient.  A class named twice is two entries.
+ *   weight, bias      device, classes x in_dim, tight; classes values, or null.  A bias of -inf takes a class out; a row for which
+ *                     none is left has NaN
+ *   label_loss, teacher_loss  device, n floats each, or null
+ *   saved             device, n x (2 + top) floats that the backward call needs, or null
+ *   workspace         device, 256-byte aligned, >= *forward_bytes of bgl_class_loss_workspace_bytes(loss, n, ...)
+ * Sums are fp32.  Outputs must not overlap inputs or each other.  n = 0 does nothing.
+ * Errors: BGL_EINVAL (null or misaligned pointers, strides, sizes < 1, temperature outside [2^-10, 2^10], unknown
+ * types, a loss without what it is of), BGL_EUNSUPPORTED (in_dim > BGL_MAX_DIM, classes > BGL_MAX_CLASSES, top > BGL_MAX_TOP),
+ * BGL_ECAPACITY (workspace too small), BGL_EHIP.
+ */
+#define BGL_MAX_CLASSES (1 << 24)
+#define BGL_MAX_TOP 1024
+
+typedef struct {
+    int32_t dtype;     /* of x, weight, bias and all gradients */
+    int32_t in_dim;
+    int32_t classes;
+    int32_t top;       /* classes that the teacher names for each row; 0: there is none */
+    float temperature; /* the teacher's */
+} bgl_class_loss_t;
+
+int bgl_class_loss_workspace_bytes(const bgl_class_loss_t *loss, int64_t n, size_t *forward_bytes,
+                                   size_t *backward_bytes);
+int bgl_class_loss_forward(const bgl_class_loss_t *loss, int64_t n, const void *x, int64_t x_stride,
+                           const void *weight, const void *bias, const int32_t *labels,
+                           const int32_t *teacher_classes, const float *teacher_scores,
+                           float *label_loss, float *teacher_loss, float *saved, void *workspace,
+                           size_t workspace_bytes, void *stream);
+
+/*
+ * Gradients of scale * sum(label_loss) + teacher_scale * sum(teacher_loss): the scores again, piece by piece, dz =
+ * scale (softmax(z) - onehot) + teacher_scale t (q - p), dx = dz W, dweight = dz' x, dbias = the sum of dz's rows.
+ *   saved       the forward call's, of the same rows, weights, labels and teacher.  labels or the teacher may be left out (null):
+ *               that loss then has no gradient
+ *   dx, dweight, dbias  each may be null (dbias is not given without dweight)
+ *   workspace   device, 256-byte aligned, >= *backward_bytes
+ * Gradients are written, not added to (n = 0: zeros); dx = 0 for rows without a label and a teacher, whose x is not read for dweight.
+ * In bf16 the products and dbias read dz rounded to bf16.  The order of the sums is fixed by n and the sizes:
+ * repeated calls give the same bits.
+ * Errors: as bgl_class_loss_forward.
+ */
+int bgl_class_loss_backward(const bgl_class_loss_t *loss, int64_t n, const void *x, int64_t x_stride,
+                            const void *weight, const void *bias, const int32_t *labels,
+                            const int32_t *teacher_classes, const float *teacher_scores,
+                            const float *saved, float scale, float teacher_scale, void *dx,
+                            int64_t dx_stride, void *dweight, void *dbias, void *workspace,
+                            size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -51,6 +51,7 @@ EXPORTS = [
     "bgl_linear_workspace_bytes", "bgl_linear_forward", "bgl_linear_backward",
     "bgl_orthogonalize_workspace_bytes", "bgl_orthogonalize",
     "bgl_layer_norm_workspace_bytes", "bgl_layer_norm_forward", "bgl_layer_norm_backward",
+    "bgl_class_loss_workspace_bytes", "bgl_class_loss_forward", "bgl_class_loss_backward",
 ]
 
 
@@ -78,6 +79,10 @@ class LinearStruct(C.Structure):
 
 class LayerNormStruct(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("width", C.c_int32), ("eps", C.c_float)]
+
+
+class ClassLossStruct(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("in_dim", C.c_int32), ("classes", C.c_int32), ("top", C.c_int32), ("temperature", C.c_float)]
 
 
 class PipelineBuffers(C.Structure):
@@ -157,6 +162,10 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     L.bgl_layer_norm_workspace_bytes.argtypes = [norm, i64, C.POINTER(C.c_size_t)]
     L.bgl_layer_norm_forward.argtypes = [norm, i64, vp, i64, vp, vp, vp, i64, vp, vp]
     L.bgl_layer_norm_backward.argtypes = [norm, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp, vp, C.c_size_t, vp]
+    loss = C.POINTER(ClassLossStruct)
+    L.bgl_class_loss_workspace_bytes.argtypes = [loss, i64, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]
+    L.bgl_class_loss_forward.argtypes = [loss, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    L.bgl_class_loss_backward.argtypes = [loss, i64, vp, i64, vp, vp, vp, vp, vp, vp, C.c_float, C.c_float, vp, i64, vp, vp, vp, C.c_size_t, vp]
     for name in EXPORTS:
         if name != "bgl_last_error":
             getattr(L, name).restype = ci
@@ -787,3 +796,65 @@ class LayerNorm:
             _weights("weight", weight, (self.width,), self.dtype), _weights("saved", saved, (n, 2), torch.float32),
             *_matrix("dx", dx, n, self.width, self.dtype), _weights("dweight", dweight, (self.width,), self.dtype),
             _weights("dbias", dbias, (self.width,), self.dtype), self.workspace.data_ptr(), self.workspace.numel(), _stream_handle(stream)))
+
+
+class ClassLoss:
+    """bgl_class_loss_forward / bgl_class_loss_backward: losses over the class scores x weight' + bias, which are not kept, for batches of up to max_rows
+    rows; owns the calls' workspaces (the backward call's is allocated with the first one), so calls on one object must follow one another in
+    stream order.
+
+    labels: (n,) int32, outside [0, classes) for rows without one.  teacher: (classes (n, top) int32, scores (n, top) float32), entries outside
+    [0, classes) not there; its distribution and the scores' are taken at `temperature`.  Like Linear, an object is kept until its calls on
+    other streams than the one it was made on have ended."""
+
+    def __init__(self, max_rows: int, in_dim: int, classes: int, dtype=torch.float32, top: int = 0, temperature: float = 1.0):
+        _require_gpu()
+        if dtype not in DTYPES:
+            raise ValueError(f"unknown dtype: {dtype}")
+        self.max_rows, self.in_dim, self.classes, self.dtype = int(max_rows), int(in_dim), int(classes), dtype
+        self.top, self.temperature = int(top), float(temperature)
+        self.struct = ClassLossStruct(DTYPES[dtype], self.in_dim, self.classes, self.top, self.temperature)
+        self._ref = C.byref(self.struct)
+        forward, backward = C.c_size_t(0), C.c_size_t(0)
+        _check(lib().bgl_class_loss_workspace_bytes(self._ref, self.max_rows, C.byref(forward), C.byref(backward)))
+        self.workspace, self.backward_workspace, self._backward_bytes = _workspace(int(forward.value)), None, int(backward.value)
+        self._made = torch.cuda.current_stream()
+
+    @property
+    def saved_width(self) -> int:
+        """Floats for each row that the backward call needs of the forward one."""
+        return 2 + self.top
+
+    def _inputs(self, x, weight, bias, labels, teacher):
+        n = int(x.shape[0])
+        if n > self.max_rows:
+            raise ValueError(f"{n} rows, the loss was made for {self.max_rows}")
+        classes, scores = (None, None) if teacher is None else teacher
+        return n, (*_matrix("x", x, n, self.in_dim, self.dtype), _weights("weight", weight, (self.classes, self.in_dim), self.dtype),
+                   _weights("bias", bias, (self.classes,), self.dtype), _weights("labels", labels, (n,), torch.int32),
+                   _weights("teacher's classes", classes, (n, self.top), torch.int32), _weights("teacher's scores", scores, (n, self.top), torch.float32))
+
+    def forward(self, x, weight, bias=None, labels=None, teacher=None, loss=None, teacher_loss=None, saved=None, stream=None) -> None:
+        """Writes what is given of loss and teacher_loss, (n,) floats each, and saved = (n, saved_width) floats (the backward call needs them).
+        Tensors that require gradients are refused as by Linear.forward."""
+        _refuse_gradients("the loss", x, weight, bias, None if teacher is None else teacher[1])
+        n, inputs = self._inputs(x, weight, bias, labels, teacher)
+        if self._made is not None:
+            _first_call(self, stream)
+        _check(lib().bgl_class_loss_forward(
+            self._ref, n, *inputs, _weights("loss", loss, (n,), torch.float32), _weights("teacher_loss", teacher_loss, (n,), torch.float32),
+            _weights("saved", saved, (n, self.saved_width), torch.float32), self.workspace.data_ptr(), self.workspace.numel(), _stream_handle(stream)))
+
+    def backward(self, x, weight, saved, bias=None, labels=None, teacher=None, scale: float = 1.0, teacher_scale: float = 1.0,
+                 dx=None, dweight=None, dbias=None, stream=None) -> None:
+        """Writes the gradients of scale * loss.sum() + teacher_scale * teacher_loss.sum() that are given memory: dx, dweight, dbias (with dweight)."""
+        n, inputs = self._inputs(x, weight, bias, labels, teacher)
+        if self.backward_workspace is None:
+            self.backward_workspace = _workspace(self._backward_bytes)
+            if stream is not None:      # (the memory may have been another tensor's on the current stream)
+                stream.wait_stream(torch.cuda.current_stream())
+        _check(lib().bgl_class_loss_backward(
+            self._ref, n, *inputs, _weights("saved", saved, (n, self.saved_width), torch.float32), float(scale), float(teacher_scale),
+            *_matrix("dx", dx, n, self.in_dim, self.dtype), _weights("dweight", dweight, (self.classes, self.in_dim), self.dtype),
+            _weights("dbias", dbias, (self.classes,), self.dtype), self.backward_workspace.data_ptr(), self.backward_workspace.numel(),
+            _stream_handle(stream)))

@@ -11,7 +11,7 @@ CSRC = os.path.join(_HERE, "csrc")
 INCLUDE = os.path.join(_ROOT, "include")
 LIB = os.path.join(_HERE, "libbgl.so")
 HIP_SOURCES = ["bgl_api.hip", "bgl_sample.hip", "bgl_cache.hip", "bgl_host_tier.hip", "bgl_order.hip", "bgl_pipeline.hip",
-               "bgl_linear.hip", "bgl_orthogonal.hip", "bgl_norm.hip"]
+               "bgl_linear.hip", "bgl_orthogonal.hip", "bgl_norm.hip", "bgl_classes.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",

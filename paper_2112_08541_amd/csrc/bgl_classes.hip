@@ -1,0 +1,794 @@
+// Losses over class scores z = x W' + b that are not kept, and their gradients.
+//
+//   labels     loss = lse(z) - z_label                               dz = s (exp(z - lse(z)) - onehot)
+//   teacher    t^2 sum p (log p - log q), p = softmax(score / t)     dz = s' t (q - p), q = softmax(z / t) = exp(z / t - lse(z / t))
+//
+//   k_class_scores   z tile by tile; forward: every tile's largest value and sums of exp, per row; backward: dz of a piece (rows x classes)
+//   k_class_top      forward: the scores of the teacher's classes; k_class_finish: the losses from all of that
+//   k_class_fix      backward: dz of the teacher's classes, over what k_class_scores left there
+//   k_class_product  dx = dz W and dW = dz' x of a piece, db = the sum of dz's rows; k_class_reduce: where several pieces or ranges share a result
+#include "bgl_internal.h"
+#include "bgl_reduce.h"
+#include "bgl_tile.h"
+
+#include <cmath>
+#include <type_traits>
+
+namespace bgl {
+namespace {
+
+using namespace tile;
+
+constexpr float kLog2e = 1.44269504088896341f;
+constexpr int64_t kPieceValues = (int64_t)1 << 25;     // of dz that exist at a time
+constexpr int64_t kPieceRows = 16384;
+constexpr int64_t kPartialBytes = (int64_t)64 << 20;   // of a forward call's tiles' maxima and sums
+
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+// exp(v - most), where most = -inf says that there is nothing
+__device__ __forceinline__ float exp_below(float v, float most) { return exp_of(v - (most == -INFINITY ? 0.0f : most)); }
+
+// The other lanes with the same lane % 16.
+template <class F>
+__device__ __forceinline__ float down_column(float v, F both)
+{
+    const auto s = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+    const uint32_t a = s[0], b = s[1];
+    v = both(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+    const auto t = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+    const uint32_t c = t[0], d = t[1];
+    return both(__builtin_bit_cast(float, c), __builtin_bit_cast(float, d));
+}
+
+template <class T>
+struct ScoreArgs {
+    const typename T::elem *x, *w, *bias;
+    const int32_t *labels;
+    int64_t x_stride, n;      // rows of the call
+    int64_t row0, rows;       // those of this launch
+    int64_t row_tiles;
+    int class0, classes;      // this launch's classes: from class0 up to `classes`
+    int all_classes;
+    bool by_rows;             // tiles of one block of rows, not of classes, follow one another on an XCD
+    int class_tiles, D;
+    float over_t;             // 1 / temperature
+    // forward: {largest, sum, sum at the temperature} of class tile t and row r at part[(t * rows + r) * 3]
+    float *part, *label_score;
+    bool two;                 // the temperature is not 1 and there is a teacher: two sums
+    // backward
+    const float *saved;       // n x width {lse, lse at the temperature or +inf, the teacher's classes' scores}
+    int saved_width;
+    float scale, teacher_scale;
+    typename T::elem *dz;     // rows x dz_stride
+    int dz_stride;
+};
+
+// One tile of classes x rows: a lane holds, of one row, 4 neighbouring classes of every 16.
+template <class T, class C, bool DZ>
+__global__ void __launch_bounds__(kThreads, 2) k_class_scores(ScoreArgs<T> a)
+{
+    using A = KcOperand<T, C::BA>;
+    using B = KcOperand<T, C::BB>;
+    __shared__ __attribute__((aligned(16))) uint32_t lds[A::LDS + B::LDS];
+    __shared__ float meet[DZ ? 1 : 3 * C::BA / 16 / C::FA * C::BB];
+    int64_t ct, rt;
+    int fast;
+    if (!tile_of(blockIdx.x, a.by_rows ? a.row_tiles : a.class_tiles, (int)(a.by_rows ? a.class_tiles : a.row_tiles), a.by_rows ? rt : ct, fast)) return;
+    (a.by_rows ? ct : rt) = fast;
+    const int c0 = a.class0 + (int)ct * C::BA, last = a.classes - 1;
+    const int64_t r0 = rt * C::BB;  // of this launch's rows
+    f32x4 acc[C::FA][C::FB] = {};
+    A weight;
+    B rows;
+    weight.init([&](int i) { return a.w + (int64_t)(c0 + i < last ? c0 + i : last) * a.D; });
+    rows.init([&](int i) { return a.x + (a.row0 + (r0 + i < a.rows ? r0 + i : a.rows - 1)) * a.x_stride; });
+    pipeline(
+        (a.D + A::BK - 1) / A::BK,
+        [&](int i) {
+            weight.load(i, a.D);
+            rows.load(i, a.D);
+        },
+        [&](int) {
+            weight.store(lds);
+            rows.store(lds + A::LDS);
+        },
+        [&](int i) {
+            const int steps = (a.D - i * A::BK + 16 * T::PER - 1) / (16 * T::PER);
+            multiply<T, A, B, C>(lds, lds + A::LDS, steps, acc, [](const auto &, const auto &) {});
+        });
+    const int l = threadIdx.x & 63, first = c0 + C::a_off() + 4 * (l >> 4);
+#pragma unroll
+    for (int i = 0; i < C::FA; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int c = first + 16 * i + j;
+            const float b = a.bias ? T::get(a.bias[c < last ? c : last]) : 0.0f;
+#pragma unroll
+            for (int t = 0; t < C::FB; ++t) acc[i][t][j] = c <= last ? acc[i][t][j] + b : -INFINITY;
+        }
+#pragma unroll
+    for (int t = 0; t < C::FB; ++t) {
+        const int in_tile = C::b_off() + 16 * t + (l & 15);
+        const int64_t r = r0 + in_tile;
+        const bool live = r < a.rows;
+        const int64_t row = a.row0 + (live ? r : a.rows - 1);
+        int label = a.labels ? a.labels[row] : -1;
+        if ((uint32_t)label >= (uint32_t)a.all_classes) label = -1;
+        if constexpr (!DZ) {
+            float most = -INFINITY, sum = 0.0f, sum_t = 0.0f;
+#pragma unroll
+            for (int i = 0; i < C::FA; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) most = fmaxf(most, acc[i][t][j]);
+            most = down_column(most, [](float p, float q) { return fmaxf(p, q); });
+#pragma unroll
+            for (int i = 0; i < C::FA; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float v = acc[i][t][j];
+                    if (first + 16 * i + j == label && live) a.label_score[row] = v;
+                    sum += exp_below(v, most);
+                    if (a.two) sum_t += exp_below(v * a.over_t, most * a.over_t);
+                }
+            sum = down_column(sum, [](float p, float q) { return p + q; });
+            if (a.two) sum_t = down_column(sum_t, [](float p, float q) { return p + q; });
+            float *to = meet + (C::a_off() / C::FA / 16 * C::BB + in_tile) * 3;
+            if (l < 16) to[0] = most, to[1] = sum, to[2] = sum_t;
+        } else {
+            const float *kept = a.saved + row * a.saved_width;
+            const float lse = kept[0], lse_t = kept[1];
+            const float s = label >= 0 ? a.scale : 0.0f, st = lse_t < INFINITY || lse_t != lse_t ? a.teacher_scale : 0.0f;
+#pragma unroll
+            for (int i = 0; i < C::FA; ++i) {
+                typename T::elem e[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float v = acc[i][t][j];
+                    float d = 0.0f;
+                    if (s != 0.0f) d = s * (exp_of(v - lse) - (first + 16 * i + j == label ? 1.0f : 0.0f));
+                    if (st != 0.0f) d = fmaf(st, exp_of(fmaf(v, a.over_t, -lse_t)), d);
+                    e[j] = T::put(d);
+                }
+                const int c = first + 16 * i;
+                typename T::elem *to = a.dz + r * a.dz_stride + (c - a.class0);
+                if (live && c - a.class0 < a.dz_stride) __builtin_memcpy(to, e, sizeof(e));  // (dz_stride is a multiple of 4; what is behind the classes is not read)
+            }
+        }
+    }
+    if constexpr (!DZ) {
+        constexpr int WA = C::BA / 16 / C::FA;
+        __syncthreads();
+        for (int in_tile = threadIdx.x; in_tile < C::BB; in_tile += kThreads) {
+            if (r0 + in_tile >= a.rows) break;
+            float most = -INFINITY, sum = 0.0f, sum_t = 0.0f;
+#pragma unroll
+            for (int w = 0; w < WA; ++w) most = fmaxf(most, meet[(w * C::BB + in_tile) * 3]);
+#pragma unroll
+            for (int w = 0; w < WA; ++w) {
+                const float *from = meet + (w * C::BB + in_tile) * 3;
+                sum += from[1] * exp_below(from[0], most);
+                if (a.two) sum_t += from[2] * exp_below(from[0] * a.over_t, most * a.over_t);
+            }
+            float *to = a.part + (ct * a.rows + r0 + in_tile) * 3;
+            to[0] = most, to[1] = sum, to[2] = sum_t;
+        }
+    }
+}
+
+template <class T>
+struct RowArgs {
+    const typename T::elem *x, *w, *bias;
+    const int32_t *labels, *top_class;
+    const float *top_score;
+    int64_t x_stride, n, row0, rows;
+    int D, classes, top, class_tiles, saved_width;
+    float t, over_t, scale, teacher_scale;
+    const float *part, *label_score;
+    float *loss, *teacher_loss;
+    float *saved;  // forward: null, or where lse, lse_t and the scores go; backward: those
+    float *z_top;  // forward: the scores of the teacher's classes, z_stride apart for each row
+    int z_stride;
+    bool two;
+    // backward: the piece of dz
+    typename T::elem *dz;
+    int class0, piece_classes, dz_stride;
+    int32_t *listed;  // the row's number, or -1 without a gradient
+};
+
+// The scores of a row's classes: a wavefront for each of four classes at a time.
+template <class T>
+__global__ void __launch_bounds__(256) k_class_top(RowArgs<T> a)
+{
+    const int64_t task = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+    const int l = threadIdx.x & 63, each = (a.top + 3) / 4;
+    const int64_t r = task / each;
+    if (r >= a.rows) return;
+    const int64_t row = a.row0 + r;
+    const int k0 = (int)(task % each) * 4;
+    const typename T::elem *x = a.x + row * a.x_stride, *w[4];
+    int c[4];
+    float z[4] = {};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        c[k] = k0 + k < a.top ? a.top_class[row * a.top + k0 + k] : -1;
+        if ((uint32_t)c[k] >= (uint32_t)a.classes) c[k] = -1;
+        w[k] = a.w + (int64_t)(c[k] < 0 ? 0 : c[k]) * a.D;
+    }
+    for (int d = l * T::VEC; d < a.D; d += 64 * T::VEC) {
+        const int left = a.D - d;
+        const auto unpack = [](const uint4 &v, float (&f)[T::VEC]) {
+            const uint32_t q[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (T::PER == 1) f[i] = __uint_as_float(q[i]);
+                else f[2 * i] = __uint_as_float(q[i] << 16), f[2 * i + 1] = __uint_as_float(q[i] & 0xffff0000u);
+            }
+        };
+        float xv[T::VEC], wv[T::VEC];
+        const bool whole = left >= T::VEC;
+        unpack(whole ? load_any<uint4>(x + d) : load_end<T>(x + d, left, a.D), xv);
+        uint4 raw[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) raw[k] = whole ? load_any<uint4>(w[k] + d) : load_end<T>(w[k] + d, left, a.D);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            unpack(raw[k], wv);
+#pragma unroll
+            for (int i = 0; i < T::VEC; ++i) z[k] = fmaf(xv[i], wv[i], z[k]);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        z[k] = sum_across<64>(z[k]);
+        if (l == 0 && k0 + k < a.top) a.z_top[row * a.z_stride + k0 + k] = z[k] + (a.bias && c[k] >= 0 ? T::get(a.bias[c[k]]) : 0.0f);
+    }
+}
+
+// The teacher's distribution of a row, for a wavefront: largest score / t and sum of exp; false where it names no class.
+template <class T>
+__device__ __forceinline__ bool teacher_of(const RowArgs<T> &a, int64_t row, float &most, float &total)
+{
+    const int l = threadIdx.x & 63;
+    most = -INFINITY, total = 0.0f;
+    float bad = 0.0f;
+    for (int k = l; k < a.top; k += 64)
+        if ((uint32_t)a.top_class[row * a.top + k] < (uint32_t)a.classes) {
+            const float v = a.top_score[row * a.top + k] * a.over_t;
+            most = fmaxf(most, v);
+            if (v != v) bad = v;
+        }
+    most = max_across<64>(most);
+    bad = sum_across<64>(bad);
+    if (bad != bad) most = bad;
+    if (most == -INFINITY) return false;
+    for (int k = l; k < a.top; k += 64)
+        if ((uint32_t)a.top_class[row * a.top + k] < (uint32_t)a.classes) total += exp_of(a.top_score[row * a.top + k] * a.over_t - most);
+    total = sum_across<64>(total);
+    return true;
+}
+
+// A wavefront for each row.
+template <class T>
+__global__ void __launch_bounds__(256) k_class_finish(RowArgs<T> a)
+{
+    const int64_t r = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+    if (r >= a.rows) return;
+    const int64_t row = a.row0 + r;
+    const int l = threadIdx.x & 63;
+    float most = -INFINITY, sum = 0.0f, sum_t = 0.0f;
+    for (int ct = l; ct < a.class_tiles; ct += 64) {
+        const float *from = a.part + (ct * a.rows + r) * 3;
+        const float m = fmaxf(most, from[0]);
+        sum = sum * exp_below(most, m) + from[1] * exp_below(from[0], m);
+        if (a.two) sum_t = sum_t * exp_below(most * a.over_t, m * a.over_t) + from[2] * exp_below(from[0] * a.over_t, m * a.over_t);
+        most = m;
+    }
+    const float m = max_across<64>(most);
+    sum = sum_across<64>(sum * exp_below(most, m));
+    sum_t = a.two ? sum_across<64>(sum_t * exp_below(most * a.over_t, m * a.over_t)) : sum;
+    const float lse = m + logf(sum), over = a.two ? a.over_t : 1.0f;
+    if (a.labels) {
+        const int label = a.labels[row];
+        const bool has = (uint32_t)label < (uint32_t)a.classes;
+        if (l == 0 && a.loss) a.loss[row] = has ? (m - a.label_score[row]) + logf(sum) : 0.0f;
+    }
+    float lse_t = INFINITY;
+    if (a.top_class) {
+        float top_most, total, kl = 0.0f;
+        const bool taught = teacher_of(a, row, top_most, total);
+        if (taught) {
+            lse_t = m * over + logf(sum_t);
+            const float log_total = logf(total);
+            for (int k = l; k < a.top; k += 64)
+                if ((uint32_t)a.top_class[row * a.top + k] < (uint32_t)a.classes) {
+                    const float v = a.top_score[row * a.top + k] * a.over_t - top_most;
+                    const float p = exp_of(v) / total;
+                    // (the scores are next to each other: what they have in common goes first)
+                    if (p != 0.0f) kl = fmaf(p, (v - log_total) + ((m - a.z_top[row * a.z_stride + k]) * a.over_t + logf(sum_t)), kl);
+                }
+            kl = sum_across<64>(kl);
+        }
+        if (l == 0 && a.teacher_loss) a.teacher_loss[row] = taught ? a.t * a.t * kl : 0.0f;
+    }
+    if (l == 0 && a.saved) a.saved[row * a.saved_width] = lse, a.saved[row * a.saved_width + 1] = lse_t;
+}
+
+// Which rows have a gradient, for the products that sum over rows: what others hold there is not read.
+template <class T>
+__global__ void __launch_bounds__(256) k_class_rows(RowArgs<T> a)
+{
+    const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (r >= a.rows) return;
+    const int64_t row = a.row0 + r;
+    const bool labelled = a.labels && (uint32_t)a.labels[row] < (uint32_t)a.classes && a.scale != 0.0f;
+    const float lse_t = a.saved[row * a.saved_width + 1];
+    const bool taught = a.top_class && lse_t != INFINITY && a.teacher_scale != 0.0f;
+    a.listed[r] = labelled || taught ? (int32_t)r : -1;
+}
+
+// dz where the teacher names a class: a wavefront for each row.  A class named twice has the sum of its shares, written by both.
+template <class T>
+__global__ void __launch_bounds__(256) k_class_fix(RowArgs<T> a)
+{
+    const int64_t r = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+    if (r >= a.rows) return;
+    const int64_t row = a.row0 + r;
+    const int l = threadIdx.x & 63;
+    float most, total;
+    if (!teacher_of(a, row, most, total)) return;
+    const float *kept = a.saved + row * a.saved_width;
+    const float lse = kept[0], lse_t = kept[1];
+    int label = a.labels ? a.labels[row] : -1;
+    if ((uint32_t)label >= (uint32_t)a.classes) label = -1;
+    for (int k = l; k < a.top; k += 64) {
+        const int c = a.top_class[row * a.top + k];
+        if (c < a.class0 || c >= a.class0 + a.piece_classes) continue;
+        float p = 0.0f;
+        for (int o = 0; o < a.top; ++o)
+            if (a.top_class[row * a.top + o] == c) p += exp_of(a.top_score[row * a.top + o] * a.over_t - most) / total;
+        const float z = kept[2 + k];
+        float d = 0.0f;
+        if (label >= 0 && a.scale != 0.0f) d = a.scale * (exp_of(z - lse) - (c == label ? 1.0f : 0.0f));
+        if (a.teacher_scale != 0.0f) d = fmaf(a.teacher_scale, exp_of(fmaf(z, a.over_t, -lse_t)) - p, d);
+        a.dz[r * a.dz_stride + (c - a.class0)] = T::put(d);
+    }
+}
+
+// ----------------------------------------------------------------- products of a piece
+template <class T>
+struct PieceArgs {
+    const typename T::elem *a, *b;  // dz; W or x
+    int64_t a_stride, b_stride;
+    const int32_t *list;            // of the summed rows (dW): the row itself, or -1 for none
+    int64_t M, K;                   // kept and summed index
+    int N, a_width;                 // columns of the result; of dz that can be read
+    int64_t row_tiles;
+    int col_tiles, shares;
+    int64_t per_share;              // of the summed index
+    typename T::elem *out, *sums;   // the result, if it is whole; M values of sums over the summed index
+    int64_t out_stride;
+    float *slots, *sum_slots;       // else shares x slot_rows x N, shares x slot_rows
+    int64_t slot_rows;
+    bool add;                       // to what is in the slots
+};
+
+// M x N = A B over the summed index, B's rows being that index.  OC: A's rows too (dW: they are batch rows), else A's rows are the result's (dx).
+template <class T, class C, bool OC, bool NARROW>
+__global__ void __launch_bounds__(kThreads, 2) k_class_product(PieceArgs<T> a)
+{
+    using A = std::conditional_t<OC, OcOperand<T, C::BA, false, false>, KcOperand<T, C::BA>>;
+    using B = OcOperand<T, C::BB, OC, NARROW>;
+    __shared__ __attribute__((aligned(16))) uint32_t lds[A::LDS + B::LDS];
+    const int share = blockIdx.y;
+    int64_t rt;
+    int ct;
+    if (!tile_of(blockIdx.x, a.row_tiles, a.col_tiles, rt, ct)) return;
+    const int64_t m0 = rt * C::BA, k0 = share * a.per_share;
+    const int n0 = ct * C::BB, K = (int)(a.K - k0 < a.per_share ? a.K - k0 : a.per_share);
+    f32x4 acc[C::FA][C::FB] = {};
+    float sums[C::FA] = {};
+    const bool summing = OC && (a.sums || a.sum_slots) && n0 == 0 && C::b_off() == 0;
+    if (K > 0) {
+        A left;
+        B right;
+        if constexpr (OC) {
+            left.init(a.a, a.a_stride, a.K, (int)m0, a.a_width);
+            left.range(nullptr, k0, K);
+        } else {
+            left.init([&](int i) { return a.a + (m0 + i < a.M ? m0 + i : a.M - 1) * a.a_stride + k0; });
+        }
+        right.init(a.b, a.b_stride, a.K, n0, a.N);
+        right.range(a.list, k0, K);
+        pipeline(
+            (K + A::BK - 1) / A::BK,
+            [&](int i) {
+                if constexpr (OC) left.load(i);
+                else left.load(i, K);
+                right.load(i);
+            },
+            [&](int) {
+                if constexpr (OC) left.settle();
+                left.store(lds);
+                right.settle();
+                right.store(lds + A::LDS);
+            },
+            [&](int i) {
+                const int steps = (K - i * A::BK + 16 * T::PER - 1) / (16 * T::PER);
+                multiply<T, A, B, C>(lds, lds + A::LDS, steps, acc, [&](const auto &f, const auto &) {
+                    if (summing) {
+#pragma unroll
+                        for (int t = 0; t < C::FA; ++t) sums[t] = T::sum(f[t], sums[t]);
+                    }
+                });
+            });
+    }
+    const int l = threadIdx.x & 63;
+    float *slot = a.slots ? a.slots + share * a.slot_rows * a.N : nullptr;
+#pragma unroll
+    for (int i = 0; i < C::FA; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t m = m0 + C::a_off() + 16 * i + 4 * (l >> 4) + j;
+            if (m >= a.M) continue;
+#pragma unroll
+            for (int t = 0; t < C::FB; ++t) {
+                const int c = n0 + C::b_off() + 16 * t + (l & 15);
+                if (c >= a.N) continue;
+                float v = acc[i][t][j];
+                if (slot) {
+                    float *to = slot + m * a.N + c;
+                    *to = a.add ? *to + v : v;
+                } else {
+                    a.out[m * a.out_stride + c] = T::put(v);
+                }
+            }
+        }
+    if (summing) {
+#pragma unroll
+        for (int t = 0; t < C::FA; ++t) {
+            const float v = down_column(sums[t], [](float p, float q) { return p + q; });
+            const int64_t m = m0 + C::a_off() + 16 * t + (l & 15);
+            if (l >= 16 || m >= a.M) continue;
+            if (a.sum_slots) {
+                float *to = a.sum_slots + share * a.slot_rows + m;
+                *to = a.add ? *to + v : v;
+            } else {
+                a.sums[m] = T::put(v);
+            }
+        }
+    }
+}
+
+template <class T>
+struct ReduceArgs {
+    const float *slots;
+    int64_t slot_values, count;  // values between slots; of the result, in rows of `width`
+    int width, shares;
+    typename T::elem *out;
+    int64_t out_stride;
+};
+template <class T>
+__global__ void __launch_bounds__(256) k_class_reduce(ReduceArgs<T> a)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= a.count) return;
+    float s = 0.0f;
+    for (int p = 0; p < a.shares; ++p) s += a.slots[p * a.slot_values + i];
+    a.out[i / a.width * a.out_stride + i % a.width] = T::put(s);
+}
+template <class T>
+__global__ void __launch_bounds__(256) k_class_zero(typename T::elem *p, int64_t count)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < count) p[i] = T::put(0.0f);
+}
+
+// ----------------------------------------------------------------- plans
+using Large = Cut<2, 2, 4, 4>;   // 128 x 128
+using Middle = Cut<2, 2, 4, 2>;  // 128 x 64
+using Low = Cut<4, 1, 2, 1>;     // 128 x 16
+
+struct Plan {
+    // forward
+    int64_t pass_rows;
+    int class_tiles;
+    size_t part_bytes, label_bytes, top_bytes, forward_bytes;
+    // backward
+    int64_t piece_rows, row_pieces, dz_stride;
+    int piece_classes, class_pieces, dx_shares, dw_shares;
+    int64_t dx_per, dw_per;
+    size_t dz_bytes, list_bytes, dx_bytes, dw_bytes, db_bytes, backward_bytes;
+};
+
+int64_t dz_stride_of(int64_t classes) { return (classes + 7) / 8 * 8; }  // (pieces of 4 are stored, and 16 bytes of bf16 read)
+
+constexpr int64_t kSharesFill = 512;  // workgroups that ranges of the summed index are to make together
+constexpr int64_t kShareLeast = 512;  // of the summed index
+
+int shares_for(int64_t tiles, int64_t summed)
+{
+    const int64_t want = kSharesFill / (tiles < 1 ? 1 : tiles), most = summed / kShareLeast;
+    return (int)(want < 1 || most < 1 ? 1 : want < most ? want : most);
+}
+
+Plan plan_of(const bgl_class_loss_t *l, int64_t n)
+{
+    Plan p{};
+    const int es = l->dtype == BGL_F32 ? 4 : 2;
+    p.class_tiles = (int)ceil_div(l->classes, Large::BA);
+    p.pass_rows = kPartialBytes / (12 * (int64_t)p.class_tiles);
+    p.pass_rows = p.pass_rows < 1024 ? 1024 : p.pass_rows / 128 * 128;
+    if (p.pass_rows > n) p.pass_rows = n;
+    p.part_bytes = round_up((size_t)p.pass_rows * p.class_tiles * 12, 256);
+    p.label_bytes = round_up((size_t)n * 4, 256);
+    p.top_bytes = round_up((size_t)n * l->top * 4, 256);
+    p.forward_bytes = p.part_bytes + p.label_bytes + p.top_bytes;
+
+    // one piece if it is small enough; else all classes of some rows (dx is then written once and dW added up), and with very many classes some
+    // classes of all rows, or of kPieceRows (dW is then written once for each of these, and dx added up); about equal ones
+    const int64_t stride = dz_stride_of(l->classes);
+    p.piece_rows = n, p.piece_classes = l->classes;
+    if (n * stride > kPieceValues) {
+        if (l->classes <= kPieceRows) {
+            p.piece_rows = (int64_t)round_up((size_t)ceil_div(n, ceil_div(n * stride, kPieceValues)), 128);
+            if (p.piece_rows > n) p.piece_rows = n;
+        } else {
+            if (n > kPieceRows) p.piece_rows = kPieceRows;
+            const int64_t fit = (int64_t)round_up((size_t)ceil_div(stride, ceil_div(p.piece_rows * stride, kPieceValues)), 256);
+            if (fit < l->classes) p.piece_classes = (int)fit;
+        }
+    }
+    p.class_pieces = (int)ceil_div(l->classes, p.piece_classes);
+    p.row_pieces = p.piece_rows > 0 ? ceil_div(n, p.piece_rows) : 0;
+    p.dz_stride = dz_stride_of(p.piece_classes);
+    p.dz_bytes = round_up((size_t)p.piece_rows * p.dz_stride * es, 256);
+    p.list_bytes = round_up((size_t)n * 4, 256);
+    const int64_t cols = ceil_div(l->in_dim, 128);
+    p.dx_shares = p.class_pieces > 1 && p.row_pieces > 1 ? 1 : shares_for(ceil_div(p.piece_rows, 128) * cols, p.piece_classes);
+    p.dx_per = round_up((size_t)ceil_div(p.piece_classes, p.dx_shares), 64);
+    p.dw_shares = shares_for(ceil_div(p.piece_classes, 128) * cols, p.piece_rows);
+    p.dw_per = round_up((size_t)ceil_div(p.piece_rows, p.dw_shares), 64);
+    p.dx_bytes = p.dx_shares > 1 || p.class_pieces > 1 ? round_up((size_t)p.dx_shares * (p.class_pieces > 1 ? n : p.piece_rows) * l->in_dim * 4, 256) : 0;
+    p.dw_bytes = p.dw_shares > 1 || p.row_pieces > 1 ? round_up((size_t)p.dw_shares * p.piece_classes * l->in_dim * 4, 256) : 0;
+    p.db_bytes = p.dw_bytes ? round_up((size_t)p.dw_shares * p.piece_classes * 4, 256) : 0;
+    p.backward_bytes = p.dz_bytes + p.list_bytes + p.dx_bytes + p.dw_bytes + p.db_bytes;
+    return p;
+}
+
+// What the backward calls of up to n rows need: no call of fewer rows needs more.  (Shares are less than kSharesFill tiles in all.)
+size_t backward_room(const bgl_class_loss_t *l, int64_t n)
+{
+    const int es = l->dtype == BGL_F32 ? 4 : 2;
+    const int64_t V = l->classes, D = l->in_dim, stride = dz_stride_of(V), shared = kSharesFill * 128;
+    const bool many = V > kPieceRows;
+    const auto least = [](int64_t a, int64_t b) { return a < b ? a : b; };
+    const auto most = [](int64_t a, int64_t b) { return a > b ? a : b; };
+    const int64_t over = many ? 256 * least(n, kPieceRows) : 128 * stride;
+    size_t bytes = round_up((size_t)least(n * stride, kPieceValues + over) * es, 256) + round_up((size_t)n * 4, 256);
+    if (V >= 2 * kShareLeast) bytes += round_up((size_t)most(many ? n : 0, least(shared, n * (V / kShareLeast))) * D * 4, 256);
+    const int64_t shares = n >= 2 * kShareLeast ? least(shared, V * (n / kShareLeast)) : 0;
+    const int64_t pieces = many ? (n > kPieceRows ? kPieceValues / kPieceRows + 256 : 0) : n * stride > kPieceValues ? V : 0;
+    bytes += round_up((size_t)most(shares, pieces) * D * 4, 256) + round_up((size_t)most(shares, pieces) * 4, 256);
+    return bytes;
+}
+
+template <class T, bool DZ>
+void launch_scores(ScoreArgs<T> &s, hipStream_t st)
+{
+    s.class_tiles = (int)ceil_div(s.classes - s.class0, 128);
+    const auto go = [&](auto cut) {
+        using C = decltype(cut);
+        s.row_tiles = ceil_div(s.rows, C::BB);
+        s.by_rows = s.row_tiles > s.class_tiles;
+        const int64_t tiles = s.by_rows ? tile_count(s.row_tiles, s.class_tiles) : tile_count(s.class_tiles, (int)s.row_tiles);
+        k_class_scores<T, C, DZ><<<dim3((unsigned)tiles), dim3(kThreads), 0, st>>>(s);
+    };
+    if (s.rows <= 16) go(Low{});
+    else if (s.rows <= 64) go(Middle{});
+    else go(Large{});
+}
+
+struct Call {
+    const bgl_class_loss_t *l;
+    int64_t n;
+    const void *x;
+    int64_t x_stride;
+    const void *weight, *bias;
+    const int32_t *labels, *top_class;
+    const float *top_score;
+    char *workspace;
+    hipStream_t stream;
+};
+
+template <class T>
+RowArgs<T> row_args(const Call &c)
+{
+    using E = typename T::elem;
+    RowArgs<T> r{};
+    r.x = (const E *)c.x, r.w = (const E *)c.weight, r.bias = (const E *)c.bias, r.labels = c.labels, r.top_class = c.top_class, r.top_score = c.top_score;
+    r.x_stride = c.x_stride, r.n = c.n, r.D = c.l->in_dim, r.classes = c.l->classes, r.top = c.l->top, r.saved_width = 2 + c.l->top;
+    r.t = c.l->temperature, r.over_t = 1.0f / c.l->temperature;
+    r.two = c.top_class && c.l->temperature != 1.0f;
+    return r;
+}
+template <class T>
+ScoreArgs<T> score_args(const Call &c)
+{
+    using E = typename T::elem;
+    ScoreArgs<T> s{};
+    s.x = (const E *)c.x, s.w = (const E *)c.weight, s.bias = (const E *)c.bias, s.labels = c.labels, s.x_stride = c.x_stride, s.n = c.n;
+    s.classes = s.all_classes = c.l->classes, s.D = c.l->in_dim, s.over_t = 1.0f / c.l->temperature, s.two = c.top_class && c.l->temperature != 1.0f;
+    s.saved_width = 2 + c.l->top;
+    return s;
+}
+
+template <class T>
+int forward(const Call &c, float *loss, float *teacher_loss, float *saved)
+{
+    const Plan p = plan_of(c.l, c.n);
+    ScoreArgs<T> s = score_args<T>(c);
+    RowArgs<T> r = row_args<T>(c);
+    s.part = (float *)c.workspace, s.label_score = (float *)(c.workspace + p.part_bytes);
+    r.part = s.part, r.label_score = s.label_score, r.class_tiles = p.class_tiles;
+    r.z_top = saved ? saved + 2 : (float *)(c.workspace + p.part_bytes + p.label_bytes), r.z_stride = saved ? r.saved_width : r.top;
+    r.loss = loss, r.teacher_loss = teacher_loss, r.saved = saved;
+    for (int64_t row0 = 0; row0 < c.n; row0 += p.pass_rows) {
+        s.row0 = r.row0 = row0, s.rows = r.rows = c.n - row0 < p.pass_rows ? c.n - row0 : p.pass_rows;
+        launch_scores<T, false>(s, c.stream);
+        if (c.top_class) k_class_top<T><<<dim3((unsigned)ceil_div(r.rows * ((r.top + 3) / 4), 4)), dim3(256), 0, c.stream>>>(r);
+        k_class_finish<T><<<dim3((unsigned)ceil_div(r.rows, 4)), dim3(256), 0, c.stream>>>(r);
+    }
+    BGL_HIP(hipGetLastError());
+    return BGL_OK;
+}
+
+template <class T, bool OC>
+void launch_product(PieceArgs<T> &a, hipStream_t st)
+{
+    a.row_tiles = ceil_div(a.M, 128), a.col_tiles = (int)ceil_div(a.N, 128);
+    const dim3 grid((unsigned)tile_count(a.row_tiles, a.col_tiles), (unsigned)a.shares);
+    if (a.N >= T::VEC) k_class_product<T, Large, OC, false><<<grid, dim3(kThreads), 0, st>>>(a);
+    else k_class_product<T, Large, OC, true><<<grid, dim3(kThreads), 0, st>>>(a);
+}
+template <class T>
+void launch_reduce(const float *slots, int64_t slot_values, int64_t rows, int width, int shares, typename T::elem *out, int64_t stride, hipStream_t st)
+{
+    ReduceArgs<T> a{slots, slot_values, rows * width, width, shares, out, stride};
+    k_class_reduce<T><<<dim3((unsigned)ceil_div(a.count, 256)), dim3(256), 0, st>>>(a);
+}
+
+template <class T>
+int backward(const Call &c, const float *saved, float scale, float teacher_scale, void *dx_, int64_t dx_stride, void *dweight_, void *dbias_)
+{
+    using E = typename T::elem;
+    E *dx = (E *)dx_, *dweight = (E *)dweight_, *dbias = (E *)dbias_;
+    const int D = c.l->in_dim, V = c.l->classes;
+    if (c.n == 0) {
+        if (dweight) k_class_zero<T><<<dim3((unsigned)ceil_div((int64_t)V * D, 256)), dim3(256), 0, c.stream>>>(dweight, (int64_t)V * D);
+        if (dbias) k_class_zero<T><<<dim3((unsigned)ceil_div(V, 256)), dim3(256), 0, c.stream>>>(dbias, V);
+        BGL_HIP(hipGetLastError());
+        return BGL_OK;
+    }
+    const Plan p = plan_of(c.l, c.n);
+    char *ws = c.workspace;
+    E *dz = (E *)ws;
+    int32_t *listed = (int32_t *)(ws += p.dz_bytes);
+    float *dx_slots = (float *)(ws += p.list_bytes), *dw_slots = (float *)(ws += p.dx_bytes), *db_slots = (float *)(ws += p.dw_bytes);
+    ScoreArgs<T> s = score_args<T>(c);
+    RowArgs<T> r = row_args<T>(c);
+    s.saved = saved, s.dz = dz, s.dz_stride = (int)p.dz_stride;
+    s.scale = r.scale = c.labels ? scale : 0.0f;
+    s.teacher_scale = r.teacher_scale = c.top_class ? teacher_scale * c.l->temperature : 0.0f;
+    r.saved = const_cast<float *>(saved), r.dz = dz, r.dz_stride = (int)p.dz_stride;
+    for (int cp = 0; cp < p.class_pieces; ++cp) {
+        const int class0 = cp * p.piece_classes, classes = V - class0 < p.piece_classes ? V - class0 : p.piece_classes;
+        for (int64_t rp = 0; rp < p.row_pieces; ++rp) {
+            const int64_t row0 = rp * p.piece_rows, rows = c.n - row0 < p.piece_rows ? c.n - row0 : p.piece_rows;
+            s.row0 = r.row0 = row0, s.rows = r.rows = rows, s.class0 = r.class0 = class0, r.piece_classes = classes, s.classes = class0 + classes;
+            r.listed = listed + row0;
+            if (cp == 0 && (dweight || dbias)) k_class_rows<T><<<dim3((unsigned)ceil_div(rows, 256)), dim3(256), 0, c.stream>>>(r);
+            launch_scores<T, true>(s, c.stream);
+            if (r.teacher_scale != 0.0f) k_class_fix<T><<<dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, c.stream>>>(r);
+            if (dx) {
+                PieceArgs<T> a{};
+                a.a = dz, a.a_stride = p.dz_stride, a.b = s.w + (int64_t)class0 * D, a.b_stride = D, a.M = rows, a.K = classes, a.N = D, a.a_width = (int)p.dz_stride;
+                a.shares = p.dx_shares, a.per_share = p.dx_per, a.out = dx + row0 * dx_stride, a.out_stride = dx_stride;
+                if (p.dx_bytes) a.slots = dx_slots + (p.class_pieces > 1 ? row0 * D : 0), a.slot_rows = p.class_pieces > 1 ? c.n : rows, a.add = cp > 0;
+                launch_product<T, false>(a, c.stream);
+                if (p.dx_bytes && p.class_pieces == 1) launch_reduce<T>(dx_slots, rows * D, rows, D, p.dx_shares, dx + row0 * dx_stride, dx_stride, c.stream);
+            }
+            if (dweight || dbias) {
+                PieceArgs<T> a{};
+                a.a = dz, a.a_stride = p.dz_stride, a.b = s.x + row0 * c.x_stride, a.b_stride = c.x_stride, a.list = listed + row0, a.M = classes, a.K = rows;
+                a.N = D, a.a_width = (int)p.dz_stride, a.shares = p.dw_shares, a.per_share = p.dw_per;
+                a.out = dweight + (int64_t)class0 * D, a.out_stride = D, a.sums = dbias ? dbias + class0 : nullptr;
+                if (p.dw_bytes) a.slots = dw_slots, a.sum_slots = dbias ? db_slots : nullptr, a.slot_rows = p.piece_classes, a.add = rp > 0;
+                launch_product<T, true>(a, c.stream);
+            }
+        }
+        if (p.dw_bytes && dweight) launch_reduce<T>(dw_slots, (int64_t)p.piece_classes * D, classes, D, p.dw_shares, dweight + (int64_t)class0 * D, D, c.stream);
+        if (p.dw_bytes && dbias) launch_reduce<T>(db_slots, p.piece_classes, 1, classes, p.dw_shares, dbias + class0, classes, c.stream);
+    }
+    if (p.dx_bytes && dx && p.class_pieces > 1) launch_reduce<T>(dx_slots, c.n * D, c.n, D, p.dx_shares, dx, dx_stride, c.stream);
+    BGL_HIP(hipGetLastError());
+    return BGL_OK;
+}
+
+int check_loss(const bgl_class_loss_t *l, int64_t n)
+{
+    if (!l) BGL_FAIL(BGL_EINVAL, "loss is null");
+    if (l->dtype != BGL_F32 && l->dtype != BGL_BF16) BGL_FAIL(BGL_EINVAL, "unknown dtype %d", l->dtype);
+    if (l->in_dim < 1 || l->classes < 1 || l->top < 0) BGL_FAIL(BGL_EINVAL, "in_dim %d, classes %d, top %d", l->in_dim, l->classes, l->top);
+    if (!(l->temperature >= 0x1p-10f && l->temperature <= 0x1p10f)) BGL_FAIL(BGL_EINVAL, "temperature %g is not in [2^-10, 2^10]", (double)l->temperature);
+    if (l->in_dim > BGL_MAX_DIM) BGL_FAIL(BGL_EUNSUPPORTED, "in_dim %d is more than %d", l->in_dim, BGL_MAX_DIM);
+    if (l->classes > BGL_MAX_CLASSES) BGL_FAIL(BGL_EUNSUPPORTED, "%d classes are more than %d", l->classes, BGL_MAX_CLASSES);
+    if (l->top > BGL_MAX_TOP) BGL_FAIL(BGL_EUNSUPPORTED, "top %d is more than %d", l->top, BGL_MAX_TOP);
+    if (n < 0 || n > INT32_MAX) BGL_FAIL(BGL_EINVAL, "%lld rows", (long long)n);
+    return BGL_OK;
+}
+int check_call(const Call &c)
+{
+    BGL_TRY(check_loss(c.l, c.n));
+    const int es = c.l->dtype == BGL_F32 ? 4 : 2;
+    BGL_TRY(check_rows("x", c.x, c.x_stride, c.l->in_dim, es, c.n > 0));
+    if ((c.n > 0 && !c.weight) || !aligned(c.weight, es) || !aligned(c.bias, es)) BGL_FAIL(BGL_EINVAL, "weight is null, or weight or bias is misaligned");
+    if (!aligned(c.labels, 4) || !aligned(c.top_class, 4) || !aligned(c.top_score, 4)) BGL_FAIL(BGL_EINVAL, "labels or the teacher's classes or scores are misaligned");
+    if (!c.top_class != !c.top_score) BGL_FAIL(BGL_EINVAL, "the teacher's classes and scores come together");
+    if (c.top_class && c.l->top == 0) BGL_FAIL(BGL_EINVAL, "the loss has no teacher (top is 0)");
+    if (c.n > 0 && !c.labels && !c.top_class) BGL_FAIL(BGL_EINVAL, "neither labels nor a teacher");
+    return BGL_OK;
+}
+int check_workspace(const void *workspace, size_t have, size_t need)
+{
+    if (need == 0) return BGL_OK;
+    if (!workspace || !aligned(workspace, 256)) BGL_FAIL(BGL_EINVAL, "workspace is null or not 256-byte aligned");
+    if (have < need) BGL_FAIL(BGL_ECAPACITY, "workspace of %zu bytes, %zu needed", have, need);
+    return BGL_OK;
+}
+
+}  // namespace
+}  // namespace bgl
+
+using namespace bgl;
+
+extern "C" int bgl_class_loss_workspace_bytes(const bgl_class_loss_t *loss, int64_t n, size_t *forward_bytes, size_t *backward_bytes)
+try {
+    if (!forward_bytes && !backward_bytes) BGL_FAIL(BGL_EINVAL, "forward_bytes and backward_bytes are null");
+    BGL_TRY(check_loss(loss, n));
+    const Plan p = plan_of(loss, n);
+    if (forward_bytes) *forward_bytes = p.forward_bytes;
+    const size_t room = backward_room(loss, n);
+    if (backward_bytes) *backward_bytes = room > p.backward_bytes ? room : p.backward_bytes;
+    return BGL_OK;
+} BGL_NOTHROW_END
+
+extern "C" int bgl_class_loss_forward(const bgl_class_loss_t *loss, int64_t n, const void *x, int64_t x_stride, const void *weight, const void *bias,
+                                      const int32_t *labels, const int32_t *teacher_classes, const float *teacher_scores, float *label_loss,
+                                      float *teacher_loss, float *saved, void *workspace, size_t workspace_bytes, void *stream)
+try {
+    const Call c{loss, n, x, x_stride, weight, bias, labels, teacher_classes, teacher_scores, (char *)workspace, (hipStream_t)stream};
+    BGL_TRY(check_call(c));
+    if (!aligned(label_loss, 4) || !aligned(teacher_loss, 4) || !aligned(saved, 4)) BGL_FAIL(BGL_EINVAL, "label_loss, teacher_loss or saved is misaligned");
+    if ((label_loss && n > 0 && !labels) || (teacher_loss && n > 0 && !teacher_classes)) BGL_FAIL(BGL_EINVAL, "a loss without its labels or teacher");
+    BGL_TRY(check_workspace(workspace, workspace_bytes, n > 0 ? plan_of(loss, n).forward_bytes : 0));
+    if (n == 0) return BGL_OK;
+    return loss->dtype == BGL_F32 ? forward<tile::F32>(c, label_loss, teacher_loss, saved) : forward<tile::BF16>(c, label_loss, teacher_loss, saved);
+} BGL_NOTHROW_END
+
+extern "C" int bgl_class_loss_backward(const bgl_class_loss_t *loss, int64_t n, const void *x, int64_t x_stride, const void *weight, const void *bias,
+                                       const int32_t *labels, const int32_t *teacher_classes, const float *teacher_scores, const float *saved, float scale,
+                                       float teacher_scale, void *dx, int64_t dx_stride, void *dweight, void *dbias, void *workspace,
+                                       size_t workspace_bytes, void *stream)
+try {
+    const Call c{loss, n, x, x_stride, weight, bias, labels, teacher_classes, teacher_scores, (char *)workspace, (hipStream_t)stream};
+    BGL_TRY(check_call(c));
+    const int es = loss->dtype == BGL_F32 ? 4 : 2;
+    BGL_TRY(check_rows("dx", dx, dx_stride, loss->in_dim, es, false));
+    if ((n > 0 && !saved) || !aligned(saved, 4)) BGL_FAIL(BGL_EINVAL, "saved is null or misaligned");
+    if (!aligned(dweight, es) || !aligned(dbias, es)) BGL_FAIL(BGL_EINVAL, "dweight or dbias is misaligned");
+    if (dbias && !dweight) BGL_FAIL(BGL_EINVAL, "dbias without dweight");
+    if (!dx && !dweight) BGL_FAIL(BGL_EINVAL, "no gradient is asked for");
+    BGL_TRY(check_workspace(workspace, workspace_bytes, n > 0 ? plan_of(loss, n).backward_bytes : 0));
+    return loss->dtype == BGL_F32 ? backward<tile::F32>(c, saved, scale, teacher_scale, dx, dx_stride, dweight, dbias)
+                                  : backward<tile::BF16>(c, saved, scale, teacher_scale, dx, dx_stride, dweight, dbias);
+} BGL_NOTHROW_END
