@@ -9,6 +9,7 @@
 //   k_class_product  dx = dz W and dW = dz' x of a piece, db = the sum of dz's rows; k_class_reduce: where several pieces or ranges share a result
 #include "bgl_internal.h"
 #include "bgl_reduce.h"
+#include "bgl_stage.h"
 #include "bgl_tile.h"
 
 #include <cmath>
@@ -19,14 +20,21 @@ namespace {
 
 using namespace tile;
 
-constexpr float kLog2e = 1.44269504088896341f;
-constexpr int64_t kPieceValues = (int64_t)1 << 25;     // of dz that exist at a time
+#pragma clang fp contract(off)  // (a base has to be the same number wherever it is used)
+
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 constexpr int64_t kPieceRows = 16384;
 constexpr int64_t kPartialBytes = (int64_t)64 << 20;   // of a forward call's tiles' maxima and sums
+constexpr int64_t kSharesFill = 512;                   // workgroups that ranges of a product's summed index are to make together
+constexpr int64_t kShareLeast = 512;                   // of the summed index, for each of them
+constexpr double kLargeProducts = 5e8;                 // of a call that is laid out for large tiles
 
+// Exponentials are powers of two: exp(k v) / 2^base with k = log2(e) or that over the temperature, as 2^(k v - base) with one rounding.  A sum of them is taken to
+// the base of its largest value, base(most) = k most, rounded: sums of two bases meet exactly, as the bases' difference has no rounding to speak of.
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
-// exp(v - most), where most = -inf says that there is nothing
-__device__ __forceinline__ float exp_below(float v, float most) { return exp_of(v - (most == -INFINITY ? 0.0f : most)); }
+__device__ __forceinline__ float base_of(float most, float k) { return most == -INFINITY ? 0.0f : most * k; }  // (nothing there: the sum is 0)
+__device__ __forceinline__ float power_to(float v, float k, float base) { return __builtin_amdgcn_exp2f(fmaf(v, k, -base)); }
+__device__ __forceinline__ float rebase(float from, float to) { return __builtin_amdgcn_exp2f(from - to); }
 
 // The other lanes with the same lane % 16.
 template <class F>
@@ -40,6 +48,16 @@ __device__ __forceinline__ float down_column(float v, F both)
     return both(__builtin_bit_cast(float, c), __builtin_bit_cast(float, d));
 }
 
+// A fp32 value as three of bf16 (bgl_stage.h).  One that is not finite, or rounds to infinity, is in the first alone.
+__device__ __forceinline__ void split(float v, uint16_t (&e)[3])
+{
+    e[0] = BF16::put(v);
+    if (fabsf(v) < INFINITY && (e[0] & 0x7fff) == 0x7f80) e[0] -= 1;  // (a value that rounds up to infinity: the largest there is)
+    const float rest = fabsf(v) < INFINITY ? v - BF16::get(e[0]) : 0.0f;
+    e[1] = BF16::put(rest);
+    e[2] = BF16::put(rest - BF16::get(e[1]));
+}
+
 template <class T>
 struct ScoreArgs {
     const typename T::elem *x, *w, *bias;
@@ -51,12 +69,12 @@ struct ScoreArgs {
     int all_classes;
     bool by_rows;             // tiles of one block of rows, not of classes, follow one another on an XCD
     int class_tiles, D;
-    float over_t;             // 1 / temperature
+    float k, k_t;             // log2(e), and over the temperature
     // forward: {largest, sum, sum at the temperature} of class tile t and row r at part[(t * rows + r) * 3]
     float *part, *label_score;
     bool two;                 // the temperature is not 1 and there is a teacher: two sums
     // backward
-    const float *saved;       // n x width {lse, lse at the temperature or +inf, the teacher's classes' scores}
+    const float *saved;       // n x width {log2 sum exp, the same at the temperature or +inf, the teacher's classes' scores}
     int saved_width;
     float scale, teacher_scale;
     typename T::elem *dz;     // rows x dz_stride
@@ -121,14 +139,15 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_scores(ScoreArgs<T> a)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) most = fmaxf(most, acc[i][t][j]);
             most = down_column(most, [](float p, float q) { return fmaxf(p, q); });
+            const float base = base_of(most, a.k), base_t = base_of(most, a.k_t);
 #pragma unroll
             for (int i = 0; i < C::FA; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float v = acc[i][t][j];
                     if (first + 16 * i + j == label && live) a.label_score[row] = v;
-                    sum += exp_below(v, most);
-                    if (a.two) sum_t += exp_below(v * a.over_t, most * a.over_t);
+                    sum += power_to(v, a.k, base);
+                    if (a.two) sum_t += power_to(v, a.k_t, base_t);
                 }
             sum = down_column(sum, [](float p, float q) { return p + q; });
             if (a.two) sum_t = down_column(sum_t, [](float p, float q) { return p + q; });
@@ -145,8 +164,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_scores(ScoreArgs<T> a)
                 for (int j = 0; j < 4; ++j) {
                     const float v = acc[i][t][j];
                     float d = 0.0f;
-                    if (s != 0.0f) d = s * (exp_of(v - lse) - (first + 16 * i + j == label ? 1.0f : 0.0f));
-                    if (st != 0.0f) d = fmaf(st, exp_of(fmaf(v, a.over_t, -lse_t)), d);
+                    if (s != 0.0f) d = s * (power_to(v, a.k, lse) - (first + 16 * i + j == label ? 1.0f : 0.0f));
+                    if (st != 0.0f) d = fmaf(st, power_to(v, a.k_t, lse_t), d);
                     e[j] = T::put(d);
                 }
                 const int c = first + 16 * i;
@@ -166,8 +185,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_scores(ScoreArgs<T> a)
 #pragma unroll
             for (int w = 0; w < WA; ++w) {
                 const float *from = meet + (w * C::BB + in_tile) * 3;
-                sum += from[1] * exp_below(from[0], most);
-                if (a.two) sum_t += from[2] * exp_below(from[0] * a.over_t, most * a.over_t);
+                sum += from[1] * rebase(base_of(from[0], a.k), base_of(most, a.k));
+                if (a.two) sum_t += from[2] * rebase(base_of(from[0], a.k_t), base_of(most, a.k_t));
             }
             float *to = a.part + (ct * a.rows + r0 + in_tile) * 3;
             to[0] = most, to[1] = sum, to[2] = sum_t;
@@ -182,7 +201,7 @@ struct RowArgs {
     const float *top_score;
     int64_t x_stride, n, row0, rows;
     int D, classes, top, class_tiles, saved_width;
-    float t, over_t, scale, teacher_scale;
+    float t, over_t, k, k_t, scale, teacher_scale;
     const float *part, *label_score;
     float *loss, *teacher_loss;
     float *saved;  // forward: null, or where lse, lse_t and the scores go; backward: those
@@ -192,6 +211,7 @@ struct RowArgs {
     // backward: the piece of dz
     typename T::elem *dz;
     int class0, piece_classes, dz_stride;
+    bool planes;     // dz is bf16, its planes dz_stride apart (fp32 only: bf16 has the same layout either way)
     int32_t *listed;  // the row's number, or -1 without a gradient
 };
 
@@ -279,38 +299,38 @@ __global__ void __launch_bounds__(256) k_class_finish(RowArgs<T> a)
     for (int ct = l; ct < a.class_tiles; ct += 64) {
         const float *from = a.part + (ct * a.rows + r) * 3;
         const float m = fmaxf(most, from[0]);
-        sum = sum * exp_below(most, m) + from[1] * exp_below(from[0], m);
-        if (a.two) sum_t = sum_t * exp_below(most * a.over_t, m * a.over_t) + from[2] * exp_below(from[0] * a.over_t, m * a.over_t);
+        sum = sum * rebase(base_of(most, a.k), base_of(m, a.k)) + from[1] * rebase(base_of(from[0], a.k), base_of(m, a.k));
+        if (a.two) sum_t = sum_t * rebase(base_of(most, a.k_t), base_of(m, a.k_t)) + from[2] * rebase(base_of(from[0], a.k_t), base_of(m, a.k_t));
         most = m;
     }
-    const float m = max_across<64>(most);
-    sum = sum_across<64>(sum * exp_below(most, m));
-    sum_t = a.two ? sum_across<64>(sum_t * exp_below(most * a.over_t, m * a.over_t)) : sum;
-    const float lse = m + logf(sum), over = a.two ? a.over_t : 1.0f;
+    const float m = max_across<64>(most), base = base_of(m, a.k), base_t = a.two ? base_of(m, a.k_t) : base;
+    sum = sum_across<64>(sum * rebase(base_of(most, a.k), base));
+    sum_t = a.two ? sum_across<64>(sum_t * rebase(base_of(most, a.k_t), base_t)) : sum;
+    const float log_sum = log2f(sum), log_sum_t = log2f(sum_t);
     if (a.labels) {
         const int label = a.labels[row];
         const bool has = (uint32_t)label < (uint32_t)a.classes;
-        if (l == 0 && a.loss) a.loss[row] = has ? (m - a.label_score[row]) + logf(sum) : 0.0f;
+        // (what the score and the sum have in common goes before the sum's logarithm comes to it)
+        if (l == 0 && a.loss) a.loss[row] = has ? kLn2 * (log_sum - fmaf(a.label_score[row], a.k, -base)) : 0.0f;
     }
     float lse_t = INFINITY;
     if (a.top_class) {
         float top_most, total, kl = 0.0f;
         const bool taught = teacher_of(a, row, top_most, total);
         if (taught) {
-            lse_t = m * over + logf(sum_t);
-            const float log_total = logf(total);
+            lse_t = base_t + log_sum_t;
+            const float log_total = log2f(total);
             for (int k = l; k < a.top; k += 64)
                 if ((uint32_t)a.top_class[row * a.top + k] < (uint32_t)a.classes) {
                     const float v = a.top_score[row * a.top + k] * a.over_t - top_most;
                     const float p = exp_of(v) / total;
-                    // (the scores are next to each other: what they have in common goes first)
-                    if (p != 0.0f) kl = fmaf(p, (v - log_total) + ((m - a.z_top[row * a.z_stride + k]) * a.over_t + logf(sum_t)), kl);
+                    if (p != 0.0f) kl = fmaf(p, (v * kLog2e - log_total) + (log_sum_t - fmaf(a.z_top[row * a.z_stride + k], a.k_t, -base_t)), kl);
                 }
             kl = sum_across<64>(kl);
         }
-        if (l == 0 && a.teacher_loss) a.teacher_loss[row] = taught ? a.t * a.t * kl : 0.0f;
+        if (l == 0 && a.teacher_loss) a.teacher_loss[row] = taught ? a.t * a.t * kLn2 * kl : 0.0f;
     }
-    if (l == 0 && a.saved) a.saved[row * a.saved_width] = lse, a.saved[row * a.saved_width + 1] = lse_t;
+    if (l == 0 && a.saved) a.saved[row * a.saved_width] = base + log_sum, a.saved[row * a.saved_width + 1] = lse_t;
 }
 
 // Which rows have a gradient, for the products that sum over rows: what others hold there is not read.
@@ -348,9 +368,17 @@ __global__ void __launch_bounds__(256) k_class_fix(RowArgs<T> a)
             if (a.top_class[row * a.top + o] == c) p += exp_of(a.top_score[row * a.top + o] * a.over_t - most) / total;
         const float z = kept[2 + k];
         float d = 0.0f;
-        if (label >= 0 && a.scale != 0.0f) d = a.scale * (exp_of(z - lse) - (c == label ? 1.0f : 0.0f));
-        if (a.teacher_scale != 0.0f) d = fmaf(a.teacher_scale, exp_of(fmaf(z, a.over_t, -lse_t)) - p, d);
-        a.dz[r * a.dz_stride + (c - a.class0)] = T::put(d);
+        if (label >= 0 && a.scale != 0.0f) d = a.scale * (power_to(z, a.k, lse) - (c == label ? 1.0f : 0.0f));
+        if (a.teacher_scale != 0.0f) d = fmaf(a.teacher_scale, power_to(z, a.k_t, lse_t) - p, d);
+        if (T::PER == 1 && a.planes) {
+            uint16_t e[3];
+            split(d, e);
+            uint16_t *to = reinterpret_cast<uint16_t *>(a.dz) + r * 3 * a.dz_stride + (c - a.class0);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) to[p * (int64_t)a.dz_stride] = e[p];
+        } else {
+            a.dz[r * a.dz_stride + (c - a.class0)] = T::put(d);
+        }
     }
 }
 
@@ -483,6 +511,293 @@ __global__ void __launch_bounds__(256) k_class_zero(typename T::elem *p, int64_t
     if (i < count) p[i] = T::put(0.0f);
 }
 
+// ----------------------------------------------------------------- large calls: operands laid out for bgl_stage.h
+// Rows of D values as rows of planes of bf16, each `padded` wide, zeros behind D and in rows from `rows` to `all_rows`.
+template <class T>
+struct LayArgs {
+    const typename T::elem *from;
+    int64_t stride, rows, all_rows;
+    int D, padded;
+    uint16_t *to;
+    // backward, x: rows without a gradient become zeros, whatever they hold
+    bool select;
+    const int32_t *labels;
+    const float *saved;
+    int saved_width, classes;
+    bool by_label, by_teacher;
+};
+template <class T>
+__global__ void __launch_bounds__(256) k_class_lay(LayArgs<T> a)
+{
+    constexpr int PLANES = T::PER == 1 ? 3 : 1;
+    const int each = a.padded / 8;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / each;
+    const int d = (int)(i % each) * 8;
+    if (row >= a.all_rows) return;
+    bool live = row < a.rows;
+    if (live && a.select) {
+        const float lse_t = a.saved[row * a.saved_width + 1];
+        live = (a.by_label && (uint32_t)a.labels[row] < (uint32_t)a.classes) || (a.by_teacher && lse_t != INFINITY);
+    }
+    uint16_t e[PLANES][8] = {};
+    if (live) {
+        const typename T::elem *from = a.from + row * a.stride + d;
+#pragma unroll
+        for (int v = 0; v < 8; v += T::VEC) {
+            if (d + v >= a.D) break;
+            const uint4 raw = d + v + T::VEC <= a.D ? load_any<uint4>(from + v) : load_end<T>(from + v, a.D - d - v, a.D);
+            if constexpr (PLANES == 1) {
+                __builtin_memcpy(e[0], &raw, 16);
+            } else {
+                const uint32_t q[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint16_t three[3];
+                    split(__uint_as_float(q[j]), three);
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) e[p][v + j] = three[p];
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < PLANES; ++p) __builtin_memcpy(a.to + (row * PLANES + p) * a.padded + d, e[p], 16);
+}
+
+// k_class_scores from laid out operands: 256 classes x 128 rows.
+template <class T>
+struct StageScoreArgs {
+    ScoreArgs<T> s;
+    const char *x, *w;           // of the call's first row, of class 0
+    int64_t x_bytes, w_bytes;    // rows
+    uint32_t x_plane, w_plane;   // planes
+};
+
+template <class T, bool DZ>
+__global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(StageScoreArgs<T> q)
+{
+    using C = stage::Cut<8, 4>;
+    using A = stage::Kc<C::BA>;
+    using B = stage::Kc<C::BB>;
+    constexpr int PLANES = T::PER == 1 ? 3 : 1;
+    __shared__ __attribute__((aligned(1024))) char lds[stage::kStages * (A::BYTES + B::BYTES)];
+    const ScoreArgs<T> &a = q.s;
+    int64_t ct, rt;
+    int fast;
+    if (!tile_of(blockIdx.x, a.by_rows ? a.row_tiles : a.class_tiles, (int)(a.by_rows ? a.class_tiles : a.row_tiles), a.by_rows ? rt : ct, fast)) return;
+    (a.by_rows ? ct : rt) = fast;
+    const int c0 = a.class0 + (int)ct * C::BA, last = a.classes - 1, l = threadIdx.x & 63;
+    const int64_t r0 = rt * C::BB;
+    A weight;
+    B rows;
+    weight.init(q.w + c0 * q.w_bytes, [&](int i) { return (uint32_t)((c0 + i < last ? i : last - c0) * q.w_bytes); });
+    rows.init(q.x + (a.row0 + r0) * q.x_bytes, [&](int i) { return (uint32_t)((r0 + i < a.rows ? i : (int)(a.rows - 1 - r0)) * q.x_bytes); });
+    const int in_tile = C::a_off() + 4 * (l >> 4), first = c0 + in_tile;
+    f32x4 acc[C::FA][C::FB];
+#pragma unroll
+    for (int i = 0; i < C::FA; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int c = first + 16 * i + j;
+            const float b = a.bias ? T::get(a.bias[c < last ? c : last]) : 0.0f;
+#pragma unroll
+            for (int t = 0; t < C::FB; ++t) acc[i][t][j] = b;
+        }
+    stage::multiply<PLANES, A, B, C>(lds, weight, rows, stage::Walk{64, 64, q.w_plane, q.x_plane, a.D}, acc, [](int, const auto &) {});
+    if (c0 + C::BA > a.classes) {
+#pragma unroll
+        for (int i = 0; i < C::FA; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (first + 16 * i + j > last) {
+#pragma unroll
+                    for (int t = 0; t < C::FB; ++t) acc[i][t][j] = -INFINITY;
+                }
+    }
+    float *meet = reinterpret_cast<float *>(lds);  // forward: largest, sum, sum at the temperature of 2 x 128 halves of rows
+#pragma unroll
+    for (int t = 0; t < C::FB; ++t) {
+        const int b = C::b_off() + 16 * t + (l & 15);
+        const int64_t r = r0 + b;
+        const bool live = r < a.rows;
+        const int64_t row = a.row0 + (live ? r : a.rows - 1);
+        int label = a.labels && live ? a.labels[row] : -1;
+        if ((uint32_t)label >= (uint32_t)a.all_classes) label = -1;
+        // the label's place among the lane's values; few tiles have one, and only these look for it
+        const int at = label - first;
+        const bool mine = at >= 0 && at < 16 * C::FA && (at & 15) < 4, any = __ballot(mine) != 0;
+        if constexpr (!DZ) {
+            float most = -INFINITY, sum = 0.0f, sum_t = 0.0f;
+#pragma unroll
+            for (int i = 0; i < C::FA; ++i) most = fmaxf(most, fmaxf(fmaxf(acc[i][t][0], acc[i][t][1]), fmaxf(acc[i][t][2], acc[i][t][3])));
+            most = down_column(most, [](float p, float q) { return fmaxf(p, q); });
+            const float base = base_of(most, a.k), base_t = base_of(most, a.k_t);
+#pragma unroll
+            for (int i = 0; i < C::FA; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum += power_to(acc[i][t][j], a.k, base);
+            if (a.two) {
+#pragma unroll
+                for (int i = 0; i < C::FA; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) sum_t += power_to(acc[i][t][j], a.k_t, base_t);
+            }
+            if (any) {
+#pragma unroll
+                for (int i = 0; i < C::FA; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (mine && at == 16 * i + j) a.label_score[row] = acc[i][t][j];
+            }
+            sum = down_column(sum, [](float p, float q) { return p + q; });
+            if (a.two) sum_t = down_column(sum_t, [](float p, float q) { return p + q; });
+            float *to = meet + (C::a_off() / (16 * C::FA) * C::BB + b) * 3;
+            if (l < 16) to[0] = most, to[1] = sum, to[2] = sum_t;
+        } else {
+            const float *kept = a.saved + row * a.saved_width;
+            const bool by_label = label >= 0 && a.scale != 0.0f, by_teacher = live && kept[1] != INFINITY && a.teacher_scale != 0.0f;
+            const float lse = by_label ? kept[0] : INFINITY, lse_t = by_teacher ? kept[1] : INFINITY;
+            const bool teachers = a.teacher_scale != 0.0f;
+            uint16_t *to = reinterpret_cast<uint16_t *>(a.dz) + r * PLANES * a.dz_stride + (first - a.class0);
+#pragma unroll
+            for (int i = 0; i < C::FA; ++i) {
+                float d[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) d[j] = a.scale * power_to(acc[i][t][j], a.k, lse);
+                if (teachers) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) d[j] = fmaf(a.teacher_scale, power_to(acc[i][t][j], a.k_t, lse_t), d[j]);
+                }
+                if (any) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (mine && at == 16 * i + j) d[j] -= a.scale;
+                }
+                if constexpr (PLANES == 1) {
+                    uint16_t e[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) e[j] = BF16::put(d[j]);
+                    __builtin_memcpy(to + 16 * i, e, sizeof(e));
+                } else {
+                    uint16_t e[3][4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint16_t three[3];
+                        split(d[j], three);
+#pragma unroll
+                        for (int p = 0; p < 3; ++p) e[p][j] = three[p];
+                    }
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) __builtin_memcpy(to + p * (int64_t)a.dz_stride + 16 * i, e[p], sizeof(e[p]));
+                }
+            }
+        }
+    }
+    if constexpr (!DZ) {
+        __syncthreads();
+        const int b = threadIdx.x;
+        if (b >= C::BB || r0 + b >= a.rows) return;
+        const float *one = meet + b * 3, *two = meet + (C::BB + b) * 3;
+        const float most = fmaxf(one[0], two[0]), base = base_of(most, a.k), base_t = base_of(most, a.k_t);
+        float *to = a.part + (ct * a.rows + r0 + b) * 3;
+        to[0] = most;
+        to[1] = one[1] * rebase(base_of(one[0], a.k), base) + two[1] * rebase(base_of(two[0], a.k), base);
+        to[2] = a.two ? one[2] * rebase(base_of(one[0], a.k_t), base_t) + two[2] * rebase(base_of(two[0], a.k_t), base_t) : 0.0f;
+    }
+}
+
+// k_class_product from laid out operands: 256 x 128.  OC: dW, else dx.
+template <class T>
+struct StagePieceArgs {
+    const char *a, *b;                 // dz; W or x
+    int64_t a_bytes, b_bytes;          // rows
+    uint32_t a_plane, b_plane;
+    int64_t M, K;                      // (dW: rows up to a multiple of 32)
+    int N, a_width, b_width;           // columns of the result, of dz and of the other that can be read
+    int64_t row_tiles;
+    int col_tiles, shares;
+    int64_t per_share;                 // a multiple of 32
+    typename T::elem *out, *sums;
+    int64_t out_stride;
+    float *slots, *sum_slots;
+    int64_t slot_rows;
+    bool add;
+};
+
+template <class T, bool OC>
+__global__ void __launch_bounds__(stage::kThreads, 2) k_class_product_stage(StagePieceArgs<T> a)
+{
+    using C = stage::Cut<8, 4>;
+    using A = std::conditional_t<OC, stage::Oc<C::BA>, stage::Kc<C::BA>>;
+    using B = stage::Oc<C::BB>;
+    constexpr int PLANES = T::PER == 1 ? 3 : 1;
+    __shared__ __attribute__((aligned(1024))) char lds[stage::kStages * (A::BYTES + B::BYTES)];
+    const int share = blockIdx.x % a.shares;
+    int64_t rt;
+    int ct;
+    if (!tile_of(blockIdx.x / a.shares, a.row_tiles, a.col_tiles, rt, ct)) return;
+    const int64_t m0 = rt * C::BA, k0 = share * a.per_share;
+    const int n0 = ct * C::BB, K = (int)(a.K - k0 < a.per_share ? a.K - k0 : a.per_share);
+    A left;
+    B right;
+    uint32_t a_block;
+    if constexpr (OC) {
+        left.init(a.a + k0 * a.a_bytes, (uint32_t)a.a_bytes, (int)m0, a.a_width);
+        a_block = (uint32_t)(stage::kStep * a.a_bytes);
+    } else {
+        left.init(a.a + m0 * a.a_bytes + k0 * 2, [&](int i) { return (uint32_t)((m0 + i < a.M ? i : (int)(a.M - 1 - m0)) * a.a_bytes); });
+        a_block = stage::kStep * 2;
+    }
+    right.init(a.b + k0 * a.b_bytes, (uint32_t)a.b_bytes, n0, a.b_width);
+    f32x4 acc[C::FA][C::FB] = {};
+    float sums[C::FA] = {};
+    const bool summing = OC && (a.sums || a.sum_slots) && n0 == 0 && C::b_off() == 0;
+    stage::multiply<PLANES, A, B, C>(lds, left, right, stage::Walk{a_block, (uint32_t)(stage::kStep * a.b_bytes), a.a_plane, a.b_plane, K}, acc, [&](int b_plane, const auto &f) {
+        if (summing && b_plane == 0) {
+#pragma unroll
+            for (int t = 0; t < C::FA; ++t) {
+                const uint4 v = __builtin_bit_cast(uint4, f[t]);
+                sums[t] = BF16::sum({v.x, v.y, v.z, v.w}, sums[t]);
+            }
+        }
+    });
+    const int l = threadIdx.x & 63;
+    float *slot = a.slots ? a.slots + share * a.slot_rows * a.N : nullptr;
+#pragma unroll
+    for (int i = 0; i < C::FA; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t m = m0 + C::a_off() + 16 * i + 4 * (l >> 4) + j;
+            if (m >= a.M) continue;
+#pragma unroll
+            for (int t = 0; t < C::FB; ++t) {
+                const int c = n0 + C::b_off() + 16 * t + (l & 15);
+                if (c >= a.N) continue;
+                const float v = acc[i][t][j];
+                if (slot) {
+                    float *to = slot + m * a.N + c;
+                    *to = a.add ? *to + v : v;
+                } else {
+                    a.out[m * a.out_stride + c] = T::put(v);
+                }
+            }
+        }
+    if (summing) {
+#pragma unroll
+        for (int t = 0; t < C::FA; ++t) {
+            const float v = down_column(sums[t], [](float p, float q) { return p + q; });
+            const int64_t m = m0 + C::a_off() + 16 * t + (l & 15);
+            if (l >= 16 || m >= a.M) continue;
+            if (a.sum_slots) {
+                float *to = a.sum_slots + share * a.slot_rows + m;
+                *to = a.add ? *to + v : v;
+            } else {
+                a.sums[m] = T::put(v);
+            }
+        }
+    }
+}
+
 // ----------------------------------------------------------------- plans
 using Large = Cut<2, 2, 4, 4>;   // 128 x 128
 using Middle = Cut<2, 2, 4, 2>;  // 128 x 64
@@ -498,12 +813,27 @@ struct Plan {
     int piece_classes, class_pieces, dx_shares, dw_shares;
     int64_t dx_per, dw_per;
     size_t dz_bytes, list_bytes, dx_bytes, dw_bytes, db_bytes, backward_bytes;
+    // large calls: laid out operands, forward (0: as they are) and backward
+    int padded;
+    size_t x_bytes, w_bytes, back_x_bytes;
 };
 
-int64_t dz_stride_of(int64_t classes) { return (classes + 7) / 8 * 8; }  // (pieces of 4 are stored, and 16 bytes of bf16 read)
-
-constexpr int64_t kSharesFill = 512;  // workgroups that ranges of the summed index are to make together
-constexpr int64_t kShareLeast = 512;  // of the summed index
+// How a call is cut up.  Small ones: tiles of 128 x 128 straight from the operands.  Large ones: 256 x 128 of operands laid out for bgl_stage.h (bf16 whose rows
+// are whole steps are laid out already).
+struct Scheme {
+    bool large;
+    int a_rows;                 // of a tile: classes of the scores; rows of dx, classes of dW
+    int64_t values, round_classes, round_rows;
+    int dz_value_bytes, planes;
+};
+Scheme scheme_of(const bgl_class_loss_t *l, bool large)
+{
+    const bool f32 = l->dtype == BGL_F32;
+    if (large) return Scheme{true, 256, (int64_t)1 << 27, 256, 128, f32 ? 6 : 2, f32 ? 3 : 1};
+    return Scheme{false, 128, (int64_t)1 << 25, 8, 1, f32 ? 4 : 2, 1};  // (pieces of 4 classes are stored, and 16 bytes of bf16 read)
+}
+bool large_call(const bgl_class_loss_t *l, int64_t n) { return n >= 256 && l->classes >= 128 && (double)n * l->classes * l->in_dim >= kLargeProducts; }
+bool laid_out(const bgl_class_loss_t *l) { return l->dtype == BGL_BF16 && l->in_dim % stage::kStep == 0; }
 
 int shares_for(int64_t tiles, int64_t summed)
 {
@@ -511,65 +841,69 @@ int shares_for(int64_t tiles, int64_t summed)
     return (int)(want < 1 || most < 1 ? 1 : want < most ? want : most);
 }
 
-Plan plan_of(const bgl_class_loss_t *l, int64_t n)
+Plan plan_of(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
 {
     Plan p{};
-    const int es = l->dtype == BGL_F32 ? 4 : 2;
-    p.class_tiles = (int)ceil_div(l->classes, Large::BA);
+    p.class_tiles = (int)ceil_div(l->classes, s.a_rows);
     p.pass_rows = kPartialBytes / (12 * (int64_t)p.class_tiles);
     p.pass_rows = p.pass_rows < 1024 ? 1024 : p.pass_rows / 128 * 128;
     if (p.pass_rows > n) p.pass_rows = n;
     p.part_bytes = round_up((size_t)p.pass_rows * p.class_tiles * 12, 256);
     p.label_bytes = round_up((size_t)n * 4, 256);
     p.top_bytes = round_up((size_t)n * l->top * 4, 256);
-    p.forward_bytes = p.part_bytes + p.label_bytes + p.top_bytes;
+    if (s.large) {
+        p.padded = (int)round_up(l->in_dim, stage::kStep);
+        p.back_x_bytes = round_up((size_t)round_up(n, stage::kStep) * p.padded * 2 * s.planes, 256);
+        if (!laid_out(l)) p.x_bytes = p.back_x_bytes, p.w_bytes = round_up((size_t)l->classes * p.padded * 2 * s.planes, 256);
+    }
+    p.forward_bytes = p.part_bytes + p.label_bytes + p.top_bytes + p.x_bytes + p.w_bytes;
 
     // one piece if it is small enough; else all classes of some rows (dx is then written once and dW added up), and with very many classes some
     // classes of all rows, or of kPieceRows (dW is then written once for each of these, and dx added up); about equal ones
-    const int64_t stride = dz_stride_of(l->classes);
+    const int64_t stride = round_up(l->classes, s.round_classes);
     p.piece_rows = n, p.piece_classes = l->classes;
-    if (n * stride > kPieceValues) {
+    if (n * stride > s.values) {
         if (l->classes <= kPieceRows) {
-            p.piece_rows = (int64_t)round_up((size_t)ceil_div(n, ceil_div(n * stride, kPieceValues)), 128);
+            p.piece_rows = (int64_t)round_up((size_t)ceil_div(n, ceil_div(n * stride, s.values)), 128);
             if (p.piece_rows > n) p.piece_rows = n;
         } else {
             if (n > kPieceRows) p.piece_rows = kPieceRows;
-            const int64_t fit = (int64_t)round_up((size_t)ceil_div(stride, ceil_div(p.piece_rows * stride, kPieceValues)), 256);
+            const int64_t fit = (int64_t)round_up((size_t)ceil_div(stride, ceil_div(p.piece_rows * stride, s.values)), 256);
             if (fit < l->classes) p.piece_classes = (int)fit;
         }
     }
     p.class_pieces = (int)ceil_div(l->classes, p.piece_classes);
     p.row_pieces = p.piece_rows > 0 ? ceil_div(n, p.piece_rows) : 0;
-    p.dz_stride = dz_stride_of(p.piece_classes);
-    p.dz_bytes = round_up((size_t)p.piece_rows * p.dz_stride * es, 256);
-    p.list_bytes = round_up((size_t)n * 4, 256);
+    p.dz_stride = round_up(p.piece_classes, s.round_classes);
+    p.dz_bytes = round_up(round_up(p.piece_rows, s.round_rows) * p.dz_stride * s.dz_value_bytes, 256);
+    p.list_bytes = s.large ? 0 : round_up((size_t)n * 4, 256);
     const int64_t cols = ceil_div(l->in_dim, 128);
-    p.dx_shares = p.class_pieces > 1 && p.row_pieces > 1 ? 1 : shares_for(ceil_div(p.piece_rows, 128) * cols, p.piece_classes);
+    p.dx_shares = p.class_pieces > 1 && p.row_pieces > 1 ? 1 : shares_for(ceil_div(p.piece_rows, s.a_rows) * cols, p.piece_classes);
     p.dx_per = round_up((size_t)ceil_div(p.piece_classes, p.dx_shares), 64);
-    p.dw_shares = shares_for(ceil_div(p.piece_classes, 128) * cols, p.piece_rows);
+    p.dw_shares = shares_for(ceil_div(p.piece_classes, s.a_rows) * cols, p.piece_rows);
     p.dw_per = round_up((size_t)ceil_div(p.piece_rows, p.dw_shares), 64);
     p.dx_bytes = p.dx_shares > 1 || p.class_pieces > 1 ? round_up((size_t)p.dx_shares * (p.class_pieces > 1 ? n : p.piece_rows) * l->in_dim * 4, 256) : 0;
     p.dw_bytes = p.dw_shares > 1 || p.row_pieces > 1 ? round_up((size_t)p.dw_shares * p.piece_classes * l->in_dim * 4, 256) : 0;
     p.db_bytes = p.dw_bytes ? round_up((size_t)p.dw_shares * p.piece_classes * 4, 256) : 0;
-    p.backward_bytes = p.dz_bytes + p.list_bytes + p.dx_bytes + p.dw_bytes + p.db_bytes;
+    p.backward_bytes = p.dz_bytes + p.list_bytes + p.dx_bytes + p.dw_bytes + p.db_bytes + p.back_x_bytes + p.w_bytes;
     return p;
 }
 
 // What the backward calls of up to n rows need: no call of fewer rows needs more.  (Shares are less than kSharesFill tiles in all.)
-size_t backward_room(const bgl_class_loss_t *l, int64_t n)
+size_t backward_room(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
 {
-    const int es = l->dtype == BGL_F32 ? 4 : 2;
-    const int64_t V = l->classes, D = l->in_dim, stride = dz_stride_of(V), shared = kSharesFill * 128;
+    const int64_t V = l->classes, D = l->in_dim, stride = round_up(V, s.round_classes), shared = kSharesFill * s.a_rows;
     const bool many = V > kPieceRows;
     const auto least = [](int64_t a, int64_t b) { return a < b ? a : b; };
     const auto most = [](int64_t a, int64_t b) { return a > b ? a : b; };
-    const int64_t over = many ? 256 * least(n, kPieceRows) : 128 * stride;
-    size_t bytes = round_up((size_t)least(n * stride, kPieceValues + over) * es, 256) + round_up((size_t)n * 4, 256);
+    const int64_t over = (many ? 256 * least(n, kPieceRows) : 128 * stride) + 128 * least(stride, s.values);
+    const Plan p = plan_of(l, n, s);
+    size_t bytes = round_up((size_t)least(round_up(n, 128) * stride, s.values + over) * s.dz_value_bytes, 256) + round_up((size_t)n * 4, 256) + p.back_x_bytes + p.w_bytes;
     if (V >= 2 * kShareLeast) bytes += round_up((size_t)most(many ? n : 0, least(shared, n * (V / kShareLeast))) * D * 4, 256);
     const int64_t shares = n >= 2 * kShareLeast ? least(shared, V * (n / kShareLeast)) : 0;
-    const int64_t pieces = many ? (n > kPieceRows ? kPieceValues / kPieceRows + 256 : 0) : n * stride > kPieceValues ? V : 0;
+    const int64_t pieces = many ? (n > kPieceRows ? s.values / kPieceRows + 256 : 0) : n * stride > s.values ? V : 0;
     bytes += round_up((size_t)most(shares, pieces) * D * 4, 256) + round_up((size_t)most(shares, pieces) * 4, 256);
-    return bytes;
+    return bytes > p.backward_bytes ? bytes : p.backward_bytes;
 }
 
 template <class T, bool DZ>
@@ -607,7 +941,7 @@ RowArgs<T> row_args(const Call &c)
     RowArgs<T> r{};
     r.x = (const E *)c.x, r.w = (const E *)c.weight, r.bias = (const E *)c.bias, r.labels = c.labels, r.top_class = c.top_class, r.top_score = c.top_score;
     r.x_stride = c.x_stride, r.n = c.n, r.D = c.l->in_dim, r.classes = c.l->classes, r.top = c.l->top, r.saved_width = 2 + c.l->top;
-    r.t = c.l->temperature, r.over_t = 1.0f / c.l->temperature;
+    r.t = c.l->temperature, r.over_t = 1.0f / c.l->temperature, r.k = kLog2e, r.k_t = (float)(1.4426950408889634 / c.l->temperature);
     r.two = c.top_class && c.l->temperature != 1.0f;
     return r;
 }
@@ -617,24 +951,74 @@ ScoreArgs<T> score_args(const Call &c)
     using E = typename T::elem;
     ScoreArgs<T> s{};
     s.x = (const E *)c.x, s.w = (const E *)c.weight, s.bias = (const E *)c.bias, s.labels = c.labels, s.x_stride = c.x_stride, s.n = c.n;
-    s.classes = s.all_classes = c.l->classes, s.D = c.l->in_dim, s.over_t = 1.0f / c.l->temperature, s.two = c.top_class && c.l->temperature != 1.0f;
+    s.classes = s.all_classes = c.l->classes, s.D = c.l->in_dim, s.k = kLog2e, s.k_t = (float)(1.4426950408889634 / c.l->temperature), s.two = c.top_class && c.l->temperature != 1.0f;
     s.saved_width = 2 + c.l->top;
     return s;
+}
+
+template <class T, bool DZ>
+void launch_scores_stage(StageScoreArgs<T> &q, hipStream_t st)
+{
+    ScoreArgs<T> &s = q.s;
+    s.class_tiles = (int)ceil_div(s.classes - s.class0, 256);
+    s.row_tiles = ceil_div(s.rows, 128);
+    s.by_rows = s.row_tiles > s.class_tiles;
+    const int64_t tiles = s.by_rows ? tile_count(s.row_tiles, s.class_tiles) : tile_count(s.class_tiles, (int)s.row_tiles);
+    k_class_scores_stage<T, DZ><<<dim3((unsigned)tiles), dim3(stage::kThreads), 0, st>>>(q);
+}
+
+template <class T>
+void launch_lay(const typename T::elem *from, int64_t stride, int64_t rows, int64_t all_rows, int D, int padded, void *to, const RowArgs<T> *select, hipStream_t st)
+{
+    LayArgs<T> a{};
+    a.from = from, a.stride = stride, a.rows = rows, a.all_rows = all_rows, a.D = D, a.padded = padded, a.to = (uint16_t *)to;
+    if (select) {
+        a.select = true, a.labels = select->labels, a.saved = select->saved, a.saved_width = select->saved_width, a.classes = select->classes;
+        a.by_label = select->labels && select->scale != 0.0f, a.by_teacher = select->top_class && select->teacher_scale != 0.0f;
+    }
+    k_class_lay<T><<<dim3((unsigned)ceil_div(all_rows * (padded / 8), 256)), dim3(256), 0, st>>>(a);
+}
+
+// Whether a call goes the large way: what is laid out already has to begin on multiples of 16 bytes.
+bool goes_large(const Call &c, bool reads_x)
+{
+    if (!large_call(c.l, c.n)) return false;
+    return !laid_out(c.l) || (aligned(c.weight, 16) && (!reads_x || (aligned(c.x, 16) && c.x_stride % 8 == 0 && c.x_stride < (int64_t)1 << 23)));
+}
+
+// The laid out weight and rows; what is laid out already is where it is.
+template <class T>
+StageScoreArgs<T> stage_args(const Call &c, const Plan &p, const Scheme &h, const ScoreArgs<T> &s, char *x, char *w, const RowArgs<T> *select)
+{
+    StageScoreArgs<T> q{};
+    q.s = s;
+    q.x_bytes = q.w_bytes = (int64_t)p.padded * h.planes * 2, q.x_plane = q.w_plane = p.padded * 2;
+    if (p.w_bytes) launch_lay<T>(s.w, s.D, s.classes, s.classes, s.D, p.padded, w, nullptr, c.stream), q.w = w;
+    else q.w = (const char *)s.w;
+    if (p.w_bytes || select) launch_lay<T>(s.x, s.x_stride, c.n, round_up(c.n, stage::kStep), s.D, p.padded, x, select, c.stream), q.x = x;
+    else q.x = (const char *)s.x, q.x_bytes = s.x_stride * 2;
+    return q;
 }
 
 template <class T>
 int forward(const Call &c, float *loss, float *teacher_loss, float *saved)
 {
-    const Plan p = plan_of(c.l, c.n);
+    const Scheme h = scheme_of(c.l, goes_large(c, true));
+    const Plan p = plan_of(c.l, c.n, h);
     ScoreArgs<T> s = score_args<T>(c);
     RowArgs<T> r = row_args<T>(c);
-    s.part = (float *)c.workspace, s.label_score = (float *)(c.workspace + p.part_bytes);
+    char *ws = c.workspace;
+    s.part = (float *)ws, s.label_score = (float *)(ws += p.part_bytes);
+    char *top = ws += p.label_bytes, *x = ws += p.top_bytes, *w = ws += p.x_bytes;
     r.part = s.part, r.label_score = s.label_score, r.class_tiles = p.class_tiles;
-    r.z_top = saved ? saved + 2 : (float *)(c.workspace + p.part_bytes + p.label_bytes), r.z_stride = saved ? r.saved_width : r.top;
+    r.z_top = saved ? saved + 2 : (float *)top, r.z_stride = saved ? r.saved_width : r.top;
     r.loss = loss, r.teacher_loss = teacher_loss, r.saved = saved;
+    StageScoreArgs<T> q{};
+    if (h.large) q = stage_args<T>(c, p, h, s, x, w, nullptr);
     for (int64_t row0 = 0; row0 < c.n; row0 += p.pass_rows) {
         s.row0 = r.row0 = row0, s.rows = r.rows = c.n - row0 < p.pass_rows ? c.n - row0 : p.pass_rows;
-        launch_scores<T, false>(s, c.stream);
+        if (h.large) q.s = s, launch_scores_stage<T, false>(q, c.stream);
+        else launch_scores<T, false>(s, c.stream);
         if (c.top_class) k_class_top<T><<<dim3((unsigned)ceil_div(r.rows * ((r.top + 3) / 4), 4)), dim3(256), 0, c.stream>>>(r);
         k_class_finish<T><<<dim3((unsigned)ceil_div(r.rows, 4)), dim3(256), 0, c.stream>>>(r);
     }
@@ -649,6 +1033,12 @@ void launch_product(PieceArgs<T> &a, hipStream_t st)
     const dim3 grid((unsigned)tile_count(a.row_tiles, a.col_tiles), (unsigned)a.shares);
     if (a.N >= T::VEC) k_class_product<T, Large, OC, false><<<grid, dim3(kThreads), 0, st>>>(a);
     else k_class_product<T, Large, OC, true><<<grid, dim3(kThreads), 0, st>>>(a);
+}
+template <class T, bool OC>
+void launch_product_stage(StagePieceArgs<T> &a, hipStream_t st)
+{
+    a.row_tiles = ceil_div(a.M, 256), a.col_tiles = (int)ceil_div(a.N, 128);
+    k_class_product_stage<T, OC><<<dim3((unsigned)(tile_count(a.row_tiles, a.col_tiles) * a.shares)), dim3(stage::kThreads), 0, st>>>(a);
 }
 template <class T>
 void launch_reduce(const float *slots, int64_t slot_values, int64_t rows, int width, int shares, typename T::elem *out, int64_t stride, hipStream_t st)
@@ -669,40 +1059,68 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
         BGL_HIP(hipGetLastError());
         return BGL_OK;
     }
-    const Plan p = plan_of(c.l, c.n);
+    const Scheme h = scheme_of(c.l, goes_large(c, false));
+    const Plan p = plan_of(c.l, c.n, h);
     char *ws = c.workspace;
     E *dz = (E *)ws;
     int32_t *listed = (int32_t *)(ws += p.dz_bytes);
     float *dx_slots = (float *)(ws += p.list_bytes), *dw_slots = (float *)(ws += p.dx_bytes), *db_slots = (float *)(ws += p.dw_bytes);
+    char *x_laid = ws += p.db_bytes, *w_laid = ws += p.back_x_bytes;
     ScoreArgs<T> s = score_args<T>(c);
     RowArgs<T> r = row_args<T>(c);
     s.saved = saved, s.dz = dz, s.dz_stride = (int)p.dz_stride;
     s.scale = r.scale = c.labels ? scale : 0.0f;
     s.teacher_scale = r.teacher_scale = c.top_class ? teacher_scale * c.l->temperature : 0.0f;
-    r.saved = const_cast<float *>(saved), r.dz = dz, r.dz_stride = (int)p.dz_stride;
+    r.saved = const_cast<float *>(saved), r.dz = dz, r.dz_stride = (int)p.dz_stride, r.planes = h.large;
+    StageScoreArgs<T> q{};
+    if (h.large) q = stage_args<T>(c, p, h, s, x_laid, w_laid, &r);
+    const int64_t dz_row = p.dz_stride * h.planes * 2;
     for (int cp = 0; cp < p.class_pieces; ++cp) {
         const int class0 = cp * p.piece_classes, classes = V - class0 < p.piece_classes ? V - class0 : p.piece_classes;
         for (int64_t rp = 0; rp < p.row_pieces; ++rp) {
             const int64_t row0 = rp * p.piece_rows, rows = c.n - row0 < p.piece_rows ? c.n - row0 : p.piece_rows;
             s.row0 = r.row0 = row0, s.rows = r.rows = rows, s.class0 = r.class0 = class0, r.piece_classes = classes, s.classes = class0 + classes;
             r.listed = listed + row0;
-            if (cp == 0 && (dweight || dbias)) k_class_rows<T><<<dim3((unsigned)ceil_div(rows, 256)), dim3(256), 0, c.stream>>>(r);
-            launch_scores<T, true>(s, c.stream);
+            if (h.large) {
+                q.s = s;
+                launch_scores_stage<T, true>(q, c.stream);
+            } else {
+                if (cp == 0 && dweight) k_class_rows<T><<<dim3((unsigned)ceil_div(rows, 256)), dim3(256), 0, c.stream>>>(r);
+                launch_scores<T, true>(s, c.stream);
+            }
             if (r.teacher_scale != 0.0f) k_class_fix<T><<<dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, c.stream>>>(r);
-            if (dx) {
+            float *slots = p.dx_bytes ? dx_slots + (p.class_pieces > 1 ? row0 * D : 0) : nullptr;
+            const int64_t slot_rows = p.class_pieces > 1 ? c.n : rows;
+            if (dx && h.large) {
+                StagePieceArgs<T> a{};
+                a.a = (const char *)dz, a.a_bytes = dz_row, a.a_plane = p.dz_stride * 2, a.b = q.w + class0 * q.w_bytes, a.b_bytes = q.w_bytes, a.b_plane = q.w_plane;
+                a.M = rows, a.K = classes, a.N = D, a.a_width = (int)p.dz_stride, a.b_width = p.padded, a.shares = p.dx_shares, a.per_share = p.dx_per;
+                a.out = dx + row0 * dx_stride, a.out_stride = dx_stride, a.slots = slots, a.slot_rows = slot_rows, a.add = cp > 0;
+                launch_product_stage<T, false>(a, c.stream);
+            } else if (dx) {
                 PieceArgs<T> a{};
                 a.a = dz, a.a_stride = p.dz_stride, a.b = s.w + (int64_t)class0 * D, a.b_stride = D, a.M = rows, a.K = classes, a.N = D, a.a_width = (int)p.dz_stride;
                 a.shares = p.dx_shares, a.per_share = p.dx_per, a.out = dx + row0 * dx_stride, a.out_stride = dx_stride;
-                if (p.dx_bytes) a.slots = dx_slots + (p.class_pieces > 1 ? row0 * D : 0), a.slot_rows = p.class_pieces > 1 ? c.n : rows, a.add = cp > 0;
+                a.slots = slots, a.slot_rows = slot_rows, a.add = cp > 0;
                 launch_product<T, false>(a, c.stream);
-                if (p.dx_bytes && p.class_pieces == 1) launch_reduce<T>(dx_slots, rows * D, rows, D, p.dx_shares, dx + row0 * dx_stride, dx_stride, c.stream);
             }
-            if (dweight || dbias) {
-                PieceArgs<T> a{};
-                a.a = dz, a.a_stride = p.dz_stride, a.b = s.x + row0 * c.x_stride, a.b_stride = c.x_stride, a.list = listed + row0, a.M = classes, a.K = rows;
-                a.N = D, a.a_width = (int)p.dz_stride, a.shares = p.dw_shares, a.per_share = p.dw_per;
+            if (slots && dx && p.class_pieces == 1) launch_reduce<T>(slots, rows * D, rows, D, p.dx_shares, dx + row0 * dx_stride, dx_stride, c.stream);
+            if (!dweight) continue;
+            const auto fill = [&](auto &a) {
+                a.M = classes, a.N = D, a.a_width = (int)p.dz_stride, a.shares = p.dw_shares, a.per_share = p.dw_per;
                 a.out = dweight + (int64_t)class0 * D, a.out_stride = D, a.sums = dbias ? dbias + class0 : nullptr;
                 if (p.dw_bytes) a.slots = dw_slots, a.sum_slots = dbias ? db_slots : nullptr, a.slot_rows = p.piece_classes, a.add = rp > 0;
+            };
+            if (h.large) {
+                StagePieceArgs<T> a{};
+                fill(a);
+                a.a = (const char *)dz, a.a_bytes = dz_row, a.a_plane = p.dz_stride * 2, a.b = q.x + row0 * q.x_bytes, a.b_bytes = q.x_bytes, a.b_plane = q.x_plane;
+                a.b_width = p.padded, a.K = round_up(rows, stage::kStep);  // (rows of zeros in both)
+                launch_product_stage<T, true>(a, c.stream);
+            } else {
+                PieceArgs<T> a{};
+                fill(a);
+                a.a = dz, a.a_stride = p.dz_stride, a.b = s.x + row0 * c.x_stride, a.b_stride = c.x_stride, a.list = listed + row0, a.K = rows;
                 launch_product<T, true>(a, c.stream);
             }
         }
@@ -712,6 +1130,19 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
     if (p.dx_bytes && dx && p.class_pieces > 1) launch_reduce<T>(dx_slots, c.n * D, c.n, D, p.dx_shares, dx, dx_stride, c.stream);
     BGL_HIP(hipGetLastError());
     return BGL_OK;
+}
+
+// Both ways' needs: which one a call goes depends on where its operands lie.
+void room_of(const bgl_class_loss_t *l, int64_t n, size_t &forward, size_t &backward)
+{
+    forward = backward = 0;
+    for (const bool large : {false, true}) {
+        if (large && !large_call(l, n)) continue;
+        const Scheme h = scheme_of(l, large);
+        const size_t f = plan_of(l, n, h).forward_bytes, b = backward_room(l, n, h);
+        if (f > forward) forward = f;
+        if (b > backward) backward = b;
+    }
 }
 
 int check_loss(const bgl_class_loss_t *l, int64_t n)
@@ -755,10 +1186,10 @@ extern "C" int bgl_class_loss_workspace_bytes(const bgl_class_loss_t *loss, int6
 try {
     if (!forward_bytes && !backward_bytes) BGL_FAIL(BGL_EINVAL, "forward_bytes and backward_bytes are null");
     BGL_TRY(check_loss(loss, n));
-    const Plan p = plan_of(loss, n);
-    if (forward_bytes) *forward_bytes = p.forward_bytes;
-    const size_t room = backward_room(loss, n);
-    if (backward_bytes) *backward_bytes = room > p.backward_bytes ? room : p.backward_bytes;
+    size_t forward, backward;
+    room_of(loss, n, forward, backward);
+    if (forward_bytes) *forward_bytes = forward;
+    if (backward_bytes) *backward_bytes = backward;
     return BGL_OK;
 } BGL_NOTHROW_END
 
@@ -770,7 +1201,7 @@ try {
     BGL_TRY(check_call(c));
     if (!aligned(label_loss, 4) || !aligned(teacher_loss, 4) || !aligned(saved, 4)) BGL_FAIL(BGL_EINVAL, "label_loss, teacher_loss or saved is misaligned");
     if ((label_loss && n > 0 && !labels) || (teacher_loss && n > 0 && !teacher_classes)) BGL_FAIL(BGL_EINVAL, "a loss without its labels or teacher");
-    BGL_TRY(check_workspace(workspace, workspace_bytes, n > 0 ? plan_of(loss, n).forward_bytes : 0));
+    BGL_TRY(check_workspace(workspace, workspace_bytes, n > 0 ? plan_of(loss, n, scheme_of(loss, goes_large(c, true))).forward_bytes : 0));
     if (n == 0) return BGL_OK;
     return loss->dtype == BGL_F32 ? forward<tile::F32>(c, label_loss, teacher_loss, saved) : forward<tile::BF16>(c, label_loss, teacher_loss, saved);
 } BGL_NOTHROW_END
@@ -788,7 +1219,7 @@ try {
     if (!aligned(dweight, es) || !aligned(dbias, es)) BGL_FAIL(BGL_EINVAL, "dweight or dbias is misaligned");
     if (dbias && !dweight) BGL_FAIL(BGL_EINVAL, "dbias without dweight");
     if (!dx && !dweight) BGL_FAIL(BGL_EINVAL, "no gradient is asked for");
-    BGL_TRY(check_workspace(workspace, workspace_bytes, n > 0 ? plan_of(loss, n).backward_bytes : 0));
+    BGL_TRY(check_workspace(workspace, workspace_bytes, n > 0 ? plan_of(loss, n, scheme_of(loss, goes_large(c, false))).backward_bytes : 0));
     return loss->dtype == BGL_F32 ? backward<tile::F32>(c, saved, scale, teacher_scale, dx, dx_stride, dweight, dbias)
                                   : backward<tile::BF16>(c, saved, scale, teacher_scale, dx, dx_stride, dweight, dbias);
 } BGL_NOTHROW_END

@@ -1,0 +1,192 @@
+// Device templates for large products of bf16 matrices on the matrix units (gfx950): tiles go from global memory straight into LDS, three stages of
+// 32 summed values deep, and from there as fragments of 16 x 16 x 32 MFMA instructions.
+//
+// Against the tiles of bgl_tile.h, which pass through registers: the loads take none, so that a wavefront keeps 128 x 64 sums (a fragment read from LDS meets
+// 8 or 4 others instead of 4) and two workgroups still share a CU, one's epilogue beside the other's products; and a step waits for loads that were asked for
+// two steps before, behind one barrier.  In return rows are read in whole 16-byte pieces: they begin on multiples of 16 bytes and are padded with zeros to
+// whole steps.
+//
+// A fp32 value is three bf16 (its first 8 bits, the next 8 of what is left, the last): all 24 bits as long as the value is above 2^-110.  A product of two is
+// the six products of parts that count, what is left out is below 2^-23 of it.  Rows hold the three parts one after the other ("planes").
+//
+// A tile of an operand in LDS, in the two orders an operand can have:
+//   summed index contiguous (Kc)   BO rows of 64 bytes, 16-byte piece p of row r at p ^ (r / 2 & 3): 8 lanes that read 16 bytes each, from rows in a row, meet
+//                                  all banks
+//   kept index contiguous (Oc)     32 rows of BO values, blocks of 16 values moved about within a row (as in bgl_tile.h); fragments by the LDS read that
+//                                  transposes 4 x 16 values among 16 lanes
+// A load of a wavefront fills 1,024 consecutive bytes of LDS, so it is the addresses it reads from that are exchanged.
+#pragma once
+
+#include "bgl_internal.h"
+#include "bgl_tile.h"
+
+namespace bgl {
+namespace stage {
+
+using tile::bf16x8;
+using tile::f32x4;
+using tile::s16x4;
+
+constexpr int kStep = 32, kStages = 3, kThreads = 256, kWaves = kThreads / kWave;
+
+__device__ __forceinline__ int wave_number() { return __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); }
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+// A buffer of all memory from `base` (the same in every lane) on.
+__device__ __forceinline__ i32x4 whole_memory_from(const char *base)
+{
+    const uint64_t at = (uint64_t)base;
+    return i32x4{(int)(uint32_t)at, (int)((uint32_t)(at >> 32) & 0xffff), -1, 0x00020000};
+}
+// 16 bytes for each lane from base + lane_offset to lds + 16 * lane.  In assembly because the compiler puts a wait for all loads before the next read of LDS where
+// it makes these loads itself; multiply() counts them.  (No vector register is written, so none can be lost to a load on its way; m0 is not kept for anything else on this GPU.)
+__device__ __forceinline__ void load_to_lds(i32x4 from, char *lds, uint32_t lane_offset)
+{
+    const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(lane_offset), "s"(from) : "memory");
+}
+
+template <int BO>
+struct Kc {
+    static constexpr int BYTES = BO * kStep * 2, LOADS = BYTES / 1024 / kWaves;
+    const char *base;
+    uint32_t off[LOADS];
+    // row(i): the byte offset of the tile's row i from base, less than 2^32; of any readable row for one that does not exist
+    template <class Row>
+    __device__ __forceinline__ void init(const char *start, Row row)
+    {
+        base = start;
+        const int l = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int r = (wave_number() * LOADS + i) * 16 + (l >> 2);
+            off[i] = row(r) + (((l & 3) ^ (r >> 1 & 3)) << 4);
+        }
+    }
+    __device__ __forceinline__ void load(char *lds, uint64_t offset, int) const
+    {
+        const auto from = whole_memory_from(base + offset);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load_to_lds(from, lds + (wave_number() * LOADS + i) * 1024, off[i]);
+    }
+    template <int F>
+    static __device__ __forceinline__ void read(const char *lds, int first, bf16x8 (&f)[F])
+    {
+        const int l = threadIdx.x & 63;
+        const char *at = lds + (first + (l & 15)) * 64 + (((l >> 4) ^ (l >> 1 & 3)) << 4);
+#pragma unroll
+        for (int t = 0; t < F; ++t) f[t] = *reinterpret_cast<const bf16x8 *>(at + t * 1024);
+    }
+};
+
+template <int BO>
+struct Oc {
+    static constexpr int BYTES = BO * kStep * 2, LOADS = BYTES / 1024 / kWaves, ROW = BO * 2;
+    const char *base;
+    uint32_t off[LOADS], stride;
+    static __device__ __forceinline__ int move(int k) { return (k & 3) | (k >> 3 & 1) << 2; }
+    static __device__ __forceinline__ int place(int k, int c) { return k * ROW + ((((c >> 4) ^ move(k)) << 4 | (c & 15)) << 1); }
+    // which of the 32 summed rows the thread's load i is of
+    static __device__ __forceinline__ int row_of(int i) { return ((wave_number() * LOADS + i) * 1024 + (int)(threadIdx.x & 63) * 16) / ROW; }
+    // base: the first summed row; columns o0 .. o0 + BO - 1 of `width` readable ones (a multiple of 8); what is behind them is anything
+    __device__ __forceinline__ void init(const char *start, uint32_t stride_bytes, int o0, int width)
+    {
+        base = start;
+        stride = stride_bytes;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int at = (wave_number() * LOADS + i) * 1024 + (int)(threadIdx.x & 63) * 16, k = at / ROW, p = at % ROW / 16;
+            const int column = o0 + (((p >> 1) ^ move(k)) << 4 | (p & 1) << 3);
+            off[i] = k * stride + (column < width ? column * 2 : 0);
+        }
+    }
+    // left: summed rows that exist from this step on; the last one stands in for others
+    __device__ __forceinline__ void load(char *lds, uint64_t offset, int left) const
+    {
+        const auto from = whole_memory_from(base + offset);
+        if (left >= kStep) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) load_to_lds(from, lds + (wave_number() * LOADS + i) * 1024, off[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int k = row_of(i), beyond = k >= left ? k - (left - 1) : 0;
+                load_to_lds(from, lds + (wave_number() * LOADS + i) * 1024, off[i] - beyond * stride);
+            }
+        }
+    }
+    template <int F>
+    static __device__ __forceinline__ void read(const char *lds, int first, bf16x8 (&f)[F])
+    {
+        const int l = threadIdx.x & 63, i = l & 15, g = l >> 4;
+#pragma unroll
+        for (int t = 0; t < F; ++t) {
+            const char *at = lds + place(8 * g + (i >> 2), first + 16 * t + 4 * (i & 3));
+            uint2 h[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                h[u] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at + 4 * u * ROW)));
+            const uint4 both{h[0].x, h[0].y, h[1].x, h[1].y};
+            f[t] = __builtin_bit_cast(bf16x8, both);
+        }
+    }
+};
+
+// How a product's steps go through its operands: bytes from one block of 32 summed values to the next, and from one plane to the next.
+struct Walk {
+    uint32_t a_block, b_block, a_plane, b_plane;
+    int count;  // of the summed index
+};
+
+// A workgroup of 2 x 2 wavefronts, each with FA x FB fragments.
+template <int FA_, int FB_>
+struct Cut {
+    static constexpr int FA = FA_, FB = FB_, BA = 32 * FA, BB = 32 * FB;
+    static __device__ __forceinline__ int a_off() { return wave_number() / 2 * 16 * FA; }
+    static __device__ __forceinline__ int b_off() { return wave_number() % 2 * 16 * FB; }
+};
+
+// Adds the product to acc.  PLANES: 1, or 3 (six products).  also(plane of b, a's fragments) sees every step.  Ends with all of LDS free.
+template <int PLANES, class A, class B, class C, class Also>
+__device__ __forceinline__ void multiply(char *lds, const A &a, const B &b, const Walk &w, f32x4 (&acc)[C::FA][C::FB], Also also)
+{
+    constexpr int PAIRS = PLANES == 1 ? 1 : 6, STAGE = A::BYTES + B::BYTES, LOADS = A::LOADS + B::LOADS;
+    constexpr uint32_t PLANE_A = 0x010210, PLANE_B = 0x211000;  // of pair p: hexadecimal digit p
+    const int steps = (w.count + kStep - 1) / kStep * PAIRS;
+    if (steps <= 0) return;
+    int block = 0, pair = 0, to = 0;  // of the next step to load
+    const auto load = [&] {
+        char *at = lds + to * STAGE;
+        const int left = w.count - block * kStep;
+        a.load(at, (uint64_t)block * w.a_block + (PLANES > 1 ? (PLANE_A >> 4 * pair & 3) * w.a_plane : 0), left);
+        b.load(at + A::BYTES, (uint64_t)block * w.b_block + (PLANES > 1 ? (PLANE_B >> 4 * pair & 3) * w.b_plane : 0), left);
+        if (++pair == PAIRS) pair = 0, ++block;
+        if (++to == kStages) to = 0;
+    };
+    load();
+    if (steps > 1) load();
+    int at = 0, plane = 0;
+    for (int s = 0; s < steps; ++s) {
+        // this step's loads have come (all wavefronts': the barrier), and the buffer of the step before has been read by all
+        if (s + 1 < steps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (s + 2 < steps) load();
+        const char *from = lds + at * STAGE;
+        bf16x8 fa[C::FA], fb[C::FB];
+        B::read(from + A::BYTES, C::b_off(), fb);
+        A::read(from, C::a_off(), fa);
+#pragma unroll
+        for (int i = 0; i < C::FA; ++i)
+#pragma unroll
+            for (int j = 0; j < C::FB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+        also(PLANE_B >> 4 * plane & 3, fa);
+        if (++plane == PAIRS) plane = 0;
+        if (++at == kStages) at = 0;
+        asm volatile("" ::: "memory");
+    }
+    __syncthreads();
+}
+
+}  // namespace stage
+}  // namespace bgl
