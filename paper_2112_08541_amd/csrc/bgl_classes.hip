@@ -24,6 +24,7 @@ using namespace tile;
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 constexpr int64_t kPieceRows = 16384;
+constexpr int64_t kPieceClasses = 256;                 // pieces of some classes only are multiples
 constexpr int64_t kPartialBytes = (int64_t)64 << 20;   // of a forward call's tiles' maxima and sums
 constexpr int64_t kSharesFill = 512;                   // workgroups that ranges of a product's summed index are to make together
 constexpr int64_t kShareLeast = 512;                   // of the summed index, for each of them
@@ -34,6 +35,12 @@ constexpr double kLargeProducts = 5e8;                 // of a call that is laid
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 __device__ __forceinline__ float base_of(float most, float k) { return most == -INFINITY ? 0.0f : most * k; }  // (nothing there: the sum is 0)
 __device__ __forceinline__ float power_to(float v, float k, float base) { return __builtin_amdgcn_exp2f(fmaf(v, k, -base)); }
+__device__ __forceinline__ float max3(float a, float b, float c)  // (of fmaxf the compiler makes two instructions more, for signalling NaN)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
 __device__ __forceinline__ float rebase(float from, float to) { return __builtin_amdgcn_exp2f(from - to); }
 
 // The other lanes with the same lane % 16.
@@ -46,6 +53,19 @@ __device__ __forceinline__ float down_column(float v, F both)
     const auto t = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
     const uint32_t c = t[0], d = t[1];
     return both(__builtin_bit_cast(float, c), __builtin_bit_cast(float, d));
+}
+
+// Large calls keep dz in blocks of 16 rows x 32 classes (bgl_stage.h), plane by plane within a block.
+constexpr int kPad = 64;                           // values that laid out rows are padded to
+// Tiles of classes that an XCD has in hand while it goes through the rows (512 values each: 3 MB beside the rows', of its L2's 4): 4,096 x 512 x 65,536 took 298 us
+// with the rows' 4 MB read again for every tile or two of classes, 255 with 16 (the products alone, with their exponentials).
+constexpr int kClassGroup = 16;
+using StageCut = stage::Cut<6, 4>;                 // scores: 192 classes x 128 rows
+using ProductCut = stage::Cut<8, 4>;               // dW: 256 classes, dx: 256 rows; x 128 columns
+constexpr int kBlockRows = 16, kBlockClasses = 32, kBlockValues = kBlockRows * kBlockClasses;
+__device__ __forceinline__ int64_t dz_block(int64_t r, int c, int stride, int planes)
+{
+    return ((r / kBlockRows * (stride / kBlockClasses) + c / kBlockClasses) * planes) * kBlockValues + r % kBlockRows * kBlockClasses + c % kBlockClasses;
 }
 
 // A fp32 value as three of bf16 (bgl_stage.h).  One that is not finite, or rounds to infinity, is in the first alone.
@@ -70,8 +90,9 @@ struct ScoreArgs {
     bool by_rows;             // tiles of one block of rows, not of classes, follow one another on an XCD
     int class_tiles, D;
     float k, k_t;             // log2(e), and over the temperature
-    // forward: {largest, sum, sum at the temperature} of class tile t and row r at part[(t * rows + r) * 3]
-    float *part, *label_score;
+    // forward: {largest, sum} of part t of the classes and row r at part[t * rows + r], the sum at the temperature at part_t[t * rows + r]
+    float2 *part;
+    float *part_t, *label_score;
     bool two;                 // the temperature is not 1 and there is a teacher: two sums
     // backward
     const float *saved;       // n x width {log2 sum exp, the same at the temperature or +inf, the teacher's classes' scores}
@@ -188,8 +209,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_scores(ScoreArgs<T> a)
                 sum += from[1] * rebase(base_of(from[0], a.k), base_of(most, a.k));
                 if (a.two) sum_t += from[2] * rebase(base_of(from[0], a.k_t), base_of(most, a.k_t));
             }
-            float *to = a.part + (ct * a.rows + r0 + in_tile) * 3;
-            to[0] = most, to[1] = sum, to[2] = sum_t;
+            a.part[ct * a.rows + r0 + in_tile] = float2{most, sum};
+            if (a.two) a.part_t[ct * a.rows + r0 + in_tile] = sum_t;
         }
     }
 }
@@ -200,9 +221,10 @@ struct RowArgs {
     const int32_t *labels, *top_class;
     const float *top_score;
     int64_t x_stride, n, row0, rows;
-    int D, classes, top, class_tiles, saved_width;
+    int D, classes, top, class_parts, saved_width;
     float t, over_t, k, k_t, scale, teacher_scale;
-    const float *part, *label_score;
+    const float2 *part;
+    const float *part_t, *label_score;
     float *loss, *teacher_loss;
     float *saved;  // forward: null, or where lse, lse_t and the scores go; backward: those
     float *z_top;  // forward: the scores of the teacher's classes, z_stride apart for each row
@@ -211,7 +233,7 @@ struct RowArgs {
     // backward: the piece of dz
     typename T::elem *dz;
     int class0, piece_classes, dz_stride;
-    bool planes;     // dz is bf16, its planes dz_stride apart (fp32 only: bf16 has the same layout either way)
+    bool blocks;     // dz lies in blocks
     int32_t *listed;  // the row's number, or -1 without a gradient
 };
 
@@ -296,11 +318,11 @@ __global__ void __launch_bounds__(256) k_class_finish(RowArgs<T> a)
     const int64_t row = a.row0 + r;
     const int l = threadIdx.x & 63;
     float most = -INFINITY, sum = 0.0f, sum_t = 0.0f;
-    for (int ct = l; ct < a.class_tiles; ct += 64) {
-        const float *from = a.part + (ct * a.rows + r) * 3;
-        const float m = fmaxf(most, from[0]);
-        sum = sum * rebase(base_of(most, a.k), base_of(m, a.k)) + from[1] * rebase(base_of(from[0], a.k), base_of(m, a.k));
-        if (a.two) sum_t = sum_t * rebase(base_of(most, a.k_t), base_of(m, a.k_t)) + from[2] * rebase(base_of(from[0], a.k_t), base_of(m, a.k_t));
+    for (int ct = l; ct < a.class_parts; ct += 64) {
+        const float2 from = a.part[ct * a.rows + r];
+        const float m = fmaxf(most, from.x);
+        sum = sum * rebase(base_of(most, a.k), base_of(m, a.k)) + from.y * rebase(base_of(from.x, a.k), base_of(m, a.k));
+        if (a.two) sum_t = sum_t * rebase(base_of(most, a.k_t), base_of(m, a.k_t)) + a.part_t[ct * a.rows + r] * rebase(base_of(from.x, a.k_t), base_of(m, a.k_t));
         most = m;
     }
     const float m = max_across<64>(most), base = base_of(m, a.k), base_t = a.two ? base_of(m, a.k_t) : base;
@@ -370,12 +392,13 @@ __global__ void __launch_bounds__(256) k_class_fix(RowArgs<T> a)
         float d = 0.0f;
         if (label >= 0 && a.scale != 0.0f) d = a.scale * (power_to(z, a.k, lse) - (c == label ? 1.0f : 0.0f));
         if (a.teacher_scale != 0.0f) d = fmaf(a.teacher_scale, power_to(z, a.k_t, lse_t) - p, d);
-        if (T::PER == 1 && a.planes) {
-            uint16_t e[3];
-            split(d, e);
-            uint16_t *to = reinterpret_cast<uint16_t *>(a.dz) + r * 3 * a.dz_stride + (c - a.class0);
+        if (a.blocks) {
+            constexpr int PLANES = T::PER == 1 ? 3 : 1;
+            uint16_t e[3] = {}, *to = reinterpret_cast<uint16_t *>(a.dz) + dz_block(r, c - a.class0, a.dz_stride, PLANES);
+            if constexpr (PLANES == 1) e[0] = BF16::put(d);
+            else split(d, e);
 #pragma unroll
-            for (int p = 0; p < 3; ++p) to[p * (int64_t)a.dz_stride] = e[p];
+            for (int p = 0; p < PLANES; ++p) to[p * kBlockValues] = e[p];
         } else {
             a.dz[r * a.dz_stride + (c - a.class0)] = T::put(d);
         }
@@ -564,7 +587,7 @@ __global__ void __launch_bounds__(256) k_class_lay(LayArgs<T> a)
     for (int p = 0; p < PLANES; ++p) __builtin_memcpy(a.to + (row * PLANES + p) * a.padded + d, e[p], 16);
 }
 
-// k_class_scores from laid out operands: 256 classes x 128 rows.
+// k_class_scores from laid out operands: 192 classes x 128 rows.
 template <class T>
 struct StageScoreArgs {
     ScoreArgs<T> s;
@@ -576,15 +599,15 @@ struct StageScoreArgs {
 template <class T, bool DZ>
 __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(StageScoreArgs<T> q)
 {
-    using C = stage::Cut<8, 4>;
-    using A = stage::Kc<C::BA>;
-    using B = stage::Kc<C::BB>;
+    using C = StageCut;
+    using A = stage::Kc<C::BA, kPad>;
+    using B = stage::Kc<C::BB, kPad>;
     constexpr int PLANES = T::PER == 1 ? 3 : 1;
-    __shared__ __attribute__((aligned(1024))) char lds[stage::kStages * (A::BYTES + B::BYTES)];
+    __shared__ __attribute__((aligned(1024))) char lds[stage::lds_bytes<A, B>()];
     const ScoreArgs<T> &a = q.s;
     int64_t ct, rt;
     int fast;
-    if (!tile_of(blockIdx.x, a.by_rows ? a.row_tiles : a.class_tiles, (int)(a.by_rows ? a.class_tiles : a.row_tiles), a.by_rows ? rt : ct, fast)) return;
+    if (!stage::tile_of(blockIdx.x, (uint32_t)(a.by_rows ? a.row_tiles : a.class_tiles), (uint32_t)(a.by_rows ? a.class_tiles : a.row_tiles), a.by_rows ? 1 : kClassGroup, a.by_rows ? rt : ct, fast)) return;
     (a.by_rows ? ct : rt) = fast;
     const int c0 = a.class0 + (int)ct * C::BA, last = a.classes - 1, l = threadIdx.x & 63;
     const int64_t r0 = rt * C::BB;
@@ -592,18 +615,43 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
     B rows;
     weight.init(q.w + c0 * q.w_bytes, [&](int i) { return (uint32_t)((c0 + i < last ? i : last - c0) * q.w_bytes); });
     rows.init(q.x + (a.row0 + r0) * q.x_bytes, [&](int i) { return (uint32_t)((r0 + i < a.rows ? i : (int)(a.rows - 1 - r0)) * q.x_bytes); });
-    const int in_tile = C::a_off() + 4 * (l >> 4), first = c0 + in_tile;
-    f32x4 acc[C::FA][C::FB];
-#pragma unroll
-    for (int i = 0; i < C::FA; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int c = first + 16 * i + j;
-            const float b = a.bias ? T::get(a.bias[c < last ? c : last]) : 0.0f;
-#pragma unroll
-            for (int t = 0; t < C::FB; ++t) acc[i][t][j] = b;
+    // what the tile's classes and rows have of their own: a value for each thread, on its way during the products
+    static_assert(C::BA <= stage::kThreads && C::BB <= stage::kThreads, "");
+    float my_bias = 0.0f, my_lse = INFINITY, my_lse_t = INFINITY;
+    int my_label = -1;
+    if (a.bias && threadIdx.x < C::BA) my_bias = T::get(a.bias[c0 + (int)threadIdx.x < last ? c0 + (int)threadIdx.x : last]);
+    if (threadIdx.x < C::BB && r0 + threadIdx.x < a.rows) {
+        const int64_t row = a.row0 + r0 + threadIdx.x;
+        if (a.labels) my_label = a.labels[row];
+        if constexpr (DZ) {
+            if (a.scale != 0.0f) my_lse = a.saved[row * a.saved_width];
+            if (a.teacher_scale != 0.0f) my_lse_t = a.saved[row * a.saved_width + 1];
         }
-    stage::multiply<PLANES, A, B, C>(lds, weight, rows, stage::Walk{64, 64, q.w_plane, q.x_plane, a.D}, acc, [](int, const auto &) {});
+    }
+    f32x4 acc[C::FA][C::FB] = {};
+    stage::multiply<PLANES, A, B, C>(lds, weight, rows, stage::Walk{2 * kPad, 2 * kPad, q.w_plane, q.x_plane, a.D, 0}, acc, [](int, const auto &) {});
+
+    if ((uint32_t)my_label >= (uint32_t)a.all_classes) my_label = -1, my_lse = INFINITY;
+    struct Own {
+        float bias[C::BA], lse[C::BB], lse_t[C::BB];
+        int label[C::BB];
+    };
+    Own &own = *reinterpret_cast<Own *>(lds);
+    if (threadIdx.x < C::BA) own.bias[threadIdx.x] = my_bias;
+    if (threadIdx.x < C::BB) {
+        own.label[threadIdx.x] = my_label;
+        if constexpr (DZ) own.lse[threadIdx.x] = my_lse, own.lse_t[threadIdx.x] = my_lse_t;
+    }
+    __syncthreads();
+    const int in_tile = C::a_off() + 4 * (l >> 4), first = c0 + in_tile;
+#pragma unroll
+    for (int i = 0; i < C::FA; ++i) {
+        const f32x4 b = *reinterpret_cast<const f32x4 *>(own.bias + in_tile + 16 * i);
+#pragma unroll
+        for (int t = 0; t < C::FB; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][t][j] += b[j];
+    }
     if (c0 + C::BA > a.classes) {
 #pragma unroll
         for (int i = 0; i < C::FA; ++i)
@@ -614,22 +662,26 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
                     for (int t = 0; t < C::FB; ++t) acc[i][t][j] = -INFINITY;
                 }
     }
-    float *meet = reinterpret_cast<float *>(lds);  // forward: largest, sum, sum at the temperature of 2 x 128 halves of rows
+    const bool teachers = DZ && a.teacher_scale != 0.0f, labels = a.labels != nullptr && (!DZ || a.scale != 0.0f);
 #pragma unroll
     for (int t = 0; t < C::FB; ++t) {
         const int b = C::b_off() + 16 * t + (l & 15);
         const int64_t r = r0 + b;
-        const bool live = r < a.rows;
-        const int64_t row = a.row0 + (live ? r : a.rows - 1);
-        int label = a.labels && live ? a.labels[row] : -1;
-        if ((uint32_t)label >= (uint32_t)a.all_classes) label = -1;
         // the label's place among the lane's values; few tiles have one, and only these look for it
-        const int at = label - first;
+        const int at = labels ? own.label[b] - first : -1;
         const bool mine = at >= 0 && at < 16 * C::FA && (at & 15) < 4, any = __ballot(mine) != 0;
+        const auto own_score = [&](int t) {
+            float v = 0.0f;
+#pragma unroll
+            for (int i = 0; i < C::FA; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v = at == 16 * i + j ? acc[i][t][j] : v;
+            return v;
+        };
         if constexpr (!DZ) {
             float most = -INFINITY, sum = 0.0f, sum_t = 0.0f;
 #pragma unroll
-            for (int i = 0; i < C::FA; ++i) most = fmaxf(most, fmaxf(fmaxf(acc[i][t][0], acc[i][t][1]), fmaxf(acc[i][t][2], acc[i][t][3])));
+            for (int i = 0; i < C::FA; ++i) most = max3(max3(most, acc[i][t][0], acc[i][t][1]), acc[i][t][2], acc[i][t][3]);
             most = down_column(most, [](float p, float q) { return fmaxf(p, q); });
             const float base = base_of(most, a.k), base_t = base_of(most, a.k_t);
 #pragma unroll
@@ -643,22 +695,18 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
                     for (int j = 0; j < 4; ++j) sum_t += power_to(acc[i][t][j], a.k_t, base_t);
             }
             if (any) {
-#pragma unroll
-                for (int i = 0; i < C::FA; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (mine && at == 16 * i + j) a.label_score[row] = acc[i][t][j];
+                const float v = own_score(t);
+                if (mine && r < a.rows) a.label_score[a.row0 + r] = v;
             }
             sum = down_column(sum, [](float p, float q) { return p + q; });
             if (a.two) sum_t = down_column(sum_t, [](float p, float q) { return p + q; });
-            float *to = meet + (C::a_off() / (16 * C::FA) * C::BB + b) * 3;
-            if (l < 16) to[0] = most, to[1] = sum, to[2] = sum_t;
+            if (l < 16 && r < a.rows) {
+                const int64_t at = (ct * 2 + C::a_off() / (16 * C::FA)) * a.rows + r;
+                a.part[at] = float2{most, sum};
+                if (a.two) a.part_t[at] = sum_t;
+            }
         } else {
-            const float *kept = a.saved + row * a.saved_width;
-            const bool by_label = label >= 0 && a.scale != 0.0f, by_teacher = live && kept[1] != INFINITY && a.teacher_scale != 0.0f;
-            const float lse = by_label ? kept[0] : INFINITY, lse_t = by_teacher ? kept[1] : INFINITY;
-            const bool teachers = a.teacher_scale != 0.0f;
-            uint16_t *to = reinterpret_cast<uint16_t *>(a.dz) + r * PLANES * a.dz_stride + (first - a.class0);
+            const float lse = own.lse[b], lse_t = own.lse_t[b];
 #pragma unroll
             for (int i = 0; i < C::FA; ++i) {
                 float d[4];
@@ -668,16 +716,12 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
 #pragma unroll
                     for (int j = 0; j < 4; ++j) d[j] = fmaf(a.teacher_scale, power_to(acc[i][t][j], a.k_t, lse_t), d[j]);
                 }
-                if (any) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (mine && at == 16 * i + j) d[j] -= a.scale;
-                }
+                uint16_t *to = reinterpret_cast<uint16_t *>(a.dz) + dz_block(r, first - a.class0 + 16 * i, a.dz_stride, PLANES);
                 if constexpr (PLANES == 1) {
                     uint16_t e[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) e[j] = BF16::put(d[j]);
-                    __builtin_memcpy(to + 16 * i, e, sizeof(e));
+                    __builtin_memcpy(to, e, sizeof(e));
                 } else {
                     uint16_t e[3][4];
 #pragma unroll
@@ -688,32 +732,34 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
                         for (int p = 0; p < 3; ++p) e[p][j] = three[p];
                     }
 #pragma unroll
-                    for (int p = 0; p < 3; ++p) __builtin_memcpy(to + p * (int64_t)a.dz_stride + 16 * i, e[p], sizeof(e[p]));
+                    for (int p = 0; p < 3; ++p) __builtin_memcpy(to + p * kBlockValues, e[p], sizeof(e[p]));
+                }
+            }
+            if (any) {  // the label's class again, with the label
+                const float v = own_score(t);
+                float d = a.scale * (power_to(v, a.k, lse) - 1.0f);
+                if (teachers) d = fmaf(a.teacher_scale, power_to(v, a.k_t, lse_t), d);
+                uint16_t e[3], *to = reinterpret_cast<uint16_t *>(a.dz) + dz_block(r, first - a.class0 + (mine ? at : 0), a.dz_stride, PLANES);
+                if constexpr (PLANES == 1) e[0] = BF16::put(d);
+                else split(d, e);
+                if (mine) {
+#pragma unroll
+                    for (int p = 0; p < PLANES; ++p) to[p * kBlockValues] = e[p];
                 }
             }
         }
-    }
-    if constexpr (!DZ) {
-        __syncthreads();
-        const int b = threadIdx.x;
-        if (b >= C::BB || r0 + b >= a.rows) return;
-        const float *one = meet + b * 3, *two = meet + (C::BB + b) * 3;
-        const float most = fmaxf(one[0], two[0]), base = base_of(most, a.k), base_t = base_of(most, a.k_t);
-        float *to = a.part + (ct * a.rows + r0 + b) * 3;
-        to[0] = most;
-        to[1] = one[1] * rebase(base_of(one[0], a.k), base) + two[1] * rebase(base_of(two[0], a.k), base);
-        to[2] = a.two ? one[2] * rebase(base_of(one[0], a.k_t), base_t) + two[2] * rebase(base_of(two[0], a.k_t), base_t) : 0.0f;
     }
 }
 
 // k_class_product from laid out operands: 256 x 128.  OC: dW, else dx.
 template <class T>
 struct StagePieceArgs {
-    const char *a, *b;                 // dz; W or x
-    int64_t a_bytes, b_bytes;          // rows
-    uint32_t a_plane, b_plane;
+    const char *a, *b;                 // dz, in blocks; W or x
+    int64_t b_bytes;                   // rows
+    uint32_t b_plane;
     int64_t M, K;                      // (dW: rows up to a multiple of 32)
-    int N, a_width, b_width;           // columns of the result, of dz and of the other that can be read
+    int N, a_stride, b_width;          // columns of the result, of dz, and of the other that can be read
+    int a_rows;                        // of dz, a multiple of 16
     int64_t row_tiles;
     int col_tiles, shares;
     int64_t per_share;                 // a multiple of 32
@@ -727,11 +773,11 @@ struct StagePieceArgs {
 template <class T, bool OC>
 __global__ void __launch_bounds__(stage::kThreads, 2) k_class_product_stage(StagePieceArgs<T> a)
 {
-    using C = stage::Cut<8, 4>;
-    using A = std::conditional_t<OC, stage::Oc<C::BA>, stage::Kc<C::BA>>;
+    using C = ProductCut;
+    using A = std::conditional_t<OC, stage::OcBlocks<C::BA>, stage::Kc<C::BA, kBlockClasses>>;
     using B = stage::Oc<C::BB>;
     constexpr int PLANES = T::PER == 1 ? 3 : 1;
-    __shared__ __attribute__((aligned(1024))) char lds[stage::kStages * (A::BYTES + B::BYTES)];
+    __shared__ __attribute__((aligned(1024))) char lds[stage::lds_bytes<A, B>()];
     const int share = blockIdx.x % a.shares;
     int64_t rt;
     int ct;
@@ -740,19 +786,23 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_product_stage(Stag
     const int n0 = ct * C::BB, K = (int)(a.K - k0 < a.per_share ? a.K - k0 : a.per_share);
     A left;
     B right;
-    uint32_t a_block;
+    // dz's blocks: 16 rows of it, one block
+    constexpr uint32_t BLOCK = kBlockValues * 2 * PLANES;
+    const uint32_t down = a.a_stride / kBlockClasses * BLOCK;
     if constexpr (OC) {
-        left.init(a.a + k0 * a.a_bytes, (uint32_t)a.a_bytes, (int)m0, a.a_width);
-        a_block = (uint32_t)(stage::kStep * a.a_bytes);
+        left.init(a.a + k0 / kBlockRows * down, down, BLOCK, (int)(m0 / kBlockClasses), a.a_stride / kBlockClasses);
     } else {
-        left.init(a.a + m0 * a.a_bytes + k0 * 2, [&](int i) { return (uint32_t)((m0 + i < a.M ? i : (int)(a.M - 1 - m0)) * a.a_bytes); });
-        a_block = stage::kStep * 2;
+        left.init(a.a + m0 / kBlockRows * down + k0 / kBlockClasses * BLOCK, [&](int i) {
+            const int most = (int)((a.a_rows - m0) / kBlockRows) - 1;
+            return (uint32_t)((i / kBlockRows < most ? i / kBlockRows : most) * down + i % kBlockRows * kBlockClasses * 2);
+        });
     }
+    const uint32_t a_block = OC ? 2 * down : BLOCK;
     right.init(a.b + k0 * a.b_bytes, (uint32_t)a.b_bytes, n0, a.b_width);
     f32x4 acc[C::FA][C::FB] = {};
     float sums[C::FA] = {};
     const bool summing = OC && (a.sums || a.sum_slots) && n0 == 0 && C::b_off() == 0;
-    stage::multiply<PLANES, A, B, C>(lds, left, right, stage::Walk{a_block, (uint32_t)(stage::kStep * a.b_bytes), a.a_plane, a.b_plane, K}, acc, [&](int b_plane, const auto &f) {
+    stage::multiply<PLANES, A, B, C>(lds, left, right, stage::Walk{a_block, (uint32_t)(A::STEP * a.b_bytes), kBlockValues * 2, a.b_plane, K, 0}, acc, [&](int b_plane, const auto &f) {
         if (summing && b_plane == 0) {
 #pragma unroll
             for (int t = 0; t < C::FA; ++t) {
@@ -806,7 +856,7 @@ using Low = Cut<4, 1, 2, 1>;     // 128 x 16
 struct Plan {
     // forward
     int64_t pass_rows;
-    int class_tiles;
+    int class_parts;
     size_t part_bytes, label_bytes, top_bytes, forward_bytes;
     // backward
     int64_t piece_rows, row_pieces, dz_stride;
@@ -818,22 +868,22 @@ struct Plan {
     size_t x_bytes, w_bytes, back_x_bytes;
 };
 
-// How a call is cut up.  Small ones: tiles of 128 x 128 straight from the operands.  Large ones: 256 x 128 of operands laid out for bgl_stage.h (bf16 whose rows
+// How a call is cut up.  Small ones: tiles of 128 x 128 straight from the operands.  Large ones: larger tiles of operands laid out for bgl_stage.h (bf16 whose rows
 // are whole steps are laid out already).
 struct Scheme {
     bool large;
-    int a_rows;                 // of a tile: classes of the scores; rows of dx, classes of dW
+    int score_classes, product_rows;  // of a tile
     int64_t values, round_classes, round_rows;
     int dz_value_bytes, planes;
 };
 Scheme scheme_of(const bgl_class_loss_t *l, bool large)
 {
     const bool f32 = l->dtype == BGL_F32;
-    if (large) return Scheme{true, 256, (int64_t)1 << 27, 256, 128, f32 ? 6 : 2, f32 ? 3 : 1};
-    return Scheme{false, 128, (int64_t)1 << 25, 8, 1, f32 ? 4 : 2, 1};  // (pieces of 4 classes are stored, and 16 bytes of bf16 read)
+    if (large) return Scheme{true, StageCut::BA, ProductCut::BA, ((int64_t)1 << 27) + ((int64_t)1 << 23), StageCut::BA, StageCut::BB, f32 ? 6 : 2, f32 ? 3 : 1};
+    return Scheme{false, 128, 128, (int64_t)1 << 25, 8, 1, f32 ? 4 : 2, 1};  // (pieces of 4 classes are stored, and 16 bytes of bf16 read)
 }
 bool large_call(const bgl_class_loss_t *l, int64_t n) { return n >= 256 && l->classes >= 128 && (double)n * l->classes * l->in_dim >= kLargeProducts; }
-bool laid_out(const bgl_class_loss_t *l) { return l->dtype == BGL_BF16 && l->in_dim % stage::kStep == 0; }
+bool laid_out(const bgl_class_loss_t *l) { return l->dtype == BGL_BF16 && l->in_dim % kPad == 0; }
 
 int shares_for(int64_t tiles, int64_t summed)
 {
@@ -844,16 +894,16 @@ int shares_for(int64_t tiles, int64_t summed)
 Plan plan_of(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
 {
     Plan p{};
-    p.class_tiles = (int)ceil_div(l->classes, s.a_rows);
-    p.pass_rows = kPartialBytes / (12 * (int64_t)p.class_tiles);
+    p.class_parts = (int)ceil_div(l->classes, s.score_classes) * (s.large ? 2 : 1);
+    p.pass_rows = kPartialBytes / (12 * (int64_t)p.class_parts);
     p.pass_rows = p.pass_rows < 1024 ? 1024 : p.pass_rows / 128 * 128;
     if (p.pass_rows > n) p.pass_rows = n;
-    p.part_bytes = round_up((size_t)p.pass_rows * p.class_tiles * 12, 256);
+    p.part_bytes = round_up((size_t)p.pass_rows * p.class_parts * 12, 256);
     p.label_bytes = round_up((size_t)n * 4, 256);
     p.top_bytes = round_up((size_t)n * l->top * 4, 256);
     if (s.large) {
-        p.padded = (int)round_up(l->in_dim, stage::kStep);
-        p.back_x_bytes = round_up((size_t)round_up(n, stage::kStep) * p.padded * 2 * s.planes, 256);
+        p.padded = (int)round_up(l->in_dim, kPad);
+        p.back_x_bytes = round_up((size_t)round_up(n, 32) * p.padded * 2 * s.planes, 256);
         if (!laid_out(l)) p.x_bytes = p.back_x_bytes, p.w_bytes = round_up((size_t)l->classes * p.padded * 2 * s.planes, 256);
     }
     p.forward_bytes = p.part_bytes + p.label_bytes + p.top_bytes + p.x_bytes + p.w_bytes;
@@ -868,7 +918,10 @@ Plan plan_of(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
             if (p.piece_rows > n) p.piece_rows = n;
         } else {
             if (n > kPieceRows) p.piece_rows = kPieceRows;
-            const int64_t fit = (int64_t)round_up((size_t)ceil_div(stride, ceil_div(p.piece_rows * stride, s.values)), 256);
+            // whole rounds of dW's workgroups, if one fits (of 4,096 x 512: two pieces of 129 x 4 tiles took a third longer than two of 128 x 4)
+            const int64_t round = kSharesFill / ceil_div(l->in_dim, 128) * s.product_rows, most = s.values / p.piece_rows;
+            int64_t fit = (int64_t)round_up((size_t)ceil_div(stride, ceil_div(p.piece_rows * stride, s.values)), kPieceClasses);
+            if (round > 0 && most >= round) fit = most / round * round;
             if (fit < l->classes) p.piece_classes = (int)fit;
         }
     }
@@ -878,9 +931,9 @@ Plan plan_of(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
     p.dz_bytes = round_up(round_up(p.piece_rows, s.round_rows) * p.dz_stride * s.dz_value_bytes, 256);
     p.list_bytes = s.large ? 0 : round_up((size_t)n * 4, 256);
     const int64_t cols = ceil_div(l->in_dim, 128);
-    p.dx_shares = p.class_pieces > 1 && p.row_pieces > 1 ? 1 : shares_for(ceil_div(p.piece_rows, s.a_rows) * cols, p.piece_classes);
+    p.dx_shares = p.class_pieces > 1 && p.row_pieces > 1 ? 1 : shares_for(ceil_div(p.piece_rows, s.product_rows) * cols, p.piece_classes);
     p.dx_per = round_up((size_t)ceil_div(p.piece_classes, p.dx_shares), 64);
-    p.dw_shares = shares_for(ceil_div(p.piece_classes, s.a_rows) * cols, p.piece_rows);
+    p.dw_shares = shares_for(ceil_div(p.piece_classes, s.product_rows) * cols, p.piece_rows);
     p.dw_per = round_up((size_t)ceil_div(p.piece_rows, p.dw_shares), 64);
     p.dx_bytes = p.dx_shares > 1 || p.class_pieces > 1 ? round_up((size_t)p.dx_shares * (p.class_pieces > 1 ? n : p.piece_rows) * l->in_dim * 4, 256) : 0;
     p.dw_bytes = p.dw_shares > 1 || p.row_pieces > 1 ? round_up((size_t)p.dw_shares * p.piece_classes * l->in_dim * 4, 256) : 0;
@@ -892,16 +945,16 @@ Plan plan_of(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
 // What the backward calls of up to n rows need: no call of fewer rows needs more.  (Shares are less than kSharesFill tiles in all.)
 size_t backward_room(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
 {
-    const int64_t V = l->classes, D = l->in_dim, stride = round_up(V, s.round_classes), shared = kSharesFill * s.a_rows;
+    const int64_t V = l->classes, D = l->in_dim, stride = round_up(V, s.round_classes), shared = kSharesFill * s.product_rows;
     const bool many = V > kPieceRows;
     const auto least = [](int64_t a, int64_t b) { return a < b ? a : b; };
     const auto most = [](int64_t a, int64_t b) { return a > b ? a : b; };
-    const int64_t over = (many ? 256 * least(n, kPieceRows) : 128 * stride) + 128 * least(stride, s.values);
+    const int64_t over = (many ? kPieceClasses * least(n, kPieceRows) : 128 * stride) + 128 * least(stride, s.values);
     const Plan p = plan_of(l, n, s);
     size_t bytes = round_up((size_t)least(round_up(n, 128) * stride, s.values + over) * s.dz_value_bytes, 256) + round_up((size_t)n * 4, 256) + p.back_x_bytes + p.w_bytes;
     if (V >= 2 * kShareLeast) bytes += round_up((size_t)most(many ? n : 0, least(shared, n * (V / kShareLeast))) * D * 4, 256);
     const int64_t shares = n >= 2 * kShareLeast ? least(shared, V * (n / kShareLeast)) : 0;
-    const int64_t pieces = many ? (n > kPieceRows ? s.values / kPieceRows + 256 : 0) : n * stride > s.values ? V : 0;
+    const int64_t pieces = many ? (n > kPieceRows ? s.values / kPieceRows + kPieceClasses : 0) : n * stride > s.values ? V : 0;
     bytes += round_up((size_t)most(shares, pieces) * D * 4, 256) + round_up((size_t)most(shares, pieces) * 4, 256);
     return bytes > p.backward_bytes ? bytes : p.backward_bytes;
 }
@@ -960,8 +1013,8 @@ template <class T, bool DZ>
 void launch_scores_stage(StageScoreArgs<T> &q, hipStream_t st)
 {
     ScoreArgs<T> &s = q.s;
-    s.class_tiles = (int)ceil_div(s.classes - s.class0, 256);
-    s.row_tiles = ceil_div(s.rows, 128);
+    s.class_tiles = (int)ceil_div(s.classes - s.class0, StageCut::BA);
+    s.row_tiles = ceil_div(s.rows, StageCut::BB);
     s.by_rows = s.row_tiles > s.class_tiles;
     const int64_t tiles = s.by_rows ? tile_count(s.row_tiles, s.class_tiles) : tile_count(s.class_tiles, (int)s.row_tiles);
     k_class_scores_stage<T, DZ><<<dim3((unsigned)tiles), dim3(stage::kThreads), 0, st>>>(q);
@@ -995,7 +1048,7 @@ StageScoreArgs<T> stage_args(const Call &c, const Plan &p, const Scheme &h, cons
     q.x_bytes = q.w_bytes = (int64_t)p.padded * h.planes * 2, q.x_plane = q.w_plane = p.padded * 2;
     if (p.w_bytes) launch_lay<T>(s.w, s.D, s.classes, s.classes, s.D, p.padded, w, nullptr, c.stream), q.w = w;
     else q.w = (const char *)s.w;
-    if (p.w_bytes || select) launch_lay<T>(s.x, s.x_stride, c.n, round_up(c.n, stage::kStep), s.D, p.padded, x, select, c.stream), q.x = x;
+    if (p.w_bytes || select) launch_lay<T>(s.x, s.x_stride, c.n, round_up(c.n, 32), s.D, p.padded, x, select, c.stream), q.x = x;
     else q.x = (const char *)s.x, q.x_bytes = s.x_stride * 2;
     return q;
 }
@@ -1008,9 +1061,9 @@ int forward(const Call &c, float *loss, float *teacher_loss, float *saved)
     ScoreArgs<T> s = score_args<T>(c);
     RowArgs<T> r = row_args<T>(c);
     char *ws = c.workspace;
-    s.part = (float *)ws, s.label_score = (float *)(ws += p.part_bytes);
+    s.part = (float2 *)ws, s.part_t = (float *)(s.part + p.pass_rows * p.class_parts), s.label_score = (float *)(ws += p.part_bytes);
     char *top = ws += p.label_bytes, *x = ws += p.top_bytes, *w = ws += p.x_bytes;
-    r.part = s.part, r.label_score = s.label_score, r.class_tiles = p.class_tiles;
+    r.part = s.part, r.part_t = s.part_t, r.label_score = s.label_score, r.class_parts = p.class_parts;
     r.z_top = saved ? saved + 2 : (float *)top, r.z_stride = saved ? r.saved_width : r.top;
     r.loss = loss, r.teacher_loss = teacher_loss, r.saved = saved;
     StageScoreArgs<T> q{};
@@ -1037,7 +1090,7 @@ void launch_product(PieceArgs<T> &a, hipStream_t st)
 template <class T, bool OC>
 void launch_product_stage(StagePieceArgs<T> &a, hipStream_t st)
 {
-    a.row_tiles = ceil_div(a.M, 256), a.col_tiles = (int)ceil_div(a.N, 128);
+    a.row_tiles = ceil_div(a.M, ProductCut::BA), a.col_tiles = (int)ceil_div(a.N, ProductCut::BB);
     k_class_product_stage<T, OC><<<dim3((unsigned)(tile_count(a.row_tiles, a.col_tiles) * a.shares)), dim3(stage::kThreads), 0, st>>>(a);
 }
 template <class T>
@@ -1071,10 +1124,9 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
     s.saved = saved, s.dz = dz, s.dz_stride = (int)p.dz_stride;
     s.scale = r.scale = c.labels ? scale : 0.0f;
     s.teacher_scale = r.teacher_scale = c.top_class ? teacher_scale * c.l->temperature : 0.0f;
-    r.saved = const_cast<float *>(saved), r.dz = dz, r.dz_stride = (int)p.dz_stride, r.planes = h.large;
+    r.saved = const_cast<float *>(saved), r.dz = dz, r.dz_stride = (int)p.dz_stride, r.blocks = h.large;
     StageScoreArgs<T> q{};
     if (h.large) q = stage_args<T>(c, p, h, s, x_laid, w_laid, &r);
-    const int64_t dz_row = p.dz_stride * h.planes * 2;
     for (int cp = 0; cp < p.class_pieces; ++cp) {
         const int class0 = cp * p.piece_classes, classes = V - class0 < p.piece_classes ? V - class0 : p.piece_classes;
         for (int64_t rp = 0; rp < p.row_pieces; ++rp) {
@@ -1093,8 +1145,8 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
             const int64_t slot_rows = p.class_pieces > 1 ? c.n : rows;
             if (dx && h.large) {
                 StagePieceArgs<T> a{};
-                a.a = (const char *)dz, a.a_bytes = dz_row, a.a_plane = p.dz_stride * 2, a.b = q.w + class0 * q.w_bytes, a.b_bytes = q.w_bytes, a.b_plane = q.w_plane;
-                a.M = rows, a.K = classes, a.N = D, a.a_width = (int)p.dz_stride, a.b_width = p.padded, a.shares = p.dx_shares, a.per_share = p.dx_per;
+                a.a = (const char *)dz, a.a_rows = (int)round_up(rows, StageCut::BB), a.b = q.w + class0 * q.w_bytes, a.b_bytes = q.w_bytes, a.b_plane = q.w_plane;
+                a.M = rows, a.K = classes, a.N = D, a.a_stride = (int)p.dz_stride, a.b_width = p.padded, a.shares = p.dx_shares, a.per_share = p.dx_per;
                 a.out = dx + row0 * dx_stride, a.out_stride = dx_stride, a.slots = slots, a.slot_rows = slot_rows, a.add = cp > 0;
                 launch_product_stage<T, false>(a, c.stream);
             } else if (dx) {
@@ -1107,20 +1159,20 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
             if (slots && dx && p.class_pieces == 1) launch_reduce<T>(slots, rows * D, rows, D, p.dx_shares, dx + row0 * dx_stride, dx_stride, c.stream);
             if (!dweight) continue;
             const auto fill = [&](auto &a) {
-                a.M = classes, a.N = D, a.a_width = (int)p.dz_stride, a.shares = p.dw_shares, a.per_share = p.dw_per;
+                a.M = classes, a.N = D, a.shares = p.dw_shares, a.per_share = p.dw_per;
                 a.out = dweight + (int64_t)class0 * D, a.out_stride = D, a.sums = dbias ? dbias + class0 : nullptr;
                 if (p.dw_bytes) a.slots = dw_slots, a.sum_slots = dbias ? db_slots : nullptr, a.slot_rows = p.piece_classes, a.add = rp > 0;
             };
             if (h.large) {
                 StagePieceArgs<T> a{};
                 fill(a);
-                a.a = (const char *)dz, a.a_bytes = dz_row, a.a_plane = p.dz_stride * 2, a.b = q.x + row0 * q.x_bytes, a.b_bytes = q.x_bytes, a.b_plane = q.x_plane;
-                a.b_width = p.padded, a.K = round_up(rows, stage::kStep);  // (rows of zeros in both)
+                a.a = (const char *)dz, a.a_rows = (int)round_up(rows, StageCut::BB), a.b = q.x + row0 * q.x_bytes, a.b_bytes = q.x_bytes, a.b_plane = q.x_plane;
+                a.a_stride = (int)p.dz_stride, a.b_width = p.padded, a.K = round_up(rows, 32);  // (rows of zeros in both)
                 launch_product_stage<T, true>(a, c.stream);
             } else {
                 PieceArgs<T> a{};
                 fill(a);
-                a.a = dz, a.a_stride = p.dz_stride, a.b = s.x + row0 * c.x_stride, a.b_stride = c.x_stride, a.list = listed + row0, a.K = rows;
+                a.a = dz, a.a_stride = p.dz_stride, a.b = s.x + row0 * c.x_stride, a.b_stride = c.x_stride, a.list = listed + row0, a.K = rows, a.a_width = (int)p.dz_stride;
                 launch_product<T, true>(a, c.stream);
             }
         }

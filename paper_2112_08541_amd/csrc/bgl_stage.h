@@ -1,19 +1,24 @@
-// Device templates for large products of bf16 matrices on the matrix units (gfx950): tiles go from global memory straight into LDS, three stages of
-// 32 summed values deep, and from there as fragments of 16 x 16 x 32 MFMA instructions.
+// Device templates for large products of bf16 matrices on the matrix units (gfx950): tiles go from global memory straight into LDS, in stages of 32 or 64
+// summed values, and from there as fragments of 16 x 16 x 32 MFMA instructions.
 //
-// Against the tiles of bgl_tile.h, which pass through registers: the loads take none, so that a wavefront keeps 128 x 64 sums (a fragment read from LDS meets
-// 8 or 4 others instead of 4) and two workgroups still share a CU, one's epilogue beside the other's products; and a step waits for loads that were asked for
-// two steps before, behind one barrier.  In return rows are read in whole 16-byte pieces: they begin on multiples of 16 bytes and are padded with zeros to
-// whole steps.
+// Against the tiles of bgl_tile.h, which pass through registers: the loads take none, so that a wavefront keeps up to 128 x 64 sums (a fragment read from LDS
+// meets 8 or 4 others instead of 4) and two workgroups still share a CU, one's epilogue beside the other's products; and a stage waits for loads that were asked
+// for a stage or two before, behind one barrier.  In return rows are read in whole 16-byte pieces: they begin on multiples of 16 bytes and are padded with
+// zeros to whole stages.
+//
+// What a load asks the L2 for are lines of 128 bytes: rows read 64 bytes at a time (stages of 32) took twice the requests and a third more time than
+// rows read 128 bytes at a time.  So rows that are given are read in stages of 64, and what is written for these products alone lies in blocks of
+// 16 rows x 32 values (1,024 bytes that one load of a wavefront takes, whichever index is summed).
 //
 // A fp32 value is three bf16 (its first 8 bits, the next 8 of what is left, the last): all 24 bits as long as the value is above 2^-110.  A product of two is
-// the six products of parts that count, what is left out is below 2^-23 of it.  Rows hold the three parts one after the other ("planes").
+// the six products of parts that count, what is left out is below 2^-23 of it.  The parts lie one after the other ("planes"): of a row, or of a block.
 //
-// A tile of an operand in LDS, in the two orders an operand can have:
-//   summed index contiguous (Kc)   BO rows of 64 bytes, 16-byte piece p of row r at p ^ (r / 2 & 3): 8 lanes that read 16 bytes each, from rows in a row, meet
-//                                  all banks
-//   kept index contiguous (Oc)     32 rows of BO values, blocks of 16 values moved about within a row (as in bgl_tile.h); fragments by the LDS read that
-//                                  transposes 4 x 16 values among 16 lanes
+// A tile of an operand in LDS:
+//   Kc        the summed index contiguous: BO rows of 2 STEP bytes, 16-byte piece p of row r at p ^ (r & 7) (64) or p ^ (r / 2 & 3) (32), so that 8 lanes that
+//             read 16 bytes each, from rows in a row, meet all banks
+//   Oc        the kept index contiguous: 32 rows of BO values, blocks of 16 values moved about within a row (as in bgl_tile.h); fragments by the LDS read
+//             that transposes 4 x 16 values among 16 lanes
+//   OcBlocks  the same from blocks of 16 x 32: 16-byte piece p of row r at p ^ 2 (r / 2 + r / 8 & 1)
 // A load of a wavefront fills 1,024 consecutive bytes of LDS, so it is the addresses it reads from that are exchanged.
 #pragma once
 
@@ -27,7 +32,7 @@ using tile::bf16x8;
 using tile::f32x4;
 using tile::s16x4;
 
-constexpr int kStep = 32, kStages = 3, kThreads = 256, kWaves = kThreads / kWave;
+constexpr int kThreads = 256, kWaves = kThreads / kWave;
 
 __device__ __forceinline__ int wave_number() { return __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); }
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -35,7 +40,7 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ i32x4 whole_memory_from(const char *base)
 {
     const uint64_t at = (uint64_t)base;
-    return i32x4{(int)(uint32_t)at, (int)((uint32_t)(at >> 32) & 0xffff), -1, 0x00020000};
+    return i32x4{__builtin_amdgcn_readfirstlane((int)(uint32_t)at), __builtin_amdgcn_readfirstlane((int)((uint32_t)(at >> 32) & 0xffff)), -1, 0x00020000};
 }
 // 16 bytes for each lane from base + lane_offset to lds + 16 * lane.  In assembly because the compiler puts a wait for all loads before the next read of LDS where
 // it makes these loads itself; multiply() counts them.  (No vector register is written, so none can be lost to a load on its way; m0 is not kept for anything else on this GPU.)
@@ -45,11 +50,13 @@ __device__ __forceinline__ void load_to_lds(i32x4 from, char *lds, uint32_t lane
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(lane_offset), "s"(from) : "memory");
 }
 
-template <int BO>
+template <int BO, int STEP_>
 struct Kc {
-    static constexpr int BYTES = BO * kStep * 2, LOADS = BYTES / 1024 / kWaves;
+    static constexpr int STEP = STEP_, PIECES = STEP / 8, BYTES = BO * STEP * 2, LOADS = BYTES / 1024 / kWaves;
+    static_assert(LOADS * kWaves * 1024 == BYTES, "");
     const char *base;
     uint32_t off[LOADS];
+    static __device__ __forceinline__ int move(int r) { return STEP == 64 ? r & 7 : r >> 1 & 3; }
     // row(i): the byte offset of the tile's row i from base, less than 2^32; of any readable row for one that does not exist
     template <class Row>
     __device__ __forceinline__ void init(const char *start, Row row)
@@ -58,8 +65,8 @@ struct Kc {
         const int l = threadIdx.x & 63;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int r = (wave_number() * LOADS + i) * 16 + (l >> 2);
-            off[i] = row(r) + (((l & 3) ^ (r >> 1 & 3)) << 4);
+            const int r = (wave_number() * LOADS + i) * (64 / PIECES) + l / PIECES;
+            off[i] = row(r) + (((l % PIECES) ^ move(r)) << 4);
         }
     }
     __device__ __forceinline__ void load(char *lds, uint64_t offset, int) const
@@ -68,19 +75,32 @@ struct Kc {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) load_to_lds(from, lds + (wave_number() * LOADS + i) * 1024, off[i]);
     }
+    // F fragments of rows from `first` on, the part'th 32 of the stage's summed values
     template <int F>
-    static __device__ __forceinline__ void read(const char *lds, int first, bf16x8 (&f)[F])
+    static __device__ __forceinline__ void read(const char *lds, int first, int part, bf16x8 (&f)[F])
     {
         const int l = threadIdx.x & 63;
-        const char *at = lds + (first + (l & 15)) * 64 + (((l >> 4) ^ (l >> 1 & 3)) << 4);
+        const char *at = lds + (first + (l & 15)) * STEP * 2 + (((part * 4 + (l >> 4)) ^ move(l & 15)) << 4);
 #pragma unroll
-        for (int t = 0; t < F; ++t) f[t] = *reinterpret_cast<const bf16x8 *>(at + t * 1024);
+        for (int t = 0; t < F; ++t) f[t] = *reinterpret_cast<const bf16x8 *>(at + t * 16 * STEP * 2);
     }
 };
 
+// A fragment of 16 kept x 32 summed values where the kept index is contiguous: lane (i / 4, i % 4) of 16 names 4 kept values of summed row i / 4, and 4 rows
+// further on, and gets kept value i of all eight.
+__device__ __forceinline__ bf16x8 transposed(const char *at, int four_rows)
+{
+    uint2 h[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+        h[u] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at + u * four_rows)));
+    const uint4 both{h[0].x, h[0].y, h[1].x, h[1].y};
+    return __builtin_bit_cast(bf16x8, both);
+}
+
 template <int BO>
 struct Oc {
-    static constexpr int BYTES = BO * kStep * 2, LOADS = BYTES / 1024 / kWaves, ROW = BO * 2;
+    static constexpr int STEP = 32, BYTES = BO * STEP * 2, LOADS = BYTES / 1024 / kWaves, ROW = BO * 2;
     const char *base;
     uint32_t off[LOADS], stride;
     static __device__ __forceinline__ int move(int k) { return (k & 3) | (k >> 3 & 1) << 2; }
@@ -103,7 +123,7 @@ struct Oc {
     __device__ __forceinline__ void load(char *lds, uint64_t offset, int left) const
     {
         const auto from = whole_memory_from(base + offset);
-        if (left >= kStep) {
+        if (left >= STEP) {
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) load_to_lds(from, lds + (wave_number() * LOADS + i) * 1024, off[i]);
         } else {
@@ -115,26 +135,66 @@ struct Oc {
         }
     }
     template <int F>
-    static __device__ __forceinline__ void read(const char *lds, int first, bf16x8 (&f)[F])
+    static __device__ __forceinline__ void read(const char *lds, int first, int, bf16x8 (&f)[F])
     {
         const int l = threadIdx.x & 63, i = l & 15, g = l >> 4;
 #pragma unroll
-        for (int t = 0; t < F; ++t) {
-            const char *at = lds + place(8 * g + (i >> 2), first + 16 * t + 4 * (i & 3));
-            uint2 h[2];
+        for (int t = 0; t < F; ++t) f[t] = transposed(lds + place(8 * g + (i >> 2), first + 16 * t + 4 * (i & 3)), 4 * ROW);
+    }
+};
+
+// Blocks of 16 summed rows x 32 kept values, 1,024 bytes each, those of 16 summed rows one after the other.  The summed rows exist to a multiple of 32.
+template <int BO>
+struct OcBlocks {
+    static constexpr int STEP = 32, ACROSS = BO / 32, BYTES = BO * STEP * 2, LOADS = BYTES / 1024 / kWaves;
+    const char *base;
+    uint32_t off[LOADS];
+    static __device__ __forceinline__ int move(int r) { return ((r >> 1) ^ (r >> 3)) & 1 ? 2 : 0; }
+    // down: bytes from 16 summed rows to the next 16, across: from a block to the next; first: of the tile's ACROSS blocks, of `blocks` that exist
+    __device__ __forceinline__ void init(const char *start, uint32_t down, uint32_t across, int first, int blocks)
+    {
+        base = start;
+        const int l = threadIdx.x & 63;
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
-                h[u] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at + 4 * u * ROW)));
-            const uint4 both{h[0].x, h[0].y, h[1].x, h[1].y};
-            f[t] = __builtin_bit_cast(bf16x8, both);
+        for (int i = 0; i < LOADS; ++i) {
+            const int q = wave_number() * LOADS + i, b = first + q % ACROSS;
+            off[i] = q / ACROSS * down + (b < blocks ? b : blocks - 1) * across + (l >> 2) * 64 + (((l & 3) ^ move(l >> 2)) << 4);
+        }
+    }
+    __device__ __forceinline__ void load(char *lds, uint64_t offset, int) const
+    {
+        const auto from = whole_memory_from(base + offset);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load_to_lds(from, lds + (wave_number() * LOADS + i) * 1024, off[i]);
+    }
+    template <int F>
+    static __device__ __forceinline__ void read(const char *lds, int first, int, bf16x8 (&f)[F])
+    {
+        const int l = threadIdx.x & 63, i = l & 15, g = l >> 4, r = 8 * (g & 1) + (i >> 2);
+#pragma unroll
+        for (int t = 0; t < F; ++t) {
+            const int c = first + 16 * t + 4 * (i & 3);
+            f[t] = transposed(lds + ((g >> 1) * ACROSS + (c >> 5)) * 1024 + r * 64 + (((c >> 3 & 3) ^ move(r)) << 4) + (c & 4) * 2, 4 * 64);
         }
     }
 };
 
-// How a product's steps go through its operands: bytes from one block of 32 summed values to the next, and from one plane to the next.
+// Tiles in an order for eight XCDs (workgroup numbers go round them): each takes every eighth of the slow tiles, `group` of these at a time, which share its L2
+// while the fast ones go by.  tile::tile_count(slow, fast) workgroups.
+__device__ __forceinline__ bool tile_of(uint32_t id, uint32_t slow_tiles, uint32_t fast_tiles, uint32_t group, int64_t &slow, int &fast)
+{
+    const uint32_t j = id >> 3, mine = (slow_tiles + 7) / 8, g = j / (group * fast_tiles) * group, in = j - g * fast_tiles;
+    const uint32_t wide = mine - g < group ? mine - g : group;
+    fast = __builtin_amdgcn_readfirstlane(in / wide);
+    slow = __builtin_amdgcn_readfirstlane((g + in % wide) * 8 + (id & 7));
+    return slow < slow_tiles;
+}
+
+// How a product goes through its operands: bytes from one stage's summed values to the next, and from one plane to the next.
 struct Walk {
     uint32_t a_block, b_block, a_plane, b_plane;
     int count;  // of the summed index
+    int first;  // stage the product begins with, less than their number; it goes round
 };
 
 // A workgroup of 2 x 2 wavefronts, each with FA x FB fragments.
@@ -145,44 +205,59 @@ struct Cut {
     static __device__ __forceinline__ int b_off() { return wave_number() % 2 * 16 * FB; }
 };
 
-// Adds the product to acc.  PLANES: 1, or 3 (six products).  also(plane of b, a's fragments) sees every step.  Ends with all of LDS free.
+// Two workgroups a CU: as many stages as 80 KB hold.
+template <class A, class B>
+constexpr int stages() { return 81920 / (A::BYTES + B::BYTES); }
+template <class A, class B>
+constexpr int lds_bytes() { return stages<A, B>() * (A::BYTES + B::BYTES); }
+
+// Adds the product to acc.  PLANES: 1, or 3 (six products).  also(plane of b, a's fragments) sees every 32 summed values.  Ends with all of LDS free.
 template <int PLANES, class A, class B, class C, class Also>
 __device__ __forceinline__ void multiply(char *lds, const A &a, const B &b, const Walk &w, f32x4 (&acc)[C::FA][C::FB], Also also)
 {
-    constexpr int PAIRS = PLANES == 1 ? 1 : 6, STAGE = A::BYTES + B::BYTES, LOADS = A::LOADS + B::LOADS;
+    static_assert(A::STEP == B::STEP, "");
+    constexpr int STEP = A::STEP, STAGES = stages<A, B>(), PAIRS = PLANES == 1 ? 1 : 6, BYTES = A::BYTES + B::BYTES, LOADS = A::LOADS + B::LOADS;
+    static_assert(STAGES == 2 || STAGES == 3, "");
     constexpr uint32_t PLANE_A = 0x010210, PLANE_B = 0x211000;  // of pair p: hexadecimal digit p
-    const int steps = (w.count + kStep - 1) / kStep * PAIRS;
+    const int blocks = (w.count + STEP - 1) / STEP, steps = blocks * PAIRS;
     if (steps <= 0) return;
-    int block = 0, pair = 0, to = 0;  // of the next step to load
+    int block = w.first, pair = 0, to = 0;  // of the next stage to load
     const auto load = [&] {
-        char *at = lds + to * STAGE;
-        const int left = w.count - block * kStep;
+        char *at = lds + to * BYTES;
+        const int left = w.count - block * STEP;
         a.load(at, (uint64_t)block * w.a_block + (PLANES > 1 ? (PLANE_A >> 4 * pair & 3) * w.a_plane : 0), left);
         b.load(at + A::BYTES, (uint64_t)block * w.b_block + (PLANES > 1 ? (PLANE_B >> 4 * pair & 3) * w.b_plane : 0), left);
-        if (++pair == PAIRS) pair = 0, ++block;
-        if (++to == kStages) to = 0;
+        if (++pair == PAIRS) {
+            pair = 0;
+            if (++block == blocks) block = 0;
+        }
+        if (++to == STAGES) to = 0;
     };
-    load();
-    if (steps > 1) load();
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s)
+        if (s < steps) load();
     int at = 0, plane = 0;
     for (int s = 0; s < steps; ++s) {
-        // this step's loads have come (all wavefronts': the barrier), and the buffer of the step before has been read by all
-        if (s + 1 < steps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+        // this stage's loads have come (all wavefronts': the barrier), and the buffer of the stage before has been read by all
+        if (STAGES == 3 && s + 1 < steps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (s + 2 < steps) load();
-        const char *from = lds + at * STAGE;
-        bf16x8 fa[C::FA], fb[C::FB];
-        B::read(from + A::BYTES, C::b_off(), fb);
-        A::read(from, C::a_off(), fa);
+        if (s + STAGES - 1 < steps) load();
+        const char *from = lds + at * BYTES;
 #pragma unroll
-        for (int i = 0; i < C::FA; ++i)
+        for (int part = 0; part < STEP / 32; ++part) {
+            bf16x8 fa[C::FA], fb[C::FB];
+            B::read(from + A::BYTES, C::b_off(), part, fb);
+            A::read(from, C::a_off(), part, fa);
 #pragma unroll
-            for (int j = 0; j < C::FB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
-        also(PLANE_B >> 4 * plane & 3, fa);
+            for (int i = 0; i < C::FA; ++i)
+#pragma unroll
+                for (int j = 0; j < C::FB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+            also(PLANE_B >> 4 * plane & 3, fa);
+        }
         if (++plane == PAIRS) plane = 0;
-        if (++at == kStages) at = 0;
+        if (++at == STAGES) at = 0;
         asm volatile("" ::: "memory");
     }
     __syncthreads();
