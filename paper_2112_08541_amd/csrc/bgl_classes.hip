@@ -237,97 +237,88 @@ struct RowArgs {
     int32_t *listed;  // the row's number, or -1 without a gradient
 };
 
-// The scores of a row's classes: a wavefront for each of four classes at a time.
+// The scores of the teacher's classes: 8 lanes for each, 128 bytes of x and of the class's row at a time.
 template <class T>
 __global__ void __launch_bounds__(256) k_class_top(RowArgs<T> a)
 {
-    const int64_t task = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
-    const int l = threadIdx.x & 63, each = (a.top + 3) / 4;
-    const int64_t r = task / each;
-    if (r >= a.rows) return;
+    constexpr int LANES = 8, AHEAD = 4;
+    const uint64_t task = (uint64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES, r = task / (uint32_t)a.top;
+    const int l = threadIdx.x % LANES;
+    if (r >= (uint64_t)a.rows) return;
     const int64_t row = a.row0 + r;
-    const int k0 = (int)(task % each) * 4;
-    const typename T::elem *x = a.x + row * a.x_stride, *w[4];
-    int c[4];
-    float z[4] = {};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        c[k] = k0 + k < a.top ? a.top_class[row * a.top + k0 + k] : -1;
-        if ((uint32_t)c[k] >= (uint32_t)a.classes) c[k] = -1;
-        w[k] = a.w + (int64_t)(c[k] < 0 ? 0 : c[k]) * a.D;
-    }
-    for (int d = l * T::VEC; d < a.D; d += 64 * T::VEC) {
-        const int left = a.D - d;
-        const auto unpack = [](const uint4 &v, float (&f)[T::VEC]) {
-            const uint32_t q[4] = {v.x, v.y, v.z, v.w};
+    const int k = (int)(task % (uint32_t)a.top), c = a.top_class[row * a.top + k];
+    float z = 0.0f;
+    if ((uint32_t)c < (uint32_t)a.classes) {
+        const typename T::elem *x = a.x + row * a.x_stride, *w = a.w + (int64_t)c * a.D;
+        const auto add = [&](const uint4 &p, const uint4 &q) {
+            const uint32_t u[4] = {p.x, p.y, p.z, p.w}, v[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if constexpr (T::PER == 1) f[i] = __uint_as_float(q[i]);
-                else f[2 * i] = __uint_as_float(q[i] << 16), f[2 * i + 1] = __uint_as_float(q[i] & 0xffff0000u);
+                if constexpr (T::PER == 1) {
+                    z = fmaf(__uint_as_float(u[i]), __uint_as_float(v[i]), z);
+                } else {
+                    z = fmaf(__uint_as_float(u[i] << 16), __uint_as_float(v[i] << 16), z);
+                    z = fmaf(__uint_as_float(u[i] & 0xffff0000u), __uint_as_float(v[i] & 0xffff0000u), z);
+                }
             }
         };
-        float xv[T::VEC], wv[T::VEC];
-        const bool whole = left >= T::VEC;
-        unpack(whole ? load_any<uint4>(x + d) : load_end<T>(x + d, left, a.D), xv);
-        uint4 raw[4];
+        constexpr int STEP = LANES * T::VEC;
+        int d = l * T::VEC;
+        for (; d + (AHEAD - 1) * STEP + T::VEC <= a.D; d += AHEAD * STEP) {
+            uint4 p[AHEAD], q[AHEAD];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) raw[k] = whole ? load_any<uint4>(w[k] + d) : load_end<T>(w[k] + d, left, a.D);
+            for (int u = 0; u < AHEAD; ++u) p[u] = load_any<uint4>(x + d + u * STEP), q[u] = load_any<uint4>(w + d + u * STEP);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            unpack(raw[k], wv);
-#pragma unroll
-            for (int i = 0; i < T::VEC; ++i) z[k] = fmaf(xv[i], wv[i], z[k]);
+            for (int u = 0; u < AHEAD; ++u) add(p[u], q[u]);
         }
+        for (; d < a.D; d += STEP) add(load_end<T>(x + d, a.D - d, a.D), load_end<T>(w + d, a.D - d, a.D));
     }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        z[k] = sum_across<64>(z[k]);
-        if (l == 0 && k0 + k < a.top) a.z_top[row * a.z_stride + k0 + k] = z[k] + (a.bias && c[k] >= 0 ? T::get(a.bias[c[k]]) : 0.0f);
-    }
+    z = sum_across<LANES>(z);
+    if (l == 0) a.z_top[row * a.z_stride + k] = z + (a.bias && (uint32_t)c < (uint32_t)a.classes ? T::get(a.bias[c]) : 0.0f);  // (0 where there is no class)
 }
 
-// The teacher's distribution of a row, for a wavefront: largest score / t and sum of exp; false where it names no class.
-template <class T>
+// The teacher's distribution of a row, for LANES neighbours: largest score / t and sum of exp; false where it names no class.
+template <int LANES, class T>
 __device__ __forceinline__ bool teacher_of(const RowArgs<T> &a, int64_t row, float &most, float &total)
 {
-    const int l = threadIdx.x & 63;
+    const int l = threadIdx.x % LANES;
     most = -INFINITY, total = 0.0f;
     float bad = 0.0f;
-    for (int k = l; k < a.top; k += 64)
+    for (int k = l; k < a.top; k += LANES)
         if ((uint32_t)a.top_class[row * a.top + k] < (uint32_t)a.classes) {
             const float v = a.top_score[row * a.top + k] * a.over_t;
             most = fmaxf(most, v);
             if (v != v) bad = v;
         }
-    most = max_across<64>(most);
-    bad = sum_across<64>(bad);
+    most = max_across<LANES>(most);
+    bad = sum_across<LANES>(bad);
     if (bad != bad) most = bad;
     if (most == -INFINITY) return false;
-    for (int k = l; k < a.top; k += 64)
+    for (int k = l; k < a.top; k += LANES)
         if ((uint32_t)a.top_class[row * a.top + k] < (uint32_t)a.classes) total += exp_of(a.top_score[row * a.top + k] * a.over_t - most);
-    total = sum_across<64>(total);
+    total = sum_across<LANES>(total);
     return true;
 }
 
-// A wavefront for each row.
-template <class T>
+// LANES neighbours for each row.
+template <class T, int LANES>
 __global__ void __launch_bounds__(256) k_class_finish(RowArgs<T> a)
 {
-    const int64_t r = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+    const int64_t r = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
     if (r >= a.rows) return;
     const int64_t row = a.row0 + r;
-    const int l = threadIdx.x & 63;
+    const int l = threadIdx.x % LANES;
     float most = -INFINITY, sum = 0.0f, sum_t = 0.0f;
-    for (int ct = l; ct < a.class_parts; ct += 64) {
+    for (int ct = l; ct < a.class_parts; ct += LANES) {
         const float2 from = a.part[ct * a.rows + r];
         const float m = fmaxf(most, from.x);
         sum = sum * rebase(base_of(most, a.k), base_of(m, a.k)) + from.y * rebase(base_of(from.x, a.k), base_of(m, a.k));
         if (a.two) sum_t = sum_t * rebase(base_of(most, a.k_t), base_of(m, a.k_t)) + a.part_t[ct * a.rows + r] * rebase(base_of(from.x, a.k_t), base_of(m, a.k_t));
         most = m;
     }
-    const float m = max_across<64>(most), base = base_of(m, a.k), base_t = a.two ? base_of(m, a.k_t) : base;
-    sum = sum_across<64>(sum * rebase(base_of(most, a.k), base));
-    sum_t = a.two ? sum_across<64>(sum_t * rebase(base_of(most, a.k_t), base_t)) : sum;
+    const float m = max_across<LANES>(most), base = base_of(m, a.k), base_t = a.two ? base_of(m, a.k_t) : base;
+    sum = sum_across<LANES>(sum * rebase(base_of(most, a.k), base));
+    sum_t = a.two ? sum_across<LANES>(sum_t * rebase(base_of(most, a.k_t), base_t)) : sum;
     const float log_sum = log2f(sum), log_sum_t = log2f(sum_t);
     if (a.labels) {
         const int label = a.labels[row];
@@ -338,17 +329,17 @@ __global__ void __launch_bounds__(256) k_class_finish(RowArgs<T> a)
     float lse_t = INFINITY;
     if (a.top_class) {
         float top_most, total, kl = 0.0f;
-        const bool taught = teacher_of(a, row, top_most, total);
+        const bool taught = teacher_of<LANES>(a, row, top_most, total);
         if (taught) {
             lse_t = base_t + log_sum_t;
             const float log_total = log2f(total);
-            for (int k = l; k < a.top; k += 64)
+            for (int k = l; k < a.top; k += LANES)
                 if ((uint32_t)a.top_class[row * a.top + k] < (uint32_t)a.classes) {
                     const float v = a.top_score[row * a.top + k] * a.over_t - top_most;
                     const float p = exp_of(v) / total;
                     if (p != 0.0f) kl = fmaf(p, (v * kLog2e - log_total) + (log_sum_t - fmaf(a.z_top[row * a.z_stride + k], a.k_t, -base_t)), kl);
                 }
-            kl = sum_across<64>(kl);
+            kl = sum_across<LANES>(kl);
         }
         if (l == 0 && a.teacher_loss) a.teacher_loss[row] = taught ? a.t * a.t * kLn2 * kl : 0.0f;
     }
@@ -377,7 +368,7 @@ __global__ void __launch_bounds__(256) k_class_fix(RowArgs<T> a)
     const int64_t row = a.row0 + r;
     const int l = threadIdx.x & 63;
     float most, total;
-    if (!teacher_of(a, row, most, total)) return;
+    if (!teacher_of<64>(a, row, most, total)) return;
     const float *kept = a.saved + row * a.saved_width;
     const float lse = kept[0], lse_t = kept[1];
     int label = a.labels ? a.labels[row] : -1;
@@ -1072,8 +1063,11 @@ int forward(const Call &c, float *loss, float *teacher_loss, float *saved)
         s.row0 = r.row0 = row0, s.rows = r.rows = c.n - row0 < p.pass_rows ? c.n - row0 : p.pass_rows;
         if (h.large) q.s = s, launch_scores_stage<T, false>(q, c.stream);
         else launch_scores<T, false>(s, c.stream);
-        if (c.top_class) k_class_top<T><<<dim3((unsigned)ceil_div(r.rows * ((r.top + 3) / 4), 4)), dim3(256), 0, c.stream>>>(r);
-        k_class_finish<T><<<dim3((unsigned)ceil_div(r.rows, 4)), dim3(256), 0, c.stream>>>(r);
+        if (c.top_class) k_class_top<T><<<dim3((unsigned)ceil_div(r.rows * r.top, 32)), dim3(256), 0, c.stream>>>(r);
+        const int values = c.top_class && r.top > p.class_parts ? r.top : p.class_parts;
+        if (values <= 8) k_class_finish<T, 4><<<dim3((unsigned)ceil_div(r.rows, 64)), dim3(256), 0, c.stream>>>(r);
+        else if (values <= 32) k_class_finish<T, 16><<<dim3((unsigned)ceil_div(r.rows, 16)), dim3(256), 0, c.stream>>>(r);
+        else k_class_finish<T, 64><<<dim3((unsigned)ceil_div(r.rows, 4)), dim3(256), 0, c.stream>>>(r);
     }
     BGL_HIP(hipGetLastError());
     return BGL_OK;

@@ -249,23 +249,31 @@ __global__ void __launch_bounds__(norm_threads<TEAM>()) k_norm_backward(NormArgs
     }
 }
 
-// The partial rows' sums: 32 columns a workgroup, every eighth row a thread.
+// The partial rows' sums: 32 columns a workgroup, every 32nd row a thread, eight of them on their way at a time.
 template <class T>
-__global__ void __launch_bounds__(256) k_norm_reduce(NormArgs<T> a)
+__global__ void __launch_bounds__(1024) k_norm_reduce(NormArgs<T> a)
 {
-    __shared__ float part[8][32];
-    const int64_t at = (int64_t)blockIdx.x * 32 + threadIdx.x % 32, all = 2 * (int64_t)a.width;
+    constexpr int LANES = 32, AHEAD = 8;
+    __shared__ float part[LANES][33];
+    const int64_t all = 2 * (int64_t)a.width, at = (int64_t)blockIdx.x * 32 + threadIdx.x % 32;
     const int lane = threadIdx.x / 32;
+    const float *from = a.partial + (at < all ? at : 0);
     float s = 0.0f;
-    if (at < all)
-        for (int p = lane; p < a.parts; p += 8) s += a.partial[p * all + at];
+    for (int p = lane; p < a.parts; p += LANES * AHEAD) {
+        float v[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) v[u] = p + u * LANES < a.parts ? from[(p + u * LANES) * all] : 0.0f;
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) s += v[u];
+    }
     part[lane][threadIdx.x % 32] = s;
     __syncthreads();
-    if (lane > 0 || at >= all) return;
-#pragma unroll
-    for (int p = 1; p < 8; ++p) s += part[p][threadIdx.x];
-    typename T::elem *to = at < a.width ? a.dweight : a.dbias;
-    if (to) to[at < a.width ? at : at - a.width] = T::put(s);
+    // a column's sums to neighbouring lanes
+    s = sum_across<32>(part[threadIdx.x % 32][lane]);
+    const int64_t c = (int64_t)blockIdx.x * 32 + lane;
+    if (threadIdx.x % 32 > 0 || c >= all) return;
+    typename T::elem *to = c < a.width ? a.dweight : a.dbias;
+    if (to) to[c < a.width ? c : c - a.width] = T::put(s);
 }
 
 int team_of(int width)
@@ -321,7 +329,7 @@ int backward(NormArgs<T> a, hipStream_t st)
         BGL_HIP(hipGetLastError());
     }
     if (sums) {
-        k_norm_reduce<T><<<dim3((unsigned)ceil_div(2 * (int64_t)a.width, 32)), dim3(256), 0, st>>>(a);
+        k_norm_reduce<T><<<dim3((unsigned)ceil_div(2 * (int64_t)a.width, 32)), dim3(1024), 0, st>>>(a);
         BGL_HIP(hipGetLastError());
     }
     return BGL_OK;
