@@ -596,8 +596,10 @@ def _weights(name: str, t: Optional[torch.Tensor], shape, dtype):
 
 def _refuse_gradients(who: str, *tensors) -> None:
     """Torch's own differentiation does not see the library's calls."""
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
-        raise ValueError(f"{who} does not record gradients: call it under torch.no_grad() and make the backward call yourself")
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError(f"{who} does not record gradients: call it under torch.no_grad() and make the backward call yourself")
 
 
 class RowGroups:

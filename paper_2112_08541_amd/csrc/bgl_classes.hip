@@ -26,8 +26,7 @@ constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 constexpr int64_t kPieceRows = 16384;
 constexpr int64_t kPieceClasses = 256;                 // pieces of some classes only are multiples
 constexpr int64_t kPartialBytes = (int64_t)64 << 20;   // of a forward call's tiles' maxima and sums
-constexpr int64_t kSharesFill = 512;                   // workgroups that ranges of a product's summed index are to make together
-constexpr int64_t kShareLeast = 512;                   // of the summed index, for each of them
+constexpr int kCus = 256;
 constexpr double kLargeProducts = 5e8;                 // of a call that is laid out for large tiles
 
 // Exponentials are powers of two: exp(k v) / 2^base with k = log2(e) or that over the temperature, as 2^(k v - base) with one rounding.  A sum of them is taken to
@@ -41,6 +40,8 @@ __device__ __forceinline__ float max3(float a, float b, float c)  // (of fmaxf t
     asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
     return r;
 }
+// The logarithm of the sum less the score, both to the sum's base (what they have in common goes before they meet), in natural units.
+__device__ __forceinline__ float loss_of(float log_sum, float score, float k, float base) { return kLn2 * (log_sum - fmaf(score, k, -base)); }
 __device__ __forceinline__ float rebase(float from, float to) { return __builtin_amdgcn_exp2f(from - to); }
 
 // The other lanes with the same lane % 16.
@@ -93,6 +94,8 @@ struct ScoreArgs {
     // forward: {largest, sum} of part t of the classes and row r at part[t * rows + r], the sum at the temperature at part_t[t * rows + r]
     float2 *part;
     float *part_t, *label_score;
+    float *loss, *kept;       // one tile has all classes and there is no teacher: the losses and what is saved (or null) instead
+    bool whole;
     bool two;                 // the temperature is not 1 and there is a teacher: two sums
     // backward
     const float *saved;       // n x width {log2 sum exp, the same at the temperature or +inf, the teacher's classes' scores}
@@ -100,6 +103,7 @@ struct ScoreArgs {
     float scale, teacher_scale;
     typename T::elem *dz;     // rows x dz_stride
     int dz_stride;
+    int32_t *listed;          // null, or the row's number among this launch's for rows with a gradient, else -1
 };
 
 // One tile of classes x rows: a lane holds, of one row, 4 neighbouring classes of every 16.
@@ -109,7 +113,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_scores(ScoreArgs<T> a)
     using A = KcOperand<T, C::BA>;
     using B = KcOperand<T, C::BB>;
     __shared__ __attribute__((aligned(16))) uint32_t lds[A::LDS + B::LDS];
-    __shared__ float meet[DZ ? 1 : 3 * C::BA / 16 / C::FA * C::BB];
+    __shared__ float meet[DZ ? 1 : 3 * C::BA / 16 / C::FA * C::BB], own_score[DZ ? 1 : C::BB];
     int64_t ct, rt;
     int fast;
     if (!tile_of(blockIdx.x, a.by_rows ? a.row_tiles : a.class_tiles, (int)(a.by_rows ? a.class_tiles : a.row_tiles), a.by_rows ? rt : ct, fast)) return;
@@ -166,7 +170,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_scores(ScoreArgs<T> a)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float v = acc[i][t][j];
-                    if (first + 16 * i + j == label && live) a.label_score[row] = v;
+                    if (first + 16 * i + j == label && live) {
+                        if (a.whole) own_score[in_tile] = v;
+                        else a.label_score[row] = v;
+                    }
                     sum += power_to(v, a.k, base);
                     if (a.two) sum_t += power_to(v, a.k_t, base_t);
                 }
@@ -178,6 +185,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_scores(ScoreArgs<T> a)
             const float *kept = a.saved + row * a.saved_width;
             const float lse = kept[0], lse_t = kept[1];
             const float s = label >= 0 ? a.scale : 0.0f, st = lse_t < INFINITY || lse_t != lse_t ? a.teacher_scale : 0.0f;
+            // (the products that sum over rows leave the others out, whatever x holds there)
+            if (a.listed && ct == 0 && C::a_off() == 0 && l < 16 && live) a.listed[r] = s != 0.0f || st != 0.0f ? (int32_t)r : -1;
 #pragma unroll
             for (int i = 0; i < C::FA; ++i) {
                 typename T::elem e[4];
@@ -209,6 +218,14 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_scores(ScoreArgs<T> a)
                 sum += from[1] * rebase(base_of(from[0], a.k), base_of(most, a.k));
                 if (a.two) sum_t += from[2] * rebase(base_of(from[0], a.k_t), base_of(most, a.k_t));
             }
+            if (a.whole) {
+                const int64_t row = a.row0 + r0 + in_tile;
+                const float base = base_of(most, a.k), log_sum = log2f(sum);
+                const bool has = (uint32_t)a.labels[row] < (uint32_t)a.all_classes;
+                if (a.loss) a.loss[row] = has ? loss_of(log_sum, own_score[in_tile], a.k, base) : 0.0f;
+                if (a.kept) a.kept[row * a.saved_width] = base + log_sum, a.kept[row * a.saved_width + 1] = INFINITY;
+                continue;
+            }
             a.part[ct * a.rows + r0 + in_tile] = float2{most, sum};
             if (a.two) a.part_t[ct * a.rows + r0 + in_tile] = sum_t;
         }
@@ -234,7 +251,6 @@ struct RowArgs {
     typename T::elem *dz;
     int class0, piece_classes, dz_stride;
     bool blocks;     // dz lies in blocks
-    int32_t *listed;  // the row's number, or -1 without a gradient
 };
 
 // The scores of the teacher's classes: 8 lanes for each, 128 bytes of x and of the class's row at a time.
@@ -323,8 +339,7 @@ __global__ void __launch_bounds__(256) k_class_finish(RowArgs<T> a)
     if (a.labels) {
         const int label = a.labels[row];
         const bool has = (uint32_t)label < (uint32_t)a.classes;
-        // (what the score and the sum have in common goes before the sum's logarithm comes to it)
-        if (l == 0 && a.loss) a.loss[row] = has ? kLn2 * (log_sum - fmaf(a.label_score[row], a.k, -base)) : 0.0f;
+        if (l == 0 && a.loss) a.loss[row] = has ? loss_of(log_sum, a.label_score[row], a.k, base) : 0.0f;
     }
     float lse_t = INFINITY;
     if (a.top_class) {
@@ -344,19 +359,6 @@ __global__ void __launch_bounds__(256) k_class_finish(RowArgs<T> a)
         if (l == 0 && a.teacher_loss) a.teacher_loss[row] = taught ? a.t * a.t * kLn2 * kl : 0.0f;
     }
     if (l == 0 && a.saved) a.saved[row * a.saved_width] = base + log_sum, a.saved[row * a.saved_width + 1] = lse_t;
-}
-
-// Which rows have a gradient, for the products that sum over rows: what others hold there is not read.
-template <class T>
-__global__ void __launch_bounds__(256) k_class_rows(RowArgs<T> a)
-{
-    const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (r >= a.rows) return;
-    const int64_t row = a.row0 + r;
-    const bool labelled = a.labels && (uint32_t)a.labels[row] < (uint32_t)a.classes && a.scale != 0.0f;
-    const float lse_t = a.saved[row * a.saved_width + 1];
-    const bool taught = a.top_class && lse_t != INFINITY && a.teacher_scale != 0.0f;
-    a.listed[r] = labelled || taught ? (int32_t)r : -1;
 }
 
 // dz where the teacher names a class: a wavefront for each row.  A class named twice has the sum of its shares, written by both.
@@ -501,22 +503,35 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_product(PieceArgs<T> a)
     }
 }
 
+// Sums over ranges: of `rows` x width values, and of `rows` more (db) if there are.
 template <class T>
 struct ReduceArgs {
-    const float *slots;
-    int64_t slot_values, count;  // values between slots; of the result, in rows of `width`
+    const float *slots, *sum_slots;
+    int64_t slot_rows, rows;  // of a slot; of the result
     int width, shares;
-    typename T::elem *out;
+    typename T::elem *out, *sums;
     int64_t out_stride;
 };
 template <class T>
 __global__ void __launch_bounds__(256) k_class_reduce(ReduceArgs<T> a)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= a.count) return;
+    const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x, values = (uint64_t)a.rows * a.width;
+    const bool second = i >= values;
+    const uint64_t at = second ? i - values : i, step = a.slot_rows * (second ? 1 : a.width);
+    if (second && (!a.sums || at >= (uint64_t)a.rows)) return;
+    const float *from = (second ? a.sum_slots : a.slots) + at;
     float s = 0.0f;
-    for (int p = 0; p < a.shares; ++p) s += a.slots[p * a.slot_values + i];
-    a.out[i / a.width * a.out_stride + i % a.width] = T::put(s);
+    int p = 0;
+    for (; p + 8 <= a.shares; p += 8) {  // (eight on their way at a time)
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = from[(p + u) * step];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s += v[u];
+    }
+    for (; p < a.shares; ++p) s += from[p * step];
+    if (second) a.sums[at] = T::put(s);
+    else a.out[a.out_stride == a.width ? at : at / (uint32_t)a.width * a.out_stride + at % (uint32_t)a.width] = T::put(s);
 }
 template <class T>
 __global__ void __launch_bounds__(256) k_class_zero(typename T::elem *p, int64_t count)
@@ -843,6 +858,8 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_product_stage(Stag
 using Large = Cut<2, 2, 4, 4>;   // 128 x 128
 using Middle = Cut<2, 2, 4, 2>;  // 128 x 64
 using Low = Cut<4, 1, 2, 1>;     // 128 x 16
+using Slim = Cut<4, 1, 1, 1>;    // 64 x 16
+using Small = Cut<2, 2, 2, 2>;   // 64 x 64
 
 struct Plan {
     // forward
@@ -851,7 +868,7 @@ struct Plan {
     size_t part_bytes, label_bytes, top_bytes, forward_bytes;
     // backward
     int64_t piece_rows, row_pieces, dz_stride;
-    int piece_classes, class_pieces, dx_shares, dw_shares;
+    int piece_classes, class_pieces, dx_shares, dw_shares, dx_tile, dw_tile;
     int64_t dx_per, dw_per;
     size_t dz_bytes, list_bytes, dx_bytes, dw_bytes, db_bytes, backward_bytes;
     // large calls: laid out operands, forward (0: as they are) and backward
@@ -866,26 +883,35 @@ struct Scheme {
     int score_classes, product_rows;  // of a tile
     int64_t values, round_classes, round_rows;
     int dz_value_bytes, planes;
+    int64_t fill, least;              // ranges of a product's summed index: workgroups they are to make together, of the index for each
 };
 Scheme scheme_of(const bgl_class_loss_t *l, bool large)
 {
     const bool f32 = l->dtype == BGL_F32;
-    if (large) return Scheme{true, StageCut::BA, ProductCut::BA, ((int64_t)1 << 27) + ((int64_t)1 << 23), StageCut::BA, StageCut::BB, f32 ? 6 : 2, f32 ? 3 : 1};
-    return Scheme{false, 128, 128, (int64_t)1 << 25, 8, 1, f32 ? 4 : 2, 1};  // (pieces of 4 classes are stored, and 16 bytes of bf16 read)
+    if (large) return Scheme{true, StageCut::BA, ProductCut::BA, ((int64_t)1 << 27) + ((int64_t)1 << 23), StageCut::BA, StageCut::BB, f32 ? 6 : 2, f32 ? 3 : 1, 2 * kCus, 512};
+    return Scheme{false, 128, 128, (int64_t)1 << 25, 8, 1, f32 ? 4 : 2, 1, kCus, 64};  // (pieces of 4 classes are stored, and 16 bytes of bf16 read)
 }
 bool large_call(const bgl_class_loss_t *l, int64_t n) { return n >= 256 && l->classes >= 128 && (double)n * l->classes * l->in_dim >= kLargeProducts; }
 bool laid_out(const bgl_class_loss_t *l) { return l->dtype == BGL_BF16 && l->in_dim % kPad == 0; }
 
-int shares_for(int64_t tiles, int64_t summed)
+// Ranges of the summed index that a product of rows x cols is made in, and the tiles' size: small calls take tiles of 64 x 64 where 128 x 128 do not fill the GPU.
+int shares_for(const Scheme &s, int64_t rows, int64_t cols, int64_t summed, int &tile)
 {
-    const int64_t want = kSharesFill / (tiles < 1 ? 1 : tiles), most = summed / kShareLeast;
-    return (int)(want < 1 || most < 1 ? 1 : want < most ? want : most);
+    const int64_t most = summed / s.least;
+    const auto fit = [&](int64_t tiles) {
+        const int64_t want = s.fill / (tiles < 1 ? 1 : tiles);
+        return want < 1 || most < 1 ? 1 : want < most ? want : most;
+    };
+    tile = s.product_rows;
+    int64_t tiles = ceil_div(rows, tile) * ceil_div(cols, 128);
+    if (!s.large && tiles * fit(tiles) < s.fill / 2) tile = 64, tiles = ceil_div(rows, 64) * ceil_div(cols, 64);
+    return (int)fit(tiles);
 }
 
 Plan plan_of(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
 {
     Plan p{};
-    p.class_parts = (int)ceil_div(l->classes, s.score_classes) * (s.large ? 2 : 1);
+    p.class_parts = (int)ceil_div(l->classes, s.score_classes) * (s.large ? 2 : 1);  // (tiles of 64 classes: only where one has them all)
     p.pass_rows = kPartialBytes / (12 * (int64_t)p.class_parts);
     p.pass_rows = p.pass_rows < 1024 ? 1024 : p.pass_rows / 128 * 128;
     if (p.pass_rows > n) p.pass_rows = n;
@@ -910,7 +936,7 @@ Plan plan_of(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
         } else {
             if (n > kPieceRows) p.piece_rows = kPieceRows;
             // whole rounds of dW's workgroups, if one fits (of 4,096 x 512: two pieces of 129 x 4 tiles took a third longer than two of 128 x 4)
-            const int64_t round = kSharesFill / ceil_div(l->in_dim, 128) * s.product_rows, most = s.values / p.piece_rows;
+            const int64_t round = s.fill / ceil_div(l->in_dim, 128) * s.product_rows, most = s.values / p.piece_rows;
             int64_t fit = (int64_t)round_up((size_t)ceil_div(stride, ceil_div(p.piece_rows * stride, s.values)), kPieceClasses);
             if (round > 0 && most >= round) fit = most / round * round;
             if (fit < l->classes) p.piece_classes = (int)fit;
@@ -921,10 +947,10 @@ Plan plan_of(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
     p.dz_stride = round_up(p.piece_classes, s.round_classes);
     p.dz_bytes = round_up(round_up(p.piece_rows, s.round_rows) * p.dz_stride * s.dz_value_bytes, 256);
     p.list_bytes = s.large ? 0 : round_up((size_t)n * 4, 256);
-    const int64_t cols = ceil_div(l->in_dim, 128);
-    p.dx_shares = p.class_pieces > 1 && p.row_pieces > 1 ? 1 : shares_for(ceil_div(p.piece_rows, s.product_rows) * cols, p.piece_classes);
+    p.dx_shares = shares_for(s, p.piece_rows, l->in_dim, p.piece_classes, p.dx_tile);
+    if (p.class_pieces > 1 && p.row_pieces > 1) p.dx_shares = 1;
     p.dx_per = round_up((size_t)ceil_div(p.piece_classes, p.dx_shares), 64);
-    p.dw_shares = shares_for(ceil_div(p.piece_classes, s.product_rows) * cols, p.piece_rows);
+    p.dw_shares = shares_for(s, p.piece_classes, l->in_dim, p.piece_rows, p.dw_tile);
     p.dw_per = round_up((size_t)ceil_div(p.piece_rows, p.dw_shares), 64);
     p.dx_bytes = p.dx_shares > 1 || p.class_pieces > 1 ? round_up((size_t)p.dx_shares * (p.class_pieces > 1 ? n : p.piece_rows) * l->in_dim * 4, 256) : 0;
     p.dw_bytes = p.dw_shares > 1 || p.row_pieces > 1 ? round_up((size_t)p.dw_shares * p.piece_classes * l->in_dim * 4, 256) : 0;
@@ -933,18 +959,18 @@ Plan plan_of(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
     return p;
 }
 
-// What the backward calls of up to n rows need: no call of fewer rows needs more.  (Shares are less than kSharesFill tiles in all.)
+// What the backward calls of up to n rows need: no call of fewer rows needs more.  (Tiles in several ranges are s.fill at most.)
 size_t backward_room(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
 {
-    const int64_t V = l->classes, D = l->in_dim, stride = round_up(V, s.round_classes), shared = kSharesFill * s.product_rows;
+    const int64_t V = l->classes, D = l->in_dim, stride = round_up(V, s.round_classes), shared = s.fill * s.product_rows;
     const bool many = V > kPieceRows;
     const auto least = [](int64_t a, int64_t b) { return a < b ? a : b; };
     const auto most = [](int64_t a, int64_t b) { return a > b ? a : b; };
     const int64_t over = (many ? kPieceClasses * least(n, kPieceRows) : 128 * stride) + 128 * least(stride, s.values);
     const Plan p = plan_of(l, n, s);
     size_t bytes = round_up((size_t)least(round_up(n, 128) * stride, s.values + over) * s.dz_value_bytes, 256) + round_up((size_t)n * 4, 256) + p.back_x_bytes + p.w_bytes;
-    if (V >= 2 * kShareLeast) bytes += round_up((size_t)most(many ? n : 0, least(shared, n * (V / kShareLeast))) * D * 4, 256);
-    const int64_t shares = n >= 2 * kShareLeast ? least(shared, V * (n / kShareLeast)) : 0;
+    if (V >= 2 * s.least) bytes += round_up((size_t)most(many ? n : 0, least(shared, n * (V / s.least))) * D * 4, 256);
+    const int64_t shares = n >= 2 * s.least ? least(shared, V * (n / s.least)) : 0;
     const int64_t pieces = many ? (n > kPieceRows ? s.values / kPieceRows + kPieceClasses : 0) : n * stride > s.values ? V : 0;
     bytes += round_up((size_t)most(shares, pieces) * D * 4, 256) + round_up((size_t)most(shares, pieces) * 4, 256);
     return bytes > p.backward_bytes ? bytes : p.backward_bytes;
@@ -953,17 +979,20 @@ size_t backward_room(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
 template <class T, bool DZ>
 void launch_scores(ScoreArgs<T> &s, hipStream_t st)
 {
-    s.class_tiles = (int)ceil_div(s.classes - s.class0, 128);
     const auto go = [&](auto cut) {
         using C = decltype(cut);
+        s.class_tiles = (int)ceil_div(s.classes - s.class0, C::BA);
         s.row_tiles = ceil_div(s.rows, C::BB);
         s.by_rows = s.row_tiles > s.class_tiles;
         const int64_t tiles = s.by_rows ? tile_count(s.row_tiles, s.class_tiles) : tile_count(s.class_tiles, (int)s.row_tiles);
         k_class_scores<T, C, DZ><<<dim3((unsigned)tiles), dim3(kThreads), 0, st>>>(s);
     };
-    if (s.rows <= 16) go(Low{});
-    else if (s.rows <= 64) go(Middle{});
-    else go(Large{});
+    // the largest tiles that the rows fill and that leave no CU without one: 1,024 x 128 x 50 f32 took 15 us in 8 tiles of 128 x 128
+    const int64_t classes = s.classes - s.class0, across = ceil_div(classes, 128);
+    if (s.rows > 64 && across * ceil_div(s.rows, 128) >= kCus) go(Large{});
+    else if (s.rows > 16 && across * ceil_div(s.rows, 64) >= kCus) go(Middle{});
+    else if (classes > 64) go(Low{});
+    else go(Slim{});
 }
 
 struct Call {
@@ -1061,8 +1090,10 @@ int forward(const Call &c, float *loss, float *teacher_loss, float *saved)
     if (h.large) q = stage_args<T>(c, p, h, s, x, w, nullptr);
     for (int64_t row0 = 0; row0 < c.n; row0 += p.pass_rows) {
         s.row0 = r.row0 = row0, s.rows = r.rows = c.n - row0 < p.pass_rows ? c.n - row0 : p.pass_rows;
+        s.loss = loss, s.kept = saved, s.whole = !h.large && !c.top_class && c.l->classes <= Large::BA;
         if (h.large) q.s = s, launch_scores_stage<T, false>(q, c.stream);
         else launch_scores<T, false>(s, c.stream);
+        if (s.whole) continue;  // (every tile has all classes)
         if (c.top_class) k_class_top<T><<<dim3((unsigned)ceil_div(r.rows * r.top, 32)), dim3(256), 0, c.stream>>>(r);
         const int values = c.top_class && r.top > p.class_parts ? r.top : p.class_parts;
         if (values <= 8) k_class_finish<T, 4><<<dim3((unsigned)ceil_div(r.rows, 64)), dim3(256), 0, c.stream>>>(r);
@@ -1074,12 +1105,16 @@ int forward(const Call &c, float *loss, float *teacher_loss, float *saved)
 }
 
 template <class T, bool OC>
-void launch_product(PieceArgs<T> &a, hipStream_t st)
+void launch_product(PieceArgs<T> &a, int tile, hipStream_t st)
 {
-    a.row_tiles = ceil_div(a.M, 128), a.col_tiles = (int)ceil_div(a.N, 128);
-    const dim3 grid((unsigned)tile_count(a.row_tiles, a.col_tiles), (unsigned)a.shares);
-    if (a.N >= T::VEC) k_class_product<T, Large, OC, false><<<grid, dim3(kThreads), 0, st>>>(a);
-    else k_class_product<T, Large, OC, true><<<grid, dim3(kThreads), 0, st>>>(a);
+    const auto go = [&](auto cut, auto narrow) {
+        using C = decltype(cut);
+        a.row_tiles = ceil_div(a.M, C::BA), a.col_tiles = (int)ceil_div(a.N, C::BB);
+        k_class_product<T, C, OC, decltype(narrow)::value><<<dim3((unsigned)tile_count(a.row_tiles, a.col_tiles), (unsigned)a.shares), dim3(kThreads), 0, st>>>(a);
+    };
+    if (a.N < T::VEC) go(Small{}, std::true_type{});  // (Large has the same rows of shorter than 16 bytes to read; one form of that will do)
+    else if (tile == 64) go(Small{}, std::false_type{});
+    else go(Large{}, std::false_type{});
 }
 template <class T, bool OC>
 void launch_product_stage(StagePieceArgs<T> &a, hipStream_t st)
@@ -1088,10 +1123,9 @@ void launch_product_stage(StagePieceArgs<T> &a, hipStream_t st)
     k_class_product_stage<T, OC><<<dim3((unsigned)(tile_count(a.row_tiles, a.col_tiles) * a.shares)), dim3(stage::kThreads), 0, st>>>(a);
 }
 template <class T>
-void launch_reduce(const float *slots, int64_t slot_values, int64_t rows, int width, int shares, typename T::elem *out, int64_t stride, hipStream_t st)
+void launch_reduce(const ReduceArgs<T> &a, hipStream_t st)
 {
-    ReduceArgs<T> a{slots, slot_values, rows * width, width, shares, out, stride};
-    k_class_reduce<T><<<dim3((unsigned)ceil_div(a.count, 256)), dim3(256), 0, st>>>(a);
+    k_class_reduce<T><<<dim3((unsigned)ceil_div(a.rows * a.width + (a.sums ? a.rows : 0), 256)), dim3(256), 0, st>>>(a);
 }
 
 template <class T>
@@ -1126,12 +1160,11 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
         for (int64_t rp = 0; rp < p.row_pieces; ++rp) {
             const int64_t row0 = rp * p.piece_rows, rows = c.n - row0 < p.piece_rows ? c.n - row0 : p.piece_rows;
             s.row0 = r.row0 = row0, s.rows = r.rows = rows, s.class0 = r.class0 = class0, r.piece_classes = classes, s.classes = class0 + classes;
-            r.listed = listed + row0;
             if (h.large) {
                 q.s = s;
                 launch_scores_stage<T, true>(q, c.stream);
             } else {
-                if (cp == 0 && dweight) k_class_rows<T><<<dim3((unsigned)ceil_div(rows, 256)), dim3(256), 0, c.stream>>>(r);
+                s.listed = cp == 0 && dweight ? listed + row0 : nullptr;
                 launch_scores<T, true>(s, c.stream);
             }
             if (r.teacher_scale != 0.0f) k_class_fix<T><<<dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, c.stream>>>(r);
@@ -1148,9 +1181,9 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
                 a.a = dz, a.a_stride = p.dz_stride, a.b = s.w + (int64_t)class0 * D, a.b_stride = D, a.M = rows, a.K = classes, a.N = D, a.a_width = (int)p.dz_stride;
                 a.shares = p.dx_shares, a.per_share = p.dx_per, a.out = dx + row0 * dx_stride, a.out_stride = dx_stride;
                 a.slots = slots, a.slot_rows = slot_rows, a.add = cp > 0;
-                launch_product<T, false>(a, c.stream);
+                launch_product<T, false>(a, p.dx_tile, c.stream);
             }
-            if (slots && dx && p.class_pieces == 1) launch_reduce<T>(slots, rows * D, rows, D, p.dx_shares, dx + row0 * dx_stride, dx_stride, c.stream);
+            if (slots && dx && p.class_pieces == 1) launch_reduce<T>({slots, nullptr, rows, rows, D, p.dx_shares, dx + row0 * dx_stride, nullptr, dx_stride}, c.stream);
             if (!dweight) continue;
             const auto fill = [&](auto &a) {
                 a.M = classes, a.N = D, a.shares = p.dw_shares, a.per_share = p.dw_per;
@@ -1167,13 +1200,13 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
                 PieceArgs<T> a{};
                 fill(a);
                 a.a = dz, a.a_stride = p.dz_stride, a.b = s.x + row0 * c.x_stride, a.b_stride = c.x_stride, a.list = listed + row0, a.K = rows, a.a_width = (int)p.dz_stride;
-                launch_product<T, true>(a, c.stream);
+                launch_product<T, true>(a, p.dw_tile, c.stream);
             }
         }
-        if (p.dw_bytes && dweight) launch_reduce<T>(dw_slots, (int64_t)p.piece_classes * D, classes, D, p.dw_shares, dweight + (int64_t)class0 * D, D, c.stream);
-        if (p.dw_bytes && dbias) launch_reduce<T>(db_slots, p.piece_classes, 1, classes, p.dw_shares, dbias + class0, classes, c.stream);
+        if (p.dw_bytes && dweight)
+            launch_reduce<T>({dw_slots, db_slots, p.piece_classes, classes, D, p.dw_shares, dweight + (int64_t)class0 * D, dbias ? dbias + class0 : nullptr, D}, c.stream);
     }
-    if (p.dx_bytes && dx && p.class_pieces > 1) launch_reduce<T>(dx_slots, c.n * D, c.n, D, p.dx_shares, dx, dx_stride, c.stream);
+    if (p.dx_bytes && dx && p.class_pieces > 1) launch_reduce<T>({dx_slots, nullptr, c.n, c.n, D, p.dx_shares, dx, nullptr, dx_stride}, c.stream);
     BGL_HIP(hipGetLastError());
     return BGL_OK;
 }

@@ -17,7 +17,7 @@ namespace {
 using namespace tile;
 
 constexpr int kValues = 16;          // of a row a thread holds
-constexpr int kMaxParts = 1024;      // workgroups of a backward call that sums weight gradients, so rows of its partial sums
+constexpr int kMaxParts = 512;       // workgroups of a backward call that sums weight gradients, so rows of its partial sums
 constexpr float kFar = 0x1p-80f;     // scales rows whose squares leave fp32's range
 
 template <class T>
