@@ -416,6 +416,24 @@ struct PieceArgs {
     bool add;                       // to what is in the slots
 };
 
+// The sums that a lane has of a product's tile: f(value, row, column) for each that exists.
+template <class C, class F>
+__device__ __forceinline__ void each_sum(int64_t m0, int64_t M, int n0, int N, f32x4 (&acc)[C::FA][C::FB], F f)
+{
+    const int l = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < C::FA; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t m = m0 + C::a_off() + 16 * i + 4 * (l >> 4) + j;
+#pragma unroll
+            for (int t = 0; t < C::FB; ++t) {
+                const int c = n0 + C::b_off() + 16 * t + (l & 15);
+                if (m < M && c < N) acc[i][t][j] = f(acc[i][t][j], m, c);
+            }
+        }
+}
+
 // M x N = A B over the summed index, B's rows being that index.  OC: A's rows too (dW: they are batch rows), else A's rows are the result's (dx).
 template <class T, class C, bool OC, bool NARROW>
 __global__ void __launch_bounds__(kThreads, 2) k_class_product(PieceArgs<T> a)
@@ -430,6 +448,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_product(PieceArgs<T> a)
     const int64_t m0 = rt * C::BA, k0 = share * a.per_share;
     const int n0 = ct * C::BB, K = (int)(a.K - k0 < a.per_share ? a.K - k0 : a.per_share);
     f32x4 acc[C::FA][C::FB] = {};
+    float *slot = a.slots ? a.slots + share * a.slot_rows * a.N : nullptr;
+    // (what is there already goes before the products: added behind them, value by value, it took longer than they did)
+    if (slot && a.add) each_sum<C>(m0, a.M, n0, a.N, acc, [&](float, int64_t m, int c) { return slot[m * a.N + c]; });
     float sums[C::FA] = {};
     const bool summing = OC && (a.sums || a.sum_slots) && n0 == 0 && C::b_off() == 0;
     if (K > 0) {
@@ -467,26 +488,11 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_product(PieceArgs<T> a)
             });
     }
     const int l = threadIdx.x & 63;
-    float *slot = a.slots ? a.slots + share * a.slot_rows * a.N : nullptr;
-#pragma unroll
-    for (int i = 0; i < C::FA; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t m = m0 + C::a_off() + 16 * i + 4 * (l >> 4) + j;
-            if (m >= a.M) continue;
-#pragma unroll
-            for (int t = 0; t < C::FB; ++t) {
-                const int c = n0 + C::b_off() + 16 * t + (l & 15);
-                if (c >= a.N) continue;
-                float v = acc[i][t][j];
-                if (slot) {
-                    float *to = slot + m * a.N + c;
-                    *to = a.add ? *to + v : v;
-                } else {
-                    a.out[m * a.out_stride + c] = T::put(v);
-                }
-            }
-        }
+    each_sum<C>(m0, a.M, n0, a.N, acc, [&](float v, int64_t m, int c) {
+        if (slot) slot[m * a.N + c] = v;
+        else a.out[m * a.out_stride + c] = T::put(v);
+        return v;
+    });
     if (summing) {
 #pragma unroll
         for (int t = 0; t < C::FA; ++t) {
@@ -503,35 +509,52 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_product(PieceArgs<T> a)
     }
 }
 
-// Sums over ranges: of `rows` x width values, and of `rows` more (db) if there are.
+// Sums over ranges: of rows x width values, four of a row a thread, and of `rows` more (db).
 template <class T>
 struct ReduceArgs {
     const float *slots, *sum_slots;
-    int64_t slot_rows, rows;  // of a slot; of the result
-    int width, shares;
-    typename T::elem *out, *sums;
+    int64_t slot_rows, rows;       // of a slot (sum_slots: `rows`); of the result
+    int slot_width, width, shares, sum_shares;
+    typename T::elem *out, *sums;  // either may be null
     int64_t out_stride;
 };
 template <class T>
 __global__ void __launch_bounds__(256) k_class_reduce(ReduceArgs<T> a)
 {
-    const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x, values = (uint64_t)a.rows * a.width;
-    const bool second = i >= values;
-    const uint64_t at = second ? i - values : i, step = a.slot_rows * (second ? 1 : a.width);
-    if (second && (!a.sums || at >= (uint64_t)a.rows)) return;
-    const float *from = (second ? a.sum_slots : a.slots) + at;
-    float s = 0.0f;
-    int p = 0;
-    for (; p + 8 <= a.shares; p += 8) {  // (eight on their way at a time)
-        float v[8];
+    const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint32_t fours = (uint32_t)(a.width + 3) / 4;
+    const uint64_t values = a.out ? (uint64_t)a.rows * fours : 0;
+    if (i < values) {
+        const uint64_t row = values >> 32 ? i / fours : (uint32_t)i / fours;
+        const int c = (int)(i - row * fours) * 4;
+        const float *from = a.slots + row * a.slot_width + c;
+        const int64_t step = a.slot_rows * a.slot_width;
+        f32x4 s = {};
+        int p = 0;
+        for (; p + 4 <= a.shares; p += 4) {  // (four on their way at a time)
+            f32x4 v[4];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) v[u] = from[(p + u) * step];
+            for (int u = 0; u < 4; ++u) v[u] = load_any<f32x4>(from + (p + u) * step);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) s += v[u];
+            for (int u = 0; u < 4; ++u) s += v[u];
+        }
+        for (; p < a.shares; ++p) s += load_any<f32x4>(from + p * step);
+        typename T::elem e[4], *to = a.out + row * a.out_stride + c;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) e[j] = T::put(s[j]);
+        if (c + 4 <= a.width) {
+            __builtin_memcpy(to, e, sizeof(e));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+                if (c + j < a.width) to[j] = e[j];
+        }
+    } else if (a.sums && i - values < (uint64_t)a.rows) {
+        const float *from = a.sum_slots + (i - values);
+        float s = 0.0f;
+        for (int p = 0; p < a.sum_shares; ++p) s += from[p * a.rows];
+        a.sums[i - values] = T::put(s);
     }
-    for (; p < a.shares; ++p) s += from[p * step];
-    if (second) a.sums[at] = T::put(s);
-    else a.out[a.out_stride == a.width ? at : at / (uint32_t)a.width * a.out_stride + at % (uint32_t)a.width] = T::put(s);
 }
 template <class T>
 __global__ void __launch_bounds__(256) k_class_zero(typename T::elem *p, int64_t count)
@@ -635,7 +658,7 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
         }
     }
     f32x4 acc[C::FA][C::FB] = {};
-    stage::multiply<PLANES, A, B, C>(lds, weight, rows, stage::Walk{2 * kPad, 2 * kPad, q.w_plane, q.x_plane, a.D, 0}, acc, [](int, const auto &) {});
+    stage::multiply<PLANES, false, A, B, C>(lds, weight, rows, stage::Walk{2 * kPad, 2 * kPad, q.w_plane, q.x_plane, a.D, 0}, acc, [](int, int, const auto &) {});
 
     if ((uint32_t)my_label >= (uint32_t)a.all_classes) my_label = -1, my_lse = INFINITY;
     struct Own {
@@ -769,12 +792,17 @@ struct StagePieceArgs {
     int64_t row_tiles;
     int col_tiles, shares;
     int64_t per_share;                 // a multiple of 32
-    typename T::elem *out, *sums;
+    typename T::elem *out;
     int64_t out_stride;
-    float *slots, *sum_slots;
-    int64_t slot_rows;
+    float *slots, *sum_slots;          // sums: shares x min(kSummers, column tiles) x 2 of them
+    int64_t slot_rows;                 // of a slot, a multiple of the tiles' as slot_width is
+    int slot_width;
     bool add;
 };
+
+// dz's sums over the rows are made by the tiles of the first columns and both halves of their wavefronts in turn, a stage each: made by one of them they took a
+// seventh of the whole product's time.
+constexpr int kSummers = 4;
 
 template <class T, bool OC>
 __global__ void __launch_bounds__(stage::kThreads, 2) k_class_product_stage(StagePieceArgs<T> a)
@@ -806,10 +834,20 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_product_stage(Stag
     const uint32_t a_block = OC ? 2 * down : BLOCK;
     right.init(a.b + k0 * a.b_bytes, (uint32_t)a.b_bytes, n0, a.b_width);
     f32x4 acc[C::FA][C::FB] = {};
+    const int l = threadIdx.x & 63;
+    // slots are whole tiles: nothing of theirs is beyond an edge.  What is there already goes before the products.
+    float *slot = a.slots ? a.slots + (share * a.slot_rows + m0 + C::a_off() + (l & 15)) * a.slot_width + n0 + C::b_off() + 4 * (l >> 4) : nullptr;
+    if (slot && a.add) {
+#pragma unroll
+        for (int i = 0; i < C::FA; ++i)
+#pragma unroll
+            for (int t = 0; t < C::FB; ++t) acc[i][t] = *reinterpret_cast<const f32x4 *>(slot + 16 * i * (int64_t)a.slot_width + 16 * t);
+    }
     float sums[C::FA] = {};
-    const bool summing = OC && (a.sums || a.sum_slots) && n0 == 0 && C::b_off() == 0;
-    stage::multiply<PLANES, A, B, C>(lds, left, right, stage::Walk{a_block, (uint32_t)(A::STEP * a.b_bytes), kBlockValues * 2, a.b_plane, K, 0}, acc, [&](int b_plane, const auto &f) {
-        if (summing && b_plane == 0) {
+    const int summers = a.col_tiles < kSummers ? a.col_tiles : kSummers, summer = 2 * ct + (C::b_off() > 0);
+    const bool summing = OC && a.sum_slots && ct < summers;
+    stage::multiply<PLANES, true, A, B, C>(lds, left, right, stage::Walk{a_block, (uint32_t)(A::STEP * a.b_bytes), kBlockValues * 2, a.b_plane, K, 0}, acc, [&](int s, int b_plane, const auto &f) {
+        if (summing && b_plane == 0 && (PLANES == 1 ? s : s / 6) % (2 * summers) == summer) {
 #pragma unroll
             for (int t = 0; t < C::FA; ++t) {
                 const uint4 v = __builtin_bit_cast(uint4, f[t]);
@@ -817,39 +855,36 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_product_stage(Stag
             }
         }
     });
-    const int l = threadIdx.x & 63;
-    float *slot = a.slots ? a.slots + share * a.slot_rows * a.N : nullptr;
+    const int64_t m1 = m0 + C::a_off() + (l & 15);
+    const int c1 = n0 + C::b_off() + 4 * (l >> 4);
+    if (slot) {
 #pragma unroll
-    for (int i = 0; i < C::FA; ++i)
+        for (int i = 0; i < C::FA; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t m = m0 + C::a_off() + 16 * i + 4 * (l >> 4) + j;
-            if (m >= a.M) continue;
+            for (int t = 0; t < C::FB; ++t) *reinterpret_cast<f32x4 *>(slot + 16 * i * (int64_t)a.slot_width + 16 * t) = acc[i][t];
+    } else {
+        typename T::elem *to = a.out + m1 * a.out_stride + c1;
+#pragma unroll
+        for (int i = 0; i < C::FA; ++i) {
+            if (m1 + 16 * i >= a.M) break;
 #pragma unroll
             for (int t = 0; t < C::FB; ++t) {
-                const int c = n0 + C::b_off() + 16 * t + (l & 15);
-                if (c >= a.N) continue;
-                const float v = acc[i][t][j];
-                if (slot) {
-                    float *to = slot + m * a.N + c;
-                    *to = a.add ? *to + v : v;
-                } else {
-                    a.out[m * a.out_stride + c] = T::put(v);
-                }
+                typename T::elem e[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) e[j] = T::put(acc[i][t][j]);
+                if (c1 + 16 * t < a.N) __builtin_memcpy(to + 16 * t, e, sizeof(e));  // (N is a multiple of 4)
             }
+            to += 16 * a.out_stride;
         }
+    }
     if (summing) {
 #pragma unroll
         for (int t = 0; t < C::FA; ++t) {
             const float v = down_column(sums[t], [](float p, float q) { return p + q; });
             const int64_t m = m0 + C::a_off() + 16 * t + (l & 15);
             if (l >= 16 || m >= a.M) continue;
-            if (a.sum_slots) {
-                float *to = a.sum_slots + share * a.slot_rows + m;
-                *to = a.add ? *to + v : v;
-            } else {
-                a.sums[m] = T::put(v);
-            }
+            float *to = a.sum_slots + ((int64_t)share * 2 * summers + summer) * a.M + m;
+            *to = a.add ? *to + v : v;
         }
     }
 }
@@ -868,8 +903,7 @@ struct Plan {
     size_t part_bytes, label_bytes, top_bytes, forward_bytes;
     // backward
     int64_t piece_rows, row_pieces, dz_stride;
-    int piece_classes, class_pieces, dx_shares, dw_shares, dx_tile, dw_tile;
-    int64_t dx_per, dw_per;
+    int piece_classes, class_pieces, dx_shares, dx_tile, slot_width;
     size_t dz_bytes, list_bytes, dx_bytes, dw_bytes, db_bytes, backward_bytes;
     // large calls: laid out operands, forward (0: as they are) and backward
     int padded;
@@ -883,13 +917,14 @@ struct Scheme {
     int score_classes, product_rows;  // of a tile
     int64_t values, round_classes, round_rows;
     int dz_value_bytes, planes;
+    int slot_round;                   // rows of a slot
     int64_t fill, least;              // ranges of a product's summed index: workgroups they are to make together, of the index for each
 };
 Scheme scheme_of(const bgl_class_loss_t *l, bool large)
 {
     const bool f32 = l->dtype == BGL_F32;
-    if (large) return Scheme{true, StageCut::BA, ProductCut::BA, ((int64_t)1 << 27) + ((int64_t)1 << 23), StageCut::BA, StageCut::BB, f32 ? 6 : 2, f32 ? 3 : 1, 2 * kCus, 512};
-    return Scheme{false, 128, 128, (int64_t)1 << 25, 8, 1, f32 ? 4 : 2, 1, kCus, 64};  // (pieces of 4 classes are stored, and 16 bytes of bf16 read)
+    if (large) return Scheme{true, StageCut::BA, ProductCut::BA, ((int64_t)1 << 27) + ((int64_t)1 << 23), StageCut::BA, StageCut::BB, f32 ? 6 : 2, f32 ? 3 : 1, ProductCut::BA, 2 * kCus, 512};
+    return Scheme{false, 128, 128, (int64_t)1 << 25, 8, 1, f32 ? 4 : 2, 1, 1, kCus, 64};  // (pieces of 4 classes are stored, and 16 bytes of bf16 read)
 }
 bool large_call(const bgl_class_loss_t *l, int64_t n) { return n >= 256 && l->classes >= 128 && (double)n * l->classes * l->in_dim >= kLargeProducts; }
 bool laid_out(const bgl_class_loss_t *l) { return l->dtype == BGL_BF16 && l->in_dim % kPad == 0; }
@@ -906,6 +941,29 @@ int shares_for(const Scheme &s, int64_t rows, int64_t cols, int64_t summed, int 
     int64_t tiles = ceil_div(rows, tile) * ceil_div(cols, 128);
     if (!s.large && tiles * fit(tiles) < s.fill / 2) tile = 64, tiles = ceil_div(rows, 64) * ceil_div(cols, 64);
     return (int)fit(tiles);
+}
+
+size_t slot_bytes(int64_t shares, int64_t rows, int64_t width) { return round_up((size_t)(shares * rows * width) * 4 + 16, 256); }  // (rows are read four values at a time)
+int64_t per_share(int64_t summed, int shares) { return (int64_t)round_up((size_t)ceil_div(summed, shares), 64); }
+int shares_used(int64_t summed, int shares) { return (int)ceil_div(summed, per_share(summed, shares)); }  // (none is empty)
+
+// dW of a piece of classes.
+struct WeightPlan {
+    int shares, tile;
+    bool slots;
+};
+WeightPlan weight_plan(const bgl_class_loss_t *l, const Scheme &s, int classes, int64_t piece_rows, int64_t row_pieces)
+{
+    WeightPlan w{};
+    w.shares = shares_for(s, classes, l->in_dim, piece_rows, w.tile);
+    w.shares = piece_rows > 0 ? shares_used(piece_rows, w.shares) : 1;
+    w.slots = w.shares > 1 || row_pieces > 1 || (s.large && l->in_dim % 4);  // (large tiles are written four values of a row at a time)
+    return w;
+}
+int summers_of(const bgl_class_loss_t *l, const Scheme &s)
+{
+    const int64_t tiles = ceil_div(l->in_dim, ProductCut::BB);
+    return s.large ? 2 * (int)(tiles < kSummers ? tiles : kSummers) : 1;
 }
 
 Plan plan_of(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
@@ -947,14 +1005,18 @@ Plan plan_of(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
     p.dz_stride = round_up(p.piece_classes, s.round_classes);
     p.dz_bytes = round_up(round_up(p.piece_rows, s.round_rows) * p.dz_stride * s.dz_value_bytes, 256);
     p.list_bytes = s.large ? 0 : round_up((size_t)n * 4, 256);
+    p.slot_width = s.large ? (int)round_up(l->in_dim, ProductCut::BB) : l->in_dim;
     p.dx_shares = shares_for(s, p.piece_rows, l->in_dim, p.piece_classes, p.dx_tile);
-    if (p.class_pieces > 1 && p.row_pieces > 1) p.dx_shares = 1;
-    p.dx_per = round_up((size_t)ceil_div(p.piece_classes, p.dx_shares), 64);
-    p.dw_shares = shares_for(s, p.piece_classes, l->in_dim, p.piece_rows, p.dw_tile);
-    p.dw_per = round_up((size_t)ceil_div(p.piece_rows, p.dw_shares), 64);
-    p.dx_bytes = p.dx_shares > 1 || p.class_pieces > 1 ? round_up((size_t)p.dx_shares * (p.class_pieces > 1 ? n : p.piece_rows) * l->in_dim * 4, 256) : 0;
-    p.dw_bytes = p.dw_shares > 1 || p.row_pieces > 1 ? round_up((size_t)p.dw_shares * p.piece_classes * l->in_dim * 4, 256) : 0;
-    p.db_bytes = p.dw_bytes ? round_up((size_t)p.dw_shares * p.piece_classes * 4, 256) : 0;
+    p.dx_shares = p.class_pieces > 1 && p.row_pieces > 1 ? 1 : shares_used(p.piece_classes, p.dx_shares);
+    p.dx_bytes = p.dx_shares > 1 || p.class_pieces > 1 || (s.large && l->in_dim % 4) ? slot_bytes(p.dx_shares, round_up(p.class_pieces > 1 ? n : p.piece_rows, s.slot_round), p.slot_width) : 0;
+    const int last = l->classes - (p.class_pieces - 1) * p.piece_classes;
+    for (const int classes : {p.piece_classes, last}) {
+        const WeightPlan w = weight_plan(l, s, classes, p.piece_rows, p.row_pieces);
+        const size_t dw = w.slots ? slot_bytes(w.shares, round_up(classes, s.slot_round), p.slot_width) : 0;
+        const size_t db = w.slots || s.large ? round_up((size_t)w.shares * summers_of(l, s) * classes * 4, 256) : 0;
+        if (dw > p.dw_bytes) p.dw_bytes = dw;
+        if (db > p.db_bytes) p.db_bytes = db;
+    }
     p.backward_bytes = p.dz_bytes + p.list_bytes + p.dx_bytes + p.dw_bytes + p.db_bytes + p.back_x_bytes + p.w_bytes;
     return p;
 }
@@ -969,10 +1031,14 @@ size_t backward_room(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
     const int64_t over = (many ? kPieceClasses * least(n, kPieceRows) : 128 * stride) + 128 * least(stride, s.values);
     const Plan p = plan_of(l, n, s);
     size_t bytes = round_up((size_t)least(round_up(n, 128) * stride, s.values + over) * s.dz_value_bytes, 256) + round_up((size_t)n * 4, 256) + p.back_x_bytes + p.w_bytes;
-    if (V >= 2 * s.least) bytes += round_up((size_t)most(many ? n : 0, least(shared, n * (V / s.least))) * D * 4, 256);
-    const int64_t shares = n >= 2 * s.least ? least(shared, V * (n / s.least)) : 0;
-    const int64_t pieces = many ? (n > kPieceRows ? s.values / kPieceRows + kPieceClasses : 0) : n * stride > s.values ? V : 0;
-    bytes += round_up((size_t)most(shares, pieces) * D * 4, 256) + round_up((size_t)most(shares, pieces) * 4, 256);
+    // (ranges of the summed index leave s.fill tiles at most; a result of one range is rounded up to tiles)
+    const int64_t width = s.large ? round_up(D, ProductCut::BB) : D, up = s.slot_round;
+    const bool odd = s.large && D % 4;
+    if (V >= 2 * s.least || (many && n > 0) || odd) bytes += slot_bytes(1, most(many || odd ? round_up(n, up) : 0, least(shared, round_up(n, up) * (V / s.least))), width);
+    const int64_t shares = n >= 2 * s.least ? least(shared, round_up(V, up) * (n / s.least)) : 0;
+    const int64_t pieces = round_up(many ? (n > kPieceRows ? s.values / kPieceRows + kPieceClasses : 0) : n * stride > s.values ? V : 0, up), odd_pieces = odd ? round_up(V, up) : 0;
+    const int64_t sums = most(most(most(shares, pieces), odd_pieces), s.large ? least(V, s.values / 128) : 0) * summers_of(l, s);
+    bytes += slot_bytes(1, most(most(shares, pieces), odd_pieces), width) + round_up((size_t)sums * 4, 256);
     return bytes > p.backward_bytes ? bytes : p.backward_bytes;
 }
 
@@ -1125,7 +1191,7 @@ void launch_product_stage(StagePieceArgs<T> &a, hipStream_t st)
 template <class T>
 void launch_reduce(const ReduceArgs<T> &a, hipStream_t st)
 {
-    k_class_reduce<T><<<dim3((unsigned)ceil_div(a.rows * a.width + (a.sums ? a.rows : 0), 256)), dim3(256), 0, st>>>(a);
+    k_class_reduce<T><<<dim3((unsigned)ceil_div((a.out ? a.rows * ceil_div(a.width, 4) : 0) + (a.sums ? a.rows : 0), 256)), dim3(256), 0, st>>>(a);
 }
 
 template <class T>
@@ -1157,6 +1223,8 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
     if (h.large) q = stage_args<T>(c, p, h, s, x_laid, w_laid, &r);
     for (int cp = 0; cp < p.class_pieces; ++cp) {
         const int class0 = cp * p.piece_classes, classes = V - class0 < p.piece_classes ? V - class0 : p.piece_classes;
+        const WeightPlan w = weight_plan(c.l, h, classes, p.piece_rows, p.row_pieces);
+        const int dx_shares = shares_used(classes, p.dx_shares);  // (the first piece's are the most)
         for (int64_t rp = 0; rp < p.row_pieces; ++rp) {
             const int64_t row0 = rp * p.piece_rows, rows = c.n - row0 < p.piece_rows ? c.n - row0 : p.piece_rows;
             s.row0 = r.row0 = row0, s.rows = r.rows = rows, s.class0 = r.class0 = class0, r.piece_classes = classes, s.classes = class0 + classes;
@@ -1168,45 +1236,49 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
                 launch_scores<T, true>(s, c.stream);
             }
             if (r.teacher_scale != 0.0f) k_class_fix<T><<<dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, c.stream>>>(r);
-            float *slots = p.dx_bytes ? dx_slots + (p.class_pieces > 1 ? row0 * D : 0) : nullptr;
-            const int64_t slot_rows = p.class_pieces > 1 ? c.n : rows;
+            float *slots = p.dx_bytes ? dx_slots + (p.class_pieces > 1 ? row0 * p.slot_width : 0) : nullptr;
+            const int64_t slot_rows = round_up(p.class_pieces > 1 ? c.n : rows, h.slot_round);
             if (dx && h.large) {
                 StagePieceArgs<T> a{};
                 a.a = (const char *)dz, a.a_rows = (int)round_up(rows, StageCut::BB), a.b = q.w + class0 * q.w_bytes, a.b_bytes = q.w_bytes, a.b_plane = q.w_plane;
-                a.M = rows, a.K = classes, a.N = D, a.a_stride = (int)p.dz_stride, a.b_width = p.padded, a.shares = p.dx_shares, a.per_share = p.dx_per;
-                a.out = dx + row0 * dx_stride, a.out_stride = dx_stride, a.slots = slots, a.slot_rows = slot_rows, a.add = cp > 0;
+                a.M = rows, a.K = classes, a.N = D, a.a_stride = (int)p.dz_stride, a.b_width = p.padded, a.shares = dx_shares, a.per_share = per_share(classes, dx_shares);
+                a.out = dx + row0 * dx_stride, a.out_stride = dx_stride, a.slots = slots, a.slot_rows = slot_rows, a.slot_width = p.slot_width, a.add = cp > 0;
                 launch_product_stage<T, false>(a, c.stream);
             } else if (dx) {
                 PieceArgs<T> a{};
                 a.a = dz, a.a_stride = p.dz_stride, a.b = s.w + (int64_t)class0 * D, a.b_stride = D, a.M = rows, a.K = classes, a.N = D, a.a_width = (int)p.dz_stride;
-                a.shares = p.dx_shares, a.per_share = p.dx_per, a.out = dx + row0 * dx_stride, a.out_stride = dx_stride;
+                a.shares = dx_shares, a.per_share = per_share(classes, dx_shares), a.out = dx + row0 * dx_stride, a.out_stride = dx_stride;
                 a.slots = slots, a.slot_rows = slot_rows, a.add = cp > 0;
                 launch_product<T, false>(a, p.dx_tile, c.stream);
             }
-            if (slots && dx && p.class_pieces == 1) launch_reduce<T>({slots, nullptr, rows, rows, D, p.dx_shares, dx + row0 * dx_stride, nullptr, dx_stride}, c.stream);
+            if (slots && dx && p.class_pieces == 1) launch_reduce<T>({slots, nullptr, slot_rows, rows, p.slot_width, D, dx_shares, 0, dx + row0 * dx_stride, nullptr, dx_stride}, c.stream);
             if (!dweight) continue;
             const auto fill = [&](auto &a) {
-                a.M = classes, a.N = D, a.shares = p.dw_shares, a.per_share = p.dw_per;
-                a.out = dweight + (int64_t)class0 * D, a.out_stride = D, a.sums = dbias ? dbias + class0 : nullptr;
-                if (p.dw_bytes) a.slots = dw_slots, a.sum_slots = dbias ? db_slots : nullptr, a.slot_rows = p.piece_classes, a.add = rp > 0;
+                a.M = classes, a.N = D, a.shares = shares_used(rows, w.shares), a.per_share = per_share(rows, a.shares);
+                a.out = dweight + (int64_t)class0 * D, a.out_stride = D, a.slot_rows = round_up(classes, h.slot_round), a.add = rp > 0;
+                if (w.slots) a.slots = dw_slots;
+                if (dbias && (w.slots || h.large)) a.sum_slots = db_slots;
             };
             if (h.large) {
                 StagePieceArgs<T> a{};
                 fill(a);
+                a.slot_width = p.slot_width;
                 a.a = (const char *)dz, a.a_rows = (int)round_up(rows, StageCut::BB), a.b = q.x + row0 * q.x_bytes, a.b_bytes = q.x_bytes, a.b_plane = q.x_plane;
                 a.a_stride = (int)p.dz_stride, a.b_width = p.padded, a.K = round_up(rows, 32);  // (rows of zeros in both)
                 launch_product_stage<T, true>(a, c.stream);
             } else {
                 PieceArgs<T> a{};
                 fill(a);
+                a.sums = dbias ? dbias + class0 : nullptr;
                 a.a = dz, a.a_stride = p.dz_stride, a.b = s.x + row0 * c.x_stride, a.b_stride = c.x_stride, a.list = listed + row0, a.K = rows, a.a_width = (int)p.dz_stride;
-                launch_product<T, true>(a, p.dw_tile, c.stream);
+                launch_product<T, true>(a, w.tile, c.stream);
             }
         }
-        if (p.dw_bytes && dweight)
-            launch_reduce<T>({dw_slots, db_slots, p.piece_classes, classes, D, p.dw_shares, dweight + (int64_t)class0 * D, dbias ? dbias + class0 : nullptr, D}, c.stream);
+        // (small calls without slots have written both already, large ones dweight)
+        E *dw_out = dweight && w.slots ? dweight + (int64_t)class0 * D : nullptr, *db_out = dbias && (w.slots || h.large) ? dbias + class0 : nullptr;
+        if (dw_out || db_out) launch_reduce<T>({dw_slots, db_slots, (int64_t)round_up(classes, h.slot_round), classes, p.slot_width, D, w.shares, w.shares * summers_of(c.l, h), dw_out, db_out, D}, c.stream);
     }
-    if (p.dx_bytes && dx && p.class_pieces > 1) launch_reduce<T>({dx_slots, nullptr, c.n, c.n, D, p.dx_shares, dx, nullptr, dx_stride}, c.stream);
+    if (p.dx_bytes && dx && p.class_pieces > 1) launch_reduce<T>({dx_slots, nullptr, (int64_t)round_up(c.n, h.slot_round), c.n, p.slot_width, D, p.dx_shares, 0, dx, nullptr, dx_stride}, c.stream);
     BGL_HIP(hipGetLastError());
     return BGL_OK;
 }

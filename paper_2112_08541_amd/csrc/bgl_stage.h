@@ -193,7 +193,7 @@ __device__ __forceinline__ bool tile_of(uint32_t id, uint32_t slow_tiles, uint32
 // How a product goes through its operands: bytes from one stage's summed values to the next, and from one plane to the next.
 struct Walk {
     uint32_t a_block, b_block, a_plane, b_plane;
-    int count;  // of the summed index
+    int count;  // of the summed index, more than 0
     int first;  // stage the product begins with, less than their number; it goes round
 };
 
@@ -211,8 +211,8 @@ constexpr int stages() { return 81920 / (A::BYTES + B::BYTES); }
 template <class A, class B>
 constexpr int lds_bytes() { return stages<A, B>() * (A::BYTES + B::BYTES); }
 
-// Adds the product to acc.  PLANES: 1, or 3 (six products).  also(plane of b, a's fragments) sees every 32 summed values.  Ends with all of LDS free.
-template <int PLANES, class A, class B, class C, class Also>
+// Adds the product to acc: of a fragment pair a lane has rows 4 (lane / 16) .. + 3 of a and row lane % 16 of b, TURNED the other way round.  PLANES: 1, or 3 (six products).  also(stage, plane of b, a's fragments) sees every 32 summed values.  Ends with all of LDS free.
+template <int PLANES, bool TURNED, class A, class B, class C, class Also>
 __device__ __forceinline__ void multiply(char *lds, const A &a, const B &b, const Walk &w, f32x4 (&acc)[C::FA][C::FB], Also also)
 {
     static_assert(A::STEP == B::STEP, "");
@@ -220,7 +220,6 @@ __device__ __forceinline__ void multiply(char *lds, const A &a, const B &b, cons
     static_assert(STAGES == 2 || STAGES == 3, "");
     constexpr uint32_t PLANE_A = 0x010210, PLANE_B = 0x211000;  // of pair p: hexadecimal digit p
     const int blocks = (w.count + STEP - 1) / STEP, steps = blocks * PAIRS;
-    if (steps <= 0) return;
     int block = w.first, pair = 0, to = 0;  // of the next stage to load
     const auto load = [&] {
         char *at = lds + to * BYTES;
@@ -237,7 +236,8 @@ __device__ __forceinline__ void multiply(char *lds, const A &a, const B &b, cons
     for (int s = 0; s < STAGES - 1; ++s)
         if (s < steps) load();
     int at = 0, plane = 0;
-    for (int s = 0; s < steps; ++s) {
+    int s = 0;
+    do {  // (a loop that may not run at all kept the sums before it beside those after it)
         // this stage's loads have come (all wavefronts': the barrier), and the buffer of the stage before has been read by all
         if (STAGES == 3 && s + 1 < steps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -253,13 +253,14 @@ __device__ __forceinline__ void multiply(char *lds, const A &a, const B &b, cons
 #pragma unroll
             for (int i = 0; i < C::FA; ++i)
 #pragma unroll
-                for (int j = 0; j < C::FB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
-            also(PLANE_B >> 4 * plane & 3, fa);
+                for (int j = 0; j < C::FB; ++j)
+                    acc[i][j] = TURNED ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0) : __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+            also(s, PLANE_B >> 4 * plane & 3, fa);
         }
         if (++plane == PAIRS) plane = 0;
         if (++at == STAGES) at = 0;
         asm volatile("" ::: "memory");
-    }
+    } while (++s < steps);
     __syncthreads();
 }
 
