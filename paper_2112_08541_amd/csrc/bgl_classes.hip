@@ -6,7 +6,7 @@
 //   k_class_scores   z tile by tile; forward: every tile's largest value and sums of exp, per row; backward: dz of a piece (rows x classes)
 //   k_class_top      forward: the scores of the teacher's classes; k_class_finish: the losses from all of that
 //   k_class_fix      backward: dz of the teacher's classes, over what k_class_scores left there
-//   k_class_product  dx = dz W and dW = dz' x of a piece, db = the sum of dz's rows; k_class_reduce: where several pieces or ranges share a result
+//   k_class_products  dx = dz W and dW = dz' x of a piece, db = the sum of dz's rows; k_class_reduce: where several pieces or ranges share a result
 #include "bgl_internal.h"
 #include "bgl_reduce.h"
 #include "bgl_stage.h"
@@ -408,6 +408,7 @@ struct PieceArgs {
     int N, a_width;                 // columns of the result; of dz that can be read
     int64_t row_tiles;
     int col_tiles, shares;
+    uint32_t tiles;                 // of a share, a multiple of 8
     int64_t per_share;              // of the summed index
     typename T::elem *out, *sums;   // the result, if it is whole; M values of sums over the summed index
     int64_t out_stride;
@@ -436,15 +437,19 @@ __device__ __forceinline__ void each_sum(int64_t m0, int64_t M, int n0, int N, f
 
 // M x N = A B over the summed index, B's rows being that index.  OC: A's rows too (dW: they are batch rows), else A's rows are the result's (dx).
 template <class T, class C, bool OC, bool NARROW>
-__global__ void __launch_bounds__(kThreads, 2) k_class_product(PieceArgs<T> a)
-{
+struct Product {
     using A = std::conditional_t<OC, OcOperand<T, C::BA, false, false>, KcOperand<T, C::BA>>;
     using B = OcOperand<T, C::BB, OC, NARROW>;
-    __shared__ __attribute__((aligned(16))) uint32_t lds[A::LDS + B::LDS];
-    const int share = blockIdx.y;
+    static constexpr int LDS = A::LDS + B::LDS;
+    static __device__ __forceinline__ void make(const PieceArgs<T> &a, uint32_t id, uint32_t *lds);
+};
+template <class T, class C, bool OC, bool NARROW>
+__device__ __forceinline__ void Product<T, C, OC, NARROW>::make(const PieceArgs<T> &a, uint32_t id, uint32_t *lds)
+{
+    const int share = (int)(id / a.tiles);
     int64_t rt;
     int ct;
-    if (!tile_of(blockIdx.x, a.row_tiles, a.col_tiles, rt, ct)) return;
+    if (!tile_of(id % a.tiles, a.row_tiles, a.col_tiles, rt, ct)) return;
     const int64_t m0 = rt * C::BA, k0 = share * a.per_share;
     const int n0 = ct * C::BB, K = (int)(a.K - k0 < a.per_share ? a.K - k0 : a.per_share);
     f32x4 acc[C::FA][C::FB] = {};
@@ -509,6 +514,17 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_product(PieceArgs<T> a)
     }
 }
 
+// Both products of a piece in one launch, dW's workgroups first: they need nothing of each other, and each fills what the other leaves free at its end.
+template <class T, class C, bool NARROW>
+__global__ void __launch_bounds__(kThreads, 2) k_class_products(PieceArgs<T> dw, PieceArgs<T> dx, uint32_t dw_groups)
+{
+    using W = Product<T, C, true, NARROW>;
+    using X = Product<T, C, false, NARROW>;
+    __shared__ __attribute__((aligned(16))) uint32_t lds[W::LDS > X::LDS ? W::LDS : X::LDS];
+    if (blockIdx.x < dw_groups) W::make(dw, blockIdx.x, lds);
+    else X::make(dx, blockIdx.x - dw_groups, lds);
+}
+
 // Sums over ranges: of rows x width values, four of a row a thread, and of `rows` more (db).
 template <class T>
 struct ReduceArgs {
@@ -519,9 +535,11 @@ struct ReduceArgs {
     int64_t out_stride;
 };
 template <class T>
-__global__ void __launch_bounds__(256) k_class_reduce(ReduceArgs<T> a)
+__global__ void __launch_bounds__(256) k_class_reduce(ReduceArgs<T> one, ReduceArgs<T> two, uint32_t one_groups)
 {
-    const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const bool first = blockIdx.x < one_groups;
+    const ReduceArgs<T> &a = first ? one : two;
+    const uint64_t i = (uint64_t)(first ? blockIdx.x : blockIdx.x - one_groups) * 256 + threadIdx.x;
     const uint32_t fours = (uint32_t)(a.width + 3) / 4;
     const uint64_t values = a.out ? (uint64_t)a.rows * fours : 0;
     if (i < values) {
@@ -780,7 +798,7 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
     }
 }
 
-// k_class_product from laid out operands: 256 x 128.  OC: dW, else dx.
+// k_class_products from laid out operands: 256 x 128.  OC: dW, else dx.
 template <class T>
 struct StagePieceArgs {
     const char *a, *b;                 // dz, in blocks; W or x
@@ -805,17 +823,21 @@ struct StagePieceArgs {
 constexpr int kSummers = 4;
 
 template <class T, bool OC>
-__global__ void __launch_bounds__(stage::kThreads, 2) k_class_product_stage(StagePieceArgs<T> a)
-{
+struct StageProduct {
     using C = ProductCut;
     using A = std::conditional_t<OC, stage::OcBlocks<C::BA>, stage::Kc<C::BA, kBlockClasses>>;
     using B = stage::Oc<C::BB>;
+    static constexpr int LDS = stage::lds_bytes<A, B>();
+    static __device__ __forceinline__ void make(const StagePieceArgs<T> &a, uint32_t id, char *lds);
+};
+template <class T, bool OC>
+__device__ __forceinline__ void StageProduct<T, OC>::make(const StagePieceArgs<T> &a, uint32_t id, char *lds)
+{
     constexpr int PLANES = T::PER == 1 ? 3 : 1;
-    __shared__ __attribute__((aligned(1024))) char lds[stage::lds_bytes<A, B>()];
-    const int share = blockIdx.x % a.shares;
+    const int share = (int)(id % (uint32_t)a.shares);
     int64_t rt;
     int ct;
-    if (!tile_of(blockIdx.x / a.shares, a.row_tiles, a.col_tiles, rt, ct)) return;
+    if (!tile_of(id / (uint32_t)a.shares, a.row_tiles, a.col_tiles, rt, ct)) return;
     const int64_t m0 = rt * C::BA, k0 = share * a.per_share;
     const int n0 = ct * C::BB, K = (int)(a.K - k0 < a.per_share ? a.K - k0 : a.per_share);
     A left;
@@ -887,6 +909,16 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_product_stage(Stag
             *to = a.add ? *to + v : v;
         }
     }
+}
+
+template <class T>
+__global__ void __launch_bounds__(stage::kThreads, 2) k_class_products_stage(StagePieceArgs<T> dw, StagePieceArgs<T> dx, uint32_t dw_groups)
+{
+    using W = StageProduct<T, true>;
+    using X = StageProduct<T, false>;
+    __shared__ __attribute__((aligned(1024))) char lds[W::LDS > X::LDS ? W::LDS : X::LDS];
+    if (blockIdx.x < dw_groups) W::make(dw, blockIdx.x, lds);
+    else X::make(dx, blockIdx.x - dw_groups, lds);
 }
 
 // ----------------------------------------------------------------- plans
@@ -1170,28 +1202,42 @@ int forward(const Call &c, float *loss, float *teacher_loss, float *saved)
     return BGL_OK;
 }
 
-template <class T, bool OC>
-void launch_product(PieceArgs<T> &a, int tile, hipStream_t st)
+// dW of a piece, dx of it, or both; tile: 64 or 128.
+template <class T>
+void launch_products(PieceArgs<T> *dw, PieceArgs<T> *dx, int tile, hipStream_t st)
 {
     const auto go = [&](auto cut, auto narrow) {
         using C = decltype(cut);
-        a.row_tiles = ceil_div(a.M, C::BA), a.col_tiles = (int)ceil_div(a.N, C::BB);
-        k_class_product<T, C, OC, decltype(narrow)::value><<<dim3((unsigned)tile_count(a.row_tiles, a.col_tiles), (unsigned)a.shares), dim3(kThreads), 0, st>>>(a);
+        uint32_t groups[2] = {};
+        for (int i = 0; i < 2; ++i)
+            if (PieceArgs<T> *a = i ? dx : dw) {
+                a->row_tiles = ceil_div(a->M, C::BA), a->col_tiles = (int)ceil_div(a->N, C::BB), a->tiles = (uint32_t)tile_count(a->row_tiles, a->col_tiles);
+                groups[i] = a->tiles * a->shares;
+            }
+        k_class_products<T, C, decltype(narrow)::value><<<dim3(groups[0] + groups[1]), dim3(kThreads), 0, st>>>(dw ? *dw : PieceArgs<T>{}, dx ? *dx : PieceArgs<T>{}, groups[0]);
     };
-    if (a.N < T::VEC) go(Small{}, std::true_type{});  // (Large has the same rows of shorter than 16 bytes to read; one form of that will do)
+    if ((dw ? dw : dx)->N < T::VEC) go(Small{}, std::true_type{});  // (one form of reading rows shorter than 16 bytes will do)
     else if (tile == 64) go(Small{}, std::false_type{});
     else go(Large{}, std::false_type{});
 }
-template <class T, bool OC>
-void launch_product_stage(StagePieceArgs<T> &a, hipStream_t st)
-{
-    a.row_tiles = ceil_div(a.M, ProductCut::BA), a.col_tiles = (int)ceil_div(a.N, ProductCut::BB);
-    k_class_product_stage<T, OC><<<dim3((unsigned)(tile_count(a.row_tiles, a.col_tiles) * a.shares)), dim3(stage::kThreads), 0, st>>>(a);
-}
 template <class T>
-void launch_reduce(const ReduceArgs<T> &a, hipStream_t st)
+void launch_products(StagePieceArgs<T> *dw, StagePieceArgs<T> *dx, hipStream_t st)
 {
-    k_class_reduce<T><<<dim3((unsigned)ceil_div((a.out ? a.rows * ceil_div(a.width, 4) : 0) + (a.sums ? a.rows : 0), 256)), dim3(256), 0, st>>>(a);
+    uint32_t groups[2] = {};
+    for (int i = 0; i < 2; ++i)
+        if (StagePieceArgs<T> *a = i ? dx : dw) {
+            a->row_tiles = ceil_div(a->M, ProductCut::BA), a->col_tiles = (int)ceil_div(a->N, ProductCut::BB);
+            groups[i] = (uint32_t)(tile_count(a->row_tiles, a->col_tiles) * a->shares);
+        }
+    k_class_products_stage<T><<<dim3(groups[0] + groups[1]), dim3(stage::kThreads), 0, st>>>(dw ? *dw : StagePieceArgs<T>{}, dx ? *dx : StagePieceArgs<T>{}, groups[0]);
+}
+// Either may have nothing to do.
+template <class T>
+void launch_reduce(const ReduceArgs<T> &one, const ReduceArgs<T> &two, hipStream_t st)
+{
+    const auto groups = [](const ReduceArgs<T> &a) { return (uint32_t)ceil_div((a.out ? a.rows * ceil_div(a.width, 4) : 0) + (a.sums ? a.rows : 0), 256); };
+    const uint32_t all = groups(one) + groups(two);
+    if (all) k_class_reduce<T><<<dim3(all), dim3(256), 0, st>>>(one, two, groups(one));
 }
 
 template <class T>
@@ -1225,6 +1271,7 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
         const int class0 = cp * p.piece_classes, classes = V - class0 < p.piece_classes ? V - class0 : p.piece_classes;
         const WeightPlan w = weight_plan(c.l, h, classes, p.piece_rows, p.row_pieces);
         const int dx_shares = shares_used(classes, p.dx_shares);  // (the first piece's are the most)
+        ReduceArgs<T> x_sums{};
         for (int64_t rp = 0; rp < p.row_pieces; ++rp) {
             const int64_t row0 = rp * p.piece_rows, rows = c.n - row0 < p.piece_rows ? c.n - row0 : p.piece_rows;
             s.row0 = r.row0 = row0, s.rows = r.rows = rows, s.class0 = r.class0 = class0, r.piece_classes = classes, s.classes = class0 + classes;
@@ -1238,47 +1285,48 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
             if (r.teacher_scale != 0.0f) k_class_fix<T><<<dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, c.stream>>>(r);
             float *slots = p.dx_bytes ? dx_slots + (p.class_pieces > 1 ? row0 * p.slot_width : 0) : nullptr;
             const int64_t slot_rows = round_up(p.class_pieces > 1 ? c.n : rows, h.slot_round);
-            if (dx && h.large) {
-                StagePieceArgs<T> a{};
-                a.a = (const char *)dz, a.a_rows = (int)round_up(rows, StageCut::BB), a.b = q.w + class0 * q.w_bytes, a.b_bytes = q.w_bytes, a.b_plane = q.w_plane;
-                a.M = rows, a.K = classes, a.N = D, a.a_stride = (int)p.dz_stride, a.b_width = p.padded, a.shares = dx_shares, a.per_share = per_share(classes, dx_shares);
-                a.out = dx + row0 * dx_stride, a.out_stride = dx_stride, a.slots = slots, a.slot_rows = slot_rows, a.slot_width = p.slot_width, a.add = cp > 0;
-                launch_product_stage<T, false>(a, c.stream);
-            } else if (dx) {
-                PieceArgs<T> a{};
-                a.a = dz, a.a_stride = p.dz_stride, a.b = s.w + (int64_t)class0 * D, a.b_stride = D, a.M = rows, a.K = classes, a.N = D, a.a_width = (int)p.dz_stride;
-                a.shares = dx_shares, a.per_share = per_share(classes, dx_shares), a.out = dx + row0 * dx_stride, a.out_stride = dx_stride;
-                a.slots = slots, a.slot_rows = slot_rows, a.add = cp > 0;
-                launch_product<T, false>(a, p.dx_tile, c.stream);
-            }
-            if (slots && dx && p.class_pieces == 1) launch_reduce<T>({slots, nullptr, slot_rows, rows, p.slot_width, D, dx_shares, 0, dx + row0 * dx_stride, nullptr, dx_stride}, c.stream);
-            if (!dweight) continue;
-            const auto fill = [&](auto &a) {
+            const auto fill_dx = [&](auto &a) {
+                a.M = rows, a.K = classes, a.N = D, a.shares = dx_shares, a.per_share = per_share(classes, dx_shares);
+                a.out = dx + row0 * dx_stride, a.out_stride = dx_stride, a.slots = slots, a.slot_rows = slot_rows, a.add = cp > 0;
+            };
+            const auto fill_dw = [&](auto &a) {
                 a.M = classes, a.N = D, a.shares = shares_used(rows, w.shares), a.per_share = per_share(rows, a.shares);
                 a.out = dweight + (int64_t)class0 * D, a.out_stride = D, a.slot_rows = round_up(classes, h.slot_round), a.add = rp > 0;
                 if (w.slots) a.slots = dw_slots;
                 if (dbias && (w.slots || h.large)) a.sum_slots = db_slots;
             };
             if (h.large) {
-                StagePieceArgs<T> a{};
-                fill(a);
-                a.slot_width = p.slot_width;
-                a.a = (const char *)dz, a.a_rows = (int)round_up(rows, StageCut::BB), a.b = q.x + row0 * q.x_bytes, a.b_bytes = q.x_bytes, a.b_plane = q.x_plane;
-                a.a_stride = (int)p.dz_stride, a.b_width = p.padded, a.K = round_up(rows, 32);  // (rows of zeros in both)
-                launch_product_stage<T, true>(a, c.stream);
+                StagePieceArgs<T> x{}, y{};
+                fill_dx(x), fill_dw(y);
+                x.b = q.w + class0 * q.w_bytes, x.b_bytes = q.w_bytes, x.b_plane = q.w_plane;
+                y.b = q.x + row0 * q.x_bytes, y.b_bytes = q.x_bytes, y.b_plane = q.x_plane;
+                y.K = round_up(rows, 32);  // (rows of zeros in both)
+                for (StagePieceArgs<T> *a : {&x, &y}) a->a = (const char *)dz, a->a_rows = (int)round_up(rows, StageCut::BB), a->a_stride = (int)p.dz_stride, a->b_width = p.padded, a->slot_width = p.slot_width;
+                launch_products<T>(dweight ? &y : nullptr, dx ? &x : nullptr, c.stream);
             } else {
-                PieceArgs<T> a{};
-                fill(a);
-                a.sums = dbias ? dbias + class0 : nullptr;
-                a.a = dz, a.a_stride = p.dz_stride, a.b = s.x + row0 * c.x_stride, a.b_stride = c.x_stride, a.list = listed + row0, a.K = rows, a.a_width = (int)p.dz_stride;
-                launch_product<T, true>(a, w.tile, c.stream);
+                PieceArgs<T> x{}, y{};
+                fill_dx(x), fill_dw(y);
+                x.b = s.w + (int64_t)class0 * D, x.b_stride = D;
+                y.b = s.x + row0 * c.x_stride, y.b_stride = c.x_stride, y.list = listed + row0, y.K = rows, y.sums = dbias ? dbias + class0 : nullptr;
+                for (PieceArgs<T> *a : {&x, &y}) a->a = dz, a->a_stride = p.dz_stride, a->a_width = (int)p.dz_stride;
+                if (dx && dweight && w.tile == p.dx_tile) {
+                    launch_products<T>(&y, &x, w.tile, c.stream);
+                } else {
+                    if (dweight) launch_products<T>(&y, nullptr, w.tile, c.stream);
+                    if (dx) launch_products<T>(nullptr, &x, p.dx_tile, c.stream);
+                }
             }
+            // (where one piece has all classes; the last piece of rows leaves it to the launch that finishes dW too)
+            x_sums = slots && dx && p.class_pieces == 1 ? ReduceArgs<T>{slots, nullptr, slot_rows, rows, p.slot_width, D, dx_shares, 0, dx + row0 * dx_stride, nullptr, dx_stride} : ReduceArgs<T>{};
+            if (x_sums.out && rp + 1 < p.row_pieces) launch_reduce<T>(x_sums, {}, c.stream);
         }
         // (small calls without slots have written both already, large ones dweight)
         E *dw_out = dweight && w.slots ? dweight + (int64_t)class0 * D : nullptr, *db_out = dbias && (w.slots || h.large) ? dbias + class0 : nullptr;
-        if (dw_out || db_out) launch_reduce<T>({dw_slots, db_slots, (int64_t)round_up(classes, h.slot_round), classes, p.slot_width, D, w.shares, w.shares * summers_of(c.l, h), dw_out, db_out, D}, c.stream);
+        ReduceArgs<T> w_sums{};
+        if (dw_out || db_out) w_sums = {dw_slots, db_slots, (int64_t)round_up(classes, h.slot_round), classes, p.slot_width, D, w.shares, w.shares * summers_of(c.l, h), dw_out, db_out, D};
+        if (p.dx_bytes && dx && cp > 0 && cp + 1 == p.class_pieces) x_sums = {dx_slots, nullptr, (int64_t)round_up(c.n, h.slot_round), c.n, p.slot_width, D, p.dx_shares, 0, dx, nullptr, dx_stride};
+        launch_reduce<T>(w_sums, x_sums, c.stream);
     }
-    if (p.dx_bytes && dx && p.class_pieces > 1) launch_reduce<T>({dx_slots, nullptr, (int64_t)round_up(c.n, h.slot_round), c.n, p.slot_width, D, p.dx_shares, 0, dx, nullptr, dx_stride}, c.stream);
     BGL_HIP(hipGetLastError());
     return BGL_OK;
 }
