@@ -60,7 +60,7 @@ __device__ __forceinline__ float down_column(float v, F both)
 constexpr int kPad = 64;                           // values that laid out rows are padded to
 // Tiles of classes that an XCD has in hand while it goes through the rows (512 values each: 3 MB beside the rows', of its L2's 4): 4,096 x 512 x 65,536 took 298 us
 // with the rows' 4 MB read again for every tile or two of classes, 255 with 16 (the products alone, with their exponentials).
-constexpr int kClassGroup = 16;
+constexpr int kClassGroup = 8;
 using StageCut = stage::Cut<6, 4>;                 // scores: 192 classes x 128 rows
 using ProductCut = stage::Cut<8, 4>;               // dW: 256 classes, dx: 256 rows; x 128 columns
 constexpr int kBlockRows = 16, kBlockClasses = 32, kBlockValues = kBlockRows * kBlockClasses;
@@ -96,7 +96,7 @@ struct ScoreArgs {
     float *part_t, *label_score;
     float *loss, *kept;       // one tile has all classes and there is no teacher: the losses and what is saved (or null) instead
     bool whole;
-    bool two;                 // the temperature is not 1 and there is a teacher: two sums
+    bool two;                 // labels, and a teacher at a temperature that is not 1: two sums (of a teacher alone, k is k_t)
     // backward
     const float *saved;       // n x width {log2 sum exp, the same at the temperature or +inf, the teacher's classes' scores}
     int saved_width;
@@ -253,44 +253,63 @@ struct RowArgs {
     bool blocks;     // dz lies in blocks
 };
 
-// The scores of the teacher's classes: 8 lanes for each, 128 bytes of x and of the class's row at a time.
+// The scores of the teacher's classes: 8 lanes for four of a row's, 128 bytes of x and of the classes' rows at a time.
 template <class T>
 __global__ void __launch_bounds__(256) k_class_top(RowArgs<T> a)
 {
-    constexpr int LANES = 8, AHEAD = 4;
-    const uint64_t task = (uint64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES, r = task / (uint32_t)a.top;
+    constexpr int LANES = 8, EACH = 4, AHEAD = 2, STEP = LANES * T::VEC;
+    const uint32_t groups = ((uint32_t)a.top + EACH - 1) / EACH;
+    const uint64_t task = (uint64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES, r = task / groups;
     const int l = threadIdx.x % LANES;
     if (r >= (uint64_t)a.rows) return;
     const int64_t row = a.row0 + r;
-    const int k = (int)(task % (uint32_t)a.top), c = a.top_class[row * a.top + k];
-    float z = 0.0f;
-    if ((uint32_t)c < (uint32_t)a.classes) {
-        const typename T::elem *x = a.x + row * a.x_stride, *w = a.w + (int64_t)c * a.D;
-        const auto add = [&](const uint4 &p, const uint4 &q) {
-            const uint32_t u[4] = {p.x, p.y, p.z, p.w}, v[4] = {q.x, q.y, q.z, q.w};
+    const int k0 = (int)(task % groups) * EACH;
+    const typename T::elem *x = a.x + row * a.x_stride, *w[EACH];
+    int c[EACH];
+    float z[EACH] = {};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (T::PER == 1) {
-                    z = fmaf(__uint_as_float(u[i]), __uint_as_float(v[i]), z);
-                } else {
-                    z = fmaf(__uint_as_float(u[i] << 16), __uint_as_float(v[i] << 16), z);
-                    z = fmaf(__uint_as_float(u[i] & 0xffff0000u), __uint_as_float(v[i] & 0xffff0000u), z);
-                }
-            }
-        };
-        constexpr int STEP = LANES * T::VEC;
-        int d = l * T::VEC;
-        for (; d + (AHEAD - 1) * STEP + T::VEC <= a.D; d += AHEAD * STEP) {
-            uint4 p[AHEAD], q[AHEAD];
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u) p[u] = load_any<uint4>(x + d + u * STEP), q[u] = load_any<uint4>(w + d + u * STEP);
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u) add(p[u], q[u]);
-        }
-        for (; d < a.D; d += STEP) add(load_end<T>(x + d, a.D - d, a.D), load_end<T>(w + d, a.D - d, a.D));
+    for (int k = 0; k < EACH; ++k) {
+        c[k] = k0 + k < a.top ? a.top_class[row * a.top + k0 + k] : -1;
+        if ((uint32_t)c[k] >= (uint32_t)a.classes) c[k] = -1;
+        w[k] = a.w + (int64_t)(c[k] < 0 ? 0 : c[k]) * a.D;  // (the first class's row stands in for none)
     }
-    z = sum_across<LANES>(z);
-    if (l == 0) a.z_top[row * a.z_stride + k] = z + (a.bias && (uint32_t)c < (uint32_t)a.classes ? T::get(a.bias[c]) : 0.0f);  // (0 where there is no class)
+    const auto add = [](const uint4 &p, const uint4 &q, float z) {
+        const uint32_t u[4] = {p.x, p.y, p.z, p.w}, v[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (T::PER == 1) {
+                z = fmaf(__uint_as_float(u[i]), __uint_as_float(v[i]), z);
+            } else {
+                z = fmaf(__uint_as_float(u[i] << 16), __uint_as_float(v[i] << 16), z);
+                z = fmaf(__uint_as_float(u[i] & 0xffff0000u), __uint_as_float(v[i] & 0xffff0000u), z);
+            }
+        }
+        return z;
+    };
+    int d = l * T::VEC;
+    for (; d + (AHEAD - 1) * STEP + T::VEC <= a.D; d += AHEAD * STEP) {
+        uint4 p[AHEAD], q[AHEAD][EACH];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            p[u] = load_any<uint4>(x + d + u * STEP);
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) q[u][k] = load_any<uint4>(w[k] + d + u * STEP);
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) z[k] = add(p[u], q[u][k], z[k]);
+    }
+    for (; d < a.D; d += STEP) {
+        const uint4 p = load_end<T>(x + d, a.D - d, a.D);
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) z[k] = add(p, load_end<T>(w[k] + d, a.D - d, a.D), z[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+        z[k] = sum_across<LANES>(z[k]);
+        if (l == 0 && k0 + k < a.top) a.z_top[row * a.z_stride + k0 + k] = c[k] < 0 ? 0.0f : z[k] + (a.bias ? T::get(a.bias[c[k]]) : 0.0f);
+    }
 }
 
 // The teacher's distribution of a row, for LANES neighbours: largest score / t and sum of exp; false where it names no class.
@@ -316,6 +335,52 @@ __device__ __forceinline__ bool teacher_of(const RowArgs<T> &a, int64_t row, flo
     return true;
 }
 
+// Many parts of many rows: added up by 16 lanes for each of 16 rows (whose parts are neighbours), into the first part's place.
+constexpr int kMergeRows = 16, kMergeLanes = 16;
+template <class T>
+__global__ void __launch_bounds__(kMergeRows *kMergeLanes) k_class_merge(RowArgs<T> a, float2 *part, float *part_t)
+{
+    constexpr int AHEAD = 8;
+    __shared__ float largest[kMergeLanes][kMergeRows], sums[kMergeLanes][kMergeRows], sums_t[kMergeLanes][kMergeRows];
+    const int i = threadIdx.x % kMergeRows, l = threadIdx.x / kMergeRows;
+    const int64_t row = (int64_t)blockIdx.x * kMergeRows + i, r = row < a.rows ? row : a.rows - 1;
+    float most = -INFINITY, sum = 0.0f, sum_t = 0.0f;
+    const auto take = [&](float base, float base_t, float largest, float s, float t) {
+        sum += s * rebase(base_of(largest, a.k), base);
+        if (a.two) sum_t += t * rebase(base_of(largest, a.k_t), base_t);
+    };
+    for (int first = l; first < a.class_parts; first += kMergeLanes * AHEAD) {
+        float2 from[AHEAD];
+        float at_t[AHEAD], m = most;
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int ct = first + u * kMergeLanes;
+            const bool there = ct < a.class_parts;
+            from[u] = there ? part[ct * a.rows + r] : float2{-INFINITY, 0.0f};
+            at_t[u] = a.two && there ? part_t[ct * a.rows + r] : 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) m = fmaxf(m, from[u].x);
+        const float base = base_of(m, a.k), base_t = base_of(m, a.k_t);
+        sum *= rebase(base_of(most, a.k), base);
+        sum_t *= rebase(base_of(most, a.k_t), base_t);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) take(base, base_t, from[u].x, from[u].y, at_t[u]);
+        most = m;
+    }
+    largest[l][i] = most, sums[l][i] = sum, sums_t[l][i] = sum_t;
+    __syncthreads();
+    if (l > 0 || row >= a.rows) return;
+    most = -INFINITY, sum = sum_t = 0.0f;
+#pragma unroll
+    for (int u = 0; u < kMergeLanes; ++u) most = fmaxf(most, largest[u][i]);
+    const float base = base_of(most, a.k), base_t = base_of(most, a.k_t);
+#pragma unroll
+    for (int u = 0; u < kMergeLanes; ++u) take(base, base_t, largest[u][i], sums[u][i], sums_t[u][i]);
+    part[row] = float2{most, sum};
+    if (a.two) part_t[row] = sum_t;
+}
+
 // LANES neighbours for each row.
 template <class T, int LANES>
 __global__ void __launch_bounds__(256) k_class_finish(RowArgs<T> a)
@@ -325,11 +390,27 @@ __global__ void __launch_bounds__(256) k_class_finish(RowArgs<T> a)
     const int64_t row = a.row0 + r;
     const int l = threadIdx.x % LANES;
     float most = -INFINITY, sum = 0.0f, sum_t = 0.0f;
-    for (int ct = l; ct < a.class_parts; ct += LANES) {
-        const float2 from = a.part[ct * a.rows + r];
-        const float m = fmaxf(most, from.x);
-        sum = sum * rebase(base_of(most, a.k), base_of(m, a.k)) + from.y * rebase(base_of(from.x, a.k), base_of(m, a.k));
-        if (a.two) sum_t = sum_t * rebase(base_of(most, a.k_t), base_of(m, a.k_t)) + a.part_t[ct * a.rows + r] * rebase(base_of(from.x, a.k_t), base_of(m, a.k_t));
+    constexpr int AHEAD = LANES == 64 ? 8 : 2;  // (parts on their way at a time: one after the other, 512 of one row took 4.6 us)
+    for (int first = l; first < a.class_parts; first += LANES * AHEAD) {
+        float2 from[AHEAD];
+        float at_t[AHEAD], m = most;
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int ct = first + u * LANES;
+            const bool there = ct < a.class_parts;
+            from[u] = there ? a.part[ct * a.rows + r] : float2{-INFINITY, 0.0f};
+            at_t[u] = a.two && there ? a.part_t[ct * a.rows + r] : 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) m = fmaxf(m, from[u].x);
+        const float base = base_of(m, a.k), base_t = base_of(m, a.k_t);
+        sum *= rebase(base_of(most, a.k), base);
+        sum_t *= rebase(base_of(most, a.k_t), base_t);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            sum += from[u].y * rebase(base_of(from[u].x, a.k), base);
+            sum_t += at_t[u] * rebase(base_of(from[u].x, a.k_t), base_t);
+        }
         most = m;
     }
     const float m = max_across<LANES>(most), base = base_of(m, a.k), base_t = a.two ? base_of(m, a.k_t) : base;
@@ -549,12 +630,12 @@ __global__ void __launch_bounds__(256) k_class_reduce(ReduceArgs<T> one, ReduceA
         const int64_t step = a.slot_rows * a.slot_width;
         f32x4 s = {};
         int p = 0;
-        for (; p + 4 <= a.shares; p += 4) {  // (four on their way at a time)
-            f32x4 v[4];
+        for (; p + 8 <= a.shares; p += 8) {  // (eight on their way at a time)
+            f32x4 v[8];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) v[u] = load_any<f32x4>(from + (p + u) * step);
+            for (int u = 0; u < 8; ++u) v[u] = load_any<f32x4>(from + (p + u) * step);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) s += v[u];
+            for (int u = 0; u < 8; ++u) s += v[u];
         }
         for (; p < a.shares; ++p) s += load_any<f32x4>(from + p * step);
         typename T::elem e[4], *to = a.out + row * a.out_stride + c;
@@ -1181,9 +1262,10 @@ int forward(const Call &c, float *loss, float *teacher_loss, float *saved)
     char *ws = c.workspace;
     s.part = (float2 *)ws, s.part_t = (float *)(s.part + p.pass_rows * p.class_parts), s.label_score = (float *)(ws += p.part_bytes);
     char *top = ws += p.label_bytes, *x = ws += p.top_bytes, *w = ws += p.x_bytes;
-    r.part = s.part, r.part_t = s.part_t, r.label_score = s.label_score, r.class_parts = p.class_parts;
+    r.part = s.part, r.part_t = s.part_t, r.label_score = s.label_score;
     r.z_top = saved ? saved + 2 : (float *)top, r.z_stride = saved ? r.saved_width : r.top;
     r.loss = loss, r.teacher_loss = teacher_loss, r.saved = saved;
+    if (!c.labels) s.k = r.k = s.k_t, s.two = r.two = false;  // (no sums but those at the temperature are asked for)
     StageScoreArgs<T> q{};
     if (h.large) q = stage_args<T>(c, p, h, s, x, w, nullptr);
     for (int64_t row0 = 0; row0 < c.n; row0 += p.pass_rows) {
@@ -1192,8 +1274,13 @@ int forward(const Call &c, float *loss, float *teacher_loss, float *saved)
         if (h.large) q.s = s, launch_scores_stage<T, false>(q, c.stream);
         else launch_scores<T, false>(s, c.stream);
         if (s.whole) continue;  // (every tile has all classes)
-        if (c.top_class) k_class_top<T><<<dim3((unsigned)ceil_div(r.rows * r.top, 32)), dim3(256), 0, c.stream>>>(r);
-        const int values = c.top_class && r.top > p.class_parts ? r.top : p.class_parts;
+        if (c.top_class) k_class_top<T><<<dim3((unsigned)ceil_div(r.rows * ((r.top + 3) / 4), 32)), dim3(256), 0, c.stream>>>(r);
+        r.class_parts = p.class_parts;
+        if (r.class_parts > 32 && r.rows >= 64) {
+            k_class_merge<T><<<dim3((unsigned)ceil_div(r.rows, kMergeRows)), dim3(kMergeRows * kMergeLanes), 0, c.stream>>>(r, s.part, s.part_t);
+            r.class_parts = 1;
+        }
+        const int values = c.top_class && r.top > r.class_parts ? r.top : r.class_parts;
         if (values <= 8) k_class_finish<T, 4><<<dim3((unsigned)ceil_div(r.rows, 64)), dim3(256), 0, c.stream>>>(r);
         else if (values <= 32) k_class_finish<T, 16><<<dim3((unsigned)ceil_div(r.rows, 16)), dim3(256), 0, c.stream>>>(r);
         else k_class_finish<T, 64><<<dim3((unsigned)ceil_div(r.rows, 4)), dim3(256), 0, c.stream>>>(r);
