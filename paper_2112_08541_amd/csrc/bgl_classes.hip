@@ -663,13 +663,15 @@ __global__ void __launch_bounds__(256) k_class_zero(typename T::elem *p, int64_t
 }
 
 // ----------------------------------------------------------------- large calls: operands laid out for bgl_stage.h
-// Rows of D values as rows of planes of bf16, each `padded` wide, zeros behind D and in rows from `rows` to `all_rows`.
+// Rows of D values as rows of planes, each `padded` wide, zeros behind D and in rows from `rows` to `all_rows`: of bf16 as they are, of fp32 as three planes of bf16
+// and (or) as two of halves times 2^-exponent, the row's own.
 template <class T>
 struct LayArgs {
     const typename T::elem *from;
     int64_t stride, rows, all_rows;
     int D, padded;
-    uint16_t *to;
+    uint16_t *to, *halves;  // either may be null
+    int32_t *exponent;
     // backward, x: rows without a gradient become zeros, whatever they hold
     bool select;
     const int32_t *labels;
@@ -678,50 +680,94 @@ struct LayArgs {
     bool by_label, by_teacher;
 };
 template <class T>
-__global__ void __launch_bounds__(256) k_class_lay(LayArgs<T> a)
+__device__ __forceinline__ bool lives(const LayArgs<T> &a, int64_t row)
 {
-    constexpr int PLANES = T::PER == 1 ? 3 : 1;
+    if (row >= a.rows) return false;
+    if (!a.select) return true;
+    const float lse_t = a.saved[row * a.saved_width + 1];
+    return (a.by_label && (uint32_t)a.labels[row] < (uint32_t)a.classes) || (a.by_teacher && lse_t != INFINITY);
+}
+__global__ void __launch_bounds__(256) k_class_lay(LayArgs<BF16> a)
+{
     const int each = a.padded / 8;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / each;
     const int d = (int)(i % each) * 8;
     if (row >= a.all_rows) return;
-    bool live = row < a.rows;
-    if (live && a.select) {
-        const float lse_t = a.saved[row * a.saved_width + 1];
-        live = (a.by_label && (uint32_t)a.labels[row] < (uint32_t)a.classes) || (a.by_teacher && lse_t != INFINITY);
+    uint4 v{0, 0, 0, 0};
+    if (d < a.D && lives(a, row)) {
+        const uint16_t *from = a.from + row * a.stride + d;
+        v = d + 8 <= a.D ? load_any<uint4>(from) : load_end<BF16>(from, a.D - d, a.D);
     }
-    uint16_t e[PLANES][8] = {};
-    if (live) {
-        const typename T::elem *from = a.from + row * a.stride + d;
+    *reinterpret_cast<uint4 *>(a.to + row * a.padded + d) = v;
+}
+// A wavefront for a row: its largest value first, then its planes.
+__global__ void __launch_bounds__(256) k_class_split(LayArgs<F32> a)
+{
+    const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+    const int l = threadIdx.x & 63;
+    if (row >= a.all_rows) return;
+    const bool live = lives(a, row);
+    const float *from = a.from + (live ? row : 0) * a.stride;
+    const auto read = [&](int d) {
+        f32x4 v = {};
+        if (live && d < a.D) v = __builtin_bit_cast(f32x4, d + 4 <= a.D ? load_any<uint4>(from + d) : load_end<F32>(from + d, a.D - d, a.D));
+        return v;
+    };
+    int exponent = 0;
+    if (a.halves) {
+        float most = 0.0f;
+        for (int d = 4 * l; d < a.D; d += 256) {
+            const f32x4 v = read(d);
 #pragma unroll
-        for (int v = 0; v < 8; v += T::VEC) {
-            if (d + v >= a.D) break;
-            const uint4 raw = d + v + T::VEC <= a.D ? load_any<uint4>(from + v) : load_end<T>(from + v, a.D - d - v, a.D);
-            if constexpr (PLANES == 1) {
-                __builtin_memcpy(e[0], &raw, 16);
-            } else {
-                const uint32_t q[4] = {raw.x, raw.y, raw.z, raw.w};
+            for (int j = 0; j < 4; ++j)
+                if (fabsf(v[j]) < INFINITY) most = fmaxf(most, fabsf(v[j]));
+        }
+        most = max_across<64>(most);
+        // the largest to [2^14, 2^15); not further than 2^115, for rows of the smallest numbers
+        if (most > 0.0f) exponent = ilogbf(most) - 14;
+        if (exponent < -115) exponent = -115;
+        if (l == 0) a.exponent[row] = exponent;
+    }
+    const float scale = ldexpf(1.0f, -exponent);
+    for (int d = 4 * l; d < a.padded; d += 256) {
+        const f32x4 v = read(d);
+        if (a.to) {
+            uint16_t e[3][4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint16_t three[3];
-                    split(__uint_as_float(q[j]), three);
+            for (int j = 0; j < 4; ++j) {
+                uint16_t three[3];
+                split(v[j], three);
 #pragma unroll
-                    for (int p = 0; p < 3; ++p) e[p][v + j] = three[p];
-                }
+                for (int p = 0; p < 3; ++p) e[p][j] = three[p];
             }
+#pragma unroll
+            for (int p = 0; p < 3; ++p) *reinterpret_cast<uint2 *>(a.to + (row * 3 + p) * a.padded + d) = __builtin_bit_cast(uint2, e[p]);
+        }
+        if (a.halves) {
+            _Float16 h[2][4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float x = v[j] * scale;
+                h[0][j] = (_Float16)x;
+                h[1][j] = fabsf(x) < INFINITY ? (_Float16)(x - (float)h[0][j]) : (_Float16)0.0f;
+            }
+#pragma unroll
+            for (int p = 0; p < 2; ++p) *reinterpret_cast<uint2 *>(a.halves + (row * 2 + p) * a.padded + d) = __builtin_bit_cast(uint2, h[p]);
         }
     }
-#pragma unroll
-    for (int p = 0; p < PLANES; ++p) __builtin_memcpy(a.to + (row * PLANES + p) * a.padded + d, e[p], 16);
 }
 
 // k_class_scores from laid out operands: 192 classes x 128 rows.
 template <class T>
 struct StageScoreArgs {
     ScoreArgs<T> s;
-    const char *x, *w;           // of the call's first row, of class 0
+    const char *x, *w;           // of the call's first row, of class 0: bf16, or two planes of halves
     int64_t x_bytes, w_bytes;    // rows
-    uint32_t x_plane, w_plane;   // planes
+    uint32_t plane;              // bytes
+    const int32_t *x_exponent, *w_exponent;  // of halves
+    // what the products of the backward call read (bf16: the same; fp32: three planes of bf16)
+    const char *x_back, *w_back;
+    int64_t x_back_bytes, w_back_bytes;
 };
 
 template <class T, bool DZ>
@@ -730,7 +776,7 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
     using C = StageCut;
     using A = stage::Kc<C::BA, kPad>;
     using B = stage::Kc<C::BB, kPad>;
-    constexpr int PLANES = T::PER == 1 ? 3 : 1;
+    constexpr int PLANES = T::PER == 1 ? 3 : 1, READ = T::PER == 1 ? 2 : 1;  // planes of dz, and of what is read
     __shared__ __attribute__((aligned(1024))) char lds[stage::lds_bytes<A, B>()];
     const ScoreArgs<T> &a = q.s;
     int64_t ct, rt;
@@ -746,7 +792,11 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
     // what the tile's classes and rows have of their own: a value for each thread, on its way during the products
     static_assert(C::BA <= stage::kThreads && C::BB <= stage::kThreads, "");
     float my_bias = 0.0f, my_lse = INFINITY, my_lse_t = INFINITY;
-    int my_label = -1;
+    int my_label = -1, my_class = 0, my_row = 0;  // (the last two: exponents)
+    if (READ == 2) {
+        if (threadIdx.x < C::BA) my_class = q.w_exponent[c0 + (int)threadIdx.x < last ? c0 + (int)threadIdx.x : last];
+        if (threadIdx.x < C::BB && r0 + threadIdx.x < a.rows) my_row = q.x_exponent[a.row0 + r0 + threadIdx.x];
+    }
     if (a.bias && threadIdx.x < C::BA) my_bias = T::get(a.bias[c0 + (int)threadIdx.x < last ? c0 + (int)threadIdx.x : last]);
     if (threadIdx.x < C::BB && r0 + threadIdx.x < a.rows) {
         const int64_t row = a.row0 + r0 + threadIdx.x;
@@ -757,16 +807,17 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
         }
     }
     f32x4 acc[C::FA][C::FB] = {};
-    stage::multiply<PLANES, false, A, B, C>(lds, weight, rows, stage::Walk{2 * kPad, 2 * kPad, q.w_plane, q.x_plane, a.D, 0}, acc, [](int, int, const auto &) {});
+    stage::multiply<READ, false, A, B, C>(lds, weight, rows, stage::Walk{2 * kPad, 2 * kPad, q.plane, q.plane, a.D, 0}, acc, [](int, int, const auto &) {});
 
     if ((uint32_t)my_label >= (uint32_t)a.all_classes) my_label = -1, my_lse = INFINITY;
     struct Own {
         float bias[C::BA], lse[C::BB], lse_t[C::BB];
-        int label[C::BB];
+        int label[C::BB], classes[C::BA], rows[C::BB];
     };
     Own &own = *reinterpret_cast<Own *>(lds);
-    if (threadIdx.x < C::BA) own.bias[threadIdx.x] = my_bias;
+    if (threadIdx.x < C::BA) own.bias[threadIdx.x] = my_bias, own.classes[threadIdx.x] = my_class;
     if (threadIdx.x < C::BB) {
+        own.rows[threadIdx.x] = my_row;
         own.label[threadIdx.x] = my_label;
         if constexpr (DZ) own.lse[threadIdx.x] = my_lse, own.lse_t[threadIdx.x] = my_lse_t;
     }
@@ -775,10 +826,16 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
 #pragma unroll
     for (int i = 0; i < C::FA; ++i) {
         const f32x4 b = *reinterpret_cast<const f32x4 *>(own.bias + in_tile + 16 * i);
+        const stage::i32x4 up = *reinterpret_cast<const stage::i32x4 *>(own.classes + in_tile + 16 * i);
 #pragma unroll
-        for (int t = 0; t < C::FB; ++t)
+        for (int t = 0; t < C::FB; ++t) {
+            const int row_up = READ == 2 ? own.rows[C::b_off() + 16 * t + (l & 15)] : 0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][t][j] += b[j];
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (READ == 2) acc[i][t][j] = ldexpf(acc[i][t][j], up[j] + row_up);
+                acc[i][t][j] += b[j];
+            }
+        }
     }
     if (c0 + C::BA > a.classes) {
 #pragma unroll
@@ -1020,7 +1077,7 @@ struct Plan {
     size_t dz_bytes, list_bytes, dx_bytes, dw_bytes, db_bytes, backward_bytes;
     // large calls: laid out operands, forward (0: as they are) and backward
     int padded;
-    size_t x_bytes, w_bytes, back_x_bytes;
+    size_t x_bytes, w_bytes, back_x_bytes, back_w_bytes;
 };
 
 // How a call is cut up.  Small ones: tiles of 128 x 128 straight from the operands.  Large ones: larger tiles of operands laid out for bgl_stage.h (bf16 whose rows
@@ -1091,8 +1148,13 @@ Plan plan_of(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
     p.top_bytes = round_up((size_t)n * l->top * 4, 256);
     if (s.large) {
         p.padded = (int)round_up(l->in_dim, kPad);
-        p.back_x_bytes = round_up((size_t)round_up(n, 32) * p.padded * 2 * s.planes, 256);
-        if (!laid_out(l)) p.x_bytes = p.back_x_bytes, p.w_bytes = round_up((size_t)l->classes * p.padded * 2 * s.planes, 256);
+        const auto bytes = [&](int64_t rows, bool back) {  // as stage_args lays them
+            if (l->dtype == BGL_BF16) return round_up((size_t)rows * p.padded * 2, 256);
+            return round_up((size_t)rows * p.padded * 4, 256) + round_up((size_t)rows * 4, 256) + (back ? round_up((size_t)rows * p.padded * 6, 256) : 0);
+        };
+        const int64_t rows = round_up(n, 32);
+        p.back_x_bytes = bytes(rows, true);
+        if (!laid_out(l)) p.x_bytes = bytes(rows, false), p.w_bytes = bytes(l->classes, false), p.back_w_bytes = bytes(l->classes, true);
     }
     p.forward_bytes = p.part_bytes + p.label_bytes + p.top_bytes + p.x_bytes + p.w_bytes;
 
@@ -1130,7 +1192,7 @@ Plan plan_of(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
         if (dw > p.dw_bytes) p.dw_bytes = dw;
         if (db > p.db_bytes) p.db_bytes = db;
     }
-    p.backward_bytes = p.dz_bytes + p.list_bytes + p.dx_bytes + p.dw_bytes + p.db_bytes + p.back_x_bytes + p.w_bytes;
+    p.backward_bytes = p.dz_bytes + p.list_bytes + p.dx_bytes + p.dw_bytes + p.db_bytes + p.back_x_bytes + p.back_w_bytes;
     return p;
 }
 
@@ -1143,7 +1205,7 @@ size_t backward_room(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
     const auto most = [](int64_t a, int64_t b) { return a > b ? a : b; };
     const int64_t over = (many ? kPieceClasses * least(n, kPieceRows) : 128 * stride) + 128 * least(stride, s.values);
     const Plan p = plan_of(l, n, s);
-    size_t bytes = round_up((size_t)least(round_up(n, 128) * stride, s.values + over) * s.dz_value_bytes, 256) + round_up((size_t)n * 4, 256) + p.back_x_bytes + p.w_bytes;
+    size_t bytes = round_up((size_t)least(round_up(n, 128) * stride, s.values + over) * s.dz_value_bytes, 256) + round_up((size_t)n * 4, 256) + p.back_x_bytes + p.back_w_bytes;
     // (ranges of the summed index leave s.fill tiles at most; a result of one range is rounded up to tiles)
     const int64_t width = s.large ? round_up(D, ProductCut::BB) : D, up = s.slot_round;
     const bool odd = s.large && D % 4;
@@ -1220,15 +1282,18 @@ void launch_scores_stage(StageScoreArgs<T> &q, hipStream_t st)
 }
 
 template <class T>
-void launch_lay(const typename T::elem *from, int64_t stride, int64_t rows, int64_t all_rows, int D, int padded, void *to, const RowArgs<T> *select, hipStream_t st)
+void launch_lay(const typename T::elem *from, int64_t stride, int64_t rows, int64_t all_rows, int D, int padded, char *planes, char *halves, int32_t *exponent,
+                const RowArgs<T> *select, hipStream_t st)
 {
     LayArgs<T> a{};
-    a.from = from, a.stride = stride, a.rows = rows, a.all_rows = all_rows, a.D = D, a.padded = padded, a.to = (uint16_t *)to;
+    a.from = from, a.stride = stride, a.rows = rows, a.all_rows = all_rows, a.D = D, a.padded = padded;
+    a.to = (uint16_t *)planes, a.halves = (uint16_t *)halves, a.exponent = exponent;
     if (select) {
         a.select = true, a.labels = select->labels, a.saved = select->saved, a.saved_width = select->saved_width, a.classes = select->classes;
         a.by_label = select->labels && select->scale != 0.0f, a.by_teacher = select->top_class && select->teacher_scale != 0.0f;
     }
-    k_class_lay<T><<<dim3((unsigned)ceil_div(all_rows * (padded / 8), 256)), dim3(256), 0, st>>>(a);
+    if constexpr (T::PER == 1) k_class_split<<<dim3((unsigned)ceil_div(all_rows, 4)), dim3(256), 0, st>>>(a);
+    else k_class_lay<<<dim3((unsigned)ceil_div(all_rows * (padded / 8), 256)), dim3(256), 0, st>>>(a);
 }
 
 // Whether a call goes the large way: what is laid out already has to begin on multiples of 16 bytes.
@@ -1238,17 +1303,33 @@ bool goes_large(const Call &c, bool reads_x)
     return !laid_out(c.l) || (aligned(c.weight, 16) && (!reads_x || (aligned(c.x, 16) && c.x_stride % 8 == 0 && c.x_stride < (int64_t)1 << 23)));
 }
 
-// The laid out weight and rows; what is laid out already is where it is.
+// The laid out weight and rows, in the workspace from x and w on; what is laid out already is where it is.  select: the backward call, which reads them twice.
 template <class T>
-StageScoreArgs<T> stage_args(const Call &c, const Plan &p, const Scheme &h, const ScoreArgs<T> &s, char *x, char *w, const RowArgs<T> *select)
+StageScoreArgs<T> stage_args(const Call &c, const Plan &p, const ScoreArgs<T> &s, char *x, char *w, const RowArgs<T> *select)
 {
+    constexpr bool F = T::PER == 1;
     StageScoreArgs<T> q{};
     q.s = s;
-    q.x_bytes = q.w_bytes = (int64_t)p.padded * h.planes * 2, q.x_plane = q.w_plane = p.padded * 2;
-    if (p.w_bytes) launch_lay<T>(s.w, s.D, s.classes, s.classes, s.D, p.padded, w, nullptr, c.stream), q.w = w;
-    else q.w = (const char *)s.w;
-    if (p.w_bytes || select) launch_lay<T>(s.x, s.x_stride, c.n, round_up(c.n, 32), s.D, p.padded, x, select, c.stream), q.x = x;
-    else q.x = (const char *)s.x, q.x_bytes = s.x_stride * 2;
+    q.plane = p.padded * 2;
+    const int64_t all_rows = round_up(c.n, 32);
+    const auto lay = [&](const typename T::elem *from, int64_t stride, int64_t rows, int64_t all, char *to, const RowArgs<T> *select, bool back, const char *&read, int64_t &bytes,
+                         const int32_t *&exponent, const char *&read_back, int64_t &back_bytes) {
+        bytes = (int64_t)p.padded * 2 * (F ? 2 : 1), back_bytes = (int64_t)p.padded * 2 * (F ? 3 : 1);
+        // fp32: halves, their exponents, planes of bf16
+        char *exponents = to + round_up((size_t)(all * bytes), 256), *planes = F ? exponents + round_up((size_t)all * 4, 256) : to;
+        read = to, read_back = planes, exponent = F ? (const int32_t *)exponents : nullptr;
+        launch_lay<T>(from, stride, rows, all, s.D, p.padded, F && !back ? nullptr : planes, F ? to : nullptr, F ? (int32_t *)exponents : nullptr, select, c.stream);
+    };
+    if (p.w_bytes) {
+        lay(s.w, s.D, s.classes, s.classes, w, nullptr, select, q.w, q.w_bytes, q.w_exponent, q.w_back, q.w_back_bytes);
+    } else {
+        q.w = q.w_back = (const char *)s.w, q.w_bytes = q.w_back_bytes = (int64_t)s.D * 2;
+    }
+    if (p.w_bytes || select) {
+        lay(s.x, s.x_stride, c.n, all_rows, x, select, select, q.x, q.x_bytes, q.x_exponent, q.x_back, q.x_back_bytes);
+    } else {
+        q.x = (const char *)s.x, q.x_bytes = s.x_stride * 2;
+    }
     return q;
 }
 
@@ -1267,7 +1348,7 @@ int forward(const Call &c, float *loss, float *teacher_loss, float *saved)
     r.loss = loss, r.teacher_loss = teacher_loss, r.saved = saved;
     if (!c.labels) s.k = r.k = s.k_t, s.two = r.two = false;  // (no sums but those at the temperature are asked for)
     StageScoreArgs<T> q{};
-    if (h.large) q = stage_args<T>(c, p, h, s, x, w, nullptr);
+    if (h.large) q = stage_args<T>(c, p, s, x, w, nullptr);
     for (int64_t row0 = 0; row0 < c.n; row0 += p.pass_rows) {
         s.row0 = r.row0 = row0, s.rows = r.rows = c.n - row0 < p.pass_rows ? c.n - row0 : p.pass_rows;
         s.loss = loss, s.kept = saved, s.whole = !h.large && !c.top_class && c.l->classes <= Large::BA;
@@ -1353,7 +1434,7 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
     s.teacher_scale = r.teacher_scale = c.top_class ? teacher_scale * c.l->temperature : 0.0f;
     r.saved = const_cast<float *>(saved), r.dz = dz, r.dz_stride = (int)p.dz_stride, r.blocks = h.large;
     StageScoreArgs<T> q{};
-    if (h.large) q = stage_args<T>(c, p, h, s, x_laid, w_laid, &r);
+    if (h.large) q = stage_args<T>(c, p, s, x_laid, w_laid, &r);
     for (int cp = 0; cp < p.class_pieces; ++cp) {
         const int class0 = cp * p.piece_classes, classes = V - class0 < p.piece_classes ? V - class0 : p.piece_classes;
         const WeightPlan w = weight_plan(c.l, h, classes, p.piece_rows, p.row_pieces);
@@ -1385,10 +1466,10 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
             if (h.large) {
                 StagePieceArgs<T> x{}, y{};
                 fill_dx(x), fill_dw(y);
-                x.b = q.w + class0 * q.w_bytes, x.b_bytes = q.w_bytes, x.b_plane = q.w_plane;
-                y.b = q.x + row0 * q.x_bytes, y.b_bytes = q.x_bytes, y.b_plane = q.x_plane;
+                x.b = q.w_back + class0 * q.w_back_bytes, x.b_bytes = q.w_back_bytes;
+                y.b = q.x_back + row0 * q.x_back_bytes, y.b_bytes = q.x_back_bytes;
                 y.K = round_up(rows, 32);  // (rows of zeros in both)
-                for (StagePieceArgs<T> *a : {&x, &y}) a->a = (const char *)dz, a->a_rows = (int)round_up(rows, StageCut::BB), a->a_stride = (int)p.dz_stride, a->b_width = p.padded, a->slot_width = p.slot_width;
+                for (StagePieceArgs<T> *a : {&x, &y}) a->a = (const char *)dz, a->a_rows = (int)round_up(rows, StageCut::BB), a->a_stride = (int)p.dz_stride, a->b_width = p.padded, a->b_plane = q.plane, a->slot_width = p.slot_width;
                 launch_products<T>(dweight ? &y : nullptr, dx ? &x : nullptr, c.stream);
             } else {
                 PieceArgs<T> x{}, y{};

@@ -10,6 +10,9 @@
 // rows read 128 bytes at a time.  So rows that are given are read in stages of 64, and what is written for these products alone lies in blocks of
 // 16 rows x 32 values (1,024 bytes that one load of a wavefront takes, whichever index is summed).
 //
+// Where a row's values differ little beside its largest, as rows of features and weights do, two halves of the value scaled by the row's own power of two are
+// as good and half the products: 22 bits of the value as far as it is above 2^-18 of the row's largest, 2^-40 of that largest below.
+//
 // A fp32 value is three bf16 (its first 8 bits, the next 8 of what is left, the last): all 24 bits as long as the value is above 2^-110.  A product of two is
 // the six products of parts that count, what is left out is below 2^-23 of it.  The parts lie one after the other ("planes"): of a row, or of a block.
 //
@@ -35,6 +38,7 @@ using tile::s16x4;
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 
 __device__ __forceinline__ int wave_number() { return __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); }
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 // A buffer of all memory from `base` (the same in every lane) on.
 __device__ __forceinline__ i32x4 whole_memory_from(const char *base)
@@ -211,14 +215,28 @@ constexpr int stages() { return 81920 / (A::BYTES + B::BYTES); }
 template <class A, class B>
 constexpr int lds_bytes() { return stages<A, B>() * (A::BYTES + B::BYTES); }
 
-// Adds the product to acc: of a fragment pair a lane has rows 4 (lane / 16) .. + 3 of a and row lane % 16 of b, TURNED the other way round.  PLANES: 1, or 3 (six products).  also(stage, plane of b, a's fragments) sees every 32 summed values.  Ends with all of LDS free.
+// The operands' planes of product p: hexadecimal digit p.
+template <int PLANES>
+struct Pairs {
+    static constexpr int COUNT = PLANES == 1 ? 1 : PLANES == 2 ? 3 : 6;
+    static constexpr uint32_t A = PLANES == 2 ? 0x100 : 0x010210, B = PLANES == 2 ? 0x010 : 0x211000;
+};
+// PLANES of 2 are halves, else bf16.
+template <int PLANES>
+__device__ __forceinline__ f32x4 mma(const bf16x8 &a, const bf16x8 &b, const f32x4 &c)
+{
+    if constexpr (PLANES == 2) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// Adds the product to acc: of a fragment pair a lane has rows 4 (lane / 16) .. + 3 of a and row lane % 16 of b, TURNED the other way round.  PLANES: 1, 2 (three products of halves) or 3 (six products).  also(stage, plane of b, a's fragments) sees every 32 summed values.  Ends with all of LDS free.
 template <int PLANES, bool TURNED, class A, class B, class C, class Also>
 __device__ __forceinline__ void multiply(char *lds, const A &a, const B &b, const Walk &w, f32x4 (&acc)[C::FA][C::FB], Also also)
 {
     static_assert(A::STEP == B::STEP, "");
-    constexpr int STEP = A::STEP, STAGES = stages<A, B>(), PAIRS = PLANES == 1 ? 1 : 6, BYTES = A::BYTES + B::BYTES, LOADS = A::LOADS + B::LOADS;
+    constexpr int STEP = A::STEP, STAGES = stages<A, B>(), PAIRS = Pairs<PLANES>::COUNT, BYTES = A::BYTES + B::BYTES, LOADS = A::LOADS + B::LOADS;
     static_assert(STAGES == 2 || STAGES == 3, "");
-    constexpr uint32_t PLANE_A = 0x010210, PLANE_B = 0x211000;  // of pair p: hexadecimal digit p
+    constexpr uint32_t PLANE_A = Pairs<PLANES>::A, PLANE_B = Pairs<PLANES>::B;
     const int blocks = (w.count + STEP - 1) / STEP, steps = blocks * PAIRS;
     int block = w.first, pair = 0, to = 0;  // of the next stage to load
     const auto load = [&] {
@@ -254,7 +272,7 @@ __device__ __forceinline__ void multiply(char *lds, const A &a, const B &b, cons
             for (int i = 0; i < C::FA; ++i)
 #pragma unroll
                 for (int j = 0; j < C::FB; ++j)
-                    acc[i][j] = TURNED ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0) : __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+                    acc[i][j] = TURNED ? mma<PLANES>(fb[j], fa[i], acc[i][j]) : mma<PLANES>(fa[i], fb[j], acc[i][j]);
             also(s, PLANE_B >> 4 * plane & 3, fa);
         }
         if (++plane == PAIRS) plane = 0;
