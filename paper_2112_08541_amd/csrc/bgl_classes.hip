@@ -79,6 +79,14 @@ __device__ __forceinline__ void split(float v, uint16_t (&e)[3])
     e[2] = BF16::put(rest - BF16::get(e[1]));
 }
 
+// dz as large calls keep it: three bf16 of fp32 layers, a half of bf16 ones.
+template <class T>
+__device__ __forceinline__ void parts(float d, uint16_t (&e)[3])
+{
+    if constexpr (T::PER == 1) split(d, e);
+    else e[0] = __builtin_bit_cast(uint16_t, (_Float16)d);
+}
+
 template <class T>
 struct ScoreArgs {
     const typename T::elem *x, *w, *bias;
@@ -102,6 +110,7 @@ struct ScoreArgs {
     int saved_width;
     float scale, teacher_scale;
     typename T::elem *dz;     // rows x dz_stride
+    typename T::elem *dz_rest;  // bf16: what rounding dz left, laid out the same
     int dz_stride;
     int32_t *listed;          // null, or the row's number among this launch's for rows with a gradient, else -1
 };
@@ -189,7 +198,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_scores(ScoreArgs<T> a)
             if (a.listed && ct == 0 && C::a_off() == 0 && l < 16 && live) a.listed[r] = s != 0.0f || st != 0.0f ? (int32_t)r : -1;
 #pragma unroll
             for (int i = 0; i < C::FA; ++i) {
-                typename T::elem e[4];
+                typename T::elem e[4], rest[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float v = acc[i][t][j];
@@ -197,10 +206,14 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_scores(ScoreArgs<T> a)
                     if (s != 0.0f) d = s * (power_to(v, a.k, lse) - (first + 16 * i + j == label ? 1.0f : 0.0f));
                     if (st != 0.0f) d = fmaf(st, power_to(v, a.k_t, lse_t), d);
                     e[j] = T::put(d);
+                    rest[j] = T::put(d - T::get(e[j]));
                 }
                 const int c = first + 16 * i;
-                typename T::elem *to = a.dz + r * a.dz_stride + (c - a.class0);
-                if (live && c - a.class0 < a.dz_stride) __builtin_memcpy(to, e, sizeof(e));  // (dz_stride is a multiple of 4; what is behind the classes is not read)
+                const int64_t at = r * a.dz_stride + (c - a.class0);  // (dz_stride is a multiple of 4; what is behind the classes is not read)
+                if (live && c - a.class0 < a.dz_stride) {
+                    __builtin_memcpy(a.dz + at, e, sizeof(e));
+                    if constexpr (T::PER == 2) __builtin_memcpy(a.dz_rest + at, rest, sizeof(rest));
+                }
             }
         }
     }
@@ -248,9 +261,9 @@ struct RowArgs {
     int z_stride;
     bool two;
     // backward: the piece of dz
-    typename T::elem *dz;
+    typename T::elem *dz, *dz_rest;
     int class0, piece_classes, dz_stride;
-    bool blocks;     // dz lies in blocks
+    bool blocks;     // dz lies in blocks, as halves or three bf16
 };
 
 // The scores of the teacher's classes: 8 lanes for four of a row's, 128 bytes of x and of the classes' rows at a time.
@@ -468,13 +481,14 @@ __global__ void __launch_bounds__(256) k_class_fix(RowArgs<T> a)
         if (a.teacher_scale != 0.0f) d = fmaf(a.teacher_scale, power_to(z, a.k_t, lse_t) - p, d);
         if (a.blocks) {
             constexpr int PLANES = T::PER == 1 ? 3 : 1;
-            uint16_t e[3] = {}, *to = reinterpret_cast<uint16_t *>(a.dz) + dz_block(r, c - a.class0, a.dz_stride, PLANES);
-            if constexpr (PLANES == 1) e[0] = BF16::put(d);
-            else split(d, e);
+            uint16_t e[3], *to = reinterpret_cast<uint16_t *>(a.dz) + dz_block(r, c - a.class0, a.dz_stride, PLANES);
+            parts<T>(d, e);
 #pragma unroll
             for (int p = 0; p < PLANES; ++p) to[p * kBlockValues] = e[p];
         } else {
-            a.dz[r * a.dz_stride + (c - a.class0)] = T::put(d);
+            const int64_t at = r * a.dz_stride + (c - a.class0);
+            a.dz[at] = T::put(d);
+            if constexpr (T::PER == 2) a.dz_rest[at] = T::put(d - T::get(a.dz[at]));
         }
     }
 }
@@ -482,7 +496,7 @@ __global__ void __launch_bounds__(256) k_class_fix(RowArgs<T> a)
 // ----------------------------------------------------------------- products of a piece
 template <class T>
 struct PieceArgs {
-    const typename T::elem *a, *b;  // dz; W or x
+    const typename T::elem *a, *a_rest, *b;  // dz, and (bf16) what rounding it left; W or x
     int64_t a_stride, b_stride;
     const int32_t *list;            // of the summed rows (dW): the row itself, or -1 for none
     int64_t M, K;                   // kept and summed index
@@ -539,14 +553,16 @@ __device__ __forceinline__ void Product<T, C, OC, NARROW>::make(const PieceArgs<
     if (slot && a.add) each_sum<C>(m0, a.M, n0, a.N, acc, [&](float, int64_t m, int c) { return slot[m * a.N + c]; });
     float sums[C::FA] = {};
     const bool summing = OC && (a.sums || a.sum_slots) && n0 == 0 && C::b_off() == 0;
-    if (K > 0) {
+    // bf16: the products of what rounding dz left come on top: with the rounded dz alone results were up to 1.4 times as far off as their own rounding is
+    for (int part = 0; K > 0 && part < (T::PER == 2 ? 2 : 1); ++part) {
+        const typename T::elem *dz = part ? a.a_rest : a.a;
         A left;
         B right;
         if constexpr (OC) {
-            left.init(a.a, a.a_stride, a.K, (int)m0, a.a_width);
+            left.init(dz, a.a_stride, a.K, (int)m0, a.a_width);
             left.range(nullptr, k0, K);
         } else {
-            left.init([&](int i) { return a.a + (m0 + i < a.M ? m0 + i : a.M - 1) * a.a_stride + k0; });
+            left.init([&](int i) { return dz + (m0 + i < a.M ? m0 + i : a.M - 1) * a.a_stride + k0; });
         }
         right.init(a.b, a.b_stride, a.K, n0, a.N);
         right.range(a.list, k0, K);
@@ -614,6 +630,8 @@ struct ReduceArgs {
     int slot_width, width, shares, sum_shares;
     typename T::elem *out, *sums;  // either may be null
     int64_t out_stride;
+    const int32_t *exponent;       // null, or values times undo 2^exponent, sums times undo
+    float undo;
 };
 template <class T>
 __global__ void __launch_bounds__(256) k_class_reduce(ReduceArgs<T> one, ReduceArgs<T> two, uint32_t one_groups)
@@ -638,9 +656,10 @@ __global__ void __launch_bounds__(256) k_class_reduce(ReduceArgs<T> one, ReduceA
             for (int u = 0; u < 8; ++u) s += v[u];
         }
         for (; p < a.shares; ++p) s += load_any<f32x4>(from + p * step);
+        const float up = a.exponent ? ldexpf(a.undo, a.exponent[0]) : 1.0f;
         typename T::elem e[4], *to = a.out + row * a.out_stride + c;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) e[j] = T::put(s[j]);
+        for (int j = 0; j < 4; ++j) e[j] = T::put(s[j] * up);
         if (c + 4 <= a.width) {
             __builtin_memcpy(to, e, sizeof(e));
         } else {
@@ -652,7 +671,7 @@ __global__ void __launch_bounds__(256) k_class_reduce(ReduceArgs<T> one, ReduceA
         const float *from = a.sum_slots + (i - values);
         float s = 0.0f;
         for (int p = 0; p < a.sum_shares; ++p) s += from[p * a.rows];
-        a.sums[i - values] = T::put(s);
+        a.sums[i - values] = T::put(a.exponent ? s * a.undo : s);
     }
 }
 template <class T>
@@ -687,18 +706,93 @@ __device__ __forceinline__ bool lives(const LayArgs<T> &a, int64_t row)
     const float lse_t = a.saved[row * a.saved_width + 1];
     return (a.by_label && (uint32_t)a.labels[row] < (uint32_t)a.classes) || (a.by_teacher && lse_t != INFINITY);
 }
+__device__ __forceinline__ uint4 eight(const LayArgs<BF16> &a, int64_t row, int d)
+{
+    if (d >= a.D || !lives(a, row)) return uint4{0, 0, 0, 0};
+    const uint16_t *from = a.from + row * a.stride + d;
+    return d + 8 <= a.D ? load_any<uint4>(from) : load_end<BF16>(from, a.D - d, a.D);
+}
 __global__ void __launch_bounds__(256) k_class_lay(LayArgs<BF16> a)
 {
     const int each = a.padded / 8;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / each;
     const int d = (int)(i % each) * 8;
-    if (row >= a.all_rows) return;
-    uint4 v{0, 0, 0, 0};
-    if (d < a.D && lives(a, row)) {
-        const uint16_t *from = a.from + row * a.stride + d;
-        v = d + 8 <= a.D ? load_any<uint4>(from) : load_end<BF16>(from, a.D - d, a.D);
+    if (row < a.all_rows) *reinterpret_cast<uint4 *>(a.to + row * a.padded + d) = eight(a, row, d);
+}
+
+// bf16 rows and weight as halves, for the backward call, whose dz is in halves: times 2^-exponent, one for all of x and one for all of W, so that the largest is
+// in [2^14, 2^15) and a bf16's eight bits fit a half's from 2^-32 of it on.  First the largest of kLayGroups shares of each, then every workgroup finds the exponent from these.
+constexpr int kLayGroups = 1024, kHalvesHead = 2 * kLayGroups * 4 + 256;
+struct HalvesArgs {
+    LayArgs<BF16> w, x;      // `halves` of both
+    uint32_t *largest;       // kLayGroups of w, kLayGroups of x
+};
+__device__ __forceinline__ uint32_t largest_of(const uint4 &v)
+{
+    const uint32_t d[4] = {v.x, v.y, v.z, v.w};
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = d[i] & 0x7fff, hi = d[i] >> 16 & 0x7fff;
+        most = lo < 0x7f80 && lo > most ? lo : most;
+        most = hi < 0x7f80 && hi > most ? hi : most;
     }
-    *reinterpret_cast<uint4 *>(a.to + row * a.padded + d) = v;
+    return most;
+}
+__device__ __forceinline__ uint32_t group_largest(uint32_t v)
+{
+    __shared__ float all[4];
+    const float w = max_across<64>((float)v);  // (15 bits)
+    if (threadIdx.x % 64 == 0) all[threadIdx.x / 64] = w;
+    __syncthreads();
+    return (uint32_t)fmaxf(fmaxf(all[0], all[1]), fmaxf(all[2], all[3]));
+}
+template <class F>
+__device__ __forceinline__ void each_eight(const LayArgs<BF16> &a, uint32_t group, uint32_t groups, F f)
+{
+    const uint64_t each = a.padded / 8, all = (uint64_t)a.all_rows * each;
+#pragma unroll 4
+    for (uint64_t i = (uint64_t)group * 256 + threadIdx.x; i < all; i += (uint64_t)groups * 256) {
+        const uint64_t row = all >> 32 ? i / each : (uint32_t)i / (uint32_t)each;
+        f((int64_t)row, (int)(i - row * each) * 8);
+    }
+}
+__global__ void __launch_bounds__(256) k_class_largest(HalvesArgs a)
+{
+    const bool second = blockIdx.x >= kLayGroups;
+    const LayArgs<BF16> &m = second ? a.x : a.w;
+    uint32_t most = 0;
+    each_eight(m, blockIdx.x % kLayGroups, kLayGroups, [&](int64_t row, int d) {
+        const uint32_t v = largest_of(eight(m, row, d));
+        most = v > most ? v : most;
+    });
+    most = group_largest(most);
+    if (threadIdx.x == 0) a.largest[blockIdx.x] = most;
+}
+__global__ void __launch_bounds__(256) k_class_halves(HalvesArgs a, uint32_t w_groups)
+{
+    const bool second = blockIdx.x >= w_groups;
+    const LayArgs<BF16> &m = second ? a.x : a.w;
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < kLayGroups / 256; ++i) {
+        const uint32_t v = a.largest[(second ? kLayGroups : 0) + i * 256 + threadIdx.x];
+        most = v > most ? v : most;
+    }
+    most = group_largest(most);
+    int exponent = most ? ilogbf(__uint_as_float(most << 16)) - 14 : 0;
+    if (exponent < -115) exponent = -115;
+    const uint32_t group = second ? blockIdx.x - w_groups : blockIdx.x;
+    if (group == 0 && threadIdx.x == 0) m.exponent[0] = exponent;
+    const float scale = ldexpf(1.0f, -exponent);
+    each_eight(m, group, second ? gridDim.x - w_groups : w_groups, [&](int64_t row, int d) {
+        const uint4 v = eight(m, row, d);
+        const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+        _Float16 h[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) h[2 * j] = (_Float16)(__uint_as_float(in[j] << 16) * scale), h[2 * j + 1] = (_Float16)(__uint_as_float(in[j] & 0xffff0000u) * scale);
+        *reinterpret_cast<uint4 *>(m.halves + row * m.padded + d) = __builtin_bit_cast(uint4, h);
+    });
 }
 // A wavefront for a row: its largest value first, then its planes.
 __global__ void __launch_bounds__(256) k_class_split(LayArgs<F32> a)
@@ -764,7 +858,7 @@ struct StageScoreArgs {
     const char *x, *w;           // of the call's first row, of class 0: bf16, or two planes of halves
     int64_t x_bytes, w_bytes;    // rows
     uint32_t plane;              // bytes
-    const int32_t *x_exponent, *w_exponent;  // of halves
+    const int32_t *x_exponent, *w_exponent;  // of halves: of every row and class (fp32), of all (bf16)
     // what the products of the backward call read (bf16: the same; fp32: three planes of bf16)
     const char *x_back, *w_back;
     int64_t x_back_bytes, w_back_bytes;
@@ -776,7 +870,8 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
     using C = StageCut;
     using A = stage::Kc<C::BA, kPad>;
     using B = stage::Kc<C::BB, kPad>;
-    constexpr int PLANES = T::PER == 1 ? 3 : 1, READ = T::PER == 1 ? 2 : 1;  // planes of dz, and of what is read
+    constexpr int PLANES = T::PER == 1 ? 3 : 1;  // of dz
+    constexpr stage::Kind READ = T::PER == 1 ? stage::TWO_HALVES : DZ ? stage::ONE_HALF : stage::ONE_BF16;
     __shared__ __attribute__((aligned(1024))) char lds[stage::lds_bytes<A, B>()];
     const ScoreArgs<T> &a = q.s;
     int64_t ct, rt;
@@ -793,7 +888,7 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
     static_assert(C::BA <= stage::kThreads && C::BB <= stage::kThreads, "");
     float my_bias = 0.0f, my_lse = INFINITY, my_lse_t = INFINITY;
     int my_label = -1, my_class = 0, my_row = 0;  // (the last two: exponents)
-    if (READ == 2) {
+    if (READ == stage::TWO_HALVES) {
         if (threadIdx.x < C::BA) my_class = q.w_exponent[c0 + (int)threadIdx.x < last ? c0 + (int)threadIdx.x : last];
         if (threadIdx.x < C::BB && r0 + threadIdx.x < a.rows) my_row = q.x_exponent[a.row0 + r0 + threadIdx.x];
     }
@@ -822,6 +917,7 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
         if constexpr (DZ) own.lse[threadIdx.x] = my_lse, own.lse_t[threadIdx.x] = my_lse_t;
     }
     __syncthreads();
+    const float all_up = READ == stage::ONE_HALF ? ldexpf(1.0f, q.w_exponent[0] + q.x_exponent[0]) : 1.0f;
     const int in_tile = C::a_off() + 4 * (l >> 4), first = c0 + in_tile;
 #pragma unroll
     for (int i = 0; i < C::FA; ++i) {
@@ -829,11 +925,12 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
         const stage::i32x4 up = *reinterpret_cast<const stage::i32x4 *>(own.classes + in_tile + 16 * i);
 #pragma unroll
         for (int t = 0; t < C::FB; ++t) {
-            const int row_up = READ == 2 ? own.rows[C::b_off() + 16 * t + (l & 15)] : 0;
+            const int row_up = READ == stage::TWO_HALVES ? own.rows[C::b_off() + 16 * t + (l & 15)] : 0;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if constexpr (READ == 2) acc[i][t][j] = ldexpf(acc[i][t][j], up[j] + row_up);
-                acc[i][t][j] += b[j];
+                if constexpr (READ == stage::TWO_HALVES) acc[i][t][j] = ldexpf(acc[i][t][j], up[j] + row_up);
+                if constexpr (READ == stage::ONE_HALF) acc[i][t][j] = fmaf(acc[i][t][j], all_up, b[j]);
+                else acc[i][t][j] += b[j];
             }
         }
     }
@@ -902,31 +999,23 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
                     for (int j = 0; j < 4; ++j) d[j] = fmaf(a.teacher_scale, power_to(acc[i][t][j], a.k_t, lse_t), d[j]);
                 }
                 uint16_t *to = reinterpret_cast<uint16_t *>(a.dz) + dz_block(r, first - a.class0 + 16 * i, a.dz_stride, PLANES);
-                if constexpr (PLANES == 1) {
-                    uint16_t e[4];
+                uint16_t e[PLANES][4];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) e[j] = BF16::put(d[j]);
-                    __builtin_memcpy(to, e, sizeof(e));
-                } else {
-                    uint16_t e[3][4];
+                for (int j = 0; j < 4; ++j) {
+                    uint16_t one[3];
+                    parts<T>(d[j], one);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        uint16_t three[3];
-                        split(d[j], three);
-#pragma unroll
-                        for (int p = 0; p < 3; ++p) e[p][j] = three[p];
-                    }
-#pragma unroll
-                    for (int p = 0; p < 3; ++p) __builtin_memcpy(to + p * kBlockValues, e[p], sizeof(e[p]));
+                    for (int p = 0; p < PLANES; ++p) e[p][j] = one[p];
                 }
+#pragma unroll
+                for (int p = 0; p < PLANES; ++p) __builtin_memcpy(to + p * kBlockValues, e[p], sizeof(e[p]));
             }
             if (any) {  // the label's class again, with the label
                 const float v = own_score(t);
                 float d = a.scale * (power_to(v, a.k, lse) - 1.0f);
                 if (teachers) d = fmaf(a.teacher_scale, power_to(v, a.k_t, lse_t), d);
                 uint16_t e[3], *to = reinterpret_cast<uint16_t *>(a.dz) + dz_block(r, first - a.class0 + (mine ? at : 0), a.dz_stride, PLANES);
-                if constexpr (PLANES == 1) e[0] = BF16::put(d);
-                else split(d, e);
+                parts<T>(d, e);
                 if (mine) {
 #pragma unroll
                     for (int p = 0; p < PLANES; ++p) to[p * kBlockValues] = e[p];
@@ -950,7 +1039,9 @@ struct StagePieceArgs {
     int64_t per_share;                 // a multiple of 32
     typename T::elem *out;
     int64_t out_stride;
-    float *slots, *sum_slots;          // sums: shares x min(kSummers, column tiles) x 2 of them
+    const int32_t *exponent;           // bf16: of b
+    float undo;                        // 1 over what dz was multiplied by: the result is the product times this and 2^exponent
+    float *slots, *sum_slots;          // (both without that)  sums: shares x min(kSummers, column tiles) x 2 of them
     int64_t slot_rows;                 // of a slot, a multiple of the tiles' as slot_width is
     int slot_width;
     bool add;
@@ -959,6 +1050,21 @@ struct StagePieceArgs {
 // dz's sums over the rows are made by the tiles of the first columns and both halves of their wavefronts in turn, a stage each: made by one of them they took a
 // seventh of the whole product's time.
 constexpr int kSummers = 4;
+
+template <stage::Kind KIND>
+__device__ __forceinline__ float sum_of(const uint4 &v, float s)
+{
+    if constexpr (stage::Pairs<KIND>::HALF) {
+        typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+        const f16x2 ones = {(_Float16)1.0f, (_Float16)1.0f};
+        const uint32_t d[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, d[i]), ones, s, false);
+        return s;
+    } else {
+        return BF16::sum({v.x, v.y, v.z, v.w}, s);
+    }
+}
 
 template <class T, bool OC>
 struct StageProduct {
@@ -971,7 +1077,8 @@ struct StageProduct {
 template <class T, bool OC>
 __device__ __forceinline__ void StageProduct<T, OC>::make(const StagePieceArgs<T> &a, uint32_t id, char *lds)
 {
-    constexpr int PLANES = T::PER == 1 ? 3 : 1;
+    constexpr stage::Kind KIND = T::PER == 1 ? stage::THREE_BF16 : stage::ONE_HALF;
+    constexpr int PLANES = stage::Pairs<KIND>::PLANES;
     const int share = (int)(id % (uint32_t)a.shares);
     int64_t rt;
     int ct;
@@ -1006,12 +1113,12 @@ __device__ __forceinline__ void StageProduct<T, OC>::make(const StagePieceArgs<T
     float sums[C::FA] = {};
     const int summers = a.col_tiles < kSummers ? a.col_tiles : kSummers, summer = 2 * ct + (C::b_off() > 0);
     const bool summing = OC && a.sum_slots && ct < summers;
-    stage::multiply<PLANES, true, A, B, C>(lds, left, right, stage::Walk{a_block, (uint32_t)(A::STEP * a.b_bytes), kBlockValues * 2, a.b_plane, K, 0}, acc, [&](int s, int b_plane, const auto &f) {
+    stage::multiply<KIND, true, A, B, C>(lds, left, right, stage::Walk{a_block, (uint32_t)(A::STEP * a.b_bytes), kBlockValues * 2, a.b_plane, K, 0}, acc, [&](int s, int b_plane, const auto &f) {
         if (summing && b_plane == 0 && (PLANES == 1 ? s : s / 6) % (2 * summers) == summer) {
 #pragma unroll
             for (int t = 0; t < C::FA; ++t) {
                 const uint4 v = __builtin_bit_cast(uint4, f[t]);
-                sums[t] = BF16::sum({v.x, v.y, v.z, v.w}, sums[t]);
+                sums[t] = sum_of<KIND>(v, sums[t]);
             }
         }
     });
@@ -1024,6 +1131,7 @@ __device__ __forceinline__ void StageProduct<T, OC>::make(const StagePieceArgs<T
             for (int t = 0; t < C::FB; ++t) *reinterpret_cast<f32x4 *>(slot + 16 * i * (int64_t)a.slot_width + 16 * t) = acc[i][t];
     } else {
         typename T::elem *to = a.out + m1 * a.out_stride + c1;
+        const float up = a.exponent ? ldexpf(a.undo, a.exponent[0]) : 1.0f;
 #pragma unroll
         for (int i = 0; i < C::FA; ++i) {
             if (m1 + 16 * i >= a.M) break;
@@ -1031,7 +1139,7 @@ __device__ __forceinline__ void StageProduct<T, OC>::make(const StagePieceArgs<T
             for (int t = 0; t < C::FB; ++t) {
                 typename T::elem e[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) e[j] = T::put(acc[i][t][j]);
+                for (int j = 0; j < 4; ++j) e[j] = T::put(acc[i][t][j] * up);
                 if (c1 + 16 * t < a.N) __builtin_memcpy(to + 16 * t, e, sizeof(e));  // (N is a multiple of 4)
             }
             to += 16 * a.out_stride;
@@ -1094,7 +1202,7 @@ Scheme scheme_of(const bgl_class_loss_t *l, bool large)
 {
     const bool f32 = l->dtype == BGL_F32;
     if (large) return Scheme{true, StageCut::BA, ProductCut::BA, ((int64_t)1 << 27) + ((int64_t)1 << 23), StageCut::BA, StageCut::BB, f32 ? 6 : 2, f32 ? 3 : 1, ProductCut::BA, 2 * kCus, 512};
-    return Scheme{false, 128, 128, (int64_t)1 << 25, 8, 1, f32 ? 4 : 2, 1, 1, kCus, 64};  // (pieces of 4 classes are stored, and 16 bytes of bf16 read)
+    return Scheme{false, 128, 128, (int64_t)1 << 25, 8, 1, 4, 1, 1, kCus, 64};  // (pieces of 4 classes are stored, and 16 bytes of bf16 read)
 }
 bool large_call(const bgl_class_loss_t *l, int64_t n) { return n >= 256 && l->classes >= 128 && (double)n * l->classes * l->in_dim >= kLargeProducts; }
 bool laid_out(const bgl_class_loss_t *l) { return l->dtype == BGL_BF16 && l->in_dim % kPad == 0; }
@@ -1149,12 +1257,12 @@ Plan plan_of(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
     if (s.large) {
         p.padded = (int)round_up(l->in_dim, kPad);
         const auto bytes = [&](int64_t rows, bool back) {  // as stage_args lays them
-            if (l->dtype == BGL_BF16) return round_up((size_t)rows * p.padded * 2, 256);
+            if (l->dtype == BGL_BF16) return round_up((size_t)rows * p.padded * 2, 256) + (back ? kHalvesHead : 0);
             return round_up((size_t)rows * p.padded * 4, 256) + round_up((size_t)rows * 4, 256) + (back ? round_up((size_t)rows * p.padded * 6, 256) : 0);
         };
         const int64_t rows = round_up(n, 32);
-        p.back_x_bytes = bytes(rows, true);
-        if (!laid_out(l)) p.x_bytes = bytes(rows, false), p.w_bytes = bytes(l->classes, false), p.back_w_bytes = bytes(l->classes, true);
+        p.back_x_bytes = bytes(rows, true), p.back_w_bytes = bytes(l->classes, true);
+        if (!laid_out(l)) p.x_bytes = bytes(rows, false), p.w_bytes = bytes(l->classes, false);
     }
     p.forward_bytes = p.part_bytes + p.label_bytes + p.top_bytes + p.x_bytes + p.w_bytes;
 
@@ -1281,54 +1389,75 @@ void launch_scores_stage(StageScoreArgs<T> &q, hipStream_t st)
     k_class_scores_stage<T, DZ><<<dim3((unsigned)tiles), dim3(stage::kThreads), 0, st>>>(q);
 }
 
+// rows of `all` rows, those behind `rows` zeros; select: rows without a gradient zeros too.
 template <class T>
-void launch_lay(const typename T::elem *from, int64_t stride, int64_t rows, int64_t all_rows, int D, int padded, char *planes, char *halves, int32_t *exponent,
-                const RowArgs<T> *select, hipStream_t st)
+LayArgs<T> lay_args(const void *from, int64_t stride, int64_t rows, int64_t all, int D, int padded, const RowArgs<T> *select)
 {
     LayArgs<T> a{};
-    a.from = from, a.stride = stride, a.rows = rows, a.all_rows = all_rows, a.D = D, a.padded = padded;
-    a.to = (uint16_t *)planes, a.halves = (uint16_t *)halves, a.exponent = exponent;
+    a.from = (const typename T::elem *)from, a.stride = stride, a.rows = rows, a.all_rows = all, a.D = D, a.padded = padded;
     if (select) {
         a.select = true, a.labels = select->labels, a.saved = select->saved, a.saved_width = select->saved_width, a.classes = select->classes;
         a.by_label = select->labels && select->scale != 0.0f, a.by_teacher = select->top_class && select->teacher_scale != 0.0f;
     }
-    if constexpr (T::PER == 1) k_class_split<<<dim3((unsigned)ceil_div(all_rows, 4)), dim3(256), 0, st>>>(a);
-    else k_class_lay<<<dim3((unsigned)ceil_div(all_rows * (padded / 8), 256)), dim3(256), 0, st>>>(a);
+    return a;
 }
 
-// Whether a call goes the large way: what is laid out already has to begin on multiples of 16 bytes.
-bool goes_large(const Call &c, bool reads_x)
+// Whether a call goes the large way: of what the forward call reads where it is, rows have to begin on multiples of 16 bytes.
+bool goes_large(const Call &c, bool forward)
 {
     if (!large_call(c.l, c.n)) return false;
-    return !laid_out(c.l) || (aligned(c.weight, 16) && (!reads_x || (aligned(c.x, 16) && c.x_stride % 8 == 0 && c.x_stride < (int64_t)1 << 23)));
+    return !forward || !laid_out(c.l) || (aligned(c.weight, 16) && aligned(c.x, 16) && c.x_stride % 8 == 0 && c.x_stride < (int64_t)1 << 23);
 }
 
-// The laid out weight and rows, in the workspace from x and w on; what is laid out already is where it is.  select: the backward call, which reads them twice.
-template <class T>
-StageScoreArgs<T> stage_args(const Call &c, const Plan &p, const ScoreArgs<T> &s, char *x, char *w, const RowArgs<T> *select)
+// The laid out weight and rows, in the workspace from x and w on; what is laid out already is where it is.  select: the backward call's.
+StageScoreArgs<F32> stage_args(const Call &c, const Plan &p, const ScoreArgs<F32> &s, char *x, char *w, const RowArgs<F32> *select)
 {
-    constexpr bool F = T::PER == 1;
-    StageScoreArgs<T> q{};
-    q.s = s;
-    q.plane = p.padded * 2;
-    const int64_t all_rows = round_up(c.n, 32);
-    const auto lay = [&](const typename T::elem *from, int64_t stride, int64_t rows, int64_t all, char *to, const RowArgs<T> *select, bool back, const char *&read, int64_t &bytes,
-                         const int32_t *&exponent, const char *&read_back, int64_t &back_bytes) {
-        bytes = (int64_t)p.padded * 2 * (F ? 2 : 1), back_bytes = (int64_t)p.padded * 2 * (F ? 3 : 1);
-        // fp32: halves, their exponents, planes of bf16
-        char *exponents = to + round_up((size_t)(all * bytes), 256), *planes = F ? exponents + round_up((size_t)all * 4, 256) : to;
-        read = to, read_back = planes, exponent = F ? (const int32_t *)exponents : nullptr;
-        launch_lay<T>(from, stride, rows, all, s.D, p.padded, F && !back ? nullptr : planes, F ? to : nullptr, F ? (int32_t *)exponents : nullptr, select, c.stream);
+    StageScoreArgs<F32> q{};
+    q.s = s, q.plane = p.padded * 2;
+    q.x_bytes = q.w_bytes = (int64_t)p.padded * 4, q.x_back_bytes = q.w_back_bytes = (int64_t)p.padded * 6;
+    // halves, their exponents, planes of bf16
+    const auto lay = [&](LayArgs<F32> a, char *to, const char *&read, const int32_t *&exponent, const char *&back) {
+        char *exponents = to + round_up((size_t)a.all_rows * p.padded * 4, 256), *planes = exponents + round_up((size_t)a.all_rows * 4, 256);
+        a.halves = (uint16_t *)to, a.exponent = (int32_t *)exponents, a.to = select ? (uint16_t *)planes : nullptr;
+        read = to, exponent = a.exponent, back = planes;
+        k_class_split<<<dim3((unsigned)ceil_div(a.all_rows, 4)), dim3(256), 0, c.stream>>>(a);
     };
-    if (p.w_bytes) {
-        lay(s.w, s.D, s.classes, s.classes, w, nullptr, select, q.w, q.w_bytes, q.w_exponent, q.w_back, q.w_back_bytes);
-    } else {
-        q.w = q.w_back = (const char *)s.w, q.w_bytes = q.w_back_bytes = (int64_t)s.D * 2;
+    lay(lay_args<F32>(s.w, s.D, s.classes, s.classes, s.D, p.padded, nullptr), w, q.w, q.w_exponent, q.w_back);
+    lay(lay_args<F32>(s.x, s.x_stride, c.n, round_up(c.n, 32), s.D, p.padded, select), x, q.x, q.x_exponent, q.x_back);
+    return q;
+}
+StageScoreArgs<BF16> stage_args(const Call &c, const Plan &p, const ScoreArgs<BF16> &s, char *x, char *w, const RowArgs<BF16> *select)
+{
+    StageScoreArgs<BF16> q{};
+    q.s = s, q.plane = p.padded * 2;
+    q.x_bytes = q.w_bytes = q.x_back_bytes = q.w_back_bytes = (int64_t)p.padded * 2;
+    LayArgs<BF16> lw = lay_args<BF16>(s.w, s.D, s.classes, s.classes, s.D, p.padded, nullptr), lx = lay_args<BF16>(s.x, s.x_stride, c.n, round_up(c.n, 32), s.D, p.padded, select);
+    if (select) {
+        // the largest of shares (at w's), the exponent, the values
+        HalvesArgs a{lw, lx, (uint32_t *)w};
+        const auto place = [&](LayArgs<BF16> &m, char *to, const char *&read, const char *&back, const int32_t *&exponent) {
+            m.exponent = (int32_t *)(to + 2 * kLayGroups * 4), m.halves = (uint16_t *)(to + kHalvesHead);
+            read = back = to + kHalvesHead, exponent = m.exponent;
+        };
+        place(a.w, w, q.w, q.w_back, q.w_exponent), place(a.x, x, q.x, q.x_back, q.x_exponent);
+        const auto groups = [&](const LayArgs<BF16> &m) {
+            const int64_t all = ceil_div(m.all_rows * (p.padded / 8), 256);
+            return (uint32_t)(all < 8 * kCus ? all : 8 * kCus);
+        };
+        k_class_largest<<<dim3(2 * kLayGroups), dim3(256), 0, c.stream>>>(a);
+        k_class_halves<<<dim3(groups(a.w) + groups(a.x)), dim3(256), 0, c.stream>>>(a, groups(a.w));
+        return q;
     }
-    if (p.w_bytes || select) {
-        lay(s.x, s.x_stride, c.n, all_rows, x, select, select, q.x, q.x_bytes, q.x_exponent, q.x_back, q.x_back_bytes);
+    q.w = (const char *)s.w, q.x = (const char *)s.x;
+    if (p.w_bytes) {
+        const auto lay = [&](LayArgs<BF16> a, char *to) {
+            a.to = (uint16_t *)to;
+            k_class_lay<<<dim3((unsigned)ceil_div(a.all_rows * (p.padded / 8), 256)), dim3(256), 0, c.stream>>>(a);
+            return to;
+        };
+        q.w = lay(lw, w), q.x = lay(lx, x);
     } else {
-        q.x = (const char *)s.x, q.x_bytes = s.x_stride * 2;
+        q.w_bytes = (int64_t)s.D * 2, q.x_bytes = s.x_stride * 2;
     }
     return q;
 }
@@ -1348,7 +1477,7 @@ int forward(const Call &c, float *loss, float *teacher_loss, float *saved)
     r.loss = loss, r.teacher_loss = teacher_loss, r.saved = saved;
     if (!c.labels) s.k = r.k = s.k_t, s.two = r.two = false;  // (no sums but those at the temperature are asked for)
     StageScoreArgs<T> q{};
-    if (h.large) q = stage_args<T>(c, p, s, x, w, nullptr);
+    if (h.large) q = stage_args(c, p, s, x, w, nullptr);
     for (int64_t row0 = 0; row0 < c.n; row0 += p.pass_rows) {
         s.row0 = r.row0 = row0, s.rows = r.rows = c.n - row0 < p.pass_rows ? c.n - row0 : p.pass_rows;
         s.loss = loss, s.kept = saved, s.whole = !h.large && !c.top_class && c.l->classes <= Large::BA;
@@ -1433,8 +1562,23 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
     s.scale = r.scale = c.labels ? scale : 0.0f;
     s.teacher_scale = r.teacher_scale = c.top_class ? teacher_scale * c.l->temperature : 0.0f;
     r.saved = const_cast<float *>(saved), r.dz = dz, r.dz_stride = (int)p.dz_stride, r.blocks = h.large;
+    s.dz_rest = r.dz_rest = dz + p.piece_rows * p.dz_stride;  // (small calls of bf16)
     StageScoreArgs<T> q{};
-    if (h.large) q = stage_args<T>(c, p, s, x_laid, w_laid, &r);
+    float undo = 1.0f;
+    if (h.large) {
+        q = stage_args(c, p, s, x_laid, w_laid, &r);
+        if (T::PER == 2) {
+            // dz in halves: a power of two takes what it can be at most, |scale| + |teacher_scale|, to [2^13, 2^14]; what is below 2^-28 of that has fewer than a half's
+            // eleven bits, and below 2^-39 none
+            const float most = fabsf(s.scale) + fabsf(s.teacher_scale);
+            if (most > 0.0f && most < INFINITY) {
+                const int up = 13 - ilogbf(most) < 100 ? 13 - ilogbf(most) : 100;
+                undo = ldexpf(1.0f, -up);
+                s.scale = r.scale = ldexpf(s.scale, up), s.teacher_scale = r.teacher_scale = ldexpf(s.teacher_scale, up);
+            }
+        }
+    }
+    const int32_t *const w_up = T::PER == 2 ? q.w_exponent : nullptr, *const x_up = T::PER == 2 ? q.x_exponent : nullptr;
     for (int cp = 0; cp < p.class_pieces; ++cp) {
         const int class0 = cp * p.piece_classes, classes = V - class0 < p.piece_classes ? V - class0 : p.piece_classes;
         const WeightPlan w = weight_plan(c.l, h, classes, p.piece_rows, p.row_pieces);
@@ -1466,17 +1610,17 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
             if (h.large) {
                 StagePieceArgs<T> x{}, y{};
                 fill_dx(x), fill_dw(y);
-                x.b = q.w_back + class0 * q.w_back_bytes, x.b_bytes = q.w_back_bytes;
-                y.b = q.x_back + row0 * q.x_back_bytes, y.b_bytes = q.x_back_bytes;
+                x.b = q.w_back + class0 * q.w_back_bytes, x.b_bytes = q.w_back_bytes, x.exponent = w_up;
+                y.b = q.x_back + row0 * q.x_back_bytes, y.b_bytes = q.x_back_bytes, y.exponent = x_up;
                 y.K = round_up(rows, 32);  // (rows of zeros in both)
-                for (StagePieceArgs<T> *a : {&x, &y}) a->a = (const char *)dz, a->a_rows = (int)round_up(rows, StageCut::BB), a->a_stride = (int)p.dz_stride, a->b_width = p.padded, a->b_plane = q.plane, a->slot_width = p.slot_width;
+                for (StagePieceArgs<T> *a : {&x, &y}) a->a = (const char *)dz, a->a_rows = (int)round_up(rows, StageCut::BB), a->a_stride = (int)p.dz_stride, a->b_width = p.padded, a->b_plane = q.plane, a->slot_width = p.slot_width, a->undo = undo;
                 launch_products<T>(dweight ? &y : nullptr, dx ? &x : nullptr, c.stream);
             } else {
                 PieceArgs<T> x{}, y{};
                 fill_dx(x), fill_dw(y);
                 x.b = s.w + (int64_t)class0 * D, x.b_stride = D;
                 y.b = s.x + row0 * c.x_stride, y.b_stride = c.x_stride, y.list = listed + row0, y.K = rows, y.sums = dbias ? dbias + class0 : nullptr;
-                for (PieceArgs<T> *a : {&x, &y}) a->a = dz, a->a_stride = p.dz_stride, a->a_width = (int)p.dz_stride;
+                for (PieceArgs<T> *a : {&x, &y}) a->a = dz, a->a_rest = s.dz_rest, a->a_stride = p.dz_stride, a->a_width = (int)p.dz_stride;
                 if (dx && dweight && w.tile == p.dx_tile) {
                     launch_products<T>(&y, &x, w.tile, c.stream);
                 } else {
@@ -1485,14 +1629,14 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
                 }
             }
             // (where one piece has all classes; the last piece of rows leaves it to the launch that finishes dW too)
-            x_sums = slots && dx && p.class_pieces == 1 ? ReduceArgs<T>{slots, nullptr, slot_rows, rows, p.slot_width, D, dx_shares, 0, dx + row0 * dx_stride, nullptr, dx_stride} : ReduceArgs<T>{};
+            x_sums = slots && dx && p.class_pieces == 1 ? ReduceArgs<T>{slots, nullptr, slot_rows, rows, p.slot_width, D, dx_shares, 0, dx + row0 * dx_stride, nullptr, dx_stride, w_up, undo} : ReduceArgs<T>{};
             if (x_sums.out && rp + 1 < p.row_pieces) launch_reduce<T>(x_sums, {}, c.stream);
         }
         // (small calls without slots have written both already, large ones dweight)
         E *dw_out = dweight && w.slots ? dweight + (int64_t)class0 * D : nullptr, *db_out = dbias && (w.slots || h.large) ? dbias + class0 : nullptr;
         ReduceArgs<T> w_sums{};
-        if (dw_out || db_out) w_sums = {dw_slots, db_slots, (int64_t)round_up(classes, h.slot_round), classes, p.slot_width, D, w.shares, w.shares * summers_of(c.l, h), dw_out, db_out, D};
-        if (p.dx_bytes && dx && cp > 0 && cp + 1 == p.class_pieces) x_sums = {dx_slots, nullptr, (int64_t)round_up(c.n, h.slot_round), c.n, p.slot_width, D, p.dx_shares, 0, dx, nullptr, dx_stride};
+        if (dw_out || db_out) w_sums = {dw_slots, db_slots, (int64_t)round_up(classes, h.slot_round), classes, p.slot_width, D, w.shares, w.shares * summers_of(c.l, h), dw_out, db_out, D, x_up, undo};
+        if (p.dx_bytes && dx && cp > 0 && cp + 1 == p.class_pieces) x_sums = {dx_slots, nullptr, (int64_t)round_up(c.n, h.slot_round), c.n, p.slot_width, D, p.dx_shares, 0, dx, nullptr, dx_stride, w_up, undo};
         launch_reduce<T>(w_sums, x_sums, c.stream);
     }
     BGL_HIP(hipGetLastError());

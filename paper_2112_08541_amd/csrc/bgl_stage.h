@@ -215,28 +215,29 @@ constexpr int stages() { return 81920 / (A::BYTES + B::BYTES); }
 template <class A, class B>
 constexpr int lds_bytes() { return stages<A, B>() * (A::BYTES + B::BYTES); }
 
-// The operands' planes of product p: hexadecimal digit p.
-template <int PLANES>
+// What operands are made of: a bf16; two halves of a value; three bf16 of a value; a half.  A, B: the planes of product p, hexadecimal digit p.
+enum Kind { ONE_BF16, TWO_HALVES, THREE_BF16, ONE_HALF };
+template <Kind KIND>
 struct Pairs {
-    static constexpr int COUNT = PLANES == 1 ? 1 : PLANES == 2 ? 3 : 6;
+    static constexpr bool HALF = KIND == TWO_HALVES || KIND == ONE_HALF;
+    static constexpr int PLANES = KIND == TWO_HALVES ? 2 : KIND == THREE_BF16 ? 3 : 1, COUNT = PLANES == 1 ? 1 : PLANES == 2 ? 3 : 6;
     static constexpr uint32_t A = PLANES == 2 ? 0x100 : 0x010210, B = PLANES == 2 ? 0x010 : 0x211000;
 };
-// PLANES of 2 are halves, else bf16.
-template <int PLANES>
+template <Kind KIND>
 __device__ __forceinline__ f32x4 mma(const bf16x8 &a, const bf16x8 &b, const f32x4 &c)
 {
-    if constexpr (PLANES == 2) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    if constexpr (Pairs<KIND>::HALF) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// Adds the product to acc: of a fragment pair a lane has rows 4 (lane / 16) .. + 3 of a and row lane % 16 of b, TURNED the other way round.  PLANES: 1, 2 (three products of halves) or 3 (six products).  also(stage, plane of b, a's fragments) sees every 32 summed values.  Ends with all of LDS free.
-template <int PLANES, bool TURNED, class A, class B, class C, class Also>
+// Adds the product to acc: of a fragment pair a lane has rows 4 (lane / 16) .. + 3 of a and row lane % 16 of b, TURNED the other way round.  also(stage, plane of b, a's fragments) sees every 32 summed values.  Ends with all of LDS free.
+template <Kind KIND, bool TURNED, class A, class B, class C, class Also>
 __device__ __forceinline__ void multiply(char *lds, const A &a, const B &b, const Walk &w, f32x4 (&acc)[C::FA][C::FB], Also also)
 {
     static_assert(A::STEP == B::STEP, "");
-    constexpr int STEP = A::STEP, STAGES = stages<A, B>(), PAIRS = Pairs<PLANES>::COUNT, BYTES = A::BYTES + B::BYTES, LOADS = A::LOADS + B::LOADS;
+    constexpr int STEP = A::STEP, STAGES = stages<A, B>(), PLANES = Pairs<KIND>::PLANES, PAIRS = Pairs<KIND>::COUNT, BYTES = A::BYTES + B::BYTES, LOADS = A::LOADS + B::LOADS;
     static_assert(STAGES == 2 || STAGES == 3, "");
-    constexpr uint32_t PLANE_A = Pairs<PLANES>::A, PLANE_B = Pairs<PLANES>::B;
+    constexpr uint32_t PLANE_A = Pairs<KIND>::A, PLANE_B = Pairs<KIND>::B;
     const int blocks = (w.count + STEP - 1) / STEP, steps = blocks * PAIRS;
     int block = w.first, pair = 0, to = 0;  // of the next stage to load
     const auto load = [&] {
@@ -272,7 +273,7 @@ __device__ __forceinline__ void multiply(char *lds, const A &a, const B &b, cons
             for (int i = 0; i < C::FA; ++i)
 #pragma unroll
                 for (int j = 0; j < C::FB; ++j)
-                    acc[i][j] = TURNED ? mma<PLANES>(fb[j], fa[i], acc[i][j]) : mma<PLANES>(fa[i], fb[j], acc[i][j]);
+                    acc[i][j] = TURNED ? mma<KIND>(fb[j], fa[i], acc[i][j]) : mma<KIND>(fa[i], fb[j], acc[i][j]);
             also(s, PLANE_B >> 4 * plane & 3, fa);
         }
         if (++plane == PAIRS) plane = 0;
