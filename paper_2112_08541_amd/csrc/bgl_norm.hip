@@ -152,7 +152,7 @@ __device__ __forceinline__ void moments(const Piece<T, TEAM> &p, float (&v)[kVal
     mean = m / scale, rest = c / scale;
 }
 
-// A row's threads: 16 values each, a team of 8 to 1,024.  A workgroup has 256 threads or one team.
+// A row's threads: 16 values each, a team of 1 to 1,024.  A workgroup has 256 threads or one team.
 template <class T, int TEAM>
 __global__ void __launch_bounds__(norm_threads<TEAM>()) k_norm_forward(NormArgs<T> a)
 {
@@ -278,7 +278,7 @@ __global__ void __launch_bounds__(1024) k_norm_reduce(NormArgs<T> a)
 
 int team_of(int width)
 {
-    int team = 8;
+    int team = 1;
     while (team * kValues < width) team *= 2;
     return team;
 }
@@ -286,14 +286,19 @@ int teams_of(int team) { return team < 256 ? 256 / team : 1; }
 
 int parts_of(int width, int64_t n)
 {
-    const int64_t groups = ceil_div(n, teams_of(team_of(width)));
-    return (int)(groups < kMaxParts ? groups : kMaxParts);
+    // (a row of partial sums is as wide as two of x: with one for each of few wide rows they took longer than these)
+    const int teams = teams_of(team_of(width));
+    const int64_t groups = teams > 1 ? ceil_div(n, teams) : ceil_div(n, 4), most = teams > 1 ? kMaxParts : kMaxParts / 2;
+    return (int)(groups < most ? groups : most);
 }
 
 template <class F>
 void with_team(int team, F f)
 {
     switch (team) {
+    case 1: return f(std::integral_constant<int, 1>{});
+    case 2: return f(std::integral_constant<int, 2>{});
+    case 4: return f(std::integral_constant<int, 4>{});
     case 8: return f(std::integral_constant<int, 8>{});
     case 16: return f(std::integral_constant<int, 16>{});
     case 32: return f(std::integral_constant<int, 32>{});
