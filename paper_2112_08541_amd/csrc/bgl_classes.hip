@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_scores(ScoreArgs<T> a)
     __shared__ float meet[DZ ? 1 : 3 * C::BA / 16 / C::FA * C::BB], own_score[DZ ? 1 : C::BB];
     int64_t ct, rt;
     int fast;
-    if (!tile_of(blockIdx.x, a.by_rows ? a.row_tiles : a.class_tiles, (int)(a.by_rows ? a.class_tiles : a.row_tiles), a.by_rows ? rt : ct, fast)) return;
+    if (!stage::tile_of(blockIdx.x, (uint32_t)(a.by_rows ? a.row_tiles : a.class_tiles), (uint32_t)(a.by_rows ? a.class_tiles : a.row_tiles), 1, a.by_rows ? rt : ct, fast)) return;
     (a.by_rows ? ct : rt) = fast;
     const int c0 = a.class0 + (int)ct * C::BA, last = a.classes - 1;
     const int64_t r0 = rt * C::BB;  // of this launch's rows
@@ -503,7 +503,7 @@ struct PieceArgs {
     int N, a_width;                 // columns of the result; of dz that can be read
     int64_t row_tiles;
     int col_tiles, shares;
-    uint32_t tiles;                 // of a share, a multiple of 8
+    uint32_t tiles;                 // of a share
     int64_t per_share;              // of the summed index
     typename T::elem *out, *sums;   // the result, if it is whole; M values of sums over the summed index
     int64_t out_stride;
@@ -544,7 +544,7 @@ __device__ __forceinline__ void Product<T, C, OC, NARROW>::make(const PieceArgs<
     const int share = (int)(id / a.tiles);
     int64_t rt;
     int ct;
-    if (!tile_of(id % a.tiles, a.row_tiles, a.col_tiles, rt, ct)) return;
+    if (!stage::tile_of(id % a.tiles, (uint32_t)a.row_tiles, a.col_tiles, 1, rt, ct)) return;
     const int64_t m0 = rt * C::BA, k0 = share * a.per_share;
     const int n0 = ct * C::BB, K = (int)(a.K - k0 < a.per_share ? a.K - k0 : a.per_share);
     f32x4 acc[C::FA][C::FB] = {};
@@ -1113,7 +1113,7 @@ __device__ __forceinline__ void StageProduct<T, OC>::make(const StagePieceArgs<T
     const int share = (int)(id % (uint32_t)a.shares);
     int64_t rt;
     int ct;
-    if (!tile_of(id / (uint32_t)a.shares, a.row_tiles, a.col_tiles, rt, ct)) return;
+    if (!stage::tile_of(id / (uint32_t)a.shares, (uint32_t)a.row_tiles, a.col_tiles, 1, rt, ct)) return;
     const int64_t m0 = rt * C::BA, k0 = share * a.per_share;
     const int n0 = ct * C::BB, K = (int)(a.K - k0 < a.per_share ? a.K - k0 : a.per_share);
     A left;
@@ -1364,7 +1364,7 @@ void launch_scores(ScoreArgs<T> &s, hipStream_t st)
         s.class_tiles = (int)ceil_div(s.classes - s.class0, C::BA);
         s.row_tiles = ceil_div(s.rows, C::BB);
         s.by_rows = s.row_tiles > s.class_tiles;
-        const int64_t tiles = s.by_rows ? tile_count(s.row_tiles, s.class_tiles) : tile_count(s.class_tiles, (int)s.row_tiles);
+        const int64_t tiles = s.by_rows ? stage::tile_count(s.row_tiles, s.class_tiles) : stage::tile_count(s.class_tiles, s.row_tiles);
         k_class_scores<T, C, DZ><<<dim3((unsigned)tiles), dim3(kThreads), 0, st>>>(s);
     };
     // the largest tiles that the rows fill and that leave no CU without one: 1,024 x 128 x 50 f32 took 15 us in 8 tiles of 128 x 128
@@ -1416,7 +1416,7 @@ void launch_scores_stage(StageScoreArgs<T> &q, hipStream_t st)
     s.class_tiles = (int)ceil_div(s.classes - s.class0, StageCut::BA);
     s.row_tiles = ceil_div(s.rows, StageCut::BB);
     s.by_rows = s.row_tiles > s.class_tiles;
-    const int64_t tiles = s.by_rows ? tile_count(s.row_tiles, s.class_tiles) : tile_count(s.class_tiles, (int)s.row_tiles);
+    const int64_t tiles = s.by_rows ? stage::tile_count(s.row_tiles, s.class_tiles) : stage::tile_count(s.class_tiles, s.row_tiles);
     k_class_scores_stage<T, DZ><<<dim3((unsigned)tiles), dim3(stage::kThreads), 0, st>>>(q);
 }
 
@@ -1539,7 +1539,7 @@ void launch_products(PieceArgs<T> *dw, PieceArgs<T> *dx, int tile, hipStream_t s
         uint32_t groups[2] = {};
         for (int i = 0; i < 2; ++i)
             if (PieceArgs<T> *a = i ? dx : dw) {
-                a->row_tiles = ceil_div(a->M, C::BA), a->col_tiles = (int)ceil_div(a->N, C::BB), a->tiles = (uint32_t)tile_count(a->row_tiles, a->col_tiles);
+                a->row_tiles = ceil_div(a->M, C::BA), a->col_tiles = (int)ceil_div(a->N, C::BB), a->tiles = (uint32_t)stage::tile_count(a->row_tiles, a->col_tiles);
                 groups[i] = a->tiles * a->shares;
             }
         k_class_products<T, C, decltype(narrow)::value><<<dim3(groups[0] + groups[1]), dim3(kThreads), 0, st>>>(dw ? *dw : PieceArgs<T>{}, dx ? *dx : PieceArgs<T>{}, groups[0]);
@@ -1555,7 +1555,7 @@ void launch_products(StagePieceArgs<T> *dw, StagePieceArgs<T> *dx, hipStream_t s
     for (int i = 0; i < 2; ++i)
         if (StagePieceArgs<T> *a = i ? dx : dw) {
             a->row_tiles = ceil_div(a->M, ProductCut::BA), a->col_tiles = (int)ceil_div(a->N, ProductCut::BB);
-            groups[i] = (uint32_t)(tile_count(a->row_tiles, a->col_tiles) * a->shares);
+            groups[i] = (uint32_t)(stage::tile_count(a->row_tiles, a->col_tiles) * a->shares);
         }
     k_class_products_stage<T><<<dim3(groups[0] + groups[1]), dim3(stage::kThreads), 0, st>>>(dw ? *dw : StagePieceArgs<T>{}, dx ? *dx : StagePieceArgs<T>{}, groups[0]);
 }

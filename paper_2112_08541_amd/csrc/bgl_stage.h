@@ -184,9 +184,16 @@ struct OcBlocks {
 };
 
 // Tiles in an order for eight XCDs (workgroup numbers go round them): each takes every eighth of the slow tiles, `group` of these at a time, which share its L2
-// while the fast ones go by.  tile::tile_count(slow, fast) workgroups.
+// while the fast ones go by.  With few slow tiles that would leave XCDs with less to do, or with nothing: then all tiles in a row.
+constexpr int64_t kDealtFrom = 64;
+inline int64_t tile_count(int64_t slow_tiles, int64_t fast_tiles) { return (slow_tiles < kDealtFrom ? slow_tiles : (slow_tiles + 7) / 8 * 8) * fast_tiles; }
 __device__ __forceinline__ bool tile_of(uint32_t id, uint32_t slow_tiles, uint32_t fast_tiles, uint32_t group, int64_t &slow, int &fast)
 {
+    if (slow_tiles < kDealtFrom) {
+        slow = __builtin_amdgcn_readfirstlane(id / fast_tiles);
+        fast = __builtin_amdgcn_readfirstlane(id % fast_tiles);
+        return true;
+    }
     const uint32_t j = id >> 3, mine = (slow_tiles + 7) / 8, g = j / (group * fast_tiles) * group, in = j - g * fast_tiles;
     const uint32_t wide = mine - g < group ? mine - g : group;
     fast = __builtin_amdgcn_readfirstlane(in / wide);
