@@ -1204,6 +1204,9 @@ using Middle = Cut<2, 2, 4, 2>;  // 128 x 64
 using Low = Cut<4, 1, 2, 1>;     // 128 x 16
 using Slim = Cut<4, 1, 1, 1>;    // 64 x 16
 using Small = Cut<2, 2, 2, 2>;   // 64 x 64
+using Flat = Cut<1, 4, 1, 2>;    // 16 x 128
+using Flat2 = Cut<1, 4, 2, 2>;   // 32 x 128
+using Flat4 = Cut<1, 4, 4, 2>;   // 64 x 128
 
 struct Plan {
     // forward
@@ -1238,7 +1241,8 @@ Scheme scheme_of(const bgl_class_loss_t *l, bool large)
 bool large_call(const bgl_class_loss_t *l, int64_t n) { return n >= 96 && l->classes >= 128 && (double)n * l->classes * l->in_dim >= kLargeProducts; }
 bool laid_out(const bgl_class_loss_t *l) { return l->dtype == BGL_BF16 && l->in_dim % kPad == 0; }
 
-// Ranges of the summed index that a product of rows x cols is made in, and the tiles' size: small calls take tiles of 64 x 64 where 128 x 128 do not fill the GPU.
+// Ranges of the summed index that a product of rows x cols is made in, and the tiles' rows: small calls take tiles of 16 x 128 for up to 16 rows (in 128 x 128 the
+// matrix units worked for nothing: a row of 133 and 37,570 classes 60 us) and of 64 x 64 where 128 x 128 do not fill the GPU.
 int shares_for(const Scheme &s, int64_t rows, int64_t cols, int64_t summed, int &tile)
 {
     const int64_t most = summed / s.least;
@@ -1246,9 +1250,9 @@ int shares_for(const Scheme &s, int64_t rows, int64_t cols, int64_t summed, int 
         const int64_t want = s.fill / (tiles < 1 ? 1 : tiles);
         return want < 1 || most < 1 ? 1 : want < most ? want : most;
     };
-    tile = s.product_rows;
+    tile = !s.large && rows <= Flat::BA ? Flat::BA : s.product_rows;
     int64_t tiles = ceil_div(rows, tile) * ceil_div(cols, 128);
-    if (!s.large && tiles * fit(tiles) < s.fill / 2) tile = 64, tiles = ceil_div(rows, 64) * ceil_div(cols, 64);
+    if (!s.large && tile != Flat::BA && tiles * fit(tiles) < s.fill / 2) tile = 64, tiles = ceil_div(rows, 64) * ceil_div(cols, 64);
     return (int)fit(tiles);
 }
 
@@ -1369,7 +1373,12 @@ void launch_scores(ScoreArgs<T> &s, hipStream_t st)
     };
     // the largest tiles that the rows fill and that leave no CU without one: 1,024 x 128 x 50 f32 took 15 us in 8 tiles of 128 x 128
     const int64_t classes = s.classes - s.class0, across = ceil_div(classes, 128);
-    if (s.rows > 64 && across * ceil_div(s.rows, 128) >= kCus) go(Large{});
+    // (13 classes of 32,780 rows of 266 f32 took 43 us in tiles of 128 classes)
+    if (classes <= 64 && s.rows >= 128 * kCus / 4) {
+        if (classes <= 16) go(Flat{});
+        else if (classes <= 32) go(Flat2{});
+        else go(Flat4{});
+    } else if (s.rows > 64 && across * ceil_div(s.rows, 128) >= kCus) go(Large{});
     else if (s.rows > 16 && across * ceil_div(s.rows, 64) >= kCus) go(Middle{});
     else if (classes > 64) go(Low{});
     else go(Slim{});
@@ -1530,7 +1539,7 @@ int forward(const Call &c, float *loss, float *teacher_loss, float *saved)
     return BGL_OK;
 }
 
-// dW of a piece, dx of it, or both; tile: 64 or 128.
+// dW of a piece, dx of it, or both; tile: its rows.
 template <class T>
 void launch_products(PieceArgs<T> *dw, PieceArgs<T> *dx, int tile, hipStream_t st)
 {
@@ -1545,7 +1554,8 @@ void launch_products(PieceArgs<T> *dw, PieceArgs<T> *dx, int tile, hipStream_t s
         k_class_products<T, C, decltype(narrow)::value><<<dim3(groups[0] + groups[1]), dim3(kThreads), 0, st>>>(dw ? *dw : PieceArgs<T>{}, dx ? *dx : PieceArgs<T>{}, groups[0]);
     };
     if ((dw ? dw : dx)->N < T::VEC) go(Small{}, std::true_type{});  // (one form of reading rows shorter than 16 bytes will do)
-    else if (tile == 64) go(Small{}, std::false_type{});
+    else if (tile == Flat::BA) go(Flat{}, std::false_type{});
+    else if (tile == Small::BA) go(Small{}, std::false_type{});
     else go(Large{}, std::false_type{});
 }
 template <class T>
