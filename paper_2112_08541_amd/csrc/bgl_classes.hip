@@ -27,7 +27,9 @@ constexpr int64_t kPieceRows = 16384;
 constexpr int64_t kPieceClasses = 256;                 // pieces of some classes only are multiples
 constexpr int64_t kPartialBytes = (int64_t)64 << 20;   // of a forward call's tiles' maxima and sums
 constexpr int kCus = 256;
-constexpr double kLargeProducts = 5e8;                 // of a call that is laid out for large tiles
+constexpr int64_t kMostThreads = (int64_t)1 << 31;     // of a launch, which has room for 2^32 - 1
+constexpr double kLargeProducts = 2e9;                 // of a call that is laid out for large tiles: 512 x 256 x 4,096 f32 took 30 + 110 us so and 19 + 58 in small ones,
+                                                       // 1,316 x 503 x 3,640 45 + 167 and 77 + 199; bf16 15 + 42 and 11 + 40, 29 + 66 and 24 + 83
 
 // Exponentials are powers of two: exp(k v) / 2^base with k = log2(e) or that over the temperature, as 2^(k v - base) with one rounding.  A sum of them is taken to
 // the base of its largest value, base(most) = k most, rounded: sums of two bases meet exactly, as the bases' difference has no rounding to speak of.
@@ -653,14 +655,15 @@ struct ReduceArgs {
 };
 // LANES neighbours share what there is to add: 1 for few ranges, 8 for many.
 template <class T, int LANES>
-__global__ void __launch_bounds__(256) k_class_reduce(ReduceArgs<T> one, ReduceArgs<T> two, uint32_t one_groups)
+__global__ void __launch_bounds__(256) k_class_reduce(ReduceArgs<T> one, ReduceArgs<T> two, uint32_t one_groups, uint32_t group0)
 {
     constexpr int PER = 256 / LANES;
     __shared__ f32x4 meet[LANES > 1 ? LANES : 1][LANES > 1 ? PER : 1];
-    const bool first = blockIdx.x < one_groups;
+    const uint32_t group = group0 + blockIdx.x;
+    const bool first = group < one_groups;
     const ReduceArgs<T> &a = first ? one : two;
     const int item = threadIdx.x % PER, lane = threadIdx.x / PER;
-    const uint64_t i = (uint64_t)(first ? blockIdx.x : blockIdx.x - one_groups) * PER + item;
+    const uint64_t i = (uint64_t)(first ? group : group - one_groups) * PER + item;
     const uint32_t fours = (uint32_t)(a.width + 3) / 4;
     const uint64_t values = a.out ? (uint64_t)a.rows * fours : 0;
     const bool value = i < values, sum = !value && a.sums && i - values < (uint64_t)a.rows;
@@ -709,8 +712,7 @@ __global__ void __launch_bounds__(256) k_class_reduce(ReduceArgs<T> one, ReduceA
 template <class T>
 __global__ void __launch_bounds__(256) k_class_zero(typename T::elem *p, int64_t count)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i < count) p[i] = T::put(0.0f);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) p[i] = T::put(0.0f);
 }
 
 // ----------------------------------------------------------------- large calls: operands laid out for bgl_stage.h
@@ -744,12 +746,18 @@ __device__ __forceinline__ uint4 eight(const LayArgs<BF16> &a, int64_t row, int 
     const uint16_t *from = a.from + row * a.stride + d;
     return d + 8 <= a.D ? load_any<uint4>(from) : load_end<BF16>(from, a.D - d, a.D);
 }
+template <class F>
+__device__ __forceinline__ void each_eight(const LayArgs<BF16> &a, uint32_t group, uint32_t groups, F f)
+{
+    const uint64_t each = a.padded / 8, all = (uint64_t)a.all_rows * each;
+    for (uint64_t i = (uint64_t)group * 256 + threadIdx.x; i < all; i += (uint64_t)groups * 256) {
+        const uint64_t row = all >> 32 ? i / each : (uint32_t)i / (uint32_t)each;
+        f((int64_t)row, (int)(i - row * each) * 8);
+    }
+}
 __global__ void __launch_bounds__(256) k_class_lay(LayArgs<BF16> a)
 {
-    const int each = a.padded / 8;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / each;
-    const int d = (int)(i % each) * 8;
-    if (row < a.all_rows) *reinterpret_cast<uint4 *>(a.to + row * a.padded + d) = eight(a, row, d);
+    each_eight(a, blockIdx.x, gridDim.x, [&](int64_t row, int d) { *reinterpret_cast<uint4 *>(a.to + row * a.padded + d) = eight(a, row, d); });
 }
 
 // bf16 rows and weight as halves, for the backward call, whose dz is in halves: times 2^-exponent, one for all of x and one for all of W, so that the largest is
@@ -778,15 +786,6 @@ __device__ __forceinline__ uint32_t group_largest(uint32_t v)
     if (threadIdx.x % 64 == 0) all[threadIdx.x / 64] = w;
     __syncthreads();
     return (uint32_t)fmaxf(fmaxf(all[0], all[1]), fmaxf(all[2], all[3]));
-}
-template <class F>
-__device__ __forceinline__ void each_eight(const LayArgs<BF16> &a, uint32_t group, uint32_t groups, F f)
-{
-    const uint64_t each = a.padded / 8, all = (uint64_t)a.all_rows * each;
-    for (uint64_t i = (uint64_t)group * 256 + threadIdx.x; i < all; i += (uint64_t)groups * 256) {
-        const uint64_t row = all >> 32 ? i / each : (uint32_t)i / (uint32_t)each;
-        f((int64_t)row, (int)(i - row * each) * 8);
-    }
 }
 __global__ void __launch_bounds__(256) k_class_largest(HalvesArgs a)
 {
@@ -826,9 +825,9 @@ __global__ void __launch_bounds__(256) k_class_halves(HalvesArgs a, uint32_t w_g
     });
 }
 // A wavefront for a row: its largest value first, then its planes.
-__global__ void __launch_bounds__(256) k_class_split(LayArgs<F32> a)
+__global__ void __launch_bounds__(256) k_class_split(LayArgs<F32> a, int64_t row0)
 {
-    const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+    const int64_t row = row0 + (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
     const int l = threadIdx.x & 63;
     if (row >= a.all_rows) return;
     const bool live = lives(a, row);
@@ -1208,6 +1207,8 @@ using Flat = Cut<1, 4, 1, 2>;    // 16 x 128
 using Flat2 = Cut<1, 4, 2, 2>;   // 32 x 128
 using Flat4 = Cut<1, 4, 4, 2>;   // 64 x 128
 
+uint32_t groups_for(int64_t groups) { return (uint32_t)(groups < kMostThreads / 256 ? groups : kMostThreads / 256); }  // (of kernels that go round)
+
 struct Plan {
     // forward
     int64_t pass_rows;
@@ -1285,6 +1286,8 @@ Plan plan_of(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
     p.class_parts = (int)ceil_div(l->classes, s.score_classes) * (s.large ? 2 : 1);  // (tiles of 64 classes: only where one has them all)
     p.pass_rows = kPartialBytes / (12 * (int64_t)p.class_parts);
     p.pass_rows = p.pass_rows < 1024 ? 1024 : p.pass_rows / 128 * 128;
+    const int64_t top_rows = kMostThreads / (2 * l->top + 8) / 128 * 128;  // (k_class_top's)
+    if (p.pass_rows > top_rows) p.pass_rows = top_rows;
     if (p.pass_rows > n) p.pass_rows = n;
     p.part_bytes = round_up((size_t)p.pass_rows * p.class_parts * 12, 256);
     p.label_bytes = round_up((size_t)n * 4, 256);
@@ -1460,7 +1463,8 @@ StageScoreArgs<F32> stage_args(const Call &c, const Plan &p, const ScoreArgs<F32
         char *exponents = to + round_up((size_t)a.all_rows * p.padded * 4, 256), *planes = exponents + round_up((size_t)a.all_rows * 4, 256);
         a.halves = (uint16_t *)to, a.exponent = (int32_t *)exponents, a.to = select ? (uint16_t *)planes : nullptr;
         read = to, exponent = a.exponent, back = planes;
-        k_class_split<<<dim3((unsigned)ceil_div(a.all_rows, 4)), dim3(256), 0, c.stream>>>(a);
+        const int64_t most = kMostThreads / 64;
+        for (int64_t row0 = 0; row0 < a.all_rows; row0 += most) k_class_split<<<dim3((unsigned)ceil_div(a.all_rows - row0 < most ? a.all_rows - row0 : most, 4)), dim3(256), 0, c.stream>>>(a, row0);
     };
     lay(lay_args<F32>(s.w, s.D, s.classes, s.classes, s.D, p.padded, nullptr), w, q.w, q.w_exponent, q.w_back);
     lay(lay_args<F32>(s.x, s.x_stride, c.n, round_up(c.n, 32), s.D, p.padded, select), x, q.x, q.x_exponent, q.x_back);
@@ -1492,7 +1496,7 @@ StageScoreArgs<BF16> stage_args(const Call &c, const Plan &p, const ScoreArgs<BF
     if (p.w_bytes) {
         const auto lay = [&](LayArgs<BF16> a, char *to) {
             a.to = (uint16_t *)to;
-            k_class_lay<<<dim3((unsigned)ceil_div(a.all_rows * (p.padded / 8), 256)), dim3(256), 0, c.stream>>>(a);
+            k_class_lay<<<dim3(groups_for(ceil_div(a.all_rows * (p.padded / 8), 256))), dim3(256), 0, c.stream>>>(a);
             return to;
         };
         q.w = lay(lw, w), q.x = lay(lx, x);
@@ -1575,10 +1579,12 @@ void launch_reduce(const ReduceArgs<T> &one, const ReduceArgs<T> &two, hipStream
 {
     const bool many = (one.out && one.shares > 8) || (one.sums && one.sum_shares > 8) || (two.out && two.shares > 8);
     const auto groups = [&](const ReduceArgs<T> &a) { return (uint32_t)ceil_div((a.out ? a.rows * ceil_div(a.width, 4) : 0) + (a.sums ? a.rows : 0), many ? 32 : 256); };
-    const uint32_t all = groups(one) + groups(two);
-    if (all == 0) return;
-    if (many) k_class_reduce<T, 8><<<dim3(all), dim3(256), 0, st>>>(one, two, groups(one));
-    else k_class_reduce<T, 1><<<dim3(all), dim3(256), 0, st>>>(one, two, groups(one));
+    const uint32_t all = groups(one) + groups(two), most = kMostThreads / 256;
+    for (uint32_t group0 = 0; group0 < all; group0 += most) {
+        const uint32_t count = all - group0 < most ? all - group0 : most;
+        if (many) k_class_reduce<T, 8><<<dim3(count), dim3(256), 0, st>>>(one, two, groups(one), group0);
+        else k_class_reduce<T, 1><<<dim3(count), dim3(256), 0, st>>>(one, two, groups(one), group0);
+    }
 }
 
 template <class T>
@@ -1588,8 +1594,9 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
     E *dx = (E *)dx_, *dweight = (E *)dweight_, *dbias = (E *)dbias_;
     const int D = c.l->in_dim, V = c.l->classes;
     if (c.n == 0) {
-        if (dweight) k_class_zero<T><<<dim3((unsigned)ceil_div((int64_t)V * D, 256)), dim3(256), 0, c.stream>>>(dweight, (int64_t)V * D);
-        if (dbias) k_class_zero<T><<<dim3((unsigned)ceil_div(V, 256)), dim3(256), 0, c.stream>>>(dbias, V);
+        const auto zero = [&](E *to, int64_t count) { k_class_zero<T><<<dim3(groups_for(ceil_div(count, 256))), dim3(256), 0, c.stream>>>(to, count); };
+        if (dweight) zero(dweight, (int64_t)V * D);
+        if (dbias) zero(dbias, V);
         BGL_HIP(hipGetLastError());
         return BGL_OK;
     }

@@ -17,6 +17,7 @@ namespace {
 using namespace tile;
 
 constexpr int kValues = 16;          // of a row a thread holds
+constexpr int64_t kMostThreads = (int64_t)1 << 31;     // of a launch, which has room for 2^32 - 1
 constexpr int kMaxParts = 512;       // workgroups of a backward call that sums weight gradients, so rows of its partial sums
 constexpr float kFar = 0x1p-80f;     // scales rows whose squares leave fp32's range
 
@@ -315,7 +316,12 @@ int forward(NormArgs<T> a, hipStream_t st)
 {
     with_team(team_of(a.width), [&](auto team) {
         constexpr int TEAM = decltype(team)::value;
-        k_norm_forward<T, TEAM><<<dim3((unsigned)ceil_div(a.n, teams_of(TEAM))), dim3(norm_threads<TEAM>()), 0, st>>>(a);
+        const int64_t n = a.n, most = kMostThreads / TEAM;
+        for (int64_t row0 = 0; row0 < n; row0 += most) {
+            a.n = n - row0 < most ? n - row0 : most;
+            k_norm_forward<T, TEAM><<<dim3((unsigned)ceil_div(a.n, teams_of(TEAM))), dim3(norm_threads<TEAM>()), 0, st>>>(a);
+            a.x += a.n * a.x_stride, a.out += a.n * a.out_stride, a.saved = a.saved ? a.saved + 2 * a.n : nullptr;
+        }
     });
     BGL_HIP(hipGetLastError());
     return BGL_OK;
@@ -329,7 +335,7 @@ int backward(NormArgs<T> a, hipStream_t st)
         with_team(team_of(a.width), [&](auto team) {
             constexpr int TEAM = decltype(team)::value;
             if (sums) k_norm_backward<T, TEAM, true><<<dim3((unsigned)a.parts), dim3(norm_threads<TEAM>()), 0, st>>>(a);
-            else k_norm_backward<T, TEAM, false><<<dim3((unsigned)ceil_div(a.n, teams_of(TEAM))), dim3(norm_threads<TEAM>()), 0, st>>>(a);
+            else k_norm_backward<T, TEAM, false><<<dim3((unsigned)ceil_div(a.n < kMostThreads / TEAM ? a.n : kMostThreads / TEAM, teams_of(TEAM))), dim3(norm_threads<TEAM>()), 0, st>>>(a);
         });
         BGL_HIP(hipGetLastError());
     }

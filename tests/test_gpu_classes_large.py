@@ -1,0 +1,173 @@
+"""Losses over class scores at sizes that are laid out for large tiles, against the definition in 64 bits.
+
+The bounds are those of the small sizes (test_gpu_classes.py: u = 2^-24, a score is off by (D + 4) u (sum|x||w| + |b|)) and what the laid out operands add.
+fp32 scores: a value is two halves of a power of two of its row, 2^-22 of itself or 2^-40 of the row's largest off; of two values' product the three larger ones of four
+parts are taken: 3 x 2^-22 = 12 u of the product, so D + 16 for D + 4, which 12 columns of zeros give the reference; a value below 2^-18 of its row's largest is off by less
+than 2^-40 of that, (x, w)'s product by 2^-40 (|w| max|x| + |x| max|w|), which `far` adds where rows reach so far.
+fp32 products: of three bf16 parts each all but the last ones: 4 u, in the 8 u of the bounds.
+bf16: products are exact; dz has eleven bits and not eight, so the type's bounds hold for it; below 2^-28 of s + s' it loses bits and is 2^-40 (s + s') off at most, which
+`far` adds too."""
+import pytest
+
+from test_gpu_classes import B, Reference, V, check, dtype_of, inputs, run, torch  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def check_large(torch, B, kind, data, t=1.0, s=0.3, st=0.7, head=None, far=False):
+    x, w, b, labels, teacher = data
+    pad = lambda v: torch.cat([v, torch.zeros((len(v), 12), dtype=v.dtype, device="cuda")], 1)      # noqa: E731
+    live = None if labels is None else ((labels >= 0) & (labels < len(w)))
+    x_ref = x if live is None or teacher is not None else torch.where(live[:, None], x, torch.zeros_like(x))      # (rows without a label may hold anything)
+    ref = Reference(torch, pad(x_ref), pad(w), b, labels, teacher, t, V[kind])
+    got = run(torch, B, kind, x, w, b, labels, teacher, t, s, st, head=head)
+    if labels is not None:
+        check("loss", got["loss"], ref.loss, ref.loss_bound)
+    if teacher is not None:
+        check("teacher_loss", got["teacher_loss"], ref.teacher_loss, ref.teacher_bound)
+    want = ref.gradients(s if labels is not None else 0.0, st if teacher is not None else 0.0)
+    D = x.shape[1]
+    more = [0.0, 0.0, 0.0]
+    if far:
+        least = 2.0 ** -40 * (abs(s) + t * abs(st))
+        more = [least * w.double().abs().sum(0), least * x_ref.double().abs().sum(0), least * len(x)]
+    for name, (value, bound), extra in zip(("dx", "dweight", "dbias"), want, more):
+        if name != "dbias":
+            value, bound = value[:, :D], bound[:, :D]
+        check(name, got[name], value, bound + extra)
+    return got
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("n,D,C,k", [(20_500, 16, 7_100, 3), (8_300, 17, 17_300, 0), (17_000, 9, 16_500, 2)])
+def test_pieces(torch, B, kind, n, D, C, k):
+    """dz in pieces of rows, of classes, and of both."""
+    data = inputs(torch, kind, n, D, C, k, seed=n)
+    got = check_large(torch, B, kind, data, t=2.0, s=1.0 / n, st=1.0 / n if k else 0.0)
+    for name in ("dx", "dweight"):
+        half = run(torch, B, kind, *data, 2.0, 1.0 / n, 1.0 / n if k else 0.0, want=(name,))
+        assert torch.equal(half[name], got[name])
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("n,D,C,k", [(97, 513, 41_003, 0), (129, 1_021, 15_999, 5), (2_003, 1_001, 1_005, 1), (16_500, 1_000, 129, 0), (40_001, 399, 131, 3), (2_100, 992, 1_024, 2)])
+def test_odd_sizes(torch, B, kind, n, D, C, k):
+    data = inputs(torch, kind, n, D, C, k, seed=n, pad=5 if n % 2 else 0, bias=n % 3 > 0)
+    got = check_large(torch, B, kind, data, t=1.5, s=1.0 / n, st=0.5 / n if k else 0.0)
+    again = run(torch, B, kind, *data, 1.5, 1.0 / n, 0.5 / n if k else 0.0)
+    assert all(torch.equal(got[i], again[i]) for i in got if got[i] is not None)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_rows_of_other_alignments(torch, B, kind):
+    """The operands one value behind a boundary of 16 bytes, and rows of x of an odd stride, beside aligned ones."""
+    n, D, C = 500, 512, 8_200
+    x, w, b, labels, _ = data = inputs(torch, kind, n, D, C, 0, seed=2)
+    check_large(torch, B, kind, data, s=1.0 / n)
+    near = lambda v: torch.cat([v.new_zeros(1), v.flatten()])[1:].view(v.shape)      # noqa: E731
+    check_large(torch, B, kind, (near(x), near(w), near(b), near(labels), None), s=1.0 / n)
+    wide = torch.full((n, D + 3), float("nan"), dtype=x.dtype, device="cuda")
+    wide[:, :D] = x
+    check_large(torch, B, kind, (wide[:, :D], w, b, labels, None), s=1.0 / n)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_rows_that_differ_much(torch, B, kind):
+    """Rows of x and of the weight from the smallest to large numbers, columns too, and scores far apart."""
+    n, D, C = 700, 320, 9_100
+    x, w, b, labels, teacher = inputs(torch, kind, n, D, C, 3, seed=3, scale=9.0)
+    t = dtype_of(torch, kind)
+    rows = 2.0 ** -(torch.arange(n, device="cuda") % 7 * 12).float()
+    x = (x.float() * rows[:, None]).to(t)
+    x[5], x[6, 1:] = 0, 0
+    w = (w.float() * 2.0 ** -(torch.arange(C, device="cuda") % 5 * 10).float()[:, None]).to(t)
+    w[7] = 0
+    check_large(torch, B, kind, (x, w, b, labels, teacher), t=2.0, far=True)
+    tiny = (x.float() * 2.0 ** -60).to(t)
+    check_large(torch, B, kind, (tiny, w, b, labels, teacher), t=2.0, far=True)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_scales(torch, B, kind):
+    """The gradients' factors, small and large: powers of two change nothing else."""
+    data = inputs(torch, kind, 400, 512, 9_900, 2, seed=8)
+    want = run(torch, B, kind, *data, 2.0, 0.25, 0.5)
+    for e in (-60, -20, 20, 40):
+        got = run(torch, B, kind, *data, 2.0, 0.25 * 2.0 ** e, 0.5 * 2.0 ** e)
+        assert all(torch.equal(got[i].float() * 2.0 ** -e, want[i].float()) for i in ("dx", "dweight", "dbias")), e
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_rows_without_a_gradient_and_classes_taken_out(torch, B, kind):
+    n, D, C = 600, 352, 9_600
+    x, w, b, labels, _ = inputs(torch, kind, n, D, C, 0, seed=5)
+    out = torch.zeros(C, dtype=torch.bool, device="cuda")
+    out[:400], out[8_000:] = True, True
+    b[out] = -float("inf")
+    labels[:] = torch.randint(400, 8_000, (n,), device="cuda", dtype=torch.int32)
+    off = torch.zeros(n, dtype=torch.bool, device="cuda")
+    off[::7], off[128:256] = True, True
+    labels[off] = -1
+    got = check_large(torch, B, kind, (x, w, b, labels, None), s=1.0 / n)
+    assert (got["dweight"][out] == 0).all() and (got["dbias"][out] == 0).all() and (got["dx"][off] == 0).all()
+    clean = run(torch, B, kind, x, w, b, labels, None, s=1.0)
+    x2 = x.clone()
+    x2[off] = float("nan")
+    x2[0], x2[7, 3], x2[14] = float("inf"), -float("inf"), torch.finfo(x.dtype).max
+    got = run(torch, B, kind, x2, w, b, labels, None, s=1.0)
+    for name in ("loss", "dx", "dweight", "dbias"):
+        assert torch.equal(got[name], clean[name]), name
+    # one that has a label spoils itself, and no other row's loss and dx
+    x2[5, 3] = float("inf")
+    got = run(torch, B, kind, x2, w, b, labels, None, s=1.0)
+    keep = [i for i in range(n) if i != 5]
+    assert not got["loss"][5].isfinite() and got["dx"][5].isnan().all()
+    assert torch.equal(got["loss"][keep], clean["loss"][keep]) and torch.equal(got["dx"][keep], clean["dx"][keep])
+
+
+def test_no_row_has_a_label(torch, B):
+    for kind in ("f32", "bf16"):
+        x, w, b, labels, teacher = inputs(torch, kind, 900, 300, 8_000, 3, seed=6)
+        labels.fill_(-1)
+        teacher[0].fill_(8_000)
+        x[:] = float("nan")
+        got = run(torch, B, kind, x, w, b, labels, teacher, 2.0, 1.0, 1.0)
+        assert all((got[k] == 0).all() for k in ("loss", "teacher_loss", "dx", "dweight", "dbias"))
+
+
+def test_one_object_for_large_and_small_calls(torch, B):
+    for kind, D, C in (("f32", 130, 5_100), ("bf16", 200, 17_000)):
+        head = B.ClassLoss(9_000, D, C, dtype_of(torch, kind), top=2, temperature=2.0)
+        for n in (9_000, 1, 4_095, 100, 600, 0, 8_191):
+            data = inputs(torch, kind, n, D, C, 2, seed=n)
+            got, want = (run(torch, B, kind, *data, 2.0, 0.1, 0.1, head=h) for h in (head, None))
+            assert all(torch.equal(got[i], want[i]) for i in got), n
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_two_graphs_and_eager_calls(torch, B, kind):
+    """Two captured calls of one object, replayed in turn between eager ones of another."""
+    n, D, C = 600, 384, 9_300
+    make = lambda seed: inputs(torch, kind, n, D, C, 4, seed=seed)      # noqa: E731
+    head = B.ClassLoss(n, D, C, dtype_of(torch, kind), top=4, temperature=2.0)
+    calls = []
+    for seed in (1, 2):
+        x, w, b, labels, teacher = data = make(seed)
+        out = {k: torch.full_like(v, 7.0) for k, v in run(torch, B, kind, *data, 2.0, 0.4, 0.6).items()}
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            head.forward(x, w, bias=b, labels=labels, teacher=teacher, loss=out["loss"], teacher_loss=out["teacher_loss"], saved=out["saved"])
+            head.backward(x, w, out["saved"], bias=b, labels=labels, teacher=teacher, scale=0.4, teacher_scale=0.6, dx=out["dx"], dweight=out["dweight"], dbias=out["dbias"])
+        calls.append((data, out, graph))
+    for seed in (11, 12, 13):
+        for i, (data, out, graph) in enumerate(calls):
+            nx, nw, nb, nl, nt = make(seed + 20 * i)
+            for t, v in zip((*data[:4], *data[4]), (nx, nw, nb, nl, *nt)):
+                t.copy_(v)
+            for t in out.values():
+                t.fill_(float("nan"))
+            graph.replay()
+            want = run(torch, B, kind, *data, 2.0, 0.4, 0.6)
+            torch.cuda.synchronize()
+            assert all(torch.equal(out[k], want[k]) for k in out), (seed, i)
