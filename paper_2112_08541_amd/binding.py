@@ -594,6 +594,16 @@ def _weights(name: str, t: Optional[torch.Tensor], shape, dtype):
     return _dev_ptr(t, dtype)
 
 
+def _on_device(owner, *tensors) -> None:
+    """The owner's memory, the current device and the tensors are of one device: a launch on another one's memory could fault."""
+    device = owner._device
+    if torch._C._cuda_getDevice() != device:
+        raise ValueError(f"made on device {device}, called with {torch._C._cuda_getDevice()} the current one")
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"expected tensors of device {device}, got one of {t.device}")
+
+
 def _refuse_gradients(who: str, *tensors) -> None:
     """Torch's own differentiation does not see the library's calls."""
     if torch.is_grad_enabled():
@@ -765,7 +775,7 @@ class LayerNorm:
         self.struct = LayerNormStruct(DTYPES[dtype], self.width, self.eps)
         self._ref = C.byref(self.struct)
         self._bytes()       # (checks the arguments)
-        self.workspace = None
+        self.workspace, self._device = None, torch.cuda.current_device()
 
     def _bytes(self) -> int:
         nbytes = C.c_size_t(0)
@@ -777,6 +787,7 @@ class LayerNorm:
         refused as by Linear.forward."""
         n = int(x.shape[0])
         _refuse_gradients("the norm", x, weight, bias)
+        _on_device(self, x, y, weight, bias, saved)
         if n > self.max_rows:
             raise ValueError(f"{n} rows, the norm was made for {self.max_rows}")
         _check(lib().bgl_layer_norm_forward(
@@ -787,6 +798,7 @@ class LayerNorm:
     def backward(self, dy, x, saved, weight=None, dx=None, dweight=None, dbias=None, stream=None) -> None:
         """Writes the gradients that are given memory: dx (which may be dy), dweight, dbias."""
         n = int(dy.shape[0])
+        _on_device(self, dy, x, saved, weight, dx, dweight, dbias)
         if n > self.max_rows:
             raise ValueError(f"{n} rows, the norm was made for {self.max_rows}")
         if self.workspace is None:
@@ -820,18 +832,19 @@ class ClassLoss:
         forward, backward = C.c_size_t(0), C.c_size_t(0)
         _check(lib().bgl_class_loss_workspace_bytes(self._ref, self.max_rows, C.byref(forward), C.byref(backward)))
         self.workspace, self.backward_workspace, self._backward_bytes = _workspace(int(forward.value)), None, int(backward.value)
-        self._made = torch.cuda.current_stream()
+        self._made, self._device = torch.cuda.current_stream(), torch.cuda.current_device()
 
     @property
     def saved_width(self) -> int:
         """Floats for each row that the backward call needs of the forward one."""
         return 2 + self.top
 
-    def _inputs(self, x, weight, bias, labels, teacher):
+    def _inputs(self, x, weight, bias, labels, teacher, *outputs):
         n = int(x.shape[0])
         if n > self.max_rows:
             raise ValueError(f"{n} rows, the loss was made for {self.max_rows}")
         classes, scores = (None, None) if teacher is None else teacher
+        _on_device(self, x, weight, bias, labels, classes, scores, *outputs)
         return n, (*_matrix("x", x, n, self.in_dim, self.dtype), _weights("weight", weight, (self.classes, self.in_dim), self.dtype),
                    _weights("bias", bias, (self.classes,), self.dtype), _weights("labels", labels, (n,), torch.int32),
                    _weights("teacher's classes", classes, (n, self.top), torch.int32), _weights("teacher's scores", scores, (n, self.top), torch.float32))
@@ -840,7 +853,7 @@ class ClassLoss:
         """Writes what is given of loss and teacher_loss, (n,) floats each, and saved = (n, saved_width) floats (the backward call needs them).
         Tensors that require gradients are refused as by Linear.forward."""
         _refuse_gradients("the loss", x, weight, bias, None if teacher is None else teacher[1])
-        n, inputs = self._inputs(x, weight, bias, labels, teacher)
+        n, inputs = self._inputs(x, weight, bias, labels, teacher, loss, teacher_loss, saved)
         if self._made is not None:
             _first_call(self, stream)
         _check(lib().bgl_class_loss_forward(
@@ -850,7 +863,7 @@ class ClassLoss:
     def backward(self, x, weight, saved, bias=None, labels=None, teacher=None, scale: float = 1.0, teacher_scale: float = 1.0,
                  dx=None, dweight=None, dbias=None, stream=None) -> None:
         """Writes the gradients of scale * loss.sum() + teacher_scale * teacher_loss.sum() that are given memory: dx, dweight, dbias (with dweight)."""
-        n, inputs = self._inputs(x, weight, bias, labels, teacher)
+        n, inputs = self._inputs(x, weight, bias, labels, teacher, saved, dx, dweight, dbias)
         if self.backward_workspace is None:
             self.backward_workspace = _workspace(self._backward_bytes)
             if stream is not None:      # (the memory may have been another tensor's on the current stream)

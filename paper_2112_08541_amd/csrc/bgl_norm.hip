@@ -33,9 +33,9 @@ struct NormArgs {
 };
 
 // A team's threads hold chunks t, t + TEAM, t + 2 TEAM, ... of 16 bytes each.
-template <class T, int TEAM>
+template <class T, int TEAM, int VALUES = kValues>
 struct Piece {
-    static constexpr int CHUNKS = kValues / T::VEC;
+    static constexpr int CHUNKS = VALUES / T::VEC;
     int first;  // the thread's first value
     int width;
     __device__ __forceinline__ Piece(int t, int w) : first(t * T::VEC), width(w) {}
@@ -49,7 +49,7 @@ struct Piece {
             if (left(c) > 0) raw[c] = whole ? load_any<uint4>(row + first + c * TEAM * T::VEC) : load_end<T>(row + first + c * TEAM * T::VEC, left(c), width);
         }
     }
-    static __device__ __forceinline__ void values(const uint4 (&raw)[CHUNKS], float (&v)[kValues])
+    static __device__ __forceinline__ void values(const uint4 (&raw)[CHUNKS], float (&v)[VALUES])
     {
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
@@ -61,7 +61,7 @@ struct Piece {
             }
         }
     }
-    __device__ __forceinline__ void load(const typename T::elem *row, float (&v)[kValues]) const
+    __device__ __forceinline__ void load(const typename T::elem *row, float (&v)[VALUES]) const
     {
         uint4 raw[CHUNKS];
         read(row, raw);
@@ -69,7 +69,7 @@ struct Piece {
     }
     // f(i): does value i exist
     __device__ __forceinline__ bool has(int i) const { return i % T::VEC < left(i / T::VEC); }
-    __device__ __forceinline__ void store(typename T::elem *row, const float (&v)[kValues]) const
+    __device__ __forceinline__ void store(typename T::elem *row, const float (&v)[VALUES]) const
     {
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
@@ -180,26 +180,26 @@ __global__ void __launch_bounds__(norm_threads<TEAM>()) k_norm_forward(NormArgs<
 }
 
 // SUMS: the weight's gradients are asked for; a thread then keeps those of its 16 columns over the rows of its team, the workgroup adds up its teams' and
-// leaves a row of partial sums.
-template <class T, int TEAM, bool SUMS>
+// leaves a row of partial sums.  The widest rows are then 512 threads of 32 values: 1,024 of 16 have 128 registers each, which these sums exceed.
+template <class T, int TEAM, bool SUMS, int VALUES = kValues>
 __global__ void __launch_bounds__(norm_threads<TEAM>()) k_norm_backward(NormArgs<T> a)
 {
     constexpr int TEAMS = norm_threads<TEAM>() / TEAM;
     __shared__ float lds[TEAM > 64 ? norm_threads<TEAM>() / 64 * 4 : 1];
-    __shared__ float sums[SUMS && TEAMS > 1 ? TEAMS * TEAM * kValues : 1];
+    __shared__ float sums[SUMS && TEAMS > 1 ? TEAMS * TEAM * VALUES : 1];
     int turn = 0;
-    const Piece<T, TEAM> p(threadIdx.x % TEAM, a.width);
+    const Piece<T, TEAM, VALUES> p(threadIdx.x % TEAM, a.width);
     const float share = 1.0f / (float)a.width;
-    float g[kValues], dg[kValues], db[kValues];
+    float g[VALUES], dg[VALUES], db[VALUES];
 #pragma unroll
-    for (int i = 0; i < kValues; ++i) g[i] = 1.0f, dg[i] = db[i] = 0.0f;
+    for (int i = 0; i < VALUES; ++i) g[i] = 1.0f, dg[i] = db[i] = 0.0f;
     if (a.weight) p.load(a.weight, g);
     const int64_t step = (int64_t)gridDim.x * TEAMS;
     // (all teams of a workgroup go round equally often: they share barriers)
     for (int64_t first = (int64_t)blockIdx.x * TEAMS; first < a.n; first += step) {
         const int64_t row = first + threadIdx.x / TEAM;
         const bool live = row < a.n;
-        float dy[kValues], h[kValues];
+        float dy[VALUES], h[VALUES];
         float c1 = 0.0f, c2 = 0.0f, r = 0.0f;
         if (live) {
             p.load(a.dy + row * a.dy_stride, dy);
@@ -207,8 +207,8 @@ __global__ void __launch_bounds__(norm_threads<TEAM>()) k_norm_backward(NormArgs
             const float mean = a.saved[2 * row];
             r = a.saved[2 * row + 1];
 #pragma unroll
-            for (int i = 0; i < kValues; ++i) {
-                h[i] = p.has(i) ? (h[i] - mean) * r : 0.0f;
+            for (int i = 0; i < VALUES; ++i) {
+                h[i] = (h[i] - mean) * r;  // (behind the row any number: dy is 0 there)
                 if constexpr (SUMS) dg[i] = fmaf(dy[i], h[i], dg[i]), db[i] += dy[i];
                 dy[i] *= g[i];
                 c1 += dy[i];
@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(norm_threads<TEAM>()) k_norm_backward(NormArgs
         if (live) {
             c1 *= share, c2 *= share;
 #pragma unroll
-            for (int i = 0; i < kValues; ++i) dy[i] = r * (dy[i] - fmaf(h[i], c2, c1));
+            for (int i = 0; i < VALUES; ++i) dy[i] = r * (dy[i] - fmaf(h[i], c2, c1));
             p.store(a.out + row * a.out_stride, dy);
         }
     }
@@ -232,18 +232,18 @@ __global__ void __launch_bounds__(norm_threads<TEAM>()) k_norm_backward(NormArgs
             if constexpr (TEAMS > 1) {
                 __syncthreads();
 #pragma unroll
-                for (int i = 0; i < kValues; ++i) sums[(team * kValues + i) * TEAM + threadIdx.x % TEAM] = which ? db[i] : dg[i];
+                for (int i = 0; i < VALUES; ++i) sums[(team * VALUES + i) * TEAM + threadIdx.x % TEAM] = which ? db[i] : dg[i];
                 __syncthreads();
-                for (int j = threadIdx.x; j < TEAM * kValues; j += norm_threads<TEAM>()) {
+                for (int j = threadIdx.x; j < TEAM * VALUES; j += norm_threads<TEAM>()) {
                     float s = 0.0f;
 #pragma unroll
-                    for (int t = 0; t < TEAMS; ++t) s += sums[t * kValues * TEAM + j];
+                    for (int t = 0; t < TEAMS; ++t) s += sums[t * VALUES * TEAM + j];
                     const int i = j / TEAM, at = (j % TEAM + i / T::VEC * TEAM) * T::VEC + i % T::VEC;
                     if (at < a.width) to[at] = s;
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < kValues; ++i)
+                for (int i = 0; i < VALUES; ++i)
                     if (p.has(i)) to[p.first + i / T::VEC * TEAM * T::VEC + i % T::VEC] = which ? db[i] : dg[i];
             }
         }
@@ -334,7 +334,8 @@ int backward(NormArgs<T> a, hipStream_t st)
     if (a.n > 0 && (sums || a.out)) {
         with_team(team_of(a.width), [&](auto team) {
             constexpr int TEAM = decltype(team)::value;
-            if (sums) k_norm_backward<T, TEAM, true><<<dim3((unsigned)a.parts), dim3(norm_threads<TEAM>()), 0, st>>>(a);
+            constexpr int LEAST = TEAM < 512 ? TEAM : 512;
+            if (sums) k_norm_backward<T, LEAST, true, kValues * TEAM / LEAST><<<dim3((unsigned)a.parts), dim3(norm_threads<LEAST>()), 0, st>>>(a);
             else k_norm_backward<T, TEAM, false><<<dim3((unsigned)ceil_div(a.n < kMostThreads / TEAM ? a.n : kMostThreads / TEAM, teams_of(TEAM))), dim3(norm_threads<TEAM>()), 0, st>>>(a);
         });
         BGL_HIP(hipGetLastError());

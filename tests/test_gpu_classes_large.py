@@ -171,3 +171,69 @@ def test_two_graphs_and_eager_calls(torch, B, kind):
             want = run(torch, B, kind, *data, 2.0, 0.4, 0.6)
             torch.cuda.synchronize()
             assert all(torch.equal(out[k], want[k]) for k in out), (seed, i)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [3, 128])
+def test_a_weight_beyond_32_bits(torch, B, kind, n):
+    """Classes from 2^31 values of the weight on; all others are taken out, so that the call of these alone is the same one."""
+    D, C, far = 260, 2_000, 8_300_000
+    x, w, b, labels, teacher = inputs(torch, kind, n, D, C, 3, seed=9)
+    small = run(torch, B, kind, x, w, b, labels, teacher, 2.0, 0.5, 0.5)
+    ref = Reference(torch, torch.cat([x, x.new_zeros((n, 12))], 1), torch.cat([w, w.new_zeros((C, 12))], 1), b, labels, teacher, 2.0, V[kind])
+    assert far * D > 2 ** 31
+    ref.sum += far / 1000 * 2.0 ** -24      # (more parts of a sum, those of the others 0)
+    w_all, b_all = torch.zeros((far + C, D), dtype=w.dtype, device="cuda"), torch.full((far + C,), -float("inf"), dtype=b.dtype, device="cuda")
+    w_all[far:], b_all[far:] = w, b
+    place = lambda c: torch.where((c >= 0) & (c < C), c + far, -1).int()      # noqa: E731
+    got = run(torch, B, kind, x, w_all, b_all, place(labels), (place(teacher[0]), teacher[1]), 2.0, 0.5, 0.5)
+    more = far / 1000 * 2.0 ** -24
+    check("loss", got["loss"], ref.loss, ref.loss_bound + more)
+    check("teacher_loss", got["teacher_loss"], ref.teacher_loss, ref.teacher_bound + 4 * more)
+    assert (got["dweight"][:far] == 0).all() and (got["dbias"][:far] == 0).all()
+    # both calls' gradients are within the bound of the value, with q off by what the sum is
+    for name, value, (want, bound) in zip(("dx", "dweight", "dbias"), (got["dx"], got["dweight"][far:], got["dbias"][far:]), ref.gradients(0.5, 0.5)):
+        want, bound = (want, bound) if name == "dbias" else (want[:, :D], bound[:, :D])
+        check(name, small[name], want, bound)
+        size = {"dx": w.double().abs().sum(0), "dweight": x.double().abs().sum(0), "dbias": n}[name]
+        check(name, value, want, bound + 2 * more * size)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("C", [7, 150])
+def test_rows_beyond_32_bits(torch, B, kind, C):
+    """The same rows 2,100 times: the same losses and dx each time; labels in the last ones alone: their dweight."""
+    n, D, times = 8_192, 130, 2_100
+    x, w, b, labels, _ = inputs(torch, kind, n, D, C, 0, seed=10)
+    head = B.ClassLoss(n * times, D, C, dtype_of(torch, kind))
+    all_x, saved = x.repeat(times, 1), torch.full((n * times, 2), 7.0, device="cuda")
+    assert all_x.numel() > 2 ** 31
+    loss, dx = torch.full((n * times,), 7.0, device="cuda"), torch.full_like(all_x, 7.0)
+    head.forward(all_x, w, bias=b, labels=labels.repeat(times), loss=loss, saved=saved)
+    head.backward(all_x, w, saved, bias=b, labels=labels.repeat(times), dx=dx)
+    ref = Reference(torch, torch.cat([x, x.new_zeros((n, 12))], 1), torch.cat([w, w.new_zeros((C, 12))], 1), b, labels, None, 1.0, V[kind])
+    check("loss", loss[-n:], ref.loss, ref.loss_bound)
+    (want_dx, dx_bound), (want_dw, dw_bound), (want_db, db_bound) = ref.gradients(1.0, 0.0)
+    check("dx", dx[-n:], want_dx[:, :D], dx_bound[:, :D])
+    assert (loss.view(times, n) == loss[-n:]).all()
+    for part in dx.view(times, n, D).split(100):
+        assert (part == dx[-n:]).all()
+    some = torch.full((n * times,), -1, dtype=torch.int32, device="cuda")
+    some[-n:] = labels
+    dw, db = torch.full_like(w, 7.0), torch.full_like(b, 7.0)
+    head.backward(all_x, w, saved, bias=b, labels=some, dweight=dw, dbias=db)
+    check("dweight", dw, want_dw[:, :D], dw_bound[:, :D])
+    check("dbias", db, want_db, db_bound)
+
+
+def test_another_device_is_refused(torch, B):
+    """An object made on another device than the current one, as far as one device can show it."""
+    x, w, labels = torch.zeros((4, 8), device="cuda"), torch.zeros((5, 8), device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    for make, call in ((lambda: B.ClassLoss(4, 8, 5), lambda o: o.forward(x, w, labels=labels)), (lambda: B.ClassLoss(4, 8, 5), lambda o: o.backward(x, w, torch.zeros((4, 2), device="cuda"), labels=labels, dx=x)),
+                       (lambda: B.LayerNorm(4, 8), lambda o: o.forward(x, x)), (lambda: B.LayerNorm(4, 8), lambda o: o.backward(x, x, torch.zeros((4, 2), device="cuda"), dx=x))):
+        o = make()
+        o._device += 1
+        with pytest.raises(ValueError, match="device"):
+            call(o)
+    with pytest.raises(ValueError, match="device"):
+        B.LayerNorm(4, 8).forward(x, x.cpu())
