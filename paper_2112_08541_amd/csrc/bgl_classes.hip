@@ -457,26 +457,48 @@ __global__ void __launch_bounds__(256) k_class_finish(RowArgs<T> a)
     if (l == 0 && a.saved) a.saved[row * a.saved_width] = base + log_sum, a.saved[row * a.saved_width + 1] = lse_t;
 }
 
-// dz where the teacher names a class: a wavefront for each row.  A class named twice has the sum of its shares, written by both.
-template <class T>
+// dz where the teacher names a class: LANES neighbours for each row, workgroups of them for each 64 classes.  A class named twice has the sum of its shares, written by both.
+template <class T, int LANES>
 __global__ void __launch_bounds__(256) k_class_fix(RowArgs<T> a)
 {
-    const int64_t r = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+    constexpr int AHEAD = 8;
+    const int64_t r = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
     if (r >= a.rows) return;
     const int64_t row = a.row0 + r;
-    const int l = threadIdx.x & 63;
+    const int l = threadIdx.x % LANES;
     float most, total;
-    if (!teacher_of<64>(a, row, most, total)) return;
+    if (!teacher_of<LANES>(a, row, most, total)) return;
     const float *kept = a.saved + row * a.saved_width;
     const float lse = kept[0], lse_t = kept[1];
     int label = a.labels ? a.labels[row] : -1;
     if ((uint32_t)label >= (uint32_t)a.classes) label = -1;
-    for (int k = l; k < a.top; k += 64) {
-        const int c = a.top_class[row * a.top + k];
-        if (c < a.class0 || c >= a.class0 + a.piece_classes) continue;
+    const int32_t *classes = a.top_class + row * a.top;
+    const auto share = [&](int k) { return exp_of(a.top_score[row * a.top + k] * a.over_t - most) / total; };
+    for (int k = (int)blockIdx.y * LANES + l; k - l < a.top; k += (int)gridDim.y * LANES) {
+        const int c = k < a.top ? classes[k] : -1;
+        const bool here = c >= a.class0 && c < a.class0 + a.piece_classes;
         float p = 0.0f;
-        for (int o = 0; o < a.top; ++o)
-            if (a.top_class[row * a.top + o] == c) p += exp_of(a.top_score[row * a.top + o] * a.over_t - most) / total;
+        if constexpr (LANES == 64) {
+            // (read by every lane from memory, 200 classes of 200 rows took 100 us)
+            for (int o = 0; o < a.top; o += 64) {
+                const int other = o + l < a.top ? classes[o + l] : -2;
+                const float its = (uint32_t)other < (uint32_t)a.classes ? share(o + l) : 0.0f;
+#pragma unroll 16
+                for (int j = 0; j < 64; ++j) {
+                    const float add = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(its), j));
+                    if (__builtin_amdgcn_readlane(other, j) == c) p += add;
+                }
+            }
+        }
+        if (!here) continue;
+        for (int o = 0; LANES < 64 && o < a.top; o += AHEAD) {
+            int other[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) other[u] = o + u < a.top ? classes[o + u] : -1;
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+                if (other[u] == c) p += share(o + u);
+        }
         const float z = kept[2 + k];
         float d = 0.0f;
         if (label >= 0 && a.scale != 0.0f) d = a.scale * (power_to(z, a.k, lse) - (c == label ? 1.0f : 0.0f));
@@ -1645,7 +1667,12 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
                 s.listed = cp == 0 && dweight ? listed + row0 : nullptr;
                 launch_scores<T, true>(s, c.stream);
             }
-            if (r.teacher_scale != 0.0f) k_class_fix<T><<<dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, c.stream>>>(r);
+            if (r.teacher_scale != 0.0f) {
+                // (20,000 rows of 8 classes, f32: backward 191 us with wavefronts, 175 with 8 lanes; a few rows leave the GPU to wavefronts)
+                if (rows < 4 * kCus || r.top > 32) k_class_fix<T, 64><<<dim3((unsigned)ceil_div(rows, 4), (unsigned)ceil_div(r.top, 64)), dim3(256), 0, c.stream>>>(r);
+                else if (r.top <= 8) k_class_fix<T, 8><<<dim3((unsigned)ceil_div(rows, 32)), dim3(256), 0, c.stream>>>(r);
+                else k_class_fix<T, 16><<<dim3((unsigned)ceil_div(rows, 16)), dim3(256), 0, c.stream>>>(r);
+            }
             float *slots = p.dx_bytes ? dx_slots + (p.class_pieces > 1 ? row0 * p.slot_width : 0) : nullptr;
             const int64_t slot_rows = round_up(p.class_pieces > 1 ? c.n : rows, h.slot_round);
             const auto fill_dx = [&](auto &a) {
