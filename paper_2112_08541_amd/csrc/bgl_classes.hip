@@ -961,7 +961,12 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
         float bias[C::BA], lse[C::BB], lse_t[C::BB];
         int label[C::BB], classes[C::BA], rows[C::BB];
     };
+    struct Meet {
+        float own[C::BB], part[2][2][C::BB];  // the label's score; largest value and sum of both halves of the classes
+    };
+    static_assert(sizeof(Own) + sizeof(Meet) <= sizeof(lds), "");
     Own &own = *reinterpret_cast<Own *>(lds);
+    Meet &meet = *reinterpret_cast<Meet *>(lds + sizeof(Own));
     if (threadIdx.x < C::BA) own.bias[threadIdx.x] = my_bias, own.classes[threadIdx.x] = my_class;
     if (threadIdx.x < C::BB) {
         own.rows[threadIdx.x] = my_row;
@@ -1030,12 +1035,16 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
             }
             if (any) {
                 const float v = own_score(t);
-                if (mine && r < a.rows) a.label_score[a.row0 + r] = v;
+                if (mine && a.whole) meet.own[b] = v;
+                else if (mine && r < a.rows) a.label_score[a.row0 + r] = v;
             }
             sum = down_column(sum, [](float p, float q) { return p + q; });
             if (a.two) sum_t = down_column(sum_t, [](float p, float q) { return p + q; });
-            if (l < 16 && r < a.rows) {
-                const int64_t at = (ct * 2 + C::a_off() / (16 * C::FA)) * a.rows + r;
+            const int half = C::a_off() / (16 * C::FA);
+            if (a.whole) {
+                if (l < 16) meet.part[0][half][b] = most, meet.part[1][half][b] = sum;
+            } else if (l < 16 && r < a.rows) {
+                const int64_t at = (ct * 2 + half) * a.rows + r;
                 a.part[at] = float2{most, sum};
                 if (a.two) a.part_t[at] = sum_t;
             }
@@ -1074,6 +1083,21 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
                 }
             }
         }
+    }
+    if constexpr (!DZ) {
+        // (204,800 x 256 x 150 bf16: 46 us with a launch of k_class_finish)
+        if (!a.whole) return;
+        __syncthreads();
+        const int b = threadIdx.x;
+        if (b >= C::BB || r0 + b >= a.rows) return;
+        const int64_t row = a.row0 + r0 + b;
+        const float most = fmaxf(meet.part[0][0][b], meet.part[0][1][b]), base = base_of(most, a.k);
+        float sum = 0.0f;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) sum += meet.part[1][half][b] * rebase(base_of(meet.part[0][half][b], a.k), base);
+        const float log_sum = log2f(sum);
+        if (a.loss) a.loss[row] = my_label >= 0 ? loss_of(log_sum, meet.own[b], a.k, base) : 0.0f;
+        if (a.kept) a.kept[row * a.saved_width] = base + log_sum, a.kept[row * a.saved_width + 1] = INFINITY;
     }
 }
 
@@ -1546,7 +1570,7 @@ int forward(const Call &c, float *loss, float *teacher_loss, float *saved)
     if (h.large) q = stage_args(c, p, s, x, w, nullptr);
     for (int64_t row0 = 0; row0 < c.n; row0 += p.pass_rows) {
         s.row0 = r.row0 = row0, s.rows = r.rows = c.n - row0 < p.pass_rows ? c.n - row0 : p.pass_rows;
-        s.loss = loss, s.kept = saved, s.whole = !h.large && !c.top_class && c.l->classes <= Large::BA;
+        s.loss = loss, s.kept = saved, s.whole = !c.top_class && c.l->classes <= (h.large ? StageCut::BA : Large::BA);
         if (h.large) q.s = s, launch_scores_stage<T, false>(q, c.stream);
         else launch_scores<T, false>(s, c.stream);
         if (s.whole) continue;  // (every tile has all classes)
