@@ -27,6 +27,7 @@ constexpr int64_t kPieceRows = 16384;
 constexpr int64_t kPieceClasses = 256;                 // pieces of some classes only are multiples
 constexpr int64_t kPartialBytes = (int64_t)64 << 20;   // of a forward call's tiles' maxima and sums
 constexpr int kCus = 256;
+constexpr int kStoredBeside = 512;                     // bytes of classes' rows that storing a tile's row in LDS takes as long as
 constexpr int64_t kMostThreads = (int64_t)1 << 31;     // of a launch, which has room for 2^32 - 1
 constexpr double kLargeProducts = 2e9;                 // of a call that is laid out for large tiles: 512 x 256 x 4,096 f32 took 30 + 110 us so and 19 + 58 in small ones,
                                                        // 1,316 x 503 x 3,640 45 + 167 and 77 + 199; bf16 15 + 42 and 11 + 40, 29 + 66 and 24 + 83
@@ -914,6 +915,10 @@ struct StageScoreArgs {
     // what the products of the backward call read (bf16: the same; fp32: three planes of bf16)
     const char *x_back, *w_back;
     int64_t x_back_bytes, w_back_bytes;
+    // forward, or null: the teacher's classes, n x top, whose scores go to z_top
+    const int32_t *top_class;
+    float *z_top;
+    int top, z_stride;
 };
 
 template <class T, bool DZ>
@@ -1000,6 +1005,43 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
 #pragma unroll
                     for (int t = 0; t < C::FB; ++t) acc[i][t][j] = -INFINITY;
                 }
+    }
+    if constexpr (!DZ) {
+        if (q.top_class) {
+            // scores of the teacher's classes: 64 rows of the tile at a time in LDS, four threads for a row (50,000 x 256 x 1,001 bf16 with 16 classes and labels: 81 us; 92
+            // with k_class_top, which reads their weights once more.  4,096 x 512 x 10,003 with 32: 79 and 80; x 40,003: 250 and 228)
+            constexpr int WIDE = C::BA + 4, ROWS = C::BB / 2, EACH = stage::kThreads / ROWS, AHEAD = 4;
+            static_assert(C::FB == 4 && sizeof(Own) + sizeof(Meet) + ROWS * WIDE * 4 <= sizeof(lds), "");
+            float *z = reinterpret_cast<float *>(lds + sizeof(Own) + sizeof(Meet));
+            const int at = threadIdx.x / EACH;
+#pragma unroll
+            for (int pass = 0; pass < 2; ++pass) {
+                const int64_t r = r0 + at / 32 * 64 + pass * 32 + at % 32, row = a.row0 + r;
+                const int k0 = threadIdx.x % EACH, mine = r < a.rows ? q.top : 0;
+                const int32_t *classes = q.top_class + row * q.top;
+                int c[AHEAD];
+                const auto ask = [&](int k) {
+#pragma unroll
+                    for (int u = 0; u < AHEAD; ++u) c[u] = k + u * EACH < mine ? classes[k + u * EACH] : 0;
+                };
+                ask(k0);
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int i = 0; i < C::FA; ++i)
+                        *reinterpret_cast<f32x4 *>(z + (C::b_off() / 2 + 16 * u + (l & 15)) * WIDE + in_tile + 16 * i) = acc[i][2 * pass + u];
+                __syncthreads();
+                for (int k = k0; k < mine; k += AHEAD * EACH) {
+#pragma unroll
+                    for (int u = 0; u < AHEAD; ++u) {
+                        const bool there = (uint32_t)c[u] < (uint32_t)a.all_classes;
+                        if (k + u * EACH < mine && (there ? (uint32_t)(c[u] - c0) < (uint32_t)C::BA : ct == 0)) q.z_top[row * q.z_stride + k + u * EACH] = there ? z[at * WIDE + c[u] - c0] : 0.0f;
+                    }
+                    ask(k + AHEAD * EACH);
+                }
+                __syncthreads();
+            }
+        }
     }
     const bool teachers = DZ && a.teacher_scale != 0.0f, labels = a.labels != nullptr && (!DZ || a.scale != 0.0f);
 #pragma unroll
@@ -1567,14 +1609,20 @@ int forward(const Call &c, float *loss, float *teacher_loss, float *saved)
     r.loss = loss, r.teacher_loss = teacher_loss, r.saved = saved;
     if (!c.labels) s.k = r.k = s.k_t, s.two = r.two = false;  // (no sums but those at the temperature are asked for)
     StageScoreArgs<T> q{};
-    if (h.large) q = stage_args(c, p, s, x, w, nullptr);
+    if (h.large) {
+        q = stage_args(c, p, s, x, w, nullptr);
+        // (what the tiles would read of the teacher's classes and store, beside the classes' rows)
+        const int64_t tiles = ceil_div(c.l->classes, StageCut::BA);
+        if (c.top_class && tiles * (4 * r.top + kStoredBeside) < (int64_t)r.top * c.l->in_dim * (int64_t)sizeof(typename T::elem))
+            q.top_class = c.top_class, q.top = r.top, q.z_top = r.z_top, q.z_stride = r.z_stride;
+    }
     for (int64_t row0 = 0; row0 < c.n; row0 += p.pass_rows) {
         s.row0 = r.row0 = row0, s.rows = r.rows = c.n - row0 < p.pass_rows ? c.n - row0 : p.pass_rows;
         s.loss = loss, s.kept = saved, s.whole = !c.top_class && c.l->classes <= (h.large ? StageCut::BA : Large::BA);
         if (h.large) q.s = s, launch_scores_stage<T, false>(q, c.stream);
         else launch_scores<T, false>(s, c.stream);
         if (s.whole) continue;  // (every tile has all classes)
-        if (c.top_class) k_class_top<T><<<dim3((unsigned)ceil_div(r.rows * ((r.top + 3) / 4), 32)), dim3(256), 0, c.stream>>>(r);
+        if (c.top_class && !q.top_class) k_class_top<T><<<dim3((unsigned)ceil_div(r.rows * ((r.top + 3) / 4), 32)), dim3(256), 0, c.stream>>>(r);
         r.class_parts = p.class_parts;
         if (r.class_parts > 32 && r.rows >= 64) {
             k_class_merge<T><<<dim3((unsigned)ceil_div(r.rows, kMergeRows)), dim3(kMergeRows * kMergeLanes), 0, c.stream>>>(r, s.part, s.part_t);
