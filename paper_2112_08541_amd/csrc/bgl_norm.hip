@@ -32,17 +32,23 @@ struct NormArgs {
     float eps;
 };
 
-// A team's threads hold chunks t, t + TEAM, t + 2 TEAM, ... of 16 bytes each.  FULL: they are all there.
-template <class T, int TEAM, int VALUES = kValues, bool FULL = false>
+// A team's threads hold chunks t, t + TEAM, t + 2 TEAM, ... of 16 bytes each.  Of the row they may have FULL ones alone, WHOLE ones
+// or none, or any part.
+enum Fit { ANY, WHOLE, FULL };
+template <class T, int TEAM, int VALUES = kValues, Fit FIT = ANY>
 struct Piece {
     static constexpr int CHUNKS = VALUES / T::VEC;
     int first;  // the thread's first value
     int width;
     __device__ __forceinline__ Piece(int t, int w) : first(t * T::VEC), width(w) {}
-    __device__ __forceinline__ int left(int c) const { return FULL ? T::VEC : width - first - c * TEAM * T::VEC; }
+    __device__ __forceinline__ int left(int c) const
+    {
+        const int values = width - first - c * TEAM * T::VEC;
+        return FIT == FULL || (FIT == WHOLE && values > 0) ? T::VEC : values;
+    }
     __device__ __forceinline__ void read(const typename T::elem *row, uint4 (&raw)[CHUNKS]) const
     {
-        const bool whole = FULL || width % T::VEC == 0;
+        const bool whole = FIT != ANY || width % T::VEC == 0;
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
             raw[c] = uint4{0, 0, 0, 0};
@@ -68,7 +74,7 @@ struct Piece {
         values(raw, v);
     }
     // f(i): does value i exist
-    __device__ __forceinline__ bool has(int i) const { return i % T::VEC < left(i / T::VEC); }
+    __device__ __forceinline__ bool has(int i) const { return FIT == WHOLE ? left(i / T::VEC) > 0 : i % T::VEC < left(i / T::VEC); }
     __device__ __forceinline__ void store(typename T::elem *row, const float (&v)[VALUES]) const
     {
 #pragma unroll
@@ -79,7 +85,7 @@ struct Piece {
             typename T::elem *to = row + first + c * TEAM * T::VEC;
             if (left(c) >= T::VEC) {
                 __builtin_memcpy(to, e, 16);
-            } else {
+            } else if (FIT == ANY) {
 #pragma unroll
                 for (int i = 0; i < T::VEC; ++i)
                     if (i < left(c)) to[i] = e[i];
@@ -112,8 +118,8 @@ constexpr int norm_threads() { return TEAM < 256 ? 256 : TEAM; }
 
 // The mean, in two parts (the values' mean as fp32 has it, and the mean of what is left then, so that rows far from zero keep their spread), and r of the row
 // that the team holds.  Where squares leave fp32's range they are taken of values scaled by a power of two (the same for the whole team).
-template <class T, int TEAM, bool FULL>
-__device__ __forceinline__ void moments(const Piece<T, TEAM, kValues, FULL> &p, float (&v)[kValues], float eps, float *lds, int &turn, float &mean, float &rest, float &r)
+template <class T, int TEAM, Fit FIT>
+__device__ __forceinline__ void moments(const Piece<T, TEAM, kValues, FIT> &p, float (&v)[kValues], float eps, float *lds, int &turn, float &mean, float &rest, float &r)
 {
 #pragma clang fp contract(off)  // (v - m with the product m unrounded would not fit the m that is kept)
     const float share = 1.0f / (float)p.width;
@@ -155,13 +161,13 @@ __device__ __forceinline__ void moments(const Piece<T, TEAM, kValues, FULL> &p, 
 
 // A row's threads: 16 values each, a team of 1 to 1,024.  A workgroup has 256 threads or one team.  FULL: rows of 16 TEAM values, which need not ask of each whether it
 // is there: with 29 vector instructions for a value the bf16 rows of 512 below took XX us.
-template <class T, int TEAM, bool FULL>
+template <class T, int TEAM, Fit FIT>
 __global__ void __launch_bounds__(norm_threads<TEAM>()) k_norm_forward(NormArgs<T> a)
 {
     constexpr int TEAMS = norm_threads<TEAM>() / TEAM;
     __shared__ float lds[TEAM > 64 ? norm_threads<TEAM>() / 64 * 4 : 1];
     int turn = 0;
-    const Piece<T, TEAM, kValues, FULL> p(threadIdx.x % TEAM, a.width);
+    const Piece<T, TEAM, kValues, FIT> p(threadIdx.x % TEAM, a.width);
     const int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TEAM;
     const bool live = row < a.n;
     if (TEAM <= 64 && !live) return;
@@ -171,7 +177,7 @@ __global__ void __launch_bounds__(norm_threads<TEAM>()) k_norm_forward(NormArgs<
     for (int i = 0; i < kValues; ++i) g[i] = 1.0f, b[i] = 0.0f;
     if (a.weight) p.load(a.weight, g);
     if (a.bias) p.load(a.bias, b);
-    moments<T, TEAM, FULL>(p, v, a.eps, lds, turn, mean, rest, r);
+    moments<T, TEAM, FIT>(p, v, a.eps, lds, turn, mean, rest, r);
     if (!live) return;
 #pragma unroll
     for (int i = 0; i < kValues; ++i) {
@@ -323,8 +329,9 @@ int forward(NormArgs<T> a, hipStream_t st)
         for (int64_t row0 = 0; row0 < n; row0 += most) {
             a.n = n - row0 < most ? n - row0 : most;
             const dim3 grid((unsigned)ceil_div(a.n, teams_of(TEAM))), threads(norm_threads<TEAM>());
-            if (a.width == TEAM * kValues) k_norm_forward<T, TEAM, true><<<grid, threads, 0, st>>>(a);
-            else k_norm_forward<T, TEAM, false><<<grid, threads, 0, st>>>(a);
+            if (a.width == TEAM * kValues) k_norm_forward<T, TEAM, FULL><<<grid, threads, 0, st>>>(a);
+            else if (a.width % T::VEC == 0) k_norm_forward<T, TEAM, WHOLE><<<grid, threads, 0, st>>>(a);
+            else k_norm_forward<T, TEAM, ANY><<<grid, threads, 0, st>>>(a);
             a.x += a.n * a.x_stride, a.out += a.n * a.out_stride, a.saved = a.saved ? a.saved + 2 * a.n : nullptr;
         }
     });
