@@ -48,7 +48,7 @@ struct Piece {
     }
     __device__ __forceinline__ void read(const typename T::elem *row, uint4 (&raw)[CHUNKS]) const
     {
-        const bool whole = FIT != ANY || width % T::VEC == 0;
+        constexpr bool whole = FIT != ANY;
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
             raw[c] = uint4{0, 0, 0, 0};
@@ -190,14 +190,14 @@ __global__ void __launch_bounds__(norm_threads<TEAM>()) k_norm_forward(NormArgs<
 
 // SUMS: the weight's gradients are asked for; a thread then keeps those of its 16 columns over the rows of its team, the workgroup adds up its teams' and
 // leaves a row of partial sums.  The widest rows are then 512 threads of 32 values: 1,024 of 16 have 128 registers each, which these sums exceed.
-template <class T, int TEAM, bool SUMS, int VALUES = kValues>
+template <class T, int TEAM, bool SUMS, Fit FIT, int VALUES = kValues>
 __global__ void __launch_bounds__(norm_threads<TEAM>()) k_norm_backward(NormArgs<T> a)
 {
     constexpr int TEAMS = norm_threads<TEAM>() / TEAM;
     __shared__ float lds[TEAM > 64 ? norm_threads<TEAM>() / 64 * 4 : 1];
     __shared__ float sums[SUMS && TEAMS > 1 ? TEAMS * TEAM * VALUES : 1];
     int turn = 0;
-    const Piece<T, TEAM, VALUES> p(threadIdx.x % TEAM, a.width);
+    const Piece<T, TEAM, VALUES, FIT> p(threadIdx.x % TEAM, a.width);
     const float share = 1.0f / (float)a.width;
     float g[VALUES], dg[VALUES], db[VALUES];
 #pragma unroll
@@ -347,8 +347,13 @@ int backward(NormArgs<T> a, hipStream_t st)
         with_team(team_of(a.width), [&](auto team) {
             constexpr int TEAM = decltype(team)::value;
             constexpr int LEAST = TEAM < 512 ? TEAM : 512;
-            if (sums) k_norm_backward<T, LEAST, true, kValues * TEAM / LEAST><<<dim3((unsigned)a.parts), dim3(norm_threads<LEAST>()), 0, st>>>(a);
-            else k_norm_backward<T, TEAM, false><<<dim3((unsigned)ceil_div(a.n < kMostThreads / TEAM ? a.n : kMostThreads / TEAM, teams_of(TEAM))), dim3(norm_threads<TEAM>()), 0, st>>>(a);
+            const auto go = [&](auto fit) {
+                constexpr Fit FIT = decltype(fit)::value;
+                if (sums) k_norm_backward<T, LEAST, true, FIT, kValues * TEAM / LEAST><<<dim3((unsigned)a.parts), dim3(norm_threads<LEAST>()), 0, st>>>(a);
+                else k_norm_backward<T, TEAM, false, FIT><<<dim3((unsigned)ceil_div(a.n < kMostThreads / TEAM ? a.n : kMostThreads / TEAM, teams_of(TEAM))), dim3(norm_threads<TEAM>()), 0, st>>>(a);
+            };
+            if (a.width % T::VEC == 0) go(std::integral_constant<Fit, WHOLE>{});
+            else go(std::integral_constant<Fit, ANY>{});
         });
         BGL_HIP(hipGetLastError());
     }
