@@ -352,7 +352,8 @@ int backward(NormArgs<T> a, hipStream_t st)
                 if (sums) k_norm_backward<T, LEAST, true, FIT, kValues * TEAM / LEAST><<<dim3((unsigned)a.parts), dim3(norm_threads<LEAST>()), 0, st>>>(a);
                 else k_norm_backward<T, TEAM, false, FIT><<<dim3((unsigned)ceil_div(a.n < kMostThreads / TEAM ? a.n : kMostThreads / TEAM, teams_of(TEAM))), dim3(norm_threads<TEAM>()), 0, st>>>(a);
             };
-            if (a.width % T::VEC == 0) go(std::integral_constant<Fit, WHOLE>{});
+            if (a.width == TEAM * kValues) go(std::integral_constant<Fit, FULL>{});
+            else if (a.width % T::VEC == 0) go(std::integral_constant<Fit, WHOLE>{});
             else go(std::integral_constant<Fit, ANY>{});
         });
         BGL_HIP(hipGetLastError());
