@@ -879,7 +879,7 @@ int bgl_layer_norm_backward(const bgl_layer_norm_t *norm, int64_t n, const void 
  *   weight, bias      device, classes x in_dim, tight; classes values, or null.  A bias of -inf takes a class out; a row for which
  *                     none is left has NaN
  *   label_loss, teacher_loss  device, n floats each, or null
- *   saved             device, n x (2 + top) floats that the backward call needs, or null
+ *   saved             device, n x (3 + top) floats (n x 2 without a teacher, top = 0) that the backward call needs, or null
  *   workspace         device, 256-byte aligned, >= *forward_bytes of bgl_class_loss_workspace_bytes(loss, n, ...)
  * Sums are fp32.  Calls of many products (n >= 96, 128 classes, 2e9 products) take fp32 x and weight as two halves each, times a power of two of
  * the row: 22 bits, or 2^-40 of the row's largest value.  Outputs must not overlap inputs or each other.  n = 0 does nothing.

@@ -837,7 +837,7 @@ class ClassLoss:
     @property
     def saved_width(self) -> int:
         """Floats for each row that the backward call needs of the forward one."""
-        return 2 + self.top
+        return 3 + self.top if self.top else 2
 
     def _inputs(self, x, weight, bias, labels, teacher, *outputs):
         n = int(x.shape[0])

@@ -53,6 +53,13 @@ __device__ __forceinline__ float max3(float a, float b, float c)  // (of fmaxf t
     asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
     return r;
 }
+// What a row keeps for its gradients, from which q is as near as its power and its sum (with the sum's logarithm in 32 bits it was off by up to that much of its last place:
+// gradients of few classes were 2e-6 off, now 3e-7).  sum_t: of scores over the temperature, +inf where the teacher names no class; behind it its classes' scores.
+__device__ __forceinline__ void keep(float *to, int width, float most, float sum, float sum_t)
+{
+    to[0] = most, to[1] = sum;
+    if (width > 2) to[2] = sum_t;
+}
 // The logarithm of the sum less the score, both to the sum's base (what they have in common goes before they meet), in natural units.
 __device__ __forceinline__ float loss_of(float log_sum, float score, float k, float base) { return kLn2 * (log_sum - fmaf(score, k, -base)); }
 __device__ __forceinline__ float rebase(float from, float to) { return __builtin_amdgcn_exp2f(from - to); }
@@ -119,7 +126,7 @@ struct ScoreArgs {
     bool whole;
     bool two;                 // labels, and a teacher at a temperature that is not 1: two sums (of a teacher alone, k is k_t)
     // backward
-    const float *saved;       // n x width {log2 sum exp, the same at the temperature or +inf, the teacher's classes' scores}
+    const float *saved;       // n x width, see keep()
     int saved_width;
     float scale, teacher_scale;
     typename T::elem *dz;     // rows x dz_stride
@@ -206,8 +213,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_scores(ScoreArgs<T> a)
             if (l < 16) to[0] = most, to[1] = sum, to[2] = sum_t;
         } else {
             const float *kept = a.saved + row * a.saved_width;
-            const float lse = kept[0], lse_t = kept[1];
-            const float s = label >= 0 ? a.scale : 0.0f, st = lse_t < INFINITY || lse_t != lse_t ? a.teacher_scale : 0.0f;
+            const float sum_t = a.teacher_scale != 0.0f ? kept[2] : INFINITY, base = base_of(kept[0], a.k), base_t = base_of(kept[0], a.k_t);
+            const float s = label >= 0 ? a.scale : 0.0f, st = sum_t != INFINITY ? a.teacher_scale : 0.0f;
+            const float share = 1.0f / kept[1], share_t = st / sum_t;
             // (the products that sum over rows leave the others out, whatever x holds there)
             if (a.listed && ct == 0 && C::a_off() == 0 && l < 16 && live) a.listed[r] = s != 0.0f || st != 0.0f ? (int32_t)r : -1;
 #pragma unroll
@@ -217,8 +225,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_scores(ScoreArgs<T> a)
                 for (int j = 0; j < 4; ++j) {
                     const float v = acc[i][t][j];
                     float d = 0.0f;
-                    if (s != 0.0f) d = s * (power_to(v, a.k, lse) - (first + 16 * i + j == label ? 1.0f : 0.0f));
-                    if (st != 0.0f) d = fmaf(st, power_to(v, a.k_t, lse_t), d);
+                    if (s != 0.0f) d = s * (power_to(v, a.k, base) * share - (first + 16 * i + j == label ? 1.0f : 0.0f));
+                    if (st != 0.0f) d = fmaf(share_t, power_to(v, a.k_t, base_t), d);
                     e[j] = T::put(d);
                     rest[j] = T::put(d - T::get(e[j]));
                 }
@@ -250,7 +258,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_scores(ScoreArgs<T> a)
                 const float base = base_of(most, a.k), log_sum = log2f(sum);
                 const bool has = (uint32_t)a.labels[row] < (uint32_t)a.all_classes;
                 if (a.loss) a.loss[row] = has ? loss_of(log_sum, own_score[in_tile], a.k, base) : 0.0f;
-                if (a.kept) a.kept[row * a.saved_width] = base + log_sum, a.kept[row * a.saved_width + 1] = INFINITY;
+                if (a.kept) keep(a.kept + row * a.saved_width, a.saved_width, most, sum, INFINITY);
                 continue;
             }
             a.part[ct * a.rows + r0 + in_tile] = float2{most, sum};
@@ -270,7 +278,7 @@ struct RowArgs {
     const float2 *part;
     const float *part_t, *label_score;
     float *loss, *teacher_loss;
-    float *saved;  // forward: null, or where lse, lse_t and the scores go; backward: those
+    float *saved;  // forward: null, or what keep() keeps and the scores; backward: those
     float *z_top;  // forward: the scores of the teacher's classes, z_stride apart for each row
     int z_stride;
     bool two;
@@ -450,12 +458,12 @@ __global__ void __launch_bounds__(256) k_class_finish(RowArgs<T> a)
         const bool has = (uint32_t)label < (uint32_t)a.classes;
         if (l == 0 && a.loss) a.loss[row] = has ? loss_of(log_sum, a.label_score[row], a.k, base) : 0.0f;
     }
-    float lse_t = INFINITY;
+    float kept_t = INFINITY;
     if (a.top_class) {
         float top_most, total, kl = 0.0f;
         const bool taught = teacher_of<LANES>(a, row, top_most, total);
         if (taught) {
-            lse_t = base_t + log_sum_t;
+            kept_t = sum_t;
             const float log_total = log2f(total);
             for (int k = l; k < a.top; k += LANES)
                 if ((uint32_t)a.top_class[row * a.top + k] < (uint32_t)a.classes) {
@@ -467,7 +475,7 @@ __global__ void __launch_bounds__(256) k_class_finish(RowArgs<T> a)
         }
         if (l == 0 && a.teacher_loss) a.teacher_loss[row] = taught ? a.t * a.t * kLn2 * kl : 0.0f;
     }
-    if (l == 0 && a.saved) a.saved[row * a.saved_width] = base + log_sum, a.saved[row * a.saved_width + 1] = lse_t;
+    if (l == 0 && a.saved) keep(a.saved + row * a.saved_width, a.saved_width, m, sum, kept_t);
 }
 
 // dz where the teacher names a class: LANES neighbours for each row, workgroups of them for each 64 classes.  A class named twice has the sum of its shares, written by both.
@@ -482,7 +490,7 @@ __global__ void __launch_bounds__(256) k_class_fix(RowArgs<T> a)
     float most, total;
     if (!teacher_of<LANES>(a, row, most, total)) return;
     const float *kept = a.saved + row * a.saved_width;
-    const float lse = kept[0], lse_t = kept[1];
+    const float base = base_of(kept[0], a.k), base_t = base_of(kept[0], a.k_t);
     int label = a.labels ? a.labels[row] : -1;
     if ((uint32_t)label >= (uint32_t)a.classes) label = -1;
     const int32_t *classes = a.top_class + row * a.top;
@@ -512,10 +520,10 @@ __global__ void __launch_bounds__(256) k_class_fix(RowArgs<T> a)
             for (int u = 0; u < AHEAD; ++u)
                 if (other[u] == c) p += share(o + u);
         }
-        const float z = kept[2 + k];
+        const float z = kept[3 + k];
         float d = 0.0f;
-        if (label >= 0 && a.scale != 0.0f) d = a.scale * (power_to(z, a.k, lse) - (c == label ? 1.0f : 0.0f));
-        if (a.teacher_scale != 0.0f) d = fmaf(a.teacher_scale, power_to(z, a.k_t, lse_t) - p, d);
+        if (label >= 0 && a.scale != 0.0f) d = a.scale * (power_to(z, a.k, base) / kept[1] - (c == label ? 1.0f : 0.0f));
+        if (a.teacher_scale != 0.0f) d = fmaf(a.teacher_scale, power_to(z, a.k_t, base_t) / kept[2] - p, d);
         if (a.blocks) {
             constexpr int PLANES = T::PER == 1 ? 3 : 1;
             uint16_t e[3], *to = reinterpret_cast<uint16_t *>(a.dz) + dz_block(r, c - a.class0, a.dz_stride, PLANES);
@@ -772,8 +780,7 @@ __device__ __forceinline__ bool lives(const LayArgs<T> &a, int64_t row)
 {
     if (row >= a.rows) return false;
     if (!a.select) return true;
-    const float lse_t = a.saved[row * a.saved_width + 1];
-    return (a.by_label && (uint32_t)a.labels[row] < (uint32_t)a.classes) || (a.by_teacher && lse_t != INFINITY);
+    return (a.by_label && (uint32_t)a.labels[row] < (uint32_t)a.classes) || (a.by_teacher && a.saved[row * a.saved_width + 2] != INFINITY);
 }
 __device__ __forceinline__ uint4 eight(const LayArgs<BF16> &a, int64_t row, int d)
 {
@@ -958,7 +965,7 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
     rows.init(q.x + (a.row0 + r0) * q.x_bytes, [&](int i) { return (uint32_t)((r0 + i < a.rows ? i : (int)(a.rows - 1 - r0)) * q.x_bytes); });
     // what the tile's classes and rows have of their own: a value for each thread, on its way during the products
     static_assert(C::BA <= stage::kThreads && C::BB <= stage::kThreads, "");
-    float my_bias = 0.0f, my_lse = INFINITY, my_lse_t = INFINITY;
+    float my_bias = 0.0f, my_most = INFINITY, my_sum = INFINITY, my_sum_t = INFINITY;  // (+inf: everything is 2^-inf of it, nothing has a share)
     int my_label = -1, my_class = 0, my_row = 0;  // (the last two: exponents)
     if (READ == stage::TWO_HALVES) {
         if (threadIdx.x < C::BA) my_class = q.w_exponent[c0 + (int)threadIdx.x < last ? c0 + (int)threadIdx.x : last];
@@ -969,16 +976,18 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
         const int64_t row = a.row0 + r0 + threadIdx.x;
         if (a.labels) my_label = a.labels[row];
         if constexpr (DZ) {
-            if (a.scale != 0.0f) my_lse = a.saved[row * a.saved_width];
-            if (a.teacher_scale != 0.0f) my_lse_t = a.saved[row * a.saved_width + 1];
+            my_most = a.saved[row * a.saved_width];
+            if (a.scale != 0.0f) my_sum = a.saved[row * a.saved_width + 1];
+            if (a.teacher_scale != 0.0f) my_sum_t = a.saved[row * a.saved_width + 2];
         }
     }
     f32x4 acc[C::FA][C::FB] = {};
     stage::multiply<READ, false, A, B, C>(lds, weight, rows, stage::Walk{2 * kPad, 2 * kPad, q.plane, q.plane, a.D, 0}, acc, [](int, int, const auto &) {});
 
-    if ((uint32_t)my_label >= (uint32_t)a.all_classes) my_label = -1, my_lse = INFINITY;
+    if ((uint32_t)my_label >= (uint32_t)a.all_classes) my_label = -1, my_sum = INFINITY;
+    if (my_sum == INFINITY && my_sum_t == INFINITY) my_most = INFINITY;  // (whatever such a row holds)
     struct Own {
-        float bias[C::BA], lse[C::BB], lse_t[C::BB];
+        float bias[C::BA], base[C::BB], base_t[C::BB], share[C::BB], share_t[C::BB];
         int label[C::BB], classes[C::BA], rows[C::BB];
     };
     struct Meet {
@@ -991,7 +1000,10 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
     if (threadIdx.x < C::BB) {
         own.rows[threadIdx.x] = my_row;
         own.label[threadIdx.x] = my_label;
-        if constexpr (DZ) own.lse[threadIdx.x] = my_lse, own.lse_t[threadIdx.x] = my_lse_t;
+        if constexpr (DZ) {
+            own.base[threadIdx.x] = base_of(my_most, a.k), own.share[threadIdx.x] = 1.0f / my_sum;
+            own.base_t[threadIdx.x] = base_of(my_most, a.k_t), own.share_t[threadIdx.x] = a.teacher_scale / my_sum_t;
+        }
     }
     __syncthreads();
     const float all_up = READ == stage::ONE_HALF ? ldexpf(1.0f, q.w_exponent[0] + q.x_exponent[0]) : 1.0f;
@@ -1106,15 +1118,15 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
                 if (a.two) a.part_t[at] = sum_t;
             }
         } else {
-            const float lse = own.lse[b], lse_t = own.lse_t[b];
+            const float base = own.base[b], base_t = own.base_t[b], share = a.scale * own.share[b], share_t = own.share_t[b];
 #pragma unroll
             for (int i = 0; i < C::FA; ++i) {
                 float d[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) d[j] = a.scale * power_to(acc[i][t][j], a.k, lse);
+                for (int j = 0; j < 4; ++j) d[j] = share * power_to(acc[i][t][j], a.k, base);
                 if (teachers) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) d[j] = fmaf(a.teacher_scale, power_to(acc[i][t][j], a.k_t, lse_t), d[j]);
+                    for (int j = 0; j < 4; ++j) d[j] = fmaf(share_t, power_to(acc[i][t][j], a.k_t, base_t), d[j]);
                 }
                 uint16_t *to = reinterpret_cast<uint16_t *>(a.dz) + dz_block(r, first - a.class0 + 16 * i, a.dz_stride, PLANES);
                 uint16_t e[PLANES][4];
@@ -1130,8 +1142,8 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
             }
             if (any) {  // the label's class again, with the label
                 const float v = own_score(t);
-                float d = a.scale * (power_to(v, a.k, lse) - 1.0f);
-                if (teachers) d = fmaf(a.teacher_scale, power_to(v, a.k_t, lse_t), d);
+                float d = a.scale * (power_to(v, a.k, base) * own.share[b] - 1.0f);
+                if (teachers) d = fmaf(share_t, power_to(v, a.k_t, base_t), d);
                 uint16_t e[3], *to = reinterpret_cast<uint16_t *>(a.dz) + dz_block(r, first - a.class0 + (mine ? at : 0), a.dz_stride, PLANES);
                 parts<T>(d, e);
                 if (mine) {
@@ -1154,7 +1166,7 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
         for (int half = 0; half < 2; ++half) sum += meet.part[1][half][b] * rebase(base_of(meet.part[0][half][b], a.k), base);
         const float log_sum = log2f(sum);
         if (a.loss) a.loss[row] = my_label >= 0 ? loss_of(log_sum, meet.own[b], a.k, base) : 0.0f;
-        if (a.kept) a.kept[row * a.saved_width] = base + log_sum, a.kept[row * a.saved_width + 1] = INFINITY;
+        if (a.kept) keep(a.kept + row * a.saved_width, a.saved_width, most, sum, INFINITY);
     }
 }
 
@@ -1503,13 +1515,15 @@ struct Call {
     hipStream_t stream;
 };
 
+int saved_width_of(const bgl_class_loss_t *l) { return l->top > 0 ? 3 + l->top : 2; }
+
 template <class T>
 RowArgs<T> row_args(const Call &c)
 {
     using E = typename T::elem;
     RowArgs<T> r{};
     r.x = (const E *)c.x, r.w = (const E *)c.weight, r.bias = (const E *)c.bias, r.labels = c.labels, r.top_class = c.top_class, r.top_score = c.top_score;
-    r.x_stride = c.x_stride, r.n = c.n, r.D = c.l->in_dim, r.classes = c.l->classes, r.top = c.l->top, r.saved_width = 2 + c.l->top;
+    r.x_stride = c.x_stride, r.n = c.n, r.D = c.l->in_dim, r.classes = c.l->classes, r.top = c.l->top, r.saved_width = saved_width_of(c.l);
     r.t = c.l->temperature, r.over_t = 1.0f / c.l->temperature, r.k = kLog2e, r.k_t = (float)(1.4426950408889634 / c.l->temperature);
     r.two = c.top_class && c.l->temperature != 1.0f;
     return r;
@@ -1521,7 +1535,7 @@ ScoreArgs<T> score_args(const Call &c)
     ScoreArgs<T> s{};
     s.x = (const E *)c.x, s.w = (const E *)c.weight, s.bias = (const E *)c.bias, s.labels = c.labels, s.x_stride = c.x_stride, s.n = c.n;
     s.classes = s.all_classes = c.l->classes, s.D = c.l->in_dim, s.k = kLog2e, s.k_t = (float)(1.4426950408889634 / c.l->temperature), s.two = c.top_class && c.l->temperature != 1.0f;
-    s.saved_width = 2 + c.l->top;
+    s.saved_width = saved_width_of(c.l);
     return s;
 }
 
@@ -1621,7 +1635,7 @@ int forward(const Call &c, float *loss, float *teacher_loss, float *saved)
     s.part = (float2 *)ws, s.part_t = (float *)(s.part + p.pass_rows * p.class_parts), s.label_score = (float *)(ws += p.part_bytes);
     char *top = ws += p.label_bytes, *x = ws += p.top_bytes, *w = ws += p.x_bytes;
     r.part = s.part, r.part_t = s.part_t, r.label_score = s.label_score;
-    r.z_top = saved ? saved + 2 : (float *)top, r.z_stride = saved ? r.saved_width : r.top;
+    r.z_top = saved ? saved + 3 : (float *)top, r.z_stride = saved ? r.saved_width : r.top;
     r.loss = loss, r.teacher_loss = teacher_loss, r.saved = saved;
     if (!c.labels) s.k = r.k = s.k_t, s.two = r.two = false;  // (no sums but those at the temperature are asked for)
     StageScoreArgs<T> q{};

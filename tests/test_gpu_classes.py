@@ -346,4 +346,4 @@ def test_refusals(torch, B):
     with pytest.raises(B.BglError):
         head.forward(x, w)
     with pytest.raises(B.BglError):
-        head.backward(x, w, torch.zeros((4, 4), device="cuda"), labels=labels)
+        head.backward(x, w, torch.zeros((4, head.saved_width), device="cuda"), labels=labels)
