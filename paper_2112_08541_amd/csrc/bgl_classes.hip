@@ -478,7 +478,7 @@ __global__ void __launch_bounds__(256) k_class_finish(RowArgs<T> a)
     if (l == 0 && a.saved) keep(a.saved + row * a.saved_width, a.saved_width, m, sum, kept_t);
 }
 
-// dz where the teacher names a class: LANES neighbours for each row, workgroups of them for each 64 classes.  A class named twice has the sum of its shares, written by both.
+// dz where the teacher names a class: LANES neighbours for each row, workgroups of them for each 64 classes.  A class named twice has the sum of its shares.
 template <class T, int LANES>
 __global__ void __launch_bounds__(256) k_class_fix(RowArgs<T> a)
 {
@@ -499,6 +499,7 @@ __global__ void __launch_bounds__(256) k_class_fix(RowArgs<T> a)
         const int c = k < a.top ? classes[k] : -1;
         const bool here = c >= a.class0 && c < a.class0 + a.piece_classes;
         float p = 0.0f;
+        bool before = false;  // an entry before this one names the class
         if constexpr (LANES == 64) {
             // (read by every lane from memory, 200 classes of 200 rows took 100 us)
             for (int o = 0; o < a.top; o += 64) {
@@ -507,7 +508,7 @@ __global__ void __launch_bounds__(256) k_class_fix(RowArgs<T> a)
 #pragma unroll 16
                 for (int j = 0; j < 64; ++j) {
                     const float add = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(its), j));
-                    if (__builtin_amdgcn_readlane(other, j) == c) p += add;
+                    if (__builtin_amdgcn_readlane(other, j) == c) p += add, before |= o + j < k;
                 }
             }
         }
@@ -518,22 +519,37 @@ __global__ void __launch_bounds__(256) k_class_fix(RowArgs<T> a)
             for (int u = 0; u < AHEAD; ++u) other[u] = o + u < a.top ? classes[o + u] : -1;
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u)
-                if (other[u] == c) p += share(o + u);
+                if (other[u] == c) p += share(o + u), before |= o + u < k;
         }
-        const float z = kept[3 + k];
+        constexpr int PLANES = T::PER == 1 ? 3 : 1;
+        uint16_t *const block = reinterpret_cast<uint16_t *>(a.dz) + (a.blocks ? dz_block(r, c - a.class0, a.dz_stride, PLANES) : 0);
+        typename T::elem *const value = a.dz + r * a.dz_stride + (c - a.class0);
         float d = 0.0f;
-        if (label >= 0 && a.scale != 0.0f) d = a.scale * (power_to(z, a.k, base) / kept[1] - (c == label ? 1.0f : 0.0f));
-        if (a.teacher_scale != 0.0f) d = fmaf(a.teacher_scale, power_to(z, a.k_t, base_t) / kept[2] - p, d);
+        if constexpr (T::PER == 1) {
+            // of what the scores' kernel made of the very score that the sum has: with one made anew, q is not near 1 as exactly as the others are near 0 (gradients of 2 classes
+            // were 2e-6 off, now 3e-7)
+            if (before) continue;
+            if (a.blocks) {
+#pragma unroll
+                for (int p = 0; p < PLANES; ++p) d += BF16::get(block[p * kBlockValues]);
+            } else {
+                d = *value;
+            }
+            d = fmaf(-a.teacher_scale, p, d);
+        } else {
+            // (there it has been rounded)
+            const float z = kept[3 + k];
+            if (label >= 0 && a.scale != 0.0f) d = a.scale * (power_to(z, a.k, base) / kept[1] - (c == label ? 1.0f : 0.0f));
+            d = fmaf(a.teacher_scale, power_to(z, a.k_t, base_t) / kept[2] - p, d);
+        }
         if (a.blocks) {
-            constexpr int PLANES = T::PER == 1 ? 3 : 1;
-            uint16_t e[3], *to = reinterpret_cast<uint16_t *>(a.dz) + dz_block(r, c - a.class0, a.dz_stride, PLANES);
+            uint16_t e[3];
             parts<T>(d, e);
 #pragma unroll
-            for (int p = 0; p < PLANES; ++p) to[p * kBlockValues] = e[p];
+            for (int p = 0; p < PLANES; ++p) block[p * kBlockValues] = e[p];
         } else {
-            const int64_t at = r * a.dz_stride + (c - a.class0);
-            a.dz[at] = T::put(d);
-            if constexpr (T::PER == 2) a.dz_rest[at] = T::put(d - T::get(a.dz[at]));
+            *value = T::put(d);
+            if constexpr (T::PER == 2) a.dz_rest[value - a.dz] = T::put(d - T::get(*value));
         }
     }
 }

@@ -237,3 +237,29 @@ def test_another_device_is_refused(torch, B):
             call(o)
     with pytest.raises(ValueError, match="device"):
         B.LayerNorm(4, 8).forward(x, x.cpu())
+
+
+@pytest.mark.parametrize("t", [1.0, 2.0])
+def test_gradients_near_certainty(torch, B, t):
+    """Scores that are exact, up to 60 and within 4 of each other, and the weight of the identity, so that dx is dz: right to 16 u of 1 however large the scores are.  A
+    power is off by 2 u and by what its argument is, half a step of one below 8 over log2(e): 4 u; a sum of two by as much; their quotient and the rest by 4 roundings:
+    together 2 (2 + 4) + 4 = 16 u."""
+    n, u = 400, 2.0 ** -24
+    g = torch.Generator(device="cuda").manual_seed(1)
+    high = torch.randint(40, 240, (n,), generator=g, device="cuda") / 4
+    x = torch.stack([high, high - torch.randint(0, 17, (n,), generator=g, device="cuda") / 4], 1)
+    x[::2] = x[::2].flip(1)
+    w = torch.eye(2, device="cuda")
+    labels = torch.randint(0, 2, (n,), generator=g, device="cuda", dtype=torch.int32)
+    z, onehot = x.double(), torch.nn.functional.one_hot(labels.long(), 2).double()
+    got = run(torch, B, "f32", x, w, None, labels, None, s=1.0, want=("dx", "dweight"))
+    assert ((got["dx"].double() - (z.softmax(1) - onehot)).abs() <= 16 * u).all()
+    classes = torch.tensor([[0, 1]], dtype=torch.int32, device="cuda").repeat(n, 1)
+    classes[::3] = classes[::3].flip(1)
+    classes[5], classes[7, 0] = 1, -1
+    scores = torch.randint(-8, 8, (n, 2), generator=g, device="cuda") / 4
+    e = (scores.double() / t).exp() * (classes >= 0)
+    p = torch.zeros((n, 2), dtype=torch.float64, device="cuda").scatter_add_(1, classes.clamp_min(0).long(), e / e.sum(1, keepdim=True))
+    got = run(torch, B, "f32", x, w, None, None, (classes, scores), t, 0.0, 1.0, want=("dx", "dweight"))
+    # (the teacher's p as well, its arguments below 8 too; the factor t is exact)
+    assert ((got["dx"].double() - t * ((z / t).softmax(1) - p)).abs() <= 2 * 16 * u * t).all()
