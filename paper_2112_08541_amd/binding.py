@@ -594,14 +594,26 @@ def _weights(name: str, t: Optional[torch.Tensor], shape, dtype):
     return _dev_ptr(t, dtype)
 
 
-def _on_device(owner, *tensors) -> None:
-    """The owner's memory, the current device and the tensors are of one device: a launch on another one's memory could fault."""
-    device = owner._device
-    if torch._C._cuda_getDevice() != device:
-        raise ValueError(f"made on device {device}, called with {torch._C._cuda_getDevice()} the current one")
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise ValueError(f"expected tensors of device {device}, got one of {t.device}")
+# Of objects that belong to one device: their memory, the current device and the tensors have to be of it, as a launch on another one's memory could fault.
+def _stream_on(device: int, stream) -> int:
+    now = torch._C._cuda_getDevice()
+    if now != device:
+        raise ValueError(f"made on device {device}, called with device {now} the current one")
+    return torch._C._cuda_getCurrentRawStream(now) if stream is None else int(stream.cuda_stream)
+
+
+def _matrix_on(device: int, name: str, t: Optional[torch.Tensor], n: int, width: int, dtype):
+    if t is not None and t.get_device() != device:
+        raise ValueError(f"{name}: expected a tensor of device {device}, got one of {t.device}")
+    return _matrix(name, t, n, width, dtype)
+
+
+def _weights_on(device: int, name: str, t: Optional[torch.Tensor], shape, dtype):
+    if t is None:
+        return None
+    if t.get_device() != device or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor of device {device}, {dtype} and shape {shape}, got {t.device}, {t.dtype}, {tuple(t.shape)}")
+    return t.data_ptr()
 
 
 def _refuse_gradients(who: str, *tensors) -> None:
@@ -785,20 +797,19 @@ class LayerNorm:
     def forward(self, x, y, weight=None, bias=None, saved=None, stream=None) -> None:
         """Writes y (which may be x), and saved = (n, 2) floats if given (the backward call needs them).  Tensors that require gradients are
         refused as by Linear.forward."""
-        n = int(x.shape[0])
+        n, d = int(x.shape[0]), self._device
         _refuse_gradients("the norm", x, weight, bias)
-        _on_device(self, x, y, weight, bias, saved)
         if n > self.max_rows:
             raise ValueError(f"{n} rows, the norm was made for {self.max_rows}")
         _check(lib().bgl_layer_norm_forward(
-            self._ref, n, *_matrix("x", x, n, self.width, self.dtype), _weights("weight", weight, (self.width,), self.dtype),
-            _weights("bias", bias, (self.width,), self.dtype), *_matrix("y", y, n, self.width, self.dtype),
-            _weights("saved", saved, (n, 2), torch.float32), _stream_handle(stream)))
+            self._ref, n, *_matrix_on(d, "x", x, n, self.width, self.dtype), _weights_on(d, "weight", weight, (self.width,), self.dtype),
+            _weights_on(d, "bias", bias, (self.width,), self.dtype), *_matrix_on(d, "y", y, n, self.width, self.dtype),
+            _weights_on(d, "saved", saved, (n, 2), torch.float32), _stream_on(d, stream)))
 
     def backward(self, dy, x, saved, weight=None, dx=None, dweight=None, dbias=None, stream=None) -> None:
         """Writes the gradients that are given memory: dx (which may be dy), dweight, dbias."""
-        n = int(dy.shape[0])
-        _on_device(self, dy, x, saved, weight, dx, dweight, dbias)
+        n, d = int(dy.shape[0]), self._device
+        on = _stream_on(d, stream)
         if n > self.max_rows:
             raise ValueError(f"{n} rows, the norm was made for {self.max_rows}")
         if self.workspace is None:
@@ -806,10 +817,10 @@ class LayerNorm:
             if stream is not None:      # (the memory may have been another tensor's on the current stream)
                 stream.wait_stream(torch.cuda.current_stream())
         _check(lib().bgl_layer_norm_backward(
-            self._ref, n, *_matrix("dy", dy, n, self.width, self.dtype), *_matrix("x", x, n, self.width, self.dtype),
-            _weights("weight", weight, (self.width,), self.dtype), _weights("saved", saved, (n, 2), torch.float32),
-            *_matrix("dx", dx, n, self.width, self.dtype), _weights("dweight", dweight, (self.width,), self.dtype),
-            _weights("dbias", dbias, (self.width,), self.dtype), self.workspace.data_ptr(), self.workspace.numel(), _stream_handle(stream)))
+            self._ref, n, *_matrix_on(d, "dy", dy, n, self.width, self.dtype), *_matrix_on(d, "x", x, n, self.width, self.dtype),
+            _weights_on(d, "weight", weight, (self.width,), self.dtype), _weights_on(d, "saved", saved, (n, 2), torch.float32),
+            *_matrix_on(d, "dx", dx, n, self.width, self.dtype), _weights_on(d, "dweight", dweight, (self.width,), self.dtype),
+            _weights_on(d, "dbias", dbias, (self.width,), self.dtype), self.workspace.data_ptr(), self.workspace.numel(), on))
 
 
 class ClassLoss:
@@ -839,37 +850,39 @@ class ClassLoss:
         """Floats for each row that the backward call needs of the forward one."""
         return 3 + self.top if self.top else 2
 
-    def _inputs(self, x, weight, bias, labels, teacher, *outputs):
-        n = int(x.shape[0])
+    def _inputs(self, x, weight, bias, labels, teacher):
+        n, d = int(x.shape[0]), self._device
         if n > self.max_rows:
             raise ValueError(f"{n} rows, the loss was made for {self.max_rows}")
         classes, scores = (None, None) if teacher is None else teacher
-        _on_device(self, x, weight, bias, labels, classes, scores, *outputs)
-        return n, (*_matrix("x", x, n, self.in_dim, self.dtype), _weights("weight", weight, (self.classes, self.in_dim), self.dtype),
-                   _weights("bias", bias, (self.classes,), self.dtype), _weights("labels", labels, (n,), torch.int32),
-                   _weights("teacher's classes", classes, (n, self.top), torch.int32), _weights("teacher's scores", scores, (n, self.top), torch.float32))
+        return n, (*_matrix_on(d, "x", x, n, self.in_dim, self.dtype), _weights_on(d, "weight", weight, (self.classes, self.in_dim), self.dtype),
+                   _weights_on(d, "bias", bias, (self.classes,), self.dtype), _weights_on(d, "labels", labels, (n,), torch.int32),
+                   _weights_on(d, "teacher's classes", classes, (n, self.top), torch.int32), _weights_on(d, "teacher's scores", scores, (n, self.top), torch.float32))
 
     def forward(self, x, weight, bias=None, labels=None, teacher=None, loss=None, teacher_loss=None, saved=None, stream=None) -> None:
         """Writes what is given of loss and teacher_loss, (n,) floats each, and saved = (n, saved_width) floats (the backward call needs them).
         Tensors that require gradients are refused as by Linear.forward."""
         _refuse_gradients("the loss", x, weight, bias, None if teacher is None else teacher[1])
-        n, inputs = self._inputs(x, weight, bias, labels, teacher, loss, teacher_loss, saved)
+        d = self._device
+        on = _stream_on(d, stream)
+        n, inputs = self._inputs(x, weight, bias, labels, teacher)
         if self._made is not None:
             _first_call(self, stream)
         _check(lib().bgl_class_loss_forward(
-            self._ref, n, *inputs, _weights("loss", loss, (n,), torch.float32), _weights("teacher_loss", teacher_loss, (n,), torch.float32),
-            _weights("saved", saved, (n, self.saved_width), torch.float32), self.workspace.data_ptr(), self.workspace.numel(), _stream_handle(stream)))
+            self._ref, n, *inputs, _weights_on(d, "loss", loss, (n,), torch.float32), _weights_on(d, "teacher_loss", teacher_loss, (n,), torch.float32),
+            _weights_on(d, "saved", saved, (n, self.saved_width), torch.float32), self.workspace.data_ptr(), self.workspace.numel(), on))
 
     def backward(self, x, weight, saved, bias=None, labels=None, teacher=None, scale: float = 1.0, teacher_scale: float = 1.0,
                  dx=None, dweight=None, dbias=None, stream=None) -> None:
         """Writes the gradients of scale * loss.sum() + teacher_scale * teacher_loss.sum() that are given memory: dx, dweight, dbias (with dweight)."""
-        n, inputs = self._inputs(x, weight, bias, labels, teacher, saved, dx, dweight, dbias)
+        d = self._device
+        on = _stream_on(d, stream)
+        n, inputs = self._inputs(x, weight, bias, labels, teacher)
         if self.backward_workspace is None:
             self.backward_workspace = _workspace(self._backward_bytes)
             if stream is not None:      # (the memory may have been another tensor's on the current stream)
                 stream.wait_stream(torch.cuda.current_stream())
         _check(lib().bgl_class_loss_backward(
-            self._ref, n, *inputs, _weights("saved", saved, (n, self.saved_width), torch.float32), float(scale), float(teacher_scale),
-            *_matrix("dx", dx, n, self.in_dim, self.dtype), _weights("dweight", dweight, (self.classes, self.in_dim), self.dtype),
-            _weights("dbias", dbias, (self.classes,), self.dtype), self.backward_workspace.data_ptr(), self.backward_workspace.numel(),
-            _stream_handle(stream)))
+            self._ref, n, *inputs, _weights_on(d, "saved", saved, (n, self.saved_width), torch.float32), float(scale), float(teacher_scale),
+            *_matrix_on(d, "dx", dx, n, self.in_dim, self.dtype), _weights_on(d, "dweight", dweight, (self.classes, self.in_dim), self.dtype),
+            _weights_on(d, "dbias", dbias, (self.classes,), self.dtype), self.backward_workspace.data_ptr(), self.backward_workspace.numel(), on))
