@@ -290,16 +290,13 @@ struct RowArgs {
 
 // The scores of the teacher's classes: 8 lanes for four of a row's, 128 bytes of x and of the classes' rows at a time.  4,096 rows of 512 bf16, 32 classes each: 20 us, 6.6
 // TB/s of rows that the L2s mostly have.
-template <class T>
-__global__ void __launch_bounds__(256) k_class_top(RowArgs<T> a)
+// keep(k, z) for each, in the first lane.
+constexpr int kTopLanes = 8, kTopEach = 4;
+template <class T, class F>
+__device__ __forceinline__ void top_scores(const RowArgs<T> a, int64_t row, int k0, F keep)
 {
-    constexpr int LANES = 8, EACH = 4, AHEAD = 2, STEP = LANES * T::VEC;
-    const uint32_t groups = ((uint32_t)a.top + EACH - 1) / EACH;
-    const uint64_t task = (uint64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES, r = task / groups;
+    constexpr int LANES = kTopLanes, EACH = kTopEach, AHEAD = 2, STEP = LANES * T::VEC;
     const int l = threadIdx.x % LANES;
-    if (r >= (uint64_t)a.rows) return;
-    const int64_t row = a.row0 + r;
-    const int k0 = (int)(task % groups) * EACH;
     const typename T::elem *x = a.x + row * a.x_stride, *w[EACH];
     int c[EACH];
     float z[EACH] = {};
@@ -344,8 +341,17 @@ __global__ void __launch_bounds__(256) k_class_top(RowArgs<T> a)
 #pragma unroll
     for (int k = 0; k < EACH; ++k) {
         z[k] = sum_across<LANES>(z[k]);
-        if (l == 0 && k0 + k < a.top) a.z_top[row * a.z_stride + k0 + k] = c[k] < 0 ? 0.0f : z[k] + (a.bias ? T::get(a.bias[c[k]]) : 0.0f);
+        if (l == 0 && k0 + k < a.top) keep(k0 + k, c[k] < 0 ? 0.0f : z[k] + (a.bias ? T::get(a.bias[c[k]]) : 0.0f));
     }
+}
+template <class T>
+__global__ void __launch_bounds__(256) k_class_top(RowArgs<T> a)
+{
+    const uint32_t groups = ((uint32_t)a.top + kTopEach - 1) / kTopEach;
+    const uint64_t task = (uint64_t)blockIdx.x * (256 / kTopLanes) + threadIdx.x / kTopLanes, r = task / groups;
+    if (r >= (uint64_t)a.rows) return;
+    const int64_t row = a.row0 + r;
+    top_scores(a, row, (int)(task % groups) * kTopEach, [=](int k, float z) { a.z_top[row * a.z_stride + k] = z; });
 }
 
 // The teacher's distribution of a row, for LANES neighbours: largest score / t and sum of exp; false where it names no class.
@@ -417,11 +423,26 @@ __global__ void __launch_bounds__(kMergeRows *kMergeLanes) k_class_merge(RowArgs
     if (a.two) part_t[row] = sum_t;
 }
 
+// TOP: with the scores of the teacher's classes, kTopHere at most, of kTopRows rows (forward call of 512 x 100 x 150 with 8 classes: 16.5 us with a launch of k_class_top, 14.1 so;
+// 20 rows with 64 classes 15 and 27; a row with 16 and 512 parts to add up 33 and 37; 100,000 rows with 4 64 and 76, as 16 lanes are many for a row).
+constexpr int kTopHere = 8, kTopRows = 64 * kCus;
 // LANES neighbours for each row: 4 for few parts and classes of the teacher (4,096 rows 4.6 us, a launch), 16, or a wavefront.
-template <class T, int LANES>
+template <class T, int LANES, bool TOP = false>
 __global__ void __launch_bounds__(256) k_class_finish(RowArgs<T> a)
 {
-    const int64_t r = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    constexpr int ROWS = 256 / LANES;
+    __shared__ float z_here[TOP ? ROWS : 1][TOP ? kTopHere + 1 : 1];
+    const int64_t first_row = (int64_t)blockIdx.x * ROWS, r = first_row + threadIdx.x / LANES;
+    if constexpr (TOP) {
+        const uint32_t groups = ((uint32_t)a.top + kTopEach - 1) / kTopEach;
+        for (uint32_t task = threadIdx.x / kTopLanes; task < ROWS * groups; task += 256 / kTopLanes) {
+            const int at = (int)(task / groups);
+            if (first_row + at >= a.rows) break;
+            const int64_t row = a.row0 + first_row + at;
+            top_scores(a, row, (int)(task % groups) * kTopEach, [&](int k, float z) { a.z_top[row * a.z_stride + k] = z_here[at][k] = z; });
+        }
+        __syncthreads();
+    }
     if (r >= a.rows) return;
     const int64_t row = a.row0 + r;
     const int l = threadIdx.x % LANES;
@@ -469,7 +490,7 @@ __global__ void __launch_bounds__(256) k_class_finish(RowArgs<T> a)
                 if ((uint32_t)a.top_class[row * a.top + k] < (uint32_t)a.classes) {
                     const float v = a.top_score[row * a.top + k] * a.over_t - top_most;
                     const float p = exp_of(v) / total;
-                    if (p != 0.0f) kl = fmaf(p, (v * kLog2e - log_total) + (log_sum_t - fmaf(a.z_top[row * a.z_stride + k], a.k_t, -base_t)), kl);
+                    if (p != 0.0f) kl = fmaf(p, (v * kLog2e - log_total) + (log_sum_t - fmaf(TOP ? z_here[threadIdx.x / LANES][k] : a.z_top[row * a.z_stride + k], a.k_t, -base_t)), kl);
                 }
             kl = sum_across<LANES>(kl);
         }
@@ -1668,14 +1689,16 @@ int forward(const Call &c, float *loss, float *teacher_loss, float *saved)
         if (h.large) q.s = s, launch_scores_stage<T, false>(q, c.stream);
         else launch_scores<T, false>(s, c.stream);
         if (s.whole) continue;  // (every tile has all classes)
-        if (c.top_class && !q.top_class) k_class_top<T><<<dim3((unsigned)ceil_div(r.rows * ((r.top + 3) / 4), 32)), dim3(256), 0, c.stream>>>(r);
+        const bool top_here = c.top_class && !q.top_class && r.top <= kTopHere && r.rows <= kTopRows && p.class_parts <= 32;
+        if (c.top_class && !q.top_class && !top_here) k_class_top<T><<<dim3((unsigned)ceil_div(r.rows * ((r.top + 3) / 4), 32)), dim3(256), 0, c.stream>>>(r);
         r.class_parts = p.class_parts;
         if (r.class_parts > 32 && r.rows >= 64) {
             k_class_merge<T><<<dim3((unsigned)ceil_div(r.rows, kMergeRows)), dim3(kMergeRows * kMergeLanes), 0, c.stream>>>(r, s.part, s.part_t);
             r.class_parts = 1;
         }
         const int values = c.top_class && r.top > r.class_parts ? r.top : r.class_parts;
-        if (values <= 8) k_class_finish<T, 4><<<dim3((unsigned)ceil_div(r.rows, 64)), dim3(256), 0, c.stream>>>(r);
+        if (top_here) k_class_finish<T, 16, true><<<dim3((unsigned)ceil_div(r.rows, 16)), dim3(256), 0, c.stream>>>(r);
+        else if (values <= 8) k_class_finish<T, 4><<<dim3((unsigned)ceil_div(r.rows, 64)), dim3(256), 0, c.stream>>>(r);
         else if (values <= 32) k_class_finish<T, 16><<<dim3((unsigned)ceil_div(r.rows, 16)), dim3(256), 0, c.stream>>>(r);
         else k_class_finish<T, 64><<<dim3((unsigned)ceil_div(r.rows, 4)), dim3(256), 0, c.stream>>>(r);
     }
