@@ -46,12 +46,35 @@ __device__ __forceinline__ i32x4 whole_memory_from(const char *base)
     const uint64_t at = (uint64_t)base;
     return i32x4{__builtin_amdgcn_readfirstlane((int)(uint32_t)at), __builtin_amdgcn_readfirstlane((int)((uint32_t)(at >> 32) & 0xffff)), -1, 0x00020000};
 }
-// 16 bytes for each lane from base + lane_offset to lds + 16 * lane.  In assembly because the compiler puts a wait for all loads before the next read of LDS where
-// it makes these loads itself; multiply() counts them.  (No vector register is written, so none can be lost to a load on its way; m0 is not kept for anything else on this GPU.)
-__device__ __forceinline__ void load_to_lds(i32x4 from, char *lds, uint32_t lane_offset)
+// LOADS times 16 bytes for each lane, from base + off[i] to lds + 1,024 i + 16 lane.  In assembly because the compiler puts a wait for all loads before the next read of LDS
+// where it makes these loads itself; multiply() counts them.  (No vector register is written, so none can be lost to a load on its way.)
+// Nothing in a block of assembly is known to the compiler as a load, so the block itself has what a load needs: the buffer's words may have been written by the vector
+// instruction (a v_readfirstlane) right before the block, 5 wait states before a load may read them, two s_mov and s_nop 2; m0 1 before a load into LDS, s_nop 0.
+// The compiler does not take m0 as something a block writes: it is put back.
+template <int LOADS>
+__device__ __forceinline__ void load_to_lds(i32x4 from, char *lds, const uint32_t (&off)[LOADS])
 {
+#define BGL_FIRST "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 2\n\tbuffer_load_dwordx4 %3, %2, 0 offen lds\n\t"
+#define BGL_NEXT(V) "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 " V ", %2, 0 offen lds\n\t"
+#define BGL_END "s_mov_b32 m0, %0"
     const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(lane_offset), "s"(from) : "memory");
+    uint32_t m0;
+    static_assert(LOADS == 2 || LOADS == 4 || LOADS == 6, "");
+    if constexpr (LOADS == 2)
+        asm volatile(BGL_FIRST BGL_NEXT("%4") BGL_END : "=&s"(m0) : "s"(to), "s"(from), "v"(off[0]), "v"(off[1]) : "memory", "scc");
+    else if constexpr (LOADS == 4)
+        asm volatile(BGL_FIRST BGL_NEXT("%4") BGL_NEXT("%5") BGL_NEXT("%6") BGL_END
+                     : "=&s"(m0)
+                     : "s"(to), "s"(from), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3])
+                     : "memory", "scc");
+    else
+        asm volatile(BGL_FIRST BGL_NEXT("%4") BGL_NEXT("%5") BGL_NEXT("%6") BGL_NEXT("%7") BGL_NEXT("%8") BGL_END
+                     : "=&s"(m0)
+                     : "s"(to), "s"(from), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "v"(off[4]), "v"(off[5])
+                     : "memory", "scc");
+#undef BGL_FIRST
+#undef BGL_NEXT
+#undef BGL_END
 }
 
 template <int BO, int STEP_>
@@ -75,9 +98,7 @@ struct Kc {
     }
     __device__ __forceinline__ void load(char *lds, uint64_t offset, int) const
     {
-        const auto from = whole_memory_from(base + offset);
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) load_to_lds(from, lds + (wave_number() * LOADS + i) * 1024, off[i]);
+        load_to_lds(whole_memory_from(base + offset), lds + wave_number() * LOADS * 1024, off);
     }
     // F fragments of rows from `first` on, the part'th 32 of the stage's summed values
     template <int F>
@@ -127,16 +148,15 @@ struct Oc {
     __device__ __forceinline__ void load(char *lds, uint64_t offset, int left) const
     {
         const auto from = whole_memory_from(base + offset);
-        if (left >= STEP) {
+        char *const to = lds + wave_number() * LOADS * 1024;
+        if (left >= STEP) return load_to_lds(from, to, off);
+        uint32_t there[LOADS];
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) load_to_lds(from, lds + (wave_number() * LOADS + i) * 1024, off[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int k = row_of(i), beyond = k >= left ? k - (left - 1) : 0;
-                load_to_lds(from, lds + (wave_number() * LOADS + i) * 1024, off[i] - beyond * stride);
-            }
+        for (int i = 0; i < LOADS; ++i) {
+            const int k = row_of(i), beyond = k >= left ? k - (left - 1) : 0;
+            there[i] = off[i] - beyond * stride;
         }
+        load_to_lds(from, to, there);
     }
     template <int F>
     static __device__ __forceinline__ void read(const char *lds, int first, int, bf16x8 (&f)[F])
@@ -167,9 +187,7 @@ struct OcBlocks {
     }
     __device__ __forceinline__ void load(char *lds, uint64_t offset, int) const
     {
-        const auto from = whole_memory_from(base + offset);
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) load_to_lds(from, lds + (wave_number() * LOADS + i) * 1024, off[i]);
+        load_to_lds(whole_memory_from(base + offset), lds + wave_number() * LOADS * 1024, off);
     }
     template <int F>
     static __device__ __forceinline__ void read(const char *lds, int first, int, bf16x8 (&f)[F])
