@@ -62,7 +62,9 @@ __device__ __forceinline__ void keep(float *to, int width, float most, float sum
 }
 // The logarithm of the sum less the score, both to the sum's base (what they have in common goes before they meet), in natural units.
 __device__ __forceinline__ float loss_of(float log_sum, float score, float k, float base) { return kLn2 * (log_sum - fmaf(score, k, -base)); }
-__device__ __forceinline__ float rebase(float from, float to) { return __builtin_amdgcn_exp2f(from - to); }
+// What a sum to the base of `most` is to be multiplied by to be to the base `to`, that of no smaller a value.  A sum of nothing has no base (base_of's 0 for it may be far
+// above `to`: 0 times 2^(0 - to) was NaN for rows whose scores are all below -88): 0, which leaves a NaN one.
+__device__ __forceinline__ float rebase(float most, float k, float to) { return most == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(base_of(most, k) - to); }
 
 // The other lanes with the same lane % 16.
 template <class F>
@@ -250,8 +252,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_scores(ScoreArgs<T> a)
 #pragma unroll
             for (int w = 0; w < WA; ++w) {
                 const float *from = meet + (w * C::BB + in_tile) * 3;
-                sum += from[1] * rebase(base_of(from[0], a.k), base_of(most, a.k));
-                if (a.two) sum_t += from[2] * rebase(base_of(from[0], a.k_t), base_of(most, a.k_t));
+                sum += from[1] * rebase(from[0], a.k, base_of(most, a.k));
+                if (a.two) sum_t += from[2] * rebase(from[0], a.k_t, base_of(most, a.k_t));
             }
             if (a.whole) {
                 const int64_t row = a.row0 + r0 + in_tile;
@@ -388,8 +390,8 @@ __global__ void __launch_bounds__(kMergeRows *kMergeLanes) k_class_merge(RowArgs
     const int64_t row = (int64_t)blockIdx.x * kMergeRows + i, r = row < a.rows ? row : a.rows - 1;
     float most = -INFINITY, sum = 0.0f, sum_t = 0.0f;
     const auto take = [&](float base, float base_t, float largest, float s, float t) {
-        sum += s * rebase(base_of(largest, a.k), base);
-        if (a.two) sum_t += t * rebase(base_of(largest, a.k_t), base_t);
+        sum += s * rebase(largest, a.k, base);
+        if (a.two) sum_t += t * rebase(largest, a.k_t, base_t);
     };
     for (int first = l; first < a.class_parts; first += kMergeLanes * AHEAD) {
         float2 from[AHEAD];
@@ -404,8 +406,8 @@ __global__ void __launch_bounds__(kMergeRows *kMergeLanes) k_class_merge(RowArgs
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) m = fmaxf(m, from[u].x);
         const float base = base_of(m, a.k), base_t = base_of(m, a.k_t);
-        sum *= rebase(base_of(most, a.k), base);
-        sum_t *= rebase(base_of(most, a.k_t), base_t);
+        sum *= rebase(most, a.k, base);
+        sum_t *= rebase(most, a.k_t, base_t);
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) take(base, base_t, from[u].x, from[u].y, at_t[u]);
         most = m;
@@ -461,18 +463,18 @@ __global__ void __launch_bounds__(256) k_class_finish(RowArgs<T> a)
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) m = fmaxf(m, from[u].x);
         const float base = base_of(m, a.k), base_t = base_of(m, a.k_t);
-        sum *= rebase(base_of(most, a.k), base);
-        sum_t *= rebase(base_of(most, a.k_t), base_t);
+        sum *= rebase(most, a.k, base);
+        sum_t *= rebase(most, a.k_t, base_t);
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-            sum += from[u].y * rebase(base_of(from[u].x, a.k), base);
-            sum_t += at_t[u] * rebase(base_of(from[u].x, a.k_t), base_t);
+            sum += from[u].y * rebase(from[u].x, a.k, base);
+            sum_t += at_t[u] * rebase(from[u].x, a.k_t, base_t);
         }
         most = m;
     }
     const float m = max_across<LANES>(most), base = base_of(m, a.k), base_t = a.two ? base_of(m, a.k_t) : base;
-    sum = sum_across<LANES>(sum * rebase(base_of(most, a.k), base));
-    sum_t = a.two ? sum_across<LANES>(sum_t * rebase(base_of(most, a.k_t), base_t)) : sum;
+    sum = sum_across<LANES>(sum * rebase(most, a.k, base));
+    sum_t = a.two ? sum_across<LANES>(sum_t * rebase(most, a.k_t, base_t)) : sum;
     const float log_sum = log2f(sum), log_sum_t = log2f(sum_t);
     if (a.labels) {
         const int label = a.labels[row];
@@ -1200,7 +1202,7 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
         const float most = fmaxf(meet.part[0][0][b], meet.part[0][1][b]), base = base_of(most, a.k);
         float sum = 0.0f;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) sum += meet.part[1][half][b] * rebase(base_of(meet.part[0][half][b], a.k), base);
+        for (int half = 0; half < 2; ++half) sum += meet.part[1][half][b] * rebase(meet.part[0][half][b], a.k, base);
         const float log_sum = log2f(sum);
         if (a.loss) a.loss[row] = my_label >= 0 ? loss_of(log_sum, meet.own[b], a.k, base) : 0.0f;
         if (a.kept) keep(a.kept + row * a.saved_width, a.saved_width, most, sum, INFINITY);
