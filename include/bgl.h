@@ -836,7 +836,8 @@ int bgl_orthogonalize(const void *update, int64_t update_matrix_stride, int64_t 
  *   weight, bias  device, width values each; null: ones, zeros
  *   y             n rows of width; may be x itself (with its stride)
  *   saved         device, n pairs of floats that receive m and r for the backward call, or null
- * Sums are fp32; squares that leave its range do no harm (rows of values up to 1e38 are normalised as others).
+ * Sums are fp32; squares that leave its range do no harm (rows of values up to 1e38 are normalised as others).  A row's differences from its mean count,
+ * however small they are beside it; rows of equal values have h = 0, so y = bias, whatever the value.
  * A row with a value that is not finite is NaN; other rows are not touched by it.
  * n = 0 does nothing.
  * Errors: BGL_EINVAL (null or misaligned pointers, strides, width < 1, eps outside

@@ -118,8 +118,10 @@ __device__ __forceinline__ void team_sums(float &a, float &b, float *lds, int &t
 template <int TEAM>
 constexpr int norm_threads() { return TEAM < 256 ? 256 : TEAM; }
 
-// The mean, in two parts (the values' mean as fp32 has it, and the mean of what is left then, so that rows far from zero keep their spread), and r of the row
-// that the team holds.  Where squares leave fp32's range they are taken of values scaled by a power of two (the same for the whole team).
+// The mean, in two parts (m, what fp32 has of the values' mean, and the mean of what is left then, so that rows far from zero keep their spread), and r of the row
+// that the team holds.  The sum that m is made of rounds as the values are large: where they differ no more than that (the mean square of x - m is below 2^-28 m^2), or their
+// squares leave fp32's range, m is made once more, of the differences from the row's first value, which are exact for values near each other, and 0 for equal ones: rows of
+// equal values are normalised to 0 whatever they are.  Beyond the range all of that is of values scaled by a power of two (the same for the whole team).
 template <class T, int TEAM, Fit FIT>
 __device__ __forceinline__ void moments(const Piece<T, TEAM, kValues, FIT> &p, float (&v)[kValues], float eps, float *lds, int &turn, float &mean, float &rest, float &r)
 {
@@ -138,26 +140,31 @@ __device__ __forceinline__ void moments(const Piece<T, TEAM, kValues, FIT> &p, f
         q = fmaf(d, d, q);
     }
     team_sums<TEAM>(c, q, lds, turn);
-    const bool far = !(q < INFINITY);
-    // (a workgroup's teams of more than a wavefront share barriers: with one team that is far all go again)
-    if (TEAM > 64 ? __syncthreads_or(far) : far) {
+    const bool far = !(q < INFINITY), again = far || q * share <= m * m * 0x1p-28f;
+    // (a workgroup's teams of more than a wavefront share barriers: where one goes again all do, and the others leave what they have)
+    if (TEAM > 64 ? __syncthreads_or(again) : again) {
         if (far) scale = kFar;
+        float one = p.first == 0 ? v[0] * scale : 0.0f, c1 = 0.0f, q1 = 0.0f;
+        team_sums<TEAM>(one, unused, lds, turn);
         s = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kValues; ++i) s += v[i] * scale;
+        for (int i = 0; i < kValues; ++i) s += p.has(i) ? v[i] * scale - one : 0.0f;
         team_sums<TEAM>(s, unused, lds, turn);
-        m = s * share, c = 0.0f, q = 0.0f;
+        const float m1 = one + s * share;
 #pragma unroll
         for (int i = 0; i < kValues; ++i) {
-            const float d = p.has(i) ? v[i] * scale - m : 0.0f;
-            c += d;
-            q = fmaf(d, d, q);
+            const float d = p.has(i) ? v[i] * scale - m1 : 0.0f;
+            c1 += d;
+            q1 = fmaf(d, d, q1);
         }
-        team_sums<TEAM>(c, q, lds, turn);
+        team_sums<TEAM>(c1, q1, lds, turn);
+        if (again) m = m1, c = c1, q = q1;
     }
     c *= share;
     const float var = fmaxf(fmaf(q, share, -c * c), 0.0f) + (q - q);  // (fmaxf would hide a NaN)
+    const float most = 1.0f / sqrtf(eps);
     r = scale / sqrtf(var + eps * scale * scale);
+    if (r > most) r = most;  // (scaled, eps may be nothing beside the variance, and that nothing too)
     mean = m / scale, rest = c / scale;
 }
 
