@@ -20,6 +20,7 @@ constexpr int kValues = 16;          // of a row a thread holds
 constexpr int64_t kMostThreads = (int64_t)1 << 31;     // of a launch, which has room for 2^32 - 1
 constexpr int kMaxParts = 512;       // workgroups of a backward call that sums weight gradients, so rows of its partial sums
 constexpr float kFar = 0x1p-80f;     // scales rows whose squares leave fp32's range
+constexpr float kAway = 16.0f;       // deviations from zero that a row's mean has at most for places behind the row to be left as they come
 
 template <class T>
 struct NormArgs {
@@ -220,15 +221,22 @@ __global__ void __launch_bounds__(norm_threads<TEAM>()) k_norm_backward(NormArgs
         const int64_t row = first + threadIdx.x / TEAM;
         const bool live = row < a.n;
         float dy[VALUES], h[VALUES];
-        float c1 = 0.0f, c2 = 0.0f, r = 0.0f;
+        float c1 = 0.0f, c2 = 0.0f, mean = 0.0f, r = 0.0f;
         if (live) {
             p.load(a.dy + row * a.dy_stride, dy);
             p.load(a.x + row * a.x_stride, h);
-            const float mean = a.saved[2 * row];
-            r = a.saved[2 * row + 1];
+            mean = a.saved[2 * row], r = a.saved[2 * row + 1];
+        }
+        // where the mean is far from zero beside the spread, places behind the row could be beyond the type
+        if (!(fabsf(mean) * r <= kAway)) {
+#pragma unroll
+            for (int i = 0; i < VALUES; ++i) h[i] = p.has(i) ? h[i] - mean : 0.0f;
+            mean = 0.0f;
+        }
+        if (live) {
 #pragma unroll
             for (int i = 0; i < VALUES; ++i) {
-                h[i] = (h[i] - mean) * r;  // (behind the row any number: dy is 0 there)
+                h[i] = (h[i] - mean) * r;  // (behind the row a number up to kAway: dy is 0 there)
                 if constexpr (SUMS) dg[i] = fmaf(dy[i], h[i], dg[i]), db[i] += dy[i];
                 dy[i] *= g[i];
                 c1 += dy[i];

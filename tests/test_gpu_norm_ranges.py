@@ -2,7 +2,7 @@
 
 The bounds are those of test_gpu_norm.py without its u |mean| r: the mean counts in the values' differences from it alone.  Where these are no more than the last places
 of the values, the mean of x - m has up to 2 sigma of absolute values (m is the nearest number to the mean, and differences are whole last places), so it is off by 60 u
-sigma, squares less the mean's square by 70 u of the variance, r by 40 u.  Together H = 40 u |h| + 80 u.
+sigma, squares less the mean's square by 70 u of the variance, r by 40 u; a mean within 16 sigma of 0 is kept in 32 bits for the backward call, 16 u.  Together H = 40 u |h| + 80 u.
 Rows of equal values have h = 0, whatever they are: y is the bias."""
 import numpy as np
 import pytest
@@ -34,10 +34,14 @@ def others(torch, kind, n, width, seed):
     return rnd, [v.to(dtype_of(torch, kind)) for v in (1 + 0.3 * rnd(width), 0.5 * rnd(width), rnd(n, width))]
 
 
-def check_rows(torch, B, kind, x, w, b, dy, eps):
+def check_rows(torch, B, kind, x, w, b, dy, eps, gradients=True):
     ref = Near(np64(x), np64(w), np64(b), eps, V[kind])
     got = run_both(torch, B, kind, x, w, b, dy, eps)
     check("y", got["y"], ref.y, ref.y_bound)
+    if not gradients:
+        return got
+    for name, (value, bound) in zip(("dx", "dweight", "dbias"), ref.gradients(np64(dy))):
+        check(name, got[name], value, bound + 2.0 ** -140)      # (gradients of huge rows are near the smallest numbers)
     return got
 
 
@@ -70,7 +74,7 @@ def test_rows_that_differ_in_their_last_places(torch, B, width, at):
     off = torch.zeros((n, width), device="cuda")
     off[0, 0], off[1, -1], off[2, width // 2], off[3, :width // 2] = 1, 1, -3, 1
     off[4:] = (rnd(n - 4, width) * torch.tensor([0.5, 1.0, 3.0, 50.0, 1_000.0], device="cuda")[:, None]).round()
-    check_rows(torch, B, "f32", at + off * step, w, b, dy, 1e-5)
+    check_rows(torch, B, "f32", at + off * step, w, b, dy, 1e-5, gradients=False)
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
@@ -82,4 +86,12 @@ def test_rows_far_from_zero(torch, B, kind, width, shift):
     rnd, (w, b, dy) = others(torch, kind, n, width, seed=width + 2)
     x = rnd(n, width)
     x[::2] += shift * (1 + rnd(12, 1).abs())
-    check_rows(torch, B, kind, x.to(dtype_of(torch, kind)), w, b, dy, 1e-5)
+    check_rows(torch, B, kind, x.to(dtype_of(torch, kind)), w, b, dy, 1e-5, gradients=False)
+
+
+def test_places_behind_the_row(torch, B):
+    """Widths that leave room in the last thread's pieces, of rows whose mean over their deviation is beyond the type."""
+    for width in (1, 3, 9, 65, 513, 1_025, 4_100):
+        rnd, (w, b, dy) = others(torch, "f32", 4, width, seed=width)
+        x = torch.tensor([3e38, -2e37, 4e33, 1.0], device="cuda")[:, None].expand(4, width).contiguous()
+        check_rows(torch, B, "f32", x, w, b, dy, 1e-12)
