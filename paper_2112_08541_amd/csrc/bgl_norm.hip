@@ -20,7 +20,7 @@ constexpr int kValues = 16;          // of a row a thread holds
 constexpr int64_t kMostThreads = (int64_t)1 << 31;     // of a launch, which has room for 2^32 - 1
 constexpr int kMaxParts = 512;       // workgroups of a backward call that sums weight gradients, so rows of its partial sums
 constexpr float kFar = 0x1p-80f;     // scales rows whose squares leave fp32's range
-constexpr float kAway = 16.0f;       // deviations from zero that a row's mean has at most for places behind the row to be left as they come
+constexpr float kAway = 16.0f;       // deviations from zero that a row's mean has at most to be used as it is kept: h is off by 2^-24 of these
 
 template <class T>
 struct NormArgs {
@@ -227,11 +227,22 @@ __global__ void __launch_bounds__(norm_threads<TEAM>()) k_norm_backward(NormArgs
             p.load(a.x + row * a.x_stride, h);
             mean = a.saved[2 * row], r = a.saved[2 * row + 1];
         }
-        // where the mean is far from zero beside the spread, places behind the row could be beyond the type
-        if (!(fabsf(mean) * r <= kAway)) {
+        // what the mean's rounding left, in rows so far from zero that it counts beside their spread; there, places behind the row could be beyond the type, too
+        const bool away = !(fabsf(mean) * r <= kAway);
+        bool any = away;
+        if constexpr (TEAM > 64 && TEAMS > 1)
+            for (int64_t other = first; other < first + TEAMS && other < a.n; ++other) any |= !(fabsf(a.saved[2 * other]) * a.saved[2 * other + 1] <= kAway);
+        if (any) {
+            float rest = 0.0f, unused = 0.0f;
 #pragma unroll
-            for (int i = 0; i < VALUES; ++i) h[i] = p.has(i) ? h[i] - mean : 0.0f;
-            mean = 0.0f;
+            for (int i = 0; i < VALUES; ++i) rest += away && p.has(i) ? h[i] - mean : 0.0f;
+            team_sums<TEAM>(rest, unused, lds, turn);
+            rest *= share;
+            if (away) {
+#pragma unroll
+                for (int i = 0; i < VALUES; ++i) h[i] = p.has(i) ? (h[i] - mean) - rest : 0.0f;
+                mean = 0.0f;
+            }
         }
         if (live) {
 #pragma unroll
