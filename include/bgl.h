@@ -882,8 +882,8 @@ int bgl_layer_norm_backward(const bgl_layer_norm_t *norm, int64_t n, const void 
  *   label_loss, teacher_loss  device, n floats each, or null
  *   saved             device, n x (3 + top) floats (n x 2 without a teacher, top = 0) that the backward call needs, or null
  *   workspace         device, 256-byte aligned, >= *forward_bytes of bgl_class_loss_workspace_bytes(loss, n, ...)
- * Sums are fp32.  Calls of many products (n >= 96, 128 classes, 2e9 products) take fp32 x and weight as two halves each, times a power of two of
- * the row: 22 bits, or 2^-40 of the row's largest value.  Outputs must not overlap inputs or each other.  n = 0 does nothing.
+ * Sums are fp32.  Calls of many products (n >= 96, 128 classes, 2e9 products) make fp32 scores and gradients from three bf16 parts of each value: 24 bits down to 2^-110.
+ * Outputs must not overlap inputs or each other.  n = 0 does nothing.
  * Errors: BGL_EINVAL (null or misaligned pointers, strides, sizes < 1, temperature outside [2^-10, 2^10], unknown
  * types, a loss without what it is of), BGL_EUNSUPPORTED (in_dim > BGL_MAX_DIM, classes > BGL_MAX_CLASSES, top > BGL_MAX_TOP),
  * BGL_ECAPACITY (workspace too small), BGL_EHIP.
@@ -917,7 +917,7 @@ int bgl_class_loss_forward(const bgl_class_loss_t *loss, int64_t n, const void *
  * Gradients are written, not added to (n = 0: zeros); dx = 0 for rows without a label and a teacher, whose x is not read for dweight.
  * dz is made in pieces of at most 2^25 values, 2^27 + 2^23 in calls of many products.  It is not rounded to the type: in fp32 it keeps 24 bits, in bf16 16, or in calls of many
  * products 11, fewer where it is below 2^-28 of |scale| + |teacher_scale| t (none below 2^-39); x and weight are halves there, exact down to 2^-32
- * of their largest finite value, and infinities in them may give NaN.  fp32 calls of many products make theirs from three bf16 parts of each value, 24 bits down to 2^-110.
+ * of their largest finite value, and infinities in them may give NaN.
  * The order of the sums is fixed by n and the sizes: repeated calls give the same bits.
  * Errors: as bgl_class_loss_forward.
  */

@@ -15,7 +15,7 @@
 //   k_class_zero              backward: the gradients of no rows
 // and for large calls, whose operands are laid out for bgl_stage.h first,
 //   k_class_scores_stage, k_class_products_stage
-//   k_class_split             fp32 operands as halves and as three bf16
+//   k_class_split             fp32 operands as three bf16
 //   k_class_lay               bf16 operands in whole steps, forward; k_class_largest, k_class_halves: as halves, backward
 #include "bgl_internal.h"
 #include "bgl_reduce.h"
@@ -798,15 +798,14 @@ __global__ void __launch_bounds__(256) k_class_zero(typename T::elem *p, int64_t
 }
 
 // ----------------------------------------------------------------- large calls: operands laid out for bgl_stage.h
-// Rows of D values as rows of planes, each `padded` wide, zeros behind D and in rows from `rows` to `all_rows`: of bf16 as they are, of fp32 as three planes of bf16
-// and (or) as two of halves times 2^-exponent, the row's own.
+// Rows of D values as rows of planes, each `padded` wide, zeros behind D and in rows from `rows` to `all_rows`: of fp32 three planes of bf16, of bf16 as they are or halves.
 template <class T>
 struct LayArgs {
     const typename T::elem *from;
     int64_t stride, rows, all_rows;
     int D, padded;
-    uint16_t *to, *halves;  // either may be null
-    int32_t *exponent;
+    uint16_t *to;
+    int32_t *exponent;  // of halves
     // backward, x: rows without a gradient become zeros, whatever they hold
     bool select;
     const int32_t *labels;
@@ -845,7 +844,7 @@ __global__ void __launch_bounds__(256) k_class_lay(LayArgs<BF16> a)
 // in [2^14, 2^15) and a bf16's eight bits fit a half's from 2^-32 of it on.  First the largest of kLayGroups shares of each, then every workgroup finds the exponent from these.
 constexpr int kLayGroups = 1024, kHalvesHead = 2 * kLayGroups * 4 + 256;
 struct HalvesArgs {
-    LayArgs<BF16> w, x;      // `halves` of both
+    LayArgs<BF16> w, x;
     uint32_t *largest;       // kLayGroups of w, kLayGroups of x
 };
 __device__ __forceinline__ uint32_t largest_of(const uint4 &v)
@@ -902,10 +901,10 @@ __global__ void __launch_bounds__(256) k_class_halves(HalvesArgs a, uint32_t w_g
         _Float16 h[8];
 #pragma unroll
         for (int j = 0; j < 4; ++j) h[2 * j] = (_Float16)(__uint_as_float(in[j] << 16) * scale), h[2 * j + 1] = (_Float16)(__uint_as_float(in[j] & 0xffff0000u) * scale);
-        *reinterpret_cast<uint4 *>(m.halves + row * m.padded + d) = __builtin_bit_cast(uint4, h);
+        *reinterpret_cast<uint4 *>(m.to + row * m.padded + d) = __builtin_bit_cast(uint4, h);
     });
 }
-// A wavefront for a row: its largest value first, then its planes.  50,001 x 256: 21 us forward (102 MB, 4.8 TB/s), 28 backward (179 MB, 6.4).
+// A wavefront for a row.  50,001 x 256: 22 us (128 MB, 5.9 TB/s).
 __global__ void __launch_bounds__(256) k_class_split(LayArgs<F32> a, int64_t row0)
 {
     const int64_t row = row0 + (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
@@ -913,69 +912,34 @@ __global__ void __launch_bounds__(256) k_class_split(LayArgs<F32> a, int64_t row
     if (row >= a.all_rows) return;
     const bool live = lives(a, row);
     const float *from = a.from + (live ? row : 0) * a.stride;
-    const auto read = [&](int d) {
+    for (int d = 4 * l; d < a.padded; d += 256) {
         f32x4 v = {};
         if (live && d < a.D) v = __builtin_bit_cast(f32x4, d + 4 <= a.D ? load_any<uint4>(from + d) : load_end<F32>(from + d, a.D - d, a.D));
-        return v;
-    };
-    int exponent = 0;
-    if (a.halves) {
-        float most = 0.0f;
-        for (int d = 4 * l; d < a.D; d += 256) {
-            const f32x4 v = read(d);
+        uint16_t e[3][4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (fabsf(v[j]) < INFINITY) most = fmaxf(most, fabsf(v[j]));
+        for (int j = 0; j < 4; ++j) {
+            uint16_t three[3];
+            split(v[j], three);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) e[p][j] = three[p];
         }
-        most = max_across<64>(most);
-        // the largest to [2^14, 2^15); not further than 2^115, for rows of the smallest numbers
-        if (most > 0.0f) exponent = ilogbf(most) - 14;
-        if (exponent < -115) exponent = -115;
-        if (l == 0) a.exponent[row] = exponent;
-    }
-    const float scale = ldexpf(1.0f, -exponent);
-    for (int d = 4 * l; d < a.padded; d += 256) {
-        const f32x4 v = read(d);
-        if (a.to) {
-            uint16_t e[3][4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint16_t three[3];
-                split(v[j], three);
-#pragma unroll
-                for (int p = 0; p < 3; ++p) e[p][j] = three[p];
-            }
-#pragma unroll
-            for (int p = 0; p < 3; ++p) *reinterpret_cast<uint2 *>(a.to + (row * 3 + p) * a.padded + d) = __builtin_bit_cast(uint2, e[p]);
-        }
-        if (a.halves) {
-            _Float16 h[2][4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float x = v[j] * scale;
-                h[0][j] = (_Float16)x;
-                h[1][j] = fabsf(x) < INFINITY ? (_Float16)(x - (float)h[0][j]) : (_Float16)0.0f;
-            }
-#pragma unroll
-            for (int p = 0; p < 2; ++p) *reinterpret_cast<uint2 *>(a.halves + (row * 2 + p) * a.padded + d) = __builtin_bit_cast(uint2, h[p]);
-        }
+        for (int p = 0; p < 3; ++p) *reinterpret_cast<uint2 *>(a.to + (row * 3 + p) * a.padded + d) = __builtin_bit_cast(uint2, e[p]);
     }
 }
 
 // k_class_scores from laid out operands: 192 classes x 128 rows, the largest tile of which two workgroups fit a CU: one's exponentials beside the other's products (a training
 // call of 4,096 x 512 x 65,536 bf16 took 1,278 us with 128 x 128, 1,227 so).  4,096 x 512 x 65,536 bf16: 306 us, 900 TFLOP/s with the exponentials (a plain library product of
-// 4,096 x 512 x 16,384 makes 831); backward 175 us for half of the classes, 785 TFLOP/s and 268 MB of dz.  1,024 x 256 x 50,001 f32: 90 us, 870 TFLOP/s of its three products of
-// halves; backward 147, with 307 MB of dz.
+// 4,096 x 512 x 16,384 makes 831); backward 175 us for half of the classes, 785 TFLOP/s and 268 MB of dz.  1,024 x 256 x 50,001 f32: 179 us, 880 TFLOP/s of its six
+// products of bf16; backward 233, with 307 MB of dz.  (From two halves of a value scaled by its row's largest, three products, these took 103 and 162: 22 bits, and what was
+// far below the row's largest lost all of them, so that a large column with small weights beside it made other columns' products wrong.)
 template <class T>
 struct StageScoreArgs {
     ScoreArgs<T> s;
-    const char *x, *w;           // of the call's first row, of class 0: bf16, or two planes of halves
+    const char *x, *w;           // of the call's first row, of class 0: three planes of bf16, or bf16 or halves
     int64_t x_bytes, w_bytes;    // rows
     uint32_t plane;              // bytes
-    const int32_t *x_exponent, *w_exponent;  // of halves: of every row and class (fp32), of all (bf16)
-    // what the products of the backward call read (bf16: the same; fp32: three planes of bf16)
-    const char *x_back, *w_back;
-    int64_t x_back_bytes, w_back_bytes;
+    const int32_t *x_exponent, *w_exponent;  // of halves
     // forward, or null: the teacher's classes, n x top, whose scores go to z_top
     const int32_t *top_class;
     float *z_top;
@@ -989,7 +953,7 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
     using A = stage::Kc<C::BA, kPad>;
     using B = stage::Kc<C::BB, kPad>;
     constexpr int PLANES = T::PER == 1 ? 3 : 1;  // of dz
-    constexpr stage::Kind READ = T::PER == 1 ? stage::TWO_HALVES : DZ ? stage::ONE_HALF : stage::ONE_BF16;
+    constexpr stage::Kind READ = T::PER == 1 ? stage::THREE_BF16 : DZ ? stage::ONE_HALF : stage::ONE_BF16;
     __shared__ __attribute__((aligned(1024))) char lds[stage::lds_bytes<A, B>()];
     const ScoreArgs<T> &a = q.s;
     int64_t ct, rt;
@@ -1005,11 +969,7 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
     // what the tile's classes and rows have of their own: a value for each thread, on its way during the products
     static_assert(C::BA <= stage::kThreads && C::BB <= stage::kThreads, "");
     float my_bias = 0.0f, my_most = INFINITY, my_sum = INFINITY, my_sum_t = INFINITY;  // (+inf: everything is 2^-inf of it, nothing has a share)
-    int my_label = -1, my_class = 0, my_row = 0;  // (the last two: exponents)
-    if (READ == stage::TWO_HALVES) {
-        if (threadIdx.x < C::BA) my_class = q.w_exponent[c0 + (int)threadIdx.x < last ? c0 + (int)threadIdx.x : last];
-        if (threadIdx.x < C::BB && r0 + threadIdx.x < a.rows) my_row = q.x_exponent[a.row0 + r0 + threadIdx.x];
-    }
+    int my_label = -1;
     if (a.bias && threadIdx.x < C::BA) my_bias = T::get(a.bias[c0 + (int)threadIdx.x < last ? c0 + (int)threadIdx.x : last]);
     if (threadIdx.x < C::BB && r0 + threadIdx.x < a.rows) {
         const int64_t row = a.row0 + r0 + threadIdx.x;
@@ -1027,7 +987,7 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
     if (my_sum == INFINITY && my_sum_t == INFINITY) my_most = INFINITY;  // (whatever such a row holds)
     struct Own {
         float bias[C::BA], base[C::BB], base_t[C::BB], share[C::BB], share_t[C::BB];
-        int label[C::BB], classes[C::BA], rows[C::BB];
+        int label[C::BB];
     };
     struct Meet {
         float own[C::BB], part[2][2][C::BB];  // the label's score; largest value and sum of both halves of the classes
@@ -1035,9 +995,8 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
     static_assert(sizeof(Own) + sizeof(Meet) <= sizeof(lds), "");
     Own &own = *reinterpret_cast<Own *>(lds);
     Meet &meet = *reinterpret_cast<Meet *>(lds + sizeof(Own));
-    if (threadIdx.x < C::BA) own.bias[threadIdx.x] = my_bias, own.classes[threadIdx.x] = my_class;
+    if (threadIdx.x < C::BA) own.bias[threadIdx.x] = my_bias;
     if (threadIdx.x < C::BB) {
-        own.rows[threadIdx.x] = my_row;
         own.label[threadIdx.x] = my_label;
         if constexpr (DZ) {
             own.base[threadIdx.x] = base_of(my_most, a.k), own.share[threadIdx.x] = 1.0f / my_sum;
@@ -1050,17 +1009,13 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
 #pragma unroll
     for (int i = 0; i < C::FA; ++i) {
         const f32x4 b = *reinterpret_cast<const f32x4 *>(own.bias + in_tile + 16 * i);
-        const stage::i32x4 up = *reinterpret_cast<const stage::i32x4 *>(own.classes + in_tile + 16 * i);
 #pragma unroll
-        for (int t = 0; t < C::FB; ++t) {
-            const int row_up = READ == stage::TWO_HALVES ? own.rows[C::b_off() + 16 * t + (l & 15)] : 0;
+        for (int t = 0; t < C::FB; ++t)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if constexpr (READ == stage::TWO_HALVES) acc[i][t][j] = ldexpf(acc[i][t][j], up[j] + row_up);
                 if constexpr (READ == stage::ONE_HALF) acc[i][t][j] = fmaf(acc[i][t][j], all_up, b[j]);
                 else acc[i][t][j] += b[j];
             }
-        }
     }
     if (c0 + C::BA > a.classes) {
 #pragma unroll
@@ -1239,7 +1194,7 @@ constexpr int kSummers = 4;
 template <stage::Kind KIND>
 __device__ __forceinline__ float sum_of(const uint4 &v, float s)
 {
-    if constexpr (stage::Pairs<KIND>::HALF) {
+    if constexpr (KIND == stage::ONE_HALF) {
         typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
         const f16x2 ones = {(_Float16)1.0f, (_Float16)1.0f};
         const uint32_t d[4] = {v.x, v.y, v.z, v.w};
@@ -1450,8 +1405,7 @@ Plan plan_of(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
     if (s.large) {
         p.padded = (int)round_up(l->in_dim, kPad);
         const auto bytes = [&](int64_t rows, bool back) {  // as stage_args lays them
-            if (l->dtype == BGL_BF16) return round_up((size_t)rows * p.padded * 2, 256) + (back ? kHalvesHead : 0);
-            return round_up((size_t)rows * p.padded * 4, 256) + round_up((size_t)rows * 4, 256) + (back ? round_up((size_t)rows * p.padded * 6, 256) : 0);
+            return round_up((size_t)rows * p.padded * 2 * s.planes, 256) + (back && l->dtype == BGL_BF16 ? kHalvesHead : 0);
         };
         const int64_t rows = round_up(n, 32);
         p.back_x_bytes = bytes(rows, true), p.back_w_bytes = bytes(l->classes, true);
@@ -1613,34 +1567,31 @@ bool goes_large(const Call &c, bool forward)
 StageScoreArgs<F32> stage_args(const Call &c, const Plan &p, const ScoreArgs<F32> &s, char *x, char *w, const RowArgs<F32> *select)
 {
     StageScoreArgs<F32> q{};
-    q.s = s, q.plane = p.padded * 2;
-    q.x_bytes = q.w_bytes = (int64_t)p.padded * 4, q.x_back_bytes = q.w_back_bytes = (int64_t)p.padded * 6;
-    // halves, their exponents, planes of bf16
-    const auto lay = [&](LayArgs<F32> a, char *to, const char *&read, const int32_t *&exponent, const char *&back) {
-        char *exponents = to + round_up((size_t)a.all_rows * p.padded * 4, 256), *planes = exponents + round_up((size_t)a.all_rows * 4, 256);
-        a.halves = (uint16_t *)to, a.exponent = (int32_t *)exponents, a.to = select ? (uint16_t *)planes : nullptr;
-        read = to, exponent = a.exponent, back = planes;
+    q.s = s, q.plane = p.padded * 2, q.x_bytes = q.w_bytes = (int64_t)p.padded * 6;
+    const auto lay = [&](LayArgs<F32> a, char *to) {
+        a.to = (uint16_t *)to;
         const int64_t most = kMostThreads / 64;
         for (int64_t row0 = 0; row0 < a.all_rows; row0 += most) k_class_split<<<dim3((unsigned)ceil_div(a.all_rows - row0 < most ? a.all_rows - row0 : most, 4)), dim3(256), 0, c.stream>>>(a, row0);
+        return to;
     };
-    lay(lay_args<F32>(s.w, s.D, s.classes, s.classes, s.D, p.padded, nullptr), w, q.w, q.w_exponent, q.w_back);
-    lay(lay_args<F32>(s.x, s.x_stride, c.n, round_up(c.n, 32), s.D, p.padded, select), x, q.x, q.x_exponent, q.x_back);
+    q.w = lay(lay_args<F32>(s.w, s.D, s.classes, s.classes, s.D, p.padded, nullptr), w);
+    q.x = lay(lay_args<F32>(s.x, s.x_stride, c.n, round_up(c.n, 32), s.D, p.padded, select), x);
     return q;
 }
 StageScoreArgs<BF16> stage_args(const Call &c, const Plan &p, const ScoreArgs<BF16> &s, char *x, char *w, const RowArgs<BF16> *select)
 {
     StageScoreArgs<BF16> q{};
     q.s = s, q.plane = p.padded * 2;
-    q.x_bytes = q.w_bytes = q.x_back_bytes = q.w_back_bytes = (int64_t)p.padded * 2;
+    q.x_bytes = q.w_bytes = (int64_t)p.padded * 2;
     LayArgs<BF16> lw = lay_args<BF16>(s.w, s.D, s.classes, s.classes, s.D, p.padded, nullptr), lx = lay_args<BF16>(s.x, s.x_stride, c.n, round_up(c.n, 32), s.D, p.padded, select);
     if (select) {
         // the largest of shares (at w's), the exponent, the values
         HalvesArgs a{lw, lx, (uint32_t *)w};
-        const auto place = [&](LayArgs<BF16> &m, char *to, const char *&read, const char *&back, const int32_t *&exponent) {
-            m.exponent = (int32_t *)(to + 2 * kLayGroups * 4), m.halves = (uint16_t *)(to + kHalvesHead);
-            read = back = to + kHalvesHead, exponent = m.exponent;
+        const auto place = [&](LayArgs<BF16> &m, char *to, const char *&read, const int32_t *&exponent) {
+            m.exponent = (int32_t *)(to + 2 * kLayGroups * 4), m.to = (uint16_t *)(to + kHalvesHead);
+            read = to + kHalvesHead, exponent = m.exponent;
         };
-        place(a.w, w, q.w, q.w_back, q.w_exponent), place(a.x, x, q.x, q.x_back, q.x_exponent);
+        place(a.w, w, q.w, q.w_exponent), place(a.x, x, q.x, q.x_exponent);
         const auto groups = [&](const LayArgs<BF16> &m) {
             const int64_t all = ceil_div(m.all_rows * (p.padded / 8), 256);
             return (uint32_t)(all < 8 * kCus ? all : 8 * kCus);
@@ -1831,8 +1782,8 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
             if (h.large) {
                 StagePieceArgs<T> x{}, y{};
                 fill_dx(x), fill_dw(y);
-                x.b = q.w_back + class0 * q.w_back_bytes, x.b_bytes = q.w_back_bytes, x.exponent = w_up;
-                y.b = q.x_back + row0 * q.x_back_bytes, y.b_bytes = q.x_back_bytes, y.exponent = x_up;
+                x.b = q.w + class0 * q.w_bytes, x.b_bytes = q.w_bytes, x.exponent = w_up;
+                y.b = q.x + row0 * q.x_bytes, y.b_bytes = q.x_bytes, y.exponent = x_up;
                 y.K = round_up(rows, 32);  // (rows of zeros in both)
                 for (StagePieceArgs<T> *a : {&x, &y}) a->a = (const char *)dz, a->a_rows = (int)round_up(rows, StageCut::BB), a->a_stride = (int)p.dz_stride, a->b_width = p.padded, a->b_plane = q.plane, a->slot_width = p.slot_width, a->undo = undo;
                 launch_products<T>(dweight ? &y : nullptr, dx ? &x : nullptr, c.stream);

@@ -10,9 +10,6 @@
 // rows read 128 bytes at a time.  So rows that are given are read in stages of 64, and what is written for these products alone lies in blocks of
 // 16 rows x 32 values (1,024 bytes that one load of a wavefront takes, whichever index is summed).
 //
-// Where a row's values differ little beside its largest, as rows of features and weights do, two halves of the value scaled by the row's own power of two are
-// as good and half the products: 22 bits of the value as far as it is above 2^-18 of the row's largest, 2^-40 of that largest below.
-//
 // A fp32 value is three bf16 (its first 8 bits, the next 8 of what is left, the last): all 24 bits as long as the value is above 2^-110.  A product of two is
 // the six products of parts that count, what is left out is below 2^-23 of it.  The parts lie one after the other ("planes"): of a row, or of a block.
 //
@@ -240,18 +237,17 @@ constexpr int stages() { return 81920 / (A::BYTES + B::BYTES); }
 template <class A, class B>
 constexpr int lds_bytes() { return stages<A, B>() * (A::BYTES + B::BYTES); }
 
-// What operands are made of: a bf16; two halves of a value; three bf16 of a value; a half.  A, B: the planes of product p, hexadecimal digit p.
-enum Kind { ONE_BF16, TWO_HALVES, THREE_BF16, ONE_HALF };
+// What operands are made of: a bf16; three bf16 of a value; a half.  A, B: the planes of product p, hexadecimal digit p.
+enum Kind { ONE_BF16, THREE_BF16, ONE_HALF };
 template <Kind KIND>
 struct Pairs {
-    static constexpr bool HALF = KIND == TWO_HALVES || KIND == ONE_HALF;
-    static constexpr int PLANES = KIND == TWO_HALVES ? 2 : KIND == THREE_BF16 ? 3 : 1, COUNT = PLANES == 1 ? 1 : PLANES == 2 ? 3 : 6;
-    static constexpr uint32_t A = PLANES == 2 ? 0x100 : 0x010210, B = PLANES == 2 ? 0x010 : 0x211000;
+    static constexpr int PLANES = KIND == THREE_BF16 ? 3 : 1, COUNT = PLANES == 1 ? 1 : 6;
+    static constexpr uint32_t A = 0x010210, B = 0x211000;
 };
 template <Kind KIND>
 __device__ __forceinline__ f32x4 mma(const bf16x8 &a, const bf16x8 &b, const f32x4 &c)
 {
-    if constexpr (Pairs<KIND>::HALF) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    if constexpr (KIND == ONE_HALF) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
