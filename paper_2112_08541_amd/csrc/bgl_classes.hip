@@ -43,9 +43,20 @@ constexpr double kLargeProducts = 2e9;                 // of a call that is laid
                                                        // 1,316 x 503 x 3,640 45 + 167 and 77 + 199; bf16 15 + 42 and 11 + 40, 29 + 66 and 24 + 83
 
 // Exponentials are powers of two: exp(k v) / 2^base with k = log2(e) or that over the temperature, as 2^(k v - base) with one rounding.  A sum of them is taken to
-// the base of its largest value, base(most) = k most, rounded: sums of two bases meet exactly, as the bases' difference has no rounding to speak of.
+// the base of its largest value, k most, rounded: what rounding leaves of it is the same for all of a sum, and sums of two bases meet exactly, as the bases' difference has no
+// rounding to speak of.  From `far` (2^24 / k) on it leaves more than 1, in the end more than a power's range: of such rows the largest value itself is taken from the others
+// first (`shift`), which is exact for those near it, and the base is 0.
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
-__device__ __forceinline__ float base_of(float most, float k) { return most == -INFINITY ? 0.0f : most * k; }  // (nothing there: the sum is 0)
+struct Base {
+    float shift, base, base_t;  // at the temperature: base_t
+};
+template <class A>
+__device__ __forceinline__ Base base_of(const A &a, float most)
+{
+    if (most == -INFINITY) return Base{0.0f, 0.0f, 0.0f};  // (nothing there: the sum is 0)
+    if (fabsf(most) < a.far) return Base{0.0f, most * a.k, most * a.k_t};
+    return Base{most, 0.0f, 0.0f};
+}
 __device__ __forceinline__ float power_to(float v, float k, float base) { return __builtin_amdgcn_exp2f(fmaf(v, k, -base)); }
 __device__ __forceinline__ float max3(float a, float b, float c)  // (of fmaxf the compiler makes two instructions more, for signalling NaN)
 {
@@ -61,10 +72,22 @@ __device__ __forceinline__ void keep(float *to, int width, float most, float sum
     if (width > 2) to[2] = sum_t;
 }
 // The logarithm of the sum less the score, both to the sum's base (what they have in common goes before they meet), in natural units.
-__device__ __forceinline__ float loss_of(float log_sum, float score, float k, float base) { return kLn2 * (log_sum - fmaf(score, k, -base)); }
+template <class A>
+__device__ __forceinline__ float loss_of(const A &a, float log_sum, float score, const Base &b) { return kLn2 * (log_sum - fmaf(score - b.shift, a.k, -b.base)); }
 // What a sum to the base of `most` is to be multiplied by to be to the base `to`, that of no smaller a value.  A sum of nothing has no base (base_of's 0 for it may be far
-// above `to`: 0 times 2^(0 - to) was NaN for rows whose scores are all below -88): 0, which leaves a NaN one.
-__device__ __forceinline__ float rebase(float most, float k, float to) { return most == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(base_of(most, k) - to); }
+// above `to`: 0 times 2^(0 - to) was NaN for rows whose scores are all below -88): 0, which leaves a NaN one.  rebase_t: of sums at the temperature.
+template <class A>
+__device__ __forceinline__ float rebase(const A &a, float most, const Base &to)
+{
+    const Base from = base_of(a, most);
+    return most == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(fmaf(from.shift - to.shift, a.k, from.base - to.base));
+}
+template <class A>
+__device__ __forceinline__ float rebase_t(const A &a, float most, const Base &to)
+{
+    const Base from = base_of(a, most);
+    return most == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(fmaf(from.shift - to.shift, a.k_t, from.base_t - to.base_t));
+}
 
 // The other lanes with the same lane % 16.
 template <class F>
@@ -120,7 +143,7 @@ struct ScoreArgs {
     int all_classes;
     bool by_rows;             // tiles of one block of rows, not of classes, follow one another on an XCD
     int class_tiles, D;
-    float k, k_t;             // log2(e), and over the temperature
+    float k, k_t, far;        // log2(e), and over the temperature; see base_of()
     // forward: {largest, sum} of part t of the classes and row r at part[t * rows + r], the sum at the temperature at part_t[t * rows + r]
     float2 *part;
     float *part_t, *label_score;
@@ -136,6 +159,16 @@ struct ScoreArgs {
     int dz_stride;
     int32_t *listed;          // null, or the row's number among this launch's for rows with a gradient, else -1
 };
+
+// The row's values of a lane's fragments less the largest, where scores are far from 0.
+template <class C>
+__device__ __forceinline__ void take_shift(f32x4 (&acc)[C::FA][C::FB], int t, float shift)
+{
+#pragma unroll
+    for (int i = 0; i < C::FA; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][t][j] -= shift;
+}
 
 // One tile of classes x rows: a lane holds, of one row, 4 neighbouring classes of every 16, so that a row's maximum and sum meet in 4 lanes.  One row of 512 and 65,536
 // classes, bf16: 13.1 us, 5.1 TB/s of the weight.  1,024 x 128 x 50 f32: 5.1 us.
@@ -196,26 +229,33 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_scores(ScoreArgs<T> a)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) most = fmaxf(most, acc[i][t][j]);
             most = down_column(most, [](float p, float q) { return fmaxf(p, q); });
-            const float base = base_of(most, a.k), base_t = base_of(most, a.k_t);
+            const Base to = base_of(a, most);
+#pragma unroll
+            for (int i = 0; i < C::FA; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (first + 16 * i + j == label && live) {
+                        if (a.whole) own_score[in_tile] = acc[i][t][j];
+                        else a.label_score[row] = acc[i][t][j];
+                    }
+            if (__any(to.shift != 0.0f)) take_shift<C>(acc, t, to.shift);
 #pragma unroll
             for (int i = 0; i < C::FA; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float v = acc[i][t][j];
-                    if (first + 16 * i + j == label && live) {
-                        if (a.whole) own_score[in_tile] = v;
-                        else a.label_score[row] = v;
-                    }
-                    sum += power_to(v, a.k, base);
-                    if (a.two) sum_t += power_to(v, a.k_t, base_t);
+                    sum += power_to(v, a.k, to.base);
+                    if (a.two) sum_t += power_to(v, a.k_t, to.base_t);
                 }
             sum = down_column(sum, [](float p, float q) { return p + q; });
             if (a.two) sum_t = down_column(sum_t, [](float p, float q) { return p + q; });
-            float *to = meet + (C::a_off() / C::FA / 16 * C::BB + in_tile) * 3;
-            if (l < 16) to[0] = most, to[1] = sum, to[2] = sum_t;
+            float *at = meet + (C::a_off() / C::FA / 16 * C::BB + in_tile) * 3;
+            if (l < 16) at[0] = most, at[1] = sum, at[2] = sum_t;
         } else {
             const float *kept = a.saved + row * a.saved_width;
-            const float sum_t = a.teacher_scale != 0.0f ? kept[2] : INFINITY, base = base_of(kept[0], a.k), base_t = base_of(kept[0], a.k_t);
+            const float sum_t = a.teacher_scale != 0.0f ? kept[2] : INFINITY;
+            const Base to = base_of(a, kept[0]);
+            if (__any(to.shift != 0.0f)) take_shift<C>(acc, t, to.shift);
             const float s = label >= 0 ? a.scale : 0.0f, st = sum_t != INFINITY ? a.teacher_scale : 0.0f;
             const float share = 1.0f / kept[1], share_t = st / sum_t;
             // (the products that sum over rows leave the others out, whatever x holds there)
@@ -227,8 +267,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_scores(ScoreArgs<T> a)
                 for (int j = 0; j < 4; ++j) {
                     const float v = acc[i][t][j];
                     float d = 0.0f;
-                    if (s != 0.0f) d = s * (power_to(v, a.k, base) * share - (first + 16 * i + j == label ? 1.0f : 0.0f));
-                    if (st != 0.0f) d = fmaf(share_t, power_to(v, a.k_t, base_t), d);
+                    if (s != 0.0f) d = s * (power_to(v, a.k, to.base) * share - (first + 16 * i + j == label ? 1.0f : 0.0f));
+                    if (st != 0.0f) d = fmaf(share_t, power_to(v, a.k_t, to.base_t), d);
                     e[j] = T::put(d);
                     rest[j] = T::put(d - T::get(e[j]));
                 }
@@ -249,17 +289,18 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_scores(ScoreArgs<T> a)
             float most = -INFINITY, sum = 0.0f, sum_t = 0.0f;
 #pragma unroll
             for (int w = 0; w < WA; ++w) most = fmaxf(most, meet[(w * C::BB + in_tile) * 3]);
+            const Base to = base_of(a, most);
 #pragma unroll
             for (int w = 0; w < WA; ++w) {
                 const float *from = meet + (w * C::BB + in_tile) * 3;
-                sum += from[1] * rebase(from[0], a.k, base_of(most, a.k));
-                if (a.two) sum_t += from[2] * rebase(from[0], a.k_t, base_of(most, a.k_t));
+                sum += from[1] * rebase(a, from[0], to);
+                if (a.two) sum_t += from[2] * rebase_t(a, from[0], to);
             }
             if (a.whole) {
                 const int64_t row = a.row0 + r0 + in_tile;
-                const float base = base_of(most, a.k), log_sum = log2f(sum);
+                const float log_sum = log2f(sum);
                 const bool has = (uint32_t)a.labels[row] < (uint32_t)a.all_classes;
-                if (a.loss) a.loss[row] = has ? loss_of(log_sum, own_score[in_tile], a.k, base) : 0.0f;
+                if (a.loss) a.loss[row] = has ? loss_of(a, log_sum, own_score[in_tile], to) : 0.0f;
                 if (a.kept) keep(a.kept + row * a.saved_width, a.saved_width, most, sum, INFINITY);
                 continue;
             }
@@ -276,7 +317,7 @@ struct RowArgs {
     const float *top_score;
     int64_t x_stride, n, row0, rows;
     int D, classes, top, class_parts, saved_width;
-    float t, over_t, k, k_t, scale, teacher_scale;
+    float t, over_t, k, k_t, far, scale, teacher_scale;
     const float2 *part;
     const float *part_t, *label_score;
     float *loss, *teacher_loss;
@@ -389,9 +430,9 @@ __global__ void __launch_bounds__(kMergeRows *kMergeLanes) k_class_merge(RowArgs
     const int i = threadIdx.x % kMergeRows, l = threadIdx.x / kMergeRows;
     const int64_t row = (int64_t)blockIdx.x * kMergeRows + i, r = row < a.rows ? row : a.rows - 1;
     float most = -INFINITY, sum = 0.0f, sum_t = 0.0f;
-    const auto take = [&](float base, float base_t, float largest, float s, float t) {
-        sum += s * rebase(largest, a.k, base);
-        if (a.two) sum_t += t * rebase(largest, a.k_t, base_t);
+    const auto take = [&](const Base &to, float largest, float s, float t) {
+        sum += s * rebase(a, largest, to);
+        if (a.two) sum_t += t * rebase_t(a, largest, to);
     };
     for (int first = l; first < a.class_parts; first += kMergeLanes * AHEAD) {
         float2 from[AHEAD];
@@ -405,11 +446,11 @@ __global__ void __launch_bounds__(kMergeRows *kMergeLanes) k_class_merge(RowArgs
         }
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) m = fmaxf(m, from[u].x);
-        const float base = base_of(m, a.k), base_t = base_of(m, a.k_t);
-        sum *= rebase(most, a.k, base);
-        sum_t *= rebase(most, a.k_t, base_t);
+        const Base to = base_of(a, m);
+        sum *= rebase(a, most, to);
+        sum_t *= rebase_t(a, most, to);
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) take(base, base_t, from[u].x, from[u].y, at_t[u]);
+        for (int u = 0; u < AHEAD; ++u) take(to, from[u].x, from[u].y, at_t[u]);
         most = m;
     }
     largest[l][i] = most, sums[l][i] = sum, sums_t[l][i] = sum_t;
@@ -418,9 +459,9 @@ __global__ void __launch_bounds__(kMergeRows *kMergeLanes) k_class_merge(RowArgs
     most = -INFINITY, sum = sum_t = 0.0f;
 #pragma unroll
     for (int u = 0; u < kMergeLanes; ++u) most = fmaxf(most, largest[u][i]);
-    const float base = base_of(most, a.k), base_t = base_of(most, a.k_t);
+    const Base to = base_of(a, most);
 #pragma unroll
-    for (int u = 0; u < kMergeLanes; ++u) take(base, base_t, largest[u][i], sums[u][i], sums_t[u][i]);
+    for (int u = 0; u < kMergeLanes; ++u) take(to, largest[u][i], sums[u][i], sums_t[u][i]);
     part[row] = float2{most, sum};
     if (a.two) part_t[row] = sum_t;
 }
@@ -462,24 +503,25 @@ __global__ void __launch_bounds__(256) k_class_finish(RowArgs<T> a)
         }
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) m = fmaxf(m, from[u].x);
-        const float base = base_of(m, a.k), base_t = base_of(m, a.k_t);
-        sum *= rebase(most, a.k, base);
-        sum_t *= rebase(most, a.k_t, base_t);
+        const Base to = base_of(a, m);
+        sum *= rebase(a, most, to);
+        sum_t *= rebase_t(a, most, to);
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-            sum += from[u].y * rebase(from[u].x, a.k, base);
-            sum_t += at_t[u] * rebase(from[u].x, a.k_t, base_t);
+            sum += from[u].y * rebase(a, from[u].x, to);
+            sum_t += at_t[u] * rebase_t(a, from[u].x, to);
         }
         most = m;
     }
-    const float m = max_across<LANES>(most), base = base_of(m, a.k), base_t = a.two ? base_of(m, a.k_t) : base;
-    sum = sum_across<LANES>(sum * rebase(most, a.k, base));
-    sum_t = a.two ? sum_across<LANES>(sum_t * rebase(most, a.k_t, base_t)) : sum;
+    const float m = max_across<LANES>(most);
+    const Base to = base_of(a, m);
+    sum = sum_across<LANES>(sum * rebase(a, most, to));
+    sum_t = a.two ? sum_across<LANES>(sum_t * rebase_t(a, most, to)) : sum;  // (if not, k and k_t are the same)
     const float log_sum = log2f(sum), log_sum_t = log2f(sum_t);
     if (a.labels) {
         const int label = a.labels[row];
         const bool has = (uint32_t)label < (uint32_t)a.classes;
-        if (l == 0 && a.loss) a.loss[row] = has ? loss_of(log_sum, a.label_score[row], a.k, base) : 0.0f;
+        if (l == 0 && a.loss) a.loss[row] = has ? loss_of(a, log_sum, a.label_score[row], to) : 0.0f;
     }
     float kept_t = INFINITY;
     if (a.top_class) {
@@ -491,8 +533,8 @@ __global__ void __launch_bounds__(256) k_class_finish(RowArgs<T> a)
             for (int k = l; k < a.top; k += LANES)
                 if ((uint32_t)a.top_class[row * a.top + k] < (uint32_t)a.classes) {
                     const float v = a.top_score[row * a.top + k] * a.over_t - top_most;
-                    const float p = exp_of(v) / total;
-                    if (p != 0.0f) kl = fmaf(p, (v * kLog2e - log_total) + (log_sum_t - fmaf(TOP ? z_here[threadIdx.x / LANES][k] : a.z_top[row * a.z_stride + k], a.k_t, -base_t)), kl);
+                    const float p = exp_of(v) / total, z = TOP ? z_here[threadIdx.x / LANES][k] : a.z_top[row * a.z_stride + k];
+                    if (p != 0.0f) kl = fmaf(p, (v * kLog2e - log_total) + (log_sum_t - fmaf(z - to.shift, a.k_t, -to.base_t)), kl);
                 }
             kl = sum_across<LANES>(kl);
         }
@@ -513,7 +555,7 @@ __global__ void __launch_bounds__(256) k_class_fix(RowArgs<T> a)
     float most, total;
     if (!teacher_of<LANES>(a, row, most, total)) return;
     const float *kept = a.saved + row * a.saved_width;
-    const float base = base_of(kept[0], a.k), base_t = base_of(kept[0], a.k_t);
+    const Base to = base_of(a, kept[0]);
     int label = a.labels ? a.labels[row] : -1;
     if ((uint32_t)label >= (uint32_t)a.classes) label = -1;
     const int32_t *classes = a.top_class + row * a.top;
@@ -561,9 +603,9 @@ __global__ void __launch_bounds__(256) k_class_fix(RowArgs<T> a)
             d = fmaf(-a.teacher_scale, p, d);
         } else {
             // (there it has been rounded)
-            const float z = kept[3 + k];
-            if (label >= 0 && a.scale != 0.0f) d = a.scale * (power_to(z, a.k, base) / kept[1] - (c == label ? 1.0f : 0.0f));
-            d = fmaf(a.teacher_scale, power_to(z, a.k_t, base_t) / kept[2] - p, d);
+            const float z = kept[3 + k] - to.shift;
+            if (label >= 0 && a.scale != 0.0f) d = a.scale * (power_to(z, a.k, to.base) / kept[1] - (c == label ? 1.0f : 0.0f));
+            d = fmaf(a.teacher_scale, power_to(z, a.k_t, to.base_t) / kept[2] - p, d);
         }
         if (a.blocks) {
             uint16_t e[3];
@@ -986,7 +1028,7 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
     if ((uint32_t)my_label >= (uint32_t)a.all_classes) my_label = -1, my_sum = INFINITY;
     if (my_sum == INFINITY && my_sum_t == INFINITY) my_most = INFINITY;  // (whatever such a row holds)
     struct Own {
-        float bias[C::BA], base[C::BB], base_t[C::BB], share[C::BB], share_t[C::BB];
+        float bias[C::BA], shift[C::BB], base[C::BB], base_t[C::BB], share[C::BB], share_t[C::BB];
         int label[C::BB];
     };
     struct Meet {
@@ -999,8 +1041,9 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
     if (threadIdx.x < C::BB) {
         own.label[threadIdx.x] = my_label;
         if constexpr (DZ) {
-            own.base[threadIdx.x] = base_of(my_most, a.k), own.share[threadIdx.x] = 1.0f / my_sum;
-            own.base_t[threadIdx.x] = base_of(my_most, a.k_t), own.share_t[threadIdx.x] = a.teacher_scale / my_sum_t;
+            const Base to = my_most == INFINITY ? Base{0.0f, INFINITY, INFINITY} : base_of(a, my_most);
+            own.shift[threadIdx.x] = to.shift, own.base[threadIdx.x] = to.base, own.base_t[threadIdx.x] = to.base_t;
+            own.share[threadIdx.x] = 1.0f / my_sum, own.share_t[threadIdx.x] = a.teacher_scale / my_sum_t;
         }
     }
     __syncthreads();
@@ -1085,21 +1128,22 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
 #pragma unroll
             for (int i = 0; i < C::FA; ++i) most = max3(max3(most, acc[i][t][0], acc[i][t][1]), acc[i][t][2], acc[i][t][3]);
             most = down_column(most, [](float p, float q) { return fmaxf(p, q); });
-            const float base = base_of(most, a.k), base_t = base_of(most, a.k_t);
-#pragma unroll
-            for (int i = 0; i < C::FA; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sum += power_to(acc[i][t][j], a.k, base);
-            if (a.two) {
-#pragma unroll
-                for (int i = 0; i < C::FA; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) sum_t += power_to(acc[i][t][j], a.k_t, base_t);
-            }
+            const Base to = base_of(a, most);
             if (any) {
                 const float v = own_score(t);
                 if (mine && a.whole) meet.own[b] = v;
                 else if (mine && r < a.rows) a.label_score[a.row0 + r] = v;
+            }
+            if (__any(to.shift != 0.0f)) take_shift<C>(acc, t, to.shift);
+#pragma unroll
+            for (int i = 0; i < C::FA; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum += power_to(acc[i][t][j], a.k, to.base);
+            if (a.two) {
+#pragma unroll
+                for (int i = 0; i < C::FA; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) sum_t += power_to(acc[i][t][j], a.k_t, to.base_t);
             }
             sum = down_column(sum, [](float p, float q) { return p + q; });
             if (a.two) sum_t = down_column(sum_t, [](float p, float q) { return p + q; });
@@ -1112,7 +1156,8 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
                 if (a.two) a.part_t[at] = sum_t;
             }
         } else {
-            const float base = own.base[b], base_t = own.base_t[b], share = a.scale * own.share[b], share_t = own.share_t[b];
+            const float shift = own.shift[b], base = own.base[b], base_t = own.base_t[b], share = a.scale * own.share[b], share_t = own.share_t[b];
+            if (__any(shift != 0.0f)) take_shift<C>(acc, t, shift);
 #pragma unroll
             for (int i = 0; i < C::FA; ++i) {
                 float d[4];
@@ -1154,12 +1199,13 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
         const int b = threadIdx.x;
         if (b >= C::BB || r0 + b >= a.rows) return;
         const int64_t row = a.row0 + r0 + b;
-        const float most = fmaxf(meet.part[0][0][b], meet.part[0][1][b]), base = base_of(most, a.k);
+        const float most = fmaxf(meet.part[0][0][b], meet.part[0][1][b]);
+        const Base to = base_of(a, most);
         float sum = 0.0f;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) sum += meet.part[1][half][b] * rebase(meet.part[0][half][b], a.k, base);
+        for (int half = 0; half < 2; ++half) sum += meet.part[1][half][b] * rebase(a, meet.part[0][half][b], to);
         const float log_sum = log2f(sum);
-        if (a.loss) a.loss[row] = my_label >= 0 ? loss_of(log_sum, meet.own[b], a.k, base) : 0.0f;
+        if (a.loss) a.loss[row] = my_label >= 0 ? loss_of(a, log_sum, meet.own[b], to) : 0.0f;
         if (a.kept) keep(a.kept + row * a.saved_width, a.saved_width, most, sum, INFINITY);
     }
 }
@@ -1508,6 +1554,7 @@ struct Call {
     hipStream_t stream;
 };
 
+float far_of(const bgl_class_loss_t *l) { return 0x1p24f / kLog2e * (l->temperature < 1.0f ? l->temperature : 1.0f); }  // (of the loss alone: both calls go by it)
 int saved_width_of(const bgl_class_loss_t *l) { return l->top > 0 ? 3 + l->top : 2; }
 
 template <class T>
@@ -1518,7 +1565,7 @@ RowArgs<T> row_args(const Call &c)
     r.x = (const E *)c.x, r.w = (const E *)c.weight, r.bias = (const E *)c.bias, r.labels = c.labels, r.top_class = c.top_class, r.top_score = c.top_score;
     r.x_stride = c.x_stride, r.n = c.n, r.D = c.l->in_dim, r.classes = c.l->classes, r.top = c.l->top, r.saved_width = saved_width_of(c.l);
     r.t = c.l->temperature, r.over_t = 1.0f / c.l->temperature, r.k = kLog2e, r.k_t = (float)(1.4426950408889634 / c.l->temperature);
-    r.two = c.top_class && c.l->temperature != 1.0f;
+    r.far = far_of(c.l), r.two = c.top_class && c.l->temperature != 1.0f;
     return r;
 }
 template <class T>
@@ -1528,7 +1575,7 @@ ScoreArgs<T> score_args(const Call &c)
     ScoreArgs<T> s{};
     s.x = (const E *)c.x, s.w = (const E *)c.weight, s.bias = (const E *)c.bias, s.labels = c.labels, s.x_stride = c.x_stride, s.n = c.n;
     s.classes = s.all_classes = c.l->classes, s.D = c.l->in_dim, s.k = kLog2e, s.k_t = (float)(1.4426950408889634 / c.l->temperature), s.two = c.top_class && c.l->temperature != 1.0f;
-    s.saved_width = saved_width_of(c.l);
+    s.far = far_of(c.l), s.saved_width = saved_width_of(c.l);
     return s;
 }
 

@@ -70,3 +70,44 @@ def test_a_class_that_is_nan_is_not_lost(torch, B, C, at):
     w[at:] = float("nan")
     labels[:] = 0
     assert run(torch, B, "f32", x, w, b, labels, None, s=1.0)["loss"].isnan().all()
+
+
+HIGH = [2.0 ** 23, -2.0 ** 24, 2.0 ** 27, -2.0 ** 30, 2.0 ** 31, -2.0 ** 33, 2.0 ** 40, -2.0 ** 100]
+
+
+@pytest.mark.parametrize("t", [1.0, 1024.0, 2.0 ** -10])
+@pytest.mark.parametrize("kind,n,C", [(kind, n, C) for kind in ("f32", "bf16") for n, C in [(50, 3), (50, 40), (70, 300), (90, 1_300), (9_000, 12)]] + [("f32", 1_300, 1_300)])
+def test_scores_beyond_the_steps_of_their_exponents(torch, B, kind, n, C, t):
+    """Scores as large as 2^100, a few steps of 1 or of their last place apart, beside ordinary ones.  The weight is the identity, so that scores are x and dx is dz; every row's own
+    step makes its distribution anything from even to a single class.  Powers are right to 6 u and 2 u of their argument (which e^-a a <= 0.4 keeps below 1 u in q), sums of
+    them to u for each of C / 16 + 40 steps and 8 u for each of the parts' 8 scalings: q to 2 (6 + 64) + C / 8 + 80 = 220 + C / 8 u, and so is a loss beside 4 u of itself."""
+    u, dtype = 2.0 ** -24, torch.float32 if kind == "f32" else torch.bfloat16
+    g = torch.Generator(device="cuda").manual_seed(C + n)
+    high = torch.tensor(HIGH + [0.0], dtype=torch.float64, device="cuda")[torch.arange(n, device="cuda") % 9]
+    place = 2.0 ** ((high.abs() + 1).log2().floor() - (23 if kind == "f32" else 7))
+    step = torch.where(torch.arange(n, device="cuda") % 2 == 0, place.clamp(min=t / 2), place.clamp(min=1.0))
+    z = high[:, None] - torch.randint(0, 9, (n, C), generator=g, device="cuda") * step[:, None] * high.sign()[:, None].where(high[:, None] != 0, torch.ones_like(high)[:, None])
+    x = z.to(dtype)
+    z = x.double()
+    w = torch.eye(C, dtype=dtype, device="cuda")
+    labels = torch.randint(0, C, (n,), generator=g, device="cuda", dtype=torch.int32)
+    classes = torch.stack([torch.randperm(C, generator=g, device="cuda")[:3] for _ in range(n)]).int()
+    scores = torch.randint(-8, 8, (n, 3), generator=g, device="cuda") * (t / 4)
+    off = (220 + C / 8) * u
+    p = torch.zeros((n, C), dtype=torch.float64, device="cuda").scatter_(1, classes.long(), (scores.double() / t).softmax(1))
+    logq, logq_t = z.log_softmax(1), (z / t).log_softmax(1)
+    loss = -logq[torch.arange(n, device="cuda"), labels.long()]
+    teacher_loss = t * t * (torch.special.xlogy(p, p) - p * logq_t).sum(1)
+    one = torch.nn.functional.one_hot(labels.long(), C)
+    for use, teacher, s, st in ((labels, None, 1.0, 0.0), (labels, (classes, scores), 1.0, 0.5), (None, (classes, scores), 0.0, 0.5)):
+        got = run(torch, B, kind, x, w, None, use, teacher, t, s, st)
+        if use is not None:
+            assert ((got["loss"].double() - loss).abs() <= off + 4 * u * loss).all()
+        if teacher is not None:
+            assert ((got["teacher_loss"].double() - teacher_loss).abs() <= t * t * off + 8 * u * teacher_loss).all()
+        dz = (s * (logq.exp() - one) if s else 0) + (st * t * (logq_t.exp() - p) if st else 0)
+        v, each = (2.0 ** -8 if kind == "bf16" else 2.0 ** -24), (s + 2 * st * t) * off
+        assert ((got["dx"].double() - dz).abs() <= 2.1 * v * dz.abs() + each).all()
+        assert got["dbias"].isfinite().all() and got["dweight"].isfinite().all()
+        want, size = dz.t() @ z, dz.abs().t().contiguous() @ z.abs()
+        assert ((got["dweight"].double() - want).abs() <= 2.1 * v * size + (n + 8) * u * size + each * z.abs().sum(0) + v * want.abs()).all()
