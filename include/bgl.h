@@ -916,8 +916,9 @@ int bgl_class_loss_forward(const bgl_class_loss_t *loss, int64_t n, const void *
  *   workspace   device, 256-byte aligned, >= *backward_bytes
  * Gradients are written, not added to (n = 0: zeros); dx = 0 for rows without a label and a teacher, whose x is not read for dweight.
  * dz is made in pieces of at most 2^25 values, 2^27 + 2^23 in calls of many products.  It is not rounded to the type: in fp32 it keeps 24 bits, in bf16 16, or in calls of many
- * products 11, fewer where it is below 2^-28 of |scale| + |teacher_scale| t (none below 2^-39); x and weight are halves there, exact down to 2^-32
- * of their largest finite value, and infinities in them may give NaN.
+ * products 11, fewer where it is below 2^-28 of |scale| + |teacher_scale| t (none below 2^-39); x and weight are halves there, exact down to 2^-32 of their largest finite
+ * value.  That is so where the rows' largest values (of x: rows with a gradient; of weight: classes) are within 2^12 of each other and scores cannot be off by 2^-23 t from it; else such calls
+ * take x and weight as they are and dz in 16 bits, in half as much time again.  A row of x or weight that is not finite may make dx of it, dweight and dbias NaN.
  * The order of the sums is fixed by n and the sizes: repeated calls give the same bits.
  * Errors: as bgl_class_loss_forward.
  */

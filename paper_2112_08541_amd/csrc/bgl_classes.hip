@@ -124,13 +124,16 @@ __device__ __forceinline__ void split(float v, uint16_t (&e)[3])
     e[2] = BF16::put(rest - BF16::get(e[1]));
 }
 
-// dz as large calls keep it: three bf16 of fp32 layers, a half of bf16 ones.
+// dz as large calls keep it: three bf16 of fp32 layers; of bf16 ones a half, or (`whole`, see k_class_halves) two bf16.
 template <class T>
-__device__ __forceinline__ void parts(float d, uint16_t (&e)[3])
+__device__ __forceinline__ void parts(float d, bool whole, uint16_t (&e)[3])
 {
     if constexpr (T::PER == 1) split(d, e);
+    else if (whole) e[0] = BF16::put(d), e[1] = BF16::put(d - BF16::get(e[0]));
     else e[0] = __builtin_bit_cast(uint16_t, (_Float16)d);
 }
+template <class T>
+__device__ __forceinline__ int dz_planes(bool whole) { return T::PER == 1 ? 3 : whole ? 2 : 1; }
 
 template <class T>
 struct ScoreArgs {
@@ -328,7 +331,8 @@ struct RowArgs {
     // backward: the piece of dz
     typename T::elem *dz, *dz_rest;
     int class0, piece_classes, dz_stride;
-    bool blocks;     // dz lies in blocks, as halves or three bf16
+    bool blocks;     // dz lies in blocks, as parts() makes them
+    const int32_t *whole;
 };
 
 // The scores of the teacher's classes: 8 lanes for four of a row's, 128 bytes of x and of the classes' rows at a time.  4,096 rows of 512 bf16, 32 classes each: 20 us, 6.6
@@ -586,8 +590,9 @@ __global__ void __launch_bounds__(256) k_class_fix(RowArgs<T> a)
             for (int u = 0; u < AHEAD; ++u)
                 if (other[u] == c) p += share(o + u), before |= o + u < k;
         }
-        constexpr int PLANES = T::PER == 1 ? 3 : 1;
-        uint16_t *const block = reinterpret_cast<uint16_t *>(a.dz) + (a.blocks ? dz_block(r, c - a.class0, a.dz_stride, PLANES) : 0);
+        const bool whole = T::PER == 2 && a.blocks && a.whole[0];
+        const int planes = dz_planes<T>(whole);
+        uint16_t *const block = reinterpret_cast<uint16_t *>(a.dz) + (a.blocks ? dz_block(r, c - a.class0, a.dz_stride, planes) : 0);
         typename T::elem *const value = a.dz + r * a.dz_stride + (c - a.class0);
         float d = 0.0f;
         if constexpr (T::PER == 1) {
@@ -596,7 +601,7 @@ __global__ void __launch_bounds__(256) k_class_fix(RowArgs<T> a)
             if (before) continue;
             if (a.blocks) {
 #pragma unroll
-                for (int p = 0; p < PLANES; ++p) d += BF16::get(block[p * kBlockValues]);
+                for (int p = 0; p < 3; ++p) d += BF16::get(block[p * kBlockValues]);
             } else {
                 d = *value;
             }
@@ -609,9 +614,10 @@ __global__ void __launch_bounds__(256) k_class_fix(RowArgs<T> a)
         }
         if (a.blocks) {
             uint16_t e[3];
-            parts<T>(d, e);
+            parts<T>(d, whole, e);
 #pragma unroll
-            for (int p = 0; p < PLANES; ++p) block[p * kBlockValues] = e[p];
+            for (int p = 0; p < 3; ++p)
+                if (p < planes) block[p * kBlockValues] = e[p];
         } else {
             *value = T::put(d);
             if constexpr (T::PER == 2) a.dz_rest[value - a.dz] = T::put(d - T::get(*value));
@@ -847,7 +853,7 @@ struct LayArgs {
     int64_t stride, rows, all_rows;
     int D, padded;
     uint16_t *to;
-    int32_t *exponent;  // of halves
+    int32_t *exponent;  // backward, bf16: of halves; behind it `whole`
     // backward, x: rows without a gradient become zeros, whatever they hold
     bool select;
     const int32_t *labels;
@@ -883,11 +889,17 @@ __global__ void __launch_bounds__(256) k_class_lay(LayArgs<BF16> a)
 }
 
 // bf16 rows and weight as halves, for the backward call, whose dz is in halves: times 2^-exponent, one for all of x and one for all of W, so that the largest is
-// in [2^14, 2^15) and a bf16's eight bits fit a half's from 2^-32 of it on.  First the largest of kLayGroups shares of each, then every workgroup finds the exponent from these.
+// in [2^14, 2^15) and a bf16's eight bits fit a half's from 2^-32 of it on; below, a value is off by 2^-39 of it at most.  That is as good as exact where no row (of x: with a
+// gradient) is far smaller than another, and no score's products: where the rows' largest values are within 12 powers of two, and where what scores can be off by,
+// 2^-38 D max|x| max|w| over the temperature, is below 2^-23.  Else (`whole`) x and W stay bf16 and dz is two of them, twice the products: of one row 2^32 above the others
+// these lost everything (4,096 x 512 x 65,536 training: 1,305 us, so 1,951).  First the largest and smallest of kLayGroups groups of rows of each, then every workgroup finds exponent and choice from them.
 constexpr int kLayGroups = 1024, kHalvesHead = 2 * kLayGroups * 4 + 256;
+constexpr int kRowsApart = 12;             // powers of two
+constexpr float kProductMost = 0x1p15f;    // D max|x| max|w|, at a temperature of 1
 struct HalvesArgs {
     LayArgs<BF16> w, x;
-    uint32_t *largest;       // kLayGroups of w, kLayGroups of x
+    uint32_t *w_sizes, *x_sizes;  // of kLayGroups groups: of the rows' largest finite values the largest, and 0x7f80 less the smallest that is not 0 (as bits of a bf16)
+    float product_most;
 };
 __device__ __forceinline__ uint32_t largest_of(const uint4 &v)
 {
@@ -901,49 +913,84 @@ __device__ __forceinline__ uint32_t largest_of(const uint4 &v)
     }
     return most;
 }
-__device__ __forceinline__ uint32_t group_largest(uint32_t v)
+// The largest over a workgroup, of COUNT numbers of up to 24 bits.
+template <int COUNT>
+__device__ __forceinline__ void group_largest(uint32_t (&v)[COUNT])
 {
-    __shared__ float all[4];
-    const float w = max_across<64>((float)v);  // (15 bits)
-    if (threadIdx.x % 64 == 0) all[threadIdx.x / 64] = w;
+    __shared__ float all[COUNT][4];
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+        const float w = max_across<64>((float)v[i]);
+        if (threadIdx.x % 64 == 0) all[i][threadIdx.x / 64] = w;
+    }
     __syncthreads();
-    return (uint32_t)fmaxf(fmaxf(all[0], all[1]), fmaxf(all[2], all[3]));
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) v[i] = (uint32_t)fmaxf(fmaxf(all[i][0], all[i][1]), fmaxf(all[i][2], all[i][3]));
 }
+// TEAM lanes for a row, four rows on their way at a time.
+template <int TEAM>
 __global__ void __launch_bounds__(256) k_class_largest(HalvesArgs a)
 {
+    constexpr int TEAMS = 256 / TEAM, AHEAD = 4;
     const bool second = blockIdx.x >= kLayGroups;
     const LayArgs<BF16> &m = second ? a.x : a.w;
-    uint32_t most = 0;
-    each_eight(m, blockIdx.x % kLayGroups, kLayGroups, [&](int64_t row, int d) {
-        const uint32_t v = largest_of(eight(m, row, d));
-        most = v > most ? v : most;
-    });
-    most = group_largest(most);
-    if (threadIdx.x == 0) a.largest[blockIdx.x] = most;
+    const int group = blockIdx.x % kLayGroups, l = (int)threadIdx.x % TEAM;
+    uint32_t v[2] = {};
+    for (int64_t row = (int64_t)group * TEAMS + threadIdx.x / TEAM; row < m.rows; row += (int64_t)kLayGroups * TEAMS * AHEAD) {
+        uint32_t most[AHEAD] = {};
+        for (int d = l * 8; d < m.D; d += TEAM * 8) {
+            uint4 u[AHEAD];
+#pragma unroll
+            for (int r = 0; r < AHEAD; ++r) u[r] = eight(m, row + (int64_t)r * kLayGroups * TEAMS, d);
+#pragma unroll
+            for (int r = 0; r < AHEAD; ++r) {
+                const uint32_t of = largest_of(u[r]);
+                most[r] = of > most[r] ? of : most[r];
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < AHEAD; ++r) {
+            const uint32_t of = (uint32_t)max_across<TEAM>((float)most[r]), under = of ? 0x7f80 - of : 0;
+            v[0] = of > v[0] ? of : v[0], v[1] = under > v[1] ? under : v[1];
+        }
+    }
+    group_largest(v);
+    uint32_t *to = (second ? a.x_sizes : a.w_sizes) + group;
+    if (threadIdx.x == 0) to[0] = v[0], to[kLayGroups] = v[1];
 }
 __global__ void __launch_bounds__(256) k_class_halves(HalvesArgs a, uint32_t w_groups)
 {
     const bool second = blockIdx.x >= w_groups;
     const LayArgs<BF16> &m = second ? a.x : a.w;
-    uint32_t most = 0;
+    uint32_t v[4] = {};  // of w, of x
 #pragma unroll
-    for (int i = 0; i < kLayGroups / 256; ++i) {
-        const uint32_t v = a.largest[(second ? kLayGroups : 0) + i * 256 + threadIdx.x];
-        most = v > most ? v : most;
-    }
-    most = group_largest(most);
-    int exponent = most ? ilogbf(__uint_as_float(most << 16)) - 14 : 0;
-    if (exponent < -115) exponent = -115;
+    for (int i = 0; i < kLayGroups / 256; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t of = (j < 2 ? a.w_sizes : a.x_sizes)[j % 2 * kLayGroups + i * 256 + threadIdx.x];
+            v[j] = of > v[j] ? of : v[j];
+        }
+    group_largest(v);
+    const auto value = [](uint32_t bits) { return __uint_as_float(bits << 16); };
+    bool whole = !(value(v[0]) * value(v[2]) * (float)m.D <= a.product_most);
+#pragma unroll
+    for (int i = 0; i < 4; i += 2)  // (below 2^-101 exponents end)
+        if (v[i] > 0) whole |= (int)(v[i] >> 7) - (int)((0x7f80 - v[i + 1]) >> 7) > kRowsApart || value(v[i]) < 0x1p-101f;
+    const float most = value(v[second ? 2 : 0]);
+    const int exponent = !whole && most > 0.0f ? ilogbf(most) - 14 : 0;
     const uint32_t group = second ? blockIdx.x - w_groups : blockIdx.x;
-    if (group == 0 && threadIdx.x == 0) m.exponent[0] = exponent;
+    if (group == 0 && threadIdx.x == 0) m.exponent[0] = exponent, m.exponent[1] = whole;
     const float scale = ldexpf(1.0f, -exponent);
     each_eight(m, group, second ? gridDim.x - w_groups : w_groups, [&](int64_t row, int d) {
-        const uint4 v = eight(m, row, d);
-        const uint32_t in[4] = {v.x, v.y, v.z, v.w};
-        _Float16 h[8];
+        uint4 v = eight(m, row, d);
+        if (!whole) {
+            const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+            _Float16 h[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) h[2 * j] = (_Float16)(__uint_as_float(in[j] << 16) * scale), h[2 * j + 1] = (_Float16)(__uint_as_float(in[j] & 0xffff0000u) * scale);
-        *reinterpret_cast<uint4 *>(m.to + row * m.padded + d) = __builtin_bit_cast(uint4, h);
+            for (int j = 0; j < 4; ++j) h[2 * j] = (_Float16)(__uint_as_float(in[j] << 16) * scale), h[2 * j + 1] = (_Float16)(__uint_as_float(in[j] & 0xffff0000u) * scale);
+            v = __builtin_bit_cast(uint4, h);
+        }
+        *reinterpret_cast<uint4 *>(m.to + row * m.padded + d) = v;
     });
 }
 // A wavefront for a row.  50,001 x 256: 22 us (128 MB, 5.9 TB/s).
@@ -981,7 +1028,7 @@ struct StageScoreArgs {
     const char *x, *w;           // of the call's first row, of class 0: three planes of bf16, or bf16 or halves
     int64_t x_bytes, w_bytes;    // rows
     uint32_t plane;              // bytes
-    const int32_t *x_exponent, *w_exponent;  // of halves
+    const int32_t *x_exponent, *w_exponent;  // of halves, and `whole` behind each
     // forward, or null: the teacher's classes, n x top, whose scores go to z_top
     const int32_t *top_class;
     float *z_top;
@@ -994,7 +1041,7 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
     using C = StageCut;
     using A = stage::Kc<C::BA, kPad>;
     using B = stage::Kc<C::BB, kPad>;
-    constexpr int PLANES = T::PER == 1 ? 3 : 1;  // of dz
+    constexpr bool CHOICE = T::PER == 2 && DZ;
     constexpr stage::Kind READ = T::PER == 1 ? stage::THREE_BF16 : DZ ? stage::ONE_HALF : stage::ONE_BF16;
     __shared__ __attribute__((aligned(1024))) char lds[stage::lds_bytes<A, B>()];
     const ScoreArgs<T> &a = q.s;
@@ -1023,7 +1070,11 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
         }
     }
     f32x4 acc[C::FA][C::FB] = {};
-    stage::multiply<READ, false, A, B, C>(lds, weight, rows, stage::Walk{2 * kPad, 2 * kPad, q.plane, q.plane, a.D, 0}, acc, [](int, int, const auto &) {});
+    const stage::Walk walk{2 * kPad, 2 * kPad, q.plane, q.plane, a.D, 0};
+    const auto nothing = [](int, int, const auto &) {};
+    const bool whole = CHOICE && q.w_exponent[1];
+    if (CHOICE && whole) stage::multiply<stage::ONE_BF16, false, A, B, C>(lds, weight, rows, walk, acc, nothing);
+    else stage::multiply<READ, false, A, B, C>(lds, weight, rows, walk, acc, nothing);
 
     if ((uint32_t)my_label >= (uint32_t)a.all_classes) my_label = -1, my_sum = INFINITY;
     if (my_sum == INFINITY && my_sum_t == INFINITY) my_most = INFINITY;  // (whatever such a row holds)
@@ -1108,6 +1159,7 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
         }
     }
     const bool teachers = DZ && a.teacher_scale != 0.0f, labels = a.labels != nullptr && (!DZ || a.scale != 0.0f);
+    const auto end = [&](auto form) {
 #pragma unroll
     for (int t = 0; t < C::FB; ++t) {
         const int b = C::b_off() + 16 * t + (l & 15);
@@ -1156,6 +1208,8 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
                 if (a.two) a.part_t[at] = sum_t;
             }
         } else {
+            constexpr bool WHOLE = decltype(form)::value;
+            constexpr int planes = T::PER == 1 ? 3 : WHOLE ? 2 : 1;
             const float shift = own.shift[b], base = own.base[b], base_t = own.base_t[b], share = a.scale * own.share[b], share_t = own.share_t[b];
             if (__any(shift != 0.0f)) take_shift<C>(acc, t, shift);
 #pragma unroll
@@ -1167,31 +1221,34 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
 #pragma unroll
                     for (int j = 0; j < 4; ++j) d[j] = fmaf(share_t, power_to(acc[i][t][j], a.k_t, base_t), d[j]);
                 }
-                uint16_t *to = reinterpret_cast<uint16_t *>(a.dz) + dz_block(r, first - a.class0 + 16 * i, a.dz_stride, PLANES);
-                uint16_t e[PLANES][4];
+                uint16_t *to = reinterpret_cast<uint16_t *>(a.dz) + dz_block(r, first - a.class0 + 16 * i, a.dz_stride, planes);
+                uint16_t e[planes][4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     uint16_t one[3];
-                    parts<T>(d[j], one);
+                    parts<T>(d[j], WHOLE, one);
 #pragma unroll
-                    for (int p = 0; p < PLANES; ++p) e[p][j] = one[p];
+                    for (int p = 0; p < planes; ++p) e[p][j] = one[p];
                 }
 #pragma unroll
-                for (int p = 0; p < PLANES; ++p) __builtin_memcpy(to + p * kBlockValues, e[p], sizeof(e[p]));
+                for (int p = 0; p < planes; ++p) __builtin_memcpy(to + p * kBlockValues, e[p], sizeof(e[p]));
             }
             if (any) {  // the label's class again, with the label
                 const float v = own_score(t);
                 float d = a.scale * (power_to(v, a.k, base) * own.share[b] - 1.0f);
                 if (teachers) d = fmaf(share_t, power_to(v, a.k_t, base_t), d);
-                uint16_t e[3], *to = reinterpret_cast<uint16_t *>(a.dz) + dz_block(r, first - a.class0 + (mine ? at : 0), a.dz_stride, PLANES);
-                parts<T>(d, e);
+                uint16_t e[3], *to = reinterpret_cast<uint16_t *>(a.dz) + dz_block(r, first - a.class0 + (mine ? at : 0), a.dz_stride, planes);
+                parts<T>(d, WHOLE, e);
                 if (mine) {
 #pragma unroll
-                    for (int p = 0; p < PLANES; ++p) to[p * kBlockValues] = e[p];
+                    for (int p = 0; p < planes; ++p) to[p * kBlockValues] = e[p];
                 }
             }
         }
     }
+    };
+    if (CHOICE && whole) end(std::true_type{});
+    else end(std::false_type{});
     if constexpr (!DZ) {
         // (204,800 x 256 x 150 bf16: 46 us with a launch of k_class_finish)
         if (!a.whole) return;
@@ -1225,7 +1282,7 @@ struct StagePieceArgs {
     int64_t per_share;                 // a multiple of 32
     typename T::elem *out;
     int64_t out_stride;
-    const int32_t *exponent;           // bf16: of b
+    const int32_t *exponent;           // bf16: of b, and `whole`
     float undo;                        // 1 over what dz was multiplied by: the result is the product times this and 2^exponent
     float *slots, *sum_slots;          // (both without that)  sums: shares x min(kSummers, column tiles) x 2 of them
     int64_t slot_rows;                 // of a slot, a multiple of the tiles' as slot_width is
@@ -1258,12 +1315,13 @@ struct StageProduct {
     using A = std::conditional_t<OC, stage::OcBlocks<C::BA>, stage::Kc<C::BA, kBlockClasses>>;
     using B = stage::Oc<C::BB>;
     static constexpr int LDS = stage::lds_bytes<A, B>();
+    template <stage::Kind KIND>
     static __device__ __forceinline__ void make(const StagePieceArgs<T> &a, uint32_t id, char *lds);
 };
 template <class T, bool OC>
+template <stage::Kind KIND>
 __device__ __forceinline__ void StageProduct<T, OC>::make(const StagePieceArgs<T> &a, uint32_t id, char *lds)
 {
-    constexpr stage::Kind KIND = T::PER == 1 ? stage::THREE_BF16 : stage::ONE_HALF;
     constexpr int PLANES = stage::Pairs<KIND>::PLANES;
     const int share = (int)(id % (uint32_t)a.shares);
     int64_t rt;
@@ -1300,7 +1358,7 @@ __device__ __forceinline__ void StageProduct<T, OC>::make(const StagePieceArgs<T
     const int summers = a.col_tiles < kSummers ? a.col_tiles : kSummers, summer = 2 * ct + (C::b_off() > 0);
     const bool summing = OC && a.sum_slots && ct < summers;
     stage::multiply<KIND, true, A, B, C>(lds, left, right, stage::Walk{a_block, (uint32_t)(A::STEP * a.b_bytes), kBlockValues * 2, a.b_plane, K, 0}, acc, [&](int s, int b_plane, const auto &f) {
-        if (summing && b_plane == 0 && (PLANES == 1 ? s : s / 6) % (2 * summers) == summer) {
+        if (summing && b_plane == 0 && s / stage::Pairs<KIND>::COUNT % (2 * summers) == summer) {
 #pragma unroll
             for (int t = 0; t < C::FA; ++t) {
                 const uint4 v = __builtin_bit_cast(uint4, f[t]);
@@ -1349,8 +1407,16 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_products_stage(Sta
     using W = StageProduct<T, true>;
     using X = StageProduct<T, false>;
     __shared__ __attribute__((aligned(1024))) char lds[W::LDS > X::LDS ? W::LDS : X::LDS];
-    if (blockIdx.x < dw_groups) W::make(dw, blockIdx.x, lds);
-    else X::make(dx, blockIdx.x - dw_groups, lds);
+    if constexpr (T::PER == 1) {
+        if (blockIdx.x < dw_groups) W::template make<stage::THREE_BF16>(dw, blockIdx.x, lds);
+        else X::template make<stage::THREE_BF16>(dx, blockIdx.x - dw_groups, lds);
+    } else if (blockIdx.x < dw_groups) {
+        if (dw.exponent[1]) W::template make<stage::TWO_BF16>(dw, blockIdx.x, lds);
+        else W::template make<stage::ONE_HALF>(dw, blockIdx.x, lds);
+    } else {
+        if (dx.exponent[1]) X::template make<stage::TWO_BF16>(dx, blockIdx.x - dw_groups, lds);
+        else X::template make<stage::ONE_HALF>(dx, blockIdx.x - dw_groups, lds);
+    }
 }
 
 // ----------------------------------------------------------------- plans
@@ -1392,7 +1458,7 @@ struct Scheme {
 Scheme scheme_of(const bgl_class_loss_t *l, bool large)
 {
     const bool f32 = l->dtype == BGL_F32;
-    if (large) return Scheme{true, StageCut::BA, ProductCut::BA, ((int64_t)1 << 27) + ((int64_t)1 << 23), StageCut::BA, StageCut::BB, f32 ? 6 : 2, f32 ? 3 : 1, ProductCut::BA, 2 * kCus, 512};
+    if (large) return Scheme{true, StageCut::BA, ProductCut::BA, ((int64_t)1 << 27) + ((int64_t)1 << 23), StageCut::BA, StageCut::BB, f32 ? 6 : 4, f32 ? 3 : 1, ProductCut::BA, 2 * kCus, 512};
     return Scheme{false, 128, 128, (int64_t)1 << 25, 8, 1, 4, 1, 1, kCus, 64};  // (pieces of 4 classes are stored, and 16 bytes of bf16 read)
 }
 bool large_call(const bgl_class_loss_t *l, int64_t n) { return n >= 96 && l->classes >= 128 && (double)n * l->classes * l->in_dim >= kLargeProducts; }
@@ -1632,8 +1698,8 @@ StageScoreArgs<BF16> stage_args(const Call &c, const Plan &p, const ScoreArgs<BF
     q.x_bytes = q.w_bytes = (int64_t)p.padded * 2;
     LayArgs<BF16> lw = lay_args<BF16>(s.w, s.D, s.classes, s.classes, s.D, p.padded, nullptr), lx = lay_args<BF16>(s.x, s.x_stride, c.n, round_up(c.n, 32), s.D, p.padded, select);
     if (select) {
-        // the largest of shares (at w's), the exponent, the values
-        HalvesArgs a{lw, lx, (uint32_t *)w};
+        // shares of sizes, the exponent and the choice, the values
+        HalvesArgs a{lw, lx, (uint32_t *)w, (uint32_t *)x, kProductMost * (c.l->temperature < 1.0f ? c.l->temperature : 1.0f)};
         const auto place = [&](LayArgs<BF16> &m, char *to, const char *&read, const int32_t *&exponent) {
             m.exponent = (int32_t *)(to + 2 * kLayGroups * 4), m.to = (uint16_t *)(to + kHalvesHead);
             read = to + kHalvesHead, exponent = m.exponent;
@@ -1643,7 +1709,9 @@ StageScoreArgs<BF16> stage_args(const Call &c, const Plan &p, const ScoreArgs<BF
             const int64_t all = ceil_div(m.all_rows * (p.padded / 8), 256);
             return (uint32_t)(all < 8 * kCus ? all : 8 * kCus);
         };
-        k_class_largest<<<dim3(2 * kLayGroups), dim3(256), 0, c.stream>>>(a);
+        if (s.D <= 64) k_class_largest<8><<<dim3(2 * kLayGroups), dim3(256), 0, c.stream>>>(a);
+        else if (s.D <= 256) k_class_largest<32><<<dim3(2 * kLayGroups), dim3(256), 0, c.stream>>>(a);
+        else k_class_largest<64><<<dim3(2 * kLayGroups), dim3(256), 0, c.stream>>>(a);
         k_class_halves<<<dim3(groups(a.w) + groups(a.x)), dim3(256), 0, c.stream>>>(a, groups(a.w));
         return q;
     }
@@ -1781,6 +1849,7 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
     float undo = 1.0f;
     if (h.large) {
         q = stage_args(c, p, s, x_laid, w_laid, &r);
+        r.whole = T::PER == 2 ? q.w_exponent + 1 : nullptr;
         if (T::PER == 2) {
             // dz in halves: a power of two takes what it can be at most, |scale| + |teacher_scale|, to [2^13, 2^14]; what is below 2^-28 of that has fewer than a half's
             // eleven bits, and below 2^-39 none

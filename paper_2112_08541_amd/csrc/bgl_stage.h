@@ -237,12 +237,12 @@ constexpr int stages() { return 81920 / (A::BYTES + B::BYTES); }
 template <class A, class B>
 constexpr int lds_bytes() { return stages<A, B>() * (A::BYTES + B::BYTES); }
 
-// What operands are made of: a bf16; three bf16 of a value; a half.  A, B: the planes of product p, hexadecimal digit p.
-enum Kind { ONE_BF16, THREE_BF16, ONE_HALF };
+// What operands are made of: a bf16; two bf16 of A's values and one of B's; three bf16 of a value; a half.  PLANES: A's.  A, B: the planes of product p, hexadecimal digit p.
+enum Kind { ONE_BF16, TWO_BF16, THREE_BF16, ONE_HALF };
 template <Kind KIND>
 struct Pairs {
-    static constexpr int PLANES = KIND == THREE_BF16 ? 3 : 1, COUNT = PLANES == 1 ? 1 : 6;
-    static constexpr uint32_t A = 0x010210, B = 0x211000;
+    static constexpr int PLANES = KIND == THREE_BF16 ? 3 : KIND == TWO_BF16 ? 2 : 1, COUNT = PLANES == 3 ? 6 : PLANES;
+    static constexpr uint32_t A = PLANES == 3 ? 0x010210 : 0x10, B = PLANES == 3 ? 0x211000 : 0;
 };
 template <Kind KIND>
 __device__ __forceinline__ f32x4 mma(const bf16x8 &a, const bf16x8 &b, const f32x4 &c)

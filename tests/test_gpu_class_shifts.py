@@ -76,7 +76,8 @@ HIGH = [2.0 ** 23, -2.0 ** 24, 2.0 ** 27, -2.0 ** 30, 2.0 ** 31, -2.0 ** 33, 2.0
 
 
 @pytest.mark.parametrize("t", [1.0, 1024.0, 2.0 ** -10])
-@pytest.mark.parametrize("kind,n,C", [(kind, n, C) for kind in ("f32", "bf16") for n, C in [(50, 3), (50, 40), (70, 300), (90, 1_300), (9_000, 12)]] + [("f32", 1_300, 1_300)])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("n,C", [(50, 3), (50, 40), (70, 300), (90, 1_300), (1_300, 1_300), (9_000, 12)])
 def test_scores_beyond_the_steps_of_their_exponents(torch, B, kind, n, C, t):
     """Scores as large as 2^100, a few steps of 1 or of their last place apart, beside ordinary ones.  The weight is the identity, so that scores are x and dx is dz; every row's own
     step makes its distribution anything from even to a single class.  Powers are right to 6 u and 2 u of their argument (which e^-a a <= 0.4 keeps below 1 u in q), sums of
