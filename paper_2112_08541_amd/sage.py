@@ -137,6 +137,9 @@ class Student:
 class TypedSage:
     """max_nodes: bound on a batch's nodes per hop, seeds first (max_nodes[h] for frontier h, as a Sampler's cap_nodes)."""
 
+    SCORES_AT_A_TIME = B.BGL_MAX_DIM     # classes whose scores best_classes() has in memory
+
+
     def __init__(self, max_nodes: Sequence[int], in_dim: int, hidden: int, num_classes: int, num_types: int,
                  dtype=torch.float32, lr: float = 0.02, head_lr: float = 0.3, beta: float = 0.9, seed: int = 0,
                  norm: bool = False, keep_scores: bool = True):
@@ -153,7 +156,9 @@ class TypedSage:
         self.input = B.Linear(max_nodes[-1], in_dim, hidden, dtype, activation="gelu", num_groups=num_types)
         self.own = [B.Linear(max_nodes[h], hidden, hidden, dtype) for h in range(self.num_hops)]
         self.near = [B.Linear(max_nodes[h], hidden, hidden, dtype, activation="gelu", residual="before") for h in range(self.num_hops)]
-        self.head = B.Linear(max_nodes[0], hidden, num_classes, dtype)
+        # (a layer has BGL_MAX_DIM columns at most, a loss without kept scores more classes)
+        self.head = B.Linear(max_nodes[0], hidden, num_classes, dtype) if keep_scores or num_classes <= B.BGL_MAX_DIM else None
+        self.max_seeds = max_nodes[0]
         self.norms = [B.LayerNorm(max_nodes[h + 1], hidden, dtype) for h in range(self.num_hops)] if norm else []
         self.norm_w, self.norm_b = [_ones(make, hidden) for _ in self.norms], [make((hidden,), 0.0, False) for _ in self.norms]
         self.loss = None if keep_scores else B.ClassLoss(max_nodes[0], hidden, num_classes, dtype)
@@ -167,10 +172,30 @@ class TypedSage:
     def forward(self, rows: torch.Tensor, types: torch.Tensor, ids: torch.Tensor, blocks) -> torch.Tensor:
         """rows: the batch's feature rows (n x in_dim); types: of every node of the graph (int32); ids: the batch's input nodes;
         blocks: per hop (row_ptr, col_local, destinations, sources).  Returns the seeds' class scores."""
+        if self.head is None:
+            raise ValueError(f"the scores of {self.num_classes} classes are not kept: best_classes() has the best ones")
         h = self.hidden_rows(rows, types, ids, blocks)
         scores = self._empty(h.shape[0], self.num_classes)
         self.head.forward(h, self.w_out.value, scores, self.b_out.value)
         return scores
+
+    def best_classes(self, rows: torch.Tensor, types: torch.Tensor, ids: torch.Tensor, blocks, top: int):
+        """Each seed's best classes (int32) and their scores, as best_classes() of forward()'s; scores are made for some classes at a time, so that memory does not grow with
+        their number."""
+        h, best = self.hidden_rows(rows, types, ids, blocks), None
+        for first in range(0, self.num_classes, self.SCORES_AT_A_TIME):
+            some = slice(first, min(first + self.SCORES_AT_A_TIME, self.num_classes))
+            scores = self._empty(h.shape[0], some.stop - first)
+            head = self.head if scores.shape[1] == self.num_classes else B.Linear(self.max_seeds, self.hidden, scores.shape[1], self.dtype)
+            head.forward(h, self.w_out.value[some], scores, self.b_out.value[some])
+            classes, values = best_classes(scores, top)
+            classes += first
+            if best is not None:
+                classes, values = torch.cat([best[0], classes], 1), torch.cat([best[1], values], 1)
+                at, values = best_classes(values, top)
+                classes = classes.gather(1, at.long())
+            best = classes, values
+        return best
 
     def hidden_rows(self, rows: torch.Tensor, types: torch.Tensor, ids: torch.Tensor, blocks) -> torch.Tensor:
         """The seeds' last hidden rows, from which forward() makes scores."""
@@ -279,7 +304,7 @@ def train_student(pipe, model: TypedSage, student: Student, seeds: torch.Tensor,
     model's scores.  Returns the loss per batch."""
     def step(rows, ids, blocks):
         n = blocks[0][2]
-        return student.train_step(rows[:n], labels[ids[:n].long()].int(), best_classes(model.forward(rows, types, ids, blocks), top))
+        return student.train_step(rows[:n], labels[ids[:n].long()].int(), model.best_classes(rows, types, ids, blocks, top))
     return torch.stack(_over_batches(pipe, model, seeds, rng_seeds, steps, step)).cpu().numpy()
 
 
