@@ -882,7 +882,7 @@ int bgl_layer_norm_backward(const bgl_layer_norm_t *norm, int64_t n, const void 
  *   label_loss, teacher_loss  device, n floats each, or null
  *   saved             device, n x (3 + top) floats (n x 2 without a teacher, top = 0) that the backward call needs, or null
  *   workspace         device, 256-byte aligned, >= *forward_bytes of bgl_class_loss_workspace_bytes(loss, n, ...)
- * Sums are fp32.  Calls of many products (n >= 96, 128 classes, 2e9 products) make fp32 scores and gradients from three bf16 parts of each value: 24 bits down to 2^-110.
+ * Sums are fp32.  Calls of many products (more than 128 rows and classes, 2e9 products) make fp32 scores and gradients from three bf16 parts of each value: 24 bits down to 2^-110.
  * Outputs must not overlap inputs or each other.  n = 0 does nothing.
  * Errors: BGL_EINVAL (null or misaligned pointers, strides, sizes < 1, temperature outside [2^-10, 2^10], unknown
  * types, a loss without what it is of), BGL_EUNSUPPORTED (in_dim > BGL_MAX_DIM, classes > BGL_MAX_CLASSES, top > BGL_MAX_TOP),

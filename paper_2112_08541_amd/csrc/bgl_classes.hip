@@ -39,8 +39,12 @@ constexpr int64_t kPartialBytes = (int64_t)64 << 20;   // of a forward call's ti
 constexpr int kCus = 256;
 constexpr int kStoredBeside = 512;                     // bytes of classes' rows that storing a tile's row in LDS takes as long as
 constexpr int64_t kMostThreads = (int64_t)1 << 31;     // of a launch, which has room for 2^32 - 1
-constexpr double kLargeProducts = 2e9;                 // of a call that is laid out for large tiles: 512 x 256 x 4,096 f32 took 30 + 110 us so and 19 + 58 in small ones,
-                                                       // 1,316 x 503 x 3,640 45 + 167 and 77 + 199; bf16 15 + 42 and 11 + 40, 29 + 66 and 24 + 83
+// Calls that are laid out for large tiles have more rows than one of these has, more classes than one of the small ones has, and many products.  us, forward + backward, in
+// small tiles and so: bf16, rows x 512 x 65,536: 128 rows 29 + 111 and 31 + 122, 160 39 + 172 and 40 + 140; 50,000 x 512 x classes: 128 classes 17 + 84 and 18 + 104, 160
+// 31 + 135 and 19 + 108; f32: 85 + 259 and 145 + 322, 197 + 471 and 172 + 388; 73 + 219 and 103 + 256, 149 + 355 and 107 + 271.  2e9 products: 512 x 256 x 16,384 bf16 19 + 59
+// and 19 + 50, f32 47 + 129 and 54 + 131; 10,000 x 256 x 1,001 bf16 17 + 70 and 16 + 60, f32 61 + 188 and 52 + 186.
+constexpr int kLargeRows = 129, kLargeClasses = 129;
+constexpr double kLargeProducts = 2e9;
 
 // Exponentials are powers of two: exp(k v) / 2^base with k = log2(e) or that over the temperature, as 2^(k v - base) with one rounding.  A sum of them is taken to
 // the base of its largest value, k most, rounded: what rounding leaves of it is the same for all of a sum, and sums of two bases meet exactly, as the bases' difference has no
@@ -1461,7 +1465,7 @@ Scheme scheme_of(const bgl_class_loss_t *l, bool large)
     if (large) return Scheme{true, StageCut::BA, ProductCut::BA, ((int64_t)1 << 27) + ((int64_t)1 << 23), StageCut::BA, StageCut::BB, f32 ? 6 : 4, f32 ? 3 : 1, ProductCut::BA, 2 * kCus, 512};
     return Scheme{false, 128, 128, (int64_t)1 << 25, 8, 1, 4, 1, 1, kCus, 64};  // (pieces of 4 classes are stored, and 16 bytes of bf16 read)
 }
-bool large_call(const bgl_class_loss_t *l, int64_t n) { return n >= 96 && l->classes >= 128 && (double)n * l->classes * l->in_dim >= kLargeProducts; }
+bool large_call(const bgl_class_loss_t *l, int64_t n) { return n >= kLargeRows && l->classes >= kLargeClasses && (double)n * l->classes * l->in_dim >= kLargeProducts; }
 bool laid_out(const bgl_class_loss_t *l) { return l->dtype == BGL_BF16 && l->in_dim % kPad == 0; }
 
 // Ranges of the summed index that a product of rows x cols is made in, and the tiles' rows: small calls take tiles of 16 x 128 for up to 16 rows (in 128 x 128 the

@@ -3,6 +3,7 @@ no row or class may lose what it has because another one is large."""
 import pytest
 
 from test_gpu_classes import B, inputs, torch  # noqa: F401
+import test_gpu_classes_large as large
 from test_gpu_classes_large import check_large
 
 pytestmark = pytest.mark.gpu
@@ -47,3 +48,15 @@ def test_columns_of_different_sizes(torch, B, kind, up):
     x[:, 3] *= 2.0 ** up
     w[:, 3] *= 2.0 ** -up
     check_large(torch, B, kind, (x, w, b, labels, teacher), t=1.5, s=1.0 / n, st=0.5 / n)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_a_weight_beyond_32_bits(torch, B, kind):
+    large.test_a_weight_beyond_32_bits(torch, B, kind, 130)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("n,D,C,k", [(128, 512, 40_003, 3), (129, 512, 40_003, 3), (129, 513, 41_003, 0), (20_001, 801, 128, 2), (20_001, 801, 129, 2), (160, 64, 200_003, 0)])
+def test_borders(torch, B, kind, n, D, C, k):
+    """From the small tiles' last row and class to the large ones' first."""
+    check_large(torch, B, kind, inputs(torch, kind, n, D, C, k, seed=n + C, pad=n % 3), t=1.5, s=1.0 / n, st=0.5 / n if k else 0.0)
