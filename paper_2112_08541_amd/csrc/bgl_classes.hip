@@ -405,7 +405,8 @@ __global__ void __launch_bounds__(256) k_class_top(RowArgs<T> a)
     top_scores(a, row, (int)(task % groups) * kTopEach, [=](int k, float z) { a.z_top[row * a.z_stride + k] = z; });
 }
 
-// The teacher's distribution of a row, for LANES neighbours: largest score / t and sum of exp; false where it names no class.
+// The teacher's distribution of a row, for LANES neighbours: largest score and the sum of exp((score - largest) / t); false where it names no class.  (Scores are taken from
+// each other before they meet the temperature: their own quotients round as they are large.)
 template <int LANES, class T>
 __device__ __forceinline__ bool teacher_of(const RowArgs<T> &a, int64_t row, float &most, float &total)
 {
@@ -414,7 +415,7 @@ __device__ __forceinline__ bool teacher_of(const RowArgs<T> &a, int64_t row, flo
     float bad = 0.0f;
     for (int k = l; k < a.top; k += LANES)
         if ((uint32_t)a.top_class[row * a.top + k] < (uint32_t)a.classes) {
-            const float v = a.top_score[row * a.top + k] * a.over_t;
+            const float v = a.top_score[row * a.top + k];
             most = fmaxf(most, v);
             if (v != v) bad = v;
         }
@@ -423,7 +424,7 @@ __device__ __forceinline__ bool teacher_of(const RowArgs<T> &a, int64_t row, flo
     if (bad != bad) most = bad;
     if (most == -INFINITY) return false;
     for (int k = l; k < a.top; k += LANES)
-        if ((uint32_t)a.top_class[row * a.top + k] < (uint32_t)a.classes) total += exp_of(a.top_score[row * a.top + k] * a.over_t - most);
+        if ((uint32_t)a.top_class[row * a.top + k] < (uint32_t)a.classes) total += exp_of((a.top_score[row * a.top + k] - most) * a.over_t);
     total = sum_across<LANES>(total);
     return true;
 }
@@ -540,7 +541,7 @@ __global__ void __launch_bounds__(256) k_class_finish(RowArgs<T> a)
             const float log_total = log2f(total);
             for (int k = l; k < a.top; k += LANES)
                 if ((uint32_t)a.top_class[row * a.top + k] < (uint32_t)a.classes) {
-                    const float v = a.top_score[row * a.top + k] * a.over_t - top_most;
+                    const float v = (a.top_score[row * a.top + k] - top_most) * a.over_t;
                     const float p = exp_of(v) / total, z = TOP ? z_here[threadIdx.x / LANES][k] : a.z_top[row * a.z_stride + k];
                     if (p != 0.0f) kl = fmaf(p, (v * kLog2e - log_total) + (log_sum_t - fmaf(z - to.shift, a.k_t, -to.base_t)), kl);
                 }
@@ -567,7 +568,7 @@ __global__ void __launch_bounds__(256) k_class_fix(RowArgs<T> a)
     int label = a.labels ? a.labels[row] : -1;
     if ((uint32_t)label >= (uint32_t)a.classes) label = -1;
     const int32_t *classes = a.top_class + row * a.top;
-    const auto share = [&](int k) { return exp_of(a.top_score[row * a.top + k] * a.over_t - most) / total; };
+    const auto share = [&](int k) { return exp_of((a.top_score[row * a.top + k] - most) * a.over_t) / total; };
     for (int k = (int)blockIdx.y * LANES + l; k - l < a.top; k += (int)gridDim.y * LANES) {
         const int c = k < a.top ? classes[k] : -1;
         const bool here = c >= a.class0 && c < a.class0 + a.piece_classes;

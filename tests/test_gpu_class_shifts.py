@@ -112,3 +112,16 @@ def test_scores_beyond_the_steps_of_their_exponents(torch, B, kind, n, C, t):
         assert got["dbias"].isfinite().all() and got["dweight"].isfinite().all()
         want, size = dz.t() @ z, dz.abs().t().contiguous() @ z.abs()
         assert ((got["dweight"].double() - want).abs() <= 2.1 * v * size + (n + 8) * u * size + each * z.abs().sum(0) + v * want.abs()).all()
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("t", [0.05, 3.0, 7.0])
+@pytest.mark.parametrize("n,D,C,k", [(70, 30, 300, 8), (70, 30, 300, 9), (1_100, 20, 90, 8), (1_100, 20, 90, 40), (600, 352, 9_600, 5)])
+def test_a_teachers_scores_far_from_zero(torch, B, kind, n, D, C, k, t):
+    """Scores that are exact when moved, so that nothing changes when they are."""
+    x, w, b, labels, teacher = inputs(torch, kind, n, D, C, k, seed=n + k)
+    scores = (teacher[1] * 128).round() / 128
+    want = run(torch, B, kind, x, w, b, labels, (teacher[0], scores), t, 0.4, 0.6)
+    for move in (-30_000.0, 1_000.0, 60_000.0):
+        got = run(torch, B, kind, x, w, b, labels, (teacher[0], scores + move), t, 0.4, 0.6)
+        assert all(torch.equal(got[i], want[i]) for i in got), move
