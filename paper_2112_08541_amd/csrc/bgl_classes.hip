@@ -57,9 +57,8 @@ struct Base {
 template <class A>
 __device__ __forceinline__ Base base_of(const A &a, float most)
 {
-    if (most == -INFINITY) return Base{0.0f, 0.0f, 0.0f};  // (nothing there: the sum is 0)
-    if (fabsf(most) < a.far) return Base{0.0f, most * a.k, most * a.k_t};
-    return Base{most, 0.0f, 0.0f};
+    const bool near = fabsf(most) < a.far, nothing = most == -INFINITY;  // (nothing there: the sum is 0)
+    return Base{near || nothing ? 0.0f : most, near ? most * a.k : 0.0f, near ? most * a.k_t : 0.0f};
 }
 __device__ __forceinline__ float power_to(float v, float k, float base) { return __builtin_amdgcn_exp2f(fmaf(v, k, -base)); }
 __device__ __forceinline__ float max3(float a, float b, float c)  // (of fmaxf the compiler makes two instructions more, for signalling NaN)
@@ -84,13 +83,15 @@ template <class A>
 __device__ __forceinline__ float rebase(const A &a, float most, const Base &to)
 {
     const Base from = base_of(a, most);
-    return most == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(fmaf(from.shift - to.shift, a.k, from.base - to.base));
+    const float power = __builtin_amdgcn_exp2f(fmaf(from.shift - to.shift, a.k, from.base - to.base));
+    return most == -INFINITY ? 0.0f : power;
 }
 template <class A>
 __device__ __forceinline__ float rebase_t(const A &a, float most, const Base &to)
 {
     const Base from = base_of(a, most);
-    return most == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(fmaf(from.shift - to.shift, a.k_t, from.base_t - to.base_t));
+    const float power = __builtin_amdgcn_exp2f(fmaf(from.shift - to.shift, a.k_t, from.base_t - to.base_t));
+    return most == -INFINITY ? 0.0f : power;
 }
 
 // The other lanes with the same lane % 16.
@@ -188,7 +189,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_class_scores(ScoreArgs<T> a)
     __shared__ float meet[DZ ? 1 : 3 * C::BA / 16 / C::FA * C::BB], own_score[DZ ? 1 : C::BB];
     int64_t ct, rt;
     int fast;
-    if (!stage::tile_of(blockIdx.x, (uint32_t)(a.by_rows ? a.row_tiles : a.class_tiles), (uint32_t)(a.by_rows ? a.class_tiles : a.row_tiles), 1, a.by_rows ? rt : ct, fast)) return;
+    const uint32_t slow_tiles = a.by_rows ? (uint32_t)a.row_tiles : a.class_tiles, fast_tiles = a.by_rows ? a.class_tiles : (uint32_t)a.row_tiles;
+    if (!stage::tile_of(blockIdx.x, slow_tiles, fast_tiles, 1, a.by_rows ? rt : ct, fast)) return;
     (a.by_rows ? ct : rt) = fast;
     const int c0 = a.class0 + (int)ct * C::BA, last = a.classes - 1;
     const int64_t r0 = rt * C::BB;  // of this launch's rows
@@ -457,7 +459,7 @@ __global__ void __launch_bounds__(kMergeRows *kMergeLanes) k_class_merge(RowArgs
         for (int u = 0; u < AHEAD; ++u) m = fmaxf(m, from[u].x);
         const Base to = base_of(a, m);
         sum *= rebase(a, most, to);
-        sum_t *= rebase_t(a, most, to);
+        if (a.two) sum_t *= rebase_t(a, most, to);
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) take(to, from[u].x, from[u].y, at_t[u]);
         most = m;
@@ -514,11 +516,11 @@ __global__ void __launch_bounds__(256) k_class_finish(RowArgs<T> a)
         for (int u = 0; u < AHEAD; ++u) m = fmaxf(m, from[u].x);
         const Base to = base_of(a, m);
         sum *= rebase(a, most, to);
-        sum_t *= rebase_t(a, most, to);
+        if (a.two) sum_t *= rebase_t(a, most, to);
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             sum += from[u].y * rebase(a, from[u].x, to);
-            sum_t += at_t[u] * rebase_t(a, from[u].x, to);
+            if (a.two) sum_t += at_t[u] * rebase_t(a, from[u].x, to);
         }
         most = m;
     }
@@ -903,7 +905,8 @@ constexpr int kRowsApart = 12;             // powers of two
 constexpr float kProductMost = 0x1p15f;    // D max|x| max|w|, at a temperature of 1
 struct HalvesArgs {
     LayArgs<BF16> w, x;
-    uint32_t *w_sizes, *x_sizes;  // of kLayGroups groups: of the rows' largest finite values the largest, and 0x7f80 less the smallest that is not 0 (as bits of a bf16)
+    // of kLayGroups groups: of the rows' largest finite values the largest, and 0x7f80 less the smallest that is not 0 (as bits of a bf16)
+    uint32_t *w_sizes, *x_sizes;
     float product_most;
 };
 __device__ __forceinline__ uint32_t largest_of(const uint4 &v)
@@ -992,7 +995,10 @@ __global__ void __launch_bounds__(256) k_class_halves(HalvesArgs a, uint32_t w_g
             const uint32_t in[4] = {v.x, v.y, v.z, v.w};
             _Float16 h[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) h[2 * j] = (_Float16)(__uint_as_float(in[j] << 16) * scale), h[2 * j + 1] = (_Float16)(__uint_as_float(in[j] & 0xffff0000u) * scale);
+            for (int j = 0; j < 4; ++j) {
+                h[2 * j] = (_Float16)(__uint_as_float(in[j] << 16) * scale);
+                h[2 * j + 1] = (_Float16)(__uint_as_float(in[j] & 0xffff0000u) * scale);
+            }
             v = __builtin_bit_cast(uint4, h);
         }
         *reinterpret_cast<uint4 *>(m.to + row * m.padded + d) = v;
@@ -1052,7 +1058,8 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
     const ScoreArgs<T> &a = q.s;
     int64_t ct, rt;
     int fast;
-    if (!stage::tile_of(blockIdx.x, (uint32_t)(a.by_rows ? a.row_tiles : a.class_tiles), (uint32_t)(a.by_rows ? a.class_tiles : a.row_tiles), a.by_rows ? 1 : kClassGroup, a.by_rows ? rt : ct, fast)) return;
+    const uint32_t slow_tiles = a.by_rows ? (uint32_t)a.row_tiles : a.class_tiles, fast_tiles = a.by_rows ? a.class_tiles : (uint32_t)a.row_tiles;
+    if (!stage::tile_of(blockIdx.x, slow_tiles, fast_tiles, a.by_rows ? 1 : kClassGroup, a.by_rows ? rt : ct, fast)) return;
     (a.by_rows ? ct : rt) = fast;
     const int c0 = a.class0 + (int)ct * C::BA, last = a.classes - 1, l = threadIdx.x & 63;
     const int64_t r0 = rt * C::BB;
@@ -1155,7 +1162,8 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
 #pragma unroll
                     for (int u = 0; u < AHEAD; ++u) {
                         const bool there = (uint32_t)c[u] < (uint32_t)a.all_classes;
-                        if (k + u * EACH < mine && (there ? (uint32_t)(c[u] - c0) < (uint32_t)C::BA : ct == 0)) q.z_top[row * q.z_stride + k + u * EACH] = there ? z[at * WIDE + c[u] - c0] : 0.0f;
+                        const bool here = there ? (uint32_t)(c[u] - c0) < (uint32_t)C::BA : ct == 0;
+                        if (k + u * EACH < mine && here) q.z_top[row * q.z_stride + k + u * EACH] = there ? z[at * WIDE + c[u] - c0] : 0.0f;
                     }
                     ask(k + AHEAD * EACH);
                 }
@@ -1362,7 +1370,8 @@ __device__ __forceinline__ void StageProduct<T, OC>::make(const StagePieceArgs<T
     float sums[C::FA] = {};
     const int summers = a.col_tiles < kSummers ? a.col_tiles : kSummers, summer = 2 * ct + (C::b_off() > 0);
     const bool summing = OC && a.sum_slots && ct < summers;
-    stage::multiply<KIND, true, A, B, C>(lds, left, right, stage::Walk{a_block, (uint32_t)(A::STEP * a.b_bytes), kBlockValues * 2, a.b_plane, K, 0}, acc, [&](int s, int b_plane, const auto &f) {
+    const stage::Walk walk{a_block, (uint32_t)(A::STEP * a.b_bytes), kBlockValues * 2, a.b_plane, K, 0};
+    stage::multiply<KIND, true, A, B, C>(lds, left, right, walk, acc, [&](int s, int b_plane, const auto &f) {
         if (summing && b_plane == 0 && s / stage::Pairs<KIND>::COUNT % (2 * summers) == summer) {
 #pragma unroll
             for (int t = 0; t < C::FA; ++t) {
@@ -1463,10 +1472,14 @@ struct Scheme {
 Scheme scheme_of(const bgl_class_loss_t *l, bool large)
 {
     const bool f32 = l->dtype == BGL_F32;
-    if (large) return Scheme{true, StageCut::BA, ProductCut::BA, ((int64_t)1 << 27) + ((int64_t)1 << 23), StageCut::BA, StageCut::BB, f32 ? 6 : 4, f32 ? 3 : 1, ProductCut::BA, 2 * kCus, 512};
+    const int64_t values = ((int64_t)1 << 27) + ((int64_t)1 << 23);
+    if (large) return Scheme{true, StageCut::BA, ProductCut::BA, values, StageCut::BA, StageCut::BB, f32 ? 6 : 4, f32 ? 3 : 1, ProductCut::BA, 2 * kCus, 512};
     return Scheme{false, 128, 128, (int64_t)1 << 25, 8, 1, 4, 1, 1, kCus, 64};  // (pieces of 4 classes are stored, and 16 bytes of bf16 read)
 }
-bool large_call(const bgl_class_loss_t *l, int64_t n) { return n >= kLargeRows && l->classes >= kLargeClasses && (double)n * l->classes * l->in_dim >= kLargeProducts; }
+bool large_call(const bgl_class_loss_t *l, int64_t n)
+{
+    return n >= kLargeRows && l->classes >= kLargeClasses && (double)n * l->classes * l->in_dim >= kLargeProducts;
+}
 bool laid_out(const bgl_class_loss_t *l) { return l->dtype == BGL_BF16 && l->in_dim % kPad == 0; }
 
 // Ranges of the summed index that a product of rows x cols is made in, and the tiles' rows: small calls take tiles of 16 x 128 for up to 16 rows (in 128 x 128 the
@@ -1484,7 +1497,8 @@ int shares_for(const Scheme &s, int64_t rows, int64_t cols, int64_t summed, int 
     return (int)fit(tiles);
 }
 
-size_t slot_bytes(int64_t shares, int64_t rows, int64_t width) { return round_up((size_t)(shares * rows * width) * 4 + 16, 256); }  // (rows are read four values at a time)
+// (rows are read four values at a time)
+size_t slot_bytes(int64_t shares, int64_t rows, int64_t width) { return round_up((size_t)(shares * rows * width) * 4 + 16, 256); }
 int64_t per_share(int64_t summed, int shares) { return (int64_t)round_up((size_t)ceil_div(summed, shares), 64); }
 int shares_used(int64_t summed, int shares) { return (int)ceil_div(summed, per_share(summed, shares)); }  // (none is empty)
 
@@ -1555,7 +1569,9 @@ Plan plan_of(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
     p.slot_width = s.large ? (int)round_up(l->in_dim, ProductCut::BB) : l->in_dim;
     p.dx_shares = shares_for(s, p.piece_rows, l->in_dim, p.piece_classes, p.dx_tile);
     p.dx_shares = p.class_pieces > 1 && p.row_pieces > 1 ? 1 : shares_used(p.piece_classes, p.dx_shares);
-    p.dx_bytes = p.dx_shares > 1 || p.class_pieces > 1 || (s.large && l->in_dim % 4) ? slot_bytes(p.dx_shares, round_up(p.class_pieces > 1 ? n : p.piece_rows, s.slot_round), p.slot_width) : 0;
+    const bool dx_slots = p.dx_shares > 1 || p.class_pieces > 1 || (s.large && l->in_dim % 4);
+    const int64_t dx_rows = round_up(p.class_pieces > 1 ? n : p.piece_rows, s.slot_round);
+    p.dx_bytes = dx_slots ? slot_bytes(p.dx_shares, dx_rows, p.slot_width) : 0;
     const int last = l->classes - (p.class_pieces - 1) * p.piece_classes;
     for (const int classes : {p.piece_classes, last}) {
         const WeightPlan w = weight_plan(l, s, classes, p.piece_rows, p.row_pieces);
@@ -1577,13 +1593,18 @@ size_t backward_room(const bgl_class_loss_t *l, int64_t n, const Scheme &s)
     const auto most = [](int64_t a, int64_t b) { return a > b ? a : b; };
     const int64_t over = (many ? kPieceClasses * least(n, kPieceRows) : 128 * stride) + 128 * least(stride, s.values);
     const Plan p = plan_of(l, n, s);
-    size_t bytes = round_up((size_t)least(round_up(n, 128) * stride, s.values + over) * s.dz_value_bytes, 256) + round_up((size_t)n * 4, 256) + p.back_x_bytes + p.back_w_bytes;
+    const int64_t dz_values = least(round_up(n, 128) * stride, s.values + over);
+    size_t bytes = round_up((size_t)dz_values * s.dz_value_bytes, 256) + round_up((size_t)n * 4, 256) + p.back_x_bytes + p.back_w_bytes;
     // (ranges of the summed index leave s.fill tiles at most; a result of one range is rounded up to tiles)
     const int64_t width = s.large ? round_up(D, ProductCut::BB) : D, up = s.slot_round;
     const bool odd = s.large && D % 4;
-    if (V >= 2 * s.least || (many && n > 0) || odd) bytes += slot_bytes(1, most(many || odd ? round_up(n, up) : 0, least(shared, round_up(n, up) * (V / s.least))), width);
+    if (V >= 2 * s.least || (many && n > 0) || odd) {
+        const int64_t dx_shares = least(shared, round_up(n, up) * (V / s.least)), dx_pieces = many || odd ? round_up(n, up) : 0;
+        bytes += slot_bytes(1, most(dx_pieces, dx_shares), width);
+    }
     const int64_t shares = n >= 2 * s.least ? least(shared, round_up(V, up) * (n / s.least)) : 0;
-    const int64_t pieces = round_up(many ? (n > kPieceRows ? s.values / kPieceRows + kPieceClasses : 0) : n * stride > s.values ? V : 0, up), odd_pieces = odd ? round_up(V, up) : 0;
+    const int64_t of_many = n > kPieceRows ? s.values / kPieceRows + kPieceClasses : 0, of_few = n * stride > s.values ? V : 0;
+    const int64_t pieces = round_up(many ? of_many : of_few, up), odd_pieces = odd ? round_up(V, up) : 0;
     const int64_t sums = most(most(most(shares, pieces), odd_pieces), s.large ? least(V, s.values / 128) : 0) * summers_of(l, s);
     bytes += slot_bytes(1, most(most(shares, pieces), odd_pieces), width) + round_up((size_t)sums * 4, 256);
     return bytes > p.backward_bytes ? bytes : p.backward_bytes;
@@ -1645,7 +1666,8 @@ ScoreArgs<T> score_args(const Call &c)
     using E = typename T::elem;
     ScoreArgs<T> s{};
     s.x = (const E *)c.x, s.w = (const E *)c.weight, s.bias = (const E *)c.bias, s.labels = c.labels, s.x_stride = c.x_stride, s.n = c.n;
-    s.classes = s.all_classes = c.l->classes, s.D = c.l->in_dim, s.k = kLog2e, s.k_t = (float)(1.4426950408889634 / c.l->temperature), s.two = c.top_class && c.l->temperature != 1.0f;
+    s.classes = s.all_classes = c.l->classes, s.D = c.l->in_dim, s.k = kLog2e, s.k_t = (float)(1.4426950408889634 / c.l->temperature);
+    s.two = c.top_class && c.l->temperature != 1.0f;
     s.far = far_of(c.l), s.saved_width = saved_width_of(c.l);
     return s;
 }
@@ -1689,7 +1711,10 @@ StageScoreArgs<F32> stage_args(const Call &c, const Plan &p, const ScoreArgs<F32
     const auto lay = [&](LayArgs<F32> a, char *to) {
         a.to = (uint16_t *)to;
         const int64_t most = kMostThreads / 64;
-        for (int64_t row0 = 0; row0 < a.all_rows; row0 += most) k_class_split<<<dim3((unsigned)ceil_div(a.all_rows - row0 < most ? a.all_rows - row0 : most, 4)), dim3(256), 0, c.stream>>>(a, row0);
+        for (int64_t row0 = 0; row0 < a.all_rows; row0 += most) {
+            const int64_t rows = a.all_rows - row0 < most ? a.all_rows - row0 : most;
+            k_class_split<<<dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, c.stream>>>(a, row0);
+        }
         return to;
     };
     q.w = lay(lay_args<F32>(s.w, s.D, s.classes, s.classes, s.D, p.padded, nullptr), w);
@@ -1701,7 +1726,8 @@ StageScoreArgs<BF16> stage_args(const Call &c, const Plan &p, const ScoreArgs<BF
     StageScoreArgs<BF16> q{};
     q.s = s, q.plane = p.padded * 2;
     q.x_bytes = q.w_bytes = (int64_t)p.padded * 2;
-    LayArgs<BF16> lw = lay_args<BF16>(s.w, s.D, s.classes, s.classes, s.D, p.padded, nullptr), lx = lay_args<BF16>(s.x, s.x_stride, c.n, round_up(c.n, 32), s.D, p.padded, select);
+    const LayArgs<BF16> lw = lay_args<BF16>(s.w, s.D, s.classes, s.classes, s.D, p.padded, nullptr);
+    const LayArgs<BF16> lx = lay_args<BF16>(s.x, s.x_stride, c.n, round_up(c.n, 32), s.D, p.padded, select);
     if (select) {
         // shares of sizes, the exponent and the choice, the values
         HalvesArgs a{lw, lx, (uint32_t *)w, (uint32_t *)x, kProductMost * (c.l->temperature < 1.0f ? c.l->temperature : 1.0f)};
@@ -1791,7 +1817,8 @@ void launch_products(PieceArgs<T> *dw, PieceArgs<T> *dx, int tile, hipStream_t s
                 a->row_tiles = ceil_div(a->M, C::BA), a->col_tiles = (int)ceil_div(a->N, C::BB), a->tiles = (uint32_t)stage::tile_count(a->row_tiles, a->col_tiles);
                 groups[i] = a->tiles * a->shares;
             }
-        k_class_products<T, C, decltype(narrow)::value><<<dim3(groups[0] + groups[1]), dim3(kThreads), 0, st>>>(dw ? *dw : PieceArgs<T>{}, dx ? *dx : PieceArgs<T>{}, groups[0]);
+        const PieceArgs<T> none{};
+        k_class_products<T, C, decltype(narrow)::value><<<dim3(groups[0] + groups[1]), dim3(kThreads), 0, st>>>(dw ? *dw : none, dx ? *dx : none, groups[0]);
     };
     if ((dw ? dw : dx)->N < T::VEC) go(Small{}, std::true_type{});  // (one form of reading rows shorter than 16 bytes will do)
     else if (tile == Flat::BA) go(Flat{}, std::false_type{});
@@ -1807,14 +1834,18 @@ void launch_products(StagePieceArgs<T> *dw, StagePieceArgs<T> *dx, hipStream_t s
             a->row_tiles = ceil_div(a->M, ProductCut::BA), a->col_tiles = (int)ceil_div(a->N, ProductCut::BB);
             groups[i] = (uint32_t)(stage::tile_count(a->row_tiles, a->col_tiles) * a->shares);
         }
-    k_class_products_stage<T><<<dim3(groups[0] + groups[1]), dim3(stage::kThreads), 0, st>>>(dw ? *dw : StagePieceArgs<T>{}, dx ? *dx : StagePieceArgs<T>{}, groups[0]);
+    const StagePieceArgs<T> none{};
+    k_class_products_stage<T><<<dim3(groups[0] + groups[1]), dim3(stage::kThreads), 0, st>>>(dw ? *dw : none, dx ? *dx : none, groups[0]);
 }
 // Either may have nothing to do.
 template <class T>
 void launch_reduce(const ReduceArgs<T> &one, const ReduceArgs<T> &two, hipStream_t st)
 {
     const bool many = (one.out && one.shares > 8) || (one.sums && one.sum_shares > 8) || (two.out && two.shares > 8);
-    const auto groups = [&](const ReduceArgs<T> &a) { return (uint32_t)ceil_div((a.out ? a.rows * ceil_div(a.width, 4) : 0) + (a.sums ? a.rows : 0), many ? 32 : 256); };
+    const auto groups = [&](const ReduceArgs<T> &a) {
+        const int64_t items = (a.out ? a.rows * ceil_div(a.width, 4) : 0) + (a.sums ? a.rows : 0);
+        return (uint32_t)ceil_div(items, many ? 32 : 256);
+    };
     const uint32_t all = groups(one) + groups(two), most = kMostThreads / 256;
     for (uint32_t group0 = 0; group0 < all; group0 += most) {
         const uint32_t count = all - group0 < most ? all - group0 : most;
@@ -1884,7 +1915,8 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
             }
             if (r.teacher_scale != 0.0f) {
                 // (20,000 rows of 8 classes, f32: backward 191 us with wavefronts, 175 with 8 lanes; a few rows leave the GPU to wavefronts)
-                if (rows < 4 * kCus || r.top > 32) k_class_fix<T, 64><<<dim3((unsigned)ceil_div(rows, 4), (unsigned)ceil_div(r.top, 64)), dim3(256), 0, c.stream>>>(r);
+                const dim3 wavefronts((unsigned)ceil_div(rows, 4), (unsigned)ceil_div(r.top, 64));
+                if (rows < 4 * kCus || r.top > 32) k_class_fix<T, 64><<<wavefronts, dim3(256), 0, c.stream>>>(r);
                 else if (r.top <= 8) k_class_fix<T, 8><<<dim3((unsigned)ceil_div(rows, 32)), dim3(256), 0, c.stream>>>(r);
                 else k_class_fix<T, 16><<<dim3((unsigned)ceil_div(rows, 16)), dim3(256), 0, c.stream>>>(r);
             }
@@ -1906,7 +1938,10 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
                 x.b = q.w + class0 * q.w_bytes, x.b_bytes = q.w_bytes, x.exponent = w_up;
                 y.b = q.x + row0 * q.x_bytes, y.b_bytes = q.x_bytes, y.exponent = x_up;
                 y.K = round_up(rows, 32);  // (rows of zeros in both)
-                for (StagePieceArgs<T> *a : {&x, &y}) a->a = (const char *)dz, a->a_rows = (int)round_up(rows, StageCut::BB), a->a_stride = (int)p.dz_stride, a->b_width = p.padded, a->b_plane = q.plane, a->slot_width = p.slot_width, a->undo = undo;
+                for (StagePieceArgs<T> *a : {&x, &y}) {
+                    a->a = (const char *)dz, a->a_rows = (int)round_up(rows, StageCut::BB), a->a_stride = (int)p.dz_stride;
+                    a->b_width = p.padded, a->b_plane = q.plane, a->slot_width = p.slot_width, a->undo = undo;
+                }
                 launch_products<T>(dweight ? &y : nullptr, dx ? &x : nullptr, c.stream);
             } else {
                 PieceArgs<T> x{}, y{};
@@ -1922,14 +1957,18 @@ int backward(const Call &c, const float *saved, float scale, float teacher_scale
                 }
             }
             // (where one piece has all classes; the last piece of rows leaves it to the launch that finishes dW too)
-            x_sums = slots && dx && p.class_pieces == 1 ? ReduceArgs<T>{slots, nullptr, slot_rows, rows, p.slot_width, D, dx_shares, 0, dx + row0 * dx_stride, nullptr, dx_stride, w_up, undo} : ReduceArgs<T>{};
+            x_sums = {};
+            if (slots && dx && p.class_pieces == 1)
+                x_sums = {slots, nullptr, slot_rows, rows, p.slot_width, D, dx_shares, 0, dx + row0 * dx_stride, nullptr, dx_stride, w_up, undo};
             if (x_sums.out && rp + 1 < p.row_pieces) launch_reduce<T>(x_sums, {}, c.stream);
         }
         // (small calls without slots have written both already, large ones dweight)
         E *dw_out = dweight && w.slots ? dweight + (int64_t)class0 * D : nullptr, *db_out = dbias && (w.slots || h.large) ? dbias + class0 : nullptr;
         ReduceArgs<T> w_sums{};
-        if (dw_out || db_out) w_sums = {dw_slots, db_slots, (int64_t)round_up(classes, h.slot_round), classes, p.slot_width, D, w.shares, w.shares * summers_of(c.l, h), dw_out, db_out, D, x_up, undo};
-        if (p.dx_bytes && dx && cp > 0 && cp + 1 == p.class_pieces) x_sums = {dx_slots, nullptr, (int64_t)round_up(c.n, h.slot_round), c.n, p.slot_width, D, p.dx_shares, 0, dx, nullptr, dx_stride, w_up, undo};
+        const int64_t dw_rows = round_up(classes, h.slot_round), dx_rows = round_up(c.n, h.slot_round);
+        if (dw_out || db_out) w_sums = {dw_slots, db_slots, dw_rows, classes, p.slot_width, D, w.shares, w.shares * summers_of(c.l, h), dw_out, db_out, D, x_up, undo};
+        if (p.dx_bytes && dx && cp > 0 && cp + 1 == p.class_pieces)
+            x_sums = {dx_slots, nullptr, dx_rows, c.n, p.slot_width, D, p.dx_shares, 0, dx, nullptr, dx_stride, w_up, undo};
         launch_reduce<T>(w_sums, x_sums, c.stream);
     }
     BGL_HIP(hipGetLastError());
@@ -1967,7 +2006,8 @@ int check_call(const Call &c)
     const int es = c.l->dtype == BGL_F32 ? 4 : 2;
     BGL_TRY(check_rows("x", c.x, c.x_stride, c.l->in_dim, es, c.n > 0));
     if ((c.n > 0 && !c.weight) || !aligned(c.weight, es) || !aligned(c.bias, es)) BGL_FAIL(BGL_EINVAL, "weight is null, or weight or bias is misaligned");
-    if (!aligned(c.labels, 4) || !aligned(c.top_class, 4) || !aligned(c.top_score, 4)) BGL_FAIL(BGL_EINVAL, "labels or the teacher's classes or scores are misaligned");
+    if (!aligned(c.labels, 4) || !aligned(c.top_class, 4) || !aligned(c.top_score, 4))
+        BGL_FAIL(BGL_EINVAL, "labels or the teacher's classes or scores are misaligned");
     if (!c.top_class != !c.top_score) BGL_FAIL(BGL_EINVAL, "the teacher's classes and scores come together");
     if (c.top_class && c.l->top == 0) BGL_FAIL(BGL_EINVAL, "the loss has no teacher (top is 0)");
     if (c.n > 0 && !c.labels && !c.top_class) BGL_FAIL(BGL_EINVAL, "neither labels nor a teacher");
