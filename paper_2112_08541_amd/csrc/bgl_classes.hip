@@ -431,7 +431,7 @@ __device__ __forceinline__ bool teacher_of(const RowArgs<T> &a, int64_t row, flo
     return true;
 }
 
-// Many parts of many rows: added up by 16 lanes for each of 16 rows (whose parts are neighbours), into the first part's place.  4,096 rows of 684 parts: 8 us.
+// Many parts of many rows: added up by 16 lanes for each of 16 rows (whose parts are neighbours), into the first part's place.  4,096 rows of 684 parts: 11 us.
 constexpr int kMergeRows = 16, kMergeLanes = 16;
 template <class T>
 __global__ void __launch_bounds__(kMergeRows *kMergeLanes) k_class_merge(RowArgs<T> a, float2 *part, float *part_t)
@@ -899,7 +899,8 @@ __global__ void __launch_bounds__(256) k_class_lay(LayArgs<BF16> a)
 // in [2^14, 2^15) and a bf16's eight bits fit a half's from 2^-32 of it on; below, a value is off by 2^-39 of it at most.  That is as good as exact where no row (of x: with a
 // gradient) is far smaller than another, and no score's products: where the rows' largest values are within 12 powers of two, and where what scores can be off by,
 // 2^-38 D max|x| max|w| over the temperature, is below 2^-23.  Else (`whole`) x and W stay bf16 and dz is two of them, twice the products: of one row 2^32 above the others
-// these lost everything (4,096 x 512 x 65,536 training: 1,305 us, so 1,951).  First the largest and smallest of kLayGroups groups of rows of each, then every workgroup finds exponent and choice from them.
+// these lost everything (4,096 x 512 x 65,536 training: 1,305 us, so 1,951).  First the largest and smallest of kLayGroups groups of rows of each, then every workgroup finds
+// exponent and choice from them.  65,536 and 4,096 rows of 512: 16 and 22 us.
 constexpr int kLayGroups = 1024, kHalvesHead = 2 * kLayGroups * 4 + 256;
 constexpr int kRowsApart = 12;             // powers of two
 constexpr float kProductMost = 0x1p15f;    // D max|x| max|w|, at a temperature of 1
@@ -1029,9 +1030,9 @@ __global__ void __launch_bounds__(256) k_class_split(LayArgs<F32> a, int64_t row
 }
 
 // k_class_scores from laid out operands: 192 classes x 128 rows, the largest tile of which two workgroups fit a CU: one's exponentials beside the other's products (a training
-// call of 4,096 x 512 x 65,536 bf16 took 1,278 us with 128 x 128, 1,227 so).  4,096 x 512 x 65,536 bf16: 306 us, 900 TFLOP/s with the exponentials (a plain library product of
-// 4,096 x 512 x 16,384 makes 831); backward 175 us for half of the classes, 785 TFLOP/s and 268 MB of dz.  1,024 x 256 x 50,001 f32: 179 us, 880 TFLOP/s of its six
-// products of bf16; backward 233, with 307 MB of dz.  (From two halves of a value scaled by its row's largest, three products, these took 103 and 162: 22 bits, and what was
+// call of 4,096 x 512 x 65,536 bf16 took 1,278 us with 128 x 128, 1,227 so).  4,096 x 512 x 65,536 bf16: 334 us, 820 TFLOP/s with the exponentials (a plain library product
+// of 4,096 x 512 x 16,384 makes 831); backward 193 us for half of the classes, 710 TFLOP/s and 268 MB of dz.  1,024 x 256 x 50,001 f32: 177 us, 890 TFLOP/s of its six
+// products of bf16; backward 229, with 307 MB of dz.  (From two halves of a value scaled by its row's largest, three products, these took 103 and 162: 22 bits, and what was
 // far below the row's largest lost all of them, so that a large column with small weights beside it made other columns' products wrong.)
 template <class T>
 struct StageScoreArgs {
@@ -1281,7 +1282,7 @@ __global__ void __launch_bounds__(stage::kThreads, 2) k_class_scores_stage(Stage
 }
 
 // k_class_products from laid out operands: 256 x 128 (eight wavefronts with 256 x 256, one workgroup a CU, were slower).  OC: dW, else dx.  Both products of 4,096 rows, 512 columns and
-// 32,768 classes, bf16: 284 us, 970 TFLOP/s; of 1,024, 256 and 50,001, f32: 355 us, 890 TFLOP/s of six bf16 products for one.
+// 32,768 classes, bf16: 300 us, 920 TFLOP/s; of 1,024, 256 and 50,001, f32: 398 us, 790 TFLOP/s of six bf16 products for one.
 template <class T>
 struct StagePieceArgs {
     const char *a, *b;                 // dz, in blocks; W or x

@@ -170,8 +170,8 @@ __device__ __forceinline__ void moments(const Piece<T, TEAM, kValues, FIT> &p, f
 }
 
 // A row's threads: 16 values each, a team of 1 to 1,024.  A workgroup has 256 threads or one team.  What fits the team
-// better asks less often whether a value is there: of 302,709 x 512 bf16 with 29 vector instructions for a value these, not the memory, took the time, 146 us; 105 now
-// (5.9 TB/s), 428,377 x 256 f32 146 (6.0 TB/s; the caches keep some of what the call before left).
+// better asks less often whether a value is there: 302,709 x 512 bf16 with 29 vector instructions for a value took 40 % longer, bound by these and not by the memory; now
+// 101 us (6.1 TB/s), 428,377 x 256 f32 140 (6.3 TB/s).
 template <class T, int TEAM, Fit FIT>
 __global__ void __launch_bounds__(norm_threads<TEAM>()) k_norm_forward(NormArgs<T> a)
 {
@@ -201,7 +201,7 @@ __global__ void __launch_bounds__(norm_threads<TEAM>()) k_norm_forward(NormArgs<
 
 // SUMS: the weight's gradients are asked for; a thread then keeps those of its 16 columns over the rows of its team, the workgroup adds up its teams' and
 // leaves a row of partial sums.  The widest rows are then 512 threads of 32 values: 1,024 of 16 have 128 registers each, which these sums exceed.
-// 428,377 x 256 f32 158 us, 302,709 x 512 bf16 120 (8.3 and 7.7 TB/s, some of it from the caches).
+// Behind the forward call of the same rows 428,377 x 256 f32 253 us, 302,709 x 512 bf16 186 (5.2 and 5.0 TB/s); of rows that the caches have in part 158 and 120.
 template <class T, int TEAM, bool SUMS, Fit FIT, int VALUES = kValues>
 __global__ void __launch_bounds__(norm_threads<TEAM>()) k_norm_backward(NormArgs<T> a)
 {
