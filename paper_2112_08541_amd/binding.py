@@ -594,12 +594,16 @@ def _weights(name: str, t: Optional[torch.Tensor], shape, dtype):
     return _dev_ptr(t, dtype)
 
 
-# Of objects that belong to one device: their memory, the current device and the tensors have to be of it, as a launch on another one's memory could fault.
+# Of objects that belong to one device: their memory, the current device, the stream and the tensors have to be of it, as a launch on another one's memory could fault.
 def _stream_on(device: int, stream) -> int:
     now = torch._C._cuda_getDevice()
     if now != device:
         raise ValueError(f"made on device {device}, called with device {now} the current one")
-    return torch._C._cuda_getCurrentRawStream(now) if stream is None else int(stream.cuda_stream)
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(now)
+    if stream.device_index != device:
+        raise ValueError(f"made on device {device}, called with a stream of device {stream.device_index}")
+    return int(stream.cuda_stream)
 
 
 def _matrix_on(device: int, name: str, t: Optional[torch.Tensor], n: int, width: int, dtype):

@@ -93,3 +93,18 @@ def test_places_behind_the_row(torch, B):
         rnd, (w, b, dy) = others(torch, "f32", 4, width, seed=width)
         x = torch.tensor([3e38, -2e37, 4e33, 1.0], device="cuda")[:, None].expand(4, width).contiguous()
         check_rows(torch, B, "f32", x, w, b, dy, 1e-12)
+
+
+def test_a_stream_of_another_device_is_refused(torch, B):
+    """As far as one device can show it; nothing is launched."""
+    class Other:
+        device_index, cuda_stream = torch.cuda.current_device() + 1, 0
+    x, w, labels = torch.zeros((4, 8), device="cuda"), torch.zeros((5, 8), device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    pairs, norm, loss = torch.zeros((4, 2), device="cuda"), B.LayerNorm(4, 8), B.ClassLoss(4, 8, 5)
+    for call in (lambda: norm.forward(x, x, stream=Other), lambda: norm.backward(x, x, pairs, dx=x, stream=Other),
+                 lambda: loss.forward(x, w, labels=labels, stream=Other), lambda: loss.backward(x, w, pairs, labels=labels, dx=x, stream=Other)):
+        with pytest.raises(ValueError, match="stream of device"):
+            call()
+    side = torch.cuda.Stream()
+    norm.forward(x, x, stream=side)
+    torch.cuda.synchronize()
